@@ -402,6 +402,152 @@ rolesub_status rolesub_full_values(const rolesub_dims* dims, rolesub_dtype dtype
                                    const uint32_t* mask, const int32_t* offsets, const void* Vp, int64_t cap_groups,
                                    void* Vh, void* workspace, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged routed cache: keys and kept value groups of growing sequences, for
+ * decoding token by token over the routed values (Sec. 3, 3.2).
+ * The cache is n_pages pages of `page` tokens. A page holds, for each of H
+ * key/value heads, its tokens' keys and, one token after another, their kept
+ * groups of z = R^T v in ascending group order:
+ *   K    [n_pages,H,page,dh]  (call dtype)
+ *   V    [n_pages,H,vcap,ds]  (call dtype), ds = dh/G
+ *   mask [n_pages,page] uint32: bit s set = group s kept (bits >= G ignored)
+ *   slot [n_pages,page] int32: where the token's groups start in V; they take
+ *        slots slot .. slot + popcount - 1. Slots outside [0, vcap) are never
+ *        written and read as zero (vcap = page * max K_i holds every budget).
+ * A sequence b is a row of page numbers table[b][0..max_pages-1] and a length
+ * lens[b]: its token t sits in row t % page of page table[b][t / page]. Several
+ * sequences may share pages that no call writes. Page numbers outside
+ * [0, n_pages) hold no tokens: they are not written, and attention does not
+ * see them. Entries past the length are not used. Lengths below 0 count as 0,
+ * lengths above max_pages*page as that.
+ *   page: 16, 32, 64, 128 or 256; dh: 64 or 128; 1 <= G <= 32 dividing dh.
+ * K, k, z, q and their outputs lie on 16-byte boundaries, V on 16 or, for
+ * smaller groups, on the group's size. Token strides, counted in elements
+ * (0: dense), are multiples of 16 bytes; a sample's tokens follow one another
+ * at that stride and samples at T times it, e.g. views of a fused projection.
+ * Unlike the other calls' samples, a sequence or a head may lie beyond 2 GiB of
+ * its tensor; one page's keys or values stay below 2 GiB.
+ * ------------------------------------------------------------------------ */
+typedef struct rolesub_pages {
+  int32_t n_pages, page, vcap;
+  int32_t H, dh, G;
+  void *K, *V;
+  uint32_t* mask;
+  int32_t* slot;
+} rolesub_pages;
+
+/* ---------------------------------------------------------------------------
+ * rolesub_rotary: queries and keys turned by their positions (the queries and
+ * keys of Sec. 3 as inputs of the attention calls), with up to 8 position axes,
+ * e.g. time, row and column of a visual token:
+ *   a_i = positions[b,t,axis[i]] * inv_freq[i]        i = 0 .. n_pairs-1
+ *   y_i = x_i cos a_i - x_j sin a_i,   y_j = x_i sin a_i + x_j cos a_i
+ * on the pairs (i, j) = (i, n_pairs + i) of every head, or (2i, 2i+1) when
+ * interleaved is non-zero; dims past 2 n_pairs are copied. inverse non-zero
+ * turns by -a (undoes the call; also its gradient).
+ *   q [B,T,H,dh], k [B,T,Hkv,dh] (dtype) with token strides q_stride and
+ *   k_stride; either may be NULL (its head count is then not used).
+ *   positions [B,T,n_axes] int32; inv_freq [n_pairs] f32; axis [n_pairs] uint8
+ *   or NULL (all axis 0); a pair whose axis is >= n_axes is not turned.
+ *   q_out, k_out: dense, or the input itself (same pointer, then the same
+ *   stride is used); otherwise they overlap no input.
+ * Angles are formed and reduced in 64 bits: exact for every int32 position.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int32_t dh, rolesub_dtype dtype,
+                              const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              const int32_t* positions, int32_t n_axes, const float* inv_freq,
+                              const uint8_t* axis, int32_t n_pairs, int32_t interleaved, int32_t inverse,
+                              void* q_out, void* k_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_cache_append: the next tokens of every sequence into its pages
+ * (the pack of Sec. 3.2, a page at a time): token j of sequence b becomes its
+ * token lens[b] + j.
+ *   k, z [B,T,H,dh] (dtype; z = R^T v as rolesub_rotate_values writes, or v
+ *   itself for a cache read with R = NULL), token strides k_stride, z_stride;
+ *   mask [B,T] uint32 as rolesub_route writes; lens [B] int32: cached tokens
+ *   before the call; n_new [B] int32 or NULL: tokens of each sequence, the
+ *   first n_new[b] of its T (clamped to [0, T]; NULL: T).
+ * Tokens past the end of the table, or in pages outside [0, n_pages), are
+ * dropped. No two sequences may write one page. lens is not changed.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_cache_append(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
+                                    const void* k, int64_t k_stride, const void* z, int64_t z_stride,
+                                    const uint32_t* mask, const int32_t* table, int32_t max_pages,
+                                    const int32_t* lens, const int32_t* n_new, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_attend_paged: attention of new tokens over the paged cache.
+ *   s[j,h,t] = scale * <q[b,j,h], K_t of head h / (Hq/H)>
+ *   P        = softmax over the t < min(lens[b], max_len, visible[b,j])
+ *   u        = sum_t P (M_t z_t),   out[b,j,h] = R_{h/(Hq/H)} u  (R NULL: u)
+ *   q [B,Tq,Hq,dh] (dtype), token stride q_stride, Hq a multiple of H;
+ *   R [H,dh,dh] or NULL; scale: 0 means 1/sqrt(dh);
+ *   visible [B,Tq] int32 or NULL: tokens each query sees (NULL: all);
+ *   max_len: no token past it is seen (0: max_pages*page). It sizes the launch
+ *   and the workspace, so a bound near the longest sequence is fastest.
+ *   out [B,Tq,Hq,dh] dense in out_dtype (f32 or the call's dtype).
+ * A query that sees no token, or whose tokens all score -inf, gives zeros. What
+ * a query does not see does not reach it, infinities and NaN included.
+ * Accumulated attention weight of every cached token (mass_out non-NULL):
+ *   mass_out[b,t] = decay * mass_in[b,t] + sum over j, h of P[j,h,t]
+ *   for t < min(lens[b], max_len); later entries are not written.
+ *   mass_in [B,mass_ld] f32 or NULL (zeros; also with decay = 0), mass_out the
+ *   same; they may be the same array. mass_ld >= max_len, 0 <= decay finite.
+ * workspace: at least rolesub_attend_paged_workspace_size() bytes (which does
+ * not fall as B, Tq or max_len grows; max_len is not 0 there), 16-byte
+ * aligned; nothing in it needs clearing; calls (and graphs) that may overlap
+ * must not share one. Results do not depend on the other sequences of a call
+ * of the same B, Tq and max_len.
+ * ------------------------------------------------------------------------ */
+size_t rolesub_attend_paged_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq,
+                                           int32_t max_len, int32_t with_mass);
+rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                    const void* q, int64_t q_stride, const int32_t* table, int32_t max_pages,
+                                    const int32_t* lens, const int32_t* visible, int32_t max_len, const void* R,
+                                    float scale, void* out, rolesub_dtype out_dtype, const float* mass_in, float decay,
+                                    float* mass_out, int64_t mass_ld, void* workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_evict_tokens: which tokens stay when a cache goes back to `keep`
+ * tokens a sequence: the first `first`, the latest `recent`, and of the others
+ * those with the most accumulated attention weight (a larger value first, equal
+ * ones, -0 equal to +0, by lower index, NaN after every number).
+ *   mass [B,mass_ld] f32; lens [B] int32, clamped to [0, max_len];
+ *   keep >= 1, first, recent >= 0, first + recent <= keep; max_len <= mass_ld
+ *   keep_idx [B,keep] int32: the kept indices, ascending, then -1
+ *   n_keep   [B] int32: how many, min(lens[b], keep)
+ *   workspace: at least rolesub_evict_workspace_size() bytes, 16-byte aligned;
+ *   nothing in it needs clearing; calls (and graphs) that may overlap must not
+ *   share one.
+ * ------------------------------------------------------------------------ */
+size_t rolesub_evict_workspace_size(int32_t B, int32_t max_len);
+rolesub_status rolesub_evict_tokens(int32_t B, int32_t max_len, const float* mass, int64_t mass_ld,
+                                    const int32_t* lens, int32_t keep, int32_t first, int32_t recent,
+                                    int32_t* keep_idx, int32_t* n_keep, void* workspace, size_t ws_bytes,
+                                    void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_cache_compact: the kept tokens of every sequence, in order, into
+ * other pages: token j of the new sequence is token keep_idx[b,j] of the old
+ * one (key, mask, groups), for j < n_keep[b] (clamped to [0, keep]).
+ *   src and dst: caches of the same H, dh, G, page and dtype; they may be the
+ *   same arrays, but no page that is written may be read by the same call, or
+ *   written for two sequences.
+ *   table [B,max_pages] and dst_table [B,dst_max_pages] int32; an index or a
+ *   source page out of range gives a key of zeros that keeps no group; tokens
+ *   past the end of dst_table, or in pages outside dst, are dropped.
+ *   mass_in [B,mass_ld], mass_out [B,mass_out_ld] f32, or both NULL:
+ *   mass_out[b,j] = mass_in[b,keep_idx[b,j]] (0 for an index outside
+ *   [0, mass_ld)); later entries are not written. The arrays do not overlap;
+ *   mass_out_ld >= keep.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pages* dst, rolesub_dtype dtype, int32_t B,
+                                     const int32_t* table, int32_t max_pages, const int32_t* keep_idx,
+                                     const int32_t* n_keep, int32_t keep, const int32_t* dst_table,
+                                     int32_t dst_max_pages, const float* mass_in, int64_t mass_ld, float* mass_out,
+                                     int64_t mass_out_ld, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

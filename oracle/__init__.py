@@ -6,3 +6,4 @@ its Python binding) never imports, calls or links anything here, and this
 package imports nothing from the product.
 """
 from .rolesub_oracle import *  # noqa: F401,F403
+from . import paged_oracle as paged  # noqa: F401

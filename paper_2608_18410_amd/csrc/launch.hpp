@@ -250,4 +250,84 @@ struct GatherParams {
 };
 hipError_t launch_gather_rows(const GatherParams& p, hipStream_t s);
 
+// Paged routed cache (rolesub_pages).
+struct PagedCache {
+  int n_pages, page, shift, vcap, H, dh, G, ds;  // page = 1 << shift
+  void *K, *V;
+  uint32_t* mask;
+  int32_t* slot;
+};
+
+struct RotaryParams {
+  int B, T, H, Hkv, dh, n_axes, n_pairs, interleaved, inverse;  // a head count of 0: that tensor is absent
+  const void *q, *k;
+  int64_t q_stride, k_stride, qo_stride, ko_stride;  // elements from token to token
+  const int32_t* positions;  // [B*T][n_axes]
+  const float* inv_freq;     // [n_pairs]
+  const uint8_t* axis;       // [n_pairs] or null
+  void *q_out, *k_out;
+};
+hipError_t launch_rotary(const RotaryParams& p, bool bf16, hipStream_t s);
+
+struct AppendParams {
+  PagedCache c;
+  int B, T, max_pages;
+  const void *k, *z;
+  int64_t k_stride, z_stride;
+  const uint32_t* mask;
+  const int32_t *table, *lens, *n_new;
+};
+hipError_t launch_append(const AppendParams& p, bool bf16, hipStream_t s);
+
+struct CompactParams {
+  PagedCache src, dst;
+  int B, keep, max_pages, dst_max_pages;
+  const int32_t *table, *keep_idx, *n_keep, *dst_table;
+  const float* mass_in;
+  float* mass_out;
+  int64_t mass_ld, mass_out_ld;
+};
+hipError_t launch_compact(const CompactParams& p, bool bf16, hipStream_t s);
+
+struct DecodeParams {
+  PagedCache c;
+  int B, Hq, rep, Tq, R, max_pages, max_len;  // rep = Hq / H, R = rep * Tq query rows of a key head
+  const void* q;
+  int64_t q_stride;
+  const int32_t *table, *lens, *visible;
+  const void* Rm;  // [H][dh][dh] or null
+  float scale;     // of the scores, in units of log2
+  void* out;
+  int out_f32;
+  const float* mass_in;
+  float decay;
+  float* mass_out;
+  int64_t mass_ld;
+  // workspace
+  int n_split, chunk;  // tokens of a split
+  float* part;         // [B][H][R][n_split][dh] sums of P z, unnormalised
+  float* stat;         // [B][H][R][n_split][2]  maximum (log2), sum of P
+  float* x;            // [B][H][R][x_ld] scores in units of log2 (with mass)
+  float* lse;          // [B][H][R] log2 of the sum of exponentials (with mass)
+  int x_ld;
+};
+struct DecodePlan {
+  int n_split, chunk, x_ld;
+  size_t off_stat, off_x, off_lse, bytes;  // of this call
+  size_t ask;  // at least bytes of every call of no more sequences, queries and tokens
+};
+DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass);
+hipError_t launch_decode(const DecodeParams& p, bool bf16, hipStream_t s);
+
+struct EvictParams {
+  int B, max_len, keep, first, recent;
+  const float* mass;  // [B][mass_ld]
+  int64_t mass_ld;
+  const int32_t* lens;
+  int32_t *keep_idx, *n_keep;  // [B][keep], [B]
+  void* ws;
+};
+size_t evict_ws_bytes(int B, int max_len);
+hipError_t launch_evict(const EvictParams& p, hipStream_t s);
+
 }  // namespace rolesub

@@ -857,3 +857,303 @@ rolesub_status rolesub_gather_tokens(int32_t B, int32_t N, int32_t K, int64_t ro
 }
 
 }  // extern "C"
+
+namespace {
+
+constexpr size_t kMaxThreads = static_cast<size_t>(1) << 32;  // of one launch
+
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Checks a paged cache (its arrays too when need) and fills c.
+rolesub_status check_pages(const char* fn, const char* name, const rolesub_pages* pg, rolesub_dtype dtype, bool need,
+                           PagedCache& c) {
+  if (!pg) return fail(ROLESUB_ERR_INVALID_ARG, "%s: %s is NULL", fn, name);
+  if (!valid_dtype(dtype)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+  const rolesub_dims d = {0, 0, pg->H, pg->dh, pg->G, 0};
+  rolesub_status st = check_value_dims(&d, fn);
+  if (st) return st;
+  st = check_groups(&d, fn, true);
+  if (st) return st;
+  if (pg->page < 16 || pg->page > 256 || (pg->page & (pg->page - 1)))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: %s: pages of %d tokens (16, 32, 64, 128 or 256)", fn, name, pg->page);
+  if (pg->n_pages < 0 || pg->vcap < 0)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: %s: n_pages and vcap must be >= 0", fn, name);
+  c = PagedCache{pg->n_pages, pg->page, __builtin_ctz(pg->page), pg->vcap, pg->H, pg->dh, pg->G, pg->dh / pg->G,
+                 pg->K, pg->V, pg->mask, pg->slot};
+  const size_t e = esize(dtype), gb = c.ds * e;
+  if (static_cast<size_t>(c.H) * c.page * c.dh * e >= kMaxRegion || static_cast<size_t>(c.H) * c.vcap * gb >= kMaxRegion)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: %s: one page's keys or values exceed 2 GiB", fn, name);
+  if (!need) return ROLESUB_OK;
+  if (c.n_pages > 0 && (!c.K || !c.mask || !c.slot || (c.vcap > 0 && !c.V)))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: %s: K, V, mask and slot must be non-NULL", fn, name);
+  if (!aligned(c.K, 16) || !aligned(c.V, std::min<size_t>(gb, 16)))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: %s: K must lie on 16 bytes, V on 16 or its group's size", fn, name);
+  return ROLESUB_OK;
+}
+
+// A [.., T, H, dh] operand's token stride (0: dense): rows of whole 16-byte pieces.
+rolesub_status check_rows(const char* fn, const char* name, const void* p, int64_t& stride, int H, int dh, size_t e) {
+  const int64_t dense = static_cast<int64_t>(H) * dh;
+  if (stride == 0) stride = dense;
+  if (stride < dense) return fail(ROLESUB_ERR_INVALID_ARG, "%s: %s: token stride %lld below H*dh", fn, name,
+                                  static_cast<long long>(stride));
+  if (!p) return fail(ROLESUB_ERR_INVALID_ARG, "%s: %s is NULL", fn, name);
+  if (!aligned(p, 16) || stride * e % 16)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: %s must lie on 16 bytes, its token stride be a multiple of 16 bytes", fn,
+                name);
+  return ROLESUB_OK;
+}
+
+size_t extent(size_t tokens, int64_t stride, int64_t row, size_t e) {
+  return tokens ? ((tokens - 1) * stride + row) * e : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+rolesub_status rolesub_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int32_t dh, rolesub_dtype dtype,
+                              const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              const int32_t* positions, int32_t n_axes, const float* inv_freq,
+                              const uint8_t* axis, int32_t n_pairs, int32_t interleaved, int32_t inverse,
+                              void* q_out, void* k_out, void* stream) {
+  const char* fn = "rolesub_rotary";
+  if (!valid_dtype(dtype)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+  if (B < 0 || T < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: B and T must be >= 0", fn);
+  if (dh != 64 && dh != 128) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: head dim %d not supported (64 or 128)", fn, dh);
+  if (n_pairs < 1 || n_pairs > dh / 2)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: n_pairs=%d outside 1..dh/2", fn, n_pairs);
+  if (n_axes < 1 || n_axes > 8) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: n_axes=%d outside 1..8", fn, n_axes);
+  const size_t n = static_cast<size_t>(B) * T, e = esize(dtype);
+  if (n == 0) return ROLESUB_OK;
+  if (!q && !k) return fail(ROLESUB_ERR_INVALID_ARG, "%s: q and k are both NULL", fn);
+  if ((q && H < 1) || (k && Hkv < 1)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: head counts must be >= 1", fn);
+  RotaryParams p = {};
+  p.B = B;
+  p.T = T;
+  p.H = q ? H : 0;
+  p.Hkv = k ? Hkv : 0;
+  p.dh = dh;
+  p.n_axes = n_axes;
+  p.n_pairs = n_pairs;
+  p.interleaved = interleaved != 0;
+  p.inverse = inverse != 0;
+  p.q = q;
+  p.k = k;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.positions = positions;
+  p.inv_freq = inv_freq;
+  p.axis = axis;
+  p.q_out = q_out;
+  p.k_out = k_out;
+  if (!positions || !inv_freq || (q && !q_out) || (k && !k_out))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  if (n * 256 >= kMaxThreads || p.H + static_cast<int64_t>(p.Hkv) > 65535)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many tokens or heads", fn);
+  rolesub_status st;
+  if (q && (st = check_rows(fn, "q", q, p.q_stride, H, dh, e))) return st;
+  if (k && (st = check_rows(fn, "k", k, p.k_stride, Hkv, dh, e))) return st;
+  if (!aligned(q_out, 16) || !aligned(k_out, 16))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: q_out and k_out must lie on 16 bytes", fn);
+  const int64_t qr = static_cast<int64_t>(H) * dh, kr = static_cast<int64_t>(Hkv) * dh;
+  p.qo_stride = q_out == q ? p.q_stride : qr;
+  p.ko_stride = k_out == k ? p.k_stride : kr;
+  const size_t nq = q ? extent(n, p.q_stride, qr, e) : 0, nk = k ? extent(n, p.k_stride, kr, e) : 0;
+  const size_t oq = q ? extent(n, p.qo_stride, qr, e) : 0, ok = k ? extent(n, p.ko_stride, kr, e) : 0;
+  const bool qi = q && q_out == q, ki = k && k_out == k;
+  if ((q && !qi && (ranges_overlap(q_out, oq, q, nq) || (k && ranges_overlap(q_out, oq, k, nk)))) ||
+      (k && !ki && (ranges_overlap(k_out, ok, k, nk) || (q && ranges_overlap(k_out, ok, q, nq)))) ||
+      (q && k && !(qi && ki) && ranges_overlap(q_out, oq, k_out, ok)))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: an output overlaps another tensor of the call", fn);
+  return from_hip(launch_rotary(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+rolesub_status rolesub_cache_append(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
+                                    const void* k, int64_t k_stride, const void* z, int64_t z_stride,
+                                    const uint32_t* mask, const int32_t* table, int32_t max_pages,
+                                    const int32_t* lens, const int32_t* n_new, void* stream) {
+  const char* fn = "rolesub_cache_append";
+  AppendParams p = {};
+  const bool work = B > 0 && T > 0 && max_pages > 0;
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, work, p.c);
+  if (st) return st;
+  if (B < 0 || T < 0 || max_pages < 0)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: B, T and max_pages must be >= 0", fn);
+  if (!work || p.c.n_pages == 0) return ROLESUB_OK;
+  if (!mask || !table || !lens) return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  p.B = B;
+  p.T = T;
+  p.max_pages = max_pages;
+  p.k = k;
+  p.z = z;
+  p.k_stride = k_stride;
+  p.z_stride = z_stride;
+  p.mask = mask;
+  p.table = table;
+  p.lens = lens;
+  p.n_new = n_new;
+  if ((st = check_rows(fn, "k", k, p.k_stride, p.c.H, p.c.dh, esize(dtype)))) return st;
+  if ((st = check_rows(fn, "z", z, p.z_stride, p.c.H, p.c.dh, esize(dtype)))) return st;
+  if (static_cast<size_t>(B) * T > 0x7FFFFFFF ||
+      static_cast<size_t>(B) * (T / p.c.page + 2) * 256 >= kMaxThreads || p.c.H > 65535)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many tokens or heads", fn);
+  return from_hip(launch_append(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+size_t rolesub_attend_paged_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq,
+                                           int32_t max_len, int32_t with_mass) {
+  if (!pages || B <= 0 || pages->H < 1 || Hq < pages->H || Tq <= 0 || max_len <= 0) return 0;
+  if (static_cast<size_t>(Hq / pages->H) * Tq > 0x7FFFFFFF) return 0;
+  return decode_plan(B, pages->H, Hq / pages->H * Tq, pages->dh, max_len, with_mass != 0).ask;
+}
+
+rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                    const void* q, int64_t q_stride, const int32_t* table, int32_t max_pages,
+                                    const int32_t* lens, const int32_t* visible, int32_t max_len, const void* R,
+                                    float scale, void* out, rolesub_dtype out_dtype, const float* mass_in, float decay,
+                                    float* mass_out, int64_t mass_ld, void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "rolesub_attend_paged";
+  DecodeParams p = {};
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, B > 0 && Tq > 0, p.c);
+  if (st) return st;
+  if (out_dtype != ROLESUB_F32 && out_dtype != dtype)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: out_dtype must be f32 or the input dtype", fn);
+  if (B < 0 || Tq < 0 || max_pages < 0 || max_len < 0)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: B, Tq, max_pages and max_len must be >= 0", fn);
+  if (Hq < 1 || Hq % p.c.H)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: %d query heads are not a multiple of %d key heads", fn, Hq, p.c.H);
+  if (!std::isfinite(scale)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: scale is not finite", fn);
+  if (!(decay >= 0.f) || !std::isfinite(decay))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: decay must be finite and >= 0", fn);
+  if (mass_in && !mass_out) return fail(ROLESUB_ERR_INVALID_ARG, "%s: mass_in without mass_out", fn);
+  if (B == 0 || Tq == 0) return ROLESUB_OK;
+  const int64_t whole = static_cast<int64_t>(max_pages) * p.c.page;
+  const int64_t ml = max_len == 0 ? whole : std::min<int64_t>(max_len, whole);
+  if (ml > (1 << 30)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: more than 2^30 tokens (pass max_len)", fn);
+  if (!q || !lens || !out || (ml > 0 && !table))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  if (mass_out && mass_ld < ml)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: mass_ld=%lld below max_len=%lld", fn, static_cast<long long>(mass_ld),
+                static_cast<long long>(ml));
+  if (mass_out && mass_in != mass_out && mass_in) {
+    const size_t n = static_cast<size_t>(B) * mass_ld * 4;
+    if (ranges_overlap(mass_in, n, mass_out, n))
+      return fail(ROLESUB_ERR_INVALID_ARG, "%s: mass_in and mass_out overlap without being one array", fn);
+  }
+  p.B = B;
+  p.Hq = Hq;
+  p.rep = Hq / p.c.H;
+  p.Tq = Tq;
+  if (static_cast<size_t>(p.rep) * Tq > 0x7FFFFFFF || static_cast<size_t>(B) * Hq * Tq * p.c.dh >= kMaxThreads)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many queries", fn);
+  p.R = p.rep * Tq;
+  p.q = q;
+  p.q_stride = q_stride;
+  if ((st = check_rows(fn, "q", q, p.q_stride, Hq, p.c.dh, esize(dtype)))) return st;
+  if (!aligned(R, 16)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: R must lie on 16 bytes", fn);
+  p.max_pages = max_pages;
+  p.max_len = static_cast<int>(ml);
+  p.table = table;
+  p.lens = lens;
+  p.visible = visible;
+  p.Rm = R;
+  p.scale = (scale == 0.f ? 1.f / std::sqrt(static_cast<float>(p.c.dh)) : scale) * 1.44269504088896341f;
+  p.out = out;
+  p.out_f32 = out_dtype == ROLESUB_F32;
+  p.mass_in = decay == 0.f ? nullptr : mass_in;
+  p.decay = decay;
+  p.mass_out = mass_out;
+  p.mass_ld = mass_ld;
+  const DecodePlan d = decode_plan(B, p.c.H, p.R, p.c.dh, p.max_len, mass_out != nullptr);
+  if (d.bytes > 0 && (!workspace || ws_bytes < d.bytes))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, %zu given", fn, d.bytes,
+                workspace ? ws_bytes : static_cast<size_t>(0));
+  if (!aligned(workspace, 16)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace must lie on 16 bytes", fn);
+  if (static_cast<size_t>(B) * p.c.H * d.n_split * ((p.R + 15) / 16) * 256 >= kMaxThreads ||
+      static_cast<size_t>(B) * (p.max_len / 256 + 1) * 256 >= kMaxThreads)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads or queries", fn);
+  char* ws = static_cast<char*>(workspace);
+  p.n_split = d.n_split;
+  p.chunk = d.chunk;
+  p.x_ld = d.x_ld;
+  p.part = reinterpret_cast<float*>(ws);
+  p.stat = reinterpret_cast<float*>(ws + d.off_stat);
+  if (mass_out) {
+    p.x = reinterpret_cast<float*>(ws + d.off_x);
+    p.lse = reinterpret_cast<float*>(ws + d.off_lse);
+  }
+  return from_hip(launch_decode(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+size_t rolesub_evict_workspace_size(int32_t B, int32_t max_len) {
+  return B <= 0 || max_len <= 0 ? 0 : evict_ws_bytes(B, max_len);
+}
+
+rolesub_status rolesub_evict_tokens(int32_t B, int32_t max_len, const float* mass, int64_t mass_ld,
+                                    const int32_t* lens, int32_t keep, int32_t first, int32_t recent,
+                                    int32_t* keep_idx, int32_t* n_keep, void* workspace, size_t ws_bytes,
+                                    void* stream) {
+  const char* fn = "rolesub_evict_tokens";
+  if (B < 0 || max_len < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: B and max_len must be >= 0", fn);
+  if (keep < 1 || first < 0 || recent < 0 || static_cast<int64_t>(first) + recent > keep)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: need keep >= 1, first, recent >= 0 and first + recent <= keep (%d, %d, %d)",
+                fn, keep, first, recent);
+  if (mass_ld < max_len)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: mass_ld=%lld below max_len=%d", fn, static_cast<long long>(mass_ld), max_len);
+  if (max_len > (1 << 30) || keep > (1 << 30) || static_cast<size_t>(B) * 1024 >= kMaxThreads)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences or tokens", fn);
+  if (B == 0) return ROLESUB_OK;
+  if ((max_len > 0 && !mass) || !lens || !keep_idx || !n_keep)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  const size_t need = rolesub_evict_workspace_size(B, max_len);
+  if (need > 0 && (!workspace || ws_bytes < need))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                workspace ? ws_bytes : static_cast<size_t>(0));
+  if (!aligned(workspace, 16)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace must lie on 16 bytes", fn);
+  EvictParams p = {B, max_len, keep, first, recent, mass, mass_ld, lens, keep_idx, n_keep, workspace};
+  return from_hip(launch_evict(p, static_cast<hipStream_t>(stream)), fn);
+}
+
+rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pages* dst, rolesub_dtype dtype, int32_t B,
+                                     const int32_t* table, int32_t max_pages, const int32_t* keep_idx,
+                                     const int32_t* n_keep, int32_t keep, const int32_t* dst_table,
+                                     int32_t dst_max_pages, const float* mass_in, int64_t mass_ld, float* mass_out,
+                                     int64_t mass_out_ld, void* stream) {
+  const char* fn = "rolesub_cache_compact";
+  CompactParams p = {};
+  const bool work = B > 0 && keep > 0;
+  rolesub_status st = check_pages(fn, "src", src, dtype, work, p.src);
+  if (st) return st;
+  if ((st = check_pages(fn, "dst", dst, dtype, work, p.dst))) return st;
+  if (B < 0 || keep < 0 || max_pages < 0 || dst_max_pages < 0)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: B, keep, max_pages and dst_max_pages must be >= 0", fn);
+  if (p.src.H != p.dst.H || p.src.dh != p.dst.dh || p.src.G != p.dst.G || p.src.page != p.dst.page)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: src and dst differ in H, dh, G or page", fn);
+  if (!mass_in != !mass_out) return fail(ROLESUB_ERR_INVALID_ARG, "%s: mass_in and mass_out go together", fn);
+  if (mass_out && (mass_ld < 0 || mass_out_ld < keep))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: need mass_ld >= 0 and mass_out_ld >= keep", fn);
+  if (!work) return ROLESUB_OK;
+  if (!keep_idx || !n_keep || (max_pages > 0 && !table) || (dst_max_pages > 0 && !dst_table))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  if (mass_out && ranges_overlap(mass_in, static_cast<size_t>(B) * mass_ld * 4, mass_out,
+                                 static_cast<size_t>(B) * mass_out_ld * 4))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: mass_in and mass_out overlap", fn);
+  if (keep > (1 << 30) || static_cast<size_t>(B) * (keep / p.src.page + 1) * 256 >= kMaxThreads || p.src.H > 65535)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, tokens or heads", fn);
+  p.B = B;
+  p.keep = keep;
+  p.max_pages = max_pages;
+  p.dst_max_pages = dst_max_pages;
+  p.table = table;
+  p.keep_idx = keep_idx;
+  p.n_keep = n_keep;
+  p.dst_table = dst_table;
+  p.mass_in = mass_in;
+  p.mass_out = mass_out;
+  p.mass_ld = mass_ld;
+  p.mass_out_ld = mass_out_ld;
+  return from_hip(launch_compact(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+}  // extern "C"

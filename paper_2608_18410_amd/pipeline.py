@@ -4,9 +4,12 @@ Orchestration only: buffers are allocated once per shape and reused, and the
 four library calls are issued in order on one stream. A batch may also be
 split into micro-batches (contiguous ranges of prefixes, each with views of
 the buffers and its own route workspace) whose calls run on separate streams.
+For decoding token by token, decode_layer grows a paged cache by the new tokens
+and attends from them, and evict_layer takes it back to a budget.
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass
 
 import torch
@@ -134,3 +137,44 @@ def run_full_layer(q, k, v, mask, Rt, R, S: int, bufs: FullWidthBuffers, budget=
     rs.full_values(R, mask, bufs.offsets, bufs.Vp, S, H, workspace=bufs.workspace, out=bufs.Vh, stream=stream)
     rs.attend_values(q, k, bufs.Vh, out=bufs.out, stream=stream)
     return bufs
+
+
+def page_count(tokens: int, page: int) -> int:
+    """Pages that hold `tokens` tokens."""
+    return -(-int(tokens) // page)
+
+
+def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.PagedCache, table, lens, new_lens,
+                 positions=None, inv_freq=None, axis=None, router: rs.Router | None = None, scores_in=None,
+                 visible=None, max_len: int = 0, mass=None, decay: float = 1.0, workspace=None, out=None,
+                 stream=None):
+    """The next T tokens of every sequence through one layer: route -> rotary ->
+    rotate -> append -> attend. h [B,T,d], q [B,T,Hq,dh], k and v [B,T,H,dh]; lens are
+    the cached tokens before them, new_lens = lens + T after (one pair of tensors
+    serves every layer of a stack). Without positions the keys and queries are taken
+    as they are. visible defaults to all cached and new tokens; for T > 1 causal
+    tokens pass visible[b, j] = lens[b] + j + 1. With mass the tokens' weight is
+    accumulated for evict_layer. Returns the attention output [B,T,Hq,dh]."""
+    mask = rs.route(types, budget, G, h=h, router=router, scores_in=scores_in, want_scores=False, want_idx=False,
+                    want_count=False, stream=stream)["mask"]
+    if positions is not None:
+        q, k = rs.rotary(q, k, positions, inv_freq, axis, stream=stream)
+    z = rs.rotate_values(v, R, stream=stream)
+    rs.cache_append(cache, k, z, mask, table, lens, stream=stream)
+    return rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
+                           workspace=workspace, out=out, stream=stream)
+
+
+def evict_layer(cache: rs.PagedCache, table, lens, mass, keep: int, first: int, recent: int, dst: rs.PagedCache,
+                dst_table, max_len: int = 0, mass_out=None, stream=None):
+    """A layer's cache back to `keep` tokens a sequence: the tokens with the most
+    accumulated weight, moved to the pages dst_table of dst (the caller's allocator
+    then has the old ones back). Returns (the new lengths [B], their weights as wide
+    as mass with zeros for the tokens to come, the kept indices [B,keep])."""
+    idx, n = rs.evict_tokens(mass, lens, keep, first, recent, max_len=max_len, stream=stream)
+    if mass_out is None:
+        mass_out = torch.empty_like(mass) if mass.shape[1] >= keep else mass.new_empty((mass.shape[0], keep))
+    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+        mass_out.zero_()
+    rs.cache_compact(cache, table, idx, n, dst, dst_table, mass=mass, mass_out=mass_out, stream=stream)
+    return n, mass_out, idx

@@ -28,6 +28,8 @@ EXPORTS = (
     "rolesub_allocate_groups", "rolesub_route_allocate_workspace_size", "rolesub_route_allocate",
     "rolesub_full_workspace_size", "rolesub_full_transpose", "rolesub_full_rotate_pack", "rolesub_full_values",
     "rolesub_attend_values", "rolesub_route_noalloc",
+    "rolesub_rotary", "rolesub_cache_append", "rolesub_attend_paged_workspace_size", "rolesub_attend_paged",
+    "rolesub_evict_workspace_size", "rolesub_evict_tokens", "rolesub_cache_compact",
 )
 ROUTE_NOALLOC_MAX_BYTES = 8 << 20
 
@@ -52,6 +54,11 @@ class RouterDesc(ctypes.Structure):
                 ("Hr", ctypes.c_int32), ("alpha_role", ctypes.c_float), ("alpha_lang", ctypes.c_float)] + \
                [(n, ctypes.c_void_p) for n in ("W_r", "b_r", "E", "W1", "b1", "W2", "b2",
                                                "W_tok", "b_tok", "W_role", "W_lang", "b_lang")]
+
+
+class PagesDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page", "vcap", "H", "dh", "G")] + \
+               [(n, ctypes.c_void_p) for n in ("K", "V", "mask", "slot")]
 
 
 _lib = None
@@ -97,6 +104,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.rolesub_full_rotate_pack.argtypes = [P, ctypes.c_int, P, P, P, P, P, I64, P, P, P, SZ, P]
     lib.rolesub_full_values.argtypes = [P, ctypes.c_int, P, P, P, P, I64, P, P, SZ, P]
     lib.rolesub_attend_values.argtypes = [P, ctypes.c_int, I32, P, P, P, ctypes.c_float, P, ctypes.c_int, P]
+    F, C = ctypes.c_float, ctypes.c_int
+    lib.rolesub_rotary.argtypes = [I32, I32, I32, I32, I32, C, P, I64, P, I64, P, I32, P, P, I32, I32, I32, P, P, P]
+    lib.rolesub_cache_append.argtypes = [P, C, I32, I32, P, I64, P, I64, P, P, I32, P, P, P]
+    lib.rolesub_attend_paged_workspace_size.argtypes = [P, I32, I32, I32, I32, I32]
+    lib.rolesub_attend_paged_workspace_size.restype = SZ
+    lib.rolesub_attend_paged.argtypes = [P, C, I32, I32, I32, P, I64, P, I32, P, P, I32, P, F, P, C, P, F, P, I64, P, SZ, P]
+    lib.rolesub_evict_workspace_size.argtypes = [I32, I32]
+    lib.rolesub_evict_workspace_size.restype = SZ
+    lib.rolesub_evict_tokens.argtypes = [I32, I32, P, I64, P, I32, I32, I32, P, P, P, SZ, P]
+    lib.rolesub_cache_compact.argtypes = [P, P, C, I32, P, I32, P, P, I32, P, I32, P, I64, P, I64, P]
     for fn in ("rolesub_rotate_values", "rolesub_route", "rolesub_route_noalloc", "rolesub_pack_kv",
                "rolesub_rotate_pack", "rolesub_attend"):
         getattr(lib, fn).restype = ctypes.c_int
@@ -664,3 +681,253 @@ def attend_values(q, k, V, scale: float = 0.0, out_dtype=None, out=None, stream=
         ctypes.byref(dims), _code(q), Tq, _ptr(q), _ptr(k, q.dtype), _ptr(V, q.dtype), ctypes.c_float(scale),
         _ptr(o), _code(o), _stream(stream)))
     return o
+
+
+# ----------------------------------------------------------------------------
+# Paged routed cache: positions, append, attention of new tokens, eviction
+# ----------------------------------------------------------------------------
+
+def _here(stream, *ts):
+    """The stream handle of a call on these tensors, which all lie on the current
+    device (the library launches there)."""
+    _same_device(*ts)
+    for t in ts:
+        if isinstance(t, _Tensor):
+            if t.is_cuda:
+                cur = torch.cuda.current_device() if _raw_device is None else _raw_device()
+                if t.device.index != cur:
+                    raise ValueError(f"tensors on {t.device}, but the current device is cuda:{cur}")
+                if stream is not None and stream.device.index != cur:
+                    raise ValueError(f"tensors on {t.device}, but the stream is on {stream.device}")
+            break
+    return _stream(stream) if torch.cuda.is_available() else None
+
+
+def _tokens(name, t):
+    """Address and token stride of a [B, T, H, dh] operand whose tokens lie at one
+    stride (dense, or a view of a fused projection)."""
+    if not t.is_cuda:
+        raise ValueError("librolesub takes device tensors only")
+    B, T, H, dh = t.shape
+    if t.is_contiguous():
+        return t.data_ptr(), H * dh
+    sb, st, sh, sd = t.stride()
+    if T == 1:
+        st = sb if B > 1 else H * dh
+    if (sd != 1 and dh > 1) or (sh != dh and H > 1) or (B > 1 and sb != T * st):
+        raise ValueError(f"{name}: heads and dims must be dense and tokens at one stride, got strides {list(t.stride())}")
+    return t.data_ptr(), st
+
+
+@dataclass
+class PagedCache:
+    """Pages of a growing routed cache (kept alive while calls are in flight):
+    K [n_pages,H,page,dh], V [n_pages,H,vcap,dh/G], mask and slot [n_pages,page]
+    int32. A sequence is a row of page numbers and a length, kept by the caller."""
+    K: torch.Tensor
+    V: torch.Tensor
+    mask: torch.Tensor
+    slot: torch.Tensor
+
+    @staticmethod
+    def allocate(n_pages, page, H, dh, G, vcap, dtype, device="cuda") -> "PagedCache":
+        """vcap: group slots of a page and head; page times the most groups a
+        token keeps holds every page."""
+        return PagedCache(K=torch.empty((n_pages, H, page, dh), dtype=dtype, device=device),
+                          V=torch.empty((n_pages, H, vcap, dh // G), dtype=dtype, device=device),
+                          mask=torch.empty((n_pages, page), dtype=torch.int32, device=device),
+                          slot=torch.empty((n_pages, page), dtype=torch.int32, device=device))
+
+    @property
+    def G(self) -> int:
+        return self.K.shape[3] // max(self.V.shape[3], 1)
+
+    def check(self, name="cache") -> None:
+        _need(f"{name}.K", self.K, (None, None, None, None), (torch.float32, torch.bfloat16))
+        n, H, page, dh = self.K.shape
+        _need(f"{name}.V", self.V, (n, H, None, None), self.K.dtype)
+        ds = self.V.shape[3]
+        if ds < 1 or dh % ds:
+            raise ValueError(f"{name}: groups of {ds} dims do not divide heads of {dh}")
+        _need(f"{name}.mask", self.mask, (n, page), _MASK)
+        _need(f"{name}.slot", self.slot, (n, page), torch.int32)
+
+    def desc(self) -> PagesDesc:
+        n, H, page, dh = self.K.shape
+        return PagesDesc(n, page, self.V.shape[2], H, dh, self.G, _ptr(self.K), _ptr(self.V), _ptr(self.mask),
+                         _ptr(self.slot))
+
+    def tensors(self):
+        return self.K, self.V, self.mask, self.slot
+
+
+def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=False, out=None, stream=None):
+    """q [B,T,H,dh] and k [B,T,Hkv,dh] (either may be None) turned by their
+    positions ([B,T], or [B,T,axes] with axis [pairs] uint8 naming each pair's).
+    out: (q_out, k_out); an input itself turns it in place. Returns (q_out, k_out)."""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q and k are both None")
+    _need("q" if q is not None else "k", some, (None, None, None, None), (torch.float32, torch.bfloat16))
+    B, T, _, dh = some.shape
+    dt = some.dtype
+    A = 1
+    if isinstance(positions, _Tensor) and positions.dim() == 3:
+        A = positions.shape[2]
+        _need("positions", positions, (B, T, None), torch.int32)
+    else:
+        _need("positions", positions, (B, T), torch.int32)
+    _need("inv_freq", inv_freq, (None,), torch.float32)
+    n = inv_freq.shape[0]
+    _need("axis", axis, (n,), torch.uint8)
+    qo, ko = (None, None) if out is None else out
+    for name, x, o in (("q", q, qo), ("k", k, ko)):
+        _need(name, x, (B, T, None, dh), dt)
+        if x is not None:
+            _need(f"{name}_out", o, tuple(x.shape), dt)
+    args = []
+    for name, x, o in (("q", q, qo), ("k", k, ko)):
+        if x is None:
+            args += [None, 0, None, 0]
+            continue
+        p, st = _tokens(name, x)
+        if o is None:
+            o = torch.empty((B, T, x.shape[2], dh), dtype=dt, device=x.device)
+            po = o.data_ptr()
+        else:
+            po, so = _tokens(f"{name}_out", o)
+            if so != (st if po == p else x.shape[2] * dh):
+                raise ValueError(f"{name}_out: must be {name} itself or contiguous")
+        args += [p, st, po, x.shape[2]]
+        qo, ko = (o, ko) if name == "q" else (qo, o)
+    s = _here(stream, some, q, k, positions, inv_freq, axis, qo, ko)
+    _check("rolesub_rotary", load().rolesub_rotary(
+        B, T, args[3], args[7], dh, _code(some), args[0], args[1], args[4], args[5], _ptr(positions), A,
+        _ptr(inv_freq), _ptr(axis), n, 1 if interleaved else 0, 1 if inverse else 0, args[2], args[6], s))
+    return (qo if q is not None else None), (ko if k is not None else None)
+
+
+def cache_append(cache: PagedCache, k, z, mask, table, lens, n_new=None, stream=None) -> PagedCache:
+    """Token j of sequence b (j < n_new[b], or all) becomes token lens[b] + j of its
+    pages: k and z [B,T,H,dh], mask [B,T]; table [B,max_pages], lens [B] int32."""
+    cache.check()
+    H, dh = cache.K.shape[1], cache.K.shape[3]
+    _need("k", k, (None, None, H, dh), cache.K.dtype)
+    B, T = k.shape[:2]
+    _need("z", z, (B, T, H, dh), cache.K.dtype)
+    _need("mask", mask, (B, T), _MASK)
+    _need("table", table, (B, None), torch.int32)
+    _need("lens", lens, (B,), torch.int32)
+    _need("n_new", n_new, (B,), torch.int32)
+    pk, sk = _tokens("k", k)
+    pz, sz = _tokens("z", z)
+    s = _here(stream, k, z, mask, table, lens, n_new, *cache.tensors())
+    desc = cache.desc()
+    _check("rolesub_cache_append", load().rolesub_cache_append(
+        ctypes.byref(desc), _code(k), B, T, pk, sk, pz, sz, _ptr(mask), _ptr(table), table.shape[1], _ptr(lens),
+        _ptr(n_new), s))
+    return cache
+
+
+def attend_paged_workspace_size(cache: PagedCache, B, Hq, Tq, max_len, mass=False) -> int:
+    n, H, page, dh = cache.K.shape
+    desc = PagesDesc(n, page, cache.V.shape[2], H, dh, cache.G, None, None, None, None)
+    return load().rolesub_attend_paged_workspace_size(ctypes.byref(desc), B, Hq, Tq, max_len, 1 if mass else 0)
+
+
+def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, visible=None, max_len: int = 0,
+                 mass=None, decay: float = 1.0, mass_out=None, workspace=None, out_dtype=None, out=None, stream=None):
+    """Attention of new tokens q [B,Tq,Hq,dh] over the cached ones; returns
+    [B,Tq,Hq,dh]. visible [B,Tq] int32: the tokens each query sees. mass [B,>=max_len]
+    f32: the tokens' accumulated weight, in place or into mass_out (which alone
+    starts from zero): decay * mass + the weight of this call's queries."""
+    cache.check()
+    n_pages, H, page, dh = cache.K.shape
+    _need("q", q, (None, None, None, dh), cache.K.dtype)
+    B, Tq, Hq, _ = q.shape
+    _need("table", table, (B, None), torch.int32)
+    _need("lens", lens, (B,), torch.int32)
+    _need("R", R, (H, dh, dh), q.dtype)
+    _need("visible", visible, (B, Tq), torch.int32)
+    _need("mass", mass, (B, None), torch.float32)
+    _need("out", out, (B, Tq, Hq, dh), (torch.float32, torch.bfloat16))
+    _need_workspace(workspace)
+    ld = 0
+    if mass_out is None:
+        mass_out = mass
+    if mass_out is not None:
+        _need("mass_out", mass_out, (B, None if mass is None else mass.shape[1]), torch.float32)
+        ld = mass_out.shape[1]
+    pq, sq = _tokens("q", q)
+    o = torch.empty((B, Tq, Hq, dh), dtype=out_dtype or q.dtype, device=q.device) if out is None else out
+    whole = table.shape[1] * page
+    ml = min(int(max_len), whole) if max_len else whole
+    if workspace is None:
+        need = attend_paged_workspace_size(cache, B, Hq, Tq, ml, mass_out is not None)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    s = _here(stream, q, table, lens, R, visible, mass, mass_out, workspace, o, *cache.tensors())
+    desc = cache.desc()
+    _check("rolesub_attend_paged", load().rolesub_attend_paged(
+        ctypes.byref(desc), _code(q), B, Hq, Tq, pq, sq, _ptr(table), table.shape[1], _ptr(lens), _ptr(visible),
+        int(max_len), _ptr(R), float(scale), _ptr(o), _code(o), _ptr(mass), float(decay), _ptr(mass_out), ld,
+        _ptr(workspace), workspace.numel(), s))
+    return o
+
+
+def evict_workspace_size(B, max_len) -> int:
+    return load().rolesub_evict_workspace_size(B, max_len)
+
+
+def evict_tokens(mass, lens, keep: int, first: int = 0, recent: int = 0, max_len: int = 0, workspace=None, out=None,
+                 stream=None):
+    """Which `keep` tokens of every sequence stay: the first, the recent, and of the
+    others those with the most mass [B,>=max_len]. Returns (keep_idx [B,keep] int32,
+    ascending, then -1; n_keep [B] int32). max_len 0: mass.shape[1]."""
+    _need("mass", mass, (None, None), torch.float32)
+    B, ld = mass.shape
+    _need("lens", lens, (B,), torch.int32)
+    _need_workspace(workspace)
+    if out is None:
+        if keep < 1:
+            raise ValueError(f"keep: expected at least 1, got {keep}")
+        out = (torch.empty((B, keep), dtype=torch.int32, device=mass.device),
+               torch.empty((B,), dtype=torch.int32, device=mass.device))
+    idx, n = out
+    _need("keep_idx", idx, (B, keep), torch.int32)
+    _need("n_keep", n, (B,), torch.int32)
+    ml = int(max_len) if max_len else ld
+    if workspace is None:
+        workspace = torch.empty(max(evict_workspace_size(B, ml), 1), dtype=torch.uint8, device=mass.device)
+    s = _here(stream, mass, lens, idx, n, workspace)
+    _check("rolesub_evict_tokens", load().rolesub_evict_tokens(
+        B, ml, _ptr(mass), ld, _ptr(lens), int(keep), int(first), int(recent), _ptr(idx), _ptr(n), _ptr(workspace),
+        workspace.numel(), s))
+    return idx, n
+
+
+def cache_compact(src: PagedCache, table, keep_idx, n_keep, dst: PagedCache, dst_table, mass=None, mass_out=None,
+                  stream=None):
+    """Token j < n_keep[b] of the pages dst_table[b] of dst becomes token
+    keep_idx[b, j] of the pages table[b] of src; mass_out[b, j] = mass[b, keep_idx[b, j]]
+    (a new [B, keep] tensor when mass comes alone). Returns mass_out (or None)."""
+    src.check("src")
+    dst.check("dst")
+    _need("keep_idx", keep_idx, (None, None), torch.int32)
+    B, keep = keep_idx.shape
+    _need("n_keep", n_keep, (B,), torch.int32)
+    _need("table", table, (B, None), torch.int32)
+    _need("dst_table", dst_table, (B, None), torch.int32)
+    _need("mass", mass, (B, None), torch.float32)
+    _need("mass_out", mass_out, (B, None), torch.float32)
+    _need("dst.K", dst.K, (None, None, None, None), src.K.dtype)
+    if mass is None and mass_out is not None:
+        raise ValueError("mass_out without mass")
+    if mass is not None and mass_out is None:
+        mass_out = torch.empty((B, keep), dtype=torch.float32, device=mass.device)
+    s = _here(stream, keep_idx, n_keep, table, dst_table, mass, mass_out, *src.tensors(), *dst.tensors())
+    a, b = src.desc(), dst.desc()
+    _check("rolesub_cache_compact", load().rolesub_cache_compact(
+        ctypes.byref(a), ctypes.byref(b), _code(src.K), B, _ptr(table), table.shape[1], _ptr(keep_idx), _ptr(n_keep),
+        keep, _ptr(dst_table), dst_table.shape[1], _ptr(mass), 0 if mass is None else mass.shape[1], _ptr(mass_out),
+        0 if mass_out is None else mass_out.shape[1], s))
+    return mass_out
