@@ -228,6 +228,14 @@ __device__ __forceinline__ float gelu_exact(float x) {
   return 0.5f * x * (x >= 0.f ? 2.f - ec : ec);
 }
 
+// What one lane of a wave writes to LDS is read by others of the same wave: the
+// LDS serves a wave in order, so only the compiler has to keep the order.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Workgroup-to-XCD placement: consecutive workgroup ids go round-robin to the
 // 8 XCDs. Given a linear id over `n` items that are naturally grouped by a
 // "key" (heads) of size nkey, return an item order that keeps every key on a

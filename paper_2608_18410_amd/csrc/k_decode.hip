@@ -16,14 +16,6 @@ namespace {
 
 __device__ __forceinline__ uint32_t group_bits(int G) { return G >= 32 ? 0xFFFFFFFFu : (1u << G) - 1u; }
 
-// What one lane of a wave writes to LDS is read by others of the same wave: the
-// LDS serves a wave in order, so only the compiler has to keep the order.
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // Four bf16 rows of 16 columns, transposed: 16 lanes give the addresses of the
 // rows' 8-byte quarters, lane i gets column i of the four rows.
 __device__ __forceinline__ bf16x4 lds_read_tr(const char* p) {
