@@ -517,8 +517,8 @@ rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dt
  *   keep >= 1, first, recent >= 0, first + recent <= keep; max_len <= mass_ld
  *   keep_idx [B,keep] int32: the kept indices, ascending, then -1
  *   n_keep   [B] int32: how many, min(lens[b], keep)
- *   workspace: at least rolesub_evict_workspace_size() bytes, 16-byte aligned;
- *   nothing in it needs clearing; calls (and graphs) that may overlap must not
+ *   workspace: at least rolesub_evict_workspace_size() bytes (which does not
+ *   fall as B or max_len grows), 16-byte aligned; nothing in it needs clearing; calls (and graphs) that may overlap must not
  *   share one.
  * ------------------------------------------------------------------------ */
 size_t rolesub_evict_workspace_size(int32_t B, int32_t max_len);

@@ -126,10 +126,11 @@ def evict(mass, lens, keep, first=0, recent=0):
         stay = list(range(ln))
         if ln > keep:
             safe = [t for t in stay if t < first or t >= ln - recent]
-            rest = [t for t in stay if first <= t < ln - recent]
+            rest = np.arange(first, ln - recent)
             # a larger value first, NaN last, then the lower index
-            rest.sort(key=lambda t: (np.isnan(mass[b, t]), -mass[b, t] if not np.isnan(mass[b, t]) else 0.0, t))
-            stay = sorted(safe + rest[: keep - len(safe)])
+            m = mass[b, first:ln - recent]
+            rest = rest[np.lexsort((rest, np.where(np.isnan(m), 0.0, -m), np.isnan(m)))]
+            stay = sorted(safe + rest[: keep - len(safe)].tolist())
         n[b] = len(stay)
         idx[b, : len(stay)] = stay
     return idx, n

@@ -1101,7 +1101,7 @@ rolesub_status rolesub_evict_tokens(int32_t B, int32_t max_len, const float* mas
                 fn, keep, first, recent);
   if (mass_ld < max_len)
     return fail(ROLESUB_ERR_INVALID_ARG, "%s: mass_ld=%lld below max_len=%d", fn, static_cast<long long>(mass_ld), max_len);
-  if (max_len > (1 << 30) || keep > (1 << 30) || static_cast<size_t>(B) * 1024 >= kMaxThreads)
+  if (max_len > (1 << 30) || keep > (1 << 30) || static_cast<size_t>(B) * 64 * 512 >= kMaxThreads)
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences or tokens", fn);
   if (B == 0) return ROLESUB_OK;
   if ((max_len > 0 && !mass) || !lens || !keep_idx || !n_keep)

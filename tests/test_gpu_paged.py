@@ -461,13 +461,16 @@ def _weights(rng, B, L, kind):
 
 @pytest.mark.parametrize("kind", ["random", "ties", "equal", "odd", "near"])
 @pytest.mark.parametrize("L,keep,first,recent", [(1, 1, 0, 0), (40, 7, 2, 3), (300, 300, 0, 0), (1025, 1, 0, 0), (1025, 1, 1, 0),
-                                                 (2048, 777, 49, 128), (5000, 4999, 0, 4999), (9000, 40, 40, 0), (70001, 5003, 5, 11)])
+                                                 (2048, 777, 49, 128), (5000, 4999, 0, 4999), (9000, 40, 40, 0), (70001, 5003, 5, 11),
+                                                 (1024, 500, 1, 1), (4096, 100, 0, 7), (4097, 4000, 3, 9), (16384, 1, 0, 0),
+                                                 (16385, 8000, 0, 8000), (24577, 9, 9, 0), (540000, 70000, 8192, 10000)])
 def test_evict(kind, L, keep, first, recent):
     rng = np.random.default_rng(L + keep)
     w = _weights(rng, 5, L, kind)
     lens = [L, max(0, L - 3), min(keep, L), min(keep + 1, L), 0]
     ref = O.evict(w, lens, keep, first, recent)
-    got = rs.evict_tokens(torch.from_numpy(w).to(DEV), ints(lens), keep, first, recent)
+    ws = torch.full((max(1, rs.evict_workspace_size(5, L)),), 255, dtype=torch.uint8, device=DEV)
+    got = rs.evict_tokens(torch.from_numpy(w).to(DEV), ints(lens), keep, first, recent, workspace=ws)
     assert np.array_equal(got[1].cpu().numpy(), ref[1])
     assert np.array_equal(got[0].cpu().numpy(), ref[0])
 

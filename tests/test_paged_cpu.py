@@ -292,6 +292,11 @@ def test_evict_validation(lib):
     assert call(mass=None) == 1 and call(lens=None) == 1 and call(idx=None) == 1 and call(n=None) == 1
     assert call(B=0) == 0 and call(B=1 << 23) == 2
     assert call(ml=(1 << 30) + 1, ld=1 << 31) == 2
+    size = lib.rolesub_evict_workspace_size
+    got = [size(3, n) for n in (1, 4096, 16384, 16385, 40000, 131071, 524288, 524289, 10 ** 6, 10 ** 9)]
+    assert got == sorted(got) and got[3] > 0 and size(4, 40000) >= size(3, 40000) and size(0, 40000) == 0
+    assert call(ml=40000, ld=40000, ws=None) == 1 and "workspace" in _last()
+    assert call(ml=40000, ld=40000, ws=ctypes.c_void_p(0x10000004)) == 1
 
 
 def test_compact_validation(lib):
