@@ -426,7 +426,8 @@ rolesub_status rolesub_full_values(const rolesub_dims* dims, rolesub_dtype dtype
  * (0: dense), are multiples of 16 bytes; a sample's tokens follow one another
  * at that stride and samples at T times it, e.g. views of a fused projection.
  * Unlike the other calls' samples, a sequence or a head may lie beyond 2 GiB of
- * its tensor; one page's keys or values stay below 2 GiB.
+ * its tensor; one page's keys or values stay below 2 GiB, and
+ * n_pages*page below 2^29.
  * ------------------------------------------------------------------------ */
 typedef struct rolesub_pages {
   int32_t n_pages, page, vcap;

@@ -3,9 +3,10 @@
 //   s[r,t] = scale <q_r, k_t>,  P = softmax over the tokens a row sees,
 //   u_r    = sum_t P[r,t] (M_t z_t),  out_r = R_h u_r
 //
-// The rows of one key head are its rep = Hq / H query heads times Tq queries.
-// Splits of `chunk` tokens are computed by separate workgroups into partial sums
-// with their maximum and sum of exponentials; k_join adds them and rotates back.
+// The rows of one key head are its rep = Hq / H query heads times Tq queries, in
+// blocks of 16. Splits of `chunk` tokens are computed by separate workgroups into
+// partial sums with their maximum and sum of exponentials, which k_join adds and
+// rotates back; a single split is finished where it was computed.
 #include <algorithm>
 
 #include "common.hpp"
@@ -30,11 +31,6 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 // score above -inf are zeros, or NaN where a score was: they are added as they are.
 __device__ __forceinline__ float weight_of(float m, float M) { return m == -__builtin_inff() ? 1.f : exp2_(m - M); }
 
-struct alignas(16) TokenRec {
-  uint32_t mask;
-  int32_t slot, page, pad;
-};
-
 template <class T, int DH>
 struct Tile {
   static constexpr bool kBf16 = sizeof(T) == 2;
@@ -48,20 +44,89 @@ struct Tile {
   static constexpr int ZLD = ROWB + (kBf16 ? 32 : 16);
   static constexpr int ZB = TK * ZLD;
   static constexpr int RLD = DH + 4;  // floats of a row while the waves' sums are added
-  static constexpr int SMEM = 4 * ZB > 4 * 16 * RLD * 4 ? 4 * ZB : 4 * 16 * RLD * 4;
+  static constexpr int RB = 16 * RLD * 4;
+  static constexpr int SMEM = 4 * ZB > 4 * RB ? 4 * ZB : 4 * RB;
   static constexpr int MB = DH / 16;
 };
 
+__device__ __forceinline__ int tokens_of(const DecodeParams& p, int b) {
+  const int64_t cap = static_cast<int64_t>(p.max_pages) << p.c.shift;
+  return static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
+}
+
+// Output rows [r0, r0 + 16) of key head h from their normalised sums u (LDS, rows of
+// RLD floats; rows past R are zero): out = R_h u on the matrix cores, R's rows as
+// the product's rows. The sums enter as two bf16 each (their rounding stays below
+// the output's), or in f32. All 256 threads.
+template <class T, int DH>
+__device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h, int r0, const float* u) {
+  using L = Tile<T, DH>;
+  constexpr int KS = L::KS, EP = L::EP;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
+  const int r = r0 + l16;
+  const float* ur = u + l16 * L::RLD;
+#pragma unroll
+  for (int mb = w; mb < L::MB; mb += 4) {
+    f32x4 o = {0, 0, 0, 0};
+    if (p.Rm) {
+      const T* Rr = static_cast<const T*>(p.Rm) + (static_cast<int64_t>(h) * DH + 16 * mb + l16) * DH;
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        const int d = (4 * j + g4) * EP;
+        const u32x4 a = *reinterpret_cast<const u32x4*>(Rr + d);
+        if constexpr (L::kBf16) {
+          bf16x8 hi, lo;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            hi[x] = fromf<bf16>(ur[d + x]);
+            lo[x] = fromf<bf16>(ur[d + x] - tof(hi[x]));
+          }
+          o = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), hi, o);
+          o = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), lo, o);
+        } else {
+          const f32x4 af = __builtin_bit_cast(f32x4, a);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o = __builtin_amdgcn_mfma_f32_16x16x4f32(af[x], ur[d + x], o, 0, 0, 0);
+        }
+      }
+    } else {
+      o = *reinterpret_cast<const f32x4*>(ur + 16 * mb + 4 * g4);
+    }
+    if (r < p.R) {
+      const int64_t at = ((static_cast<int64_t>(b) * p.Tq + r / p.rep) * p.Hq + h * p.rep + r % p.rep) * DH + 16 * mb + 4 * g4;
+      if (p.out_f32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = o;
+      } else {
+        T* y = static_cast<T*>(p.out) + at;
+        if constexpr (L::kBf16) {
+          const u32x2 v = {pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+          *reinterpret_cast<u32x2*>(y) = v;
+        } else {
+          *reinterpret_cast<f32x4*>(y) = o;
+        }
+      }
+    }
+  }
+}
+
+// One split of one key head and 16 * WR rows: wave w takes row block w % WR and every
+// (4 / WR)-th tile of tokens. Nothing is shared between the waves until their sums
+// are added, so no wave waits for another: each loads its next tile's keys and
+// kept groups into registers while it works on the current one, and the masks and
+// slots that address them a tile earlier still. A block of 16 tokens lies in one
+// page, so its keys and its groups are each one buffer resource: a dropped group or
+// a page that is none is an offset past it, which reads zeros and moves nothing.
 // SUB: value groups in a 16-byte piece of a row (1: a piece lies in one group).
-template <class T, int DH, int RT, int SUB>
-__global__ __launch_bounds__(256) void k_decode(DecodeParams p) {
+template <class T, int DH, int WR, int SUB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4))) void k_decode(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, NVI = L::NVI, MB = L::MB, RLD = L::RLD;
+  constexpr int WT = 4 / WR, STEP = WT * TK, TPP = 64 / NB;  // tiles whose pages one load brings
   __shared__ __attribute__((aligned(16))) char smem[L::SMEM];
-  __shared__ TokenRec s_rec[4][TK];
-  __shared__ float s_m[4][16 * RT], s_l[4][16 * RT];
+  __shared__ u32x2 s_rec[4][TK];
+  __shared__ float s_m[4][16], s_l[4][16];
   const PagedCache& c = p.c;
-  const int nrt = (p.R + 16 * RT - 1) / (16 * RT);
+  const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
   int lin = blockIdx.x;
   const int rtile = lin % nrt;
   lin /= nrt;
@@ -70,345 +135,441 @@ __global__ __launch_bounds__(256) void k_decode(DecodeParams p) {
   const int h = lin % c.H, b = lin / c.H;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15,
             g4 = lane >> 4;
-  const int64_t cap = static_cast<int64_t>(p.max_pages) << c.shift;
-  const int len = static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
-  const int c0 = sp * p.chunk;
-  if (c0 >= len) return;
+  const int len = tokens_of(p, b), c0 = sp * p.chunk;
+  if (c0 >= len && (p.n_split > 1 || sp > 0)) return;
   const uint32_t gm = group_bits(c.G);
+  const int shift = c.shift, pmask = c.page - 1, gb = c.ds * static_cast<int>(sizeof(T));
 
-  int lim[RT];  // tokens this lane's rows see
-  int top = 0;
-  uint4 qf[RT][KS];
+  // this lane's row, its query and the tokens it sees
+  const int r = (rtile * WR + w % WR) * 16 + l16;
+  int lim = 0;
+  u32x4 qf[KS];
 #pragma unroll
-  for (int k = 0; k < RT; ++k) {
-    const int r = (rtile * RT + k) * 16 + l16;
-    lim[k] = 0;
+  for (int j = 0; j < KS; ++j) qf[j] = u32x4{0, 0, 0, 0};
+  if (r < p.R) {
+    const int jq = r / p.rep, hq = h * p.rep + r % p.rep;
+    lim = p.visible ? min(len, max(p.visible[static_cast<int64_t>(b) * p.Tq + jq], 0)) : len;
+    const T* q = static_cast<const T*>(p.q) + (static_cast<int64_t>(b) * p.Tq + jq) * p.q_stride +
+                 static_cast<int64_t>(hq) * DH;
 #pragma unroll
-    for (int j = 0; j < KS; ++j) qf[k][j] = uint4{0, 0, 0, 0};
-    if (r < p.R) {
-      const int jq = r / p.rep, hq = h * p.rep + r % p.rep;
-      lim[k] = p.visible ? min(len, max(p.visible[static_cast<int64_t>(b) * p.Tq + jq], 0)) : len;
-      const T* q = static_cast<const T*>(p.q) + (static_cast<int64_t>(b) * p.Tq + jq) * p.q_stride +
-                   static_cast<int64_t>(hq) * DH;
-#pragma unroll
-      for (int j = 0; j < KS; ++j) qf[k][j] = *reinterpret_cast<const uint4*>(q + (4 * j + g4) * EP);
-    }
-    top = max(top, lim[k]);
+    for (int j = 0; j < KS; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + (4 * j + g4) * EP);
   }
+  int top = lim;
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor(top, o, kWave));
   const int end = min(c0 + p.chunk, __builtin_amdgcn_readfirstlane(top));
+  const int first = c0 + (w / WR) * TK;
 
-  float m[RT], l[RT];
-  f32x4 acc[RT][MB];
+  const rsrc_t r_table = make_rsrc(p.table + static_cast<int64_t>(b) * p.max_pages,
+                                   clamp_bytes(static_cast<size_t>(p.max_pages) * 4));
+  const uint32_t meta_bytes = static_cast<uint32_t>(c.n_pages) << (shift + 2);  // below 2 GiB
+  const rsrc_t r_mask = make_rsrc(c.mask, meta_bytes), r_slot = make_rsrc(c.slot, meta_bytes);
+  const int64_t kstep = static_cast<int64_t>(c.page) * L::ROWB, vstep = static_cast<int64_t>(c.vcap) * gb;
+
+  // a lane's pieces of the values: always the same part of a row
+  const int pc = lane % L::LPT, vt = lane / L::LPT;
+  const int vg = SUB == 1 ? pc * 16 / gb : pc * SUB;
+  const uint32_t vin = SUB == 1 ? static_cast<uint32_t>(pc * 16 % gb) : 0u;
+
   char* zt = smem + w * L::ZB;
-  TokenRec* rec = s_rec[w];
+  u32x2* rec = s_rec[w];
+  float* px = p.x ? p.x + ((static_cast<int64_t>(b) * c.H + h) * p.R + r) * p.x_ld : nullptr;
+
+  float m, l;
+  f32x4 acc[MB];
   // The second round runs only where the first one's sums are not finite: it adds
   // token by token, so that an infinity or NaN in a value reaches the rows that
   // see its token and no other (a matrix product multiplies it by their zeros).
 #pragma unroll 1
   for (int round = 0; round < 2; ++round) {
+    m = -__builtin_inff();
+    l = 0.f;
 #pragma unroll
-    for (int k = 0; k < RT; ++k) {
-      m[k] = -__builtin_inff();
-      l[k] = 0.f;
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb) acc[k][mb] = f32x4{0, 0, 0, 0};
-    }
-#pragma unroll 1
-    for (int t0 = c0 + w * TK; t0 < end; t0 += 4 * TK) {
-      TokenRec mine = {0, 0, -1, 0};
-      if (lane < TK && t0 + lane < end) {
-        const int t = t0 + lane;
-        const int32_t pg = p.table[static_cast<int64_t>(b) * p.max_pages + (t >> c.shift)];
-        if (static_cast<uint32_t>(pg) < static_cast<uint32_t>(c.n_pages)) {
-          const int64_t meta = (static_cast<int64_t>(pg) << c.shift) + (t & (c.page - 1));
-          mine = TokenRec{c.mask[meta] & gm, c.slot[meta], pg, 0};
-        }
+    for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0, 0, 0, 0};
+    int pgs = -1;     // lane j: the page of block j % NB of the (j / NB)-th of TPP tiles
+    int pg1[NB];      // pages of the next tile, whose masks and slots are on their way
+    uint32_t mk1 = 0;
+    int sl1 = 0;
+    u32x4 kf[NB][KS], vf[NVI];
+    bool there[NB], there1[NB];
+
+    auto request_meta = [&](int i) {
+      const int t0 = first + i * STEP;
+      if (i % TPP == 0) {
+        const int t = t0 + lane / NB * STEP + lane % NB * 16;
+        const int v = static_cast<int>(bload4(r_table, oob_unless(t < end, static_cast<uint32_t>(t >> shift) * 4u)));
+        pgs = t < end && static_cast<uint32_t>(v) < static_cast<uint32_t>(c.n_pages) ? v : -1;
       }
-      if (lane < TK) rec[lane] = mine;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) pg1[nb] = __builtin_amdgcn_readlane(pgs, i % TPP * NB + nb);
+      const int t = t0 + lane, pg = NB == 2 && lane >= 16 ? pg1[NB - 1] : pg1[0];
+      const uint32_t off = oob_unless(lane < TK && t < end && pg >= 0,
+                                      (static_cast<uint32_t>(pg) << (shift + 2)) + static_cast<uint32_t>(t & pmask) * 4u);
+      mk1 = bload4(r_mask, off);
+      sl1 = static_cast<int>(bload4(r_slot, off));
+    };
+    auto request_tile = [&](int i) {  // of the pages pg1
+      const int t0 = first + i * STEP;
+      if (lane < TK) rec[lane] = u32x2{mk1 & gm, static_cast<uint32_t>(sl1)};
       wave_lds_order();
-      // scores: tokens are the rows of the product, queries its columns
-      bool there[NB];
-      f32x4 s[RT][NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const int pg = __builtin_amdgcn_readlane(mine.page, 16 * nb);  // a page holds whole blocks of 16 tokens
-        there[nb] = pg >= 0;
+        there1[nb] = pg1[nb] >= 0;
+        const int64_t at = static_cast<int64_t>(max(pg1[nb], 0)) * c.H + h;
+        const rsrc_t rk = make_rsrc(static_cast<const char*>(c.K) + at * kstep,
+                                    there1[nb] ? static_cast<uint32_t>(kstep) : 0u);
+        const uint32_t ko = static_cast<uint32_t>(((t0 + 16 * nb) & pmask) + l16) * L::ROWB + 16 * g4;
 #pragma unroll
-        for (int k = 0; k < RT; ++k) s[k][nb] = f32x4{0, 0, 0, 0};
-        if (!there[nb]) continue;
-        const int row = (t0 + 16 * nb) & (c.page - 1);
-        const char* kp = static_cast<const char*>(c.K) +
-                         (((static_cast<int64_t>(pg) * c.H + h) << c.shift) + row + l16) * L::ROWB + 16 * g4;
-        uint4 kf[KS];
+        for (int j = 0; j < KS; ++j) kf[nb][j] = bload16(rk, ko + 64 * j);
+      }
 #pragma unroll
-        for (int j = 0; j < KS; ++j) kf[j] = *reinterpret_cast<const uint4*>(kp + 64 * j);
+      for (int nb = 0; nb < NB; ++nb) {
+        const int64_t at = static_cast<int64_t>(max(pg1[nb], 0)) * c.H + h;
+        const rsrc_t rv = make_rsrc(static_cast<const char*>(c.V) + at * vstep,
+                                    there1[nb] ? static_cast<uint32_t>(vstep) : 0u);
 #pragma unroll
-        for (int j = 0; j < KS; ++j)
+        for (int i2 = nb * NVI / NB; i2 < (nb + 1) * NVI / NB; ++i2) {
+          const u32x2 t = rec[i2 * L::TPI + vt];
+          uint32_t sl = t.y + __popc(t.x & ((1u << vg) - 1u));
+          if constexpr (SUB == 1) {
+            vf[i2] = bload16(rv, ((t.x >> vg) & 1u) && sl < static_cast<uint32_t>(c.vcap) ? sl * gb + vin : kOOB);
+          } else {
+            uint32_t* vv = reinterpret_cast<uint32_t*>(&vf[i2]);
 #pragma unroll
-          for (int k = 0; k < RT; ++k) {
-            if constexpr (L::kBf16) {
-              s[k][nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, kf[j]), __builtin_bit_cast(bf16x8, qf[k][j]), s[k][nb]);
-            } else {
-              const f32x4 a = __builtin_bit_cast(f32x4, kf[j]), q = __builtin_bit_cast(f32x4, qf[k][j]);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) s[k][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], q[i], s[k][nb], 0, 0, 0);
+            for (int u = 0; u < SUB; ++u) {
+              const bool on = (t.x >> (vg + u)) & 1u;
+              const uint32_t off = on && sl < static_cast<uint32_t>(c.vcap) ? sl * gb : kOOB;
+              if constexpr (SUB == 2) {
+                const u32x2 x = bload8(rv, off);
+                vv[2 * u] = x.x;
+                vv[2 * u + 1] = x.y;
+              } else {
+                vv[u] = bload4(rv, off);
+              }
+              sl += on;
             }
           }
+        }
+      }
+    };
+
+    request_meta(0);
+    request_tile(0);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) there[nb] = there1[nb];
+    request_meta(1);
+#pragma unroll 1
+    for (int i = 0, t0 = first; t0 < end; ++i, t0 += STEP) {
+      // scores: tokens are the rows of the product, queries its columns
+      f32x4 s[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        s[nb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          if constexpr (L::kBf16) {
+            s[nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, kf[nb][j]), __builtin_bit_cast(bf16x8, qf[j]), s[nb]);
+          } else {
+            const f32x4 a = __builtin_bit_cast(f32x4, kf[nb][j]), q = __builtin_bit_cast(f32x4, qf[j]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[x], q[x], s[nb], 0, 0, 0);
+          }
+        }
       }
       // the tile's kept groups into their places, dropped ones as zeros
 #pragma unroll
-      for (int i = 0; i < NVI; ++i) {
-        const int tk = i * L::TPI + lane / L::LPT, pc = lane % L::LPT;
-        const TokenRec r = rec[tk];
-        const int64_t base = (static_cast<int64_t>(r.page) * c.H + h) * c.vcap;
-        uint4 v = {0, 0, 0, 0};
-        if constexpr (SUB == 1) {
-          const int g = pc * EP / c.ds, sl = r.slot + __popc(r.mask & ((1u << g) - 1u));
-          if (((r.mask >> g) & 1u) && static_cast<uint32_t>(sl) < static_cast<uint32_t>(c.vcap))
-            v = *reinterpret_cast<const uint4*>(static_cast<const T*>(c.V) + (base + sl) * c.ds + pc * EP % c.ds);
-        } else {
-          constexpr int W = 4 / SUB;  // 32-bit words of a group
-          uint32_t* vv = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-          for (int u = 0; u < SUB; ++u) {
-            const int g = pc * SUB + u, sl = r.slot + __popc(r.mask & ((1u << g) - 1u));
-            if (((r.mask >> g) & 1u) && static_cast<uint32_t>(sl) < static_cast<uint32_t>(c.vcap)) {
-              const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const T*>(c.V) + (base + sl) * c.ds);
-#pragma unroll
-              for (int x = 0; x < W; ++x) vv[u * W + x] = src[x];
-            }
-          }
-        }
-        *reinterpret_cast<uint4*>(zt + tk * L::ZLD + 16 * pc) = v;
-      }
+      for (int x = 0; x < NVI; ++x) *reinterpret_cast<u32x4*>(zt + (x * L::TPI + vt) * L::ZLD + 16 * pc) = vf[x];
       wave_lds_order();
+      bool now[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) now[nb] = there[nb];
+      request_tile(i + 1);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) there[nb] = there1[nb];
+      request_meta(i + 2);
       // softmax against the running maximum
+      float mx = -__builtin_inff();
 #pragma unroll
-      for (int k = 0; k < RT; ++k) {
-        float mx = -__builtin_inff();
+      for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool see = there[nb] && t0 + 16 * nb + 4 * g4 + i < lim[k];
-            s[k][nb][i] = see ? s[k][nb][i] * p.scale : -__builtin_inff();
-            mx = fmaxf(mx, s[k][nb][i]);
-          }
-          const int r = (rtile * RT + k) * 16 + l16, t = t0 + 16 * nb + 4 * g4;
-          if (p.x && r < p.R && t < end)
-            *reinterpret_cast<f32x4*>(p.x + ((static_cast<int64_t>(b) * c.H + h) * p.R + r) * p.x_ld + t) = s[k][nb];
+        for (int x = 0; x < 4; ++x) {
+          const bool see = now[nb] && t0 + 16 * nb + 4 * g4 + x < lim;
+          s[nb][x] = see ? s[nb][x] * p.scale : -__builtin_inff();
+          mx = fmaxf(mx, s[nb][x]);
         }
-        mx = max_xor32(max_xor16(mx));
-        const float mn = fmaxf(m[k], mx), ms = mn == -__builtin_inff() ? 0.f : mn;
-        const float al = exp2_(m[k] - ms);
-        m[k] = mn;
-        float sum = 0.f;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[k][nb][i] = exp2_(s[k][nb][i] - ms);
-            sum += s[k][nb][i];
-          }
-        l[k] = l[k] * al + sum;
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) acc[k][mb] *= al;
+        const int t = t0 + 16 * nb + 4 * g4;
+        if (px && r < p.R && t < end) *reinterpret_cast<f32x4*>(px + t) = s[nb];
       }
+      mx = max_xor32(max_xor16(mx));
+      const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.f : mn;
+      if (__any(mn > m)) {
+        const float al = exp2_(m - ms);
+        l *= al;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) acc[mb] *= al;
+        m = mn;
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          s[nb][x] = exp2_(s[nb][x] - ms);
+          l += s[nb][x];
+        }
       if (round == 0) {
         if constexpr (L::kBf16) {
           // weights as two bf16 each, so that their rounding stays below the output's
-          bf16x8 hi[RT], lo[RT];
+          bf16x8 hi, lo;
 #pragma unroll
-          for (int k = 0; k < RT; ++k)
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              const float pv = s[k][x / 4][x % 4];
-              hi[k][x] = fromf<bf16>(pv);
-              lo[k][x] = fromf<bf16>(pv - tof(hi[k][x]));
-            }
+          for (int x = 0; x < 8; ++x) {
+            const float pv = s[x / 4][x % 4];
+            hi[x] = fromf<bf16>(pv);
+            lo[x] = fromf<bf16>(pv - tof(hi[x]));
+          }
           const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb) {
             const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
             const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-            for (int k = 0; k < RT; ++k) {
-              acc[k][mb] = mfma_16x16x32(a, hi[k], acc[k][mb]);
-              acc[k][mb] = mfma_16x16x32(a, lo[k], acc[k][mb]);
-            }
+            acc[mb] = mfma_16x16x32(a, hi, acc[mb]);
+            acc[mb] = mfma_16x16x32(a, lo, acc[mb]);
           }
         } else {
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float a = *reinterpret_cast<const float*>(zt + (4 * g4 + i) * L::ZLD + 4 * (16 * mb + l16));
-#pragma unroll
-              for (int k = 0; k < RT; ++k)
-                acc[k][mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[k][0][i], acc[k][mb], 0, 0, 0);
+            for (int x = 0; x < 4; ++x) {
+              const float a = *reinterpret_cast<const float*>(zt + (4 * g4 + x) * L::ZLD + 4 * (16 * mb + l16));
+              acc[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][x], acc[mb], 0, 0, 0);
             }
         }
       } else {
 #pragma unroll 1
-        for (int q = 0; q < 4; ++q)  // tokens 4q + i of each block: lane group q holds their weights
+        for (int q = 0; q < 4; ++q)  // tokens 4q + x of each block: lane group q holds their weights
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int tk = 16 * nb + 4 * q + i;
+            for (int x = 0; x < 4; ++x) {
+              const int tk = 16 * nb + 4 * q + x;
               const T* z = reinterpret_cast<const T*>(zt + tk * L::ZLD);
+              const float pv = __shfl(s[nb][x], 16 * q + l16, kWave);
+              if (t0 + tk < lim)
 #pragma unroll
-              for (int k = 0; k < RT; ++k) {
-                const float pv = __shfl(s[k][nb][i], 16 * q + l16, kWave);
-                if (t0 + tk < lim[k])
+                for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                  for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) acc[k][mb][x] += pv * tof(z[16 * mb + 4 * g4 + x]);
-              }
+                  for (int y = 0; y < 4; ++y) acc[mb][y] += pv * tof(z[16 * mb + 4 * g4 + y]);
             }
       }
       wave_lds_order();
     }
     bool bad = false;
 #pragma unroll
-    for (int k = 0; k < RT; ++k)
+    for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[k][mb][x]);
+      for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
     if (!__any(bad)) break;
   }
 
-  // the four waves' sums, in the order of the waves
-#pragma unroll
-  for (int k = 0; k < RT; ++k) {
-    l[k] = add_xor32(add_xor16(l[k]));
-    if (g4 == 0) {
-      s_m[w][16 * k + l16] = m[k];
-      s_l[w][16 * k + l16] = l[k];
-    }
+  // the sums of the waves of one row block, in their order
+  l = add_xor32(add_xor16(l));
+  if (g4 == 0) {
+    s_m[w][l16] = m;
+    s_l[w][l16] = l;
   }
+  __syncthreads();  // also: no wave reads its tile any more
   float* red = reinterpret_cast<float*>(smem);
+  {
+    float M = s_m[w % WR][l16];
 #pragma unroll
-  for (int k = 0; k < RT; ++k) {
-    __syncthreads();
-    const int rr = 16 * k + l16;
-    const float M = fmaxf(fmaxf(s_m[0][rr], s_m[1][rr]), fmaxf(s_m[2][rr], s_m[3][rr]));
-    const float f = weight_of(m[k], M);
+    for (int v = 1; v < WT; ++v) M = fmaxf(M, s_m[w % WR + v * WR][l16]);
+    const float f = weight_of(m, M);
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
-      *reinterpret_cast<f32x4*>(red + (w * 16 + l16) * RLD + 16 * mb + 4 * g4) = acc[k][mb] * f;
-    __syncthreads();
-    for (int u = tid; u < 16 * DH / 4; u += 256) {
-      const int row = u / (DH / 4), d = u % (DH / 4) * 4, r = (rtile * RT + k) * 16 + row;
-      if (r >= p.R) continue;
-      f32x4 a = *reinterpret_cast<const f32x4*>(red + row * RLD + d);
+      *reinterpret_cast<f32x4*>(red + (w * 16 + l16) * RLD + 16 * mb + 4 * g4) = acc[mb] * f;
+  }
+  __syncthreads();
+  const int64_t rows0 = (static_cast<int64_t>(b) * c.H + h) * p.R;
+#pragma unroll 1
+  for (int u = tid; u < 16 * WR * (DH / 4); u += 256) {
+    const int row = u / (DH / 4), d = u % (DH / 4) * 4, rb = row / 16, rr = row % 16, rg = rtile * 16 * WR + row;
+    float M = s_m[rb][rr];
 #pragma unroll
-      for (int v = 1; v < 4; ++v) a += *reinterpret_cast<const f32x4*>(red + (v * 16 + row) * RLD + d);
-      const int64_t at = ((static_cast<int64_t>(b) * c.H + h) * p.R + r) * p.n_split + sp;
-      *reinterpret_cast<f32x4*>(p.part + at * DH + d) = a;
-      if (d == 0) {
-        const int rw = 16 * k + row;
-        const float M2 = fmaxf(fmaxf(s_m[0][rw], s_m[1][rw]), fmaxf(s_m[2][rw], s_m[3][rw]));
-        float sum = 0.f;
-        for (int v = 0; v < 4; ++v) sum += s_l[v][rw] * weight_of(s_m[v][rw], M2);
-        p.stat[2 * at] = M2;
-        p.stat[2 * at + 1] = sum;
-      }
+    for (int v = 1; v < WT; ++v) M = fmaxf(M, s_m[rb + v * WR][rr]);
+    float sum = 0.f;
+    f32x4 a = {0, 0, 0, 0};
+#pragma unroll
+    for (int v = 0; v < WT; ++v) {
+      sum += s_l[rb + v * WR][rr] * weight_of(s_m[rb + v * WR][rr], M);
+      a += *reinterpret_cast<const f32x4*>(red + ((rb + v * WR) * 16 + rr) * RLD + d);
+    }
+    if (p.n_split == 1) {
+      if (rg >= p.R || sum == 0.f) a = f32x4{0, 0, 0, 0};
+      else a /= sum;
+      *reinterpret_cast<f32x4*>(red + (rb * 16 + rr) * RLD + d) = a;  // read by this thread only
+    }
+    if (rg >= p.R) continue;
+    const int64_t at = (rows0 + rg) * p.n_split + sp;
+    if (p.n_split > 1) *reinterpret_cast<f32x4*>(p.part + at * DH + d) = a;
+    if (d == 0 && p.stat) {
+      p.stat[2 * at] = M;
+      p.stat[2 * at + 1] = sum;
+    }
+  }
+  if (p.n_split == 1) {
+    __syncthreads();
+#pragma unroll 1
+    for (int rb = 0; rb < WR; ++rb) {
+      const int r0 = (rtile * WR + rb) * 16;
+      if (r0 < p.R) finish_rows<T, DH>(p, b, h, r0, red + rb * 16 * RLD);
     }
   }
 }
 
-// The splits of one query head's row added, normalised and rotated back.
+// log2 of a row's sum of exponentials from its splits' statistics, and the maximum.
+__device__ __forceinline__ void join_stat(const float* st, int ns, int from, int step, float& M, float& sum) {
+  M = -__builtin_inff();
+  sum = 0.f;
+  for (int i = from; i < ns; i += step) M = fmaxf(M, st[2 * i]);
+  for (int o = 1; o < step; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, kWave));
+  for (int i = from; i < ns; i += step) sum += st[2 * i + 1] * weight_of(st[2 * i], M);
+  for (int o = 1; o < step; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+}
+
+// The splits of 16 rows of one key head added, normalised and rotated back.
 template <class T, int DH>
-__global__ __launch_bounds__(DH) void k_join(DecodeParams p) {
-  __shared__ float u[DH];
+__device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, char* smem) {
+  using L = Tile<T, DH>;
+  constexpr int Q = DH / 4;  // 16-byte pieces of a row
+  float* u = reinterpret_cast<float*>(smem);                      // [16][RLD]
+  f32x4* red = reinterpret_cast<f32x4*>(smem + L::RB);            // [256]
+  float* s_M = reinterpret_cast<float*>(smem + L::RB + 4096);     // [16] maxima, [16] inverse sums
   const PagedCache& c = p.c;
-  const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x;  // [b][h][r]
-  const int r = static_cast<int>(row % p.R), h = static_cast<int>(row / p.R % c.H);
-  const int b = static_cast<int>(row / p.R / c.H);
-  const int64_t cap = static_cast<int64_t>(p.max_pages) << c.shift;
-  const int len = static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
+  const int nrb = (p.R + 15) / 16, tid = threadIdx.x;
+  const int r0 = static_cast<int>(blk % nrb) * 16, h = static_cast<int>(blk / nrb % c.H), b = static_cast<int>(blk / nrb / c.H);
+  const int ns = (tokens_of(p, b) + p.chunk - 1) / p.chunk, nr = min(16, p.R - r0);
+  const int64_t cell0 = ((static_cast<int64_t>(b) * c.H + h) * p.R + r0) * p.n_split;
+  {
+    const int row = tid / 16;
+    float M = -__builtin_inff(), sum = 0.f;
+    join_stat(p.stat + 2 * (cell0 + static_cast<int64_t>(min(row, nr - 1)) * p.n_split), ns, tid % 16, 16, M, sum);
+    if (tid % 16 == 0) {
+      s_M[row] = M;
+      s_M[16 + row] = sum == 0.f || row >= nr ? 0.f : 1.f / sum;
+    }
+  }
+  __syncthreads();
+  // few rows: their splits are shared out among groups of threads
+  const int items = nr * Q, groups = max(1, 256 / items);
+  for (int it0 = 0; it0 < 16 * Q; it0 += 256) {
+    const int it = it0 + tid % (groups > 1 ? items : 256), g = groups > 1 ? tid / items : 0;
+    f32x4 a = {0, 0, 0, 0};
+    const int row = it / Q, d = it % Q;
+    if (row < nr && g < groups) {
+      const int64_t cell = cell0 + static_cast<int64_t>(row) * p.n_split;
+      const float M = s_M[row];
+#pragma unroll 4
+      for (int i = g; i < ns; i += groups)
+        a += *reinterpret_cast<const f32x4*>(p.part + (cell + i) * DH + 4 * d) * weight_of(p.stat[2 * (cell + i)], M);
+    }
+    if (groups > 1) {
+      red[tid] = a;
+      __syncthreads();
+      if (tid < items)
+        for (int v = 1; v < groups; ++v) a += red[tid + v * items];
+      if (tid < items) *reinterpret_cast<f32x4*>(u + row * L::RLD + 4 * d) = s_M[16 + row] == 0.f ? f32x4{0, 0, 0, 0} : a * s_M[16 + row];
+      for (int z = tid; z < (16 - nr) * Q; z += 256)
+        *reinterpret_cast<f32x4*>(u + (nr + z / Q) * L::RLD + z % Q * 4) = f32x4{0, 0, 0, 0};
+      break;
+    }
+    *reinterpret_cast<f32x4*>(u + row * L::RLD + 4 * d) = s_M[16 + row] == 0.f ? f32x4{0, 0, 0, 0} : a * s_M[16 + row];
+  }
+  __syncthreads();
+  finish_rows<T, DH>(p, b, h, r0, u);
+}
+
+// mass_out[b,t] = decay mass_in[b,t] + the token's weight in every row: 256 tokens,
+// the rows in batches whose sums of exponentials every workgroup takes for itself.
+constexpr int kMassRows = 512;
+__device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int nblk, char* smem) {
+  float* s_lse = reinterpret_cast<float*>(smem);
+  int* s_lim = reinterpret_cast<int*>(smem + kMassRows * 4);
+  const PagedCache& c = p.c;
+  const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, t = static_cast<int>(blk % nblk) * 256 + tid;
+  const int len = tokens_of(p, b);
+  if (t - tid >= len) return;
   const int ns = (len + p.chunk - 1) / p.chunk;
-  const float* st = p.stat + 2 * row * p.n_split;
-  float M = -__builtin_inff(), sum = 0.f, x = 0.f;
-  for (int i = 0; i < ns; ++i) M = fmaxf(M, st[2 * i]);
-  for (int i = 0; i < ns; ++i) {
-    const float f = weight_of(st[2 * i], M);
-    sum += f * st[2 * i + 1];
-    x += f * p.part[(row * p.n_split + i) * DH + tid];
-  }
-  x = sum == 0.f ? 0.f : x / sum;
-  if (p.lse && tid == 0) p.lse[row] = sum == 0.f ? -__builtin_inff() : M + __log2f(sum);
-  if (p.Rm) {
-    u[tid] = x;
-    __syncthreads();
-    const T* R = static_cast<const T*>(p.Rm) + (static_cast<int64_t>(h) * DH + tid) * DH;
-    x = 0.f;
-    for (int j = 0; j < DH; ++j) x += tof(R[j]) * u[j];
-  }
-  const int64_t o = ((static_cast<int64_t>(b) * p.Tq + r / p.rep) * p.Hq + h * p.rep + r % p.rep) * DH + tid;
-  if (p.out_f32)
-    static_cast<float*>(p.out)[o] = x;
-  else
-    static_cast<T*>(p.out)[o] = fromf<T>(x);
-}
-
-// mass_out[b,t] = decay mass_in[b,t] + the token's weight in every row.
-__global__ __launch_bounds__(256) void k_mass(DecodeParams p, int nblk) {
-  const PagedCache& c = p.c;
-  const int b = blockIdx.x / nblk, t = blockIdx.x % nblk * 256 + threadIdx.x;
-  const int64_t cap = static_cast<int64_t>(p.max_pages) << c.shift;
-  const int len = static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
-  if (t >= len) return;
+  const int64_t rows = static_cast<int64_t>(c.H) * p.R, row0 = b * rows;
   float sum = 0.f;
-  for (int64_t hr = 0; hr < static_cast<int64_t>(c.H) * p.R; ++hr) {
-    const int64_t row = static_cast<int64_t>(b) * c.H * p.R + hr;
-    const int lim = p.visible ? p.visible[static_cast<int64_t>(b) * p.Tq + hr % p.R / p.rep] : len;
-    const float lse = p.lse[row];
-    if (t < lim && lse != -__builtin_inff()) sum += exp2_(p.x[row * p.x_ld + t] - lse);
+  for (int64_t q0 = 0; q0 < rows; q0 += kMassRows) {
+    const int n = static_cast<int>(min(rows - q0, static_cast<int64_t>(kMassRows)));
+    __syncthreads();
+    for (int q = tid / 16; q < n; q += 16) {
+      float M, l;
+      join_stat(p.stat + 2 * (row0 + q0 + q) * p.n_split, ns, tid % 16, 16, M, l);
+      if (tid % 16 == 0) {
+        s_lse[q] = M + __log2f(l);  // -inf where nothing was seen
+        s_lim[q] = l == 0.f ? 0
+                   : p.visible ? p.visible[static_cast<int64_t>(b) * p.Tq + (q0 + q) % p.R / p.rep] : len;
+      }
+    }
+    __syncthreads();
+    if (t < len)
+#pragma unroll 8
+      for (int q = 0; q < n; ++q) {
+        const float x = p.x[(row0 + q0 + q) * p.x_ld + t];
+        sum += t < s_lim[q] ? exp2_(x - s_lse[q]) : 0.f;
+      }
   }
-  const int64_t at = static_cast<int64_t>(b) * p.mass_ld + t;
-  p.mass_out[at] = p.mass_in ? p.decay * p.mass_in[at] + sum : sum;
+  if (t < len) {
+    const int64_t at = static_cast<int64_t>(b) * p.mass_ld + t;
+    p.mass_out[at] = p.mass_in ? p.decay * p.mass_in[at] + sum : sum;
+  }
 }
 
-template <class T, int DH, int RT>
-void go(const DecodeParams& p, dim3 grid, hipStream_t s) {
+// What follows the splits: the first `joins` workgroups finish the outputs, the
+// others add the weights.
+template <class T, int DH>
+__global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nblk) {
+  using L = Tile<T, DH>;
+  constexpr int S = L::RB + 4096 + 128;
+  __shared__ __attribute__((aligned(16))) char smem[S > kMassRows * 8 ? S : kMassRows * 8];
+  if (static_cast<int>(blockIdx.x) < joins)
+    join_rows<T, DH>(p, blockIdx.x, smem);
+  else
+    add_mass(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, smem);
+}
+
+int row_blocks(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }  // blocks of 16 rows of a workgroup
+
+template <class T, int DH, int WR>
+void go(const DecodeParams& p, hipStream_t s) {
   const int sub = p.c.ds >= Tile<T, DH>::EP ? 1 : Tile<T, DH>::EP / p.c.ds;
-  auto kern = sub == 1 ? k_decode<T, DH, RT, 1> : k_decode<T, DH, RT, 2>;
+  auto kern = sub == 1 ? k_decode<T, DH, WR, 1> : k_decode<T, DH, WR, 2>;
   if constexpr (sizeof(T) == 2) {
-    if (sub == 4) kern = k_decode<T, DH, RT, 4>;
+    if (sub == 4) kern = k_decode<T, DH, WR, 4>;
   }
-  hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, p);
+  const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(256), 0, s, p);
 }
-
-int row_blocks(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }  // blocks of 16 rows a workgroup takes
 
 template <class T, int DH>
 hipError_t launch(const DecodeParams& p, hipStream_t s) {
-  const int RT = row_blocks(p.R), nrt = (p.R + 16 * RT - 1) / (16 * RT);
-  const dim3 grid(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B);
-  if (p.n_split > 0) {
-    if (RT == 1)
-      go<T, DH, 1>(p, grid, s);
-    else if (RT == 2)
-      go<T, DH, 2>(p, grid, s);
-    else
-      go<T, DH, 4>(p, grid, s);
-  }
-  hipLaunchKernelGGL((k_join<T, DH>), dim3(static_cast<unsigned>(p.B) * p.c.H * p.R), dim3(DH), 0, s, p);
-  if (p.mass_out && p.max_len > 0) {
-    const int nblk = (p.max_len + 255) / 256;
-    hipLaunchKernelGGL(k_mass, dim3(static_cast<unsigned>(p.B) * nblk), dim3(256), 0, s, p, nblk);
-  }
+  const int WR = row_blocks(p.R);
+  if (WR == 1)
+    go<T, DH, 1>(p, s);
+  else if (WR == 2)
+    go<T, DH, 2>(p, s);
+  else
+    go<T, DH, 4>(p, s);
+  const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0, nblk = p.mass_out ? (p.max_len + 255) / 256 : 0;
+  if (joins + nblk > 0)
+    hipLaunchKernelGGL((k_join<T, DH>), dim3(static_cast<unsigned>(joins) + static_cast<unsigned>(nblk) * p.B), dim3(256),
+                       0, s, p, joins, nblk);
   return hipGetLastError();
 }
 
 constexpr int64_t kSplitWgs = 2048;  // workgroups that the splits are made for
+constexpr int64_t kMaxSplits = 256;  // that k_join adds up
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
@@ -416,23 +577,22 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass) {
   DecodePlan d;
-  const int RT = row_blocks(R), nrt = (R + 16 * RT - 1) / (16 * RT);
+  const int WR = row_blocks(R), nrt = (R + 16 * WR - 1) / (16 * WR);
   const int64_t units = (static_cast<int64_t>(max_len) + 127) / 128;  // of 128 tokens, a tile for each of four waves
   const int64_t wgs = static_cast<int64_t>(B) * H * nrt;
-  const int64_t per = std::max<int64_t>(1, (units * wgs + kSplitWgs - 1) / kSplitWgs);
+  const int64_t per = std::max((units * wgs + kSplitWgs - 1) / kSplitWgs, (units + kMaxSplits - 1) / kMaxSplits);
   d.chunk = static_cast<int>(128 * std::max<int64_t>(1, std::min(per, units)));
-  d.n_split = static_cast<int>((static_cast<int64_t>(max_len) + d.chunk - 1) / d.chunk);
+  d.n_split = std::max(1, static_cast<int>((static_cast<int64_t>(max_len) + d.chunk - 1) / d.chunk));
   d.x_ld = (max_len + 3) / 4 * 4;
   const size_t rows = static_cast<size_t>(B) * H * R, cells = rows * d.n_split;
-  d.off_stat = up256(cells * dh * 4);
-  d.off_x = d.off_stat + up256(cells * 8);
-  d.off_lse = d.off_x + (mass ? up256(rows * d.x_ld * 4) : 0);
-  d.bytes = d.off_lse + (mass ? up256(rows * 4) : 0);
+  d.off_stat = d.n_split > 1 ? up256(cells * dh * 4) : 0;
+  d.off_x = d.off_stat + (d.n_split > 1 || mass ? up256(cells * 8) : 0);
+  d.bytes = d.off_x + (mass ? up256(rows * d.x_ld * 4) : 0);
   // what to ask a caller for: a bound on the above that does not fall as B, Tq or
   // max_len grows (n_split <= kSplitWgs / wgs + 1 and R <= 64 nrt)
-  const size_t most = std::min(rows * static_cast<size_t>(units),
+  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)),
                                std::min<size_t>(R, 64) * static_cast<size_t>(kSplitWgs) + rows);
-  d.ask = up256(most * dh * 4) + up256(most * 8) + (mass ? up256(rows * d.x_ld * 4) + up256(rows * 4) : 0);
+  d.ask = up256(most * dh * 4) + up256(most * 8) + (mass ? up256(rows * d.x_ld * 4) : 0);
   return d;
 }
 

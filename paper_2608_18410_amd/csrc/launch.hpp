@@ -305,15 +305,14 @@ struct DecodeParams {
   int64_t mass_ld;
   // workspace
   int n_split, chunk;  // tokens of a split
-  float* part;         // [B][H][R][n_split][dh] sums of P z, unnormalised
-  float* stat;         // [B][H][R][n_split][2]  maximum (log2), sum of P
+  float* part;         // [B][H][R][n_split][dh] sums of P z, unnormalised (with splits)
+  float* stat;         // [B][H][R][n_split][2]  maximum (log2), sum of P (with splits or mass)
   float* x;            // [B][H][R][x_ld] scores in units of log2 (with mass)
-  float* lse;          // [B][H][R] log2 of the sum of exponentials (with mass)
   int x_ld;
 };
 struct DecodePlan {
   int n_split, chunk, x_ld;
-  size_t off_stat, off_x, off_lse, bytes;  // of this call
+  size_t off_stat, off_x, bytes;  // of this call
   size_t ask;  // at least bytes of every call of no more sequences, queries and tokens
 };
 DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass);

@@ -883,6 +883,8 @@ rolesub_status check_pages(const char* fn, const char* name, const rolesub_pages
   const size_t e = esize(dtype), gb = c.ds * e;
   if (static_cast<size_t>(c.H) * c.page * c.dh * e >= kMaxRegion || static_cast<size_t>(c.H) * c.vcap * gb >= kMaxRegion)
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: %s: one page's keys or values exceed 2 GiB", fn, name);
+  if (static_cast<int64_t>(c.n_pages) * c.page >= (1 << 29))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: %s: 2^29 tokens or more", fn, name);
   if (!need) return ROLESUB_OK;
   if (c.n_pages > 0 && (!c.K || !c.mask || !c.slot || (c.vcap > 0 && !c.V)))
     return fail(ROLESUB_ERR_INVALID_ARG, "%s: %s: K, V, mask and slot must be non-NULL", fn, name);
@@ -1071,18 +1073,15 @@ rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dt
                 workspace ? ws_bytes : static_cast<size_t>(0));
   if (!aligned(workspace, 16)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace must lie on 16 bytes", fn);
   if (static_cast<size_t>(B) * p.c.H * d.n_split * ((p.R + 15) / 16) * 256 >= kMaxThreads ||
-      static_cast<size_t>(B) * (p.max_len / 256 + 1) * 256 >= kMaxThreads)
+      (static_cast<size_t>(B) * p.c.H * ((p.R + 15) / 16) + static_cast<size_t>(B) * (p.max_len / 256 + 1)) * 256 >= kMaxThreads)
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads or queries", fn);
   char* ws = static_cast<char*>(workspace);
   p.n_split = d.n_split;
   p.chunk = d.chunk;
   p.x_ld = d.x_ld;
   p.part = reinterpret_cast<float*>(ws);
-  p.stat = reinterpret_cast<float*>(ws + d.off_stat);
-  if (mass_out) {
-    p.x = reinterpret_cast<float*>(ws + d.off_x);
-    p.lse = reinterpret_cast<float*>(ws + d.off_lse);
-  }
+  if (d.off_x > d.off_stat) p.stat = reinterpret_cast<float*>(ws + d.off_stat);
+  if (mass_out) p.x = reinterpret_cast<float*>(ws + d.off_x);
   return from_hip(launch_decode(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
 }
 
