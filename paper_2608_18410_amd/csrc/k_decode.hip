@@ -109,6 +109,101 @@ __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h,
   }
 }
 
+// One 64-byte step of the scores of 16 tokens (rows) and 16 queries (columns).
+template <class T>
+__device__ __forceinline__ f32x4 score_step(u32x4 k, u32x4 q, f32x4 s) {
+  if constexpr (sizeof(T) == 2) {
+    return mfma_16x16x32(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q), s);
+  } else {
+    const f32x4 a = __builtin_bit_cast(f32x4, k), x = __builtin_bit_cast(f32x4, q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], x[i], s, 0, 0, 0);
+    return s;
+  }
+}
+
+// A lane's part of row r's query: the dims that its part of a key is multiplied by.
+template <class T, int DH>
+__device__ __forceinline__ void load_query(const DecodeParams& p, int b, int h, int r, int g4, u32x4* qf) {
+  using L = Tile<T, DH>;
+#pragma unroll
+  for (int j = 0; j < L::KS; ++j) qf[j] = u32x4{0, 0, 0, 0};
+  if (r >= p.R) return;
+  const T* q = static_cast<const T*>(p.q) + (static_cast<int64_t>(b) * p.Tq + r / p.rep) * p.q_stride +
+               static_cast<int64_t>(h * p.rep + r % p.rep) * DH;
+#pragma unroll
+  for (int j = 0; j < L::KS; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + (4 * j + g4) * L::EP);
+}
+
+// A wave's sums again, token by token, where they were not finite: an infinity or
+// NaN in a value then reaches the rows that see its token and no other (a matrix
+// product multiplies it by their zeros). Scores and weights are the same; the sums
+// stay in LDS, so that this takes no registers from the loop it follows.
+template <class T, int DH>
+__device__ __forceinline__ void one_by_one(const DecodeParams& p, int b, int h, int r, int first, int step, int end,
+                                           int lim, char* zt, float& m, float& l, f32x4* acc) {
+  using L = Tile<T, DH>;
+  constexpr int KS = L::KS, MB = L::MB;
+  static_assert(L::ZB >= 16 * DH * 4, "a wave's sums fit its tile");
+  const PagedCache& c = p.c;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+  const uint32_t gm = group_bits(c.G);
+  float* sum = reinterpret_cast<float*>(zt) + l16 * DH + 4 * g4;  // this lane's: dims 16 mb + 4 g4 + 0..3
+  m = -__builtin_inff();
+  l = 0.f;
+#pragma unroll 1
+  for (int d = 0; d < DH; d += 16) *reinterpret_cast<f32x4*>(sum + d) = f32x4{0, 0, 0, 0};
+#pragma unroll 1
+  for (int tile = first; tile < end; tile += step)
+#pragma unroll 1
+    for (int t0 = tile; t0 < min(tile + L::TK, end); t0 += 16) {
+      const int pg = p.table[static_cast<int64_t>(b) * p.max_pages + (t0 >> c.shift)];
+      if (static_cast<uint32_t>(pg) >= static_cast<uint32_t>(c.n_pages)) continue;
+      const int row = t0 & (c.page - 1);
+      const int64_t head = static_cast<int64_t>(pg) * c.H + h;
+      const char* kp = static_cast<const char*>(c.K) + ((head << c.shift) + row + l16) * L::ROWB + 16 * g4;
+      u32x4 qf[KS];
+      load_query<T, DH>(p, b, h, r, g4, qf);
+      f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < KS; ++j) s = score_step<T>(*reinterpret_cast<const u32x4*>(kp + 64 * j), qf[j], s);
+      float mx = -__builtin_inff();
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        s[x] = t0 + 4 * g4 + x < lim ? s[x] * p.scale : -__builtin_inff();
+        mx = fmaxf(mx, s[x]);
+      }
+      mx = max_xor32(max_xor16(mx));
+      const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.f : mn, al = exp2_(m - ms);
+      m = mn;
+      l *= al;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        s[x] = exp2_(s[x] - ms);
+        l += s[x];
+      }
+#pragma unroll 1
+      for (int d = 0; d < DH; d += 16) *reinterpret_cast<f32x4*>(sum + d) *= al;
+#pragma unroll 1
+      for (int tk = 0; tk < min(16, end - t0); ++tk) {  // lane group tk / 4 holds its weights
+        const float mine = tk % 4 == 0 ? s[0] : tk % 4 == 1 ? s[1] : tk % 4 == 2 ? s[2] : s[3];
+        const float pv = __shfl(mine, 16 * (tk / 4) + l16, kWave);
+        const int64_t meta = (static_cast<int64_t>(pg) << c.shift) + row + tk;
+        const uint32_t mk = c.mask[meta] & gm, slot = static_cast<uint32_t>(c.slot[meta]);
+        if (t0 + tk >= lim) continue;
+#pragma unroll 1
+        for (int x = 0; x < DH / 4; ++x) {
+          const int d = x / 4 * 16 + x % 4, g = (d + 4 * g4) / c.ds;
+          const uint32_t sl = slot + __popc(mk & ((1u << g) - 1u));
+          if (((mk >> g) & 1u) && sl < static_cast<uint32_t>(c.vcap))
+            sum[d] += pv * tof(static_cast<const T*>(c.V)[(head * c.vcap + sl) * c.ds + (d + 4 * g4) % c.ds]);
+        }
+      }
+    }
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) acc[mb] = *reinterpret_cast<f32x4*>(sum + 16 * mb);
+}
+
 // One split of one key head and 16 * WR rows: wave w takes row block w % WR and every
 // (4 / WR)-th tile of tokens. Nothing is shared between the waves until their sums
 // are added, so no wave waits for another: each loads its next tile's keys and
@@ -144,16 +239,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   const int r = (rtile * WR + w % WR) * 16 + l16;
   int lim = 0;
   u32x4 qf[KS];
-#pragma unroll
-  for (int j = 0; j < KS; ++j) qf[j] = u32x4{0, 0, 0, 0};
-  if (r < p.R) {
-    const int jq = r / p.rep, hq = h * p.rep + r % p.rep;
-    lim = p.visible ? min(len, max(p.visible[static_cast<int64_t>(b) * p.Tq + jq], 0)) : len;
-    const T* q = static_cast<const T*>(p.q) + (static_cast<int64_t>(b) * p.Tq + jq) * p.q_stride +
-                 static_cast<int64_t>(hq) * DH;
-#pragma unroll
-    for (int j = 0; j < KS; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + (4 * j + g4) * EP);
-  }
+  load_query<T, DH>(p, b, h, r, g4, qf);
+  if (r < p.R) lim = p.visible ? min(len, max(p.visible[static_cast<int64_t>(b) * p.Tq + r / p.rep], 0)) : len;
   int top = lim;
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor(top, o, kWave));
@@ -175,17 +262,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   u32x2* rec = s_rec[w];
   float* px = p.x ? p.x + ((static_cast<int64_t>(b) * c.H + h) * p.R + r) * p.x_ld : nullptr;
 
-  float m, l;
+  float m = -__builtin_inff(), l = 0.f;
   f32x4 acc[MB];
-  // The second round runs only where the first one's sums are not finite: it adds
-  // token by token, so that an infinity or NaN in a value reaches the rows that
-  // see its token and no other (a matrix product multiplies it by their zeros).
-#pragma unroll 1
-  for (int round = 0; round < 2; ++round) {
-    m = -__builtin_inff();
-    l = 0.f;
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0, 0, 0, 0};
+  for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0, 0, 0, 0};
+  {
     int pgs = -1;     // lane j: the page of block j % NB of the (j / NB)-th of TPP tiles
     int pg1[NB];      // pages of the next tile, whose masks and slots are on their way
     uint32_t mk1 = 0;
@@ -266,15 +347,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       for (int nb = 0; nb < NB; ++nb) {
         s[nb] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          if constexpr (L::kBf16) {
-            s[nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, kf[nb][j]), __builtin_bit_cast(bf16x8, qf[j]), s[nb]);
-          } else {
-            const f32x4 a = __builtin_bit_cast(f32x4, kf[nb][j]), q = __builtin_bit_cast(f32x4, qf[j]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) s[nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[x], q[x], s[nb], 0, 0, 0);
-          }
-        }
+        for (int j = 0; j < KS; ++j) s[nb] = score_step<T>(kf[nb][j], qf[j], s[nb]);
       }
       // the tile's kept groups into their places, dropped ones as zeros
 #pragma unroll
@@ -316,59 +389,41 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
           s[nb][x] = exp2_(s[nb][x] - ms);
           l += s[nb][x];
         }
-      if (round == 0) {
-        if constexpr (L::kBf16) {
-          // weights as two bf16 each, so that their rounding stays below the output's
-          bf16x8 hi, lo;
+      if constexpr (L::kBf16) {
+        // weights as two bf16 each, so that their rounding stays below the output's
+        bf16x8 hi, lo;
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const float pv = s[x / 4][x % 4];
-            hi[x] = fromf<bf16>(pv);
-            lo[x] = fromf<bf16>(pv - tof(hi[x]));
-          }
-          const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
+        for (int x = 0; x < 8; ++x) {
+          const float pv = s[x / 4][x % 4];
+          hi[x] = fromf<bf16>(pv);
+          lo[x] = fromf<bf16>(pv - tof(hi[x]));
+        }
+        const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
 #pragma unroll
-          for (int mb = 0; mb < MB; ++mb) {
-            const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
-            const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-            acc[mb] = mfma_16x16x32(a, hi, acc[mb]);
-            acc[mb] = mfma_16x16x32(a, lo, acc[mb]);
-          }
-        } else {
-#pragma unroll
-          for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const float a = *reinterpret_cast<const float*>(zt + (4 * g4 + x) * L::ZLD + 4 * (16 * mb + l16));
-              acc[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][x], acc[mb], 0, 0, 0);
-            }
+        for (int mb = 0; mb < MB; ++mb) {
+          const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
+          const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+          acc[mb] = mfma_16x16x32(a, hi, acc[mb]);
+          acc[mb] = mfma_16x16x32(a, lo, acc[mb]);
         }
       } else {
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q)  // tokens 4q + x of each block: lane group q holds their weights
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
+        for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int tk = 16 * nb + 4 * q + x;
-              const T* z = reinterpret_cast<const T*>(zt + tk * L::ZLD);
-              const float pv = __shfl(s[nb][x], 16 * q + l16, kWave);
-              if (t0 + tk < lim)
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                  for (int y = 0; y < 4; ++y) acc[mb][y] += pv * tof(z[16 * mb + 4 * g4 + y]);
-            }
+          for (int x = 0; x < 4; ++x) {
+            const float a = *reinterpret_cast<const float*>(zt + (4 * g4 + x) * L::ZLD + 4 * (16 * mb + l16));
+            acc[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][x], acc[mb], 0, 0, 0);
+          }
       }
       wave_lds_order();
     }
-    bool bad = false;
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
-    if (!__any(bad)) break;
   }
+  bool bad = false;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
+  if (__any(bad)) one_by_one<T, DH>(p, b, h, r, first, STEP, end, lim, zt, m, l, acc);
 
   // the sums of the waves of one row block, in their order
   l = add_xor32(add_xor16(l));
