@@ -54,57 +54,92 @@ __device__ __forceinline__ int tokens_of(const DecodeParams& p, int b) {
   return static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
 }
 
+// Waits until a matrix product's result may be read by other instructions. The
+// compiler spaces them within a block; where a branch followed the product and the
+// read came first after the join, it left the read too early (stale values of the
+// first element read, in a build with the rotation optional inside one function).
+// Placed after products that end a block.
+template <int N>
+__device__ __forceinline__ void settle(f32x4 (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+  asm volatile("s_nop 15" : "+v"(x[0]));
+#pragma unroll
+  for (int i = 1; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
+// R_h's rows for the matrix cores: wave w's blocks of 16 output dims, w, w + 4, ...
+template <class T, int DH>
+struct Rotation {
+  using L = Tile<T, DH>;
+  static constexpr int N = L::MB / 4;
+  u32x4 a[N][L::KS];
+  __device__ __forceinline__ void load(const DecodeParams& p, int h) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
+    if (!p.Rm) return;
+    const T* R = static_cast<const T*>(p.Rm) + (static_cast<int64_t>(h) * DH + 16 * w + l16) * DH + g4 * L::EP;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < L::KS; ++j) a[i][j] = *reinterpret_cast<const u32x4*>(R + 64 * i * DH + 4 * j * L::EP);
+  }
+};
+
 // Output rows [r0, r0 + 16) of key head h from their normalised sums u (LDS, rows of
 // RLD floats; rows past R are zero): out = R_h u on the matrix cores, R's rows as
 // the product's rows. The sums enter as two bf16 each (their rounding stays below
 // the output's), or in f32. All 256 threads.
 template <class T, int DH>
-__device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h, int r0, const float* u) {
+__device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h, int r0, const float* u,
+                                            const Rotation<T, DH>& rot) {
   using L = Tile<T, DH>;
-  constexpr int KS = L::KS, EP = L::EP;
+  constexpr int KS = L::KS, EP = L::EP, N = L::MB / 4;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
   const int r = r0 + l16;
   const float* ur = u + l16 * L::RLD;
+  f32x4 o[N];
+  if (p.Rm) {
 #pragma unroll
-  for (int mb = w; mb < L::MB; mb += 4) {
-    f32x4 o = {0, 0, 0, 0};
-    if (p.Rm) {
-      const T* Rr = static_cast<const T*>(p.Rm) + (static_cast<int64_t>(h) * DH + 16 * mb + l16) * DH;
+    for (int i = 0; i < N; ++i) o[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < KS; ++j) {
-        const int d = (4 * j + g4) * EP;
-        const u32x4 a = *reinterpret_cast<const u32x4*>(Rr + d);
-        if constexpr (L::kBf16) {
-          bf16x8 hi, lo;
+    for (int j = 0; j < KS; ++j) {
+      const int d = (4 * j + g4) * EP;
+      if constexpr (L::kBf16) {
+        bf16x8 hi, lo;
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            hi[x] = fromf<bf16>(ur[d + x]);
-            lo[x] = fromf<bf16>(ur[d + x] - tof(hi[x]));
-          }
-          o = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), hi, o);
-          o = mfma_16x16x32(__builtin_bit_cast(bf16x8, a), lo, o);
-        } else {
-          const f32x4 af = __builtin_bit_cast(f32x4, a);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) o = __builtin_amdgcn_mfma_f32_16x16x4f32(af[x], ur[d + x], o, 0, 0, 0);
+        for (int x = 0; x < 8; ++x) {
+          hi[x] = fromf<bf16>(ur[d + x]);
+          lo[x] = fromf<bf16>(ur[d + x] - tof(hi[x]));
         }
-      }
-    } else {
-      o = *reinterpret_cast<const f32x4*>(ur + 16 * mb + 4 * g4);
-    }
-    if (r < p.R) {
-      const int64_t at = ((static_cast<int64_t>(b) * p.Tq + r / p.rep) * p.Hq + h * p.rep + r % p.rep) * DH + 16 * mb + 4 * g4;
-      if (p.out_f32) {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = o;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          o[i] = mfma_16x16x32(__builtin_bit_cast(bf16x8, rot.a[i][j]), hi, o[i]);
+          o[i] = mfma_16x16x32(__builtin_bit_cast(bf16x8, rot.a[i][j]), lo, o[i]);
+        }
       } else {
-        T* y = static_cast<T*>(p.out) + at;
-        if constexpr (L::kBf16) {
-          const u32x2 v = {pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
-          *reinterpret_cast<u32x2*>(y) = v;
-        } else {
-          *reinterpret_cast<f32x4*>(y) = o;
+        const f32x4 uf = *reinterpret_cast<const f32x4*>(ur + d);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const f32x4 af = __builtin_bit_cast(f32x4, rot.a[i][j]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(af[x], uf[x], o[i], 0, 0, 0);
         }
       }
+    }
+    settle(o);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = *reinterpret_cast<const f32x4*>(ur + 16 * (w + 4 * i) + 4 * g4);
+  }
+  if (r >= p.R) return;
+  const int64_t at = ((static_cast<int64_t>(b) * p.Tq + r / p.rep) * p.Hq + h * p.rep + r % p.rep) * DH + 16 * w + 4 * g4;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (p.out_f32 || !L::kBf16) {
+      *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at + 64 * i) = o[i];
+    } else {
+      const u32x2 v = {pack_bf16x2(o[i][0], o[i][1]), pack_bf16x2(o[i][2], o[i][3])};
+      *reinterpret_cast<u32x2*>(static_cast<T*>(p.out) + at + 64 * i) = v;
     }
   }
 }
@@ -274,25 +309,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     u32x4 kf[NB][KS], vf[NVI];
     bool there[NB], there1[NB];
 
-    auto request_meta = [&](int i) {
-      const int t0 = first + i * STEP;
-      if (i % TPP == 0) {
-        const int t = t0 + lane / NB * STEP + lane % NB * 16;
-        const int v = static_cast<int>(bload4(r_table, oob_unless(t < end, static_cast<uint32_t>(t >> shift) * 4u)));
-        pgs = t < end && static_cast<uint32_t>(v) < static_cast<uint32_t>(c.n_pages) ? v : -1;
-      }
+    // pages of tiles i .. i + TPP - 1
+    auto request_pages = [&](int i) {
+      const int t = first + i * STEP + lane / NB * STEP + lane % NB * 16;
+      pgs = static_cast<int>(bload4(r_table, static_cast<uint32_t>(t >> shift) * 4u));  // past the row: 0
+    };
+    auto take_pages = [&](int i) {  // of tile i, pages that are none as -1
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) pg1[nb] = __builtin_amdgcn_readlane(pgs, i % TPP * NB + nb);
-      const int t = t0 + lane, pg = NB == 2 && lane >= 16 ? pg1[NB - 1] : pg1[0];
+      for (int nb = 0; nb < NB; ++nb) {
+        const int t = first + i * STEP + 16 * nb, v = __builtin_amdgcn_readlane(pgs, i % TPP * NB + nb);
+        pg1[nb] = t < end && static_cast<uint32_t>(v) < static_cast<uint32_t>(c.n_pages) ? v : -1;
+      }
+    };
+    auto request_meta = [&](int i) {  // of the pages pg1
+      const int t = first + i * STEP + lane, pg = NB == 2 && lane >= 16 ? pg1[NB - 1] : pg1[0];
       const uint32_t off = oob_unless(lane < TK && t < end && pg >= 0,
                                       (static_cast<uint32_t>(pg) << (shift + 2)) + static_cast<uint32_t>(t & pmask) * 4u);
       mk1 = bload4(r_mask, off);
       sl1 = static_cast<int>(bload4(r_slot, off));
     };
-    auto request_tile = [&](int i) {  // of the pages pg1
+    auto request_keys = [&](int i) {
       const int t0 = first + i * STEP;
-      if (lane < TK) rec[lane] = u32x2{mk1 & gm, static_cast<uint32_t>(sl1)};
-      wave_lds_order();
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         there1[nb] = pg1[nb] >= 0;
@@ -303,27 +340,34 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 #pragma unroll
         for (int j = 0; j < KS; ++j) kf[nb][j] = bload16(rk, ko + 64 * j);
       }
+    };
+    auto request_values = [&]() {
+      if (lane < TK) rec[lane] = u32x2{mk1 & gm, static_cast<uint32_t>(sl1)};
+      wave_lds_order();
+      u32x2 tk[NVI];
+#pragma unroll
+      for (int x = 0; x < NVI; ++x) tk[x] = rec[x * L::TPI + vt];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const int64_t at = static_cast<int64_t>(max(pg1[nb], 0)) * c.H + h;
         const rsrc_t rv = make_rsrc(static_cast<const char*>(c.V) + at * vstep,
                                     there1[nb] ? static_cast<uint32_t>(vstep) : 0u);
 #pragma unroll
-        for (int i2 = nb * NVI / NB; i2 < (nb + 1) * NVI / NB; ++i2) {
-          const u32x2 t = rec[i2 * L::TPI + vt];
+        for (int x = nb * NVI / NB; x < (nb + 1) * NVI / NB; ++x) {
+          const u32x2 t = tk[x];
           uint32_t sl = t.y + __popc(t.x & ((1u << vg) - 1u));
           if constexpr (SUB == 1) {
-            vf[i2] = bload16(rv, ((t.x >> vg) & 1u) && sl < static_cast<uint32_t>(c.vcap) ? sl * gb + vin : kOOB);
+            vf[x] = bload16(rv, ((t.x >> vg) & 1u) && sl < static_cast<uint32_t>(c.vcap) ? sl * gb + vin : kOOB);
           } else {
-            uint32_t* vv = reinterpret_cast<uint32_t*>(&vf[i2]);
+            uint32_t* vv = reinterpret_cast<uint32_t*>(&vf[x]);
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
               const bool on = (t.x >> (vg + u)) & 1u;
               const uint32_t off = on && sl < static_cast<uint32_t>(c.vcap) ? sl * gb : kOOB;
               if constexpr (SUB == 2) {
-                const u32x2 x = bload8(rv, off);
-                vv[2 * u] = x.x;
-                vv[2 * u + 1] = x.y;
+                const u32x2 y = bload8(rv, off);
+                vv[2 * u] = y.x;
+                vv[2 * u + 1] = y.y;
               } else {
                 vv[u] = bload4(rv, off);
               }
@@ -333,11 +377,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
         }
       }
     };
+    auto next_pages = [&](int i) {
+      if (i % TPP == 0) request_pages(i);
+      take_pages(i);
+    };
 
+    request_pages(0);  // before the lengths are looked at
+    take_pages(0);
     request_meta(0);
-    request_tile(0);
+    request_keys(0);
+    request_values();
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) there[nb] = there1[nb];
+    next_pages(1);
     request_meta(1);
 #pragma unroll 1
     for (int i = 0, t0 = first; t0 < end; ++i, t0 += STEP) {
@@ -356,9 +408,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       bool now[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) now[nb] = there[nb];
-      request_tile(i + 1);
+      request_keys(i + 1);
+      request_values();
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) there[nb] = there1[nb];
+      next_pages(i + 2);
       request_meta(i + 2);
       // softmax against the running maximum
       float mx = -__builtin_inff();
@@ -416,6 +470,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
           }
       }
       wave_lds_order();
+      settle(acc);
     }
   }
   bool bad = false;
@@ -425,6 +480,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
   if (__any(bad)) one_by_one<T, DH>(p, b, h, r, first, STEP, end, lim, zt, m, l, acc);
 
+  Rotation<T, DH> rot;
+  if (p.n_split == 1) rot.load(p, h);
   // the sums of the waves of one row block, in their order
   l = add_xor32(add_xor16(l));
   if (g4 == 0) {
@@ -475,7 +532,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 #pragma unroll 1
     for (int rb = 0; rb < WR; ++rb) {
       const int r0 = (rtile * WR + rb) * 16;
-      if (r0 < p.R) finish_rows<T, DH>(p, b, h, r0, red + rb * 16 * RLD);
+      if (r0 < p.R) finish_rows<T, DH>(p, b, h, r0, red + rb * 16 * RLD, rot);
     }
   }
 }
@@ -501,6 +558,8 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
   const PagedCache& c = p.c;
   const int nrb = (p.R + 15) / 16, tid = threadIdx.x;
   const int r0 = static_cast<int>(blk % nrb) * 16, h = static_cast<int>(blk / nrb % c.H), b = static_cast<int>(blk / nrb / c.H);
+  Rotation<T, DH> rot;
+  rot.load(p, h);
   const int ns = (tokens_of(p, b) + p.chunk - 1) / p.chunk, nr = min(16, p.R - r0);
   const int64_t cell0 = ((static_cast<int64_t>(b) * c.H + h) * p.R + r0) * p.n_split;
   {
@@ -539,43 +598,51 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
     *reinterpret_cast<f32x4*>(u + row * L::RLD + 4 * d) = s_M[16 + row] == 0.f ? f32x4{0, 0, 0, 0} : a * s_M[16 + row];
   }
   __syncthreads();
-  finish_rows<T, DH>(p, b, h, r0, u);
+  finish_rows<T, DH>(p, b, h, r0, u, rot);
 }
 
-// mass_out[b,t] = decay mass_in[b,t] + the token's weight in every row: 256 tokens,
-// the rows in batches whose sums of exponentials every workgroup takes for itself.
-constexpr int kMassRows = 512;
+// mass_out[b,t] = decay mass_in[b,t] + the token's weight in every row. A workgroup
+// takes 64 tokens, its four waves a quarter of the rows each, in batches whose sums
+// of exponentials it takes for itself while the scores are on their way.
+constexpr int kMassRows = 32;
 __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int nblk, char* smem) {
+  constexpr int M4 = kMassRows / 4;
   float* s_lse = reinterpret_cast<float*>(smem);
   int* s_lim = reinterpret_cast<int*>(smem + kMassRows * 4);
+  float* s_sum = reinterpret_cast<float*>(smem + kMassRows * 8);
   const PagedCache& c = p.c;
-  const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, t = static_cast<int>(blk % nblk) * 256 + tid;
-  const int len = tokens_of(p, b);
-  if (t - tid >= len) return;
-  const int ns = (len + p.chunk - 1) / p.chunk;
+  const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int t0 = static_cast<int>(blk % nblk) * 64, t = t0 + lane, len = tokens_of(p, b);
+  if (t0 >= len) return;
+  const int ns = (len + p.chunk - 1) / p.chunk, tr = min(t, p.x_ld - 1);
   const int64_t rows = static_cast<int64_t>(c.H) * p.R, row0 = b * rows;
   float sum = 0.f;
   for (int64_t q0 = 0; q0 < rows; q0 += kMassRows) {
     const int n = static_cast<int>(min(rows - q0, static_cast<int64_t>(kMassRows)));
+    float x[M4];
+#pragma unroll
+    for (int i = 0; i < M4; ++i) x[i] = p.x[(row0 + q0 + min(4 * i + w, n - 1)) * p.x_ld + tr];
     __syncthreads();
-    for (int q = tid / 16; q < n; q += 16) {
+    // 8 lanes a row
+    {
+      const int q = tid / 8;
       float M, l;
-      join_stat(p.stat + 2 * (row0 + q0 + q) * p.n_split, ns, tid % 16, 16, M, l);
-      if (tid % 16 == 0) {
+      join_stat(p.stat + 2 * (row0 + q0 + min(q, n - 1)) * p.n_split, ns, tid % 8, 8, M, l);
+      if (tid % 8 == 0) {
         s_lse[q] = M + __log2f(l);  // -inf where nothing was seen
-        s_lim[q] = l == 0.f ? 0
-                   : p.visible ? p.visible[static_cast<int64_t>(b) * p.Tq + (q0 + q) % p.R / p.rep] : len;
+        s_lim[q] = l == 0.f || q >= n ? 0
+                   : p.visible        ? p.visible[static_cast<int64_t>(b) * p.Tq + (q0 + q) % p.R / p.rep]
+                                      : len;
       }
     }
     __syncthreads();
-    if (t < len)
-#pragma unroll 8
-      for (int q = 0; q < n; ++q) {
-        const float x = p.x[(row0 + q0 + q) * p.x_ld + t];
-        sum += t < s_lim[q] ? exp2_(x - s_lse[q]) : 0.f;
-      }
+#pragma unroll
+    for (int i = 0; i < M4; ++i) sum += t < s_lim[4 * i + w] ? exp2_(x[i] - s_lse[4 * i + w]) : 0.f;
   }
-  if (t < len) {
+  s_sum[tid] = sum;
+  __syncthreads();
+  if (w == 0 && t < len) {
+    sum = (sum + s_sum[64 + lane]) + (s_sum[128 + lane] + s_sum[192 + lane]);
     const int64_t at = static_cast<int64_t>(b) * p.mass_ld + t;
     p.mass_out[at] = p.mass_in ? p.decay * p.mass_in[at] + sum : sum;
   }
@@ -586,8 +653,8 @@ __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int
 template <class T, int DH>
 __global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nblk) {
   using L = Tile<T, DH>;
-  constexpr int S = L::RB + 4096 + 128;
-  __shared__ __attribute__((aligned(16))) char smem[S > kMassRows * 8 ? S : kMassRows * 8];
+  __shared__ __attribute__((aligned(16))) char smem[L::RB + 4096 + 128];
+  static_assert(sizeof(smem) >= kMassRows * 8 + 1024, "both halves fit");
   if (static_cast<int>(blockIdx.x) < joins)
     join_rows<T, DH>(p, blockIdx.x, smem);
   else
@@ -616,14 +683,14 @@ hipError_t launch(const DecodeParams& p, hipStream_t s) {
     go<T, DH, 2>(p, s);
   else
     go<T, DH, 4>(p, s);
-  const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0, nblk = p.mass_out ? (p.max_len + 255) / 256 : 0;
+  const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0, nblk = p.mass_out ? (p.max_len + 63) / 64 : 0;
   if (joins + nblk > 0)
     hipLaunchKernelGGL((k_join<T, DH>), dim3(static_cast<unsigned>(joins) + static_cast<unsigned>(nblk) * p.B), dim3(256),
                        0, s, p, joins, nblk);
   return hipGetLastError();
 }
 
-constexpr int64_t kSplitWgs = 2048;  // workgroups that the splits are made for
+constexpr int64_t kSplitWgs = 512;  // workgroups that the splits are made for
 constexpr int64_t kMaxSplits = 256;  // that k_join adds up
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }

@@ -1073,7 +1073,7 @@ rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dt
                 workspace ? ws_bytes : static_cast<size_t>(0));
   if (!aligned(workspace, 16)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace must lie on 16 bytes", fn);
   if (static_cast<size_t>(B) * p.c.H * d.n_split * ((p.R + 15) / 16) * 256 >= kMaxThreads ||
-      (static_cast<size_t>(B) * p.c.H * ((p.R + 15) / 16) + static_cast<size_t>(B) * (p.max_len / 256 + 1)) * 256 >= kMaxThreads)
+      (static_cast<size_t>(B) * p.c.H * ((p.R + 15) / 16) + static_cast<size_t>(B) * (p.max_len / 64 + 1)) * 256 >= kMaxThreads)
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads or queries", fn);
   char* ws = static_cast<char*>(workspace);
   p.n_split = d.n_split;
