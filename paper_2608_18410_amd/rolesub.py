@@ -687,39 +687,73 @@ def attend_values(q, k, V, scale: float = 0.0, out_dtype=None, out=None, stream=
 # Paged routed cache: positions, append, attention of new tokens, eviction
 # ----------------------------------------------------------------------------
 
-def _here(stream, *ts):
-    """The stream handle of a call on these tensors, which all lie on the current
-    device (the library launches there)."""
+def _current():
+    """The current device's index (-1 without one)."""
+    try:
+        return torch.cuda.current_device() if _raw_device is None else _raw_device()
+    except (RuntimeError, AssertionError):
+        return -1
+
+
+def _args(stream, spec, *caches):
+    """Addresses of the tensors of spec, (name, tensor or None, shape, dtype) each, and
+    the stream's handle. All lie dense on the current device (the library launches
+    there), the caches too; what fails the short way is looked at in detail, shapes
+    before devices."""
+    cur, out, n = _current(), [], len(spec)
+    for c in caches:
+        if c._ready != cur:
+            spec = c.spec() + tuple(spec)
+    for _, t, shape, dtype in spec:
+        if t is None:
+            out.append(None)
+        elif isinstance(t, _Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == cur and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            break
+    else:
+        if cur >= 0 and (stream is None or stream.device_index == cur):
+            for c in caches:
+                if c._ready != cur:
+                    object.__setattr__(c, "_ready", cur)
+            return out[len(out) - n:], _stream(stream)
+    for name, t, shape, dtype in spec:
+        _need(name, t, shape, dtype)
+    out = [_ptr(t) for _, t, _, _ in spec]
+    _on_current(cur, stream, [t for _, t, _, _ in spec])
+    for c in caches:
+        object.__setattr__(c, "_ready", cur)
+    return out[len(out) - n:], _stream(stream)
+
+
+def _on_current(cur, stream, ts):
     _same_device(*ts)
     for t in ts:
-        if isinstance(t, _Tensor):
-            if t.is_cuda:
-                cur = torch.cuda.current_device() if _raw_device is None else _raw_device()
-                if t.device.index != cur:
-                    raise ValueError(f"tensors on {t.device}, but the current device is cuda:{cur}")
-                if stream is not None and stream.device.index != cur:
-                    raise ValueError(f"tensors on {t.device}, but the stream is on {stream.device}")
-            break
-    return _stream(stream) if torch.cuda.is_available() else None
+        if t is not None and t.get_device() != cur:
+            raise ValueError(f"tensors on {t.device}, but the current device is cuda:{cur}")
+    if stream is not None and stream.device_index != cur:
+        raise ValueError(f"the stream is on cuda:{stream.device_index}, but the current device is cuda:{cur}")
 
 
-def _tokens(name, t):
-    """Address and token stride of a [B, T, H, dh] operand whose tokens lie at one
-    stride (dense, or a view of a fused projection)."""
-    if not t.is_cuda:
-        raise ValueError("librolesub takes device tensors only")
-    B, T, H, dh = t.shape
+def _rows(name, t):
+    """Token stride of a [B, T, H, dh] operand whose tokens lie at one stride (dense,
+    or a view of a fused projection), and a dense stand-in for _args: the operand
+    itself, or one row of it, which shares its address, type and device."""
     if t.is_contiguous():
-        return t.data_ptr(), H * dh
+        return t.shape[2] * t.shape[3], t
+    B, T, H, dh = t.shape
     sb, st, sh, sd = t.stride()
     if T == 1:
         st = sb if B > 1 else H * dh
     if (sd != 1 and dh > 1) or (sh != dh and H > 1) or (B > 1 and sb != T * st):
         raise ValueError(f"{name}: heads and dims must be dense and tokens at one stride, got strides {list(t.stride())}")
-    return t.data_ptr(), st
+    return st, t[0, 0, 0]
 
 
-@dataclass
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+@dataclass(frozen=True)
 class PagedCache:
     """Pages of a growing routed cache (kept alive while calls are in flight):
     K [n_pages,H,page,dh], V [n_pages,H,vcap,dh/G], mask and slot [n_pages,page]
@@ -728,6 +762,22 @@ class PagedCache:
     V: torch.Tensor
     mask: torch.Tensor
     slot: torch.Tensor
+
+    def __post_init__(self):
+        _need("K", self.K, (None, None, None, None), _FLOATS)
+        n, H, page, dh = self.K.shape
+        _need("V", self.V, (n, H, None, None), self.K.dtype)
+        ds = self.V.shape[3]
+        if ds < 1 or dh % ds:
+            raise ValueError(f"V: groups of {ds} dims do not divide heads of {dh}")
+        _need("mask", self.mask, (n, page), _MASK)
+        _need("slot", self.slot, (n, page), torch.int32)
+        put = object.__setattr__
+        put(self, "G", dh // ds)
+        # the library's description of the cache, made once
+        put(self, "_desc", PagesDesc(n, page, self.V.shape[2], H, dh, dh // ds, None, None, None, None))
+        put(self, "_at", None)
+        put(self, "_ready", None)  # the device its arrays were found dense on
 
     @staticmethod
     def allocate(n_pages, page, H, dh, G, vcap, dtype, device="cuda") -> "PagedCache":
@@ -738,27 +788,24 @@ class PagedCache:
                           mask=torch.empty((n_pages, page), dtype=torch.int32, device=device),
                           slot=torch.empty((n_pages, page), dtype=torch.int32, device=device))
 
-    @property
-    def G(self) -> int:
-        return self.K.shape[3] // max(self.V.shape[3], 1)
+    def spec(self):
+        return tuple((n, t, t.shape, t.dtype) for n, t in zip(("K", "V", "mask", "slot"), self.tensors()))
 
-    def check(self, name="cache") -> None:
-        _need(f"{name}.K", self.K, (None, None, None, None), (torch.float32, torch.bfloat16))
-        n, H, page, dh = self.K.shape
-        _need(f"{name}.V", self.V, (n, H, None, None), self.K.dtype)
-        ds = self.V.shape[3]
-        if ds < 1 or dh % ds:
-            raise ValueError(f"{name}: groups of {ds} dims do not divide heads of {dh}")
-        _need(f"{name}.mask", self.mask, (n, page), _MASK)
-        _need(f"{name}.slot", self.slot, (n, page), torch.int32)
-
-    def desc(self) -> PagesDesc:
-        n, H, page, dh = self.K.shape
-        return PagesDesc(n, page, self.V.shape[2], H, dh, self.G, _ptr(self.K), _ptr(self.V), _ptr(self.mask),
-                         _ptr(self.slot))
+    def desc(self):
+        """The description with the arrays' present addresses."""
+        d, at = self._desc, (self.K.data_ptr(), self.V.data_ptr(), self.mask.data_ptr(), self.slot.data_ptr())
+        if at != self._at:
+            d.K, d.V, d.mask, d.slot = at
+            object.__setattr__(self, "_at", at)
+        return ctypes.byref(d)
 
     def tensors(self):
         return self.K, self.V, self.mask, self.slot
+
+
+def _width(t):
+    """Columns of a matrix argument for its spec (None sends it to the detailed check)."""
+    return t.shape[1] if isinstance(t, _Tensor) and t.dim() == 2 else None
 
 
 def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=False, out=None, stream=None):
@@ -768,71 +815,71 @@ def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=Fals
     some = q if q is not None else k
     if some is None:
         raise ValueError("q and k are both None")
-    _need("q" if q is not None else "k", some, (None, None, None, None), (torch.float32, torch.bfloat16))
-    B, T, _, dh = some.shape
+    _need("q" if q is not None else "k", some, (None, None, None, None), _FLOATS)
+    B, T, H, dh = some.shape
     dt = some.dtype
-    A = 1
+    spec, A, n = [], 1, None
     if isinstance(positions, _Tensor) and positions.dim() == 3:
         A = positions.shape[2]
-        _need("positions", positions, (B, T, None), torch.int32)
+        spec.append(("positions", positions, (B, T, A), torch.int32))
     else:
-        _need("positions", positions, (B, T), torch.int32)
-    _need("inv_freq", inv_freq, (None,), torch.float32)
-    n = inv_freq.shape[0]
-    _need("axis", axis, (n,), torch.uint8)
+        spec.append(("positions", positions, (B, T), torch.int32))
+    if isinstance(inv_freq, _Tensor) and inv_freq.dim() == 1:
+        n = inv_freq.shape[0]
+    spec.append(("inv_freq", inv_freq, (n,), torch.float32))
+    spec.append(("axis", axis, (n,), torch.uint8))
     qo, ko = (None, None) if out is None else out
-    for name, x, o in (("q", q, qo), ("k", k, ko)):
-        _need(name, x, (B, T, None, dh), dt)
-        if x is not None:
-            _need(f"{name}_out", o, tuple(x.shape), dt)
-    args = []
-    for name, x, o in (("q", q, qo), ("k", k, ko)):
+    heads, strides, outs = [0, 0], [0, 0], [qo, ko]
+    for i, (name, x) in enumerate((("q", q), ("k", k))):
+        o = outs[i]
         if x is None:
-            args += [None, 0, None, 0]
+            outs[i] = None
+            spec += [(name, None, None, None)] * 2
             continue
-        p, st = _tokens(name, x)
+        if x is not some:
+            _need(name, x, (B, T, None, dh), dt)
+        heads[i] = x.shape[2]
+        strides[i], row = _rows(name, x)
         if o is None:
-            o = torch.empty((B, T, x.shape[2], dh), dtype=dt, device=x.device)
-            po = o.data_ptr()
+            o = outs[i] = torch.empty_like(x) if row is x else torch.empty(x.shape, dtype=dt, device=x.device)
+            orow = o
         else:
-            po, so = _tokens(f"{name}_out", o)
-            if so != (st if po == p else x.shape[2] * dh):
+            _need(f"{name}_out", o, x.shape, dt)
+            so, orow = _rows(f"{name}_out", o)
+            if orow is not o and (so != strides[i] or o.data_ptr() != x.data_ptr()):
                 raise ValueError(f"{name}_out: must be {name} itself or contiguous")
-        args += [p, st, po, x.shape[2]]
-        qo, ko = (o, ko) if name == "q" else (qo, o)
-    s = _here(stream, some, q, k, positions, inv_freq, axis, qo, ko)
+            if orow is o and o.data_ptr() == x.data_ptr() and row is not x and o.numel():
+                raise ValueError(f"{name}_out: must be {name} itself or lie apart from it")
+        spec += [(name, row, row.shape, dt), (f"{name}_out", orow, orow.shape, dt)]
+    (pp, pf, pa, pq, pqo, pk, pko), s = _args(stream, spec)
     _check("rolesub_rotary", load().rolesub_rotary(
-        B, T, args[3], args[7], dh, _code(some), args[0], args[1], args[4], args[5], _ptr(positions), A,
-        _ptr(inv_freq), _ptr(axis), n, 1 if interleaved else 0, 1 if inverse else 0, args[2], args[6], s))
-    return (qo if q is not None else None), (ko if k is not None else None)
+        B, T, heads[0], heads[1], dh, _code(some), pq, strides[0], pk, strides[1], pp, A, pf, pa, n,
+        1 if interleaved else 0, 1 if inverse else 0, pqo, pko, s))
+    return outs[0], outs[1]
 
 
 def cache_append(cache: PagedCache, k, z, mask, table, lens, n_new=None, stream=None) -> PagedCache:
     """Token j of sequence b (j < n_new[b], or all) becomes token lens[b] + j of its
     pages: k and z [B,T,H,dh], mask [B,T]; table [B,max_pages], lens [B] int32."""
-    cache.check()
-    H, dh = cache.K.shape[1], cache.K.shape[3]
-    _need("k", k, (None, None, H, dh), cache.K.dtype)
+    _, H, _, dh = cache.K.shape
+    dt = cache.K.dtype
+    _need("k", k, (None, None, H, dh), dt)
     B, T = k.shape[:2]
-    _need("z", z, (B, T, H, dh), cache.K.dtype)
-    _need("mask", mask, (B, T), _MASK)
-    _need("table", table, (B, None), torch.int32)
-    _need("lens", lens, (B,), torch.int32)
-    _need("n_new", n_new, (B,), torch.int32)
-    pk, sk = _tokens("k", k)
-    pz, sz = _tokens("z", z)
-    s = _here(stream, k, z, mask, table, lens, n_new, *cache.tensors())
-    desc = cache.desc()
+    _need("z", z, k.shape, dt)
+    sk, rk = _rows("k", k)
+    sz, rz = _rows("z", z)
+    W = _width(table)
+    (pk, pz, pmask, pt, pl, pn), s = _args(stream, (
+        ("k", rk, rk.shape, dt), ("z", rz, rz.shape, dt),
+        ("mask", mask, (B, T), mask.dtype if getattr(mask, "dtype", None) in _MASK else _MASK),
+        ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32), ("n_new", n_new, (B,), torch.int32)), cache)
     _check("rolesub_cache_append", load().rolesub_cache_append(
-        ctypes.byref(desc), _code(k), B, T, pk, sk, pz, sz, _ptr(mask), _ptr(table), table.shape[1], _ptr(lens),
-        _ptr(n_new), s))
+        cache.desc(), _CODES[dt], B, T, pk, sk, pz, sz, pmask, pt, W, pl, pn, s))
     return cache
 
 
 def attend_paged_workspace_size(cache: PagedCache, B, Hq, Tq, max_len, mass=False) -> int:
-    n, H, page, dh = cache.K.shape
-    desc = PagesDesc(n, page, cache.V.shape[2], H, dh, cache.G, None, None, None, None)
-    return load().rolesub_attend_paged_workspace_size(ctypes.byref(desc), B, Hq, Tq, max_len, 1 if mass else 0)
+    return load().rolesub_attend_paged_workspace_size(ctypes.byref(cache._desc), B, Hq, Tq, max_len, 1 if mass else 0)
 
 
 def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, visible=None, max_len: int = 0,
@@ -841,36 +888,32 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
     [B,Tq,Hq,dh]. visible [B,Tq] int32: the tokens each query sees. mass [B,>=max_len]
     f32: the tokens' accumulated weight, in place or into mass_out (which alone
     starts from zero): decay * mass + the weight of this call's queries."""
-    cache.check()
-    n_pages, H, page, dh = cache.K.shape
-    _need("q", q, (None, None, None, dh), cache.K.dtype)
-    B, Tq, Hq, _ = q.shape
-    _need("table", table, (B, None), torch.int32)
-    _need("lens", lens, (B,), torch.int32)
-    _need("R", R, (H, dh, dh), q.dtype)
-    _need("visible", visible, (B, Tq), torch.int32)
-    _need("mass", mass, (B, None), torch.float32)
-    _need("out", out, (B, Tq, Hq, dh), (torch.float32, torch.bfloat16))
-    _need_workspace(workspace)
-    ld = 0
+    _, H, page, dh = cache.K.shape
+    dt = cache.K.dtype
+    _need("q", q, (None, None, None, dh), dt)
+    shape = q.shape
+    B, Tq, Hq, _ = shape
+    sq, rq = _rows("q", q)
+    W, ld = _width(table), 0
     if mass_out is None:
         mass_out = mass
     if mass_out is not None:
-        _need("mass_out", mass_out, (B, None if mass is None else mass.shape[1]), torch.float32)
-        ld = mass_out.shape[1]
-    pq, sq = _tokens("q", q)
-    o = torch.empty((B, Tq, Hq, dh), dtype=out_dtype or q.dtype, device=q.device) if out is None else out
-    whole = table.shape[1] * page
-    ml = min(int(max_len), whole) if max_len else whole
+        ld = _width(mass_out) if mass is None else _width(mass)
+    o = torch.empty(shape, dtype=out_dtype or dt, device=q.device) if out is None else out
+    odt = o.dtype if isinstance(o, _Tensor) and o.dtype in _CODES else _FLOATS
     if workspace is None:
-        need = attend_paged_workspace_size(cache, B, Hq, Tq, ml, mass_out is not None)
+        whole = (W or 0) * page
+        need = attend_paged_workspace_size(cache, B, Hq, Tq, min(int(max_len), whole) if max_len else whole,
+                                           mass_out is not None)
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
-    s = _here(stream, q, table, lens, R, visible, mass, mass_out, workspace, o, *cache.tensors())
-    desc = cache.desc()
+    ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
+    (pq, pt, pl, pR, pv, pmi, pmo, po, pw), s = _args(stream, (
+        ("q", rq, rq.shape, dt), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
+        ("R", R, (H, dh, dh), dt), ("visible", visible, (B, Tq), torch.int32), ("mass", mass, (B, ld), torch.float32),
+        ("mass_out", mass_out, (B, ld), torch.float32), ("out", o, shape, odt), ("workspace", workspace, (ws,), torch.uint8)), cache)
     _check("rolesub_attend_paged", load().rolesub_attend_paged(
-        ctypes.byref(desc), _code(q), B, Hq, Tq, pq, sq, _ptr(table), table.shape[1], _ptr(lens), _ptr(visible),
-        int(max_len), _ptr(R), float(scale), _ptr(o), _code(o), _ptr(mass), float(decay), _ptr(mass_out), ld,
-        _ptr(workspace), workspace.numel(), s))
+        cache.desc(), _CODES[dt], B, Hq, Tq, pq, sq, pt, W, pl, pv, int(max_len), pR, float(scale), po,
+        _CODES[odt], pmi, float(decay), pmo, ld, pw, ws, s))
     return o
 
 
@@ -885,23 +928,21 @@ def evict_tokens(mass, lens, keep: int, first: int = 0, recent: int = 0, max_len
     ascending, then -1; n_keep [B] int32). max_len 0: mass.shape[1]."""
     _need("mass", mass, (None, None), torch.float32)
     B, ld = mass.shape
-    _need("lens", lens, (B,), torch.int32)
-    _need_workspace(workspace)
     if out is None:
         if keep < 1:
             raise ValueError(f"keep: expected at least 1, got {keep}")
-        out = (torch.empty((B, keep), dtype=torch.int32, device=mass.device),
-               torch.empty((B,), dtype=torch.int32, device=mass.device))
+        dev = mass.device
+        out = (torch.empty((B, keep), dtype=torch.int32, device=dev), torch.empty((B,), dtype=torch.int32, device=dev))
     idx, n = out
-    _need("keep_idx", idx, (B, keep), torch.int32)
-    _need("n_keep", n, (B,), torch.int32)
     ml = int(max_len) if max_len else ld
     if workspace is None:
         workspace = torch.empty(max(evict_workspace_size(B, ml), 1), dtype=torch.uint8, device=mass.device)
-    s = _here(stream, mass, lens, idx, n, workspace)
+    ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
+    (pm, pl, pi, pn, pw), s = _args(stream, (
+        ("mass", mass, (B, ld), torch.float32), ("lens", lens, (B,), torch.int32), ("keep_idx", idx, (B, keep), torch.int32),
+        ("n_keep", n, (B,), torch.int32), ("workspace", workspace, (ws,), torch.uint8)))
     _check("rolesub_evict_tokens", load().rolesub_evict_tokens(
-        B, ml, _ptr(mass), ld, _ptr(lens), int(keep), int(first), int(recent), _ptr(idx), _ptr(n), _ptr(workspace),
-        workspace.numel(), s))
+        B, ml, pm, ld, pl, int(keep), int(first), int(recent), pi, pn, pw, ws, s))
     return idx, n
 
 
@@ -910,24 +951,19 @@ def cache_compact(src: PagedCache, table, keep_idx, n_keep, dst: PagedCache, dst
     """Token j < n_keep[b] of the pages dst_table[b] of dst becomes token
     keep_idx[b, j] of the pages table[b] of src; mass_out[b, j] = mass[b, keep_idx[b, j]]
     (a new [B, keep] tensor when mass comes alone). Returns mass_out (or None)."""
-    src.check("src")
-    dst.check("dst")
     _need("keep_idx", keep_idx, (None, None), torch.int32)
     B, keep = keep_idx.shape
-    _need("n_keep", n_keep, (B,), torch.int32)
-    _need("table", table, (B, None), torch.int32)
-    _need("dst_table", dst_table, (B, None), torch.int32)
-    _need("mass", mass, (B, None), torch.float32)
-    _need("mass_out", mass_out, (B, None), torch.float32)
-    _need("dst.K", dst.K, (None, None, None, None), src.K.dtype)
+    dt = src.K.dtype
+    _need("dst.K", dst.K, (None, None, None, None), dt)
     if mass is None and mass_out is not None:
         raise ValueError("mass_out without mass")
     if mass is not None and mass_out is None:
         mass_out = torch.empty((B, keep), dtype=torch.float32, device=mass.device)
-    s = _here(stream, keep_idx, n_keep, table, dst_table, mass, mass_out, *src.tensors(), *dst.tensors())
-    a, b = src.desc(), dst.desc()
+    W, D, L, M = _width(table), _width(dst_table), _width(mass), _width(mass_out)
+    (pi, pn, pt, pd, pm, pmo), s = _args(stream, (
+        ("keep_idx", keep_idx, (B, keep), torch.int32), ("n_keep", n_keep, (B,), torch.int32),
+        ("table", table, (B, W), torch.int32), ("dst_table", dst_table, (B, D), torch.int32),
+        ("mass", mass, (B, L), torch.float32), ("mass_out", mass_out, (B, M), torch.float32)), src, dst)
     _check("rolesub_cache_compact", load().rolesub_cache_compact(
-        ctypes.byref(a), ctypes.byref(b), _code(src.K), B, _ptr(table), table.shape[1], _ptr(keep_idx), _ptr(n_keep),
-        keep, _ptr(dst_table), dst_table.shape[1], _ptr(mass), 0 if mass is None else mass.shape[1], _ptr(mass_out),
-        0 if mass_out is None else mass_out.shape[1], s))
+        src.desc(), dst.desc(), _CODES[dt], B, pt, W, pi, pn, keep, pd, D, pm, L or 0, pmo, M or 0, s))
     return mass_out

@@ -264,8 +264,9 @@ def test_attend_paged_validation(lib):
     assert call(mi=A0) == 1 and "without mass_out" in _last()
     assert call(mo=A0, ld=31) == 1 and "mass_ld" in _last()
     assert call(mi=A0, mo=ctypes.c_void_p(0x10000010), ld=32) == 1 and "overlap" in _last()
-    assert call(ws=None) == 1 and "workspace" in _last()
-    assert call(wsb=16) == 1 and call(ws=ctypes.c_void_p(0x10000004)) == 1
+    assert call(mp=100, ws=None) == 1 and "workspace" in _last()  # splits need one
+    assert call(mp=100, wsb=16) == 1 and call(ws=ctypes.c_void_p(0x10000004)) == 1
+    assert call(mo=A1, ld=32, wsb=16) == 1 and "workspace" in _last()  # and weights
     assert call(R=ctypes.c_void_p(0x10000008)) == 2 and call(q=ctypes.c_void_p(0x10000008)) == 2
     assert call(qs=260) == 2 and call(qs=64) == 1
     assert call(mp=1 << 27) == 2 and "max_len" in _last()
