@@ -157,6 +157,65 @@ __device__ __forceinline__ f32x4 score_step(u32x4 k, u32x4 q, f32x4 s) {
   }
 }
 
+// A 16-byte part of a token's expanded value row: the parts of its kept groups, zeros
+// for dropped ones. vg: the part's first group; vin: its place in the group where
+// that is wider (SUB == 1).
+template <int SUB>
+__device__ __forceinline__ u32x4 request_piece(rsrc_t rv, uint32_t mask, uint32_t slot, int vg, uint32_t vin, int gb,
+                                               uint32_t vcap) {
+  uint32_t sl = slot + __popc(mask & ((1u << vg) - 1u));
+  if constexpr (SUB == 1) return bload16(rv, ((mask >> vg) & 1u) && sl < vcap ? sl * gb + vin : kOOB);
+  u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < SUB; ++u) {
+    const bool on = (mask >> (vg + u)) & 1u;
+    const uint32_t off = on && sl < vcap ? sl * gb : kOOB;
+    if constexpr (SUB == 2) {
+      const u32x2 y = bload8(rv, off);
+      v[2 * u] = y.x;
+      v[2 * u + 1] = y.y;
+    } else {
+      v[u] = bload4(rv, off);
+    }
+    sl += on;
+  }
+  return v;
+}
+
+// The tile's values times its weights s, added to the sums (dims the rows of the
+// product, queries its columns).
+template <class T, int DH>
+__device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4* acc) {
+  using L = Tile<T, DH>;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+  if constexpr (L::kBf16) {
+    // weights as two bf16 each, so that their rounding stays below the output's
+    bf16x8 hi, lo;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float pv = s[x / 4][x % 4];
+      hi[x] = fromf<bf16>(pv);
+      lo[x] = fromf<bf16>(pv - tof(hi[x]));
+    }
+    const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb) {
+      const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
+      const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+      acc[mb] = mfma_16x16x32(a, hi, acc[mb]);
+      acc[mb] = mfma_16x16x32(a, lo, acc[mb]);
+    }
+  } else {
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float a = *reinterpret_cast<const float*>(zt + (4 * g4 + x) * L::ZLD + 4 * (16 * mb + l16));
+        acc[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][x], acc[mb], 0, 0, 0);
+      }
+  }
+}
+
 // A lane's part of row r's query: the dims that its part of a key is multiplied by.
 template <class T, int DH>
 __device__ __forceinline__ void load_query(const DecodeParams& p, int b, int h, int r, int g4, u32x4* qf) {
@@ -237,6 +296,72 @@ __device__ __forceinline__ void one_by_one(const DecodeParams& p, int b, int h, 
     }
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb) acc[mb] = *reinterpret_cast<f32x4*>(sum + 16 * mb);
+}
+
+// The end of a split: the sums of the waves of each row block added in their order,
+// and left for k_join or, where there is no other split, finished. All 256 threads.
+template <class T, int DH, int WR>
+__device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, int rtile, int sp, float m, float l,
+                                          const f32x4* acc, char* smem, float (*s_m)[16], float (*s_l)[16]) {
+  using L = Tile<T, DH>;
+  constexpr int MB = L::MB, RLD = L::RLD, WT = 4 / WR;
+  const PagedCache& c = p.c;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
+  Rotation<T, DH> rot;
+  if (p.n_split == 1) rot.load(p, h);
+  // the sums of the waves of one row block, in their order
+  l = add_xor32(add_xor16(l));
+  if (g4 == 0) {
+    s_m[w][l16] = m;
+    s_l[w][l16] = l;
+  }
+  __syncthreads();  // also: no wave reads its tile any more
+  float* red = reinterpret_cast<float*>(smem);
+  {
+    float M = s_m[w % WR][l16];
+#pragma unroll
+    for (int v = 1; v < WT; ++v) M = fmaxf(M, s_m[w % WR + v * WR][l16]);
+    const float f = weight_of(m, M);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+      *reinterpret_cast<f32x4*>(red + (w * 16 + l16) * RLD + 16 * mb + 4 * g4) = acc[mb] * f;
+  }
+  __syncthreads();
+  const int64_t rows0 = (static_cast<int64_t>(b) * c.H + h) * p.R;
+#pragma unroll 1
+  for (int u = tid; u < 16 * WR * (DH / 4); u += 256) {
+    const int row = u / (DH / 4), d = u % (DH / 4) * 4, rb = row / 16, rr = row % 16, rg = rtile * 16 * WR + row;
+    float M = s_m[rb][rr];
+#pragma unroll
+    for (int v = 1; v < WT; ++v) M = fmaxf(M, s_m[rb + v * WR][rr]);
+    float sum = 0.f;
+    f32x4 a = {0, 0, 0, 0};
+#pragma unroll
+    for (int v = 0; v < WT; ++v) {
+      sum += s_l[rb + v * WR][rr] * weight_of(s_m[rb + v * WR][rr], M);
+      a += *reinterpret_cast<const f32x4*>(red + ((rb + v * WR) * 16 + rr) * RLD + d);
+    }
+    if (p.n_split == 1) {
+      if (rg >= p.R || sum == 0.f) a = f32x4{0, 0, 0, 0};
+      else a /= sum;
+      *reinterpret_cast<f32x4*>(red + (rb * 16 + rr) * RLD + d) = a;  // read by this thread only
+    }
+    if (rg >= p.R) continue;
+    const int64_t at = (rows0 + rg) * p.n_split + sp;
+    if (p.n_split > 1) *reinterpret_cast<f32x4*>(p.part + at * DH + d) = a;
+    if (d == 0 && p.stat) {
+      p.stat[2 * at] = M;
+      p.stat[2 * at + 1] = sum;
+    }
+  }
+  if (p.n_split == 1) {
+    __syncthreads();
+#pragma unroll 1
+    for (int rb = 0; rb < WR; ++rb) {
+      const int r0 = (rtile * WR + rb) * 16;
+      if (r0 < p.R) finish_rows<T, DH>(p, b, h, r0, red + rb * 16 * RLD, rot);
+    }
+  }
 }
 
 // One split of one key head and 16 * WR rows: wave w takes row block w % WR and every
@@ -354,26 +479,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
                                     there1[nb] ? static_cast<uint32_t>(vstep) : 0u);
 #pragma unroll
         for (int x = nb * NVI / NB; x < (nb + 1) * NVI / NB; ++x) {
-          const u32x2 t = tk[x];
-          uint32_t sl = t.y + __popc(t.x & ((1u << vg) - 1u));
-          if constexpr (SUB == 1) {
-            vf[x] = bload16(rv, ((t.x >> vg) & 1u) && sl < static_cast<uint32_t>(c.vcap) ? sl * gb + vin : kOOB);
-          } else {
-            uint32_t* vv = reinterpret_cast<uint32_t*>(&vf[x]);
-#pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-              const bool on = (t.x >> (vg + u)) & 1u;
-              const uint32_t off = on && sl < static_cast<uint32_t>(c.vcap) ? sl * gb : kOOB;
-              if constexpr (SUB == 2) {
-                const u32x2 y = bload8(rv, off);
-                vv[2 * u] = y.x;
-                vv[2 * u + 1] = y.y;
-              } else {
-                vv[u] = bload4(rv, off);
-              }
-              sl += on;
-            }
-          }
+          vf[x] = request_piece<SUB>(rv, tk[x].x, tk[x].y, vg, vin, gb, static_cast<uint32_t>(c.vcap));
         }
       }
     };
@@ -443,32 +549,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
           s[nb][x] = exp2_(s[nb][x] - ms);
           l += s[nb][x];
         }
-      if constexpr (L::kBf16) {
-        // weights as two bf16 each, so that their rounding stays below the output's
-        bf16x8 hi, lo;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const float pv = s[x / 4][x % 4];
-          hi[x] = fromf<bf16>(pv);
-          lo[x] = fromf<bf16>(pv - tof(hi[x]));
-        }
-        const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-          const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
-          const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-          acc[mb] = mfma_16x16x32(a, hi, acc[mb]);
-          acc[mb] = mfma_16x16x32(a, lo, acc[mb]);
-        }
-      } else {
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const float a = *reinterpret_cast<const float*>(zt + (4 * g4 + x) * L::ZLD + 4 * (16 * mb + l16));
-            acc[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][x], acc[mb], 0, 0, 0);
-          }
-      }
+      weigh_tile<T, DH>(zt, s, acc);
       wave_lds_order();
       settle(acc);
     }
@@ -480,61 +561,199 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
   if (__any(bad)) one_by_one<T, DH>(p, b, h, r, first, STEP, end, lim, zt, m, l, acc);
 
-  Rotation<T, DH> rot;
-  if (p.n_split == 1) rot.load(p, h);
-  // the sums of the waves of one row block, in their order
-  l = add_xor32(add_xor16(l));
-  if (g4 == 0) {
-    s_m[w][l16] = m;
-    s_l[w][l16] = l;
-  }
-  __syncthreads();  // also: no wave reads its tile any more
-  float* red = reinterpret_cast<float*>(smem);
-  {
-    float M = s_m[w % WR][l16];
+  add_waves<T, DH, WR>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
+}
+
+// One split of one key head and 64 rows, 16 a wave: the four waves share each tile of
+// tokens. Its keys and kept groups come into registers a tile ahead, a quarter a
+// wave, and go from there to one of two LDS tiles, so that one barrier a tile is
+// enough: between two barriers the waves write the next tile and compute on this one.
+// (With a tile to each wave, as above, every wave fetches and expands all of it:
+// 16 sequences of up to 361 tokens and 56 queries took 42 us.)
+template <class T, int DH, int SUB>
+__global__ __launch_bounds__(256) void k_decode_rows(DecodeParams p) {
+  using L = Tile<T, DH>;
+  constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, MB = L::MB;
+  constexpr int KLD = L::ROWB + 16, KB = TK * KLD, BUF = KB + L::ZB;
+  constexpr int TPP = 256 / L::LPT, NP = TK / TPP;  // tokens of a pass of the workgroup, passes
+  static_assert(NP >= 1 && (16 % TPP == 0 || TPP % 16 == 0), "a wave's pass lies in one block of 16 tokens");
+  constexpr int SMEM = 2 * BUF > 4 * L::RB ? 2 * BUF : 4 * L::RB;
+  constexpr int TPG = 64 / NB;  // tiles whose pages one load brings
+  __shared__ __attribute__((aligned(16))) char smem[SMEM];
+  __shared__ float s_m[4][16], s_l[4][16];
+  static_assert(SMEM / 4 >= 16 * DH * 4, "a wave's sums fit its quarter");
+  const PagedCache& c = p.c;
+  const int nrt = (p.R + 63) / 64;
+  int lin = blockIdx.x;
+  const int rtile = lin % nrt;
+  lin /= nrt;
+  const int sp = lin % p.n_split;
+  lin /= p.n_split;
+  const int h = lin % c.H, b = lin / c.H;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15,
+            g4 = lane >> 4;
+  const int len = tokens_of(p, b), c0 = sp * p.chunk;
+  if (c0 >= len && p.n_split > 1) return;
+  const uint32_t gm = group_bits(c.G);
+  const int shift = c.shift, pmask = c.page - 1, gb = c.ds * static_cast<int>(sizeof(T));
+  const int r = (rtile * 4 + w) * 16 + l16;
+  u32x4 qf[KS];
+  load_query<T, DH>(p, b, h, r, g4, qf);
+  int lim = 0;
+  if (r < p.R) lim = p.visible ? min(len, max(p.visible[static_cast<int64_t>(b) * p.Tq + r / p.rep], 0)) : len;
+  int top = lim;
 #pragma unroll
-    for (int v = 1; v < WT; ++v) M = fmaxf(M, s_m[w % WR + v * WR][l16]);
-    const float f = weight_of(m, M);
+  for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor(top, o, kWave));
+  if (lane == 0) s_m[w][0] = __int_as_float(top);
+  __syncthreads();
+  int all = max(max(__float_as_int(s_m[0][0]), __float_as_int(s_m[1][0])),
+                max(__float_as_int(s_m[2][0]), __float_as_int(s_m[3][0])));
+  const int end = min(c0 + p.chunk, __builtin_amdgcn_readfirstlane(all));
+
+  const rsrc_t r_table = make_rsrc(p.table + static_cast<int64_t>(b) * p.max_pages,
+                                   clamp_bytes(static_cast<size_t>(p.max_pages) * 4));
+  const uint32_t meta_bytes = static_cast<uint32_t>(c.n_pages) << (shift + 2);  // below 2 GiB
+  const rsrc_t r_mask = make_rsrc(c.mask, meta_bytes), r_slot = make_rsrc(c.slot, meta_bytes);
+  const int64_t kstep = static_cast<int64_t>(c.page) * L::ROWB, vstep = static_cast<int64_t>(c.vcap) * gb;
+
+  // this thread's pieces: part pc of tokens vt + TPP x of every tile
+  const int pc = tid % L::LPT, vt = tid / L::LPT;
+  const int vg = SUB == 1 ? pc * 16 / gb : pc * SUB;
+  const uint32_t vin = SUB == 1 ? static_cast<uint32_t>(pc * 16 % gb) : 0u;
+  float* px = p.x ? p.x + ((static_cast<int64_t>(b) * c.H + h) * p.R + r) * p.x_ld : nullptr;
+
+  int pgs = 0;                    // lane j: the page of block j % NB of the (j / NB)-th of TPG tiles
+  uint32_t there = 0, now = 0;    // bit nb: that block's page is one (of the tile in registers, in hand)
+  int pg1[NP], pgm[NP];           // pages of this wave's passes: of the tile whose masks are asked for next
+  uint32_t mk[NP];
+  int sl0[NP];
+  u32x4 kf[NP], vf[NP];
+  auto block_of = [&](int x) { return (x * TPP + w * (64 / L::LPT)) / 16; };  // of this wave's pass x
+  auto take_pages = [&](int i) {
+    if (i % TPG == 0) {
+      const int t = c0 + i * TK + lane / NB * TK + lane % NB * 16;
+      pgs = static_cast<int>(bload4(r_table, static_cast<uint32_t>(t >> shift) * 4u));  // past the row: 0
+    }
+    there = 0;
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-      *reinterpret_cast<f32x4*>(red + (w * 16 + l16) * RLD + 16 * mb + 4 * g4) = acc[mb] * f;
+    for (int nb = 0; nb < NB; ++nb) {
+      const int v = __builtin_amdgcn_readlane(pgs, i % TPG * NB + nb);
+      const bool in = c0 + i * TK + 16 * nb < end && static_cast<uint32_t>(v) < static_cast<uint32_t>(c.n_pages);
+      there |= in ? 1u << nb : 0u;
+#pragma unroll
+      for (int x = 0; x < NP; ++x)
+        if (block_of(x) == nb) pg1[x] = in ? v : -1;
+    }
+  };
+  auto request_meta = [&](int i) {
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      const int t = c0 + i * TK + x * TPP + vt;
+      const uint32_t off = oob_unless(t < end && pg1[x] >= 0,
+                                      (static_cast<uint32_t>(pg1[x]) << (shift + 2)) + static_cast<uint32_t>(t & pmask) * 4u);
+      mk[x] = bload4(r_mask, off);
+      sl0[x] = static_cast<int>(bload4(r_slot, off));
+      pgm[x] = pg1[x];
+    }
+  };
+  auto request_tile = [&](int i) {  // whose masks have been asked for
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      const int64_t at = static_cast<int64_t>(max(pgm[x], 0)) * c.H + h;
+      const rsrc_t rk = make_rsrc(static_cast<const char*>(c.K) + at * kstep, pgm[x] >= 0 ? static_cast<uint32_t>(kstep) : 0u);
+      const int t = c0 + i * TK + x * TPP + vt;
+      kf[x] = bload16(rk, static_cast<uint32_t>(t & pmask) * L::ROWB + 16 * pc);
+    }
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      const int64_t at = static_cast<int64_t>(max(pgm[x], 0)) * c.H + h;
+      const rsrc_t rv = make_rsrc(static_cast<const char*>(c.V) + at * vstep, pgm[x] >= 0 ? static_cast<uint32_t>(vstep) : 0u);
+      vf[x] = request_piece<SUB>(rv, mk[x] & gm, static_cast<uint32_t>(sl0[x]), vg, vin, gb, static_cast<uint32_t>(c.vcap));
+    }
+  };
+  auto put_tile = [&](char* buf) {
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      *reinterpret_cast<u32x4*>(buf + (x * TPP + vt) * KLD + 16 * pc) = kf[x];
+      *reinterpret_cast<u32x4*>(buf + KB + (x * TPP + vt) * L::ZLD + 16 * pc) = vf[x];
+    }
+  };
+
+  float m = -__builtin_inff(), l = 0.f;
+  f32x4 acc[MB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0, 0, 0, 0};
+  uint32_t there0, there1;
+  take_pages(0);
+  there0 = there;
+  request_meta(0);
+  request_tile(0);
+  take_pages(1);
+  there1 = there;
+  request_meta(1);
+  put_tile(smem);
+  request_tile(1);
+  take_pages(2);
+  request_meta(2);
+#pragma unroll 1
+  for (int i = 0, t0 = c0; t0 < end; ++i, t0 += TK) {
+    __syncthreads();
+    const char* buf = smem + (i & 1) * BUF;
+    now = there0;
+    put_tile(smem + ((i + 1) & 1) * BUF);
+    there0 = there1;
+    there1 = there;
+    request_tile(i + 2);
+    take_pages(i + 3);
+    request_meta(i + 3);
+    f32x4 s[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      s[nb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < KS; ++j)
+        s[nb] = score_step<T>(*reinterpret_cast<const u32x4*>(buf + (16 * nb + l16) * KLD + 64 * j + 16 * g4), qf[j], s[nb]);
+    }
+    settle(s);
+    float mx = -__builtin_inff();
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const bool see = ((now >> nb) & 1u) && t0 + 16 * nb + 4 * g4 + x < lim;
+        s[nb][x] = see ? s[nb][x] * p.scale : -__builtin_inff();
+        mx = fmaxf(mx, s[nb][x]);
+      }
+      const int t = t0 + 16 * nb + 4 * g4;
+      if (px && r < p.R && t < end) *reinterpret_cast<f32x4*>(px + t) = s[nb];
+    }
+    mx = max_xor32(max_xor16(mx));
+    const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.f : mn;
+    if (__any(mn > m)) {
+      const float al = exp2_(m - ms);
+      l *= al;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) acc[mb] *= al;
+      m = mn;
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        s[nb][x] = exp2_(s[nb][x] - ms);
+        l += s[nb][x];
+      }
+    weigh_tile<T, DH>(buf + KB, s, acc);
+    settle(acc);
   }
   __syncthreads();
-  const int64_t rows0 = (static_cast<int64_t>(b) * c.H + h) * p.R;
-#pragma unroll 1
-  for (int u = tid; u < 16 * WR * (DH / 4); u += 256) {
-    const int row = u / (DH / 4), d = u % (DH / 4) * 4, rb = row / 16, rr = row % 16, rg = rtile * 16 * WR + row;
-    float M = s_m[rb][rr];
+  bool bad = false;
 #pragma unroll
-    for (int v = 1; v < WT; ++v) M = fmaxf(M, s_m[rb + v * WR][rr]);
-    float sum = 0.f;
-    f32x4 a = {0, 0, 0, 0};
+  for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-    for (int v = 0; v < WT; ++v) {
-      sum += s_l[rb + v * WR][rr] * weight_of(s_m[rb + v * WR][rr], M);
-      a += *reinterpret_cast<const f32x4*>(red + ((rb + v * WR) * 16 + rr) * RLD + d);
-    }
-    if (p.n_split == 1) {
-      if (rg >= p.R || sum == 0.f) a = f32x4{0, 0, 0, 0};
-      else a /= sum;
-      *reinterpret_cast<f32x4*>(red + (rb * 16 + rr) * RLD + d) = a;  // read by this thread only
-    }
-    if (rg >= p.R) continue;
-    const int64_t at = (rows0 + rg) * p.n_split + sp;
-    if (p.n_split > 1) *reinterpret_cast<f32x4*>(p.part + at * DH + d) = a;
-    if (d == 0 && p.stat) {
-      p.stat[2 * at] = M;
-      p.stat[2 * at + 1] = sum;
-    }
-  }
-  if (p.n_split == 1) {
-    __syncthreads();
-#pragma unroll 1
-    for (int rb = 0; rb < WR; ++rb) {
-      const int r0 = (rtile * WR + rb) * 16;
-      if (r0 < p.R) finish_rows<T, DH>(p, b, h, r0, red + rb * 16 * RLD, rot);
-    }
-  }
+    for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
+  if (__any(bad)) one_by_one<T, DH>(p, b, h, r, c0, TK, end, lim, smem + w * (SMEM / 4), m, l, acc);
+  add_waves<T, DH, 4>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
 }
 
 // log2 of a row's sum of exponentials from its splits' statistics, and the maximum.
@@ -663,12 +882,20 @@ __global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nbl
 
 int row_blocks(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }  // blocks of 16 rows of a workgroup
 
+template <class T, int DH, int WR, int SUB>
+constexpr auto kernel_of() {
+  if constexpr (WR == 4)
+    return k_decode_rows<T, DH, SUB>;
+  else
+    return k_decode<T, DH, WR, SUB>;
+}
+
 template <class T, int DH, int WR>
 void go(const DecodeParams& p, hipStream_t s) {
   const int sub = p.c.ds >= Tile<T, DH>::EP ? 1 : Tile<T, DH>::EP / p.c.ds;
-  auto kern = sub == 1 ? k_decode<T, DH, WR, 1> : k_decode<T, DH, WR, 2>;
+  auto kern = sub == 1 ? kernel_of<T, DH, WR, 1>() : kernel_of<T, DH, WR, 2>();
   if constexpr (sizeof(T) == 2) {
-    if (sub == 4) kern = k_decode<T, DH, WR, 4>;
+    if (sub == 4) kern = kernel_of<T, DH, WR, 4>();
   }
   const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(256), 0, s, p);
