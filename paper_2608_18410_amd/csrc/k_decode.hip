@@ -54,6 +54,10 @@ __device__ __forceinline__ int tokens_of(const DecodeParams& p, int b) {
   return static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
 }
 
+// Waits here for a load. In a branch, so that what follows it does not wait on every
+// path: there the wait would be for whatever else is under way.
+__device__ __forceinline__ void arrived(int& x) { asm volatile("" : "+v"(x)); }
+
 // Waits until a matrix product's result may be read by other instructions. The
 // compiler spaces them within a block; where a branch followed the product and the
 // read came first after the join, it left the read too early (stale values of the
@@ -484,7 +488,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       }
     };
     auto next_pages = [&](int i) {
-      if (i % TPP == 0) request_pages(i);
+      if (i % TPP == 0) {
+        request_pages(i);
+        arrived(pgs);
+      }
       take_pages(i);
     };
 
@@ -571,7 +578,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 // (With a tile to each wave, as above, every wave fetches and expands all of it:
 // 16 sequences of up to 361 tokens and 56 queries took 42 us.)
 template <class T, int DH, int SUB>
-__global__ __launch_bounds__(256) void k_decode_rows(DecodeParams p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 3 : 4))) void k_decode_rows(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, MB = L::MB;
   constexpr int KLD = L::ROWB + 16, KB = TK * KLD, BUF = KB + L::ZB;
@@ -633,6 +640,7 @@ __global__ __launch_bounds__(256) void k_decode_rows(DecodeParams p) {
     if (i % TPG == 0) {
       const int t = c0 + i * TK + lane / NB * TK + lane % NB * 16;
       pgs = static_cast<int>(bload4(r_table, static_cast<uint32_t>(t >> shift) * 4u));  // past the row: 0
+      arrived(pgs);
     }
     there = 0;
 #pragma unroll
