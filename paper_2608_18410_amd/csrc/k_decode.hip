@@ -25,6 +25,9 @@ __device__ __forceinline__ bf16x4 lds_read_tr(const char* p) {
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)(p)));
 }
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Factor of sums taken against the maximum m once the maximum is M. Sums without a
@@ -52,6 +55,34 @@ struct Tile {
 __device__ __forceinline__ int tokens_of(const DecodeParams& p, int b) {
   const int64_t cap = static_cast<int64_t>(p.max_pages) << p.c.shift;
   return static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
+}
+
+// Eight floats as the sum of two bf16 each.
+__device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8& hi, bf16x8& lo) {
+  u32x4 h, l;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2 x = i < 2 ? f32x2{a[2 * i], a[2 * i + 1]} : f32x2{b[2 * i - 4], b[2 * i - 3]};
+    h[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+    const f32x2 y = {x[0] - __uint_as_float(h[i] << 16), x[1] - __uint_as_float(h[i] & 0xFFFF0000u)};
+    l[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+  }
+  hi = __builtin_bit_cast(bf16x8, h);
+  lo = __builtin_bit_cast(bf16x8, l);
+}
+
+// Order of N steps of R LDS reads that feed M matrix products each: the reads run A
+// steps ahead (left to itself the compiler waits for each).
+template <int N, int R, int M, int A>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int kDsRead = 0x100, kMfma = 0x008;
+  __builtin_amdgcn_sched_group_barrier(kDsRead, A * R, 0);
+#pragma unroll
+  for (int i = 0; i + A < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, M, 0);
+    __builtin_amdgcn_sched_group_barrier(kDsRead, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kMfma, A * M, 0);
 }
 
 // Waits here for a load. In a branch, so that what follows it does not wait on every
@@ -110,11 +141,7 @@ __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h,
       const int d = (4 * j + g4) * EP;
       if constexpr (L::kBf16) {
         bf16x8 hi, lo;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          hi[x] = fromf<bf16>(ur[d + x]);
-          lo[x] = fromf<bf16>(ur[d + x] - tof(hi[x]));
-        }
+        split_bf16(*reinterpret_cast<const f32x4*>(ur + d), *reinterpret_cast<const f32x4*>(ur + d + 4), hi, lo);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           o[i] = mfma_16x16x32(__builtin_bit_cast(bf16x8, rot.a[i][j]), hi, o[i]);
@@ -186,21 +213,74 @@ __device__ __forceinline__ u32x4 request_piece(rsrc_t rv, uint32_t mask, uint32_
   return v;
 }
 
+// A tile's scores s become weights: exponentials against the reference m, which the
+// sums l and acc are kept against. It is raised, and they are scaled, only when some
+// row's maximum passes it by more than 2^8: up to there nothing can overflow, and
+// what the weights round to is relative to themselves. ok: blocks of 16 tokens that
+// are there; lim: tokens the lane's row sees, least: those all rows see. SHORT: tiles
+// that all rows see whole take a way without the comparisons (worth it where the
+// kernel is bound by such instructions; the branch costs registers).
+template <class T, int DH, bool SHORT>
+__device__ __forceinline__ void soften(const DecodeParams& p, f32x4* s, uint32_t ok, int t0, int lim, int least, int end,
+                                       int r, float* px, float& m, float& l, f32x4* acc) {
+  using L = Tile<T, DH>;
+  constexpr int NB = L::NB;
+  constexpr float kSlack = 8.f;
+  const int g4 = (threadIdx.x & 63) >> 4;
+  if (SHORT && t0 + L::TK <= least && ok == (1u << NB) - 1u) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[nb][x] *= p.scale;
+  } else {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const bool see = ((ok >> nb) & 1u) && t0 + 16 * nb + 4 * g4 + x < lim;
+        s[nb][x] = see ? s[nb][x] * p.scale : -__builtin_inff();
+      }
+  }
+  if (p.x) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int t = t0 + 16 * nb + 4 * g4;
+      if (r < p.R && t < end) *reinterpret_cast<f32x4*>(px + t) = s[nb];
+    }
+  }
+  float mx = s[0][0];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) mx = fmaxf(mx, s[nb][x]);
+  mx = max_xor32(max_xor16(mx));
+  if (__any(mx > m + kSlack)) {
+    const float mn = fmaxf(m, mx), al = mn == -__builtin_inff() ? 0.f : exp2_(m - mn);
+    m = mn;
+    l *= al;
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb) acc[mb] *= al;
+  }
+  const float ms = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      s[nb][x] = exp2_(s[nb][x] - ms);
+      l += s[nb][x];
+    }
+}
+
 // The tile's values times its weights s, added to the sums (dims the rows of the
-// product, queries its columns).
-template <class T, int DH>
+// product, queries its columns). A: steps by which LDS reads run ahead.
+template <class T, int DH, int A>
 __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4* acc) {
   using L = Tile<T, DH>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   if constexpr (L::kBf16) {
     // weights as two bf16 each, so that their rounding stays below the output's
     bf16x8 hi, lo;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      const float pv = s[x / 4][x % 4];
-      hi[x] = fromf<bf16>(pv);
-      lo[x] = fromf<bf16>(pv - tof(hi[x]));
-    }
+    split_bf16(s[0], s[L::NB - 1], hi, lo);
     const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb) {
@@ -209,6 +289,7 @@ __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4
       acc[mb] = mfma_16x16x32(a, hi, acc[mb]);
       acc[mb] = mfma_16x16x32(a, lo, acc[mb]);
     }
+    if constexpr (A > 0) reads_ahead<L::MB, 2, 2, A>();
   } else {
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb)
@@ -405,9 +486,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   u32x4 qf[KS];
   load_query<T, DH>(p, b, h, r, g4, qf);
   if (r < p.R) lim = p.visible ? min(len, max(p.visible[static_cast<int64_t>(b) * p.Tq + r / p.rep], 0)) : len;
-  int top = lim;
+  int top = lim, low = r < p.R ? lim : 0x7FFFFFFF;
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor(top, o, kWave));
+  for (int o = 1; o < 16; o <<= 1) {
+    top = max(top, __shfl_xor(top, o, kWave));
+    low = min(low, __shfl_xor(low, o, kWave));
+  }
+  const int least = __builtin_amdgcn_readfirstlane(low);
   const int end = min(c0 + p.chunk, __builtin_amdgcn_readfirstlane(top));
   const int first = c0 + (w / WR) * TK;
 
@@ -415,7 +500,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
                                    clamp_bytes(static_cast<size_t>(p.max_pages) * 4));
   const uint32_t meta_bytes = static_cast<uint32_t>(c.n_pages) << (shift + 2);  // below 2 GiB
   const rsrc_t r_mask = make_rsrc(c.mask, meta_bytes), r_slot = make_rsrc(c.slot, meta_bytes);
-  const int64_t kstep = static_cast<int64_t>(c.page) * L::ROWB, vstep = static_cast<int64_t>(c.vcap) * gb;
+  // bytes of a head's part of a page, and of a page (below 2 GiB)
+  const uint32_t kstep = static_cast<uint32_t>(c.page) * L::ROWB, vstep = static_cast<uint32_t>(c.vcap) * gb;
+  const uint32_t kpage = kstep * c.H, vpage = vstep * c.H;
+  const char* khead = static_cast<const char*>(c.K) + static_cast<size_t>(h) * kstep;
+  const char* vhead = static_cast<const char*>(c.V) + static_cast<size_t>(h) * vstep;
 
   // a lane's pieces of the values: always the same part of a row
   const int pc = lane % L::LPT, vt = lane / L::LPT;
@@ -462,9 +551,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         there1[nb] = pg1[nb] >= 0;
-        const int64_t at = static_cast<int64_t>(max(pg1[nb], 0)) * c.H + h;
-        const rsrc_t rk = make_rsrc(static_cast<const char*>(c.K) + at * kstep,
-                                    there1[nb] ? static_cast<uint32_t>(kstep) : 0u);
+        const rsrc_t rk = make_rsrc(khead + static_cast<uint64_t>(max(pg1[nb], 0)) * kpage, there1[nb] ? kstep : 0u);
         const uint32_t ko = static_cast<uint32_t>(((t0 + 16 * nb) & pmask) + l16) * L::ROWB + 16 * g4;
 #pragma unroll
         for (int j = 0; j < KS; ++j) kf[nb][j] = bload16(rk, ko + 64 * j);
@@ -473,17 +560,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     auto request_values = [&]() {
       if (lane < TK) rec[lane] = u32x2{mk1 & gm, static_cast<uint32_t>(sl1)};
       wave_lds_order();
-      u32x2 tk[NVI];
-#pragma unroll
-      for (int x = 0; x < NVI; ++x) tk[x] = rec[x * L::TPI + vt];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const int64_t at = static_cast<int64_t>(max(pg1[nb], 0)) * c.H + h;
-        const rsrc_t rv = make_rsrc(static_cast<const char*>(c.V) + at * vstep,
-                                    there1[nb] ? static_cast<uint32_t>(vstep) : 0u);
+        constexpr int N = NVI / NB;
+        u32x2 tk[N];
 #pragma unroll
-        for (int x = nb * NVI / NB; x < (nb + 1) * NVI / NB; ++x) {
-          vf[x] = request_piece<SUB>(rv, tk[x].x, tk[x].y, vg, vin, gb, static_cast<uint32_t>(c.vcap));
+        for (int x = 0; x < N; ++x) tk[x] = rec[(nb * N + x) * L::TPI + vt];
+        const rsrc_t rv = make_rsrc(vhead + static_cast<uint64_t>(max(pg1[nb], 0)) * vpage, there1[nb] ? vstep : 0u);
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+          vf[nb * N + x] = request_piece<SUB>(rv, tk[x].x, tk[x].y, vg, vin, gb, static_cast<uint32_t>(c.vcap));
         }
       }
     };
@@ -509,7 +595,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       // scores: tokens are the rows of the product, queries its columns
       f32x4 s[NB];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
+      for (int nb = 0; nb < NB; ++nb) {  // in the order the keys arrive
         s[nb] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < KS; ++j) s[nb] = score_step<T>(kf[nb][j], qf[j], s[nb]);
@@ -527,36 +613,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       for (int nb = 0; nb < NB; ++nb) there[nb] = there1[nb];
       next_pages(i + 2);
       request_meta(i + 2);
-      // softmax against the running maximum
-      float mx = -__builtin_inff();
+      uint32_t ok = 0;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const bool see = now[nb] && t0 + 16 * nb + 4 * g4 + x < lim;
-          s[nb][x] = see ? s[nb][x] * p.scale : -__builtin_inff();
-          mx = fmaxf(mx, s[nb][x]);
-        }
-        const int t = t0 + 16 * nb + 4 * g4;
-        if (px && r < p.R && t < end) *reinterpret_cast<f32x4*>(px + t) = s[nb];
-      }
-      mx = max_xor32(max_xor16(mx));
-      const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.f : mn;
-      if (__any(mn > m)) {
-        const float al = exp2_(m - ms);
-        l *= al;
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) acc[mb] *= al;
-        m = mn;
-      }
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          s[nb][x] = exp2_(s[nb][x] - ms);
-          l += s[nb][x];
-        }
-      weigh_tile<T, DH>(zt, s, acc);
+      for (int nb = 0; nb < NB; ++nb) ok |= now[nb] ? 1u << nb : 0u;
+      soften<T, DH, false>(p, s, ok, t0, lim, least, end, r, px, m, l, acc);
+      weigh_tile<T, DH, 0>(zt, s, acc);
       wave_lds_order();
       settle(acc);
     }
@@ -608,9 +669,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   load_query<T, DH>(p, b, h, r, g4, qf);
   int lim = 0;
   if (r < p.R) lim = p.visible ? min(len, max(p.visible[static_cast<int64_t>(b) * p.Tq + r / p.rep], 0)) : len;
-  int top = lim;
+  int top = lim, low = r < p.R ? lim : 0x7FFFFFFF;
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor(top, o, kWave));
+  for (int o = 1; o < 16; o <<= 1) {
+    top = max(top, __shfl_xor(top, o, kWave));
+    low = min(low, __shfl_xor(low, o, kWave));
+  }
+  const int least = __builtin_amdgcn_readfirstlane(low);
   if (lane == 0) s_m[w][0] = __int_as_float(top);
   __syncthreads();
   int all = max(max(__float_as_int(s_m[0][0]), __float_as_int(s_m[1][0])),
@@ -621,7 +686,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
                                    clamp_bytes(static_cast<size_t>(p.max_pages) * 4));
   const uint32_t meta_bytes = static_cast<uint32_t>(c.n_pages) << (shift + 2);  // below 2 GiB
   const rsrc_t r_mask = make_rsrc(c.mask, meta_bytes), r_slot = make_rsrc(c.slot, meta_bytes);
-  const int64_t kstep = static_cast<int64_t>(c.page) * L::ROWB, vstep = static_cast<int64_t>(c.vcap) * gb;
+  // bytes of a head's part of a page, and of a page (below 2 GiB)
+  const uint32_t kstep = static_cast<uint32_t>(c.page) * L::ROWB, vstep = static_cast<uint32_t>(c.vcap) * gb;
+  const uint32_t kpage = kstep * c.H, vpage = vstep * c.H;
+  const char* khead = static_cast<const char*>(c.K) + static_cast<size_t>(h) * kstep;
+  const char* vhead = static_cast<const char*>(c.V) + static_cast<size_t>(h) * vstep;
 
   // this thread's pieces: part pc of tokens vt + TPP x of every tile
   const int pc = tid % L::LPT, vt = tid / L::LPT;
@@ -667,15 +736,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   auto request_tile = [&](int i) {  // whose masks have been asked for
 #pragma unroll
     for (int x = 0; x < NP; ++x) {
-      const int64_t at = static_cast<int64_t>(max(pgm[x], 0)) * c.H + h;
-      const rsrc_t rk = make_rsrc(static_cast<const char*>(c.K) + at * kstep, pgm[x] >= 0 ? static_cast<uint32_t>(kstep) : 0u);
+      const rsrc_t rk = make_rsrc(khead + static_cast<uint64_t>(max(pgm[x], 0)) * kpage, pgm[x] >= 0 ? kstep : 0u);
       const int t = c0 + i * TK + x * TPP + vt;
       kf[x] = bload16(rk, static_cast<uint32_t>(t & pmask) * L::ROWB + 16 * pc);
     }
 #pragma unroll
     for (int x = 0; x < NP; ++x) {
-      const int64_t at = static_cast<int64_t>(max(pgm[x], 0)) * c.H + h;
-      const rsrc_t rv = make_rsrc(static_cast<const char*>(c.V) + at * vstep, pgm[x] >= 0 ? static_cast<uint32_t>(vstep) : 0u);
+      const rsrc_t rv = make_rsrc(vhead + static_cast<uint64_t>(max(pgm[x], 0)) * vpage, pgm[x] >= 0 ? vstep : 0u);
       vf[x] = request_piece<SUB>(rv, mk[x] & gm, static_cast<uint32_t>(sl0[x]), vg, vin, gb, static_cast<uint32_t>(c.vcap));
     }
   };
@@ -716,42 +783,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     request_meta(i + 3);
     f32x4 s[NB];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      s[nb] = f32x4{0, 0, 0, 0};
+    for (int nb = 0; nb < NB; ++nb) s[nb] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < KS; ++j)
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
         s[nb] = score_step<T>(*reinterpret_cast<const u32x4*>(buf + (16 * nb + l16) * KLD + 64 * j + 16 * g4), qf[j], s[nb]);
-    }
     settle(s);
-    float mx = -__builtin_inff();
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const bool see = ((now >> nb) & 1u) && t0 + 16 * nb + 4 * g4 + x < lim;
-        s[nb][x] = see ? s[nb][x] * p.scale : -__builtin_inff();
-        mx = fmaxf(mx, s[nb][x]);
-      }
-      const int t = t0 + 16 * nb + 4 * g4;
-      if (px && r < p.R && t < end) *reinterpret_cast<f32x4*>(px + t) = s[nb];
-    }
-    mx = max_xor32(max_xor16(mx));
-    const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.f : mn;
-    if (__any(mn > m)) {
-      const float al = exp2_(m - ms);
-      l *= al;
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb) acc[mb] *= al;
-      m = mn;
-    }
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        s[nb][x] = exp2_(s[nb][x] - ms);
-        l += s[nb][x];
-      }
-    weigh_tile<T, DH>(buf + KB, s, acc);
+    soften<T, DH, true>(p, s, now, t0, lim, least, end, r, px, m, l, acc);
+    weigh_tile<T, DH, 2>(buf + KB, s, acc);
     settle(acc);
   }
   __syncthreads();
