@@ -305,6 +305,7 @@ struct DecodeParams {
   int64_t mass_ld;
   // workspace
   int n_split, chunk;  // tokens of a split
+  int ordered;         // sequences by their lengths (set by the launcher)
   float* part;         // [B][H][R][n_split][dh] sums of P z, unnormalised (with splits)
   float* stat;         // [B][H][R][n_split][2]  maximum (log2), sum of P (with splits or mass)
   float* x;            // [B][H][R][x_ld] scores in units of log2 (with mass)
