@@ -750,6 +750,16 @@ def _rows(name, t):
     return st, t[0, 0, 0]
 
 
+def _operand(name, t, H, dh, dtype):
+    """Shape, token stride and stand-in of a [B, T, H (None: any), dh] operand."""
+    shape = t.shape if isinstance(t, _Tensor) and t.dtype is dtype else ()
+    if len(shape) != 4 or shape[3] != dh or (H is not None and shape[2] != H):
+        _need(name, t, (None, None, H, dh), dtype)
+    if t.is_contiguous():
+        return shape, shape[2] * dh, t
+    return shape, *_rows(name, t)
+
+
 _FLOATS = (torch.float32, torch.bfloat16)
 
 
@@ -773,7 +783,8 @@ class PagedCache:
         _need("mask", self.mask, (n, page), _MASK)
         _need("slot", self.slot, (n, page), torch.int32)
         put = object.__setattr__
-        put(self, "G", dh // ds)
+        for name, x in (("G", dh // ds), ("H", H), ("dh", dh), ("page", page), ("dtype", self.K.dtype)):
+            put(self, name, x)
         # the library's description of the cache, made once
         put(self, "_desc", PagesDesc(n, page, self.V.shape[2], H, dh, dh // ds, None, None, None, None))
         put(self, "_at", None)
@@ -815,8 +826,10 @@ def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=Fals
     some = q if q is not None else k
     if some is None:
         raise ValueError("q and k are both None")
-    _need("q" if q is not None else "k", some, (None, None, None, None), _FLOATS)
-    B, T, H, dh = some.shape
+    shape = some.shape if isinstance(some, _Tensor) else ()
+    if len(shape) != 4 or some.dtype not in _FLOATS:
+        _need("q" if q is not None else "k", some, (None, None, None, None), _FLOATS)
+    B, T, H, dh = shape
     dt = some.dtype
     spec, A, n = [], 1, None
     if isinstance(positions, _Tensor) and positions.dim() == 3:
@@ -836,15 +849,19 @@ def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=Fals
             outs[i] = None
             spec += [(name, None, None, None)] * 2
             continue
-        if x is not some:
-            _need(name, x, (B, T, None, dh), dt)
-        heads[i] = x.shape[2]
-        strides[i], row = _rows(name, x)
+        if x is some:
+            xs = shape
+            strides[i], row = _rows(name, x)
+        else:
+            xs, strides[i], row = _operand(name, x, None, dh, dt)
+            if xs[0] != B or xs[1] != T:
+                _need(name, x, (B, T, None, dh), dt)
+        heads[i] = xs[2]
         if o is None:
-            o = outs[i] = torch.empty_like(x) if row is x else torch.empty(x.shape, dtype=dt, device=x.device)
+            o = outs[i] = torch.empty_like(x) if row is x else torch.empty(xs, dtype=dt, device=x.device)
             orow = o
         else:
-            _need(f"{name}_out", o, x.shape, dt)
+            _need(f"{name}_out", o, xs, dt)
             so, orow = _rows(f"{name}_out", o)
             if orow is not o and (so != strides[i] or o.data_ptr() != x.data_ptr()):
                 raise ValueError(f"{name}_out: must be {name} itself or contiguous")
@@ -861,12 +878,10 @@ def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=Fals
 def cache_append(cache: PagedCache, k, z, mask, table, lens, n_new=None, stream=None) -> PagedCache:
     """Token j of sequence b (j < n_new[b], or all) becomes token lens[b] + j of its
     pages: k and z [B,T,H,dh], mask [B,T]; table [B,max_pages], lens [B] int32."""
-    _, H, _, dh = cache.K.shape
-    dt = cache.K.dtype
-    _need("k", k, (None, None, H, dh), dt)
-    B, T = k.shape[:2]
-    _need("z", z, k.shape, dt)
-    sk, rk = _rows("k", k)
+    dt = cache.dtype
+    shape, sk, rk = _operand("k", k, cache.H, cache.dh, dt)
+    B, T = shape[:2]
+    _need("z", z, shape, dt)
     sz, rz = _rows("z", z)
     W = _width(table)
     (pk, pz, pmask, pt, pl, pn), s = _args(stream, (
@@ -888,12 +903,9 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
     [B,Tq,Hq,dh]. visible [B,Tq] int32: the tokens each query sees. mass [B,>=max_len]
     f32: the tokens' accumulated weight, in place or into mass_out (which alone
     starts from zero): decay * mass + the weight of this call's queries."""
-    _, H, page, dh = cache.K.shape
-    dt = cache.K.dtype
-    _need("q", q, (None, None, None, dh), dt)
-    shape = q.shape
+    H, dh, dt = cache.H, cache.dh, cache.dtype
+    shape, sq, rq = _operand("q", q, None, dh, dt)
     B, Tq, Hq, _ = shape
-    sq, rq = _rows("q", q)
     W, ld = _width(table), 0
     if mass_out is None:
         mass_out = mass
@@ -902,7 +914,7 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
     o = torch.empty(shape, dtype=out_dtype or dt, device=q.device) if out is None else out
     odt = o.dtype if isinstance(o, _Tensor) and o.dtype in _CODES else _FLOATS
     if workspace is None:
-        whole = (W or 0) * page
+        whole = (W or 0) * cache.page
         need = attend_paged_workspace_size(cache, B, Hq, Tq, min(int(max_len), whole) if max_len else whole,
                                            mass_out is not None)
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
@@ -926,8 +938,10 @@ def evict_tokens(mass, lens, keep: int, first: int = 0, recent: int = 0, max_len
     """Which `keep` tokens of every sequence stay: the first, the recent, and of the
     others those with the most mass [B,>=max_len]. Returns (keep_idx [B,keep] int32,
     ascending, then -1; n_keep [B] int32). max_len 0: mass.shape[1]."""
-    _need("mass", mass, (None, None), torch.float32)
-    B, ld = mass.shape
+    shape = mass.shape if isinstance(mass, _Tensor) else ()
+    if len(shape) != 2:
+        _need("mass", mass, (None, None), torch.float32)
+    B, ld = shape
     if out is None:
         if keep < 1:
             raise ValueError(f"keep: expected at least 1, got {keep}")
@@ -951,10 +965,13 @@ def cache_compact(src: PagedCache, table, keep_idx, n_keep, dst: PagedCache, dst
     """Token j < n_keep[b] of the pages dst_table[b] of dst becomes token
     keep_idx[b, j] of the pages table[b] of src; mass_out[b, j] = mass[b, keep_idx[b, j]]
     (a new [B, keep] tensor when mass comes alone). Returns mass_out (or None)."""
-    _need("keep_idx", keep_idx, (None, None), torch.int32)
-    B, keep = keep_idx.shape
-    dt = src.K.dtype
-    _need("dst.K", dst.K, (None, None, None, None), dt)
+    shape = keep_idx.shape if isinstance(keep_idx, _Tensor) else ()
+    if len(shape) != 2:
+        _need("keep_idx", keep_idx, (None, None), torch.int32)
+    B, keep = shape
+    dt = src.dtype
+    if dst.dtype is not dt:
+        _need("dst.K", dst.K, (None, None, None, None), dt)
     if mass is None and mass_out is not None:
         raise ValueError("mass_out without mass")
     if mass is not None and mass_out is None:
