@@ -998,7 +998,14 @@ hipError_t launch(DecodeParams p, hipStream_t s) {
   return hipGetLastError();
 }
 
-constexpr int64_t kSplitWgs = 512;  // workgroups that the splits are made for
+// Workgroups that the splits are made for: two for each of the 256 CUs. More splits
+// cost more to add up than they even out: 64 sequences of 256 to 2048 tokens and 8
+// key heads take 60 us in one split each, 73 in two, 66 in four; 16 of 361 tokens
+// and 56 queries 40 against 64. Short sequences in one split without the weights, whose
+// adding takes the second launch anyway, would save that launch (one of 305 tokens, 32
+// heads: 12.2 against 14.4 us), but a call's outputs would then depend on whether it
+// adds up weights.
+constexpr int64_t kSplitWgs = 512;
 constexpr int64_t kMaxSplits = 256;  // that k_join adds up
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
