@@ -160,14 +160,15 @@ __global__ __launch_bounds__(NT) void k_evict_one(EvictParams p) {
 // workgroup leaves its histogram; those of the next launch add them up, each for
 // itself, so that nothing is cleared and no count depends on an order.
 struct EvictWs {
-  int* hist[3];   // [B][C][bins]
-  int* above[2];  // [B][C] keys above the digit found at levels 0, 1
-  int* state[2];  // [B][2] digits found, keys left to keep, after levels 0, 1
+  uint16_t* hist[3];  // [B][C][bins], counts of at most kMaxChunk
+  int* above[2];      // [B][C] keys above the digit found at levels 0, 1
+  int* state[2];      // [B][2] digits found, keys left to keep, after levels 0, 1
 };
 
 constexpr int kPassWg = 512;
 constexpr int kChunk = 4096;    // tokens of a workgroup's round: 8 a thread, all requested at once
 constexpr int kMaxChunks = 64;  // histograms that each workgroup adds up
+constexpr int kMaxChunk = 61440;  // except where chunks would pass this (counts are kept in 16 bits)
 
 template <int LEVEL>
 __global__ __launch_bounds__(kPassWg) void k_evict_pass(EvictParams p, EvictWs ws, int C, int chunk) {
@@ -175,6 +176,15 @@ __global__ __launch_bounds__(kPassWg) void k_evict_pass(EvictParams p, EvictWs w
   __shared__ int hist[LEVEL < 3 ? level_bins(LEVEL % 3) : 1];
   __shared__ int wsum[NT / 64], s_out[2], cnt[LEVEL == 3 ? 64 : 1];
   const int b = blockIdx.x / C, c = blockIdx.x % C, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  // the last level's histograms are asked for before anything else is known (rows past
+  // the sequence's chunks are not counted)
+  constexpr int L = LEVEL > 0 ? LEVEL - 1 : 0, PNB = level_bins(L), PER = PNB / NT, ROWS = LEVEL > 0 ? 32 : 1;
+  typedef uint16_t vec __attribute__((ext_vector_type(PER)));
+  const uint16_t* rows = ws.hist[L] + static_cast<int64_t>(b) * C * PNB + (PNB - (tid + 1) * PER);
+  vec v[ROWS];
+  if constexpr (LEVEL > 0)
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x) v[x] = *reinterpret_cast<const vec*>(rows + static_cast<int64_t>(min(x, C - 1)) * PNB);
   const Range r = range_of(p, b);
   int32_t* out = p.keep_idx + static_cast<int64_t>(b) * p.keep;
   if (LEVEL == 3 && c == 0 && tid == 0) p.n_keep[b] = r.n;
@@ -197,23 +207,26 @@ __global__ __launch_bounds__(kPassWg) void k_evict_pass(EvictParams p, EvictWs w
   uint32_t found = 0;
   int need = r.need, eq_before = 0, gt_before = 0;
   if (LEVEL > 0 && need > 0) {
-    constexpr int L = LEVEL > 0 ? LEVEL - 1 : 0, NB = level_bins(L), PER = NB / NT;
+    constexpr int NB = PNB;
     if (L > 0) {
       found = ws.state[L - 1][2 * b];
       need = ws.state[L - 1][2 * b + 1];
     }
-    const int* h = ws.hist[L] + static_cast<int64_t>(b) * C * NB + (NB - (tid + 1) * PER);
     int sum[PER] = {}, own[PER] = {}, pre[PER] = {};
-    typedef int vec __attribute__((ext_vector_type(PER)));
-#pragma unroll 16
-    for (int x = 0; x < used; ++x) {
-      const vec v = *reinterpret_cast<const vec*>(h + static_cast<int64_t>(x) * NB);
+    for (int x0 = 0; x0 < used; x0 += ROWS) {
+      if (x0 > 0)
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        sum[j] += v[PER - 1 - j];
-        own[j] = x == c ? v[PER - 1 - j] : own[j];
-        pre[j] += x < c ? v[PER - 1 - j] : 0;
-      }
+        for (int x = 0; x < ROWS; ++x)
+          v[x] = *reinterpret_cast<const vec*>(rows + static_cast<int64_t>(min(x0 + x, C - 1)) * PNB);
+#pragma unroll
+      for (int x = 0; x < ROWS; ++x)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          const int n = x0 + x < used ? v[x][PER - 1 - j] : 0;
+          sum[j] += n;
+          own[j] = x0 + x == c ? n : own[j];
+          pre[j] += x0 + x < c ? n : 0;
+        }
     }
     int d, above;
     find_digit<NT, PER>(sum, need, wsum, s_out, d, above);
@@ -259,8 +272,8 @@ __global__ __launch_bounds__(kPassWg) void k_evict_pass(EvictParams p, EvictWs w
         if (level_has(LEVEL, k, found)) atomicAdd(&hist[level_digit(LEVEL, k)], 1);
       }
     __syncthreads();
-    int* h = ws.hist[LEVEL] + (static_cast<int64_t>(b) * C + c) * NB;
-    for (int i = tid; i < NB; i += NT) h[i] = hist[i];
+    uint16_t* h = ws.hist[LEVEL] + (static_cast<int64_t>(b) * C + c) * NB;
+    for (int i = tid; i < NB; i += NT) h[i] = static_cast<uint16_t>(hist[i]);
   } else {
     const uint32_t thr = r.need > 0 ? found : 0xFFFFFFFFu;
     const int ties = r.need > 0 ? need : 0;
@@ -308,15 +321,18 @@ constexpr int kOneWg = 16384;   // tokens whose keys one workgroup holds in regi
 
 int chunk_of(int max_len) {
   const int64_t c = (static_cast<int64_t>(max_len) + kMaxChunks - 1) / kMaxChunks;
-  return static_cast<int>(std::max<int64_t>(kChunk, (c + kChunk - 1) / kChunk * kChunk));
+  return static_cast<int>(std::min<int64_t>(kMaxChunk, std::max<int64_t>(kChunk, (c + kChunk - 1) / kChunk * kChunk)));
 }
+
+size_t hist_bytes(size_t n) { return (n * (2048 + 2048 + 1024) * sizeof(uint16_t) + 15) & ~static_cast<size_t>(15); }
 
 }  // namespace
 
 size_t evict_ws_bytes(int B, int max_len) {
   if (max_len <= kOneWg) return 0;
-  const size_t C = std::min((max_len + kChunk - 1) / kChunk, kMaxChunks);  // at least the chunks of every shorter length
-  return (B * C * (2048 + 2048 + 1024 + 2) + static_cast<size_t>(B) * 4) * sizeof(int);
+  // at least the chunks of every shorter length
+  const size_t C = std::max(std::min((max_len + kChunk - 1) / kChunk, kMaxChunks), (max_len + kMaxChunk - 1) / kMaxChunk);
+  return hist_bytes(B * C) + (B * C * 2 + static_cast<size_t>(B) * 4) * sizeof(int);
 }
 
 hipError_t launch_evict(const EvictParams& p, hipStream_t s) {
@@ -331,11 +347,12 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t s) {
     const int chunk = chunk_of(p.max_len), C = (p.max_len + chunk - 1) / chunk;
     const size_t n = static_cast<size_t>(p.B) * C;
     EvictWs ws;
-    int* at = static_cast<int*>(p.ws);
+    uint16_t* bins = static_cast<uint16_t*>(p.ws);
     for (int l = 0; l < 3; ++l) {
-      ws.hist[l] = at;
-      at += n * level_bins(l);
+      ws.hist[l] = bins;
+      bins += n * level_bins(l);
     }
+    int* at = reinterpret_cast<int*>(static_cast<char*>(p.ws) + hist_bytes(n));
     for (int l = 0; l < 2; ++l) {
       ws.above[l] = at;
       at += n;

@@ -91,23 +91,23 @@ __global__ __launch_bounds__(256) void k_append_few(AppendParams p, int np, int 
   }
 }
 
-// What a workgroup knows of its page's tokens while it copies them: where each
-// token's key and first group come from (rows and slots of head 0; negative: zeros),
-// and whose group every slot holds.
+// What a workgroup knows of its page's tokens while it copies them: the row each
+// token's key comes from (of head 0; negative: zeros), how far its groups' slots move
+// (of head 0), and whose group every slot holds (kNone: zeros).
+constexpr uint16_t kNone = 0xFFFF;
 struct PageMap {
-  int64_t krow[kMaxPage], vrow[kMaxPage];
-  int32_t from[kMaxPage], slot[kMaxPage];
+  int64_t krow[kMaxPage], vmove[kMaxPage];
   uint16_t owner[kMaxPage * 32];
 };
 
 // Rows and slots of HB heads from h0, the same piece of every head by one thread, so
 // that HB * U loads are on their way at once and each address is worked out once.
 // Keys: rows of 2^lkp pieces; tokens [0, m) go to rows r0 + t of the page. Values:
-// slots [s0, s1), whole groups of gb bytes in pieces of VB.
+// slots [0, slots), whole groups of gb bytes in pieces of VB.
 template <int VB, int HB>
 __device__ __forceinline__ void copy_page(const PageMap& g, const char* ksrc, int64_t krowb, int64_t khead, const char* vsrc,
-                                          int64_t vhead, int32_t vmax, const PagedCache& d, int64_t page, int r0, int m,
-                                          int s0, int s1, int h0, int e) {
+                                          int64_t vhead, const PagedCache& d, int64_t page, int r0, int m,
+                                          int slots, int h0, int e) {
   constexpr int U = 8 / HB;
   typedef typename Piece<VB>::t piece;
   const int tid = threadIdx.x, row = d.dh * e, lkp = __builtin_ctz(row / 16), gb = d.ds * e;
@@ -137,16 +137,14 @@ __device__ __forceinline__ void copy_page(const PageMap& g, const char* ksrc, in
   const int lpg = __builtin_ctz(gb / VB);  // pieces of a group
   char* vd = static_cast<char*>(d.V) + (page * d.H + h0) * d.vcap * static_cast<int64_t>(gb);
   const int64_t vdh = static_cast<int64_t>(d.vcap) * gb;
-  const int p0 = s0 << lpg, p1 = s1 << lpg;
-  for (int u0 = p0 + tid; u0 < p1; u0 += 256 * U) {
+  const int p1 = slots << lpg;
+  for (int u0 = tid; u0 < p1; u0 += 256 * U) {
     piece x[U][HB];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = min(u0 + 256 * i, p1 - 1), sl = u >> lpg, t = g.owner[sl - s0];
-      const int r = sl - g.slot[t];  // the token's r-th kept group
-      const uint32_t fr = static_cast<uint32_t>(g.from[t]) + r;
-      const bool in = g.krow[t] >= 0 && fr < static_cast<uint32_t>(vmax);
-      const char* v = vsrc + (g.vrow[t] + r) * gb + (u & ((1 << lpg) - 1)) * VB;
+      const int u = min(u0 + 256 * i, p1 - 1), sl = u >> lpg, t = g.owner[sl];
+      const bool in = t != kNone;
+      const char* v = vsrc + (in ? g.vmove[t] + sl : 0) * gb + (u & ((1 << lpg) - 1)) * VB;
 #pragma unroll
       for (int h = 0; h < HB; ++h) {
         x[i][h] = piece{};
@@ -207,7 +205,7 @@ __global__ __launch_bounds__(256) void k_append(AppendParams p, int np, int e) {
   }
   __syncthreads();
   const int row = c.dh * e, gb = c.ds * e, h0 = blockIdx.y * HB;
-  copy_page<VB, HB>(g, static_cast<const char*>(p.k), p.k_stride * e, row, nullptr, 0, 0, c, page, r0, m, 0, 0, h0, e);
+  copy_page<VB, HB>(g, static_cast<const char*>(p.k), p.k_stride * e, row, nullptr, 0, c, page, r0, m, 0, h0, e);
   const int lpg = __builtin_ctz(gb / VB);
   char* vd = static_cast<char*>(c.V) + (static_cast<int64_t>(page) * c.H + h0) * c.vcap * static_cast<int64_t>(gb);
   const int64_t vdh = static_cast<int64_t>(c.vcap) * gb;
@@ -275,10 +273,11 @@ __global__ __launch_bounds__(256) void k_compact(CompactParams p, int np, int e)
   if (tid == 255) s_total = at + cnt;
   if (tid < m) {
     g.krow[tid] = spage < 0 ? -1 : ((static_cast<int64_t>(spage) * c.H) << c.shift) + srow;
-    g.vrow[tid] = static_cast<int64_t>(spage) * c.H * c.vcap + from;
-    g.from[tid] = from;
-    g.slot[tid] = at;
-    for (int x = 0; x < cnt; ++x) g.owner[at + x] = static_cast<uint16_t>(tid);
+    g.vmove[tid] = static_cast<int64_t>(spage) * c.H * c.vcap + from - at;
+    for (int x = 0; x < cnt; ++x) {
+      const uint32_t fr = static_cast<uint32_t>(from) + x;
+      g.owner[at + x] = fr < static_cast<uint32_t>(c.vcap) ? static_cast<uint16_t>(tid) : kNone;
+    }
     if (blockIdx.y == 0) {
       const int64_t meta = (static_cast<int64_t>(page) << c.shift) + tid;
       d.mask[meta] = whole;
@@ -288,7 +287,7 @@ __global__ __launch_bounds__(256) void k_compact(CompactParams p, int np, int e)
   __syncthreads();
   const int row = c.dh * e, gb = c.ds * e;
   copy_page<VB, HB>(g, static_cast<const char*>(c.K), row, static_cast<int64_t>(row) << c.shift,
-                    static_cast<const char*>(c.V), static_cast<int64_t>(c.vcap) * gb, c.vcap, d, page, 0, m, 0,
+                    static_cast<const char*>(c.V), static_cast<int64_t>(c.vcap) * gb, d, page, 0, m,
                     min(s_total, d.vcap), blockIdx.y * HB, e);
 }
 
