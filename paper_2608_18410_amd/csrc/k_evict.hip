@@ -339,6 +339,8 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t s) {
   const dim3 one(static_cast<unsigned>(p.B));
   if (p.max_len <= 1024) {
     hipLaunchKernelGGL((k_evict_one<256, 4>), one, dim3(256), 0, s, p);
+  } else if (p.max_len <= 2048) {
+    hipLaunchKernelGGL((k_evict_one<512, 4>), one, dim3(512), 0, s, p);
   } else if (p.max_len <= 4096) {
     hipLaunchKernelGGL((k_evict_one<1024, 4>), one, dim3(1024), 0, s, p);
   } else if (p.max_len <= kOneWg) {
