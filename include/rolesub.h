@@ -451,8 +451,9 @@ typedef struct rolesub_pages {
  *   positions [B,T,n_axes] int32; inv_freq [n_pairs] f32; axis [n_pairs] uint8
  *   or NULL (all axis 0); a pair whose axis is >= n_axes is not turned.
  *   q_out, k_out: dense, or the input itself (same pointer, then the same
- *   stride is used); otherwise they overlap no input.
- * Angles are formed and reduced in 64 bits: exact for every int32 position.
+ *   stride is used); otherwise no output overlaps another tensor of the call.
+ * Whole turns are taken off the angles in more than 64 bits: positions of any size
+ * lose nothing.
  * ------------------------------------------------------------------------ */
 rolesub_status rolesub_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int32_t dh, rolesub_dtype dtype,
                               const void* q, int64_t q_stride, const void* k, int64_t k_stride,

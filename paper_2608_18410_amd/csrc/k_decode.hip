@@ -648,7 +648,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       soften<T, DH, false>(p, s, ok, t0, lim, least, end, r, px, m, l, acc);
       weigh_tile<T, DH, 0>(zt, s, acc);
       wave_lds_order();
-      settle(acc);
     }
   }
   bool bad = false;
@@ -820,10 +819,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
         s[nb] = score_step<T>(*reinterpret_cast<const u32x4*>(buf + (16 * nb + l16) * KLD + 64 * j + 16 * g4), qf[j], s[nb]);
-    settle(s);
     soften<T, DH, true>(p, s, now, t0, lim, least, end, r, px, m, l, acc);
     weigh_tile<T, DH, 2>(buf + KB, s, acc);
-    settle(acc);
   }
   __syncthreads();
   bool bad = false;

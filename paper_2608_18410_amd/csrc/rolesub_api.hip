@@ -906,8 +906,15 @@ rolesub_status check_rows(const char* fn, const char* name, const void* p, int64
   return ROLESUB_OK;
 }
 
-size_t extent(size_t tokens, int64_t stride, int64_t row, size_t e) {
-  return tokens ? ((tokens - 1) * stride + row) * e : 0;
+// Whether two sets of n rows (of ra and rb elements, sa and sb apart) share an element.
+// Rows of one stride may interleave, as the parts of a fused projection do.
+bool rows_overlap(const void* a, int64_t sa, int64_t ra, const void* b, int64_t sb, int64_t rb, size_t n, size_t e) {
+  if (!ranges_overlap(a, ((n - 1) * sa + ra) * e, b, ((n - 1) * sb + rb) * e)) return false;
+  if (sa != sb) return true;
+  const int64_t row = sa * static_cast<int64_t>(e);
+  int64_t d = (static_cast<const char*>(b) - static_cast<const char*>(a)) % row;
+  if (d < 0) d += row;
+  return d < ra * static_cast<int64_t>(e) || d + rb * static_cast<int64_t>(e) > row;
 }
 
 }  // namespace
@@ -961,13 +968,17 @@ rolesub_status rolesub_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int3
   const int64_t qr = static_cast<int64_t>(H) * dh, kr = static_cast<int64_t>(Hkv) * dh;
   p.qo_stride = q_out == q ? p.q_stride : qr;
   p.ko_stride = k_out == k ? p.k_stride : kr;
-  const size_t nq = q ? extent(n, p.q_stride, qr, e) : 0, nk = k ? extent(n, p.k_stride, kr, e) : 0;
-  const size_t oq = q ? extent(n, p.qo_stride, qr, e) : 0, ok = k ? extent(n, p.ko_stride, kr, e) : 0;
-  const bool qi = q && q_out == q, ki = k && k_out == k;
-  if ((q && !qi && (ranges_overlap(q_out, oq, q, nq) || (k && ranges_overlap(q_out, oq, k, nk)))) ||
-      (k && !ki && (ranges_overlap(k_out, ok, k, nk) || (q && ranges_overlap(k_out, ok, q, nq)))) ||
-      (q && k && !(qi && ki) && ranges_overlap(q_out, oq, k_out, ok)))
-    return fail(ROLESUB_ERR_INVALID_ARG, "%s: an output overlaps another tensor of the call", fn);
+  struct Rows {
+    const void* p;
+    int64_t stride, row;
+  } const t[4] = {{q, p.q_stride, qr}, {k, p.k_stride, kr}, {q ? q_out : nullptr, p.qo_stride, qr},
+                  {k ? k_out : nullptr, p.ko_stride, kr}};
+  for (int o = 2; o < 4; ++o)
+    for (int x = 0; x < 4; ++x) {
+      if (!t[o].p || !t[x].p || x == o || (x == o - 2 && t[x].p == t[o].p)) continue;  // an input itself
+      if (rows_overlap(t[o].p, t[o].stride, t[o].row, t[x].p, t[x].stride, t[x].row, n, e))
+        return fail(ROLESUB_ERR_INVALID_ARG, "%s: an output overlaps another tensor of the call", fn);
+    }
   return from_hip(launch_rotary(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
 }
 
@@ -1053,7 +1064,8 @@ rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dt
   p.q = q;
   p.q_stride = q_stride;
   if ((st = check_rows(fn, "q", q, p.q_stride, Hq, p.c.dh, esize(dtype)))) return st;
-  if (!aligned(R, 16)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: R must lie on 16 bytes", fn);
+  if (!aligned(R, 16) || !aligned(out, 16))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: R and out must lie on 16 bytes", fn);
   p.max_pages = max_pages;
   p.max_len = static_cast<int>(ml);
   p.table = table;

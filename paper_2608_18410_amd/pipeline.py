@@ -139,6 +139,12 @@ def run_full_layer(q, k, v, mask, Rt, R, S: int, bufs: FullWidthBuffers, budget=
     return bufs
 
 
+def _current_stream(stream):
+    """stream as the current one, so that what a chain of calls allocates in between
+    belongs to it."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
 def page_count(tokens: int, page: int) -> int:
     """Pages that hold `tokens` tokens."""
     return -(-int(tokens) // page)
@@ -155,14 +161,15 @@ def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.Page
     as they are. visible defaults to all cached and new tokens; for T > 1 causal
     tokens pass visible[b, j] = lens[b] + j + 1. With mass the tokens' weight is
     accumulated for evict_layer. Returns the attention output [B,T,Hq,dh]."""
-    mask = rs.route(types, budget, G, h=h, router=router, scores_in=scores_in, want_scores=False, want_idx=False,
-                    want_count=False, stream=stream)["mask"]
-    if positions is not None:
-        q, k = rs.rotary(q, k, positions, inv_freq, axis, stream=stream)
-    z = rs.rotate_values(v, R, stream=stream)
-    rs.cache_append(cache, k, z, mask, table, lens, stream=stream)
-    return rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
-                           workspace=workspace, out=out, stream=stream)
+    with _current_stream(stream):
+        mask = rs.route(types, budget, G, h=h, router=router, scores_in=scores_in, want_scores=False, want_idx=False,
+                        want_count=False)["mask"]
+        if positions is not None:
+            q, k = rs.rotary(q, k, positions, inv_freq, axis)
+        z = rs.rotate_values(v, R)
+        rs.cache_append(cache, k, z, mask, table, lens)
+        return rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
+                               workspace=workspace, out=out)
 
 
 def evict_layer(cache: rs.PagedCache, table, lens, mass, keep: int, first: int, recent: int, dst: rs.PagedCache,
@@ -171,10 +178,10 @@ def evict_layer(cache: rs.PagedCache, table, lens, mass, keep: int, first: int, 
     accumulated weight, moved to the pages dst_table of dst (the caller's allocator
     then has the old ones back). Returns (the new lengths [B], their weights as wide
     as mass with zeros for the tokens to come, the kept indices [B,keep])."""
-    idx, n = rs.evict_tokens(mass, lens, keep, first, recent, max_len=max_len, stream=stream)
-    if mass_out is None:
-        mass_out = torch.empty_like(mass) if mass.shape[1] >= keep else mass.new_empty((mass.shape[0], keep))
-    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+    with _current_stream(stream):
+        idx, n = rs.evict_tokens(mass, lens, keep, first, recent, max_len=max_len)
+        if mass_out is None:
+            mass_out = torch.empty_like(mass) if mass.shape[1] >= keep else mass.new_empty((mass.shape[0], keep))
         mass_out.zero_()
-    rs.cache_compact(cache, table, idx, n, dst, dst_table, mass=mass, mass_out=mass_out, stream=stream)
-    return n, mass_out, idx
+        rs.cache_compact(cache, table, idx, n, dst, dst_table, mass=mass, mass_out=mass_out)
+        return n, mass_out, idx

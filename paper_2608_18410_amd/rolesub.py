@@ -735,6 +735,14 @@ def _on_current(cur, stream, ts):
         raise ValueError(f"the stream is on cuda:{stream.device_index}, but the current device is cuda:{cur}")
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor for a call on `stream` (None: the current one)."""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None and t.is_cuda:
+        t.record_stream(stream)
+    return t
+
+
 def _rows(name, t):
     """Token stride of a [B, T, H, dh] operand whose tokens lie at one stride (dense,
     or a view of a fused projection), and a dense stand-in for _args: the operand
@@ -763,7 +771,7 @@ def _operand(name, t, H, dh, dtype):
 _FLOATS = (torch.float32, torch.bfloat16)
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class PagedCache:
     """Pages of a growing routed cache (kept alive while calls are in flight):
     K [n_pages,H,page,dh], V [n_pages,H,vcap,dh/G], mask and slot [n_pages,page]
@@ -858,7 +866,7 @@ def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=Fals
                 _need(name, x, (B, T, None, dh), dt)
         heads[i] = xs[2]
         if o is None:
-            o = outs[i] = torch.empty_like(x) if row is x else torch.empty(xs, dtype=dt, device=x.device)
+            o = outs[i] = torch.empty_like(x) if row is x and stream is None else _empty(xs, dt, x.device, stream)
             orow = o
         else:
             _need(f"{name}_out", o, xs, dt)
@@ -911,13 +919,13 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
         mass_out = mass
     if mass_out is not None:
         ld = _width(mass_out) if mass is None else _width(mass)
-    o = torch.empty(shape, dtype=out_dtype or dt, device=q.device) if out is None else out
+    o = _empty(shape, out_dtype or dt, q.device, stream) if out is None else out
     odt = o.dtype if isinstance(o, _Tensor) and o.dtype in _CODES else _FLOATS
     if workspace is None:
         whole = (W or 0) * cache.page
         need = attend_paged_workspace_size(cache, B, Hq, Tq, min(int(max_len), whole) if max_len else whole,
                                            mass_out is not None)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(need, 1), torch.uint8, q.device, stream)
     ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
     (pq, pt, pl, pR, pv, pmi, pmo, po, pw), s = _args(stream, (
         ("q", rq, rq.shape, dt), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
@@ -945,12 +953,11 @@ def evict_tokens(mass, lens, keep: int, first: int = 0, recent: int = 0, max_len
     if out is None:
         if keep < 1:
             raise ValueError(f"keep: expected at least 1, got {keep}")
-        dev = mass.device
-        out = (torch.empty((B, keep), dtype=torch.int32, device=dev), torch.empty((B,), dtype=torch.int32, device=dev))
+        out = (_empty((B, keep), torch.int32, mass.device, stream), _empty((B,), torch.int32, mass.device, stream))
     idx, n = out
     ml = int(max_len) if max_len else ld
     if workspace is None:
-        workspace = torch.empty(max(evict_workspace_size(B, ml), 1), dtype=torch.uint8, device=mass.device)
+        workspace = _empty(max(evict_workspace_size(B, ml), 1), torch.uint8, mass.device, stream)
     ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
     (pm, pl, pi, pn, pw), s = _args(stream, (
         ("mass", mass, (B, ld), torch.float32), ("lens", lens, (B,), torch.int32), ("keep_idx", idx, (B, keep), torch.int32),
@@ -975,7 +982,7 @@ def cache_compact(src: PagedCache, table, keep_idx, n_keep, dst: PagedCache, dst
     if mass is None and mass_out is not None:
         raise ValueError("mass_out without mass")
     if mass is not None and mass_out is None:
-        mass_out = torch.empty((B, keep), dtype=torch.float32, device=mass.device)
+        mass_out = _empty((B, keep), torch.float32, mass.device, stream)
     W, D, L, M = _width(table), _width(dst_table), _width(mass), _width(mass_out)
     (pi, pn, pt, pd, pm, pmo), s = _args(stream, (
         ("keep_idx", keep_idx, (B, keep), torch.int32), ("n_keep", n_keep, (B,), torch.int32),

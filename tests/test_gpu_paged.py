@@ -355,7 +355,7 @@ def test_rotary(dtype, dh, pairs, interleaved):
     q, k = dev(rng.standard_normal((B, T, 6, dh)), dtype), dev(rng.standard_normal((B, T, 2, dh)), dtype)
     pos = rng.integers(-100, 5000, (B, T, A))
     pos[0, 0] = 0
-    pos[1, 1] = (2 ** 31 - 1, -2 ** 31, 10 ** 6)
+    pos[1, 1] = (2 ** 31 - 1, -2 ** 31, 10 ** 6)  # (the oracle's angles are long doubles)
     f = (10000.0 ** (-np.arange(pairs) / pairs)).astype(np.float32)
     ax = rng.integers(0, A, pairs).astype(np.uint8)
     ax[0] = A if pairs > 1 else 0  # an axis that is none: not turned
@@ -482,6 +482,10 @@ def test_evict_bounds_and_lengths():
     for ml in (0, 300, 12):
         ref = O.evict(w[:, :ml] if ml else w, lens, 20, 1, 2)
         got = rs.evict_tokens(torch.from_numpy(w).to(DEV), ints(lens), 20, 1, 2, max_len=ml)
+        assert np.array_equal(got[0].cpu().numpy(), ref[0]) and np.array_equal(got[1].cpu().numpy(), ref[1])
+    for keep in (500, 501, 5000):  # nothing to evict, more places than tokens
+        got = rs.evict_tokens(torch.from_numpy(w).to(DEV), ints([500, 0, 499, 3]), keep, 7, 9)
+        ref = O.evict(w, [500, 0, 499, 3], keep, 7, 9)
         assert np.array_equal(got[0].cpu().numpy(), ref[0]) and np.array_equal(got[1].cpu().numpy(), ref[1])
     e = rs.evict_tokens(torch.empty((0, 9), device=DEV), ints([]), 3)
     assert e[0].shape == (0, 3)
@@ -618,6 +622,25 @@ def test_side_stream_and_device_checks():
         got = rs.attend_paged(q, c, t, n)
     s.synchronize()
     assert torch.equal(got, want)
+    # a whole layer step on a side stream, with what it allocates in between
+    rng2 = np.random.default_rng(1)
+    k, v = (dev(rng2.standard_normal((2, 1, 2, 64)), bf) for _ in range(2))
+    R, sc = rotations(rng2, 2, 64, bf), torch.rand((2, 1, 8), device=DEV)
+    m = torch.rand((2, 176), device=DEV)
+    res = []
+    for st in (None, s):
+        cc = rs.PagedCache(*[x.clone() for x in c.tensors()])
+        dd = rs.PagedCache(*[x.clone() for x in c.tensors()])
+        mass = m.clone()
+        torch.cuda.synchronize()
+        out = decode_layer(None, q, k, v, torch.zeros((2, 1), dtype=torch.uint8, device=DEV), R,
+                           rs.make_budget(rs.TOPK, (4,) * 4), 8, cc, t, n, n + 1, positions=n.view(2, 1),
+                           inv_freq=torch.ones(32, device=DEV), scores_in=sc, mass=mass, stream=st)
+        torch.cuda.synchronize()
+        res.append((out, mass, *evict_layer(cc, t, n + 1, mass, 60, 2, 3, dd, t[:, :4].contiguous(), stream=st), *dd.tensors()))
+        torch.cuda.synchronize()
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
     with pytest.raises(ValueError, match="device"):
         rs.attend_paged(q, c, t.cpu(), n)
 

@@ -233,6 +233,11 @@ def test_rotary_validation(lib):
     assert call(q=ctypes.c_void_p(0x10000004)) == 2
     assert call(qo=ctypes.c_void_p(0x10000010)) == 1 and "overlaps" in _last()
     assert call(qo=A1) == 1 and call(ko=A3) == 1
+    assert call(q=A0, k=A0, qo=A0, ko=A0, H=2) == 1 and call(q=A0, k=A0, qo=A0, H=2) == 1  # one tensor turned twice
+    # a query and a key of one fused row that share dims, in place
+    near = ctypes.c_void_p(0x10000000 + 3 * 64 * 2)
+    assert call(qs=512, ks=512, k=near, qo=A0, ko=near) == 1 and "overlaps" in _last()
+    assert call(qs=512, ks=640, k=ctypes.c_void_p(0x10000000 + 4 * 64 * 2), qo=A0) == 1
     assert call(B=0, q=A0) == 0
     assert call(B=1 << 20, T=1 << 10) == 2 and "too many" in _last()
 
@@ -267,7 +272,7 @@ def test_attend_paged_validation(lib):
     assert call(mp=100, ws=None) == 1 and "workspace" in _last()  # splits need one
     assert call(mp=100, wsb=16) == 1 and call(ws=ctypes.c_void_p(0x10000004)) == 1
     assert call(mo=A1, ld=32, wsb=16) == 1 and "workspace" in _last()  # and weights
-    assert call(R=ctypes.c_void_p(0x10000008)) == 2 and call(q=ctypes.c_void_p(0x10000008)) == 2
+    assert call(R=ctypes.c_void_p(0x10000008)) == 2 and call(out=ctypes.c_void_p(0x10000008)) == 2 and call(q=ctypes.c_void_p(0x10000008)) == 2
     assert call(qs=260) == 2 and call(qs=64) == 1
     assert call(mp=1 << 27) == 2 and "max_len" in _last()
     assert call(B=0) == 0 and call(Tq=0) == 0
