@@ -57,6 +57,11 @@ __device__ __forceinline__ int tokens_of(const DecodeParams& p, int b) {
   return static_cast<int>(min(static_cast<int64_t>(min(max(p.lens[b], 0), p.max_len)), cap));
 }
 
+template <bool ONCE>
+__device__ __forceinline__ u32x4 bload16_hint(rsrc_t r, uint32_t off) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, static_cast<int>(off), 0, ONCE ? 2 : 0));
+}
+
 // Eight floats as the sum of two bf16 each.
 __device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8& hi, bf16x8& lo) {
   u32x4 h, l;
@@ -484,7 +489,8 @@ __device__ __forceinline__ int in_order(const DecodeParams& p, int o, int wgs, i
 // page, so its keys and its groups are each one buffer resource: a dropped group or
 // a page that is none is an offset past it, which reads zeros and moves nothing.
 // SUB: value groups in a 16-byte piece of a row (1: a piece lies in one group).
-template <class T, int DH, int WR, int SUB>
+// ONCE: keys are loaded so that they leave the caches to other data (kOnceTokens).
+template <class T, int DH, int WR, int SUB, bool ONCE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4))) void k_decode(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, NVI = L::NVI, MB = L::MB, RLD = L::RLD;
@@ -583,7 +589,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
         const rsrc_t rk = make_rsrc(khead + static_cast<uint64_t>(max(pg1[nb], 0)) * kpage, there1[nb] ? kstep : 0u);
         const uint32_t ko = static_cast<uint32_t>(((t0 + 16 * nb) & pmask) + l16) * L::ROWB + 16 * g4;
 #pragma unroll
-        for (int j = 0; j < KS; ++j) kf[nb][j] = bload16(rk, ko + 64 * j);
+        for (int j = 0; j < KS; ++j) kf[nb][j] = bload16_hint<ONCE>(rk, ko + 64 * j);
       }
     };
     auto request_values = [&]() {
@@ -958,20 +964,25 @@ __global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nbl
 
 int row_blocks(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }  // blocks of 16 rows of a workgroup
 
+// Sequences from which on keys pass the caches by: 64 of up to 2048 tokens and 8 key
+// heads 51.5 -> 47, 64 of 1152 49.5 -> 45.5, two of 131071 and 32 heads 560 -> 550 us, but
+// 128 of 305 and 32 heads 100 -> 107.
+constexpr int kOnceTokens = 1024;
+
 template <class T, int DH, int WR, int SUB>
-constexpr auto kernel_of() {
+auto kernel_of(const DecodeParams& p) {
   if constexpr (WR == 4)
     return k_decode_rows<T, DH, SUB>;
   else
-    return k_decode<T, DH, WR, SUB>;
+    return p.max_len >= kOnceTokens ? k_decode<T, DH, WR, SUB, true> : k_decode<T, DH, WR, SUB, false>;
 }
 
 template <class T, int DH, int WR>
 void go(const DecodeParams& p, hipStream_t s) {
   const int sub = p.c.ds >= Tile<T, DH>::EP ? 1 : Tile<T, DH>::EP / p.c.ds;
-  auto kern = sub == 1 ? kernel_of<T, DH, WR, 1>() : kernel_of<T, DH, WR, 2>();
+  auto kern = sub == 1 ? kernel_of<T, DH, WR, 1>(p) : kernel_of<T, DH, WR, 2>(p);
   if constexpr (sizeof(T) == 2) {
-    if (sub == 4) kern = kernel_of<T, DH, WR, 4>();
+    if (sub == 4) kern = kernel_of<T, DH, WR, 4>(p);
   }
   const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(256), 0, s, p);
