@@ -966,7 +966,10 @@ int row_blocks(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }  // blocks of 16
 
 // Sequences from which on keys pass the caches by: 64 of up to 2048 tokens and 8 key
 // heads 51.5 -> 47, 64 of 1152 49.5 -> 45.5, two of 131071 and 32 heads 560 -> 550 us, but
-// 128 of 305 and 32 heads 100 -> 107.
+// 128 of 305 and 32 heads 100 -> 107. Not where scores are kept for the tokens' weights,
+// whose stores go through the same caches: two of 131071 and 32 heads 631 -> 676, and 8
+// heads of 4 rows 182 -> 195, four of 32768 and 32 heads 319 -> 335, though shorter
+// batches would gain (64 of up to 2048, 8 heads of 4 rows 64.6 -> 59.2).
 constexpr int kOnceTokens = 1024;
 
 template <class T, int DH, int WR, int SUB>
@@ -974,7 +977,7 @@ auto kernel_of(const DecodeParams& p) {
   if constexpr (WR == 4)
     return k_decode_rows<T, DH, SUB>;
   else
-    return p.max_len >= kOnceTokens ? k_decode<T, DH, WR, SUB, true> : k_decode<T, DH, WR, SUB, false>;
+    return p.max_len >= kOnceTokens && !p.x ? k_decode<T, DH, WR, SUB, true> : k_decode<T, DH, WR, SUB, false>;
 }
 
 template <class T, int DH, int WR>
