@@ -933,8 +933,9 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
 }
 
 // mass_out[b,t] = decay mass_in[b,t] + the token's weight in every row. A workgroup
-// takes 64 tokens, its four waves every fourth row each: the rows' sums of exponentials
-// first, J rows of each 8 lanes at a time, while the first scores are on their way.
+// takes TB tokens, and the lanes of one every (256 / TB)-th row each: the rows' sums of
+// exponentials first, J rows of each 8 lanes at a time, while the first scores are on
+// their way.
 constexpr int kMassRows = 512;
 template <int J>
 __device__ __forceinline__ void row_sums(const DecodeParams& p, int b, int64_t row0, int n, int ns, int len, float* s_lse, int* s_lim) {
@@ -956,47 +957,55 @@ __device__ __forceinline__ void row_sums(const DecodeParams& p, int b, int64_t r
       }
   }
 }
+// U: scores of a lane in flight, and as many that it works on; PH lanes share a token.
+template <int J, int U, int PH>
+__device__ __forceinline__ float add_rows(const DecodeParams& p, int b, int64_t row0, int n, int ns, int len, int t, int ph,
+                                          float sum, float* s_lse, int* s_lim) {
+  const float* px = p.x + row0 * p.x_ld + min(t, p.x_ld - 1);
+  float x[U], y[U] = {};
+#pragma unroll
+  for (int i = 0; i < U; ++i) x[i] = px[static_cast<int64_t>(min(PH * i + ph, n - 1)) * p.x_ld];
+  row_sums<J>(p, b, row0, n, ns, len, s_lse, s_lim);
+  __syncthreads();
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += PH * U) {
+    if (i0 + PH * U < n)
+#pragma unroll
+      for (int i = 0; i < U; ++i) y[i] = px[static_cast<int64_t>(min(i0 + PH * (U + i) + ph, n - 1)) * p.x_ld];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int q = i0 + PH * i + ph;
+      sum += t < s_lim[q] ? exp2_(x[i] - s_lse[q]) : 0.f;
+      x[i] = y[i];
+    }
+  }
+  return sum;
+}
+template <int TB>
 __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int nblk, char* smem) {
-  constexpr int U = 8;  // scores of a lane in flight, and as many that it works on
+  constexpr int PH = 256 / TB;
   float* s_lse = reinterpret_cast<float*>(smem);
   int* s_lim = reinterpret_cast<int*>(smem + kMassRows * 4);
   float* s_sum = reinterpret_cast<float*>(smem + kMassRows * 8);
-  const PagedCache& c = p.c;
-  const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int t0 = static_cast<int>(blk % nblk) * 64, t = t0 + lane, len = tokens_of(p, b);
+  const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, ph = tid / TB;
+  const int t0 = static_cast<int>(blk % nblk) * TB, t = t0 + tid % TB, len = tokens_of(p, b);
   if (t0 >= len) return;
-  const int ns = (len + p.chunk - 1) / p.chunk, tr = min(t, p.x_ld - 1);
-  const int64_t rows = static_cast<int64_t>(c.H) * p.R, row0 = b * rows;
+  const int ns = (len + p.chunk - 1) / p.chunk;
+  const int64_t rows = static_cast<int64_t>(p.c.H) * p.R, row0 = b * rows;
   float sum = 0.f;
   for (int64_t q0 = 0; q0 < rows; q0 += kMassRows) {
     const int n = static_cast<int>(min(rows - q0, static_cast<int64_t>(kMassRows)));
-    const float* px = p.x + (row0 + q0) * p.x_ld + tr;
-    float x[U], y[U] = {};
-#pragma unroll
-    for (int i = 0; i < U; ++i) x[i] = px[static_cast<int64_t>(min(4 * i + w, n - 1)) * p.x_ld];
     if (q0) __syncthreads();
-    if (n <= 32)
-      row_sums<1>(p, b, row0 + q0, n, ns, len, s_lse, s_lim);
-    else
-      row_sums<4>(p, b, row0 + q0, n, ns, len, s_lse, s_lim);
-    __syncthreads();
-#pragma unroll 1
-    for (int i0 = 0; i0 < n; i0 += 4 * U) {
-      if (i0 + 4 * U < n)
-#pragma unroll
-        for (int i = 0; i < U; ++i) y[i] = px[static_cast<int64_t>(min(i0 + 4 * (U + i) + w, n - 1)) * p.x_ld];
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int q = i0 + 4 * i + w;
-        sum += t < s_lim[q] ? exp2_(x[i] - s_lse[q]) : 0.f;
-        x[i] = y[i];
-      }
-    }
+    sum = n <= 32 ? add_rows<1, 32 / PH, PH>(p, b, row0 + q0, n, ns, len, t, ph, sum, s_lse, s_lim)
+                  : add_rows<4, TB == 64 ? 16 : 8, PH>(p, b, row0 + q0, n, ns, len, t, ph, sum, s_lse, s_lim);
   }
   s_sum[tid] = sum;
   __syncthreads();
-  if (w == 0 && t < len) {
-    sum = (sum + s_sum[64 + lane]) + (s_sum[128 + lane] + s_sum[192 + lane]);
+  if (ph == 0 && t < len) {
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PH; i += 4)
+      sum += (s_sum[TB * i + tid] + s_sum[TB * (i + 1) + tid]) + (s_sum[TB * (i + 2) + tid] + s_sum[TB * (i + 3) + tid]);
     const int64_t at = static_cast<int64_t>(b) * p.mass_ld + t;
     p.mass_out[at] = p.mass_in ? p.decay * p.mass_in[at] + sum : sum;
   }
@@ -1005,14 +1014,16 @@ __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int
 // What follows the splits: the first `joins` workgroups finish the outputs, the
 // others add the weights.
 template <class T, int DH>
-__global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nblk) {
+__global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nblk, int tb) {
   using L = Tile<T, DH>;
   __shared__ __attribute__((aligned(16))) char smem[L::RB + 4096 + 128];
   static_assert(sizeof(smem) >= kMassRows * 8 + 1024, "both halves fit");
   if (static_cast<int>(blockIdx.x) < joins)
     join_rows<T, DH>(p, blockIdx.x, smem);
+  else if (tb == 64)
+    add_mass<64>(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, smem);
   else
-    add_mass(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, smem);
+    add_mass<16>(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, smem);
 }
 
 // Blocks of 16 rows of a workgroup. From 17 rows on a tile of bfloat16 tokens is worth
@@ -1061,10 +1072,14 @@ hipError_t launch(DecodeParams p, hipStream_t s) {
     go<T, DH, 4>(p, s);
   else if constexpr (!share_from_17(sizeof(T) == 2, DH))
     go<T, DH, 2>(p, s);
-  const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0, nblk = p.mass_out ? (p.max_len + 63) / 64 : 0;
+  const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0;
+  // many rows and blocks of 64 tokens on half the CUs or fewer: of 16 (305 tokens and 1280
+  // rows 55 -> 35 us, two of 3447 and 528 rows 73 -> 62)
+  const int tb = static_cast<int64_t>(p.B) * ((p.max_len + 63) / 64) <= 128 && static_cast<int64_t>(p.c.H) * p.R > 128 ? 16 : 64;
+  const int nblk = p.mass_out ? (p.max_len + tb - 1) / tb : 0;
   if (joins + nblk > 0)
     hipLaunchKernelGGL((k_join<T, DH>), dim3(static_cast<unsigned>(joins) + static_cast<unsigned>(nblk) * p.B), dim3(256),
-                       0, s, p, joins, nblk);
+                       0, s, p, joins, nblk, tb);
   return hipGetLastError();
 }
 

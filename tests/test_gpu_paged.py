@@ -288,6 +288,37 @@ def test_attend_long(dtype, n):
     assert bool(((m[0].double() - w).abs() <= (2 * EPS * (dh + 8) * A + 200 * EPS + EPS * n) * w + 1e-30).all())
 
 
+@pytest.mark.parametrize("dtype,dh,rep", [(bf, 128, 1), (bf, 128, 20), (bf, 64, 20), (f32, 64, 3), (f32, 128, 33)])
+def test_attend_long_ragged(dtype, dh, rep):
+    """Splits of 2048 tokens, nine of them: most sequences end in the first, some in the last."""
+    rng, c, t, n, q = case(13, [17000], P=64, H=1, rep=rep, dh=dh, dtype=dtype)
+    lens = [0, 17000, 1, 2047, 2048, 2049, 16384, 16385, 9000, 300] + [64] * 54
+    B, top = len(lens), max(lens)
+    order = torch.stack([torch.randperm(t.shape[1], generator=torch.Generator().manual_seed(b)) for b in range(B)])
+    table = t[0].cpu()[order].to(DEV)
+    q = dev(rng.standard_normal((B, 1, rep, dh)), dtype)
+    m = torch.zeros((B, top), device=DEV)
+    out = rs.attend_paged(q, c, table, ints(lens), max_len=top, mass=m, out_dtype=f32)
+    assert not out[0].any() and not m[0].any()
+    for b in list(range(1, 11)) + [63]:
+        k = lens[b]
+        ref, size, w, A = _dense_attend(q[b:b + 1], c, table[b:b + 1], k)
+        rel = 2 * EPS * (dh + 8) * A + 2.0 ** -17 + EPS * (k + 40)
+        assert bool(((out[b, 0].double() - ref).abs() <= (rel + 2.0 ** -23) * size).all()), b
+        assert bool(((m[b, :k].double() - w).abs() <= (2 * EPS * (dh + 8) * A + (200 + k) * EPS) * w + 1e-30).all()), b
+        assert not m[b, k:].any()
+    # without the weights the keys take another way
+    assert torch.equal(out, rs.attend_paged(q, c, table, ints(lens), max_len=top, out_dtype=f32))
+
+
+@pytest.mark.parametrize("B", [2, 30])
+@pytest.mark.parametrize("dtype", [bf, f32])
+def test_attend_weights_of_many_rows(B, dtype):
+    rng, c, t, n, q = case(14, ([300, 17] * B)[:B], H=3, rep=16, Tq=13, dtype=dtype)
+    vis = ints(rng.integers(-2, 320, (B, 13)))
+    check_attend(q, c, t, n, visible=vis, mass=dev(rng.random((B, 304)), f32), decay=0.5)
+
+
 @pytest.mark.parametrize("dtype", [bf, f32])
 def test_attend_same_bits_again(dtype):
     rng, c, t, n, q = case(10, [300, 161, 5], rep=4, Tq=2, H=4, dh=128, dtype=dtype)
