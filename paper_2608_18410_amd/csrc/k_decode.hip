@@ -933,7 +933,7 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
 }
 
 // mass_out[b,t] = decay mass_in[b,t] + the token's weight in every row. A workgroup
-// takes TB tokens, and the lanes of one every (256 / TB)-th row each: the rows' sums of
+// takes `per` blocks of TB tokens, and the lanes of one every (256 / TB)-th row each: the rows' sums of
 // exponentials first, J rows of each 8 lanes at a time, while the first scores are on
 // their way.
 constexpr int kMassRows = 512;
@@ -960,13 +960,15 @@ __device__ __forceinline__ void row_sums(const DecodeParams& p, int b, int64_t r
 // U: scores of a lane in flight, and as many that it works on; PH lanes share a token.
 template <int J, int U, int PH>
 __device__ __forceinline__ float add_rows(const DecodeParams& p, int b, int64_t row0, int n, int ns, int len, int t, int ph,
-                                          float sum, float* s_lse, int* s_lim) {
+                                          bool fresh, float sum, float* s_lse, int* s_lim) {
   const float* px = p.x + row0 * p.x_ld + min(t, p.x_ld - 1);
   float x[U], y[U] = {};
 #pragma unroll
   for (int i = 0; i < U; ++i) x[i] = px[static_cast<int64_t>(min(PH * i + ph, n - 1)) * p.x_ld];
-  row_sums<J>(p, b, row0, n, ns, len, s_lse, s_lim);
-  __syncthreads();
+  if (fresh) {
+    row_sums<J>(p, b, row0, n, ns, len, s_lse, s_lim);
+    __syncthreads();
+  }
 #pragma unroll 1
   for (int i0 = 0; i0 < n; i0 += PH * U) {
     if (i0 + PH * U < n)
@@ -982,48 +984,52 @@ __device__ __forceinline__ float add_rows(const DecodeParams& p, int b, int64_t 
   return sum;
 }
 template <int TB>
-__device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int nblk, char* smem) {
+__device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int nblk, int per, char* smem) {
   constexpr int PH = 256 / TB;
   float* s_lse = reinterpret_cast<float*>(smem);
   int* s_lim = reinterpret_cast<int*>(smem + kMassRows * 4);
   float* s_sum = reinterpret_cast<float*>(smem + kMassRows * 8);
-  const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, ph = tid / TB;
-  const int t0 = static_cast<int>(blk % nblk) * TB, t = t0 + tid % TB, len = tokens_of(p, b);
-  if (t0 >= len) return;
+  const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, ph = tid / TB, len = tokens_of(p, b);
+  const int first = static_cast<int>(blk % nblk) * TB * per, end = min(len, first + TB * per);
   const int ns = (len + p.chunk - 1) / p.chunk;
   const int64_t rows = static_cast<int64_t>(p.c.H) * p.R, row0 = b * rows;
-  float sum = 0.f;
-  for (int64_t q0 = 0; q0 < rows; q0 += kMassRows) {
-    const int n = static_cast<int>(min(rows - q0, static_cast<int64_t>(kMassRows)));
-    if (q0) __syncthreads();
-    sum = n <= 32 ? add_rows<1, 32 / PH, PH>(p, b, row0 + q0, n, ns, len, t, ph, sum, s_lse, s_lim)
-                  : add_rows<4, TB == 64 ? 16 : 8, PH>(p, b, row0 + q0, n, ns, len, t, ph, sum, s_lse, s_lim);
-  }
-  s_sum[tid] = sum;
-  __syncthreads();
-  if (ph == 0 && t < len) {
-    sum = 0.f;
+#pragma unroll 1
+  for (int t0 = first; t0 < end; t0 += TB) {
+    const int t = t0 + tid % TB;
+    float sum = 0.f;
+    for (int64_t q0 = 0; q0 < rows; q0 += kMassRows) {
+      const int n = static_cast<int>(min(rows - q0, static_cast<int64_t>(kMassRows)));
+      const bool fresh = t0 == first || rows > kMassRows;
+      if (q0 || t0 > first) __syncthreads();
+      sum = n <= 32 ? add_rows<1, 32 / PH, PH>(p, b, row0 + q0, n, ns, len, t, ph, fresh, sum, s_lse, s_lim)
+                    : add_rows<4, TB == 64 ? 16 : 8, PH>(p, b, row0 + q0, n, ns, len, t, ph, fresh, sum, s_lse, s_lim);
+    }
+    s_sum[tid] = sum;
+    __syncthreads();
+    if (ph == 0 && t < len) {
+      sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < PH; i += 4)
-      sum += (s_sum[TB * i + tid] + s_sum[TB * (i + 1) + tid]) + (s_sum[TB * (i + 2) + tid] + s_sum[TB * (i + 3) + tid]);
-    const int64_t at = static_cast<int64_t>(b) * p.mass_ld + t;
-    p.mass_out[at] = p.mass_in ? p.decay * p.mass_in[at] + sum : sum;
+      for (int i = 0; i < PH; i += 4)
+        sum += (s_sum[TB * i + tid] + s_sum[TB * (i + 1) + tid]) + (s_sum[TB * (i + 2) + tid] + s_sum[TB * (i + 3) + tid]);
+      const int64_t at = static_cast<int64_t>(b) * p.mass_ld + t;
+      p.mass_out[at] = p.mass_in ? p.decay * p.mass_in[at] + sum : sum;
+    }
   }
 }
 
 // What follows the splits: the first `joins` workgroups finish the outputs, the
 // others add the weights.
 template <class T, int DH>
-__global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nblk, int tb) {
+__global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nblk, int tb, int per) {
   using L = Tile<T, DH>;
   __shared__ __attribute__((aligned(16))) char smem[L::RB + 4096 + 128];
   static_assert(sizeof(smem) >= kMassRows * 8 + 1024, "both halves fit");
   if (static_cast<int>(blockIdx.x) < joins)
     join_rows<T, DH>(p, blockIdx.x, smem);
   else if (tb == 64)
-    add_mass<64>(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, smem);
+    add_mass<64>(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, per, smem);
   else
-    add_mass<16>(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, smem);
+    add_mass<16>(p, static_cast<int64_t>(blockIdx.x) - joins, nblk, 1, smem);
 }
 
 // Blocks of 16 rows of a workgroup. From 17 rows on a tile of bfloat16 tokens is worth
@@ -1073,13 +1079,17 @@ hipError_t launch(DecodeParams p, hipStream_t s) {
   else if constexpr (!share_from_17(sizeof(T) == 2, DH))
     go<T, DH, 2>(p, s);
   const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0;
+  const int64_t blocks = static_cast<int64_t>(p.B) * ((p.max_len + 63) / 64), rows = static_cast<int64_t>(p.c.H) * p.R;
   // many rows and blocks of 64 tokens on half the CUs or fewer: of 16 (305 tokens and 1280
   // rows 55 -> 35 us, two of 3447 and 528 rows 73 -> 62)
-  const int tb = static_cast<int64_t>(p.B) * ((p.max_len + 63) / 64) <= 128 && static_cast<int64_t>(p.c.H) * p.R > 128 ? 16 : 64;
-  const int nblk = p.mass_out ? (p.max_len + tb - 1) / tb : 0;
+  const int tb = blocks <= 128 && rows > 128 ? 16 : 64;
+  // many blocks: up to eight a workgroup, for which it takes the rows' sums once (64
+  // sequences of 16384 tokens, 8 key heads of 4 rows 719 -> 705 us; 8 of 20000, 4 of 64 139 -> 141)
+  const int per = rows > kMassRows ? 1 : static_cast<int>(std::min<int64_t>(8, std::max<int64_t>(1, blocks / 1024)));
+  const int nblk = p.mass_out ? (p.max_len + tb * per - 1) / (tb * per) : 0;
   if (joins + nblk > 0)
     hipLaunchKernelGGL((k_join<T, DH>), dim3(static_cast<unsigned>(joins) + static_cast<unsigned>(nblk) * p.B), dim3(256),
-                       0, s, p, joins, nblk, tb);
+                       0, s, p, joins, nblk, tb, per);
   return hipGetLastError();
 }
 
