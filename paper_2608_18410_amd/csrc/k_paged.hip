@@ -34,7 +34,8 @@ template <> struct Piece<16> { typedef u32x4 t; };
 // A few new tokens of one page, every piece of its heads a thread's. One workgroup: sequence b, the i-th page its new tokens
 // touch, heads [blockIdx.y * hpb, ...). The page's new tokens [t0, t1) take slots
 // behind those its last cached token holds; an exclusive sum of their counts gives
-// each its first. VB: bytes of a value piece, the group's or 16.
+// each its first. VB: bytes of a value piece, the group's or 16. Bound by the chain length,
+// page, last token, copy: 64 new tokens of 32 heads (0.4 MB) 3.7 us.
 template <int VB>
 __global__ __launch_bounds__(256) void k_append_few(AppendParams p, int np, int hpb, int e) {
   __shared__ uint32_t s_mask[kMaxPage];
@@ -181,7 +182,9 @@ __device__ __forceinline__ void copy_page(const PageMap& g, const char* ksrc, in
 
 // Many new tokens, a page of them a workgroup: sequence b, the i-th page its new
 // tokens touch, HB heads. The groups of a new token lie apart in z (every G-th is
-// there), so a slot's source is its token's row and the group it holds.
+// there), so a slot's source is its token's row and the group it holds. 16 times up to 305
+// tokens of 32 heads (67 MB) 17 us, 3.9 TB/s: bound by the two exclusive sums before the copies begin
+// and then by memory.
 template <int VB, int HB>
 __global__ __launch_bounds__(256) void k_append(AppendParams p, int np, int e) {
   __shared__ PageMap g;
@@ -252,7 +255,9 @@ __global__ __launch_bounds__(256) void k_append(AppendParams p, int np, int e) {
 
 // Kept tokens into one new page. One workgroup: sequence b, its i-th new page, HB
 // heads. Each new token's source page, row and slot come from its old index; its new
-// slots from an exclusive sum over the page.
+// slots from an exclusive sum over the page. Bound by memory: 32 sequences that keep up
+// to 777 of 2048 tokens (8 heads; 146 MB) 36 us, 4.1 TB/s; 4 that keep 8192 of 131071 (210
+// MB) 48 us, 4.4.
 template <int VB, int HB>
 __global__ __launch_bounds__(256) void k_compact(CompactParams p, int np, int e) {
   __shared__ PageMap g;
