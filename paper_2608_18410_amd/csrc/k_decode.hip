@@ -865,18 +865,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 }
 
 // The maxima and sums of exponentials of J rows from their splits' statistics; `step`
-// lanes share a row's splits. The rows' loads are in flight together.
+// lanes share a row's splits. The rows' loads are in flight together, and a lane's first
+// split is read once.
 template <int J>
 __device__ __forceinline__ void join_stat(const float* const (&st)[J], int ns, int from, int step, float (&M)[J], float (&sum)[J]) {
+  float2 v[J];
 #pragma unroll
-  for (int j = 0; j < J; ++j) M[j] = -__builtin_inff(), sum[j] = 0.f;
-  for (int i = from; i < ns; i += step)
+  for (int j = 0; j < J; ++j) {
+    v[j] = float2{-__builtin_inff(), 0.f};
+    if (from < ns) v[j] = *reinterpret_cast<const float2*>(st[j] + 2 * from);
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) M[j] = v[j].x;
+  for (int i = from + step; i < ns; i += step)
 #pragma unroll
     for (int j = 0; j < J; ++j) M[j] = fmaxf(M[j], st[j][2 * i]);
   for (int o = 1; o < step; o <<= 1)
 #pragma unroll
     for (int j = 0; j < J; ++j) M[j] = fmaxf(M[j], __shfl_xor(M[j], o, kWave));
-  for (int i = from; i < ns; i += step)
+#pragma unroll
+  for (int j = 0; j < J; ++j) sum[j] = v[j].y * weight_of(v[j].x, M[j]);
+  for (int i = from + step; i < ns; i += step)
 #pragma unroll
     for (int j = 0; j < J; ++j) sum[j] += st[j][2 * i + 1] * weight_of(st[j][2 * i], M[j]);
   for (int o = 1; o < step; o <<= 1)
@@ -945,35 +954,38 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
 // their way.
 constexpr int kMassRows = 512;
 template <int J>
-__device__ __forceinline__ void row_sums(const DecodeParams& p, int b, int64_t row0, int n, int ns, int len, float* s_lse, int* s_lim) {
+__device__ __forceinline__ void row_sums(const DecodeParams& p, int b, int q1, int64_t row0, int n, int ns, int len, float* s_lse, int* s_lim) {
   const int tid = threadIdx.x;
   for (int q0 = 0; q0 < n; q0 += 32 * J) {
     const float* st[J];
     float M[J], l[J];
+    int lim[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) st[j] = p.stat + 2 * (row0 + min(q0 + 32 * j + tid / 8, n - 1)) * p.n_split;
+    for (int j = 0; j < J; ++j) {
+      const int q = min(q0 + 32 * j + tid / 8, n - 1);
+      st[j] = p.stat + 2 * (row0 + q) * p.n_split;
+      lim[j] = p.visible ? p.visible[static_cast<int64_t>(b) * p.Tq + (q1 + q) % p.R / p.rep] : len;
+    }
     join_stat<J>(st, ns, tid % 8, 8, M, l);
     if (tid % 8 == 0)
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const int q = q0 + 32 * j + tid / 8;
         s_lse[q] = M[j] + __log2f(l[j]);  // -inf where nothing was seen
-        s_lim[q] = l[j] == 0.f || q >= n ? 0
-                   : p.visible           ? p.visible[static_cast<int64_t>(b) * p.Tq + (row0 + q) % p.R / p.rep]
-                                         : len;
+        s_lim[q] = l[j] == 0.f || q >= n ? 0 : lim[j];
       }
   }
 }
 // U: scores of a lane in flight, and as many that it works on; PH lanes share a token.
 template <int J, int U, int PH>
-__device__ __forceinline__ float add_rows(const DecodeParams& p, int b, int64_t row0, int n, int ns, int len, int t, int ph,
+__device__ __forceinline__ float add_rows(const DecodeParams& p, int b, int q1, int64_t row0, int n, int ns, int len, int t, int ph,
                                           bool fresh, float sum, float* s_lse, int* s_lim) {
   const float* px = p.x + row0 * p.x_ld + min(t, p.x_ld - 1);
   float x[U], y[U] = {};
 #pragma unroll
   for (int i = 0; i < U; ++i) x[i] = px[static_cast<int64_t>(min(PH * i + ph, n - 1)) * p.x_ld];
   if (fresh) {
-    row_sums<J>(p, b, row0, n, ns, len, s_lse, s_lim);
+    row_sums<J>(p, b, q1, row0, n, ns, len, s_lse, s_lim);
     __syncthreads();
   }
 #pragma unroll 1
@@ -999,17 +1011,18 @@ __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int
   const int b = static_cast<int>(blk / nblk), tid = threadIdx.x, ph = tid / TB, len = tokens_of(p, b);
   const int first = static_cast<int>(blk % nblk) * TB * per, end = min(len, first + TB * per);
   const int ns = (len + p.chunk - 1) / p.chunk;
-  const int64_t rows = static_cast<int64_t>(p.c.H) * p.R, row0 = b * rows;
+  const int rows = p.c.H * p.R;  // at most 2^28: a launch has 16 threads a row and less than 2^32
+  const int64_t row0 = static_cast<int64_t>(b) * rows;
 #pragma unroll 1
   for (int t0 = first; t0 < end; t0 += TB) {
     const int t = t0 + tid % TB;
     float sum = 0.f;
-    for (int64_t q0 = 0; q0 < rows; q0 += kMassRows) {
-      const int n = static_cast<int>(min(rows - q0, static_cast<int64_t>(kMassRows)));
+    for (int q0 = 0; q0 < rows; q0 += kMassRows) {
+      const int n = min(rows - q0, kMassRows);
       const bool fresh = t0 == first || rows > kMassRows;
       if (q0 || t0 > first) __syncthreads();
-      sum = n <= 32 ? add_rows<1, 32 / PH, PH>(p, b, row0 + q0, n, ns, len, t, ph, fresh, sum, s_lse, s_lim)
-                    : add_rows<4, TB == 64 ? 16 : 8, PH>(p, b, row0 + q0, n, ns, len, t, ph, fresh, sum, s_lse, s_lim);
+      sum = n <= 32 ? add_rows<1, 32 / PH, PH>(p, b, q0, row0 + q0, n, ns, len, t, ph, fresh, sum, s_lse, s_lim)
+                    : add_rows<4, TB == 64 ? 16 : 8, PH>(p, b, q0, row0 + q0, n, ns, len, t, ph, fresh, sum, s_lse, s_lim);
     }
     s_sum[tid] = sum;
     __syncthreads();
@@ -1089,7 +1102,7 @@ hipError_t launch(DecodeParams p, hipStream_t s) {
   const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0;
   const int64_t blocks = static_cast<int64_t>(p.B) * ((p.max_len + 63) / 64), rows = static_cast<int64_t>(p.c.H) * p.R;
   // many rows and blocks of 64 tokens on half the CUs or fewer: of 16 (305 tokens and 1280
-  // rows 55 -> 35 us, two of 3447 and 528 rows 73 -> 62)
+  // rows 55 -> 35 us, two of 3447 and 528 rows 73 -> 55)
   const int tb = blocks <= 128 && rows > 128 ? 16 : 64;
   // many blocks: up to eight a workgroup, for which it takes the rows' sums once (64
   // sequences of 16384 tokens, 8 key heads of 4 rows 719 -> 705 us; 8 of 20000, 4 of 64 139 -> 141)
