@@ -1039,7 +1039,7 @@ __device__ __forceinline__ void add_mass(const DecodeParams& p, int64_t blk, int
 
 // What follows the splits: the first `joins` workgroups finish the outputs, the
 // others add the weights. A chain of dependent loads, 5 us for one of 305 tokens and 32
-// heads; two of 131071 read 34 MB of scores and 32 splits' sums in 18 us.
+// heads; two of 131071 read 34 MB of scores and 32 splits' sums in 21 us.
 template <class T, int DH>
 __global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nblk, int tb, int per) {
   using L = Tile<T, DH>;
