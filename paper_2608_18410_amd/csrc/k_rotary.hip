@@ -25,7 +25,7 @@ __device__ __forceinline__ void angle(int32_t pos, float f, float& c, float& s) 
 // unit u is the pieces at u*V and n + u*V (halves), or the one piece of pairs at
 // u*V (interleaved). Bound by memory: 32768 tokens of 32 + 8 heads of 128 (bf16, a
 // view of a fused projection) move 671 MB in 124 us, 5.4 TB/s; one thread per pair
-// and head (below) took 289.
+// and head took 289.
 template <class T, bool IL>
 __global__ __launch_bounds__(256) void k_rotary_rows(RotaryParams p, int chunks, int chunk) {
   constexpr int V = 16 / sizeof(T), NC = IL ? V / 2 : V, U = 4;
@@ -113,42 +113,90 @@ __global__ __launch_bounds__(256) void k_rotary_rows(RotaryParams p, int chunks,
   }
 }
 
-// Any number of pairs. One workgroup turns the heads [blockIdx.y * hpb, ...) of one token: one thread
-// per pair (and per dim past the pairs) and head.
-template <class T>
-__global__ __launch_bounds__(256) void k_rotary_any(RotaryParams p, int hpb) {
-  __shared__ float cs[kMaxPairs], sn[kMaxPairs];
-  const int64_t tok = blockIdx.x;
-  const int tid = threadIdx.x, n = p.n_pairs;
-  if (tid < n) {
-    const int ax = p.axis ? p.axis[tid] : 0;
+// Any number of pairs: a wave turns heads [hw * chunk, ...) of one token, a lane one
+// 16-byte piece of a row, with the cosines and sines of its elements in registers for
+// all heads. In halves the other elements of its pairs lie n behind or before: one more
+// load of the same row at whatever alignment, two in the piece that element n cuts. Such
+// a load may begin before the row or end past it, but stays within the rows of the
+// tensor; the first and the last token's come one by one. In pairs (IL) the piece holds
+// them. A wave has loaded a row whole before it writes it, so rows may be turned in
+// place. 32768 tokens of 32 + 8 heads of 128 (bf16) and 63 pairs in halves take 211 us, bound by
+// the loads off their alignment (the cut piece's one by one: 232; a thread for each pair
+// and head: 304); 33712 of 16 + 16 heads and 50 pairs in pairs (552 MB) 108, 5.1 TB/s.
+template <class T, bool IL>
+__global__ __launch_bounds__(256) void k_rotary_any(RotaryParams p, int chunks, int chunk) {
+  constexpr int V = 16 / sizeof(T), U = 4;
+  __shared__ float cs[4][2][kMaxPairs];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + w;
+  const int64_t tok = job / chunks;
+  if (tok >= static_cast<int64_t>(p.B) * p.T) return;
+  const int n = p.n_pairs, lpr = p.dh / V, hs = 64 / lpr;  // lanes of a row, heads of a step
+  const int hl = lane / lpr, e0 = lane % lpr * V;
+  const int h0 = static_cast<int>(job % chunks) * chunk, h1 = min(h0 + chunk, p.H + p.Hkv);
+  if (lane < n) {
+    const int ax = p.axis ? p.axis[lane] : 0;
     float c = 1.f, s = 0.f;
-    if (ax < p.n_axes) angle(p.positions[tok * p.n_axes + ax], p.inv_freq[tid], c, s);
-    cs[tid] = c;
-    sn[tid] = p.inverse ? -s : s;
+    if (ax < p.n_axes) angle(p.positions[tok * p.n_axes + ax], p.inv_freq[lane], c, s);
+    cs[w][0][lane] = c;
+    cs[w][1][lane] = p.inverse ? -s : s;
   }
-  __syncthreads();
-  const int units = p.dh - n;  // pairs, then single dims
-  const int h0 = blockIdx.y * hpb, h1 = min(h0 + hpb, p.H + p.Hkv);
-  for (int i = tid; i < (h1 - h0) * units; i += 256) {
-    const int h = h0 + i / units, u = i % units;
-    const T* src;
-    T* dst;
-    if (h < p.H) {
-      src = static_cast<const T*>(p.q) + tok * p.q_stride + static_cast<int64_t>(h) * p.dh;
-      dst = static_cast<T*>(p.q_out) + tok * p.qo_stride + static_cast<int64_t>(h) * p.dh;
-    } else {
-      src = static_cast<const T*>(p.k) + tok * p.k_stride + static_cast<int64_t>(h - p.H) * p.dh;
-      dst = static_cast<T*>(p.k_out) + tok * p.ko_stride + static_cast<int64_t>(h - p.H) * p.dh;
+  wave_lds_order();
+  float c[V], s[V];
+#pragma unroll
+  for (int x = 0; x < V; ++x) {
+    const int e = e0 + x, i = IL ? e / 2 : e < n ? e : e - n;
+    const bool on = e < 2 * n, low = IL ? e % 2 == 0 : e < n;
+    c[x] = on ? cs[w][0][on ? i : 0] : 1.f;
+    s[x] = on ? (low ? -cs[w][1][on ? i : 0] : cs[w][1][on ? i : 0]) : 0.f;
+  }
+  const bool edge = tok == 0 || tok == static_cast<int64_t>(p.B) * p.T - 1;
+  const bool low = !IL && e0 < n, high = !IL && e0 + V > n && e0 < 2 * n;  // pieces of either half
+  for (int hb = h0; hb < h1; hb += hs * U) {
+    u32x4 a[U], b[U], d[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int h = hb + i * hs + hl;
+      if (h >= h1) continue;
+      const bool isq = h < p.H;
+      const T* row = static_cast<const T*>(isq ? p.q : p.k) + tok * (isq ? p.q_stride : p.k_stride) +
+                     static_cast<int64_t>(isq ? h : h - p.H) * p.dh;
+      a[i] = *reinterpret_cast<const u32x4*>(row + e0);
+      if constexpr (!IL) {
+        b[i] = d[i] = a[i];
+        if (!edge) {
+          if (low) __builtin_memcpy(&b[i], row + e0 + n, 16);
+          if (high) __builtin_memcpy(&d[i], row + e0 - n, 16);
+        } else {
+          T* vb = reinterpret_cast<T*>(&b[i]);
+#pragma unroll
+          for (int x = 0; x < V; ++x) {
+            const int e = e0 + x;
+            vb[x] = row[e < n ? e + n : e < 2 * n ? e - n : e];
+          }
+          d[i] = b[i];
+        }
+      }
     }
-    if (u >= n) {
-      dst[n + u] = src[n + u];
-      continue;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int h = hb + i * hs + hl;
+      if (h >= h1) continue;
+      const bool isq = h < p.H;
+      T* row = static_cast<T*>(isq ? p.q_out : p.k_out) + tok * (isq ? p.qo_stride : p.ko_stride) +
+               static_cast<int64_t>(isq ? h : h - p.H) * p.dh;
+      const T* xa = reinterpret_cast<const T*>(&a[i]);
+      const T* xb = reinterpret_cast<const T*>(&b[i]);
+      const T* xd = reinterpret_cast<const T*>(&d[i]);
+      u32x4 y;
+      T* vy = reinterpret_cast<T*>(&y);
+#pragma unroll
+      for (int x = 0; x < V; ++x) {
+        const float r = tof(xa[x]) * c[x] + tof(IL ? xa[x ^ 1] : e0 + x < n ? xb[x] : xd[x]) * s[x];
+        vy[x] = e0 + x < 2 * n ? fromf<T>(r) : xa[x];
+      }
+      *reinterpret_cast<u32x4*>(row + e0) = y;
     }
-    const int a = p.interleaved ? 2 * u : u, b = p.interleaved ? 2 * u + 1 : n + u;
-    const float xa = tof(src[a]), xb = tof(src[b]), c = cs[u], s = sn[u];
-    dst[a] = fromf<T>(xa * c - xb * s);
-    dst[b] = fromf<T>(xa * s + xb * c);
   }
 }
 
@@ -157,18 +205,14 @@ void launch(const RotaryParams& p, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
   const int heads = p.H + p.Hkv;
   const size_t tok = static_cast<size_t>(p.B) * p.T;
-  if ((p.interleaved ? 2 * p.n_pairs : p.n_pairs) % V) {
-    constexpr int hpb = 16;
-    const dim3 grid(static_cast<unsigned>(tok), (heads + hpb - 1) / hpb);
-    hipLaunchKernelGGL(k_rotary_any<T>, grid, dim3(256), 0, s, p, hpb);
-    return;
-  }
   // a wave per token where there are tokens enough for every wave slot (256 CUs of
   // 16 waves and more): its cosines serve all heads; with fewer the heads are split
   const int chunk = tok >= 4096 ? heads : tok >= 1024 ? (heads + 1) / 2 : 8;
   const int chunks = (heads + chunk - 1) / chunk;
   const dim3 grid(static_cast<unsigned>((tok * chunks + 3) / 4));
-  auto kern = p.interleaved ? k_rotary_rows<T, true> : k_rotary_rows<T, false>;
+  const bool whole = (p.interleaved ? 2 * p.n_pairs : p.n_pairs) % V == 0;  // pieces lie in one half
+  auto kern = p.interleaved ? (whole ? k_rotary_rows<T, true> : k_rotary_any<T, true>)
+                            : (whole ? k_rotary_rows<T, false> : k_rotary_any<T, false>);
   hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, p, chunks, chunk);
 }
 

@@ -428,6 +428,33 @@ def test_rotary_views_and_in_place(dtype):
     assert empty[0].shape == (0, T, H, dh)
 
 
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,n", [(64, 31), (64, 30), (64, 13), (128, 63), (128, 61), (128, 50), (128, 3), (64, 2)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_odd_pairs_views_in_place(dtype, dh, n, interleaved):
+    """What lies around a row and past its pairs reaches nothing and is kept to the bit."""
+    rng = np.random.default_rng(n)
+    H, Hkv, bits = 5, 2, torch.int16 if dtype == bf else i32
+    for B, T in ((1, 1), (1, 2), (3, 7), (2, 700)):
+        qkv = dev(rng.standard_normal((B, T, (H + Hkv + 1) * dh)), dtype)
+        qkv[..., (H + Hkv) * dh:] = float("nan")
+        rows = qkv[..., :(H + Hkv) * dh].unflatten(2, (H + Hkv, dh))
+        rows[..., 2 * n:] = torch.tensor([float("nan"), -0.0, float("inf"), 1.0], device=DEV).repeat(dh)[:dh - 2 * n].to(dtype)
+        before = qkv.clone()
+        q, k = rows[:, :, :H], rows[:, :, H:]
+        pos, f = rng.integers(0, 999, (B, T, 1)), rng.random(n).astype(np.float32)
+        want = rs.rotary(q.contiguous(), k.contiguous(), ints(pos), torch.from_numpy(f).to(DEV), interleaved=interleaved)
+        rs.rotary(q, k, ints(pos), torch.from_numpy(f).to(DEV), interleaved=interleaved, out=(q, k))
+        for x, w in ((q, want[0]), (k, want[1])):
+            assert torch.equal(x.contiguous().view(bits), w.view(bits))
+        old = before[..., :(H + Hkv) * dh].unflatten(2, (H + Hkv, dh))
+        assert torch.equal(rows[..., 2 * n:].contiguous().view(bits), old[..., 2 * n:].contiguous().view(bits))
+        assert torch.equal(qkv[..., (H + Hkv) * dh:].contiguous().view(bits), before[..., (H + Hkv) * dh:].contiguous().view(bits))
+        x = num(old[..., :2 * n])
+        ref = O.rotary(x, pos, f, None, interleaved)
+        assert (np.abs(num(rows[..., :2 * n]) - ref) <= _rotary_tol(x, ref, dtype)).all()
+
+
 # ---- append --------------------------------------------------------------
 
 def _same_cache(c, cn):
