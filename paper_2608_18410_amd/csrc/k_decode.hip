@@ -224,10 +224,11 @@ __device__ __forceinline__ u32x4 request_piece(rsrc_t rv, uint32_t mask, uint32_
 // what the weights round to is relative to themselves. ok: blocks of 16 tokens that
 // are there; lim: tokens the lane's row sees, least: those all rows see. SHORT: tiles
 // that all rows see whole take a way without the comparisons (worth it where the
-// kernel is bound by such instructions; the branch costs registers).
+// kernel is bound by such instructions; the branch costs registers). Scores that are kept
+// for the tokens' weights go to px, or to lx in LDS where there is one row.
 template <class T, int DH, bool SHORT>
 __device__ __forceinline__ void soften(const DecodeParams& p, f32x4* s, uint32_t ok, int t0, int lim, int least, int end,
-                                       int r, float* px, float& m, float& l, f32x4* acc) {
+                                       int r, float* px, float* lx, float& m, float& l, f32x4* acc) {
   using L = Tile<T, DH>;
   constexpr int NB = L::NB;
   constexpr float kSlack = 8.f;
@@ -246,7 +247,11 @@ __device__ __forceinline__ void soften(const DecodeParams& p, f32x4* s, uint32_t
         s[nb][x] = see ? s[nb][x] * p.scale : -__builtin_inff();
       }
   }
-  if (p.x) {
+  if (lx) {
+    if ((threadIdx.x & 15) == 0)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) *reinterpret_cast<f32x4*>(lx + 16 * nb + 4 * g4) = s[nb];
+  } else if (px) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int t = t0 + 16 * nb + 4 * g4;
@@ -521,8 +526,8 @@ __device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len
 // ONCE: keys are loaded so that they leave the caches to other data (kOnceTokens).
 // Bound by memory from a few thousand tokens on: 64 sequences of 256 to 2048 tokens, 8
 // key heads of 4 rows (219 MB) 45 us, 4.8 TB/s; two of 131071 tokens and 32 heads (3.36
-// GB) 547 us, 6.1 TB/s, and 622 where the scores are stored for the weights, more than
-// their 33 MB explain. Below that by a chain of dependent loads (length, page, mask, key and value): one
+// GB) 547 us, 6.1 TB/s, and about 610 where the scores are stored for the weights, more
+// than their 33 MB explain. Below that by a chain of dependent loads (length, page, mask, key and value): one
 // of 305 tokens 8 us.
 template <class T, int DH, int WR, int SUB, bool ONCE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4))) void k_decode(DecodeParams p) {
@@ -577,7 +582,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 
   char* zt = smem + w * L::ZB;
   u32x2* rec = s_rec[w];
-  float* px = p.x ? p.x + ((static_cast<int64_t>(b) * c.H + h) * p.R + r) * p.x_ld : nullptr;
+  constexpr int XW = WR == 1 ? 4 : 1;
+  __shared__ __attribute__((aligned(16))) float s_x[XW][256];
+  float* px = p.x ? p.x + ((static_cast<int64_t>(b) * c.H + h) * p.R + (p.R == 1 ? 0 : r)) * p.x_ld : nullptr;
 
   float m = -__builtin_inff(), l = 0.f;
   f32x4 acc[MB];
@@ -680,7 +687,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       uint32_t ok = 0;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) ok |= now[nb] ? 1u << nb : 0u;
-      soften<T, DH, false>(p, s, ok, t0, lim, least, end, r, px, m, l, acc);
+      // one row's scores are kept in pieces of 1 KB where there are that many: two of
+      // 131071 tokens and 32 heads 645 -> 632 us, 8 of 8192 and 8 heads 50.5 -> 49, but one
+      // of 305 8.1 -> 8.6
+      constexpr int XL = TK / 4, XT = 64 / XL;  // lanes of a tile's scores, tiles of a store
+      const bool alone = WR == 1 && p.x && p.R == 1 && p.chunk >= XT * STEP;
+      soften<T, DH, false>(p, s, ok, t0, lim, least, end, r, px, alone ? s_x[w % XW] + i % XT * TK : nullptr, m, l, acc);
+      if (alone && (i % XT == XT - 1 || t0 + STEP >= end)) {
+        wave_lds_order();
+        const int k = lane / XL, t = t0 + (k - i % XT) * STEP + lane % XL * 4;
+        if (k <= i % XT && t < end) *reinterpret_cast<f32x4*>(px + t) = *reinterpret_cast<const f32x4*>(s_x[w % XW] + 4 * lane);
+      }
       weigh_tile<T, DH, 0>(zt, s, acc);
       wave_lds_order();
     }
@@ -851,7 +868,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
         s[nb] = score_step<T>(*reinterpret_cast<const u32x4*>(buf + (16 * nb + l16) * KLD + 64 * j + 16 * g4), qf[j], s[nb]);
-    soften<T, DH, true>(p, s, now, t0, lim, least, end, r, px, m, l, acc);
+    soften<T, DH, true>(p, s, now, t0, lim, least, end, r, px, nullptr, m, l, acc);
     weigh_tile<T, DH, 2>(buf + KB, s, acc);
   }
   __syncthreads();

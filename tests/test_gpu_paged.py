@@ -113,6 +113,16 @@ def test_attend_lengths(dtype, dh, G):
     check_attend(q, c, t, n, rotations(rng, 2, dh, dtype))
 
 
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_attend_one_row_keeps_weights(dtype, dh):
+    lens = EDGES + [511, 512, 513, 767, 1000, 1025, 2100]
+    rng, c, t, n, q = case(15, lens, P=32, dh=dh, dtype=dtype)
+    mass = dev(rng.random((len(lens), 2100)), f32)
+    check_attend(q, c, t, n, max_len=2100, visible=ints(rng.integers(0, 2300, (len(lens), 1))), mass=mass, decay=0.9)
+    check_attend(q[:2].contiguous(), c, t[-2:].contiguous(), n[-2:].contiguous(), max_len=2100, mass=mass[:2].contiguous())
+
+
 @pytest.mark.parametrize("P", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("dtype", [bf, f32])
 def test_attend_pages(P, dtype):
@@ -288,7 +298,8 @@ def test_attend_long(dtype, n):
     assert bool(((m[0].double() - w).abs() <= (2 * EPS * (dh + 8) * A + 200 * EPS + EPS * n) * w + 1e-30).all())
 
 
-@pytest.mark.parametrize("dtype,dh,rep", [(bf, 128, 1), (bf, 128, 20), (bf, 64, 20), (f32, 64, 3), (f32, 128, 33)])
+@pytest.mark.parametrize("dtype,dh,rep", [(bf, 128, 1), (bf, 64, 1), (f32, 64, 1), (f32, 128, 1),
+                                          (bf, 128, 20), (bf, 64, 20), (f32, 64, 3), (f32, 128, 33)])
 def test_attend_long_ragged(dtype, dh, rep):
     """Splits of 2048 tokens, nine of them: most sequences end in the first, some in the last."""
     rng, c, t, n, q = case(13, [17000], P=64, H=1, rep=rep, dh=dh, dtype=dtype)
