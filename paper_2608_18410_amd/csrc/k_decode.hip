@@ -62,18 +62,26 @@ __device__ __forceinline__ u32x4 bload16_hint(rsrc_t r, uint32_t off) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, static_cast<int>(off), 0, ONCE ? 2 : 0));
 }
 
-// Eight floats as the sum of two bf16 each.
-__device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8& hi, bf16x8& lo) {
-  u32x4 h, l;
+// Eight floats as the sum of three bf16 each: 8 of their 24 bits a part, and exact, as
+// what a part leaves is a difference of near floats (down to 2^-110, where the last part
+// leaves the range). Two parts, 17 bits, put float32 outputs off by up to 2^-16; the
+// third costs 7 % where rows share tiles (16 sequences of up to 361 tokens and 56
+// queries, 32 heads 29.2 -> 31.1 us, 8 of 305 and 305 52 -> 56.5) and nothing where
+// calls are bound by memory.
+constexpr int kParts = 3;
+__device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8 (&part)[kParts]) {
+  u32x4 v[kParts];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const f32x2 x = i < 2 ? f32x2{a[2 * i], a[2 * i + 1]} : f32x2{b[2 * i - 4], b[2 * i - 3]};
-    h[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-    const f32x2 y = {x[0] - __uint_as_float(h[i] << 16), x[1] - __uint_as_float(h[i] & 0xFFFF0000u)};
-    l[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+    f32x2 x = i < 2 ? f32x2{a[2 * i], a[2 * i + 1]} : f32x2{b[2 * i - 4], b[2 * i - 3]};
+#pragma unroll
+    for (int n = 0; n < kParts; ++n) {
+      v[n][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+      x = f32x2{x[0] - __uint_as_float(v[n][i] << 16), x[1] - __uint_as_float(v[n][i] & 0xFFFF0000u)};
+    }
   }
-  hi = __builtin_bit_cast(bf16x8, h);
-  lo = __builtin_bit_cast(bf16x8, l);
+#pragma unroll
+  for (int n = 0; n < kParts; ++n) part[n] = __builtin_bit_cast(bf16x8, v[n]);
 }
 
 // Order of N steps of R LDS reads that feed M matrix products each: the reads run A
@@ -127,8 +135,7 @@ struct Rotation {
 
 // Output rows [r0, r0 + 16) of key head h from their normalised sums u (LDS, rows of
 // RLD floats; rows past R are zero): out = R_h u on the matrix cores, R's rows as
-// the product's rows. The sums enter as two bf16 each (their rounding stays below
-// the output's), or in f32. All 256 threads.
+// the product's rows. The sums enter as bf16 parts, or in f32. All 256 threads.
 template <class T, int DH>
 __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h, int r0, const float* u,
                                             const Rotation<T, DH>& rot) {
@@ -145,13 +152,12 @@ __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h,
     for (int j = 0; j < KS; ++j) {
       const int d = (4 * j + g4) * EP;
       if constexpr (L::kBf16) {
-        bf16x8 hi, lo;
-        split_bf16(*reinterpret_cast<const f32x4*>(ur + d), *reinterpret_cast<const f32x4*>(ur + d + 4), hi, lo);
+        bf16x8 part[kParts];
+        split_bf16(*reinterpret_cast<const f32x4*>(ur + d), *reinterpret_cast<const f32x4*>(ur + d + 4), part);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          o[i] = mfma_16x16x32(__builtin_bit_cast(bf16x8, rot.a[i][j]), hi, o[i]);
-          o[i] = mfma_16x16x32(__builtin_bit_cast(bf16x8, rot.a[i][j]), lo, o[i]);
-        }
+        for (int n = 0; n < kParts; ++n)
+#pragma unroll
+          for (int i = 0; i < N; ++i) o[i] = mfma_16x16x32(__builtin_bit_cast(bf16x8, rot.a[i][j]), part[n], o[i]);
       } else {
         const f32x4 uf = *reinterpret_cast<const f32x4*>(ur + d);
 #pragma unroll
@@ -288,18 +294,17 @@ __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4
   using L = Tile<T, DH>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   if constexpr (L::kBf16) {
-    // weights as two bf16 each, so that their rounding stays below the output's
-    bf16x8 hi, lo;
-    split_bf16(s[0], s[L::NB - 1], hi, lo);
+    bf16x8 part[kParts];
+    split_bf16(s[0], s[L::NB - 1], part);
     const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb) {
       const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
       const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-      acc[mb] = mfma_16x16x32(a, hi, acc[mb]);
-      acc[mb] = mfma_16x16x32(a, lo, acc[mb]);
+#pragma unroll
+      for (int n = 0; n < kParts; ++n) acc[mb] = mfma_16x16x32(a, part[n], acc[mb]);
     }
-    if constexpr (A > 0) reads_ahead<L::MB, 2, 2, A>();
+    if constexpr (A > 0) reads_ahead<L::MB, 2, kParts, A>();
   } else {
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb)

@@ -1,0 +1,47 @@
+"""Forms of the paged routed cache's calls that larger batches, many rows and narrow
+groups take, and bounds of their numbers, on the GPU."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_18410_amd as rs
+from tests._gpu_util import DEV
+from tests.test_gpu_paged import bf, case, dev, f32, i32, ints, num, rotations  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    rs.load()
+
+
+# ---- numbers -------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,rows", [(64, 1), (128, 16), (64, 24), (128, 24), (64, 60), (128, 70)])
+@pytest.mark.parametrize("rotated", [False, True])
+@pytest.mark.parametrize("max_len", [2, 3000])
+def test_weights_hold_32_bits(dtype, dh, rows, rotated, max_len):
+    """Two tokens, of scores 0 and x in [-2, 0] and values 0 and 1: exp(x) / (1 + exp(x)). In
+    units of 2^-24, x in log2 units comes out within 3 |x log2(e)| (two constants' and the
+    product's rounding), the weight within ln(2) of that and 2 of the exponential, the sum
+    and the quotient within 1 each, and a join of splits within 3 more: 20 holds all."""
+    rng = np.random.default_rng(rows)
+    B, P = 7, 16
+    K = torch.zeros((B, 1, P, dh), dtype=dtype, device=DEV)
+    V = torch.full((B, 1, P, dh), float("nan"), dtype=dtype, device=DEV)
+    K[:, 0, 1, 0] = 1
+    V[:, 0, 0], V[:, 0, 1] = 0, 1
+    c = rs.PagedCache(K, V, torch.ones((B, P), dtype=i32, device=DEV), ints([list(range(P))] * B))
+    W = max(1, -(-max_len // P))
+    table = torch.arange(B, device=DEV, dtype=i32)[:, None].repeat(1, W).contiguous()
+    q = torch.zeros((B, 1, rows, dh), dtype=dtype, device=DEV)
+    q[..., 0] = dev(-2 * rng.random((B, 1, rows)), dtype)
+    R = torch.eye(dh, device=DEV, dtype=dtype).flip(0)[None].contiguous() if rotated else None
+    out = rs.attend_paged(q, c, table, ints([2] * B), R, scale=1.0, max_len=max_len, out_dtype=f32)
+    e = torch.exp(q[..., :1].double())
+    want = (e / (1 + e)).expand(-1, -1, -1, dh)
+    assert float(((out.double() - want).abs() / want).max()) <= 20 * 2.0 ** -24
