@@ -45,3 +45,20 @@ def test_weights_hold_32_bits(dtype, dh, rows, rotated, max_len):
     e = torch.exp(q[..., :1].double())
     want = (e / (1 + e)).expand(-1, -1, -1, dh)
     assert float(((out.double() - want).abs() / want).max()) <= 20 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,rows", [(64, 1), (128, 3), (64, 24), (128, 24)])
+@pytest.mark.parametrize("max_len", [40, 3000])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf")])
+def test_infinite_sums_are_rotated(dtype, dh, rows, max_len, bad):
+    """One infinite dim of one value that is seen: an infinity of R's sign in every dim."""
+    rng, c, t, n, q = case(21, [40, 33], rep=rows, dh=dh, G=1, kmin=1, dtype=dtype, width=-(-max_len // 16))
+    R = rotations(rng, 2, dh, dtype)
+    want = rs.attend_paged(q, c, t, n, R, max_len=max_len)
+    c.V[int(t[0, 1]), 1, int(c.slot[int(t[0, 1]), 5]), 3] = bad
+    got = rs.attend_paged(q, c, t, n, R, max_len=max_len)
+    assert (R != 0).all()
+    sign = (torch.sign(R[1, :, 3].float()) * bad).expand(rows, dh)
+    assert torch.equal(got[0, 0, rows:].float(), sign)
+    assert torch.equal(got[0, 0, :rows], want[0, 0, :rows]) and torch.equal(got[1], want[1])
