@@ -177,7 +177,16 @@ def evict_layer(cache: rs.PagedCache, table, lens, mass, keep: int, first: int, 
     """A layer's cache back to `keep` tokens a sequence: the tokens with the most
     accumulated weight, moved to the pages dst_table of dst (the caller's allocator
     then has the old ones back). Returns (the new lengths [B], their weights as wide
-    as mass with zeros for the tokens to come, the kept indices [B,keep])."""
+    as mass with zeros for the tokens to come, the kept indices [B,keep]). mass_out
+    [B,>=keep] lies apart from mass."""
+    if mass_out is not None:  # before anything is written: clearing it must not clear mass
+        if mass_out.dim() != 2 or mass_out.shape[0] != mass.shape[0] or mass_out.shape[1] < keep:
+            raise ValueError(f"mass_out: expected [{mass.shape[0]}, >= {keep}], got {list(mass_out.shape)}")
+        if mass_out.dtype is not torch.float32 or mass_out.device != mass.device or not mass_out.is_contiguous():
+            raise ValueError(f"mass_out: expected a contiguous float32 tensor on {mass.device}")
+        a, b = mass.data_ptr(), mass_out.data_ptr()
+        if a < b + mass_out.nbytes and b < a + mass.nbytes:
+            raise ValueError("mass_out overlaps mass")
     with _current_stream(stream):
         idx, n = rs.evict_tokens(mass, lens, keep, first, recent, max_len=max_len)
         if mass_out is None:

@@ -1,0 +1,44 @@
+"""decode_layer and evict_layer without a GPU: what they refuse before anything is written,
+and the order of their calls on one stream."""
+import pytest
+import torch
+
+import paper_2608_18410_amd as rs
+from paper_2608_18410_amd import pipeline
+
+i32 = torch.int32
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's calls recorded, their outputs plain tensors."""
+    done = []
+
+    def evict_tokens(mass, lens, keep, *a, **kw):
+        done.append("evict_tokens")
+        return torch.zeros((mass.shape[0], keep), dtype=i32), torch.zeros(mass.shape[0], dtype=i32)
+
+    def cache_compact(src, table, idx, n, dst, dst_table, mass, mass_out):
+        done.append("cache_compact")
+        if mass.data_ptr() == mass_out.data_ptr():
+            raise rs.RolesubError("rolesub_cache_compact", 1, "mass_in and mass_out overlap")
+        return mass_out
+
+    monkeypatch.setattr(pipeline.rs, "evict_tokens", evict_tokens)
+    monkeypatch.setattr(pipeline.rs, "cache_compact", cache_compact)
+    return done
+
+
+def test_evict_layer_refuses_before_it_clears_weights(calls):
+    base = torch.rand(3 * 40)
+    mass = base[:80].view(2, 40)
+    kept = base.clone()
+    go = lambda out, m=mass: pipeline.evict_layer(None, None, None, m, 8, 0, 0, None, None, mass_out=out)  # noqa: E731
+    for bad in (mass, base[40:].view(2, 40), base[72:120].view(2, 24), base[:80].view(2, 40)[:, :8], torch.rand(2, 7),
+                torch.rand(3, 8), torch.rand(2, 8, 1), torch.rand(2, 8, dtype=torch.float64), torch.rand(8, 2).T):
+        with pytest.raises(ValueError):
+            go(bad)
+        assert torch.equal(base, kept) and not calls
+    out = go(base[80:].view(2, 20))[1]
+    assert not out.any() and torch.equal(base[:80], kept[:80]) and calls == ["evict_tokens", "cache_compact"]
+    assert go(None)[1].shape == (2, 40)
