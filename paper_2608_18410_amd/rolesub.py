@@ -737,11 +737,17 @@ def _on_current(cur, stream, ts):
         raise ValueError(f"the stream is on cuda:{stream.device_index}, but the current device is cuda:{cur}")
 
 
-def _empty(shape, dtype, device, stream):
-    """A new tensor for a call on `stream` (None: the current one)."""
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None and t.is_cuda:
-        t.record_stream(stream)
+def _empty(shape, dtype, device, stream, output=True):
+    """A new tensor for a call on `stream` (None: the current one). It comes out of that
+    stream's memory: a block of the current stream's could still be in use by what is
+    pending there, which `stream` does not wait for. An output is the current
+    stream's as well, where the caller goes on with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if output and t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
     return t
 
 
@@ -928,7 +934,7 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
         whole = (W or 0) * cache.page
         need = attend_paged_workspace_size(cache, B, Hq, Tq, min(int(max_len), whole) if max_len else whole,
                                            mass_out is not None)
-        workspace = _empty(max(need, 1), torch.uint8, q.device, stream)
+        workspace = _empty(max(need, 1), torch.uint8, q.device, stream, output=False)
     ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
     (pq, pt, pl, pR, pv, pmi, pmo, po, pw), s = _args(stream, (
         ("q", q, dq, dt), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
@@ -960,7 +966,7 @@ def evict_tokens(mass, lens, keep: int, first: int = 0, recent: int = 0, max_len
     idx, n = out
     ml = int(max_len) if max_len else ld
     if workspace is None:
-        workspace = _empty(max(evict_workspace_size(B, ml), 1), torch.uint8, mass.device, stream)
+        workspace = _empty(max(evict_workspace_size(B, ml), 1), torch.uint8, mass.device, stream, output=False)
     ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
     (pm, pl, pi, pn, pw), s = _args(stream, (
         ("mass", mass, (B, ld), torch.float32), ("lens", lens, (B,), torch.int32), ("keep_idx", idx, (B, keep), torch.int32),

@@ -62,3 +62,38 @@ def test_infinite_sums_are_rotated(dtype, dh, rows, max_len, bad):
     sign = (torch.sign(R[1, :, 3].float()) * bad).expand(rows, dh)
     assert torch.equal(got[0, 0, rows:].float(), sign)
     assert torch.equal(got[0, 0, :rows], want[0, 0, :rows]) and torch.equal(got[1], want[1])
+
+
+# ---- streams -------------------------------------------------------------
+
+def test_calls_on_a_stream_beside_pending_work():
+    """The current stream is busy with blocks that its pool has back already: what a call
+    on another stream allocates is none of them, and its results stay as they are."""
+    rng, c, t, n, q = case(22, [300, 161], rep=2, dh=64)
+    mass = torch.rand((2, 304), device=DEV)
+    pos, f = torch.randint(0, 99, (2, 1), device=DEV, dtype=i32), torch.rand(32, device=DEV)
+    dst = rs.PagedCache(*[x.clone() for x in c.tensors()])
+
+    def calls(st):
+        m = mass.clone() if st is None else m1
+        out = rs.attend_paged(q, c, t, n, mass=m, stream=st)
+        y, _ = rs.rotary(q, None, pos, f, stream=st)
+        idx, k = rs.evict_tokens(mass, n, 40, 1, 2, stream=st)
+        return out, y, idx, k, rs.cache_compact(c, t, idx, k, dst, t, mass=mass, stream=st)
+
+    want = calls(None)
+    sizes = [max(1, x.nbytes) for x in want] + [rs.attend_paged_workspace_size(c, 2, 4, 1, 304, mass=True)]
+    m1 = mass.clone()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)  # some ms
+    for _ in range(3):
+        junk = [torch.empty(x, dtype=torch.uint8, device=DEV) for x in sizes for _ in range(4)]
+        for x in junk:
+            x.fill_(255)
+        del junk, x
+    got = calls(s)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
