@@ -225,6 +225,20 @@ def _stream(stream=None):
     return _raw_stream(_raw_device())
 
 
+def _empty(shape, dtype, device, stream, output=True):
+    """A new tensor for a call on `stream` (None: the current one). It comes out of that
+    stream's memory: a block of the current stream's could still be in use by what is
+    pending there, which `stream` does not wait for. An output is the current
+    stream's as well, where the caller goes on with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if output and t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def make_budget(mode=TOPK, k_by_type=(0, 0, 0, 0), tau=0.0, kmin=0, kmax=0) -> Budget:
     b = Budget()
     b.mode = mode
@@ -288,7 +302,7 @@ def rotate_values(v: torch.Tensor, R: torch.Tensor, out: torch.Tensor | None = N
     _need("R", R, (H, dh, dh), v.dtype)
     _need("out", out, (B, T, H, dh), v.dtype)
     _same_device(v, R, out)
-    z = torch.empty_like(v) if out is None else out
+    z = _empty(v.shape, v.dtype, v.device, stream) if out is None else out
     dims = Dims(B, T, H, dh, 1, 0)
     _check("rolesub_rotate_values", load().rolesub_rotate_values(
         ctypes.byref(dims), _code(v), _ptr(v), _ptr(R, v.dtype), _ptr(z, v.dtype), _stream(stream)))
@@ -326,7 +340,7 @@ def route(token_type: torch.Tensor, budget: Budget, G: int, h: torch.Tensor | No
     def buf(name, shape, dtype, want=True):
         if not want:
             return None
-        return o[name] if name in o else torch.empty(shape, dtype=dtype, device=dev)
+        return o[name] if name in o else _empty(shape, dtype, dev, stream)
 
     mask = buf("mask", (B, T), torch.int32)
     idx = buf("idx", (B, T, G), torch.uint8, want_idx)
@@ -338,7 +352,7 @@ def route(token_type: torch.Tensor, budget: Budget, G: int, h: torch.Tensor | No
     if scores_in is None and router is not None:
         if workspace is None:
             ws_bytes = load().rolesub_route_workspace_size(ctypes.byref(dims), ctypes.byref(desc))
-            workspace = torch.empty(max(ws_bytes, 1), dtype=torch.uint8, device=dev)
+            workspace = _empty(max(ws_bytes, 1), torch.uint8, dev, stream, output=False)
         ws_ptr, ws_bytes = _ptr(workspace), workspace.numel()
     _check("rolesub_route", load().rolesub_route(
         ctypes.byref(dims), F32 if dtype == torch.float32 else BF16,
@@ -390,8 +404,8 @@ def pack_kv(z: torch.Tensor, mask: torch.Tensor, G: int, cap: int, budget: Budge
         _need("offsets", out[0], (B, T + 1), torch.int32)
         _need("Vp", out[1], (B, H, cap, ds), z.dtype)
     _same_device(z, mask, *(out or ()))
-    offsets = torch.empty((B, T + 1), dtype=torch.int32, device=z.device) if out is None else out[0]
-    Vp = torch.empty((B, H, cap, ds), dtype=z.dtype, device=z.device) if out is None else out[1]
+    offsets = _empty((B, T + 1), torch.int32, z.device, stream) if out is None else out[0]
+    Vp = _empty((B, H, cap, ds), z.dtype, z.device, stream) if out is None else out[1]
     dims = Dims(B, T, H, dh, G, 0)
     tc = _I32x4(*type_counts) if type_counts is not None else None
     _check("rolesub_pack_kv", load().rolesub_pack_kv(
@@ -412,8 +426,8 @@ def rotate_pack(v: torch.Tensor, R: torch.Tensor, mask: torch.Tensor, G: int, ca
         _need("offsets", out[0], (B, T + 1), torch.int32)
         _need("Vp", out[1], (B, H, cap, ds), v.dtype)
     _same_device(v, R, mask, *(out or ()))
-    offsets = torch.empty((B, T + 1), dtype=torch.int32, device=v.device) if out is None else out[0]
-    Vp = torch.empty((B, H, cap, ds), dtype=v.dtype, device=v.device) if out is None else out[1]
+    offsets = _empty((B, T + 1), torch.int32, v.device, stream) if out is None else out[0]
+    Vp = _empty((B, H, cap, ds), v.dtype, v.device, stream) if out is None else out[1]
     dims = Dims(B, T, H, dh, G, 0)
     tc = _I32x4(*type_counts) if type_counts is not None else None
     _check("rolesub_rotate_pack", load().rolesub_rotate_pack(
@@ -437,7 +451,7 @@ def attend(q, k, mask, offsets, Vp, R, G: int, scale: float = 0.0, out_dtype=Non
     _need("out", out, (B, Tq, H, dh), (torch.float32, torch.bfloat16))
     _same_device(q, k, mask, offsets, Vp, R, out)
     odt = q.dtype if out_dtype is None else out_dtype
-    o = torch.empty((B, Tq, H, dh), dtype=odt, device=q.device) if out is None else out
+    o = _empty((B, Tq, H, dh), odt, q.device, stream) if out is None else out
     dims = Dims(B, T, H, dh, G, 0)
     _check("rolesub_attend", load().rolesub_attend(
         ctypes.byref(dims), _code(q), Tq, _ptr(q), _ptr(k, q.dtype), _ptr(mask), _ptr(offsets, torch.int32),
@@ -460,7 +474,7 @@ def attend_causal(q, k, mask, offsets, Vp, R, G: int, scale: float = 0.0, out_dt
     _need("out", out, (B, T, H, dh), (torch.float32, torch.bfloat16))
     _same_device(q, k, mask, offsets, Vp, R, out)
     odt = q.dtype if out_dtype is None else out_dtype
-    o = torch.empty((B, T, H, dh), dtype=odt, device=q.device) if out is None else out
+    o = _empty((B, T, H, dh), odt, q.device, stream) if out is None else out
     dims = Dims(B, T, H, dh, G, 0)
     _check("rolesub_attend_causal", load().rolesub_attend_causal(
         ctypes.byref(dims), _code(q), _ptr(q), _ptr(k, q.dtype), _ptr(mask), _ptr(offsets, torch.int32),
@@ -482,7 +496,7 @@ def retain_tokens(scores, seg_len, seg_keep, out=None, stream=None):
     lens = (ctypes.c_int32 * n)(*[int(x) for x in seg_len])
     keeps = (ctypes.c_int32 * n)(*[int(x) for x in seg_keep])
     K = int(sum(seg_keep))
-    o = torch.empty((B, K), dtype=torch.int32, device=scores.device) if out is None else out
+    o = _empty((B, K), torch.int32, scores.device, stream) if out is None else out
     _check("rolesub_retain_tokens", load().rolesub_retain_tokens(
         B, N, n, lens, keeps, _ptr(scores, torch.float32), _ptr(o, torch.int32), _stream(stream)))
     return o
@@ -497,7 +511,7 @@ def gather_tokens(x, idx, out=None, stream=None):
     K = idx.shape[1]
     _need("out", out, (B, K) + tuple(x.shape[2:]), x.dtype)
     _same_device(x, idx, out)
-    o = torch.empty((B, K) + tuple(x.shape[2:]), dtype=x.dtype, device=x.device) if out is None else out
+    o = _empty((B, K) + tuple(x.shape[2:]), x.dtype, x.device, stream) if out is None else out
     row_bytes = x[0, 0].numel() * x.element_size() if N else 0
     _check("rolesub_gather_tokens", load().rolesub_gather_tokens(
         B, N, K, row_bytes, _ptr(idx, torch.int32), _ptr(x), _ptr(o), _stream(stream)))
@@ -524,7 +538,7 @@ def allocate_groups(priority, token_type, k_by_type, G: int, scores=None, *, wan
     def buf(name, shape, dtype, want=True):
         if not want:
             return None
-        return o[name] if name in o else torch.empty(shape, dtype=dtype, device=dev)
+        return o[name] if name in o else _empty(shape, dtype, dev, stream)
 
     sel = scores is not None
     kk = buf("k", (B, T), torch.uint8, want_k)
@@ -570,7 +584,7 @@ def route_allocate(token_type, k_by_type, G: int, h, router: Router, w_pri, *, w
     def buf(name, shape, dtype, want=True):
         if not want:
             return None
-        return o[name] if name in o else torch.empty(shape, dtype=dtype, device=dev)
+        return o[name] if name in o else _empty(shape, dtype, dev, stream)
 
     mask = buf("mask", (B, T), torch.int32)
     idx = buf("idx", (B, T, G), torch.uint8, want_idx)
@@ -582,7 +596,7 @@ def route_allocate(token_type, k_by_type, G: int, h, router: Router, w_pri, *, w
     desc = router.desc()
     if workspace is None:
         ws_bytes = load().rolesub_route_allocate_workspace_size(ctypes.byref(dims), ctypes.byref(desc))
-        workspace = torch.empty(max(ws_bytes, 1), dtype=torch.uint8, device=dev)
+        workspace = _empty(max(ws_bytes, 1), torch.uint8, dev, stream, output=False)
     kby = _I32x4(*[int(x) for x in k_by_type])
     _check("rolesub_route_allocate", load().rolesub_route_allocate(
         ctypes.byref(dims), F32 if h.dtype == torch.float32 else BF16, ctypes.byref(desc), _ptr(w_pri, h.dtype),
@@ -606,7 +620,7 @@ def full_transpose(R, out=None, stream=None):
     _need("R", R, (n, n))
     _need("out", out, (n, n), R.dtype)
     _same_device(R, out)
-    Rt = torch.empty_like(R) if out is None else out
+    Rt = _empty(R.shape, R.dtype, R.device, stream) if out is None else out
     _check("rolesub_full_transpose", load().rolesub_full_transpose(n, _code(R), _ptr(R), _ptr(Rt, R.dtype),
                                                                    _stream(stream)))
     return Rt
@@ -626,11 +640,11 @@ def full_rotate_pack(v, Rt, mask, S: int, cap: int, budget: Budget | None = None
     _need_workspace(workspace)
     _same_device(v, Rt, mask, workspace, *(out or ()))
     if out is None:
-        out = (torch.empty((B, T + 1), dtype=torch.int32, device=v.device),
-               torch.empty((B, cap, dv // S), dtype=v.dtype, device=v.device))
+        out = (_empty((B, T + 1), torch.int32, v.device, stream),
+               _empty((B, cap, dv // S), v.dtype, v.device, stream))
     offsets, Vp = out
     if workspace is None:
-        workspace = torch.empty(max(full_workspace_size(B, T, S), 1), dtype=torch.uint8, device=v.device)
+        workspace = _empty(max(full_workspace_size(B, T, S), 1), torch.uint8, v.device, stream, output=False)
     tc = _I32x4(*[int(x) for x in type_counts]) if type_counts is not None else None
     dims = Dims(B, T, H, dh, S, 0)
     _check("rolesub_full_rotate_pack", load().rolesub_full_rotate_pack(
@@ -654,9 +668,9 @@ def full_values(R, mask, offsets, Vp, S: int, H: int, workspace=None, out=None, 
     _need("out", out, (B, H, T, dh), Vp.dtype)
     _need_workspace(workspace)
     _same_device(Vp, offsets, R, mask, out, workspace)
-    Vh = torch.empty((B, H, T, dh), dtype=Vp.dtype, device=Vp.device) if out is None else out
+    Vh = _empty((B, H, T, dh), Vp.dtype, Vp.device, stream) if out is None else out
     if workspace is None:
-        workspace = torch.empty(max(full_workspace_size(B, T, S), 1), dtype=torch.uint8, device=Vp.device)
+        workspace = _empty(max(full_workspace_size(B, T, S), 1), torch.uint8, Vp.device, stream, output=False)
     dims = Dims(B, T, H, dh, S, 0)
     _check("rolesub_full_values", load().rolesub_full_values(
         ctypes.byref(dims), _code(Vp), _ptr(R, Vp.dtype), _ptr(mask), _ptr(offsets, torch.int32), _ptr(Vp),
@@ -675,7 +689,7 @@ def attend_values(q, k, V, scale: float = 0.0, out_dtype=None, out=None, stream=
     _need("out", out, (B, Tq, H, dh), (torch.float32, torch.bfloat16))
     _same_device(q, k, V, out)
     od = out.dtype if out is not None else (out_dtype or q.dtype)
-    o = torch.empty((B, Tq, H, dh), dtype=od, device=q.device) if out is None else out
+    o = _empty((B, Tq, H, dh), od, q.device, stream) if out is None else out
     dims = Dims(B, T, H, dh, 1, 0)
     _check("rolesub_attend_values", load().rolesub_attend_values(
         ctypes.byref(dims), _code(q), Tq, _ptr(q), _ptr(k, q.dtype), _ptr(V, q.dtype), ctypes.c_float(scale),
@@ -735,20 +749,6 @@ def _on_current(cur, stream, ts):
             raise ValueError(f"tensors on {t.device}, but the current device is cuda:{cur}")
     if stream is not None and stream.device_index != cur:
         raise ValueError(f"the stream is on cuda:{stream.device_index}, but the current device is cuda:{cur}")
-
-
-def _empty(shape, dtype, device, stream, output=True):
-    """A new tensor for a call on `stream` (None: the current one). It comes out of that
-    stream's memory: a block of the current stream's could still be in use by what is
-    pending there, which `stream` does not wait for. An output is the current
-    stream's as well, where the caller goes on with it."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if output and t.is_cuda:
-        t.record_stream(torch.cuda.current_stream(t.device))
-    return t
 
 
 def _rows(name, t):

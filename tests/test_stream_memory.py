@@ -58,3 +58,38 @@ def allocations(monkeypatch, call):
 def test_paged_calls_allocate_on_their_stream(monkeypatch, name):
     got = allocations(monkeypatch, PAGED[name])
     assert got and all(got)
+
+
+def _router():
+    d, C, G, d_e, Hr = 32, 3, 8, 4, 16
+    return rs.Router.mlp2(*(z(*x) for x in ((C, d), (C,), (C, d_e), (Hr, 2 * d + d_e), (Hr,), (G, Hr), (G,))))
+
+
+def _prefix_calls():
+    B, T, H, dh, G, S = 2, 6, 2, 64, 8, 4
+    q, v, R = z(B, T, H, dh), z(B, T, H, dh), z(H, dh, dh)
+    mask, off, vp = z(B, T, dtype=i32), z(B, T + 1, dtype=i32), z(B, H, T * G, dh // G)
+    types, h, budget = z(B, T, dtype=u8), z(B, T, 32), rs.make_budget(rs.TOPK, (4,) * 4)
+    Rw, vpw = z(H * dh, H * dh), z(B, T * S, H * dh // S)
+    return {
+        "rotate_values": lambda s: rs.rotate_values(v, R, stream=s),
+        "route": lambda s: rs.route(types, budget, G, h=h, router=_router(), stream=s),
+        "pack_kv": lambda s: rs.pack_kv(v, mask, G, T * G, stream=s),
+        "rotate_pack": lambda s: rs.rotate_pack(v, R, mask, G, T * G, stream=s),
+        "attend": lambda s: rs.attend(q, q, mask, off, vp, R, G, stream=s),
+        "attend_causal": lambda s: rs.attend_causal(q, q, mask, off, vp, R, G, stream=s),
+        "retain_tokens": lambda s: rs.retain_tokens(z(B, 9, dtype=f32), (9,), (4,), stream=s),
+        "gather_tokens": lambda s: rs.gather_tokens(q, z(B, 3, dtype=i32), stream=s),
+        "allocate_groups": lambda s: rs.allocate_groups(z(B, T, dtype=f32), types, (4,) * 4, G, z(B, T, G, dtype=f32), stream=s),
+        "route_allocate": lambda s: rs.route_allocate(types, (4,) * 4, G, h, _router(), z(3), stream=s),
+        "full_transpose": lambda s: rs.full_transpose(Rw, stream=s),
+        "full_rotate_pack": lambda s: rs.full_rotate_pack(v, Rw, mask, S, T * S, stream=s),
+        "full_values": lambda s: rs.full_values(Rw, mask, off, vpw, S, H, stream=s),
+        "attend_values": lambda s: rs.attend_values(q, q, z(B, H, T, dh), stream=s),
+    }
+
+
+@pytest.mark.parametrize("name", list(_prefix_calls()))
+def test_prefix_calls_allocate_on_their_stream(monkeypatch, name):
+    got = allocations(monkeypatch, _prefix_calls()[name])
+    assert got and all(got)
