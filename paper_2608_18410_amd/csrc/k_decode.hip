@@ -1173,7 +1173,7 @@ DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass) {
   d.x_ld = (max_len + 3) / 4 * 4;
   const size_t rows = static_cast<size_t>(B) * H * R, cells = rows * d.n_split;
   d.off_stat = d.n_split > 1 ? up256(cells * dh * 4) : 0;
-  d.off_x = d.off_stat + (d.n_split > 1 || mass ? up256(cells * 8) : 0);
+  d.off_x = d.off_stat + (d.n_split > 1 || (mass && max_len > 0) ? up256(cells * 8) : 0);
   d.bytes = d.off_x + (mass ? up256(rows * d.x_ld * 4) : 0);
   // what to ask a caller for: a bound on the above that does not fall as B, Tq or
   // max_len grows (n_split <= kSplitWgs / wgs + 1, or for splits of kLongUnits and more

@@ -64,6 +64,24 @@ def test_infinite_sums_are_rotated(dtype, dh, rows, max_len, bad):
     assert torch.equal(got[0, 0, :rows], want[0, 0, :rows]) and torch.equal(got[1], want[1])
 
 
+# ---- smallest calls ------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("rows", [1, 24, 40])
+def test_empty_tables(dtype, rows):
+    """No page a sequence: zeros, and no weight written."""
+    rng, c, t, n, q = case(23, [5, 0, 30], rep=rows, dh=128, dtype=dtype)
+    none = t[:, :0].contiguous()
+    R = rotations(rng, 2, 128, dtype)
+    for ld in (0, 9):
+        mass = torch.full((3, ld), 7.0, device=DEV)
+        for kw in ({}, dict(mass=mass), dict(mass_out=mass), dict(mass=mass, max_len=5)):
+            out = rs.attend_paged(q, c, none, n, R, **kw)
+            assert not out.any() and (mass == 7).all()
+    one = torch.zeros((3, 1), device=DEV)
+    assert not rs.attend_paged(q, c, t, n * 0, R, max_len=1, mass=one).any() and not one.any()
+
+
 # ---- streams -------------------------------------------------------------
 
 def test_calls_on_a_stream_beside_pending_work():

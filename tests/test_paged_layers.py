@@ -1,5 +1,7 @@
 """decode_layer and evict_layer without a GPU: what they refuse before anything is written,
-and the order of their calls on one stream."""
+and calls of the C ABI on empty inputs."""
+import ctypes
+
 import pytest
 import torch
 
@@ -42,3 +44,19 @@ def test_evict_layer_refuses_before_it_clears_weights(calls):
     out = go(base[80:].view(2, 20))[1]
     assert not out.any() and torch.equal(base[:80], kept[:80]) and calls == ["evict_tokens", "cache_compact"]
     assert go(None)[1].shape == (2, 40)
+
+
+def test_an_empty_table_needs_no_workspace_for_weights():
+    """The smallest calls: no page a sequence. What the size query answers is enough; here the
+    launch that follows finds no device, on the GPU the outputs are zeros."""
+    lib, a = rs.load(), ctypes.c_void_p(0x10000000)
+    for mp, ml in ((0, 0), (0, 7)):
+        pg = rs.PagesDesc(5, 16, 64, 2, 64, 8, a, a, a, a)
+        need = lib.rolesub_attend_paged_workspace_size(ctypes.byref(pg), 3, 4, 1, 0, 1)
+        assert need == 0
+        if torch.cuda.is_available():
+            continue
+        st = lib.rolesub_attend_paged(ctypes.byref(pg), rs.BF16, 3, 4, 1, a, 0, None, mp, a, None, ml, None, 0.0,
+                                      ctypes.c_void_p(0x20000000), rs.BF16, None, 1.0, ctypes.c_void_p(0x30000000), 0, None, 0,
+                                      None)
+        assert "workspace" not in lib.rolesub_last_error().decode() and st != 1
