@@ -8,6 +8,7 @@ namespace rolesub {
 namespace {
 
 constexpr int kMaxPairs = 64;
+constexpr float kStays = 2.f;  // in a cosine's place: no axis turns the pair
 
 // cos and sin of pos * f. The product of a 31-bit integer and a 24-bit float and its
 // share of a turn are held in two doubles each, and whole turns are taken off before
@@ -46,7 +47,8 @@ __global__ __launch_bounds__(256) void k_rotary_rows(RotaryParams p, int chunks,
     return static_cast<char*>(const_cast<void*>(base)) + (tok * st + static_cast<int64_t>(isq ? h : h - p.H) * p.dh) * sizeof(T);
   };
   float c[NC] = {}, s[NC] = {};
-  bool first = true;
+  uint32_t stay = 0;  // pairs that no axis turns: copied (a zero times what is not finite would reach the other)
+  bool first = true, some = false;
   for (int hb = h0; hb < h1; hb += hs * U) {
     u32x4 a[U], b[U];
 #pragma unroll
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(256) void k_rotary_rows(RotaryParams p, int chunks,
       first = false;
       if (lane < n) {
         const int ax = p.axis ? p.axis[lane] : 0;
-        float cc = 1.f, ss = 0.f;
+        float cc = kStays, ss = 0.f;
         if (ax < p.n_axes) angle(p.positions[tok * p.n_axes + ax], p.inv_freq[lane], cc, ss);
         cs[w][0][lane] = cc;
         cs[w][1][lane] = p.inverse ? -ss : ss;
@@ -77,7 +79,9 @@ __global__ __launch_bounds__(256) void k_rotary_rows(RotaryParams p, int chunks,
           c[x + 1] = cv.y;
           s[x] = sv.x;
           s[x + 1] = sv.y;
+          stay |= (cv.x == kStays ? 1u << x : 0u) | (cv.y == kStays ? 2u << x : 0u);
         }
+      some = __any(stay != 0u);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -99,6 +103,19 @@ __global__ __launch_bounds__(256) void k_rotary_rows(RotaryParams p, int chunks,
         } else {
           va[x] = fromf<T>(r0);
           vb[x] = fromf<T>(r1);
+        }
+      }
+      if (some) {
+#pragma unroll
+        for (int x = 0; x < NC; ++x) {
+          if (!((stay >> x) & 1u)) continue;
+          if constexpr (IL) {
+            va[2 * x] = xa[2 * x];
+            va[2 * x + 1] = xa[2 * x + 1];
+          } else {
+            va[x] = xa[x];
+            vb[x] = xb[x];
+          }
         }
       }
       *reinterpret_cast<u32x4*>(y + oa * sizeof(T)) = ya;
@@ -136,19 +153,21 @@ __global__ __launch_bounds__(256) void k_rotary_any(RotaryParams p, int chunks, 
   const int h0 = static_cast<int>(job % chunks) * chunk, h1 = min(h0 + chunk, p.H + p.Hkv);
   if (lane < n) {
     const int ax = p.axis ? p.axis[lane] : 0;
-    float c = 1.f, s = 0.f;
+    float c = kStays, s = 0.f;
     if (ax < p.n_axes) angle(p.positions[tok * p.n_axes + ax], p.inv_freq[lane], c, s);
     cs[w][0][lane] = c;
     cs[w][1][lane] = p.inverse ? -s : s;
   }
   wave_lds_order();
   float c[V], s[V];
+  uint32_t turn = 0;  // elements that are turned; the others are copied
 #pragma unroll
   for (int x = 0; x < V; ++x) {
     const int e = e0 + x, i = IL ? e / 2 : e < n ? e : e - n;
-    const bool on = e < 2 * n, low = IL ? e % 2 == 0 : e < n;
+    const bool on = e < 2 * n && cs[w][0][e < 2 * n ? i : 0] != kStays, low = IL ? e % 2 == 0 : e < n;
     c[x] = on ? cs[w][0][on ? i : 0] : 1.f;
     s[x] = on ? (low ? -cs[w][1][on ? i : 0] : cs[w][1][on ? i : 0]) : 0.f;
+    turn |= on ? 1u << x : 0u;
   }
   const bool edge = tok == 0 || tok == static_cast<int64_t>(p.B) * p.T - 1;
   const bool low = !IL && e0 < n, high = !IL && e0 + V > n && e0 < 2 * n;  // pieces of either half
@@ -193,7 +212,7 @@ __global__ __launch_bounds__(256) void k_rotary_any(RotaryParams p, int chunks, 
 #pragma unroll
       for (int x = 0; x < V; ++x) {
         const float r = tof(xa[x]) * c[x] + tof(IL ? xa[x ^ 1] : e0 + x < n ? xb[x] : xd[x]) * s[x];
-        vy[x] = e0 + x < 2 * n ? fromf<T>(r) : xa[x];
+        vy[x] = (turn >> x) & 1u ? fromf<T>(r) : xa[x];
       }
       *reinterpret_cast<u32x4*>(row + e0) = y;
     }

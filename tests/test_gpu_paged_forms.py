@@ -64,6 +64,35 @@ def test_infinite_sums_are_rotated(dtype, dh, rows, max_len, bad):
     assert torch.equal(got[0, 0, :rows], want[0, 0, :rows]) and torch.equal(got[1], want[1])
 
 
+# ---- rotary --------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,pairs", [(64, 32), (128, 64), (128, 24), (64, 13), (128, 63)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens", [3, 1025, 4097])
+def test_pairs_of_no_axis_are_copied(dtype, dh, pairs, interleaved, tokens):
+    """Infinities, NaN and zeros of either sign in pairs whose axis is none stay where they are."""
+    rng = np.random.default_rng(pairs)
+    bits = torch.int16 if dtype == bf else i32
+    q = dev(rng.standard_normal((1, tokens, 3, dh)), dtype)
+    ax = rng.integers(0, 2, pairs).astype(np.uint8)
+    still = rng.random(pairs) < 0.4
+    still[0] = True
+    ax[still] = rng.choice([2, 7, 255], int(still.sum()))
+    i = torch.from_numpy(np.nonzero(still)[0]).to(DEV)
+    a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + pairs)
+    odd = torch.tensor([float("inf"), float("-inf"), -0.0, 0.0, 1.5], device=DEV, dtype=dtype)
+    for e in (a, b):
+        q[..., e] = odd[torch.randint(0, 5, (1, tokens, 3, len(e)), device=DEV)]
+    pos, f = torch.randint(1, 999, (1, tokens, 2), device=DEV, dtype=i32), torch.rand(pairs, device=DEV) + 0.01
+    y, _ = rs.rotary(q, None, pos, f, torch.from_numpy(ax).to(DEV), interleaved=interleaved)
+    for e in (a, b):
+        assert torch.equal(y[..., e].contiguous().view(bits), q[..., e].contiguous().view(bits))
+    rest = torch.ones(dh, dtype=torch.bool, device=DEV)
+    rest[a], rest[b] = False, False
+    assert torch.isfinite(y[..., rest]).all()
+
+
 # ---- smallest calls ------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [bf, f32])
