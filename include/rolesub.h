@@ -452,8 +452,8 @@ typedef struct rolesub_pages {
  *   or NULL (all axis 0); a pair whose axis is >= n_axes is not turned.
  *   q_out, k_out: dense, or the input itself (same pointer, then the same
  *   stride is used); otherwise no output overlaps another tensor of the call.
- * Whole turns are taken off the angles in more than 64 bits: positions of any size
- * lose nothing.
+ * Whole turns are taken off the angles in two doubles: nothing is lost while
+ * |positions * inv_freq| stays below 2^75.
  * ------------------------------------------------------------------------ */
 rolesub_status rolesub_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int32_t dh, rolesub_dtype dtype,
                               const void* q, int64_t q_stride, const void* k, int64_t k_stride,

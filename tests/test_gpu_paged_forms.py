@@ -5,8 +5,9 @@ import pytest
 import torch
 
 import paper_2608_18410_amd as rs
+from oracle import paged as O
 from tests._gpu_util import DEV
-from tests.test_gpu_paged import bf, case, dev, f32, i32, ints, num, rotations  # noqa: F401
+from tests.test_gpu_paged import _rotary_tol, bf, case, dev, f32, i32, ints, num, rotations  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -91,6 +92,19 @@ def test_pairs_of_no_axis_are_copied(dtype, dh, pairs, interleaved, tokens):
     rest = torch.ones(dh, dtype=torch.bool, device=DEV)
     rest[a], rest[b] = False, False
     assert torch.isfinite(y[..., rest]).all()
+
+
+def test_far_angles():
+    """Products of position and frequency up to 2^75, which the oracle's long doubles hold."""
+    rng = np.random.default_rng(3)
+    T, n, dh = 400, 32, 64
+    x = dev(rng.standard_normal((1, T, 2, dh)), f32)
+    pos = rng.integers(-2 ** 31, 2 ** 31, (1, T, 1))
+    f = (2.0 ** rng.uniform(-20, 44, n)).astype(np.float32)
+    for inverse in (False, True):
+        y, _ = rs.rotary(x, None, ints(pos), torch.from_numpy(f).to(DEV), inverse=inverse)
+        ref = O.rotary(num(x), pos, f, inverse=inverse)
+        assert (np.abs(num(y) - ref) <= _rotary_tol(num(x), ref, f32)).all()
 
 
 # ---- smallest calls ------------------------------------------------------
