@@ -926,7 +926,7 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
   constexpr int Q = DH / 4;  // 16-byte pieces of a row
   float* u = reinterpret_cast<float*>(smem);                      // [16][RLD]
   f32x4* red = reinterpret_cast<f32x4*>(smem + L::RB);            // [256]
-  float* s_M = reinterpret_cast<float*>(smem + L::RB + 4096);     // [16] maxima, [16] inverse sums
+  float* s_M = reinterpret_cast<float*>(smem + L::RB + 4096);     // [16] maxima, [16] sums
   const PagedCache& c = p.c;
   const int nrb = (p.R + 15) / 16, tid = threadIdx.x;
   const int r0 = static_cast<int>(blk % nrb) * 16, h = static_cast<int>(blk / nrb % c.H), b = static_cast<int>(blk / nrb / c.H);
@@ -941,7 +941,7 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
     join_stat(st, ns, tid % 16, 16, M, sum);
     if (tid % 16 == 0) {
       s_M[row] = M[0];
-      s_M[16 + row] = sum[0] == 0.f || row >= nr ? 0.f : 1.f / sum[0];
+      s_M[16 + row] = row >= nr ? 0.f : sum[0];
     }
   }
   __syncthreads();
@@ -963,12 +963,12 @@ __device__ __forceinline__ void join_rows(const DecodeParams& p, int64_t blk, ch
       __syncthreads();
       if (tid < items)
         for (int v = 1; v < groups; ++v) a += red[tid + v * items];
-      if (tid < items) *reinterpret_cast<f32x4*>(u + row * L::RLD + 4 * d) = s_M[16 + row] == 0.f ? f32x4{0, 0, 0, 0} : a * s_M[16 + row];
+      if (tid < items) *reinterpret_cast<f32x4*>(u + row * L::RLD + 4 * d) = s_M[16 + row] == 0.f ? f32x4{0, 0, 0, 0} : a / s_M[16 + row];
       for (int z = tid; z < (16 - nr) * Q; z += 256)
         *reinterpret_cast<f32x4*>(u + (nr + z / Q) * L::RLD + z % Q * 4) = f32x4{0, 0, 0, 0};
       break;
     }
-    *reinterpret_cast<f32x4*>(u + row * L::RLD + 4 * d) = s_M[16 + row] == 0.f ? f32x4{0, 0, 0, 0} : a * s_M[16 + row];
+    *reinterpret_cast<f32x4*>(u + row * L::RLD + 4 * d) = s_M[16 + row] == 0.f ? f32x4{0, 0, 0, 0} : a / s_M[16 + row];
   }
   __syncthreads();
   finish_rows<T, DH>(p, b, h, r0, u, rot);

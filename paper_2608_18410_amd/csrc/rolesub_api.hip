@@ -1072,7 +1072,8 @@ rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dt
   p.lens = lens;
   p.visible = visible;
   p.Rm = R;
-  p.scale = (scale == 0.f ? 1.f / std::sqrt(static_cast<float>(p.c.dh)) : scale) * 1.44269504088896341f;
+  // rounded once
+  p.scale = static_cast<float>((scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(p.c.dh)) : scale) * 1.44269504088896341);
   p.out = out;
   p.out_f32 = out_dtype == ROLESUB_F32;
   p.mass_in = decay == 0.f ? nullptr : mass_in;

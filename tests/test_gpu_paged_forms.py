@@ -49,6 +49,21 @@ def test_weights_hold_32_bits(dtype, dh, rows, rotated, max_len):
 
 
 @pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,rows", [(64, 1), (128, 3), (64, 40), (128, 24)])
+@pytest.mark.parametrize("max_len", [304, 3000])
+def test_equal_weights_of_ones_give_one(dtype, dh, rows, max_len):
+    """n tokens of score 0 and value 1: the sums are n exactly, and n / n is 1."""
+    lens = list(range(304))
+    P = 16
+    c = rs.PagedCache(torch.randn((19, 1, P, dh), device=DEV).to(dtype), torch.ones((19, 1, P, dh), dtype=dtype, device=DEV),
+                      torch.ones((19, P), dtype=i32, device=DEV), ints([list(range(P))] * 19))
+    table = torch.arange(-(-max_len // P), device=DEV, dtype=i32).expand(304, -1).contiguous()
+    out = rs.attend_paged(torch.zeros((304, 1, rows, dh), dtype=dtype, device=DEV), c, table, ints(lens), max_len=max_len,
+                          out_dtype=f32)
+    assert not out[0].any() and (out[1:] == 1).all()
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
 @pytest.mark.parametrize("dh,rows", [(64, 1), (128, 3), (64, 24), (128, 24)])
 @pytest.mark.parametrize("max_len", [40, 3000])
 @pytest.mark.parametrize("bad", [float("inf"), float("-inf")])
