@@ -488,7 +488,8 @@ rolesub_status rolesub_cache_append(const rolesub_pages* pages, rolesub_dtype dt
  *   visible [B,Tq] int32 or NULL: tokens each query sees (NULL: all);
  *   max_len: no token past it is seen (0: max_pages*page). It sizes the launch
  *   and the workspace, so a bound near the longest sequence is fastest.
- *   out [B,Tq,Hq,dh] dense in out_dtype (f32 or the call's dtype).
+ *   out [B,Tq,Hq,dh] dense in out_dtype (f32 or the call's dtype); it may be q
+ *   itself where that is dense and of the same type.
  * A query that sees no token, or whose tokens all score -inf, gives zeros. What
  * a query does not see does not reach it, infinities and NaN included.
  * Accumulated attention weight of every cached token (mass_out non-NULL):
@@ -499,8 +500,9 @@ rolesub_status rolesub_cache_append(const rolesub_pages* pages, rolesub_dtype dt
  * workspace: at least rolesub_attend_paged_workspace_size() bytes (which does
  * not fall as B, Tq or max_len grows; max_len is not 0 there), 16-byte
  * aligned; nothing in it needs clearing; calls (and graphs) that may overlap
- * must not share one. Results do not depend on the other sequences of a call
- * of the same B, Tq and max_len.
+ * must not share one. No output and no part of the workspace lies in another
+ * operand, except as above. Results do not depend on the other sequences of a
+ * call of the same B, Tq and max_len.
  * ------------------------------------------------------------------------ */
 size_t rolesub_attend_paged_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq,
                                            int32_t max_len, int32_t with_mass);

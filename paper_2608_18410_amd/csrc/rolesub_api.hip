@@ -5,6 +5,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 
@@ -917,6 +918,21 @@ bool rows_overlap(const void* a, int64_t sa, int64_t ra, const void* b, int64_t 
   return d < ra * static_cast<int64_t>(e) || d + rb * static_cast<int64_t>(e) > row;
 }
 
+// Whether the outputs of a call lie apart from each other and from its inputs (NULL: absent).
+struct Operand {
+  const char* name;
+  const void* p;
+  size_t bytes;
+};
+rolesub_status apart(const char* fn, std::initializer_list<Operand> outs, std::initializer_list<Operand> ins) {
+  for (const Operand* o = outs.begin(); o != outs.end(); ++o)
+    for (int side = 0; side < 2; ++side)
+      for (const Operand* x = side ? ins.begin() : o + 1; x != (side ? ins.end() : outs.end()); ++x)
+        if (o->p && x->p && o->bytes && x->bytes && ranges_overlap(o->p, o->bytes, x->p, x->bytes))
+          return fail(ROLESUB_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, o->name, x->name);
+  return ROLESUB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1088,6 +1104,21 @@ rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dt
   if (static_cast<size_t>(B) * p.c.H * d.n_split * ((p.R + 15) / 16) * 256 >= kMaxThreads ||
       (static_cast<size_t>(B) * p.c.H * ((p.R + 15) / 16) + static_cast<size_t>(B) * (p.max_len / 64 + 1)) * 256 >= kMaxThreads)
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads or queries", fn);
+  const size_t e = esize(dtype), nq = static_cast<size_t>(B) * Tq, qrow = static_cast<size_t>(Hq) * p.c.dh,
+               np = static_cast<size_t>(p.c.n_pages), nm = ((static_cast<size_t>(B) - 1) * mass_ld + ml) * 4;
+  const size_t nout = nq * qrow * (p.out_f32 ? 4 : e), nqin = ((nq - 1) * p.q_stride + qrow) * e;
+  st = apart(fn, {{"out", out, nout}, {"mass_out", mass_out, nm}, {"workspace", workspace, d.bytes}},
+             {{"q", out == q && nout == nqin ? nullptr : q, nqin},
+              {"mass_in", mass_in == mass_out ? nullptr : mass_in, nm},
+              {"R", R, static_cast<size_t>(p.c.H) * p.c.dh * p.c.dh * e},
+              {"K", p.c.K, np * p.c.H * p.c.page * p.c.dh * e},
+              {"V", p.c.V, np * p.c.H * p.c.vcap * p.c.ds * e},
+              {"mask", p.c.mask, np * p.c.page * 4},
+              {"slot", p.c.slot, np * p.c.page * 4},
+              {"table", table, static_cast<size_t>(B) * max_pages * 4},
+              {"lens", lens, static_cast<size_t>(B) * 4},
+              {"visible", visible, nq * 4}});
+  if (st) return st;
   char* ws = static_cast<char*>(workspace);
   p.n_split = d.n_split;
   p.chunk = d.chunk;

@@ -122,6 +122,18 @@ def test_far_angles():
         assert (np.abs(num(y) - ref) <= _rotary_tol(num(x), ref, f32)).all()
 
 
+# ---- in place ------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,rows", [(64, 1), (128, 5), (64, 24), (128, 24), (64, 40)])
+@pytest.mark.parametrize("max_len", [161, 3000])
+def test_attend_into_its_queries(dtype, dh, rows, max_len):
+    rng, c, t, n, q = case(24, [161, 90, 3, 0] * 5, rep=rows, dh=dh, dtype=dtype, width=-(-max_len // 16))
+    R = rotations(rng, 2, dh, dtype)
+    want = rs.attend_paged(q, c, t, n, R, max_len=max_len)
+    assert rs.attend_paged(q, c, t, n, R, max_len=max_len, out=q) is q and torch.equal(q, want)
+
+
 # ---- smallest calls ------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [bf, f32])

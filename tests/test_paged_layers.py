@@ -60,3 +60,36 @@ def test_an_empty_table_needs_no_workspace_for_weights():
                                       ctypes.c_void_p(0x20000000), rs.BF16, None, 1.0, ctypes.c_void_p(0x30000000), 0, None, 0,
                                       None)
         assert "workspace" not in lib.rolesub_last_error().decode() and st != 1
+
+
+def test_attend_paged_refuses_operands_that_overlap():
+    lib = rs.load()
+    P = ctypes.c_void_p
+    base = dict(K=0x10000000, V=0x20000000, mask=0x30000000, slot=0x31000000, q=0x40000000, table=0x50000000, lens=0x51000000,
+                visible=0x52000000, R=0x53000000, out=0x60000000, mi=0x70000000, mo=0x70000000, ws=0x80000000)
+    dense = 3 * 2 * 4 * 64 * 2
+
+    def call(qs=0, odt=rs.BF16, **kw):
+        a = {k: P(v) for k, v in {**base, **kw}.items()}
+        pg = rs.PagesDesc(5, 16, 64, 2, 64, 8, a["K"], a["V"], a["mask"], a["slot"])
+        need = lib.rolesub_attend_paged_workspace_size(ctypes.byref(pg), 3, 4, 2, 320, 1)
+        st = lib.rolesub_attend_paged(ctypes.byref(pg), rs.BF16, 3, 4, 2, a["q"], qs, a["table"], 20, a["lens"], a["visible"], 0,
+                                      a["R"], 0.0, a["out"], odt, a["mi"], 1.0, a["mo"], 320, a["ws"], need, None)
+        return st, lib.rolesub_last_error().decode()
+
+    if torch.cuda.is_available():
+        pytest.skip("calls that pass the checks would be launched")
+    for out in ("out", "mo", "ws"):
+        for x, v in base.items():
+            if x == out or {x, out} == {"mi", "mo"}:
+                continue
+            kw = {out: v, **({"mi": v} if out == "mo" and x != "mi" else {})}
+            if (out, x) != ("out", "q"):
+                st, why = call(**kw)
+                assert st == 1 and "overlap" in why, (out, x, why)
+    assert call(mo=base["mi"] + 64)[0] == 1
+    assert call(out=base["q"] + 16)[0] == 1 and call(out=base["q"] + dense - 16)[0] == 1
+    assert call(out=base["q"], odt=rs.F32)[0] == 1 and call(out=base["q"], qs=512)[0] == 1
+    for kw in ({}, dict(out=base["q"]), dict(out=base["q"] + dense), dict(out=base["q"] - dense), dict(mi=base["mi"] + 3 * 320 * 4)):
+        st, why = call(**kw)  # what is allowed comes as far as the launch, which finds no device
+        assert st == 4 and "overlap" not in why, (kw, why)
