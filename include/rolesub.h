@@ -522,8 +522,9 @@ rolesub_status rolesub_attend_paged(const rolesub_pages* pages, rolesub_dtype dt
  *   keep_idx [B,keep] int32: the kept indices, ascending, then -1
  *   n_keep   [B] int32: how many, min(lens[b], keep)
  *   workspace: at least rolesub_evict_workspace_size() bytes (which does not
- *   fall as B or max_len grows), 16-byte aligned; nothing in it needs clearing; calls (and graphs) that may overlap must not
- *   share one.
+ *   fall as B or max_len grows), 16-byte aligned; nothing in it needs clearing;
+ *   calls (and graphs) that may overlap must not share one. No output (n_keep is
+ *   not lens) and no part of the workspace lies in another operand.
  * ------------------------------------------------------------------------ */
 size_t rolesub_evict_workspace_size(int32_t B, int32_t max_len);
 rolesub_status rolesub_evict_tokens(int32_t B, int32_t max_len, const float* mass, int64_t mass_ld,

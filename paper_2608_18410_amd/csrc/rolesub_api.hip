@@ -1154,6 +1154,12 @@ rolesub_status rolesub_evict_tokens(int32_t B, int32_t max_len, const float* mas
     return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, %zu given", fn, need,
                 workspace ? ws_bytes : static_cast<size_t>(0));
   if (!aligned(workspace, 16)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace must lie on 16 bytes", fn);
+  // a length or weight that changes under way would make workgroups disagree on the counts
+  const size_t rows = static_cast<size_t>(B);
+  const rolesub_status st = apart(
+      fn, {{"keep_idx", keep_idx, rows * keep * 4}, {"n_keep", n_keep, rows * 4}, {"workspace", workspace, need}},
+      {{"mass", mass, max_len > 0 ? ((rows - 1) * mass_ld + max_len) * 4 : 0}, {"lens", lens, rows * 4}});
+  if (st) return st;
   EvictParams p = {B, max_len, keep, first, recent, mass, mass_ld, lens, keep_idx, n_keep, workspace};
   return from_hip(launch_evict(p, static_cast<hipStream_t>(stream)), fn);
 }

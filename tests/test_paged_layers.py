@@ -93,3 +93,27 @@ def test_attend_paged_refuses_operands_that_overlap():
     for kw in ({}, dict(out=base["q"]), dict(out=base["q"] + dense), dict(out=base["q"] - dense), dict(mi=base["mi"] + 3 * 320 * 4)):
         st, why = call(**kw)  # what is allowed comes as far as the launch, which finds no device
         assert st == 4 and "overlap" not in why, (kw, why)
+
+
+def test_evict_refuses_operands_that_overlap():
+    """The new lengths in the old ones' place, for one: other workgroups still read those."""
+    lib, P = rs.load(), ctypes.c_void_p
+    base = dict(mass=0x10000000, lens=0x20000000, idx=0x30000000, n=0x40000000, ws=0x50000000)
+
+    def call(**kw):
+        a = {k: P(v) for k, v in {**base, **kw}.items()}
+        need = lib.rolesub_evict_workspace_size(3, 40000)
+        st = lib.rolesub_evict_tokens(3, 40000, a["mass"], 40000, a["lens"], 8, 1, 2, a["idx"], a["n"], a["ws"], need, None)
+        return st, lib.rolesub_last_error().decode()
+
+    if torch.cuda.is_available():
+        pytest.skip("calls that pass the checks would be launched")
+    for out in ("idx", "n", "ws"):
+        for x, v in base.items():
+            if x != out:
+                st, why = call(**{out: v})
+                assert st == 1 and "overlap" in why, (out, x, why)
+    assert call(n=base["lens"] + 8)[0] == 1 and call(idx=base["mass"] + 3 * 40000 * 4 - 4)[0] == 1
+    for kw in ({}, dict(n=base["lens"] + 12), dict(idx=base["mass"] + 3 * 40000 * 4)):
+        st, why = call(**kw)
+        assert st == 4 and "overlap" not in why, (kw, why)
