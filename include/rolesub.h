@@ -471,7 +471,8 @@ rolesub_status rolesub_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int3
  *   before the call; n_new [B] int32 or NULL: tokens of each sequence, the
  *   first n_new[b] of its T (clamped to [0, T]; NULL: T).
  * Tokens past the end of the table, or in pages outside [0, n_pages), are
- * dropped. No two sequences may write one page. lens is not changed.
+ * dropped. No two sequences may write one page, and no page that is written holds
+ * k or z; mask, table, lens and n_new lie outside the cache. lens is not changed.
  * ------------------------------------------------------------------------ */
 rolesub_status rolesub_cache_append(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
                                     const void* k, int64_t k_stride, const void* z, int64_t z_stride,
@@ -545,7 +546,8 @@ rolesub_status rolesub_evict_tokens(int32_t B, int32_t max_len, const float* mas
  *   mass_in [B,mass_ld], mass_out [B,mass_out_ld] f32, or both NULL:
  *   mass_out[b,j] = mass_in[b,keep_idx[b,j]] (0 for an index outside
  *   [0, mass_ld)); later entries are not written. The arrays do not overlap;
- *   mass_out_ld >= keep.
+ *   mass_out_ld >= keep. keep_idx, n_keep and the tables lie apart from mass_out
+ *   and outside dst, and so do mass_in and mass_out.
  * ------------------------------------------------------------------------ */
 rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pages* dst, rolesub_dtype dtype, int32_t B,
                                      const int32_t* table, int32_t max_pages, const int32_t* keep_idx,

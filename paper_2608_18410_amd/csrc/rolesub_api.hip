@@ -933,6 +933,17 @@ rolesub_status apart(const char* fn, std::initializer_list<Operand> outs, std::i
   return ROLESUB_OK;
 }
 
+// The same for a cache that a call writes, against what its workgroups find their way by.
+rolesub_status cache_apart(const char* fn, const PagedCache& c, size_t e, std::initializer_list<Operand> ins) {
+  const size_t n = static_cast<size_t>(c.n_pages), heads = n * c.H;
+  for (const Operand& o : {Operand{"K", c.K, heads * c.page * c.dh * e}, Operand{"V", c.V, heads * c.vcap * c.ds * e},
+                           Operand{"mask", c.mask, n * c.page * 4}, Operand{"slot", c.slot, n * c.page * 4}}) {
+    const rolesub_status st = apart(fn, {o}, ins);
+    if (st) return st;
+  }
+  return ROLESUB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1027,6 +1038,10 @@ rolesub_status rolesub_cache_append(const rolesub_pages* pages, rolesub_dtype dt
   if (static_cast<size_t>(B) * T > 0x7FFFFFFF ||
       static_cast<size_t>(B) * (T / p.c.page + 2) * 256 >= kMaxThreads || p.c.H > 65535)
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many tokens or heads", fn);
+  const size_t rows = static_cast<size_t>(B);
+  st = cache_apart(fn, p.c, esize(dtype), {{"the new tokens' mask", mask, rows * T * 4}, {"table", table, rows * max_pages * 4},
+                                           {"lens", lens, rows * 4}, {"n_new", n_new, rows * 4}});
+  if (st) return st;
   return from_hip(launch_append(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
 }
 
@@ -1202,6 +1217,13 @@ rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pag
   p.mass_out = mass_out;
   p.mass_ld = mass_ld;
   p.mass_out_ld = mass_out_ld;
+  const size_t rows = static_cast<size_t>(B), mo = mass_out ? ((rows - 1) * mass_out_ld + keep) * 4 : 0;
+  const Operand idx = {"keep_idx", keep_idx, rows * keep * 4}, kept = {"n_keep", n_keep, rows * 4},
+                from = {"table", table, rows * max_pages * 4}, to = {"dst_table", dst_table, rows * dst_max_pages * 4};
+  const size_t mi = mass_in && mass_ld > 0 ? rows * mass_ld * 4 : 0;
+  if ((st = apart(fn, {{"mass_out", mass_out, mo}}, {idx, kept, from, to}))) return st;
+  if ((st = cache_apart(fn, p.dst, esize(dtype), {idx, kept, from, to, {"mass_in", mass_in, mi}, {"mass_out", mass_out, mo}})))
+    return st;
   return from_hip(launch_compact(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
 }
 

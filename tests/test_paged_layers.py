@@ -117,3 +117,32 @@ def test_evict_refuses_operands_that_overlap():
     for kw in ({}, dict(n=base["lens"] + 12), dict(idx=base["mass"] + 3 * 40000 * 4)):
         st, why = call(**kw)
         assert st == 4 and "overlap" not in why, (kw, why)
+
+
+def test_append_and_compact_refuse_lengths_and_tables_inside_the_cache():
+    lib, P = rs.load(), ctypes.c_void_p
+    if torch.cuda.is_available():
+        pytest.skip("calls that pass the checks would be launched")
+    K, V, M, S = 0x10000000, 0x20000000, 0x30000000, 0x31000000
+    inside = (K, K + 5 * 2 * 16 * 64 * 2 - 4, V, V + 5 * 2 * 64 * 8 * 2 - 4, M, M + 5 * 16 * 4 - 4, S, S + 5 * 16 * 4 - 4)
+    pg = ctypes.byref(rs.PagesDesc(5, 16, 64, 2, 64, 8, *map(P, (K, V, M, S))))
+    other = ctypes.byref(rs.PagesDesc(5, 16, 64, 2, 64, 8, *map(P, (0x41000000, 0x42000000, 0x43000000, 0x44000000))))
+
+    def append(mask=0x50000000, table=0x51000000, lens=0x52000000, n=0x53000000, k=0x54000000):
+        st = lib.rolesub_cache_append(pg, rs.BF16, 2, 3, P(k), 0, P(0x55000000), 0, P(mask), P(table), 2, P(lens), P(n), None)
+        return st, lib.rolesub_last_error().decode()
+
+    def compact(src=other, idx=0x50000000, n=0x51000000, table=0x52000000, dt=0x53000000, mi=0x54000000, mo=0x55000000):
+        st = lib.rolesub_cache_compact(src, pg, rs.BF16, 2, P(table), 2, P(idx), P(n), 4, P(dt), 2, P(mi), 40, P(mo), 9, None)
+        return st, lib.rolesub_last_error().decode()
+
+    for call, names in ((append, ("mask", "table", "lens", "n")), (compact, ("idx", "n", "table", "dt", "mi", "mo"))):
+        for name in names:
+            for at in inside:
+                st, why = call(**{name: at})
+                assert st == 1 and "overlaps" in why, (call, name, hex(at), why)
+    for name, at in (("idx", 0x55000000), ("n", 0x55000008), ("table", 0x55000000 + 4 * 12), ("dt", 0x55000000 - 12)):
+        assert compact(**{name: at})[0] == 1, name
+    # keys of other pages are no matter of the host's, and src may be dst
+    for st, why in (append(), append(k=K), compact(), compact(src=pg), compact(table=0x55000000 + 4 * 13)):
+        assert st == 4 and "overlap" not in why, why
