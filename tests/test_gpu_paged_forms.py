@@ -6,8 +6,9 @@ import torch
 
 import paper_2608_18410_amd as rs
 from oracle import paged as O
+from paper_2608_18410_amd.pipeline import decode_layer
 from tests._gpu_util import DEV
-from tests.test_gpu_paged import _rotary_tol, bf, case, dev, f32, i32, ints, num, rotations  # noqa: F401
+from tests.test_gpu_paged import _rotary_tol, _same_cache, bf, case, dev, f32, full_cache, i32, ints, num, rotations, to_np
 
 pytestmark = pytest.mark.gpu
 
@@ -17,6 +18,310 @@ def _need_gpu():
     if not torch.cuda.is_available():
         pytest.skip("needs a GPU")
     rs.load()
+
+
+# ---- attention's forms ---------------------------------------------------
+
+def dense(c, row, n):
+    """Keys and values [n, H, dh] of a sequence's first n tokens, float64, dropped groups as zeros."""
+    P, G, vcap = c.page, c.G, c.V.shape[2]
+    t = torch.arange(n, device=DEV)
+    pg, r = row.long()[t // P], t % P
+    on = (c.mask[pg, r].long()[:, None] >> torch.arange(G, device=DEV)) & 1
+    at = c.slot[pg, r].long()[:, None] + on.cumsum(1) - on
+    z = c.V[pg[:, None], :, at.clamp(0, vcap - 1)].double()  # [n, G, H, ds]
+    z = torch.where(((on > 0) & (at >= 0) & (at < vcap))[..., None, None], z, 0.0)
+    return c.K[pg, :, r].double(), z.transpose(1, 2).flatten(2)
+
+
+def reference(q, c, table, lens, R, scale, visible):
+    """out, the sum of |R| P |z| behind each output, and each token's weight."""
+    B, Tq, Hq, dh = q.shape
+    H, top = c.H, max(1, max(lens))
+    rep = Hq // H
+    out, size = torch.zeros((2, B, Tq, Hq, dh), dtype=torch.float64, device=DEV)
+    mass = torch.zeros((B, top), dtype=torch.float64, device=DEV)
+    for b, n in enumerate(lens):
+        if n == 0:
+            continue
+        K, Z = dense(c, table[b], n)
+        see = torch.full((Tq,), n, device=DEV) if visible is None else visible[b].long().clamp(max=n)
+        hide = (torch.arange(n, device=DEV)[None] >= see[:, None])[:, None].expand(Tq, rep, n).reshape(Tq * rep, n)
+        for h in range(H):
+            x = (q[b, :, h * rep:(h + 1) * rep].double().reshape(-1, dh) @ K[:, h].T.contiguous()) * scale
+            p = torch.softmax(x.masked_fill(hide, float("-inf")), -1).nan_to_num(0.0)
+            u, a = p @ Z[:, h], p @ Z[:, h].abs()
+            if R is not None:
+                Rt = R[h].double().T.contiguous()
+                u, a = u @ Rt, a @ Rt.abs()
+            out[b, :, h * rep:(h + 1) * rep] = u.view(Tq, rep, dh)
+            size[b, :, h * rep:(h + 1) * rep] = a.view(Tq, rep, dh)
+            mass[b, :n] += p.sum(0)
+    return out, size, mass
+
+
+def hold(q, c, table, lens, R=None, visible=None, max_len=0, scale=2.0 ** -5, with_mass=False):
+    """A call of small whole queries and keys, whose scores and scaled scores (below 8) are
+    exact, against float64. In units of u = 2^-24 the relative errors are: of a score in
+    log2 units 2 (constant, product) and 1 of the difference to the reference, on at most 12
+    and 24, times ln 2: 34; the exponential 2; a row's sum of weights, added one by one by
+    64 lanes of a wave and up to 256 splits, (tokens of a split) / 16 + 270; the sums of
+    values 3 times (tokens of a split) / 128 and the products of a step, 32, and as many
+    splits; the rotation 3 dh; the quotient and the output 2. Splits have at most 4096 tokens
+    here. A token's weight takes log2 of the sum (below 40, two roundings and one of the
+    difference) in place of the quotient, and the rows' sum."""
+    rows, dh, n = q.shape[1] * q.shape[2], q.shape[3], min(max(lens), 4096)
+    part = 34 + 2 + (n / 16 + 270) + 3 * (n / 128) + 32 + 256 + 2
+    ref, size, w = reference(q, c, table, lens, R, scale, visible)
+    m0 = torch.rand((len(lens), table.shape[1] * c.page), device=DEV)
+    m = m0.clone() if with_mass else None
+    out = rs.attend_paged(q, c, table, ints(lens), R, scale=scale, visible=visible, max_len=max_len, mass=m, decay=0.5,
+                          out_dtype=f32)
+    u = 2.0 ** -24
+    err, tol = (out.double() - ref).abs(), (part + (3 * dh if R is not None else 0)) * u * size
+    assert bool((err <= tol).all()), float((err / tol.clamp(min=1e-300)).max())
+    if with_mass:
+        for b, k in enumerate(lens):
+            want = w[b, :k] + 0.5 * m0[b, :k].double()
+            assert bool(((m[b, :k].double() - want).abs() <= (part + 84 + rows) * u * want).all()), b
+            assert torch.equal(m[b, k:], m0[b, k:])
+    rounded = rs.attend_paged(q, c, table, ints(lens), R, scale=scale, visible=visible, max_len=max_len)
+    assert rounded.dtype is q.dtype and torch.equal(rounded, out.to(q.dtype))
+
+
+def whole(seed, lens, **kw):
+    """A case whose queries and keys are whole numbers up to 2."""
+    rng, c, t, n, q = case(seed, lens, **kw)
+    c.K.copy_(torch.randint(-2, 3, c.K.shape, device=DEV))
+    q.copy_(torch.randint(-2, 3, q.shape, device=DEV))
+    return rng, c, t, q
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("B,H,rep,dh,top", [(64, 8, 1, 64, 600), (201, 3, 1, 64, 1100), (64, 8, 20, 128, 520), (50, 8, 2, 128, 512),
+                                            (256, 1, 130, 64, 530)])
+def test_batches_in_order_of_length(dtype, B, H, rep, dh, top):
+    """One split, 257 to 768 workgroups, bounds of 512 tokens and more: every sequence once,
+    equal and empty ones too."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, top + 1, B)
+    lens[rng.permutation(B)[:5]] = 0
+    lens[rng.permutation(B)[:9]] = 77
+    lens[int(rng.integers(B))] = top
+    units = -(-top // 128)
+    assert 512 * (units - 1) < units * B * H * -(-rep // 64) and B * H * -(-rep // 64) <= 768
+    rng, c, t, q = whole(40, [top], H=H, rep=rep, dh=dh, dtype=dtype, P=32)
+    table = torch.stack([t[0][torch.randperm(t.shape[1], device=DEV)] for _ in range(B)]).contiguous()
+    q = torch.randint(-2, 3, (B, 1, H * rep, dh), device=DEV).to(dtype)
+    hold(q, c, table, lens.tolist())
+    hold(q, c, table, lens.tolist(), rotations(rng, H, dh, dtype), with_mass=True)
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,G", [(64, 8), (64, 16), (64, 32), (128, 8), (128, 16), (128, 32), (128, 2)])
+@pytest.mark.parametrize("rep,Tq", [(1, 1), (1, 17), (4, 6), (1, 33), (5, 13)])
+def test_many_rows_over_groups_of_any_width(dtype, dh, G, rep, Tq):
+    lens = [161, 0, 37, 300]
+    rng, c, t, q = whole(41, lens, H=2, rep=rep, Tq=Tq, dh=dh, G=G, kmax=max(1, G - 1), dtype=dtype)
+    vis = ints(rng.integers(-2, 320, (4, Tq)))
+    hold(q, c, t, lens, rotations(rng, 2, dh, dtype), visible=vis, with_mass=True)
+    hold(q, c, t, lens, visible=vis)
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,G", [(64, 32), (64, 16), (128, 32), (128, 16), (128, 8)])
+@pytest.mark.parametrize("rows", [1, 24, 40])
+def test_long_bounds_over_groups_of_any_width(dtype, dh, G, rows):
+    """From a bound of 1024 tokens on keys are loaded past the caches, and splits joined."""
+    lens = [1024, 2100, 5, 0, 1999]
+    rng, c, t, q = whole(42, lens, H=2, rep=rows, dh=dh, G=G, dtype=dtype, P=64)
+    hold(q, c, t, lens, rotations(rng, 2, dh, dtype), max_len=2100)
+    hold(q, c, t, lens, max_len=2100, with_mass=True)
+
+
+@pytest.mark.parametrize("dtype,n", [(bf, 70001), (f32, 33333)])
+@pytest.mark.parametrize("rep", [1, 4, 24])
+def test_long_sequences_of_exact_scores(dtype, n, rep):
+    rng, c, t, q = whole(43, [n], P=64, H=1, rep=rep, dh=128, dtype=dtype, kmax=6)
+    hold(q, c, t, [n], rotations(rng, 1, 128, dtype), with_mass=True)
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,Tq", [(128, 1), (128, 3), (64, 24), (128, 24), (64, 50), (128, 70)])
+@pytest.mark.parametrize("max_len", [144, 3000])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_unseen_values_in_many_rows(dtype, dh, Tq, max_len, bad):
+    """What lies past the lengths is not seen at all; a value that the last query alone
+    sees reaches it, in its groups, and no other."""
+    lens = [70, 130]
+    rng, c, t, q = whole(44, lens, H=2, Tq=Tq, dh=dh, G=8, kmin=1, kmax=5, dtype=dtype, width=-(-max_len // 16))
+    n = ints(lens)
+    vis = torch.full((2, Tq), 60, device=DEV, dtype=i32)
+    vis[:, -1] = 200
+    clean = rs.attend_paged(q, c, t, n, visible=vis, scale=2.0 ** -5, max_len=max_len)
+    for b, k in enumerate(lens):
+        pg = int(t[b, k // 16])
+        c.K[pg, :, k % 16:] = bad
+        c.V[pg, :, int(c.slot[pg, k % 16]):] = bad
+    assert torch.equal(clean, rs.attend_paged(q, c, t, n, visible=vis, scale=2.0 ** -5, max_len=max_len))
+    pg, r = int(t[0, 65 // 16]), 65 % 16
+    m = int(c.mask[pg, r]) & 255
+    first = int(c.slot[pg, r])
+    c.V[pg, :, first:first + bin(m).count("1")] = bad
+    out = rs.attend_paged(q, c, t, n, visible=vis, scale=2.0 ** -5, max_len=max_len)
+    assert torch.equal(out[1], clean[1])
+    hit = torch.tensor([bool(m >> g & 1) for g in range(8)], device=DEV).repeat_interleave(dh // 8).expand(2, dh)
+    assert torch.equal(~torch.isfinite(out[0, -1]), hit)
+    # the others: sums of one wave taken again token by token may be rounded otherwise
+    ref, size, _ = reference(q, c, t, [65, 0], None, 2.0 ** -5, vis)
+    for o in (out, clean):
+        err = (o[0, :-1].double() - ref[0, :-1]).abs()
+        assert bool((err <= 800 * 2.0 ** -24 * size[0, :-1] + (2.0 ** -8 if dtype is bf else 0) * ref[0, :-1].abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,H,rep", [(128, 3, 2), (64, 2, 5)])
+def test_prompts_into_an_empty_cache(dtype, dh, H, rep):
+    """A causal prompt of 305 tokens through decode_layer, and eight more tokens in one
+    call: against float64 over the cache as it then is, in the units of hold."""
+    rng = np.random.default_rng(dh)
+    B, G, P, W, kv = 3, 8, 32, 10, 5
+    c = rs.PagedCache.allocate(B * W, P, H, dh, G, P * kv, dtype, device=DEV)
+    table = ints(rng.permutation(B * W).reshape(B, W))
+    R, budget = rotations(rng, H, dh, dtype), rs.make_budget(rs.TOPK, (kv,) * 4)
+    mass = torch.zeros((B, W * P), device=DEV)
+    done = 0
+    for T in (305, 8):
+        q, k = (torch.randint(-1, 2, (B, T, n, dh), device=DEV).to(dtype) for n in (H * rep, H))
+        v = dev(rng.standard_normal((B, T, H, dh)), dtype)
+        vis = (done + 1 + torch.arange(T, device=DEV, dtype=i32)).expand(B, T).contiguous()
+        before = mass.clone()
+        lens, done = ints([done] * B), done + T
+        out = decode_layer(None, q, k, v, torch.zeros((B, T), dtype=torch.uint8, device=DEV), R, budget, G, c, table, lens,
+                           lens + T, scores_in=torch.rand((B, T, G), device=DEV), visible=vis, mass=mass, decay=0.5)
+        ref, size, w = reference(q, c, table, [done] * B, R, dh ** -0.5, vis)
+        part, u = 34 + 2 + (done / 16 + 270) + 3 * (done / 128) + 32 + 256 + 2, 2.0 ** -24
+        tol = (part + 3 * dh) * u * size
+        assert bool(((out.double() - ref).abs() <= tol + (2.0 ** -8 if dtype is bf else 0) * (ref.abs() + tol)).all())
+        want = w + 0.5 * before[:, :done].double()
+        assert bool(((mass[:, :done].double() - want).abs() <= (part + 84 + T * H * rep) * u * want).all())
+        assert not mass[:, done:].any()
+
+
+# ---- append and compaction -----------------------------------------------
+
+FORMS = [(bf, 64, 32), (bf, 64, 16), (bf, 64, 8), (bf, 128, 4), (f32, 64, 32), (f32, 64, 16), (bf, 128, 1)]  # groups of 4 to 256 bytes
+
+
+def bits_of(m, G):
+    return [g for g in range(G) if m >> g & 1]
+
+
+def equal_caches(c, want):
+    for a, b in zip(c.tensors(), want):
+        assert torch.equal(a, b)
+
+
+def put(want, pages, rows, slots, keys, groups, toks, masks):
+    """Tokens into copies of a cache's arrays: keys [n, H, dh], groups (token, group, slot) of z [n, H, G, ds]."""
+    K, V, M, S = want
+    K[pages, :, rows] = keys
+    M[pages, rows], S[pages, rows] = masks, slots
+    i, g, sl = (torch.tensor(x, device=DEV, dtype=torch.long) for x in zip(*toks))
+    V[pages[i], :, sl] = groups[i, :, g]
+
+
+@pytest.mark.parametrize("dtype,dh,G", FORMS)
+@pytest.mark.parametrize("H", [5, 8, 7])
+def test_append_of_many_pages(dtype, dh, G, H):
+    """At least 512 workgroups of four heads each: all of the cache, to the bit."""
+    rng = np.random.default_rng(G + H)
+    B, T, P = 16, 305, 16
+    W = -(-(T + 40) // P)
+    c = full_cache(rng, B * W + 3, P, H, dh, G, G, dtype)
+    assert B * (((P - 1 + T - 1) // P) + 1) * -(-H // 4) >= 512
+    table, lens, new = rng.permutation(B * W + 3)[: B * W].reshape(B, W), rng.integers(0, 40, B), rng.integers(0, T + 1, B)
+    new[:3], lens[1] = (T, T - 1, 0), 16
+    k, z = (dev(rng.standard_normal((B, T, H, dh)), dtype) for _ in range(2))
+    m = rng.integers(0, 1 << min(G, 31), (B, T))
+    want = [x.clone() for x in c.tensors()]
+    slot, mask = c.slot.cpu().numpy(), c.mask.cpu().numpy()
+    pages, rows, slots, toks, src = [], [], [], [], []
+    for b in range(B):
+        at = 0
+        if lens[b] % P:
+            pg, r = table[b, lens[b] // P], lens[b] % P - 1
+            at = slot[pg, r] + len(bits_of(int(mask[pg, r]), G))
+        for j in range(new[b]):
+            t = lens[b] + j
+            at = 0 if t % P == 0 else at
+            gs = bits_of(int(m[b, j]), G)
+            toks += [(len(pages), g, at + i) for i, g in enumerate(gs)]
+            pages.append(table[b, t // P]), rows.append(t % P), slots.append(at), src.append(b * T + j)
+            at += len(gs)
+    src = torch.tensor(src, device=DEV)
+    put(want, ints(pages).long(), ints(rows).long(), ints(slots), k.flatten(0, 1)[src], z.flatten(0, 1).unflatten(2, (G, -1))[src],
+        toks, ints(m.reshape(-1))[src])
+    rs.cache_append(c, k, z, ints(m), ints(table), ints(lens), n_new=ints(new))
+    equal_caches(c, want)
+
+
+@pytest.mark.parametrize("dtype,dh,G", FORMS)
+@pytest.mark.parametrize("H", [3, 12])
+@pytest.mark.parametrize("T", [1, 2, 7])
+def test_append_of_a_few_tokens(dtype, dh, G, H, T):
+    """Within a page and over its edge, with counts, pages that are none and few slots."""
+    rng = np.random.default_rng(T + G)
+    B, P, W = 6, 16, 3
+    for vcap in (P * G, 3 * G):
+        c = full_cache(rng, B * W + 1, P, H, dh, G, G, dtype, vcap=vcap)
+        cn = to_np(c)
+        table = rng.permutation(B * W + 1)[: B * W].reshape(B, W)
+        table[4, 1], table[5, 0] = -1, B * W + 1
+        for lens, new in (([0, 15, 16, 9, 14, 3], None), ([31, 32, 10, 47, 48, 40], [T, 0, T + 5, 1, 2, -1])):
+            k, z = (dev(rng.standard_normal((B, T, H, dh)), dtype) for _ in range(2))
+            m = rng.integers(0, 1 << 32, (B, T)).astype(np.uint32)
+            rs.cache_append(c, k, z, torch.from_numpy(m.view(np.int32)).to(DEV), ints(table), ints(lens),
+                            n_new=None if new is None else ints(new))
+            O.append(cn, num(k), num(z), m, table, lens, new)
+            _same_cache(c, cn)
+
+
+@pytest.mark.parametrize("dtype,dh,G", FORMS)
+@pytest.mark.parametrize("H", [5, 8, 7])
+def test_compact_of_many_pages(dtype, dh, G, H):
+    """At least 512 workgroups of four heads each: all of the destination, to the bit."""
+    rng = np.random.default_rng(G + H)
+    B, L, keep, P = 24, 400, 205, 16
+    W, D = -(-L // P), -(-keep // P)
+    src, dst = (full_cache(rng, n, P, H, dh, G, G, dtype) for n in (B * W + 1, B * D + 2))
+    assert B * D * -(-H // 4) >= 512
+    ts, td = rng.permutation(B * W + 1)[: B * W].reshape(B, W), rng.permutation(B * D + 2)[: B * D].reshape(B, D)
+    idx = np.sort(np.stack([rng.permutation(L)[:keep] for _ in range(B)]), 1)
+    n = rng.integers(0, keep + 1, B)
+    n[:2] = keep, 0
+    want = [x.clone() for x in dst.tensors()]
+    slot, mask = src.slot.cpu().numpy(), src.mask.cpu().numpy()
+    pages, rows, slots, toks, spage, srow, first = [], [], [], [], [], [], []
+    for b in range(B):
+        at = 0
+        for j in range(n[b]):
+            at = 0 if j % P == 0 else at
+            pg, r = ts[b, idx[b, j] // P], idx[b, j] % P
+            cnt = len(bits_of(int(mask[pg, r]), G))
+            toks += [(len(pages), i, at + i) for i in range(cnt)]
+            pages.append(td[b, j // P]), rows.append(j % P), slots.append(at)
+            spage.append(pg), srow.append(r), first.append(slot[pg, r])
+            at += cnt
+    sp, sr, at = (torch.tensor(x, device=DEV, dtype=torch.long) for x in (spage, srow, first))
+    held = src.V[sp[:, None], :, (at[:, None] + torch.arange(G, device=DEV)).clamp(max=src.V.shape[2] - 1)].transpose(1, 2)
+    put(want, ints(pages).long(), ints(rows).long(), ints(slots), src.K[sp, :, sr], held, toks, src.mask[sp, sr])
+    mass = torch.rand((B, L), device=DEV)
+    mo = torch.full((B, keep), 7.0, device=DEV)
+    rs.cache_compact(src, ints(ts), ints(idx), ints(n), dst, ints(td), mass=mass, mass_out=mo)
+    equal_caches(dst, want)
+    take = torch.arange(keep, device=DEV) < ints(n)[:, None]
+    assert torch.equal(mo, torch.where(take, mass.gather(1, ints(idx).long()), torch.full_like(mo, 7.0)))
 
 
 # ---- numbers -------------------------------------------------------------
@@ -107,6 +412,36 @@ def test_pairs_of_no_axis_are_copied(dtype, dh, pairs, interleaved, tokens):
     rest = torch.ones(dh, dtype=torch.bool, device=DEV)
     rest[a], rest[b] = False, False
     assert torch.isfinite(y[..., rest]).all()
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("H,Hkv", [(32, 8), (25, 8), (70, 3)])
+@pytest.mark.parametrize("dh,pairs", [(128, 64), (128, 63), (64, 16), (64, 13)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("B,T", [(2, 2049), (1, 1500), (3, 37)])
+def test_rotary_of_many_heads(dtype, H, Hkv, dh, pairs, interleaved, B, T):
+    """More heads than a wave takes at once, all of them or a part a wave: a sample of
+    tokens against the oracle, and the same bits in place on a fused projection."""
+    rng = np.random.default_rng(H + pairs)
+    qkv = torch.randn((B, T, (H + 2 * Hkv) * dh), device=DEV).to(dtype)
+    q, k = qkv[..., :H * dh].unflatten(2, (H, dh)), qkv[..., H * dh:(H + Hkv) * dh].unflatten(2, (Hkv, dh))
+    pos, f = rng.integers(0, 9999, (B, T, 2)), (10000.0 ** (-np.arange(pairs) / pairs)).astype(np.float32)
+    ax = rng.integers(0, 2, pairs).astype(np.uint8)
+    args = (ints(pos), torch.from_numpy(f).to(DEV), torch.from_numpy(ax).to(DEV))
+    yq, yk = rs.rotary(q, k, *args, interleaved=interleaved)
+    toks = sorted({0, 1, T // 2, T - 1})
+    for x, y in ((q, yq), (k, yk)):
+        xs = num(x[:, toks])
+        ref = O.rotary(xs, pos[:, toks], f, ax, interleaved)
+        assert (np.abs(num(y[:, toks]) - ref) <= _rotary_tol(xs, ref, dtype)).all()
+    # every token: what it gives alone
+    some = torch.randint(0, B * T, (40,), device=DEV)
+    alone = rs.rotary(q.flatten(0, 1)[some][None].contiguous(), k.flatten(0, 1)[some][None].contiguous(),
+                      args[0].flatten(0, 1)[some][None].contiguous(), *args[1:], interleaved=interleaved)
+    assert torch.equal(alone[0][0], yq.flatten(0, 1)[some]) and torch.equal(alone[1][0], yk.flatten(0, 1)[some])
+    rest = qkv[..., (H + Hkv) * dh:].clone()
+    rs.rotary(q, k, *args, interleaved=interleaved, out=(q, k))
+    assert torch.equal(q, yq) and torch.equal(k, yk) and torch.equal(qkv[..., (H + Hkv) * dh:], rest)
 
 
 def test_far_angles():
