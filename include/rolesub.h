@@ -495,7 +495,8 @@ rolesub_status rolesub_cache_append(const rolesub_pages* pages, rolesub_dtype dt
  * a query does not see does not reach it, infinities and NaN included.
  * Accumulated attention weight of every cached token (mass_out non-NULL):
  *   mass_out[b,t] = decay * mass_in[b,t] + sum over j, h of P[j,h,t]
- *   for t < min(lens[b], max_len); later entries are not written.
+ *   for t < min(lens[b], max_len); later entries are not written. Tokens that
+ *   are new add to what mass_in holds for them: zeros, where nothing was yet.
  *   mass_in [B,mass_ld] f32 or NULL (zeros; also with decay = 0), mass_out the
  *   same; they may be the same array. mass_ld >= max_len, 0 <= decay finite.
  * workspace: at least rolesub_attend_paged_workspace_size() bytes (which does

@@ -158,9 +158,12 @@ def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.Page
     rotate -> append -> attend. h [B,T,d], q [B,T,Hq,dh], k and v [B,T,H,dh]; lens are
     the cached tokens before them, new_lens = lens + T after (one pair of tensors
     serves every layer of a stack). Without positions the keys and queries are taken
-    as they are. visible defaults to all cached and new tokens; for T > 1 causal
-    tokens pass visible[b, j] = lens[b] + j + 1. With mass the tokens' weight is
-    accumulated for evict_layer. Returns the attention output [B,T,Hq,dh]."""
+    as they are. visible defaults to all cached and new tokens, as a chunk of actions
+    decoded in parallel sees itself whole; the tokens of a causal prompt (T > 1) must
+    pass visible[b, j] = lens[b] + j + 1. With mass the tokens' weight is accumulated
+    for evict_layer: past the cached tokens it must hold zeros, as evict_layer leaves
+    it, since new tokens add to what is there. Returns the attention output
+    [B,T,Hq,dh]."""
     with _current_stream(stream):
         mask = rs.route(types, budget, G, h=h, router=router, scores_in=scores_in, want_scores=False, want_idx=False,
                         want_count=False)["mask"]

@@ -919,7 +919,8 @@ def attend_paged(q, cache: PagedCache, table, lens, R=None, scale: float = 0.0, 
     """Attention of new tokens q [B,Tq,Hq,dh] over the cached ones; returns
     [B,Tq,Hq,dh]. visible [B,Tq] int32: the tokens each query sees. mass [B,>=max_len]
     f32: the tokens' accumulated weight, in place or into mass_out (which alone
-    starts from zero): decay * mass + the weight of this call's queries."""
+    starts from zero): decay * mass + the weight of this call's queries, for every
+    token below lens, so entries of tokens that are new must hold zeros."""
     H, dh, dt = cache.H, cache.dh, cache.dtype
     shape, sq, dq = _operand("q", q, None, dh, dt)
     B, Tq, Hq, _ = shape
