@@ -106,11 +106,13 @@ __device__ __forceinline__ void reads_ahead() {
 // path: there the wait would be for whatever else is under way.
 __device__ __forceinline__ void arrived(int& x) { asm volatile("" : "+v"(x)); }
 
-// Waits until a matrix product's result may be read by other instructions. The
-// compiler spaces them within a block; where a branch followed the product and the
-// read came first after the join, it left the read too early (stale values of the
-// first element read, in a build with the rotation optional inside one function).
-// Placed after products that end a block.
+// Waits until a matrix product's result may be read by other instructions. In straight
+// code the compiler keeps the states between them (8 for the bf16 product, 10 for the
+// float32 one). Without this, the assembly of k_join in bf16 has products into
+// accumulation registers, a branch (around the way without a rotation), and on its taken
+// side v_accvgpr_read of them three instructions later; the first elements came out
+// stale. Placed after products that end a block; tests/test_mfma_waits.py looks at the
+// assembly for any other.
 template <int N>
 __device__ __forceinline__ void settle(f32x4 (&x)[N]) {
 #pragma unroll
