@@ -67,10 +67,8 @@ __device__ __forceinline__ u32x4 bload16_hint(rsrc_t r, uint32_t off) {
 // leaves the range). Two parts, 17 bits, put float32 outputs off by up to 2^-16; the
 // third costs 7 % where rows share tiles (16 sequences of up to 361 tokens and 56
 // queries, 32 heads 29.2 -> 31.1 us, 8 of 305 and 305 52 -> 56.5) and nothing where
-// calls are bound by memory. INF: an infinity is its first part, and the others zero
-// (a difference of infinities would make it NaN).
+// calls are bound by memory. An infinity's other parts are NaN.
 constexpr int kParts = 3;
-template <bool INF>
 __device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8 (&part)[kParts]) {
   u32x4 v[kParts];
 #pragma unroll
@@ -79,9 +77,7 @@ __device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8 (&part)[kPar
 #pragma unroll
     for (int n = 0; n < kParts; ++n) {
       v[n][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-      const f32x2 y = {__uint_as_float(v[n][i] << 16), __uint_as_float(v[n][i] & 0xFFFF0000u)};
-#pragma unroll
-      for (int k = 0; k < 2; ++k) x[k] = INF && __builtin_isinf(y[k]) ? 0.f : x[k] - y[k];
+      x = f32x2{x[0] - __uint_as_float(v[n][i] << 16), x[1] - __uint_as_float(v[n][i] & 0xFFFF0000u)};
     }
   }
 #pragma unroll
@@ -159,7 +155,7 @@ __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h,
       const int d = (4 * j + g4) * EP;
       if constexpr (L::kBf16) {
         bf16x8 part[kParts];
-        split_bf16<true>(*reinterpret_cast<const f32x4*>(ur + d), *reinterpret_cast<const f32x4*>(ur + d + 4), part);
+        split_bf16(*reinterpret_cast<const f32x4*>(ur + d), *reinterpret_cast<const f32x4*>(ur + d + 4), part);
 #pragma unroll
         for (int n = 0; n < kParts; ++n)
 #pragma unroll
@@ -175,6 +171,26 @@ __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h,
       }
     }
     settle(o);
+    if constexpr (L::kBf16) {
+      // infinite sums, whose other parts are NaN, once more from the float32 numbers (16
+      // sequences and 56 queries, as above: 32.4 us; with a test of every part 34.8)
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(o[i][x]);
+      if (__any(bad)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const T* R = static_cast<const T*>(p.Rm) + (static_cast<int64_t>(h) * DH + 16 * (w + 4 * i) + 4 * g4) * DH;
+          o[i] = f32x4{0, 0, 0, 0};
+#pragma unroll 1
+          for (int d = 0; d < DH; ++d)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[i][x] += tof(R[x * DH + d]) * ur[d];
+        }
+      }
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = *reinterpret_cast<const f32x4*>(ur + 16 * (w + 4 * i) + 4 * g4);
@@ -301,7 +317,7 @@ __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   if constexpr (L::kBf16) {
     bf16x8 part[kParts];
-    split_bf16<false>(s[0], s[L::NB - 1], part);
+    split_bf16(s[0], s[L::NB - 1], part);
     const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb) {
