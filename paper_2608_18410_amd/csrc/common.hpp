@@ -137,6 +137,9 @@ __device__ __forceinline__ uint32_t top_k_pairs(const float* g, int G, int K) {
   return m;
 }
 
+// The bits of a mask that stand for groups.
+__device__ __forceinline__ uint32_t group_bits(int G) { return G >= 32 ? 0xFFFFFFFFu : (1u << G) - 1u; }
+
 // Number of groups kept by one token (Sec. 3.5).
 __device__ __forceinline__ int budget_k(int mode, const int* k_by_type, int type, float tau,
                                         int kmin, int kmax, int G, int n_above) {
@@ -226,6 +229,26 @@ __device__ __forceinline__ float gelu_exact(float x) {
   // changes the result by about 2e-6 relative, well inside the erfc fit
   const float ec = t * __builtin_amdgcn_exp2f(fmaf(-z, z, P) * 1.44269504088896341f);
   return 0.5f * x * (x >= 0.f ? 2.f - ec : ec);
+}
+
+// Exclusive sum over the NT threads of a workgroup. AGAIN: wsum (a word a wave) has been
+// read before, by a scan or its kind, which a barrier first lets end.
+template <int NT, bool AGAIN>
+__device__ __forceinline__ int group_scan(int x, int* wsum) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int s = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(s, o, kWave);
+    if (lane >= o) s += y;
+  }
+  if constexpr (AGAIN) __syncthreads();
+  if (lane == 63) wsum[w] = s;
+  __syncthreads();
+  int base = 0;
+#pragma unroll
+  for (int v = 0; v < NT / 64; ++v) base += v < w ? wsum[v] : 0;
+  return base + s - x;
 }
 
 // What one lane of a wave writes to LDS is read by others of the same wave: the

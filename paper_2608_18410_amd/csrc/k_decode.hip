@@ -15,8 +15,6 @@
 namespace rolesub {
 namespace {
 
-__device__ __forceinline__ uint32_t group_bits(int G) { return G >= 32 ? 0xFFFFFFFFu : (1u << G) - 1u; }
-
 // Four bf16 rows of 16 columns, transposed: 16 lanes give the addresses of the
 // rows' 8-byte quarters, lane i gets column i of the four rows.
 __device__ __forceinline__ bf16x4 lds_read_tr(const char* p) {

@@ -28,26 +28,6 @@ __device__ __forceinline__ int level_digit(int level, uint32_t key) {
   return (key >> level_shift(level)) & (level_bins(level) - 1);
 }
 
-// Exclusive sum over the NT threads of a workgroup (and a barrier at its start,
-// so that wsum may be reused).
-template <int NT>
-__device__ __forceinline__ int scan(int x, int* wsum) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int s = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(s, o, kWave);
-    if (lane >= o) s += y;
-  }
-  __syncthreads();
-  if (lane == 63) wsum[w] = s;
-  __syncthreads();
-  int base = 0;
-#pragma unroll
-  for (int v = 0; v < NT / 64; ++v) base += v < w ? wsum[v] : 0;
-  return base + s - x;
-}
-
 // The largest digit that at least `need` (>= 1) keys reach, and how many are above
 // it. Thread t holds the counts of bins top - j, top = NB - 1 - t * PER.
 template <int NT, int PER>
@@ -55,7 +35,7 @@ __device__ __forceinline__ void find_digit(const int* cnt, int need, int* wsum, 
   int mine = 0;
 #pragma unroll
   for (int j = 0; j < PER; ++j) mine += cnt[j];
-  int e = scan<NT>(mine, wsum);
+  int e = group_scan<NT, true>(mine, wsum);
   if (e < need && need <= e + mine) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -145,7 +125,7 @@ __global__ __launch_bounds__(NT) void k_evict_one(EvictParams p) {
   }
   __syncthreads();
   const int mine = tid < ITS * NW ? cnt[tid] : 0;  // both counts stay below 2^15 in sum
-  const int before = scan<NT>(mine, wsum);
+  const int before = group_scan<NT, true>(mine, wsum);
   if (tid < ITS * NW) cnt[tid] = before;
   __syncthreads();
   const uint64_t below = (1ull << lane) - 1ull;
@@ -243,7 +223,7 @@ __global__ __launch_bounds__(kPassWg) void k_evict_pass(EvictParams p, EvictWs w
       eq += bin == d ? pre[j] : 0;
     }
     if (LEVEL < 3) {
-      const int a = scan<NT>(mine, wsum) + mine;  // the last thread holds the sum
+      const int a = group_scan<NT, true>(mine, wsum) + mine;  // the last thread holds the sum
       if (tid == NT - 1) ws.above[L][static_cast<int64_t>(b) * C + c] = a;
       if (c == 0 && tid == 0) {
         ws.state[L][2 * b] = found;
@@ -252,9 +232,9 @@ __global__ __launch_bounds__(kPassWg) void k_evict_pass(EvictParams p, EvictWs w
     } else {
       for (int x = tid; x < c; x += NT)
         mine += ws.above[0][static_cast<int64_t>(b) * C + x] + ws.above[1][static_cast<int64_t>(b) * C + x];
-      const int g = scan<NT>(mine, wsum) + mine;
+      const int g = group_scan<NT, true>(mine, wsum) + mine;
       if (tid == NT - 1) s_out[0] = g;  // s_out was read before the scan's barriers
-      const int e = scan<NT>(eq, wsum) + eq;
+      const int e = group_scan<NT, true>(eq, wsum) + eq;
       if (tid == NT - 1) s_out[1] = e;
       __syncthreads();
       gt_before = s_out[0];

@@ -8,24 +8,6 @@ namespace {
 
 constexpr int kMaxPage = 256;
 
-__device__ __forceinline__ uint32_t group_bits(int G) { return G >= 32 ? 0xFFFFFFFFu : (1u << G) - 1u; }
-
-// Exclusive sum over the 256 threads of a workgroup.
-__device__ __forceinline__ int scan256(int x, int* wsum) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int s = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(s, o, kWave);
-    if (lane >= o) s += y;
-  }
-  if (lane == 63) wsum[w] = s;
-  __syncthreads();
-  int base = 0;
-  for (int v = 0; v < w; ++v) base += wsum[v];
-  return base + s - x;
-}
-
 template <int VB> struct Piece;
 template <> struct Piece<4> { typedef uint32_t t; };
 template <> struct Piece<8> { typedef u32x2 t; };
@@ -59,7 +41,7 @@ __global__ __launch_bounds__(256) void k_append_few(AppendParams p, int np, int 
   const uint32_t mine = tid < m ? p.mask[j0 + tid] & gm : 0u;
   int base = 0;
   if (r0 > 0) base = c.slot[meta + r0 - 1] + __popc(c.mask[meta + r0 - 1] & gm);
-  const int at = base + scan256(__popc(mine), wsum);
+  const int at = base + group_scan<256, false>(__popc(mine), wsum);
   if (tid < m) {
     s_mask[tid] = mine;
     s_slot[tid] = at;
@@ -209,7 +191,7 @@ __global__ __launch_bounds__(256) void k_append(AppendParams p, int np, int e) {
   const uint32_t whole = tid < m ? p.mask[j0 + tid] : 0u, mine = whole & gm;
   int base = 0;
   if (r0 > 0) base = c.slot[meta + r0 - 1] + __popc(c.mask[meta + r0 - 1] & gm);
-  const int cnt = __popc(mine), at = scan256(cnt, wsum);
+  const int cnt = __popc(mine), at = group_scan<256, false>(cnt, wsum);
   if (tid == 255) s_total = at + cnt;
   if (tid < m) {
     g.krow[tid] = j0 + tid;
@@ -291,7 +273,7 @@ __global__ __launch_bounds__(256) void k_compact(CompactParams p, int np, int e)
   if (i >= p.dst_max_pages) return;
   const int32_t page = p.dst_table[static_cast<int64_t>(b) * p.dst_max_pages + i];
   if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(d.n_pages)) return;
-  const int cnt = __popc(mine), at = scan256(cnt, wsum);
+  const int cnt = __popc(mine), at = group_scan<256, false>(cnt, wsum);
   if (tid == 255) s_total = at + cnt;
   if (tid < m) {
     g.krow[tid] = spage < 0 ? -1 : ((static_cast<int64_t>(spage) * c.H) << c.shift) + srow;
