@@ -444,12 +444,12 @@ typedef struct rolesub_pages {
  *   a_i = positions[b,t,axis[i]] * inv_freq[i]        i = 0 .. n_pairs-1
  *   y_i = x_i cos a_i - x_j sin a_i,   y_j = x_i sin a_i + x_j cos a_i
  * on the pairs (i, j) = (i, n_pairs + i) of every head, or (2i, 2i+1) when
- * interleaved is non-zero; dims past 2 n_pairs are copied. inverse non-zero
+ * interleaved is non-zero; other dims are copied. inverse non-zero
  * turns by -a (undoes the call; also its gradient).
  *   q [B,T,H,dh], k [B,T,Hkv,dh] (dtype) with token strides q_stride and
  *   k_stride; either may be NULL (its head count is then not used).
  *   positions [B,T,n_axes] int32; inv_freq [n_pairs] f32; axis [n_pairs] uint8
- *   or NULL (all axis 0); a pair whose axis is >= n_axes is not turned.
+ *   or NULL (all axis 0); a pair whose axis is >= n_axes is copied.
  *   q_out, k_out: dense, or the input itself (same pointer, then the same
  *   stride is used); otherwise no output overlaps another tensor of the call.
  * Whole turns are taken off the angles in two doubles: nothing is lost while

@@ -551,7 +551,7 @@ __device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len
 // ONCE: keys are loaded so that they leave the caches to other data (kOnceTokens).
 // Bound by memory from a few thousand tokens on: 64 sequences of 256 to 2048 tokens, 8
 // key heads of 4 rows (219 MB) 45 us, 4.8 TB/s; two of 131071 tokens and 32 heads (3.36
-// GB) 547 us, 6.1 TB/s, and about 610 where the scores are stored for the weights, more
+// GB) 547 us, 6.1 TB/s, and 608 where the scores are stored for the weights, more
 // than their 33 MB explain. Below that by a chain of dependent loads (length, page, mask, key and value): one
 // of 305 tokens 8 us.
 template <class T, int DH, int WR, int SUB, bool ONCE>
@@ -742,9 +742,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 // wave, and go from there to one of two LDS tiles, so that one barrier a tile is
 // enough: between two barriers the waves write the next tile and compute on this one.
 // (With a tile to each wave, as above, every wave fetches and expands all of it:
-// 16 sequences of up to 361 tokens and 56 queries took 42 us.) Bound by vector
-// instructions: those 16, 32 heads, 28 us; 64 of 361 issue 275 a tile and wave, for which
-// the vector units are busy half of the time.
+// 16 sequences of up to 361 tokens and 56 queries took 42 us.) Those 16, 32 heads, take 32
+// us; 64 of 361 108. No one unit bounds it: of the waves' time there a third is spent
+// waiting for data or a barrier and a third for a turn to issue, among 267 vector
+// instructions a tile and wave, 32 of them products; 12 instructions fewer changed nothing.
+// A quarter of the LDS cycles are bank conflicts.
 template <class T, int DH, int SUB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 3 : 4))) void k_decode_rows(DecodeParams p) {
   using L = Tile<T, DH>;
@@ -1097,9 +1099,9 @@ __global__ __launch_bounds__(256) void k_join(DecodeParams p, int joins, int nbl
 
 // Blocks of 16 rows of a workgroup. From 17 rows on a tile of bfloat16 tokens is worth
 // sharing among all four waves where its keys and values are 32 KB and more (4: dims
-// of 128): 8 sequences of 8192 tokens, 8 key heads of 32 rows 72 -> 60 us, 42 of 4748 to
-// 12482 of 20 rows 377 -> 270, but 64 of 361 of 24 rows 27.2 -> 28; dims of 64, 8 of 8192
-// of 5 rows 37.9 -> 39.8; float32, 8 of 8192 of 20 rows 143 -> 180.
+// of 128): 8 sequences of 8192 tokens, 8 key heads of 32 rows 75 -> 69 us, 42 of 4748 to
+// 12482 of 20 rows 391 -> 281, but 64 of 361 of 24 rows 26.9 -> 28.3; dims of 64, 8 of 8192
+// of 20 rows 37.9 -> 40.7; float32, 8 of 8192 of 20 rows 143 -> 180.
 constexpr bool share_from_17(bool bf16, int dh) { return bf16 && dh == 128; }
 int row_blocks(int R, bool bf16, int dh) { return R <= 16 ? 1 : R <= 32 && !share_from_17(bf16, dh) ? 2 : 4; }
 
