@@ -762,7 +762,8 @@ def _rows(name, t):
     sb, st, sh, sd = t.stride()
     if T == 1:
         st = sb if B > 1 else H * dh
-    if (sd != 1 and dh > 1) or (sh != dh and H > 1) or (B > 1 and sb != T * st):
+    # (a stride of 0, an expanded operand, would be taken for dense rows)
+    if (sd != 1 and dh > 1) or (sh != dh and H > 1) or (B > 1 and sb != T * st) or st < H * dh:
         raise ValueError(f"{name}: heads and dims must be dense and tokens at one stride, got strides {list(t.stride())}")
     return st, None
 

@@ -46,6 +46,27 @@ def test_evict_layer_refuses_before_it_clears_weights(calls):
     assert go(None)[1].shape == (2, 40)
 
 
+def test_expanded_operands_are_refused():
+    """One token for many, without its own memory: not rows at a stride."""
+    bf = torch.bfloat16
+    z = lambda *s, dtype=bf: torch.zeros(s, dtype=dtype)  # noqa: E731
+    f = z(32, dtype=torch.float32)
+    cache = rs.PagedCache(K=z(5, 2, 16, 64), V=z(5, 2, 64, 8), mask=z(5, 16, dtype=i32), slot=z(5, 16, dtype=i32))
+    for B, T in ((3, 1), (1, 3), (3, 2)):
+        table, lens = z(B, 2, dtype=i32), z(B, dtype=i32)
+        x, ok = z(1, 1, 2, 64).expand(B, T, 2, 64), z(B, T, 2, 64)
+        for call in (lambda: rs.rotary(x, None, z(B, T, dtype=i32), f), lambda: rs.rotary(ok, x, z(B, T, dtype=i32), f),
+                     lambda: rs.rotary(ok, None, z(B, T, dtype=i32), f, out=(x, None)),
+                     lambda: rs.attend_paged(x, cache, table, lens),
+                     lambda: rs.cache_append(cache, x, ok, z(B, T, dtype=i32), table, lens),
+                     lambda: rs.cache_append(cache, ok, x, z(B, T, dtype=i32), table, lens)):
+            with pytest.raises(ValueError, match="one stride"):
+                call()
+    one = torch.zeros(9, 2, 64, dtype=bf)[4].expand(1, 1, 2, 64)  # a single token is its own memory
+    with pytest.raises(ValueError, match="device tensors only"):
+        rs.rotary(one, None, z(1, 1, dtype=i32), f)
+
+
 def test_an_empty_table_needs_no_workspace_for_weights():
     """The smallest calls: no page a sequence. What the size query answers is enough; here the
     launch that follows finds no device, on the GPU the outputs are zeros."""
