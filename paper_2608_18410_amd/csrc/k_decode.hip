@@ -550,7 +550,7 @@ __device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len
 // SUB: value groups in a 16-byte piece of a row (1: a piece lies in one group).
 // ONCE: keys are loaded so that they leave the caches to other data (kOnceTokens).
 // Bound by memory from a few thousand tokens on: 64 sequences of 256 to 2048 tokens, 8
-// key heads of 4 rows (219 MB) 45 us, 4.8 TB/s; two of 131071 tokens and 32 heads (3.36
+// key heads of 4 rows (219 MB) 46 us, 4.7 TB/s; two of 131071 tokens and 32 heads (3.36
 // GB) 547 us, 6.1 TB/s, and 608 where the scores are stored for the weights, more
 // than their 33 MB explain. Below that by a chain of dependent loads (length, page, mask, key and value): one
 // of 305 tokens 8 us.
