@@ -145,6 +145,15 @@ def _current_stream(stream):
     return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
+def _returned(stream, *outputs):
+    """Outputs of a chain on `stream`, marked as in use by the caller's stream too."""
+    if stream is not None:
+        for t in outputs:
+            if t.is_cuda:
+                t.record_stream(torch.cuda.current_stream(t.device))
+    return outputs
+
+
 def page_count(tokens: int, page: int) -> int:
     """Pages that hold `tokens` tokens."""
     return -(-int(tokens) // page)
@@ -171,8 +180,9 @@ def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.Page
             q, k = rs.rotary(q, k, positions, inv_freq, axis)
         z = rs.rotate_values(v, R)
         rs.cache_append(cache, k, z, mask, table, lens)
-        return rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
-                               workspace=workspace, out=out)
+        out = rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
+                              workspace=workspace, out=out)
+    return _returned(stream, out)[0]
 
 
 def evict_layer(cache: rs.PagedCache, table, lens, mass, keep: int, first: int, recent: int, dst: rs.PagedCache,
@@ -196,4 +206,4 @@ def evict_layer(cache: rs.PagedCache, table, lens, mass, keep: int, first: int, 
             mass_out = torch.empty_like(mass) if mass.shape[1] >= keep else mass.new_empty((mass.shape[0], keep))
         mass_out.zero_()
         rs.cache_compact(cache, table, idx, n, dst, dst_table, mass=mass, mass_out=mass_out)
-        return n, mass_out, idx
+    return _returned(stream, n, mass_out, idx)

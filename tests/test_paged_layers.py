@@ -46,6 +46,47 @@ def test_evict_layer_refuses_before_it_clears_weights(calls):
     assert go(None)[1].shape == (2, 40)
 
 
+def test_layers_mark_their_outputs_for_the_callers_stream(monkeypatch):
+    """What is allocated on the chain's stream goes on with the caller's."""
+    marked, now = [], ["caller"]
+
+    class Out:
+        is_cuda, device, shape = True, "cuda:0", (2, 40)
+
+        def __init__(self, name):
+            self.name = name
+
+        def record_stream(self, s):
+            marked.append((self.name, s))
+
+        def zero_(self):
+            pass
+
+    class On:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            now.append(self.s)
+
+        def __exit__(self, *a):
+            now.pop()
+
+    monkeypatch.setattr(pipeline.torch.cuda, "stream", On)
+    monkeypatch.setattr(pipeline.torch.cuda, "current_stream", lambda d=None: now[-1])
+    monkeypatch.setattr(pipeline.torch, "empty_like", lambda t: Out("mass"))
+    monkeypatch.setattr(pipeline.rs, "route", lambda *a, **kw: {"mask": None})
+    monkeypatch.setattr(pipeline.rs, "rotate_values", lambda *a, **kw: None)
+    monkeypatch.setattr(pipeline.rs, "cache_append", lambda *a, **kw: None)
+    monkeypatch.setattr(pipeline.rs, "attend_paged", lambda *a, **kw: Out("out"))
+    monkeypatch.setattr(pipeline.rs, "evict_tokens", lambda *a, **kw: (Out("idx"), Out("n")))
+    monkeypatch.setattr(pipeline.rs, "cache_compact", lambda *a, **kw: None)
+    for stream in (None, "side"):
+        pipeline.decode_layer(*[None] * 12, stream=stream)
+        pipeline.evict_layer(None, None, None, Out("old"), 8, 0, 0, None, None, stream=stream)
+        assert marked == ([] if stream is None else [(x, "caller") for x in ("out", "n", "mass", "idx")])
+
+
 def test_expanded_operands_are_refused():
     """One token for many, without its own memory: not rows at a stride."""
     bf = torch.bfloat16
