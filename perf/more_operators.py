@@ -1,0 +1,743 @@
+"""Calls of the paged routed cache that long histories, drafted tokens and normed heads need, in plain torch and through the library.
+
+A case is one pass of one of:
+  norm    queries and keys divided by each head's root mean square, weighted, and turned by their positions
+  append  new tokens into a cache straight from the projections: keys normed and turned, values taken into the routing
+          space, their kept groups packed; queries normed and turned beside them
+  tree    attention of drafted tokens that form a tree, each over the cached tokens and its own ancestors: the masks from
+          the tokens' parents, then the attention
+  accept  drafted tokens appended, then the path of the last accepted one moved behind the cached tokens
+  sparse  a decoding step over few pages of a long history: the last page's bounds brought up to date, the pages chosen
+          whose bounds promise the highest scores, attention over those
+A cache holds pages of `page` tokens: keys K [pages, heads, page, dh]; the kept value groups of a page's tokens one after
+another, V [pages, heads, slots, dh/G]; each token's group mask and first slot. A sequence is a row of page numbers and a length.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+DEV = "cuda"
+EPS = 1e-6
+
+
+# ---------------------------------------------------------------------------
+# cases
+
+def _norm(name, **kw):
+    return {**dict(name=name, kind="norm", dtype="bf16", B=1, T=1, H=32, Hkv=32, dh=128, axes=3, pairs=64, pmax=4096,
+                   fused=False, interleaved=False), **kw}
+
+
+def _cache(name, kind, **kw):
+    return {**dict(name=name, kind=kind, dtype="bf16", B=1, lo=0, hi=0, page=64, Hkv=32, dh=128, G=8, kv=4, kl=6), **kw}
+
+
+def _append(name, **kw):
+    return {**_cache(name, "append", H=32, T=1, ragged=False, norm=True, R=True, axes=3, pairs=64, pmax=4096, fused=False,
+                     interleaved=False), **kw}
+
+
+def _tree(name, **kw):
+    return {**_cache(name, "tree", H=32, T=8, ragged=False, shared=False, R=True), **kw}
+
+
+def _accept(name, **kw):
+    return {**_cache(name, "accept", T=8, ragged=False, shared=False), **kw}
+
+
+def _sparse(name, **kw):
+    return {**_cache(name, "sparse", H=32, Tq=1, n_sel=32, first=1, recent=2, causal=False, R=True), **kw}
+
+
+def listed():
+    return [
+        # one robot's next token, three position axes: latency
+        _norm("norm-b1-token"),
+        # a batch of video prefixes straight from a fused projection: the largest of its kind
+        _norm("norm-b16-video", B=16, T=2048, Hkv=8, fused=True),
+        # one new token for each of 64 sequences
+        _append("append-b64-token", B=64, lo=113, hi=305, page=16, Hkv=8),
+        # prefixes of up to 305 tokens, from a fused projection, written behind what is cached
+        _append("append-b16-prefix", B=16, lo=0, hi=57, T=305, ragged=True, fused=True),
+        # one robot checks a draft of eight tokens over its prefix: latency
+        _tree("tree-b1-305", lo=305, hi=305),
+        # ordinary serving: 32 sequences of mixed lengths, drafts of up to 24 tokens, four query heads a key head
+        _tree("tree-b32-gqa", B=32, lo=256, hi=4096, T=24, page=16, Hkv=8, G=16, kv=4, kl=16, ragged=True),
+        # float32 evaluation of a smaller backbone, one tree for all sequences, odd lengths
+        _tree("tree-f32-dh64", dtype="f32", B=5, lo=1001, hi=3001, T=11, page=32, H=16, Hkv=4, dh=64, G=16, kv=5, kl=9, shared=True),
+        # one robot keeps what it accepts of eight drafted tokens
+        _accept("accept-b1-8", lo=305, hi=305),
+        # a batch, drafts of up to 60 tokens over several pages
+        _accept("accept-b32-60", B=32, lo=256, hi=1500, T=60, page=16, ragged=True),
+        # a history of a few thousand tokens: latency
+        _sparse("sparse-b1-2801", lo=2801, hi=2801, page=16, n_sel=24),
+        # a batch of mixed lengths, some shorter than what is chosen, four query heads a key head
+        _sparse("sparse-b32-8192", B=32, lo=900, hi=8192, Hkv=8, G=16, kv=4, kl=16),
+        # long histories: the largest
+        _sparse("sparse-b8-131071", B=8, lo=110001, hi=131071, Hkv=8, n_sel=128, first=1, recent=4),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["norm", "append", "append", "tree", "tree", "accept", "sparse", "sparse"])
+    dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
+    H, Hkv = rng.choice([(32, 32), (32, 8), (16, 16), (16, 4), (12, 4), (8, 1), (5, 5), (32, 2)])
+    dh = rng.choice([128, 128, 64])
+    e = 4 if dtype == "f32" else 2
+    turn = dict(axes=rng.randint(1, 4), pairs=rng.choice([dh // 2, dh // 2, dh // 4, rng.randint(1, dh // 2)]),
+                pmax=_log(rng, 64, 1 << 20), fused=rng.random() < 0.4, interleaved=rng.random() < 0.4)
+    if kind == "norm":
+        B = _log(rng, 1, 64)
+        return dict(kind=kind, dtype=dtype, B=B, T=max(1, min(_log(rng, 1, 4096), (32768 * 40 * 256) // (B * (H + Hkv) * dh * e))),
+                    H=H, Hkv=Hkv, dh=dh, **turn)
+    G = rng.choice([4, 8, 8, 16, 32])
+    c = dict(kind=kind, dtype=dtype, B=_log(rng, 1, 96), page=rng.choice([16, 32, 64, 64, 128, 256]), Hkv=Hkv, dh=dh, G=G,
+             kv=rng.randint(1, G), kl=rng.randint(1, G))
+    row = Hkv * dh * e
+    c["R"] = rng.random() < 0.7
+    if kind == "append":
+        c["H"] = rng.choice([H, H, H, 0])
+        c["T"] = max(1, min(_log(rng, 1, 700), (16 * 305 * 96 * 256) // (c["B"] * (2 * Hkv + c["H"]) * dh * e)))
+        c["lo"], c["hi"] = 0, rng.randint(0, 300)
+        return dict(c, ragged=rng.random() < 0.5, norm=rng.random() < 0.7, **turn)
+    if kind in ("tree", "accept"):
+        c["T"] = _log(rng, 1, 100)
+        # the keys and the products of a batch within those of the largest listed one
+        c["hi"] = max(1, min(_log(rng, 1, 16384), (32 * 4096 * 8 * 256) // (c["B"] * row)))
+        c["lo"] = rng.randint(0, c["hi"])
+        c["ragged"], c["shared"] = rng.random() < 0.5, rng.random() < 0.4
+        if kind == "tree":
+            c["H"] = H
+            c["T"] = max(1, min(c["T"], 10 ** 8 // (c["B"] * H * c["hi"]), (32 * 24 * 32 * 256) // (c["B"] * H * dh * e)))
+        else:
+            del c["R"]
+            c["T"] = max(1, min(c["T"], (32 * 60 * 32 * 256) // (c["B"] * row)))
+        return c
+    c["H"] = H
+    c["hi"] = max(c["page"], min(_log(rng, 64, 131071), (8 * 131071 * 8 * 256) // (c["B"] * row)))
+    c["lo"] = rng.randint(0, c["hi"])
+    c["Tq"] = min(rng.choice([1, 1, 1, rng.randint(2, 8)]), max(1, (8 * 2048 * 32) // (c["B"] * H * (c["hi"] // c["page"] + 1))))
+    most = max(1, (8 * 128 * 64 * 8 * 256) // (c["B"] * c["Tq"] * row * c["page"]))
+    c["n_sel"] = max(1, min(_log(rng, 1, 200), most))
+    c["first"] = rng.randint(0, min(2, c["n_sel"] // 2))
+    c["recent"] = rng.randint(0, min(6, c["n_sel"] - c["first"]))
+    c["causal"] = rng.random() < 0.5
+    return c
+
+
+def _lens(c):
+    """The lengths of a case's sequences, evenly from the longest to the shortest."""
+    return [c["hi"] - (c["hi"] - c["lo"]) * i // max(1, c["B"] - 1) for i in range(c["B"])]
+
+
+def _news(c):
+    """New tokens of each sequence: all, or evenly from all to (almost) none."""
+    return [c["T"] - (c["T"] * i // c["B"] if c["ragged"] else 0) for i in range(c["B"])]
+
+
+# ---------------------------------------------------------------------------
+# inputs
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(int(seed))
+
+
+def _rotations(g, n, size):
+    """n orthonormal size x size matrices: Walsh-Hadamard matrices between random sign flips."""
+    h = torch.ones((1, 1), dtype=torch.float64, device=DEV)
+    while h.shape[0] < size:
+        h = torch.cat((torch.cat((h, h), 1), torch.cat((h, -h), 1)), 0)
+    h = h / math.sqrt(size)
+    s = (torch.randint(0, 2, (3, n, size), generator=g, device=DEV) * 2 - 1).to(torch.float64)
+    return torch.matmul(s[0][:, :, None] * h * s[1][:, None, :], h * s[2][:, None, :])
+
+
+def _masks(c, g, *shape):
+    """Group masks: a quarter of the tokens (language) keep kl groups, the others (visual) kv."""
+    G = c["G"]
+    r = torch.rand((*shape, G), generator=g, device=DEV).argsort(-1).argsort(-1)
+    k = torch.where(torch.rand(shape, generator=g, device=DEV) < 0.25, c["kl"], c["kv"])
+    return ((r < k[..., None]).long() << torch.arange(G, device=DEV)).sum(-1).int()
+
+
+def _groups(mask, G):
+    """0/1 for each of a token's groups."""
+    return (mask.long()[..., None] >> torch.arange(G, device=DEV)) & 1
+
+
+def _pages(c, n_pages, g, dt):
+    """A cache whose pages are all full."""
+    P, H, dh, G = c["page"], c["Hkv"], c["dh"], c["G"]
+    vcap = P * max(c["kv"], c["kl"])
+    mask = _masks(c, g, n_pages, P)
+    n = _groups(mask, G).sum(-1)
+    return dict(K=torch.randn((n_pages, H, P, dh), generator=g, device=DEV, dtype=dt),
+                V=torch.randn((n_pages, H, vcap, dh // G), generator=g, device=DEV, dtype=dt),
+                mask=mask, slot=(n.cumsum(1) - n).int())
+
+
+def _table(B, width, g):
+    return torch.randperm(B * width, generator=g, device=DEV).reshape(B, width).int()
+
+
+def _ints(values):
+    return torch.tensor(values, dtype=torch.int32, device=DEV)
+
+
+def _turns(c, g):
+    n, A = c["pairs"], c["axes"]
+    i = torch.arange(n, device=DEV, dtype=torch.float64)
+    axis = (i * A / n).to(torch.uint8) if not c["interleaved"] else (i % A).to(torch.uint8)
+    weight = lambda: (1 + 0.1 * torch.randn(c["dh"], generator=g, device=DEV)).to(DT[c["dtype"]])  # noqa: E731
+    return dict(positions=torch.randint(0, c["pmax"], (c["B"], c["T"], A), generator=g, device=DEV, dtype=torch.int32),
+                inv_freq=(10000.0 ** (-i / n)).float(), axis=axis, wq=weight(), wk=weight())
+
+
+def _parents(rng, T):
+    """A drafted tree: half of the tokens go on where the last one stood, the others branch off anywhere before."""
+    return [j - 1 if rng.random() < 0.5 else rng.randint(-1, j - 1) for j in range(T)]
+
+
+def _tree_bits(parents):
+    """Ancestor bits (themselves among them), one whole number a drafted token."""
+    bits = []
+    for j, p in enumerate(parents):
+        bits.append((bits[p] if p >= 0 else 0) | 1 << j)
+    return bits
+
+
+def _words(rows, T):
+    """Ancestor bits as int32 words [.., T, ceil(T / 32)]."""
+    w = [[[(b >> 32 * i) & 0xFFFFFFFF for i in range(-(-T // 32))] for b in r] for r in rows]
+    return (torch.tensor(w, dtype=torch.int64) + 2 ** 31).remainder(2 ** 32).sub(2 ** 31).to(torch.int32).to(DEV)
+
+
+def _inputs(c, seed):
+    g, dt, rng = _gen(seed), DT[c["dtype"]], random.Random(seed)
+    randn = lambda *s: torch.randn(s, generator=g, device=DEV, dtype=dt)  # noqa: E731
+    B, Hkv, dh, kind = c["B"], c["Hkv"], c["dh"], c["kind"]
+    s = {}
+    if kind in ("norm", "append"):
+        T, H = c["T"], c["H"]
+        s = _turns(c, g)
+        if c["fused"]:
+            qkv = randn(B, T, (H + 2 * Hkv) * dh)
+            q, k, v = (x.unflatten(2, (-1, dh)) if x.shape[2] else None
+                       for x in qkv.split((H * dh, Hkv * dh, Hkv * dh), 2))
+        else:
+            q, k, v = randn(B, T, H, dh) if H else None, randn(B, T, Hkv, dh), randn(B, T, Hkv, dh)
+        s.update(q=q, k=k, v=v)
+        if kind == "norm":
+            return s
+    P = c["page"]
+    lens = _lens(c)
+    rng.shuffle(lens)
+    width = max(1, -(-(c["hi"] + c.get("T", 0)) // P))
+    s.update(_pages(c, B * width, g, dt), table=_table(B, width, g), lens=_ints(lens))
+    if "T" in c:
+        new = _news(c)
+        rng.shuffle(new)
+        s["n_new"] = _ints(new)
+        s["new_mask"] = _masks(c, g, B, c["T"])
+    s["R"] = _rotations(g, Hkv, dh).to(dt) if c.get("R") else None
+    if kind in ("tree", "accept"):
+        par = [_parents(rng, c["T"]) for _ in range(1 if c["shared"] else B)]
+        s["parents"] = _ints(par)
+    if kind == "tree":
+        s["q"] = randn(B, c["T"], c["H"], dh)
+    elif kind == "accept":
+        s["tree"] = _words([_tree_bits(p) for p in par], c["T"])
+        # the last accepted token of each draft; of a few none is
+        s["leaf"] = _ints([-1 if rng.random() < 0.1 else rng.randrange(n) if n else -1 for n in new])
+        s.update(k=randn(B, c["T"], Hkv, dh), z=randn(B, c["T"], Hkv, dh))
+    elif kind == "sparse":
+        s["q"] = randn(B, c["Tq"], c["H"], dh)
+        s["visible"] = (s["lens"][:, None] - torch.arange(c["Tq"] - 1, -1, -1, device=DEV, dtype=torch.int32)).clamp(min=0) \
+            if c["causal"] and c["Tq"] > 1 else None
+        # what a program holds: the bounds of all pages, of the last ones before their newest token
+        s["bounds"] = torch.stack((s["K"].amin(2), s["K"].amax(2)), 2)
+        for b, n in enumerate(lens):
+            if n and n % P != 1:
+                pg, r = int(s["table"][b, (n - 1) // P]), (n - 1) % P
+                s["bounds"][pg] = torch.stack((s["K"][pg, :, :r].amin(1), s["K"][pg, :, :r].amax(1)), 1) if r else 0
+    return s
+
+
+def prepare(case, seed):
+    c = case
+    s = dict(_inputs(c, seed), c=c)
+    if c["kind"] in ("tree", "sparse"):
+        s["out"] = torch.empty_like(s["q"])
+    if own:
+        import paper_2608_18410_amd as rs
+        if c["kind"] != "norm":
+            s["cache"] = rs.PagedCache(s["K"], s["V"], s["mask"], s["slot"])
+        room = lambda n: torch.empty(max(n, 1), dtype=torch.uint8, device=DEV)  # noqa: E731
+        if c["kind"] == "tree":
+            s["ws"] = room(rs.attend_tree_workspace_size(s["cache"], c["B"], c["H"], c["T"], c["hi"] + c["T"]))
+        elif c["kind"] == "sparse":
+            s["ws"] = room(max(rs.select_pages_workspace_size(s["cache"], c["B"], c["Tq"], c["hi"], c["n_sel"]),
+                               rs.attend_selected_workspace_size(s["cache"], c["B"], c["H"], c["Tq"], c["n_sel"])))
+    return s
+
+
+# ---------------------------------------------------------------------------
+# one pass through the library
+
+def _run_own(s):
+    import paper_2608_18410_amd as rs
+    c = s["c"]
+    if c["kind"] == "norm":
+        q, k = rs.norm_rotary(s["q"], s["k"], s["wq"], s["wk"], EPS, s["positions"], s["inv_freq"], s["axis"],
+                              interleaved=c["interleaved"])
+        return {"q": q, "k": k}
+    cached = {x: s[x] for x in ("K", "V", "mask", "slot")}
+    if c["kind"] == "append":
+        w = {"q_weight": s["wq"] if c["H"] else None, "k_weight": s["wk"], "eps": EPS} if c["norm"] else {}
+        q = rs.append_rotary(s["cache"], s["k"], s["v"], s["new_mask"], s["table"], s["lens"], s["positions"], s["inv_freq"],
+                             s["axis"], R=s["R"], q=s["q"], interleaved=c["interleaved"], n_new=s["n_new"], **w)
+        return {"q": q, **cached}
+    if c["kind"] == "tree":
+        tree, depth = rs.tree_masks(s["parents"])
+        out = rs.attend_tree(s["q"], s["cache"], s["table"], s["lens"], tree, s["R"], n_new=s["n_new"],
+                             max_len=c["hi"] + c["T"], workspace=s["ws"], out=s["out"])
+        return {"tree": tree, "depth": depth, "out": out}
+    if c["kind"] == "accept":
+        rs.cache_append(s["cache"], s["k"], s["z"], s["new_mask"], s["table"], s["lens"], n_new=s["n_new"])
+        n = rs.cache_accept(s["cache"], s["table"], s["lens"], s["tree"], s["leaf"])
+        return {"lens": n, **cached}
+    rs.page_bounds(s["cache"], s["table"], s["lens"], s["bounds"], 1)
+    sel = rs.select_pages(s["q"], s["cache"], s["bounds"], s["table"], s["lens"], c["n_sel"], first=c["first"],
+                          recent=c["recent"], visible=s["visible"], max_len=c["hi"], workspace=s["ws"])
+    out = rs.attend_selected(s["q"], s["cache"], s["table"], s["lens"], sel, s["R"], visible=s["visible"],
+                             workspace=s["ws"], out=s["out"])
+    return {"bounds": s["bounds"], "sel": sel, "out": out}
+
+
+# ---------------------------------------------------------------------------
+# the same in plain torch
+
+def _turn(x, cos, sin, n, interleaved):
+    """Pairs (i, i + n), or (2i, 2i + 1), of the last dimension turned; the dimensions past 2n stay."""
+    a, b = (x[..., 0: 2 * n: 2], x[..., 1: 2 * n: 2]) if interleaved else (x[..., :n], x[..., n: 2 * n])
+    ya, yb = a * cos - b * sin, a * sin + b * cos
+    y = torch.stack((ya, yb), -1).flatten(-2) if interleaved else torch.cat((ya, yb), -1)
+    return torch.cat((y, x[..., 2 * n:]), -1)
+
+
+def _plain_turned(s, norm):
+    c = s["c"]
+    a = s["positions"].double()[..., s["axis"].long()] * s["inv_freq"].double()
+    cos, sin = torch.cos(a).float()[:, :, None], torch.sin(a).float()[:, :, None]
+    out = []
+    for x, w in ((s["q"], s["wq"]), (s["k"], s["wk"])):
+        if x is None:
+            out.append(None)
+            continue
+        y = x.float()
+        if norm:
+            y = y / torch.sqrt((y * y).mean(-1, keepdim=True) + EPS) * w.float()
+        out.append(_turn(y, cos, sin, c["pairs"], c["interleaved"]).to(x.dtype))
+    return out
+
+
+def _plain_norm(s):
+    q, k = _plain_turned(s, True)
+    return {"q": q, "k": k}
+
+
+def _put(dst, page, row, take, k, z_groups, mask, page_start):
+    """Tokens [B, T] into pages: keys k [B, T, H, dh], groups z [B, T, H, G, ds]; `take` says which are there, page_start
+    the slots taken before a token's page-mates among them."""
+    G = z_groups.shape[3]
+    bits = _groups(mask, G) * take[..., None]
+    n = bits.sum(-1)
+    before = n.cumsum(1) - n
+    first = torch.cat((torch.ones_like(page[:, :1], dtype=torch.bool), page[:, 1:] != page[:, :-1]), 1)
+    base = torch.where(first, before, torch.zeros_like(before)).cummax(1).values
+    start = before - base + page_start
+    p, r = page[take], row[take]
+    dst["K"][p, :, r] = k[take]
+    dst["mask"][p, r] = mask[take]
+    dst["slot"][p, r] = start[take].int()
+    at = start[..., None] + bits.cumsum(-1) - bits
+    kept = bits > 0
+    dst["V"][page[..., None].expand_as(kept)[kept], :, at[kept]] = z_groups.transpose(2, 3)[kept]
+
+
+def _places(s, n):
+    """Pages and rows of the n places behind the cached tokens, and the slots that those of the first page have taken."""
+    P, G = s["c"]["page"], s["c"]["G"]
+    lens = s["lens"].long()[:, None]
+    t = lens + torch.arange(n, device=DEV)[None]
+    page, row = torch.gather(s["table"].long(), 1, t // P), t % P
+    prev = (lens - 1).clamp(min=0)
+    pp, pr = torch.gather(s["table"].long(), 1, prev // P), prev % P
+    used = s["slot"][pp, pr].long() + _groups(s["mask"][pp, pr], G).sum(-1)
+    return page, row, torch.where((lens % P > 0) & (t // P == lens // P), used, torch.zeros_like(used))
+
+
+def _plain_put_new(s, k, z):
+    c = s["c"]
+    page, row, used = _places(s, c["T"])
+    take = torch.arange(c["T"], device=DEV)[None] < s["n_new"].long()[:, None]
+    _put(s, page, row, take, k, z.unflatten(3, (c["G"], -1)), s["new_mask"], used)
+
+
+def _plain_append(s):
+    q, k = _plain_turned(s, s["c"]["norm"])
+    z = s["v"]
+    if s["R"] is not None:
+        z = torch.matmul(z.float().transpose(1, 2), s["R"].float()).transpose(1, 2).to(z.dtype)
+    _plain_put_new(s, k, z)
+    return {"q": q, **{x: s[x] for x in ("K", "V", "mask", "slot")}}
+
+
+def _fetch(s, page, row):
+    """Keys [.., Hkv, dh], groups [.., Hkv, G, ds] (dropped ones zero) and masks of cached tokens."""
+    G = s["c"]["G"]
+    m = s["mask"][page, row]
+    bits = _groups(m, G)
+    at = (s["slot"][page, row].long()[..., None] + bits.cumsum(-1) - bits).clamp(max=s["V"].shape[2] - 1)
+    z = s["V"][page[..., None], :, at] * bits[..., None, None].to(s["V"].dtype)
+    return s["K"][page, :, row], z.transpose(-3, -2), m
+
+
+def _softmax_sum(x, see, z):
+    """Softmax over what each row sees, times the values; zeros where it sees nothing."""
+    top = torch.where(see, x, -1e30).amax(-1, keepdim=True)
+    e = torch.where(see, torch.exp(x - top), 0.0)
+    return torch.matmul(e / e.sum(-1, keepdim=True).clamp(min=1e-30), z)
+
+
+def _plain_tree(s):
+    c = s["c"]
+    T, P, H, Hkv, dh, L = c["T"], c["page"], c["H"], c["Hkv"], c["dh"], c["hi"] + c["T"]
+    # ancestors [trees, T, T] and their numbers, a generation at a time
+    up = s["parents"].long()
+    see = torch.eye(T, dtype=torch.bool, device=DEV).repeat(up.shape[0], 1, 1)
+    at, depth = up, torch.zeros_like(up)
+    for _ in range(T - 1):
+        there = at >= 0
+        see.scatter_(2, at.clamp(min=0)[..., None], see.gather(2, at.clamp(min=0)[..., None]) | there[..., None])
+        depth = depth + there
+        at = torch.where(there, up.gather(1, at.clamp(min=0)), -1)
+    W = -(-T // 32)
+    pad = torch.cat((see, see.new_zeros((*see.shape[:2], 32 * W - T))), 2).unflatten(2, (W, 32)).long()
+    word = (pad << torch.arange(32, device=DEV)).sum(-1)
+    tree = torch.where(word >= 2 ** 31, word - 2 ** 32, word).int()
+    # attention
+    t = torch.arange(L, device=DEV)
+    step = max(1, (1 << 30) // max(1, L * Hkv * dh * 4))  # sequences at a time: about 1 GiB of keys
+    for b in range(0, c["B"], step):
+        sl = slice(b, b + step)
+        K, z, _ = _fetch(s, s["table"][sl].long()[:, t // P], (t % P).expand(s["table"][sl].shape[0], L))
+        K, z = K.float().transpose(1, 2), z.float().flatten(3).transpose(1, 2)  # [b, Hkv, L, dh]
+        q = s["q"][sl].float().unflatten(2, (Hkv, H // Hkv)).permute(0, 2, 3, 1, 4).flatten(2, 3)  # [b, Hkv, rep * T, dh]
+        x = torch.matmul(q, K.transpose(2, 3)) / math.sqrt(dh)
+        i = t - s["lens"][sl].long()[:, None]  # [b, L]: which drafted token, cached ones below 0
+        n = s["n_new"][sl].long()
+        anc = (see if c["shared"] else see[sl]).expand(i.shape[0], T, T)
+        anc = torch.gather(anc, 2, i.clamp(0, T - 1)[:, None].expand(-1, T, -1))
+        ok = ((i < 0)[:, None] | (anc & ((i >= 0) & (i < n[:, None]))[:, None])) & (torch.arange(T, device=DEV) < n[:, None])[..., None]
+        u = _softmax_sum(x, ok.repeat(1, H // Hkv, 1)[:, None], z)
+        if s["R"] is not None:
+            u = torch.matmul(u, s["R"].float().transpose(1, 2))
+        s["out"][sl] = u.unflatten(2, (H // Hkv, T)).permute(0, 3, 1, 2, 4).flatten(2, 3).to(s["out"].dtype)
+    return {"tree": tree, "depth": depth.int(), "out": s["out"]}
+
+
+def _plain_accept(s):
+    c = s["c"]
+    T, G = c["T"], c["G"]
+    _plain_put_new(s, s["k"], s["z"])
+    page, row, used = _places(s, T)
+    i = torch.arange(T, device=DEV)
+    leaf = s["leaf"].long()
+    rows = s["tree"].expand(c["B"], -1, -1)[torch.arange(c["B"], device=DEV), leaf.clamp(min=0)].long()  # [B, words]
+    on = ((rows[:, i // 32] >> (i % 32)) & 1).bool() & (leaf >= 0)[:, None]
+    n = on.sum(1)
+    frm = torch.sort(torch.where(on, i, T), 1).values.clamp(max=T - 1)
+    k, z, m = _fetch(s, page.gather(1, frm), row.gather(1, frm))
+    _put(s, page, row, i < n[:, None], k, z, m, used)
+    return {"lens": s["lens"] + n.int(), **{x: s[x] for x in ("K", "V", "mask", "slot")}}
+
+
+def _plain_sparse(s):
+    c = s["c"]
+    B, P, H, Hkv, dh, Tq, G, n_sel = c["B"], c["page"], c["H"], c["Hkv"], c["dh"], c["Tq"], c["G"], c["n_sel"]
+    rep, W = H // Hkv, s["table"].shape[1]
+    lens, table = s["lens"].long(), s["table"].long()
+    # the last page's bounds
+    last = (lens - 1).clamp(min=0)
+    pg = torch.gather(table, 1, (last // P)[:, None])[:, 0]
+    there = (torch.arange(P, device=DEV) <= (last % P)[:, None])[:, None, :, None]
+    K = s["K"][pg]
+    new = torch.stack((torch.where(there, K, math.inf).amin(2), torch.where(there, K, -math.inf).amax(2)), 2)
+    some = lens > 0
+    s["bounds"][pg[some]] = new[some]
+    # the highest score a key within the bounds could have, of the heads that share a key head the highest; in 64 bits, as
+    # many pages are near the border, rounded once
+    see = lens[:, None].expand(B, Tq)
+    if s["visible"] is not None:
+        see = torch.minimum(see, s["visible"].long())
+    count = (see + P - 1) // P  # [B, Tq]
+    q = s["q"].double().unflatten(2, (Hkv, rep)).transpose(1, 2)  # [B, Hkv, Tq, rep, dh]
+    score = torch.empty((B, Tq, Hkv, W), device=DEV)
+    step = max(1, (1 << 30) // (W * Hkv * dh * 16))
+    for b in range(0, B, step):
+        sl = slice(b, b + step)
+        bd = s["bounds"][table[sl]].double()  # [b, W, Hkv, 2, dh]
+        both = torch.cat((bd[..., 0, :], bd[..., 1, :]), -1).transpose(1, 2)  # [b, Hkv, W, 2 dh]
+        x = torch.cat((q[sl].clamp(max=0), q[sl].clamp(min=0)), -1).flatten(2, 3)  # [b, Hkv, Tq rep, 2 dh]
+        score[sl] = torch.matmul(x, both.transpose(2, 3)).unflatten(2, (Tq, rep)).amax(3).transpose(1, 2).float()
+    i = torch.arange(W, device=DEV)
+    n = count[:, :, None, None]
+    key = torch.where((i < c["first"]) | (i >= n - c["recent"]), math.inf, score)
+    key = torch.where(i < n, key, -math.inf)
+    order = torch.sort(key, dim=-1, descending=True, stable=True).indices[..., :n_sel]
+    if order.shape[-1] < n_sel:
+        order = torch.cat((order, order.new_full((*order.shape[:-1], n_sel - order.shape[-1]), W)), -1)
+    take = torch.arange(n_sel, device=DEV) < n
+    sel = torch.where(take, order, W).sort(-1).values
+    sel = torch.where(take, sel, -1)
+    # attention over their tokens
+    R = None if s["R"] is None else s["R"].float().transpose(1, 2)
+    step = max(1, (1 << 28) // (Tq * Hkv * n_sel * P * dh))
+    h = torch.arange(Hkv, device=DEV)[:, None]
+    for b in range(0, B, step):
+        sl = slice(b, b + step)
+        at = sel[sl].clamp(min=0)
+        page = torch.gather(table[sl][:, None, None].expand(-1, Tq, Hkv, -1), 3, at)  # [b, Tq, Hkv, n_sel]
+        K = s["K"][page, h].float().flatten(3, 4)  # [b, Tq, Hkv, n_sel P, dh]
+        m = s["mask"][page]
+        bits = _groups(m, G)
+        slot = (s["slot"][page].long()[..., None] + bits.cumsum(-1) - bits).clamp(max=s["V"].shape[2] - 1)
+        z = s["V"][page[..., None, None], h[:, :, None, None], slot].float() * bits[..., None]
+        z = z.flatten(5).flatten(3, 4)
+        t = (at[..., None] * P + torch.arange(P, device=DEV))
+        ok = ((t < see[sl][:, :, None, None, None]) & (sel[sl] >= 0)[..., None]).flatten(3)
+        x = torch.matmul(s["q"][sl].float().unflatten(2, (Hkv, rep)), K.transpose(3, 4)) / math.sqrt(dh)
+        u = _softmax_sum(x, ok[:, :, :, None], z)
+        if R is not None:
+            u = torch.matmul(u, R)
+        s["out"][sl] = u.flatten(2, 3).to(s["out"].dtype)
+    return {"bounds": s["bounds"], "sel": sel.int(), "out": s["out"]}
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"norm": _plain_norm, "append": _plain_append, "tree": _plain_tree, "accept": _plain_accept,
+            "sparse": _plain_sparse}[state["c"]["kind"]](state)
+
+
+# ---------------------------------------------------------------------------
+# the least work of a pass
+
+def work(case):
+    c = case
+    e = 2 if c["dtype"] == "bf16" else 4
+    dh, Hkv = c["dh"], c["Hkv"]
+    if c["kind"] == "norm":
+        n = c["B"] * c["T"]
+        return {"bytes": n * (2 * (c["H"] + Hkv) * dh * e + 4 * c["axes"]) + 5 * c["pairs"] + 2 * dh * e,
+                "flops": n * ((c["H"] + Hkv) * (c["pairs"] * 6 + 4 * dh) + 40 * c["pairs"])}
+    row = Hkv * dh * e
+    kept = (0.25 * c["kl"] + 0.75 * c["kv"]) / c["G"]  # share of a value
+    turn = Hkv * dh * dh
+    if c["kind"] == "append":
+        # key and value in, key and kept groups out; all queries, those behind a sequence's new tokens too
+        n, q = sum(_news(c)), c["B"] * c["T"]
+        value = 1 + kept if c["R"] else 2 * kept
+        return {"bytes": int(n * (row * (2 + value) + 12) + q * (2 * c["H"] * dh * e + 4 * c["axes"]) + (turn * e if c["R"] else 0)),
+                "flops": int(n * 2 * turn * c["R"] + (n * Hkv + q * c["H"]) * (6 * c["pairs"] + (4 * dh if c["norm"] else 0)))}
+    if c["kind"] == "accept":
+        n = sum(_news(c))
+        moved = sum(min(x, 2 + x / 8) for x in _news(c))  # about as many of a tree's tokens lie on a path
+        return {"bytes": int((n + moved) * (2 * row * (1 + kept) + 16)), "flops": 0}
+    if c["kind"] == "tree":
+        by, fl = 0, 0
+        for x, n in zip(_lens(c), _news(c)):
+            by += (x + n) * (row * (1 + kept) + 8)
+            fl += 2 * (x + min(n, 8)) * n * c["H"] * dh * (1 + kept)
+        heads = c["B"] * c["T"] * c["H"] * dh
+        by += 2 * heads * e + (1 if c["shared"] else c["B"]) * c["T"] * (8 + 4 * (-(-c["T"] // 32)))
+        if c["R"]:
+            by += turn * e
+            fl += 2 * heads * dh
+        return {"bytes": int(by), "flops": int(fl)}
+    # every page's bounds once for a sequence's queries, the chosen pages for each query
+    pages, tokens = 0, 0
+    for x in _lens(c):
+        pages += -(-x // c["page"])
+        tokens += c["Tq"] * min(x, c["n_sel"] * c["page"])
+    heads = c["B"] * c["Tq"] * c["H"] * dh
+    by = pages * 2 * row + tokens * (row * (1 + kept) + 8) + 2 * heads * e + c["B"] * c["page"] * row
+    fl = pages * c["Tq"] * c["H"] * dh * 2 + 2 * tokens * c["H"] * dh * (1 + kept)
+    if c["R"]:
+        by += turn * e
+        fl += 2 * heads * dh
+    return {"bytes": int(by), "flops": int(fl)}
+
+
+# ---------------------------------------------------------------------------
+# the same in 64 bits, from the formulas, one sequence at a time
+
+def _dense(s, pages, n, c):
+    """Keys and masked values [n, Hkv, dh] of the first n tokens of these pages."""
+    P, G = c["page"], c["G"]
+    ks, vs = [], []
+    for i, p in enumerate(pages[: -(-n // P)]):
+        m = min(P, n - i * P)
+        ks.append(s["K"][p, :, :m].double().transpose(0, 1))
+        on = _groups(s["mask"][p, :m], G).bool()  # [m, G]
+        v = torch.zeros((m, G, c["Hkv"], c["dh"] // G), dtype=torch.float64, device=DEV)
+        tok, grp = on.nonzero(as_tuple=True)  # a page's groups lie in this order
+        v[tok, grp] = s["V"][p, :, : tok.numel()].double().transpose(0, 1)
+        vs.append(v.transpose(1, 2).flatten(2))
+    return torch.cat(ks), torch.cat(vs)
+
+
+def _exact_turned(s, c, x, w):
+    n = c["pairs"]
+    ang = torch.stack([s["positions"][..., int(a)].double() * f.double() for a, f in zip(s["axis"].tolist(), s["inv_freq"])], -1)
+    y = x.double()
+    if w is not None:
+        y = y * torch.rsqrt(y.square().sum(-1, keepdim=True) / c["dh"] + EPS) * w.double()
+    i = torch.arange(n, device=DEV)
+    i, j = (2 * i, 2 * i + 1) if c["interleaved"] else (i, i + n)
+    zc = torch.complex(y[..., i], y[..., j]) * torch.polar(torch.ones_like(ang), ang)[:, :, None]
+    y = y.clone()
+    y[..., i], y[..., j] = zc.real, zc.imag
+    return y
+
+
+def _exact_put(s, c, K, V, k, z):
+    """New tokens written one by one."""
+    P, G = c["page"], c["G"]
+    on = _groups(s["new_mask"], G).bool().cpu()
+    table, lens, new = s["table"].tolist(), s["lens"].tolist(), s["n_new"].tolist()
+    old = _groups(s["mask"], G).sum(-1).cpu()
+    for b in range(c["B"]):
+        used = int(old[table[b][lens[b] // P], : lens[b] % P].sum()) if lens[b] % P else 0
+        for j in range(new[b]):
+            p, r = table[b][(lens[b] + j) // P], (lens[b] + j) % P
+            used = 0 if r == 0 else used
+            g = on[b, j].nonzero()[:, 0]
+            K[p, :, r] = k[b, j]
+            V[p, :, used: used + len(g)] = z[b, j].unflatten(1, (G, -1))[:, g.to(DEV)]
+            used += len(g)
+
+
+def _exact_append(s, c):
+    K, V = s["K"].double(), s["V"].double()
+    z = s["v"].double()
+    if s["R"] is not None:
+        z = (z.unsqueeze(-2) @ s["R"].double()).squeeze(-2)
+    norm = c["norm"]
+    _exact_put(s, c, K, V, _exact_turned(s, c, s["k"], s["wk"] if norm else None), z)
+    q = None if s["q"] is None else _exact_turned(s, c, s["q"], s["wq"] if norm else None)
+    return {"q": q, "K": K, "V": V, "mask": None, "slot": None}
+
+
+def _exact_accept(s, c):
+    K, V = s["K"].double(), s["V"].double()
+    k, z = s["k"].double(), s["z"].double()
+    _exact_put(s, c, K, V, k, z)
+    P, G = c["page"], c["G"]
+    on = _groups(s["new_mask"], G).bool().cpu()
+    old = _groups(s["mask"], G).sum(-1).cpu()
+    table, lens, tree = s["table"].tolist(), s["lens"].tolist(), s["tree"].tolist()
+    for b, leaf in enumerate(s["leaf"].tolist()):
+        if leaf < 0:
+            continue
+        words = tree[0 if c["shared"] else b][leaf]
+        path = [i for i in range(c["T"]) if words[i // 32] >> (i % 32) & 1]
+        used = int(old[table[b][lens[b] // P], : lens[b] % P].sum()) if lens[b] % P else 0
+        for j, i in enumerate(path):  # from the new tokens themselves
+            p, r = table[b][(lens[b] + j) // P], (lens[b] + j) % P
+            used = 0 if r == 0 else used
+            g = on[b, i].nonzero()[:, 0].to(DEV)
+            K[p, :, r] = k[b, i]
+            V[p, :, used: used + len(g)] = z[b, i].unflatten(1, (G, -1))[:, g]
+            used += len(g)
+    return {"lens": None, "K": K, "V": V, "mask": None, "slot": None}
+
+
+def _exact_heads(s, c, b, j, K, V, hidden, out, heads):
+    rep = c["H"] // c["Hkv"]
+    for h in heads:
+        kv = h // rep
+        x = (s["q"][b, j, h].double() @ K[:, kv].T) * c["dh"] ** -0.5
+        p = torch.softmax(x.masked_fill(hidden, -math.inf), -1).nan_to_num(0.0)
+        u = p @ V[:, kv]
+        out[b, j, h] = u if s["R"] is None else s["R"][kv].double() @ u
+
+
+def _exact_tree(s, c):
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device=DEV)
+    table, par = s["table"].tolist(), s["parents"].tolist()
+    if sum(_news(c)) * c["H"] > 30000:
+        return None
+    for b, (n, new) in enumerate(zip(s["lens"].tolist(), s["n_new"].tolist())):
+        if n + new == 0:
+            continue
+        K, V = _dense(s, table[b], n + new, c)
+        bits = _tree_bits(par[0 if c["shared"] else b])
+        for j in range(new):
+            hidden = torch.tensor([False] * n + [not bits[j] >> i & 1 for i in range(new)], device=DEV)
+            _exact_heads(s, c, b, j, K, V, hidden, out, range(c["H"]))
+    return {"tree": None, "depth": None, "out": out}
+
+
+def _exact_sparse(s, c):
+    P, Hkv, Tq = c["page"], c["Hkv"], c["Tq"]
+    rep = c["H"] // Hkv
+    if c["B"] * Tq * c["H"] > 4000:
+        return None
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device=DEV)
+    bounds = s["bounds"].double()
+    table = s["table"].tolist()
+    for b, n in enumerate(s["lens"].tolist()):
+        if n:
+            p, r = table[b][(n - 1) // P], (n - 1) % P + 1
+            bounds[p, :, 0], bounds[p, :, 1] = s["K"][p, :, :r].double().amin(1), s["K"][p, :, :r].double().amax(1)
+    for b, n in enumerate(s["lens"].tolist()):
+        for j in range(Tq):
+            see = n if s["visible"] is None else min(n, int(s["visible"][b, j]))
+            m = -(-see // P)
+            if m == 0:
+                continue
+            bd = bounds[s["table"][b, :m].long()]  # [m, Hkv, 2, dh]
+            for h in range(Hkv):
+                q = s["q"][b, j, h * rep: (h + 1) * rep].double()[:, None]
+                score = torch.maximum(q * bd[:, h, 0], q * bd[:, h, 1]).sum(-1).amax(0).float()
+                i = torch.arange(m, device=DEV)
+                if m > c["n_sel"]:
+                    safe = (i < c["first"]) | (i >= m - c["recent"])
+                    free = i[~safe]
+                    best = free[torch.argsort(-score[free], stable=True)[: c["n_sel"] - int(safe.sum())]]
+                    i = torch.cat((i[safe], best)).sort().values
+                hidden = torch.cat([torch.arange(x * P, x * P + P, device=DEV) >= see for x in i.tolist()])
+                pages = [table[b][x] for x in i.tolist()]
+                one = dict(s, K=s["K"][:, h: h + 1], V=s["V"][:, h: h + 1])
+                K, V = _dense(one, pages, P * len(pages), dict(c, Hkv=1))
+                K, V = K.expand(-1, Hkv, -1), V.expand(-1, Hkv, -1)
+                _exact_heads(s, c, b, j, K, V, hidden, out, range(h * rep, (h + 1) * rep))
+    return {"bounds": bounds, "sel": None, "out": out}
+
+
+def exact(case, seed):
+    s, c = _inputs(case, seed), case
+    if c["kind"] == "norm":
+        return {"q": _exact_turned(s, c, s["q"], s["wq"]), "k": _exact_turned(s, c, s["k"], s["wk"])}
+    return {"append": _exact_append, "tree": _exact_tree, "accept": _exact_accept, "sparse": _exact_sparse}[c["kind"]](s, c)
