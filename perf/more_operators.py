@@ -284,7 +284,7 @@ def prepare(case, seed):
         if c["kind"] == "tree":
             s["ws"] = room(rs.attend_tree_workspace_size(s["cache"], c["B"], c["H"], c["T"], c["hi"] + c["T"]))
         elif c["kind"] == "sparse":
-            s["ws"] = room(max(rs.select_pages_workspace_size(s["cache"], c["B"], c["Tq"], c["hi"], c["n_sel"]),
+            s["ws"] = room(max(rs.select_pages_workspace_size(s["cache"], c["B"], c["Tq"], c["hi"]),
                                rs.attend_selected_workspace_size(s["cache"], c["B"], c["H"], c["Tq"], c["n_sel"])))
     return s
 
