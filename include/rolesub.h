@@ -556,6 +556,157 @@ rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pag
                                      int32_t dst_max_pages, const float* mass_in, int64_t mass_ld, float* mass_out,
                                      int64_t mass_out_ld, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * rolesub_norm_rotary: queries and keys divided by the root mean square of their
+ * head, weighted, and turned by their positions in the same pass (the queries and
+ * keys of Sec. 3 as inputs of the attention calls):
+ *   n = x w / sqrt(mean(x^2) + eps)   per token and head, then rolesub_rotary's turn
+ * in 32 bits throughout, rounded once.
+ *   q_weight, k_weight [dh] (dtype) or NULL: that tensor is not normed, only turned
+ *   (then with rolesub_rotary's results, bit for bit); eps > 0, finite.
+ *   The other arguments, strides, outputs and errors are those of rolesub_rotary.
+ * A head whose squares pass the range of 32 bits is normed all the same; an infinity
+ * gives NaN in its place and zeros in its head's other dims before the turn.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_norm_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int32_t dh, rolesub_dtype dtype,
+                                   const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                   const void* q_weight, const void* k_weight, float eps, const int32_t* positions,
+                                   int32_t n_axes, const float* inv_freq, const uint8_t* axis, int32_t n_pairs,
+                                   int32_t interleaved, void* q_out, void* k_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_append_rotary: the next tokens of every sequence from their projections
+ * into its pages: rolesub_norm_rotary of the keys, rolesub_rotate_values of the
+ * values (Sec. 3.2) and rolesub_cache_append in one pass, with the queries normed
+ * and turned beside them; neither the turned keys nor z are stored elsewhere.
+ *   q [B,T,Hq,dh] or NULL (Hq, q_weight and q_out are then not used), k and v
+ *   [B,T,H,dh] (dtype), token strides q_stride, k_stride, v_stride;
+ *   R [H,dh,dh] or NULL (v is kept as it is, for a cache read with R = NULL);
+ *   q_weight, k_weight, eps, positions .. interleaved as rolesub_norm_rotary;
+ *   mask, table, lens, n_new and what is dropped as rolesub_cache_append;
+ *   q_out: all T tokens' queries, dense, or q itself.
+ * The cache holds the bits that the separate calls would leave there. No operand lies
+ * in the cache, and q_out in none but q; lens is not changed.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_append_rotary(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T, int32_t Hq,
+                                     const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                     int64_t v_stride, const void* R, const uint32_t* mask, const void* q_weight,
+                                     const void* k_weight, float eps, const int32_t* positions, int32_t n_axes,
+                                     const float* inv_freq, const uint8_t* axis, int32_t n_pairs, int32_t interleaved,
+                                     const int32_t* table, int32_t max_pages, const int32_t* lens, const int32_t* n_new,
+                                     void* q_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Drafted tokens: several continuations of a sequence at once, as a tree whose tokens
+ * lie behind the cached ones, each parent before its children. They are appended like
+ * other tokens, attend to the cached tokens and to their ancestors, and of those that
+ * are accepted the last one's path is kept.
+ *
+ * rolesub_tree_masks: the tokens' ancestors from their parents.
+ *   parents [B,T] int32: the parent's number among the T drafted tokens; a number that
+ *   is not below the token's own, or negative: a child of the cached tokens
+ *   tree  [B,T,ceil(T/32)] uint32: bit i % 32 of word i / 32 set for the token itself
+ *         and each of its ancestors
+ *   depth [B,T] int32 or NULL: how many ancestors (its place is lens + depth)
+ * T <= 256. No output lies in another operand.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_tree_masks(int32_t B, int32_t T, const int32_t* parents, uint32_t* tree, int32_t* depth,
+                                  void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_attend_tree: attention of drafted tokens over the paged cache, which holds
+ * them from lens[b] on: rolesub_attend_paged where row j of sequence b sees
+ *   the tokens t < lens[b], and lens[b] + i for i < n_new[b] with bit i of tree[b,j].
+ *   lens [B] int32: cached tokens before the drafted ones; n_new [B] int32 or NULL:
+ *   drafted tokens of each sequence (clamped to [0, Tq]; NULL: Tq); a row past them
+ *   sees nothing and gives zeros
+ *   tree [trees,Tq,ceil(Tq/32)] uint32, trees = B, or 1: one for all sequences. Any
+ *   bits may be set; those of tokens past n_new[b] are not looked at
+ *   max_len: no token past it is seen (0: max_pages*page); it bounds lens + n_new
+ * Tq <= 256. The other arguments, the workspace and errors as rolesub_attend_paged;
+ * no weights are added up, as it is not known yet which tokens stay.
+ * ------------------------------------------------------------------------ */
+size_t rolesub_attend_tree_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq, int32_t max_len);
+rolesub_status rolesub_attend_tree(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                   const void* q, int64_t q_stride, const int32_t* table, int32_t max_pages,
+                                   const int32_t* lens, const int32_t* n_new, const uint32_t* tree, int32_t trees,
+                                   int32_t max_len, const void* R, float scale, void* out, rolesub_dtype out_dtype,
+                                   void* workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_cache_accept: the path of the last accepted drafted token moved behind the
+ * cached tokens, in the pages where it lies: with i_0 < i_1 < .. the bits set in
+ * tree[b, leaf[b]], token lens[b] + i_j becomes token lens[b] + j (key, mask, groups).
+ *   leaf [B] int32: the last accepted token's number among the T drafted ones; outside
+ *   [0, T) none is accepted
+ *   tree [trees,T,ceil(T/32)], trees = B or 1; bits from T on are not looked at
+ *   new_lens [B] int32 or NULL: lens[b] + how many were kept
+ * The drafted tokens were appended behind lens[b] by one call or several; the entries
+ * past the new length are of no sequence any more. A path token that is not cached (past
+ * the table, or in a page that is none) becomes a key of zeros that keeps no group. T <=
+ * 256; no two sequences may hold drafted tokens in one page; table, lens, tree, leaf and
+ * new_lens lie outside the cache and new_lens apart from the others.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_cache_accept(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
+                                    const int32_t* table, int32_t max_pages, const int32_t* lens, const uint32_t* tree,
+                                    int32_t trees, const int32_t* leaf, int32_t* new_lens, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Few pages of a long history: each query and key head attends to the tokens of the
+ * pages that can hold the highest scores, which bounds of their keys tell.
+ *
+ * rolesub_page_bounds: the bounds of the pages that hold a sequence's last T tokens
+ * (T >= the longest sequence: all), over the tokens that lie in them:
+ *   bounds[page,h,0,d] = min_t K[page,h,t,d],  bounds[page,h,1,d] = max_t K[page,h,t,d]
+ *   bounds [n_pages,H,2,dh] (dtype), 16-byte aligned, outside the cache and apart from
+ *   table and lens; lens [B] int32 counts the new tokens. Other pages' are not written.
+ * NaN is passed over (a dim of nothing else has +inf below -inf). To be called after
+ * tokens are appended, and, for all pages, after they are moved.
+ * ------------------------------------------------------------------------ */
+rolesub_status rolesub_page_bounds(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
+                                   const int32_t* table, int32_t max_pages, const int32_t* lens, void* bounds,
+                                   void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_select_pages: which n_sel pages each query and key head attends to: the first
+ * `first` and the last `recent` of those it sees, and of the others the ones with the
+ * highest bounds (a larger one first, equal ones by lower index, NaN after every number):
+ *   bound(i, head) = sum_d (q_d < 0 ? q_d lo_d : q_d hi_d), the highest over the Hq / H
+ *   heads of a key head; no key of the page scores higher. Summed in 64 bits and rounded
+ *   to 32 once. (With a negative scale, pass the negated queries.)
+ *   q [B,Tq,Hq,dh] (dtype), token stride q_stride; bounds as rolesub_page_bounds leaves
+ *   them; table, lens, visible, max_len as rolesub_attend_paged. A query sees the pages
+ *   of its min(lens[b], max_len, visible[b,j]) tokens; one that is none has bound NaN.
+ *   n_sel >= 1; first, recent >= 0, first + recent <= n_sel
+ *   sel [B,Tq,H,n_sel] int32: the pages' numbers in the sequence, ascending, then -1
+ *   workspace: at least rolesub_select_pages_workspace_size() bytes (which does not
+ *   fall as B, Tq or max_len grows), 16-byte aligned; nothing in it needs clearing;
+ *   calls (and graphs) that may overlap must not share one. sel and the workspace lie
+ *   apart from the other operands.
+ * ------------------------------------------------------------------------ */
+size_t rolesub_select_pages_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Tq, int32_t max_len);
+rolesub_status rolesub_select_pages(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                    const void* q, int64_t q_stride, const void* bounds, const int32_t* table,
+                                    int32_t max_pages, const int32_t* lens, const int32_t* visible, int32_t max_len,
+                                    int32_t n_sel, int32_t first, int32_t recent, int32_t* sel, void* workspace,
+                                    size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * rolesub_attend_selected: rolesub_attend_paged where head group h of query j sees the
+ * tokens t < min(lens[b], visible[b,j]) of the pages sel[b,j,h,:].
+ *   sel [B,Tq,H,n_sel] int32: pages by their number in the sequence, in any order; a
+ *   number outside [0, max_pages) stands for no page, and a page listed twice counts
+ *   twice. n_sel >= 1; n_sel*page and max_pages*page at most 2^30.
+ *   The other arguments, the workspace (its own size) and errors as
+ *   rolesub_attend_paged; no weights are added up.
+ * ------------------------------------------------------------------------ */
+size_t rolesub_attend_selected_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq, int32_t n_sel);
+rolesub_status rolesub_attend_selected(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                       const void* q, int64_t q_stride, const int32_t* table, int32_t max_pages,
+                                       const int32_t* lens, const int32_t* visible, const int32_t* sel, int32_t n_sel,
+                                       const void* R, float scale, void* out, rolesub_dtype out_dtype, void* workspace,
+                                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -152,3 +152,180 @@ def compact(src, table, keep_idx, n_keep, dst, dst_table):
             if at is not None:
                 place(dst, at, slot, x[0], x[1], x[2], G)
             slot += len(kept(x[2], G))
+
+
+# ---- normed heads, drafted tokens, few pages ------------------------------
+
+def norm(x, weight, eps):
+    """x [..,dh] over its root mean square, weighted."""
+    x = np.asarray(x, dtype=np.longdouble)
+    y = x / np.sqrt((x * x).mean(-1, keepdims=True) + np.longdouble(eps)) * np.asarray(weight, dtype=np.longdouble)
+    return y.astype(np.float64)
+
+
+def norm_rotary(x, weight, eps, positions, inv_freq, axis=None, interleaved=False):
+    return rotary(x if weight is None else norm(x, weight, eps), positions, inv_freq, axis, interleaved)
+
+
+def tree_masks(parents):
+    """Ancestors of each drafted token, itself among them, as sets; and how many others."""
+    sets = []
+    for row in np.asarray(parents).tolist():
+        mine = []
+        for j, p in enumerate(row):
+            mine.append((mine[p] if 0 <= p < j else set()) | {j})
+        sets.append(mine)
+    return sets, [[len(s) - 1 for s in row] for row in sets]
+
+
+def tree_words(sets, T):
+    """The same as words [.., T, ceil(T / 32)]."""
+    w = np.zeros((len(sets), T, -(-T // 32)), dtype=np.uint32)
+    for b, row in enumerate(sets):
+        for j, s in enumerate(row):
+            for i in s:
+                w[b, j, i // 32] |= np.uint32(1 << (i % 32))
+    return w
+
+
+def attend_over(q, cache, sees, R=None, scale=0.0):
+    """q [B,Tq,Hq,dh] over the cells (page, row) that sees(b, j, key head) lists. As `attend`: out, and what its error is
+    measured by."""
+    B, Tq, Hq, dh = q.shape
+    H, vcap, ds = cache["K"].shape[1], cache["V"].shape[2], cache["V"].shape[3]
+    rep, G = Hq // H, dh // ds
+    scale = scale or dh ** -0.5
+    out, size, logit = np.zeros(q.shape), np.zeros(q.shape), 0.0
+    for b in range(B):
+        for j in range(Tq):
+            for g in range(H):
+                cells = sees(b, j, g)
+                if not cells:
+                    continue
+                K = np.stack([np.asarray(cache["K"][p, g, r], dtype=np.float64) for p, r in cells])
+                Z = np.zeros((len(cells), G, ds))
+                for t, (p, r) in enumerate(cells):
+                    for i, x in enumerate(kept(cache["mask"][p, r], G)):
+                        s = int(cache["slot"][p, r]) + i
+                        if 0 <= s < vcap:
+                            Z[t, x] = cache["V"][p, g, s]
+                Z = Z.reshape(len(cells), dh)
+                for h in range(g * rep, (g + 1) * rep):
+                    qv = np.asarray(q[b, j, h], dtype=np.float64)
+                    s = K @ qv * scale
+                    logit = max(logit, float(np.max(np.abs(K) @ np.abs(qv))) * abs(scale))
+                    e = np.exp(s - s.max())
+                    p = e / e.sum()
+                    u, a = p @ Z, p @ np.abs(Z)
+                    if R is not None:
+                        Rh = np.asarray(R[g], dtype=np.float64)
+                        u, a = Rh @ u, np.abs(Rh) @ a
+                    out[b, j, h], size[b, j, h] = u, a
+    return out, size, logit
+
+
+def tree_sees(cache, table, lens, sets, Tq, n_new=None, max_len=0):
+    """What rows of drafted tokens see, for attend_over."""
+    cap = table.shape[1] * cache["K"].shape[2]
+    cap = min(cap, max_len) if max_len else cap
+
+    def sees(b, j, g):
+        n = Tq if n_new is None else min(max(int(n_new[b]), 0), Tq)
+        if j >= n:
+            return []
+        base = max(int(lens[b]), 0)
+        mine = sets[b if len(sets) > 1 else 0][j]
+        ts = list(range(min(base, cap))) + [base + i for i in sorted(mine) if i < n and base + i < cap]
+        return [x for x in (cell(cache, table[b], t) for t in ts) if x is not None]
+    return sees
+
+
+def accept(cache, table, lens, sets, leaf):
+    """Moves the paths in place and returns the new lengths."""
+    P = cache["K"].shape[2]
+    G = cache["K"].shape[3] // cache["V"].shape[3]
+    old = {x: cache[x].copy() for x in cache}
+    new = []
+    for b in range(table.shape[0]):
+        base = min(max(int(lens[b]), 0), table.shape[1] * P)
+        rows = sets[b if len(sets) > 1 else 0]
+        path = sorted(rows[int(leaf[b])]) if 0 <= int(leaf[b]) < len(rows) else []
+        new.append(base + len(path))
+        slot = 0
+        first = cell(old, table[b], base - 1) if base % P else None
+        if first is not None:
+            slot = int(old["slot"][first]) + len(kept(old["mask"][first], G))
+        for j, i in enumerate(path):
+            t = base + j
+            if t % P == 0:
+                slot = 0
+            src, dst = cell(old, table[b], base + i), cell(cache, table[b], t)
+            x = token(old, table[b], base + i)
+            if x is None:
+                x = (np.zeros(old["K"].shape[1::2]), np.zeros((old["K"].shape[1], G, old["V"].shape[3])), 0)
+            mask = 0 if src is None else old["mask"][src]
+            if dst is not None:
+                place(cache, dst, slot, x[0], x[1], mask, G)
+            slot += len(kept(mask, G))
+    return np.array(new)
+
+
+def page_bounds(cache, table, lens, bounds, T):
+    """Writes into bounds [n,H,2,dh] in place."""
+    P = cache["K"].shape[2]
+    for b in range(table.shape[0]):
+        n = min(max(int(lens[b]), 0), table.shape[1] * P)
+        for i in range(max(n - T, 0) // P, -(-n // P)):
+            pg = int(table[b, i])
+            if T > 0 and 0 <= pg < cache["K"].shape[0]:
+                k = cache["K"][pg, :, :min(P, n - i * P)]
+                bounds[pg, :, 0] = np.fmin.reduce(np.where(np.isnan(k), np.inf, k), axis=1)
+                bounds[pg, :, 1] = np.fmax.reduce(np.where(np.isnan(k), -np.inf, k), axis=1)
+
+
+def select_pages(q, cache, bounds, table, lens, n_sel, first=0, recent=0, visible=None, max_len=0):
+    B, Tq, Hq, dh = q.shape
+    n_pages, H, P = cache["K"].shape[:3]
+    rep, cap = Hq // H, table.shape[1] * P
+    cap = min(cap, max_len) if max_len else cap
+    sel = np.full((B, Tq, H, n_sel), -1, dtype=np.int32)
+    for b in range(B):
+        for j in range(Tq):
+            n = min(max(int(lens[b]), 0), cap)
+            n = n if visible is None else min(n, max(int(visible[b, j]), 0))
+            m = -(-n // P)
+            for g in range(H):
+                score = np.full(m, np.nan, dtype=np.float32)
+                for i in range(m):
+                    pg = int(table[b, i])
+                    if not 0 <= pg < n_pages:
+                        continue
+                    lo, hi = bounds[pg, g]
+                    best = []
+                    for h in range(g * rep, (g + 1) * rep):
+                        x = np.asarray(q[b, j, h], dtype=np.float64)
+                        with np.errstate(invalid="ignore"):
+                            best.append(np.float32(np.where(x < 0, x * lo, x * hi).sum()))
+                    score[i] = np.nan if np.isnan(best).any() else max(best)
+                if m <= n_sel:
+                    mine = list(range(m))
+                else:
+                    safe = [i for i in range(m) if i < first or i >= m - recent]
+                    free = np.array([i for i in range(m) if first <= i < m - recent], dtype=int)
+                    s = score[free]
+                    order = np.lexsort((free, np.where(np.isnan(s), 0.0, -s), np.isnan(s)))
+                    mine = sorted(safe + free[order][: n_sel - len(safe)].tolist())
+                sel[b, j, g, : len(mine)] = mine
+    return sel
+
+
+def selected_sees(cache, table, lens, sel, visible=None):
+    """What rows see of listed pages, for attend_over."""
+    P = cache["K"].shape[2]
+
+    def sees(b, j, g):
+        n = min(max(int(lens[b]), 0), table.shape[1] * P)
+        n = n if visible is None else min(n, int(visible[b, j]))
+        ts = [i * P + r for i in sel[b, j, g].tolist() if 0 <= i < table.shape[1] for r in range(P) if i * P + r < n]
+        return [x for x in (cell(cache, table[b], t) for t in ts) if x is not None]
+    return sees

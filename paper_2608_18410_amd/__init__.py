@@ -11,4 +11,6 @@ from .rolesub import (  # noqa: F401
     route_allocate, route_allocate_workspace_size, full_workspace_size, full_transpose, full_rotate_pack,
     full_values, attend_values, route_noalloc, ROUTE_NOALLOC_MAX_BYTES, PagedCache, PagesDesc, rotary,
     cache_append, attend_paged, attend_paged_workspace_size, evict_tokens, evict_workspace_size, cache_compact,
+    norm_rotary, append_rotary, tree_masks, attend_tree, attend_tree_workspace_size, cache_accept, page_bounds,
+    select_pages, select_pages_workspace_size, attend_selected, attend_selected_workspace_size,
 )

@@ -29,6 +29,22 @@ __device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// Waits until a matrix product's result may be read by other instructions. In straight
+// code the compiler keeps the states between them (8 for the bf16 product, 10 for the
+// float32 one). Without this, the assembly of k_join in bf16 has products into
+// accumulation registers, a branch (around the way without a rotation), and on its taken
+// side v_accvgpr_read of them three instructions later; the first elements came out
+// stale. Placed after products that end a block; tests/test_mfma_waits.py looks at the
+// assembly for any other.
+template <int N>
+__device__ __forceinline__ void settle(f32x4 (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+  asm volatile("s_nop 15" : "+v"(x[0]));
+#pragma unroll
+  for (int i = 1; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   bf16 a = static_cast<bf16>(lo), b = static_cast<bf16>(hi);
   return static_cast<uint32_t>(__builtin_bit_cast(uint16_t, a)) |

@@ -1,0 +1,390 @@
+// Queries and keys divided by their heads' root mean square, weighted, and turned by
+// their positions:
+//   n = x w / sqrt(mean x^2 + eps),  y_i = n_i cos a_i - n_j sin a_i,  y_j = n_i sin a_i + n_j cos a_i,
+// and the same on the way into the paged cache, with the values taken into the routing
+// space, z = R^T v, and their kept groups packed.
+#include <algorithm>
+
+#include "common.hpp"
+#include "launch.hpp"
+#include "rotary.hpp"
+
+namespace rolesub {
+namespace {
+
+// Where a call's new token (b, j) goes in the cache.
+struct Spot {
+  int page, row;  // -1: nowhere
+};
+__device__ __forceinline__ Spot spot_of(const TurnParams& p, int64_t tok) {
+  const PagedCache& c = p.c;
+  const int b = static_cast<int>(tok / p.T), j = static_cast<int>(tok % p.T);
+  const int64_t cap = static_cast<int64_t>(p.max_pages) << c.shift;
+  const int64_t t = min(static_cast<int64_t>(max(p.lens[b], 0)), cap) + j;
+  if (t >= cap || (p.n_new && j >= p.n_new[b])) return Spot{-1, 0};
+  const int page = p.table[static_cast<int64_t>(b) * p.max_pages + (t >> c.shift)];
+  return Spot{static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages) ? page : -1, static_cast<int>(t & (c.page - 1))};
+}
+
+// Heads [h0, h1) of one token's rows (queries first, then keys), a wave's work. A lane
+// holds a 16-byte piece of a row, and for all rows the factors of its elements: an
+// element becomes m1 f1 + m2 f2 of itself and the other of its pair, times its row's
+// 1 / root. Without a norm this is in every bit what the rotation's own kernels give,
+// which is why m1 is the pair's first element where they multiply that first. In halves the other
+// elements lie n behind or before: the rows' pieces go through LDS (a wave's rows of a
+// step, with a piece's room before and behind). WHOLE: pieces lie in one half.
+template <class T, bool IL, bool WHOLE, bool CACHE>
+__device__ __forceinline__ void turn_rows(const TurnParams& p, int64_t tok, int h0, int h1, char* stage, float (*cs)[kMaxPairs]) {
+  constexpr int V = 16 / sizeof(T), U = 4;
+  const int lane = threadIdx.x & 63;
+  const int n = p.n_pairs, lpr = p.dh / V, hs = 64 / lpr, hl = lane / lpr, e0 = lane % lpr * V;
+  Spot spot = {-1, 0};
+  if constexpr (CACHE) spot = spot_of(p, tok);
+  bool first = true;
+  float c[V], s[V];  // of the elements' pairs, s with the sign of the other element's share
+  uint32_t turn = 0;
+#pragma unroll 1
+  for (int seg = 0; seg < 2; ++seg) {
+    const int s0 = seg ? max(h0, p.H) - p.H : h0, s1 = seg ? h1 - p.H : min(h1, p.H);
+    if (s0 >= s1 || (CACHE && seg && spot.page < 0)) continue;
+    const T* in = static_cast<const T*>(seg ? p.k : p.q) + tok * (seg ? p.k_stride : p.q_stride) + e0;
+    T* out;
+    int64_t ld = p.dh;
+    if (CACHE && seg) {
+      out = static_cast<T*>(p.c.K) + (((static_cast<int64_t>(spot.page) * p.c.H) << p.c.shift) + spot.row) * p.dh + e0;
+      ld <<= p.c.shift;
+    } else {
+      out = static_cast<T*>(seg ? p.k_out : p.q_out) + tok * (seg ? p.ko_stride : p.qo_stride) + e0;
+    }
+    const T* weight = static_cast<const T*>(seg ? p.wk : p.wq);
+    float f1[V], f2[V], wt[V];
+    const bool high = !IL && e0 >= n && e0 < 2 * n;  // WHOLE: the lane's piece
+    bool fresh = true;
+    for (int hb = s0; hb < s1; hb += hs * U) {
+      u32x4 a[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = min(hb + i * hs + hl, s1 - 1);
+        a[i] = *reinterpret_cast<const u32x4*>(in + static_cast<int64_t>(h) * p.dh);
+      }
+      if (first) {  // while the first rows are on their way: a pair a lane, then through LDS
+        first = false;
+        if (lane < n) {
+          const int ax = p.axis ? p.axis[lane] : 0;
+          float cc = kStays, ss = 0.f;
+          if (ax < p.n_axes) angle(p.positions[tok * p.n_axes + ax], p.inv_freq[lane], cc, ss);
+          cs[0][lane] = cc;
+          cs[1][lane] = ss;
+        }
+        wave_lds_order();
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          const int e = e0 + x, i = IL ? e / 2 : e < n ? e : e - n;
+          const bool in2 = e < 2 * n, on = in2 && cs[0][in2 ? i : 0] != kStays, low = IL ? e % 2 == 0 : e < n;
+          c[x] = on ? cs[0][i] : 1.f;
+          s[x] = on ? (low ? -cs[1][i] : cs[1][i]) : -0.f;
+          turn |= on ? 1u << x : 0u;
+        }
+      }
+      if (fresh) {
+        fresh = false;
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          const int e = e0 + x, o = IL ? e ^ 1 : e < n ? e + n : e < 2 * n ? e - n : e;
+          wt[x] = weight ? tof(weight[e]) : 1.f;
+          f1[x] = c[x] * wt[x];
+          f2[x] = s[x] * (weight ? tof(weight[o]) : 1.f);
+          // the pair's first element first
+          if ((IL && WHOLE && x % 2) || (WHOLE && high)) {
+            const float y = f1[x];
+            f1[x] = f2[x];
+            f2[x] = y;
+          }
+        }
+      }
+      if constexpr (!IL) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) *reinterpret_cast<u32x4*>(stage + 16 + (i * 64 + lane) * 16) = a[i];
+        wave_lds_order();
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = hb + i * hs + hl;
+        u32x4 b = a[i];
+        if constexpr (!IL) {
+          const char* me = stage + 16 + (i * 64 + lane) * 16;
+          const int off = n * static_cast<int>(sizeof(T));
+          if constexpr (WHOLE) {
+            b = u32x4{0, 0, 0, 0};
+            if (e0 < 2 * n) b = *reinterpret_cast<const u32x4*>(high ? me - off : me + off);
+          } else {
+            u32x4 d = b;
+            if (e0 < n) __builtin_memcpy(&b, me + off, 16);
+            if (e0 + V > n && e0 < 2 * n) __builtin_memcpy(&d, me - off, 16);
+            const T* vb = reinterpret_cast<const T*>(&b);
+            T* vd = reinterpret_cast<T*>(&d);
+#pragma unroll
+            for (int x = 0; x < V; ++x) vd[x] = e0 + x < n ? vb[x] : vd[x];
+            b = d;
+          }
+        }
+        const T* xa = reinterpret_cast<const T*>(&a[i]);
+        const T* xb = reinterpret_cast<const T*>(&b);
+        float inv = 1.f;
+        if (weight) {
+          float sq = 0.f;
+#pragma unroll
+          for (int x = 0; x < V; ++x) sq += tof(xa[x]) * tof(xa[x]);
+          for (int o = 1; o < lpr; o <<= 1) sq += __shfl_xor(sq, o, kWave);
+          inv = __builtin_amdgcn_rsqf(sq / static_cast<float>(p.dh) + p.eps);
+          if (__any(!(sq < __builtin_inff()))) {  // squares past the range, or what is not finite: 2^-64 of the elements
+            float small = 0.f;
+#pragma unroll
+            for (int x = 0; x < V; ++x) {
+              const float y = tof(xa[x]) * 0x1p-64f;
+              small += y * y;
+            }
+            for (int o = 1; o < lpr; o <<= 1) small += __shfl_xor(small, o, kWave);
+            if (!(sq < __builtin_inff())) inv = __builtin_amdgcn_rsqf(small / static_cast<float>(p.dh)) * 0x1p-64f;
+          }
+        }
+        u32x4 y;
+        T* vy = reinterpret_cast<T*>(&y);
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          const float me = tof(xa[x]), other = tof(IL ? xa[x ^ 1] : xb[x]);
+          const bool swap = WHOLE && (IL ? x % 2 == 1 : high);
+          float r = __builtin_fmaf(swap ? other : me, f1[x], (swap ? me : other) * f2[x]);
+          if (!((turn >> x) & 1u)) r = me * wt[x];
+          vy[x] = fromf<T>(weight ? r * inv : r);
+          if (!weight && !((turn >> x) & 1u)) vy[x] = xa[x];
+        }
+        if (h < s1) *reinterpret_cast<u32x4*>(out + h * ld) = y;
+      }
+      wave_lds_order();
+    }
+  }
+}
+
+constexpr int kStage = 4 * 64 * 16 + 32;  // bytes of a wave's rows in LDS
+
+// A wave turns heads [hw * chunk, ...) of one token.
+template <class T, bool IL, bool WHOLE>
+__global__ __launch_bounds__(256) void k_norm_rotary(TurnParams p, int chunks, int chunk) {
+  __shared__ __attribute__((aligned(16))) char stage[4][kStage];
+  __shared__ float cs[4][2][kMaxPairs];
+  const int w = threadIdx.x >> 6;
+  const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + w, tok = job / chunks;
+  if (tok >= static_cast<int64_t>(p.B) * p.T) return;
+  const int h0 = static_cast<int>(job % chunks) * chunk;
+  turn_rows<T, IL, WHOLE, false>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), stage[w], cs[w]);
+}
+
+// Slots of the kRun tokens from n0 on (tokens of all sequences one after another): behind
+// their page-mates, by an exclusive sum over the run and the 255 tokens before it.
+constexpr int kRun = 64;
+struct RunMeta {
+  int64_t page[kRun];  // -1: dropped
+  uint32_t mask[kRun];
+  int slot[kRun];
+};
+__device__ __forceinline__ void run_meta(const TurnParams& p, int64_t n0, int h, RunMeta& m, int* s_sum, int* wsum) {
+  const PagedCache& c = p.c;
+  const int tid = threadIdx.x;
+  const int64_t all = static_cast<int64_t>(p.B) * p.T, w0 = n0 - 256;  // the window: 256 + 64 tokens, two a thread
+  const uint32_t gm = group_bits(c.G);
+  int cnt[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int64_t t = w0 + 2 * tid + x;
+    cnt[x] = 2 * tid + x < 256 + kRun && t >= 0 && t < all ? __popc(p.mask[t] & gm) : 0;
+  }
+  const int before = group_scan<256, false>(cnt[0] + cnt[1], wsum);
+  if (tid < (256 + kRun) / 2) {
+    s_sum[2 * tid] = before;
+    s_sum[2 * tid + 1] = before + cnt[0];
+  }
+  __syncthreads();
+  if (tid < kRun) {
+    const int64_t tok = n0 + tid;
+    Spot s = {-1, 0};
+    if (tok < all) s = spot_of(p, tok);
+    m.page[tid] = s.page;
+    if (s.page >= 0) {
+      const int j = static_cast<int>(tok % p.T), mates = min(s.row, j);  // new ones before it in its page
+      int used = s_sum[256 + tid] - s_sum[256 + tid - mates];
+      const int64_t meta = static_cast<int64_t>(s.page) << c.shift;
+      if (s.row > j) used += c.slot[meta + s.row - j - 1] + __popc(c.mask[meta + s.row - j - 1] & gm);
+      const uint32_t whole = p.mask[tok];
+      m.mask[tid] = whole & gm;
+      m.slot[tid] = used;
+      if (h == 0) {
+        c.mask[meta + s.row] = whole;
+        c.slot[meta + s.row] = used;
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// Four dims of a rotated value from dim d on into the groups that keep them.
+template <class T>
+__device__ __forceinline__ void put_dims(const PagedCache& c, int64_t page, int h, uint32_t mask, int slot, int d, f32x4 z) {
+  T v[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) v[x] = fromf<T>(z[x]);
+  T* base = static_cast<T*>(c.V) + (page * c.H + h) * c.vcap * static_cast<int64_t>(c.ds);
+  auto at = [&](int g) {  // of group g, or null
+    const uint32_t sl = static_cast<uint32_t>(slot) + __popc(mask & ((1u << g) - 1u));
+    return ((mask >> g) & 1u) && sl < static_cast<uint32_t>(c.vcap) ? base + static_cast<int64_t>(sl) * c.ds : nullptr;
+  };
+  if (c.ds >= 4) {
+    T* to = at(d / c.ds);
+    if (to) __builtin_memcpy(__builtin_assume_aligned(to + d % c.ds, 4 * sizeof(T)), v, 4 * sizeof(T));
+  } else {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      T* to = at(d / 2 + u);
+      if (to) __builtin_memcpy(__builtin_assume_aligned(to, 2 * sizeof(T)), v + 2 * u, 2 * sizeof(T));
+    }
+  }
+}
+
+// z = R_h^T v of a run's tokens for one head, on the matrix cores: dims of z are the
+// product's rows, tokens its columns, 16 a wave. R_h lies in LDS.
+template <class T, int DH>
+struct Values {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int EP = 16 / sizeof(T), ROWB = DH * sizeof(T), KS = ROWB / 64, MB = DH / 16;
+  static constexpr int LD = ROWB + (kBf16 ? 32 : 16), BYTES = DH * LD;
+};
+template <class T, int DH>
+__device__ __forceinline__ void rotate_run(const TurnParams& p, int64_t n0, int h, const RunMeta& m, const char* R) {
+  using L = Values<T, DH>;
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef s16x4 __attribute__((address_space(3))) * p3;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4, i = 16 * w + l16;
+  const int64_t all = static_cast<int64_t>(p.B) * p.T, tok = min(n0 + i, all - 1);
+  const T* v = static_cast<const T*>(p.v) + tok * p.v_stride + static_cast<int64_t>(h) * DH + g4 * L::EP;
+  u32x4 vf[L::KS];
+#pragma unroll
+  for (int j = 0; j < L::KS; ++j) vf[j] = *reinterpret_cast<const u32x4*>(v + 4 * j * L::EP);
+  f32x4 z[L::MB];
+#pragma unroll
+  for (int mb = 0; mb < L::MB; ++mb) z[mb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < L::KS; ++j)
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb) {
+      if constexpr (L::kBf16) {
+        const char* r = R + (32 * j + 8 * g4 + l16 / 4) * L::LD + 8 * (l16 % 4) + 32 * mb;
+        const bf16x4 a0 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)(r)));
+        const bf16x4 a1 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)(r + 4 * L::LD)));
+        z[mb] = mfma_16x16x32(__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(bf16x8, vf[j]), z[mb]);
+      } else {
+        const f32x4 x = __builtin_bit_cast(f32x4, vf[j]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float a = *reinterpret_cast<const float*>(R + (16 * j + 4 * g4 + k) * L::LD + 4 * (16 * mb + l16));
+          z[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, x[k], z[mb], 0, 0, 0);
+        }
+      }
+    }
+  settle(z);
+  if (m.page[i] < 0) return;
+#pragma unroll
+  for (int mb = 0; mb < L::MB; ++mb) put_dims<T>(p.c, m.page[i], h, m.mask[i], m.slot[i], 16 * mb + 4 * g4, z[mb]);
+}
+
+// An append. The first `vals` workgroups bring the values of one head and run of tokens,
+// the others turn the rows of queries and keys.
+template <class T, int DH, bool IL, bool WHOLE>
+__global__ __launch_bounds__(256) void k_append_rotary(TurnParams p, int vals, int chunks, int chunk) {
+  using L = Values<T, DH>;
+  constexpr int ROWS = 4 * kStage + 4 * 2 * kMaxPairs * 4;
+  constexpr int META = sizeof(RunMeta) + (256 + kRun + 4) * 4;
+  __shared__ __attribute__((aligned(16))) char smem[ROWS > L::BYTES + META ? ROWS : L::BYTES + META];
+  const int tid = threadIdx.x, w = tid >> 6;
+  if (static_cast<int>(blockIdx.x) < vals) {
+    const int h = blockIdx.x % p.c.H;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x / p.c.H) * kRun;
+    RunMeta& m = *reinterpret_cast<RunMeta*>(smem + L::BYTES);
+    int* s_sum = reinterpret_cast<int*>(smem + L::BYTES + sizeof(RunMeta));
+    int* wsum = s_sum + 256 + kRun;
+    if (p.Rm) {
+      constexpr int PP = L::ROWB / 16, N = DH * PP / 256;
+      const char* R = static_cast<const char*>(p.Rm) + static_cast<int64_t>(h) * DH * L::ROWB;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int u = tid + 256 * i;
+        *reinterpret_cast<u32x4*>(smem + u / PP * L::LD + u % PP * 16) = *reinterpret_cast<const u32x4*>(R + u * 16);
+      }
+      run_meta(p, n0, h, m, s_sum, wsum);
+      rotate_run<T, DH>(p, n0, h, m, smem);
+    } else {
+      run_meta(p, n0, h, m, s_sum, wsum);
+      for (int u = tid; u < kRun * (DH / 4); u += 256) {
+        const int i = u / (DH / 4), d = u % (DH / 4) * 4;
+        if (m.page[i] < 0) continue;
+        const T* v = static_cast<const T*>(p.v) + (n0 + i) * p.v_stride + static_cast<int64_t>(h) * DH + d;
+        put_dims<T>(p.c, m.page[i], h, m.mask[i], m.slot[i], d, f32x4{tof(v[0]), tof(v[1]), tof(v[2]), tof(v[3])});
+      }
+    }
+    return;
+  }
+  const int64_t job = static_cast<int64_t>(blockIdx.x - vals) * 4 + w, tok = job / chunks;
+  if (tok >= static_cast<int64_t>(p.B) * p.T) return;
+  const int h0 = static_cast<int>(job % chunks) * chunk;
+  turn_rows<T, IL, WHOLE, true>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), smem + w * kStage,
+                                reinterpret_cast<float(*)[kMaxPairs]>(smem + 4 * kStage) + 2 * w);
+}
+
+// Heads of a wave, as the rotation's kernels choose.
+int heads_of(size_t tok, int heads) { return tok >= 4096 ? heads : tok >= 1024 ? (heads + 1) / 2 : 8; }
+
+template <class T>
+bool whole(const TurnParams& p) {
+  return (p.interleaved ? 2 * p.n_pairs : p.n_pairs) % (16 / static_cast<int>(sizeof(T))) == 0;
+}
+
+template <class T>
+void launch(const TurnParams& p, hipStream_t s) {
+  const int heads = p.H + p.Hkv;
+  const size_t tok = static_cast<size_t>(p.B) * p.T;
+  const int chunk = heads_of(tok, heads), chunks = (heads + chunk - 1) / chunk;
+  auto kern = p.interleaved ? (whole<T>(p) ? k_norm_rotary<T, true, true> : k_norm_rotary<T, true, false>)
+                            : (whole<T>(p) ? k_norm_rotary<T, false, true> : k_norm_rotary<T, false, false>);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((tok * chunks + 3) / 4)), dim3(256), 0, s, p, chunks, chunk);
+}
+
+template <class T, int DH>
+void launch_in(const TurnParams& p, hipStream_t s) {
+  const int heads = p.H + p.Hkv;
+  const size_t tok = static_cast<size_t>(p.B) * p.T;
+  const int chunk = heads_of(tok, heads), chunks = (heads + chunk - 1) / chunk;
+  const size_t vals = (tok + kRun - 1) / kRun * p.c.H;
+  auto kern = p.interleaved ? (whole<T>(p) ? k_append_rotary<T, DH, true, true> : k_append_rotary<T, DH, true, false>)
+                            : (whole<T>(p) ? k_append_rotary<T, DH, false, true> : k_append_rotary<T, DH, false, false>);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(vals + (tok * chunks + 3) / 4)), dim3(256), 0, s, p, static_cast<int>(vals),
+                     chunks, chunk);
+}
+
+}  // namespace
+
+hipError_t launch_norm_rotary(const TurnParams& p, bool bf16, hipStream_t s) {
+  if (bf16)
+    launch<__bf16>(p, s);
+  else
+    launch<float>(p, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_append_rotary(const TurnParams& p, bool bf16, hipStream_t s) {
+  if (bf16)
+    p.dh == 128 ? launch_in<__bf16, 128>(p, s) : launch_in<__bf16, 64>(p, s);
+  else
+    p.dh == 128 ? launch_in<float, 128>(p, s) : launch_in<float, 64>(p, s);
+  return hipGetLastError();
+}
+
+}  // namespace rolesub

@@ -250,6 +250,8 @@ struct GatherParams {
 };
 hipError_t launch_gather_rows(const GatherParams& p, hipStream_t s);
 
+constexpr int kMaxTree = 256;  // drafted tokens of a sequence
+
 // Paged routed cache (rolesub_pages).
 struct PagedCache {
   int n_pages, page, shift, vcap, H, dh, G, ds;  // page = 1 << shift
@@ -310,6 +312,13 @@ struct DecodeParams {
   float* stat;         // [B][H][R][n_split][2]  maximum (log2), sum of P (with splits or mass)
   float* x;            // [B][H][R][x_ld] scores in units of log2 (with mass)
   int x_ld;
+  // drafted tokens: the last n_new[b] (null: Tq) of max_len, behind lens[b]
+  const uint32_t* tree;  // [trees][Tq][ceil(Tq / 32)], trees 1 or B
+  const int32_t* n_new;
+  int trees;
+  // listed pages: B counts queries, per of them a sequence, each with Tq = 1; max_len = n_sel pages
+  const int32_t* sel;  // [B][H][n_sel]
+  int n_sel, per;
 };
 struct DecodePlan {
   int n_split, chunk, x_ld;
@@ -318,6 +327,66 @@ struct DecodePlan {
 };
 DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass);
 hipError_t launch_decode(const DecodeParams& p, bool bf16, hipStream_t s);
+hipError_t launch_decode_tree(const DecodeParams& p, bool bf16, hipStream_t s);
+hipError_t launch_decode_listed(const DecodeParams& p, bool bf16, hipStream_t s);
+
+struct TreeParams {
+  int B, T;
+  const int32_t* parents;  // [B][T]
+  uint32_t* tree;          // [B][T][ceil(T / 32)]
+  int32_t* depth;          // [B][T] or null
+};
+hipError_t launch_tree_masks(const TreeParams& p, hipStream_t s);
+
+struct AcceptParams {
+  PagedCache c;
+  int B, T, trees, max_pages;
+  const int32_t *table, *lens, *leaf;
+  const uint32_t* tree;  // [trees][T][ceil(T / 32)], trees 1 or B
+  int32_t* new_lens;     // [B] or null
+};
+hipError_t launch_accept(const AcceptParams& p, bool bf16, hipStream_t s);
+
+struct BoundsParams {
+  PagedCache c;
+  int B, T, max_pages;  // the pages of the last T tokens
+  const int32_t *table, *lens;
+  void* bounds;  // [n_pages][H][2][dh]
+};
+hipError_t launch_page_bounds(const BoundsParams& p, bool bf16, hipStream_t s);
+
+struct SelectParams {
+  PagedCache c;
+  int B, Tq, rep, max_pages, max_len;
+  const void *q, *bounds;
+  int64_t q_stride;
+  const int32_t *table, *lens, *visible;
+  int ld;         // pages of max_len
+  float* scores;  // [B][Tq][H][ld]
+  int32_t* counts;  // [B][Tq][H] pages that a query sees
+};
+hipError_t launch_page_scores(const SelectParams& p, bool bf16, hipStream_t s);
+
+struct TurnParams {
+  int B, T, H, Hkv, dh, n_axes, n_pairs, interleaved;  // a head count of 0: that tensor is absent
+  const void *q, *k;
+  int64_t q_stride, k_stride, qo_stride, ko_stride;  // elements from token to token
+  const void *wq, *wk;  // [dh] weights of the norm, or null: not normed
+  float eps;
+  const int32_t* positions;  // [B*T][n_axes]
+  const float* inv_freq;     // [n_pairs]
+  const uint8_t* axis;       // [n_pairs] or null
+  void *q_out, *k_out;       // k_out null: into the cache
+  // an append
+  PagedCache c;
+  int max_pages;
+  const void *v, *Rm;  // Rm [Hkv][dh][dh] or null
+  int64_t v_stride;
+  const uint32_t* mask;
+  const int32_t *table, *lens, *n_new;
+};
+hipError_t launch_norm_rotary(const TurnParams& p, bool bf16, hipStream_t s);
+hipError_t launch_append_rotary(const TurnParams& p, bool bf16, hipStream_t s);
 
 struct EvictParams {
   int B, max_len, keep, first, recent;

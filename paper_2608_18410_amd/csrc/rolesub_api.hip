@@ -944,6 +944,83 @@ rolesub_status cache_apart(const char* fn, const PagedCache& c, size_t e, std::i
   return ROLESUB_OK;
 }
 
+// The sizes that calls which turn heads share.
+rolesub_status check_turn(const char* fn, int32_t B, int32_t T, int32_t dh, rolesub_dtype dtype, float eps, int32_t n_axes,
+                          int32_t n_pairs) {
+  if (!valid_dtype(dtype)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+  if (B < 0 || T < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: B and T must be >= 0", fn);
+  if (dh != 64 && dh != 128) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: head dim %d not supported (64 or 128)", fn, dh);
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: eps must be finite and > 0", fn);
+  if (n_pairs < 1 || n_pairs > dh / 2)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: n_pairs=%d outside 1..dh/2", fn, n_pairs);
+  if (n_axes < 1 || n_axes > 8) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: n_axes=%d outside 1..8", fn, n_axes);
+  return ROLESUB_OK;
+}
+
+// The same for attention of new tokens, before anything is looked at.
+rolesub_status check_attend(const char* fn, rolesub_dtype dtype, rolesub_dtype out_dtype, const PagedCache& c, int32_t B,
+                            int32_t Hq, int32_t Tq, int32_t max_pages, float scale) {
+  if (out_dtype != ROLESUB_F32 && out_dtype != dtype)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: out_dtype must be f32 or the input dtype", fn);
+  if (B < 0 || Tq < 0 || max_pages < 0)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: B, Tq and max_pages must be >= 0", fn);
+  if (Hq < 1 || Hq % c.H)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: %d query heads are not a multiple of %d key heads", fn, Hq, c.H);
+  if (!std::isfinite(scale)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: scale is not finite", fn);
+  return ROLESUB_OK;
+}
+
+// Queries, outputs and workspace of attention over p.B sequences of p.Tq queries and
+// p.max_len tokens (`seqs` sequences in the table); `more`: what else must not change.
+rolesub_status set_attend(const char* fn, DecodeParams& p, rolesub_dtype dtype, int32_t Hq, const void* q, int64_t q_stride,
+                          const int32_t* table, int32_t max_pages, const void* R, float scale, void* out,
+                          rolesub_dtype out_dtype, void* workspace, size_t ws_bytes, int32_t seqs,
+                          std::initializer_list<Operand> more) {
+  const PagedCache& c = p.c;
+  const size_t e = esize(dtype), nq = static_cast<size_t>(p.B) * p.Tq;
+  p.Hq = Hq;
+  p.rep = Hq / c.H;
+  if (static_cast<size_t>(p.rep) * p.Tq > 0x7FFFFFFF || nq * Hq * c.dh >= kMaxThreads)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many queries", fn);
+  p.R = p.rep * p.Tq;
+  p.q = q;
+  p.q_stride = q_stride;
+  rolesub_status st = check_rows(fn, "q", q, p.q_stride, Hq, c.dh, e);
+  if (st) return st;
+  if (!aligned(R, 16) || !aligned(out, 16))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: R and out must lie on 16 bytes", fn);
+  p.max_pages = max_pages;
+  p.table = table;
+  p.Rm = R;
+  p.scale = static_cast<float>((scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(c.dh)) : scale) * 1.44269504088896341);
+  p.out = out;
+  p.out_f32 = out_dtype == ROLESUB_F32;
+  const DecodePlan d = decode_plan(p.B, c.H, p.R, c.dh, p.max_len, false);
+  if (d.bytes > 0 && (!workspace || ws_bytes < d.bytes))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, %zu given", fn, d.bytes,
+                workspace ? ws_bytes : static_cast<size_t>(0));
+  if (!aligned(workspace, 16)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace must lie on 16 bytes", fn);
+  if (static_cast<size_t>(p.B) * c.H * d.n_split * ((p.R + 15) / 16) * 256 >= kMaxThreads)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads or queries", fn);
+  const size_t qrow = static_cast<size_t>(Hq) * c.dh, np = static_cast<size_t>(c.n_pages);
+  const size_t nout = nq * qrow * (p.out_f32 ? 4 : e), nqin = ((nq - 1) * p.q_stride + qrow) * e;
+  const Operand to = {"out", out, nout}, ws = {"workspace", workspace, d.bytes};
+  st = apart(fn, {to, ws}, {{"q", out == q && nout == nqin ? nullptr : q, nqin},
+                            {"R", R, static_cast<size_t>(c.H) * c.dh * c.dh * e},
+                            {"K", c.K, np * c.H * c.page * c.dh * e},
+                            {"V", c.V, np * c.H * c.vcap * c.ds * e},
+                            {"mask", c.mask, np * c.page * 4},
+                            {"slot", c.slot, np * c.page * 4},
+                            {"table", table, static_cast<size_t>(seqs) * max_pages * 4}});
+  if (st || (st = apart(fn, {to}, more)) || (st = apart(fn, {ws}, more))) return st;
+  p.n_split = d.n_split;
+  p.chunk = d.chunk;
+  p.x_ld = d.x_ld;
+  p.part = static_cast<float*>(workspace);
+  if (d.off_x > d.off_stat) p.stat = reinterpret_cast<float*>(static_cast<char*>(workspace) + d.off_stat);
+  return ROLESUB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1225,6 +1302,404 @@ rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pag
   if ((st = cache_apart(fn, p.dst, esize(dtype), {idx, kept, from, to, {"mass_in", mass_in, mi}, {"mass_out", mass_out, mo}})))
     return st;
   return from_hip(launch_compact(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+rolesub_status rolesub_norm_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int32_t dh, rolesub_dtype dtype,
+                                   const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                   const void* q_weight, const void* k_weight, float eps, const int32_t* positions,
+                                   int32_t n_axes, const float* inv_freq, const uint8_t* axis, int32_t n_pairs,
+                                   int32_t interleaved, void* q_out, void* k_out, void* stream) {
+  const char* fn = "rolesub_norm_rotary";
+  TurnParams p = {};
+  rolesub_status st = check_turn(fn, B, T, dh, dtype, eps, n_axes, n_pairs);
+  if (st) return st;
+  const size_t n = static_cast<size_t>(B) * T, e = esize(dtype);
+  if (n == 0) return ROLESUB_OK;
+  if (!q && !k) return fail(ROLESUB_ERR_INVALID_ARG, "%s: q and k are both NULL", fn);
+  if ((q && H < 1) || (k && Hkv < 1)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: head counts must be >= 1", fn);
+  if (!positions || !inv_freq || (q && !q_out) || (k && !k_out))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  p.H = q ? H : 0;
+  p.Hkv = k ? Hkv : 0;
+  if (n * 256 >= kMaxThreads || p.H + static_cast<int64_t>(p.Hkv) > 65535)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many tokens or heads", fn);
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  if (q && (st = check_rows(fn, "q", q, p.q_stride, H, dh, e))) return st;
+  if (k && (st = check_rows(fn, "k", k, p.k_stride, Hkv, dh, e))) return st;
+  if ((q && !aligned(q_out, 16)) || (k && !aligned(k_out, 16)))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: q_out and k_out must lie on 16 bytes", fn);
+  const int64_t qr = static_cast<int64_t>(H) * dh, kr = static_cast<int64_t>(Hkv) * dh;
+  p.qo_stride = q_out == q ? p.q_stride : qr;
+  p.ko_stride = k_out == k ? p.k_stride : kr;
+  struct Rows {
+    const void* p;
+    int64_t stride, row;
+  } const t[4] = {{q, p.q_stride, qr}, {k, p.k_stride, kr}, {q ? q_out : nullptr, p.qo_stride, qr},
+                  {k ? k_out : nullptr, p.ko_stride, kr}};
+  for (int o = 2; o < 4; ++o) {
+    for (int x = 0; x < 4; ++x) {
+      if (!t[o].p || !t[x].p || x == o || (x == o - 2 && t[x].p == t[o].p)) continue;  // an input itself
+      if (rows_overlap(t[o].p, t[o].stride, t[o].row, t[x].p, t[x].stride, t[x].row, n, e))
+        return fail(ROLESUB_ERR_INVALID_ARG, "%s: an output overlaps another tensor of the call", fn);
+    }
+    if (!t[o].p) continue;
+    st = apart(fn, {{o == 2 ? "q_out" : "k_out", t[o].p, ((n - 1) * t[o].stride + t[o].row) * e}},
+               {{"q_weight", q_weight, dh * e}, {"k_weight", k_weight, dh * e}, {"positions", positions, n * n_axes * 4},
+                {"inv_freq", inv_freq, static_cast<size_t>(n_pairs) * 4}, {"axis", axis, static_cast<size_t>(n_pairs)}});
+    if (st) return st;
+  }
+  p.B = B;
+  p.T = T;
+  p.dh = dh;
+  p.n_axes = n_axes;
+  p.n_pairs = n_pairs;
+  p.interleaved = interleaved != 0;
+  p.q = q;
+  p.k = k;
+  p.wq = q_weight;
+  p.wk = k_weight;
+  p.eps = eps;
+  p.positions = positions;
+  p.inv_freq = inv_freq;
+  p.axis = axis;
+  p.q_out = q_out;
+  p.k_out = k_out;
+  return from_hip(launch_norm_rotary(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+rolesub_status rolesub_append_rotary(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T, int32_t Hq,
+                                     const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                     int64_t v_stride, const void* R, const uint32_t* mask, const void* q_weight,
+                                     const void* k_weight, float eps, const int32_t* positions, int32_t n_axes,
+                                     const float* inv_freq, const uint8_t* axis, int32_t n_pairs, int32_t interleaved,
+                                     const int32_t* table, int32_t max_pages, const int32_t* lens, const int32_t* n_new,
+                                     void* q_out, void* stream) {
+  const char* fn = "rolesub_append_rotary";
+  TurnParams p = {};
+  const bool work = B > 0 && T > 0;
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, work && max_pages > 0, p.c);
+  if (st) return st;
+  if (max_pages < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: max_pages must be >= 0", fn);
+  if ((st = check_turn(fn, B, T, p.c.dh, dtype, eps, n_axes, n_pairs))) return st;
+  if (!work) return ROLESUB_OK;
+  const size_t n = static_cast<size_t>(B) * T, rows = static_cast<size_t>(B), e = esize(dtype);
+  const int dh = p.c.dh;
+  if (q && Hq < 1) return fail(ROLESUB_ERR_INVALID_ARG, "%s: head counts must be >= 1", fn);
+  if (!mask || (max_pages > 0 && !table) || !lens || !positions || !inv_freq || (q && !q_out))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  p.H = q ? Hq : 0;
+  p.Hkv = p.c.H;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  if (q && (st = check_rows(fn, "q", q, p.q_stride, Hq, dh, e))) return st;
+  if ((st = check_rows(fn, "k", k, p.k_stride, p.c.H, dh, e))) return st;
+  if ((st = check_rows(fn, "v", v, p.v_stride, p.c.H, dh, e))) return st;
+  if ((q && !aligned(q_out, 16)) || !aligned(R, 16))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: q_out and R must lie on 16 bytes", fn);
+  // workgroups: four waves of eight heads or more, and a run of 64 tokens a head
+  if (p.H + static_cast<int64_t>(p.Hkv) > 65535 ||
+      (n * ((p.H + static_cast<size_t>(p.Hkv) + 7) / 8) / 4 + (n / 64 + 1) * p.Hkv + 1) * 256 >= kMaxThreads)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many tokens or heads", fn);
+  const int64_t qr = static_cast<int64_t>(Hq) * dh, kr = static_cast<int64_t>(p.c.H) * dh;
+  p.qo_stride = q_out == q ? p.q_stride : qr;
+  const Operand in[] = {{"k", k, ((n - 1) * p.k_stride + kr) * e}, {"v", v, ((n - 1) * p.v_stride + kr) * e},
+                        {"R", R, static_cast<size_t>(kr) * dh * e}, {"q_weight", q_weight, dh * e},
+                        {"k_weight", k_weight, dh * e}, {"positions", positions, n * n_axes * 4},
+                        {"inv_freq", inv_freq, static_cast<size_t>(n_pairs) * 4}, {"axis", axis, static_cast<size_t>(n_pairs)},
+                        {"the new tokens' mask", mask, n * 4}, {"table", table, rows * max_pages * 4},
+                        {"lens", lens, rows * 4}, {"n_new", n_new, rows * 4}};
+  const Operand qo = {"q_out", q ? q_out : nullptr, q ? ((n - 1) * p.qo_stride + qr) * e : 0};
+  // workgroups read all of these at times of their own
+  for (const Operand& x : in) {
+    if ((st = cache_apart(fn, p.c, e, {x}))) return st;
+    const bool fused = q && x.p && (x.p == k || x.p == v);  // rows of one stride may interleave
+    if (fused) {
+      const int64_t stride = x.p == k ? p.k_stride : p.v_stride;
+      if (rows_overlap(q_out, p.qo_stride, qr, x.p, stride, kr, n, e))
+        return fail(ROLESUB_ERR_INVALID_ARG, "%s: q_out overlaps %s", fn, x.name);
+    } else if ((st = apart(fn, {qo}, {x}))) {
+      return st;
+    }
+  }
+  if (q) {
+    const Operand qi = {"q", q, ((n - 1) * p.q_stride + qr) * e};
+    if ((st = cache_apart(fn, p.c, e, {qi, qo}))) return st;
+    if (q_out != q && rows_overlap(q_out, p.qo_stride, qr, q, p.q_stride, qr, n, e))
+      return fail(ROLESUB_ERR_INVALID_ARG, "%s: q_out overlaps q", fn);
+  }
+  p.B = B;
+  p.T = T;
+  p.dh = dh;
+  p.n_axes = n_axes;
+  p.n_pairs = n_pairs;
+  p.interleaved = interleaved != 0;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.Rm = R;
+  p.mask = mask;
+  p.wq = q_weight;
+  p.wk = k_weight;
+  p.eps = eps;
+  p.positions = positions;
+  p.inv_freq = inv_freq;
+  p.axis = axis;
+  p.table = table;
+  p.max_pages = max_pages;
+  p.lens = lens;
+  p.n_new = n_new;
+  p.q_out = q_out;
+  return from_hip(launch_append_rotary(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+rolesub_status rolesub_tree_masks(int32_t B, int32_t T, const int32_t* parents, uint32_t* tree, int32_t* depth,
+                                  void* stream) {
+  const char* fn = "rolesub_tree_masks";
+  if (B < 0 || T < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: B and T must be >= 0", fn);
+  if (T > kMaxTree) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: T=%d above %d", fn, T, kMaxTree);
+  if (B == 0 || T == 0) return ROLESUB_OK;
+  if (!parents || !tree) return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  if (static_cast<size_t>(B) * 256 >= kMaxThreads) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many trees", fn);
+  const size_t n = static_cast<size_t>(B) * T * 4;
+  const rolesub_status st = apart(fn, {{"tree", tree, n * ((T + 31) / 32)}, {"depth", depth, n}}, {{"parents", parents, n}});
+  if (st) return st;
+  return from_hip(launch_tree_masks(TreeParams{B, T, parents, tree, depth}, static_cast<hipStream_t>(stream)), fn);
+}
+
+size_t rolesub_attend_tree_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq, int32_t max_len) {
+  return rolesub_attend_paged_workspace_size(pages, B, Hq, Tq, max_len, 0);
+}
+
+rolesub_status rolesub_attend_tree(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                   const void* q, int64_t q_stride, const int32_t* table, int32_t max_pages,
+                                   const int32_t* lens, const int32_t* n_new, const uint32_t* tree, int32_t trees,
+                                   int32_t max_len, const void* R, float scale, void* out, rolesub_dtype out_dtype,
+                                   void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "rolesub_attend_tree";
+  DecodeParams p = {};
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, B > 0 && Tq > 0, p.c);
+  if (st) return st;
+  if ((st = check_attend(fn, dtype, out_dtype, p.c, B, Hq, Tq, max_pages, scale))) return st;
+  if (max_len < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: max_len must be >= 0", fn);
+  if (Tq > kMaxTree) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: Tq=%d above %d", fn, Tq, kMaxTree);
+  if (B == 0 || Tq == 0) return ROLESUB_OK;
+  if (trees != 1 && trees != B)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: trees=%d is neither 1 nor B=%d", fn, trees, B);
+  const int64_t all = static_cast<int64_t>(max_pages) * p.c.page;
+  const int64_t ml = max_len == 0 ? all : std::min<int64_t>(max_len, all);
+  if (ml > (1 << 30)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: more than 2^30 tokens (pass max_len)", fn);
+  if (!q || !lens || !out || !tree || (ml > 0 && !table))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  p.B = B;
+  p.Tq = Tq;
+  p.max_len = static_cast<int>(ml);
+  p.lens = lens;
+  p.n_new = n_new;
+  p.tree = tree;
+  p.trees = trees;
+  const size_t nq = static_cast<size_t>(B) * Tq;
+  st = set_attend(fn, p, dtype, Hq, q, q_stride, table, max_pages, R, scale, out, out_dtype, workspace, ws_bytes, B,
+                  {{"lens", lens, static_cast<size_t>(B) * 4}, {"n_new", n_new, static_cast<size_t>(B) * 4},
+                   {"tree", tree, (trees > 1 ? nq : Tq) * ((Tq + 31) / 32) * 4}});
+  if (st) return st;
+  return from_hip(launch_decode_tree(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+rolesub_status rolesub_cache_accept(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
+                                    const int32_t* table, int32_t max_pages, const int32_t* lens, const uint32_t* tree,
+                                    int32_t trees, const int32_t* leaf, int32_t* new_lens, void* stream) {
+  const char* fn = "rolesub_cache_accept";
+  AcceptParams p = {};
+  const bool work = B > 0;
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, work && max_pages > 0, p.c);
+  if (st) return st;
+  if (B < 0 || T < 0 || max_pages < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: B, T and max_pages must be >= 0", fn);
+  if (T > kMaxTree) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: T=%d above %d", fn, T, kMaxTree);
+  if (!work) return ROLESUB_OK;
+  if (trees != 1 && trees != B)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: trees=%d is neither 1 nor B=%d", fn, trees, B);
+  if ((T > 0 && !tree) || !leaf || !lens || (max_pages > 0 && !table))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  if (static_cast<size_t>(B) * 256 >= kMaxThreads || p.c.H > 65535)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences or heads", fn);
+  const size_t rows = static_cast<size_t>(B);
+  const Operand to = {"new_lens", new_lens, rows * 4}, tb = {"table", table, rows * max_pages * 4}, ln = {"lens", lens, rows * 4},
+                lf = {"leaf", leaf, rows * 4}, tr = {"tree", tree, static_cast<size_t>(trees) * T * ((T + 31) / 32) * 4};
+  if ((st = apart(fn, {to}, {tb, ln, lf, tr}))) return st;
+  if ((st = cache_apart(fn, p.c, esize(dtype), {tb, ln, lf, tr, to}))) return st;
+  p.B = B;
+  p.T = T;
+  p.trees = trees;
+  p.max_pages = max_pages;
+  p.table = table;
+  p.lens = lens;
+  p.leaf = leaf;
+  p.tree = tree;
+  p.new_lens = new_lens;
+  return from_hip(launch_accept(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+rolesub_status rolesub_page_bounds(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
+                                   const int32_t* table, int32_t max_pages, const int32_t* lens, void* bounds,
+                                   void* stream) {
+  const char* fn = "rolesub_page_bounds";
+  BoundsParams p = {};
+  const bool work = B > 0 && T > 0 && max_pages > 0;
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, work, p.c);
+  if (st) return st;
+  if (B < 0 || T < 0 || max_pages < 0) return fail(ROLESUB_ERR_INVALID_ARG, "%s: B, T and max_pages must be >= 0", fn);
+  if (!work || p.c.n_pages == 0) return ROLESUB_OK;
+  if (!table || !lens || !bounds) return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  if (!aligned(bounds, 16)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: bounds must lie on 16 bytes", fn);
+  const int64_t np = std::min<int64_t>(max_pages, static_cast<int64_t>(T) / p.c.page + 2);
+  if (static_cast<double>(B) * np * p.c.H * 64 >= static_cast<double>(kMaxThreads))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, pages or heads", fn);
+  const size_t e = esize(dtype), rows = static_cast<size_t>(B);
+  const Operand out = {"bounds", bounds, static_cast<size_t>(p.c.n_pages) * p.c.H * 2 * p.c.dh * e};
+  if ((st = apart(fn, {out}, {{"table", table, rows * max_pages * 4}, {"lens", lens, rows * 4}}))) return st;
+  if ((st = cache_apart(fn, p.c, e, {out}))) return st;
+  p.B = B;
+  p.T = T;
+  p.max_pages = max_pages;
+  p.table = table;
+  p.lens = lens;
+  p.bounds = bounds;
+  return from_hip(launch_page_bounds(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
+}
+
+namespace {
+
+// Workspace of a choice of pages: scores, how many pages each query sees and how many it
+// gets, and the selection's own.
+struct SelectPlan {
+  int64_t rows, ld;
+  size_t off_count, off_kept, off_evict, bytes;
+};
+SelectPlan select_plan(int64_t B, int64_t Tq, int H, int page, int64_t max_len) {
+  SelectPlan d;
+  d.rows = B * Tq * H;
+  d.ld = (max_len + page - 1) / page;
+  d.off_count = align256(static_cast<size_t>(d.rows) * d.ld * 4);
+  d.off_kept = d.off_count + align256(static_cast<size_t>(d.rows) * 4);
+  d.off_evict = d.off_kept + align256(static_cast<size_t>(d.rows) * 4);
+  d.bytes = d.off_evict + rolesub_evict_workspace_size(static_cast<int32_t>(d.rows), static_cast<int32_t>(d.ld));
+  return d;
+}
+
+}  // namespace
+
+size_t rolesub_select_pages_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Tq, int32_t max_len) {
+  if (!pages || B <= 0 || Tq <= 0 || max_len < 0 || pages->H < 1 || pages->page < 1) return 0;
+  if (static_cast<double>(B) * Tq * pages->H > 0x7FFFFFFF) return 0;
+  return select_plan(B, Tq, pages->H, pages->page, max_len).bytes;
+}
+
+rolesub_status rolesub_select_pages(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                    const void* q, int64_t q_stride, const void* bounds, const int32_t* table,
+                                    int32_t max_pages, const int32_t* lens, const int32_t* visible, int32_t max_len,
+                                    int32_t n_sel, int32_t first, int32_t recent, int32_t* sel, void* workspace,
+                                    size_t ws_bytes, void* stream) {
+  const char* fn = "rolesub_select_pages";
+  SelectParams p = {};
+  const bool work = B > 0 && Tq > 0;
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, work, p.c);
+  if (st) return st;
+  if (B < 0 || Tq < 0 || max_pages < 0 || max_len < 0)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: B, Tq, max_pages and max_len must be >= 0", fn);
+  if (Hq < 1 || Hq % p.c.H)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: %d query heads are not a multiple of %d key heads", fn, Hq, p.c.H);
+  if (n_sel < 1 || first < 0 || recent < 0 || static_cast<int64_t>(first) + recent > n_sel)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: need n_sel >= 1, first, recent >= 0 and first + recent <= n_sel (%d, %d, %d)",
+                fn, n_sel, first, recent);
+  if (!work) return ROLESUB_OK;
+  const int64_t all = static_cast<int64_t>(max_pages) * p.c.page;
+  const int64_t ml = max_len == 0 ? all : std::min<int64_t>(max_len, all);
+  if (ml > (1 << 30)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: more than 2^30 tokens (pass max_len)", fn);
+  if (!q || !lens || !sel || (ml > 0 && (!table || !bounds)))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  if (!aligned(bounds, 16)) return fail(ROLESUB_ERR_UNSUPPORTED, "%s: bounds must lie on 16 bytes", fn);
+  p.q_stride = q_stride;
+  if ((st = check_rows(fn, "q", q, p.q_stride, Hq, p.c.dh, esize(dtype)))) return st;
+  const size_t e = esize(dtype), nq = static_cast<size_t>(B) * Tq, qrow = static_cast<size_t>(Hq) * p.c.dh;
+  // the selection has up to 64 workgroups of 512 threads a row
+  if (static_cast<double>(nq) * p.c.H * 64 * 512 >= static_cast<double>(kMaxThreads) ||
+      static_cast<double>(Hq / p.c.H) * Tq > 0x7FFFFFFF || n_sel > (1 << 30) ||
+      static_cast<double>(B) * p.c.H * ((ml / p.c.page + 65) / 64) * 256 >= static_cast<double>(kMaxThreads))
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads, queries or pages", fn);
+  const SelectPlan d = select_plan(B, Tq, p.c.H, p.c.page, ml);
+  if (!workspace || ws_bytes < d.bytes)
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, %zu given", fn, d.bytes,
+                workspace ? ws_bytes : static_cast<size_t>(0));
+  if (!aligned(workspace, 16)) return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace must lie on 16 bytes", fn);
+  const size_t rows = static_cast<size_t>(d.rows), np = static_cast<size_t>(p.c.n_pages);
+  st = apart(fn, {{"sel", sel, rows * n_sel * 4}, {"workspace", workspace, d.bytes}},
+             {{"q", q, ((nq - 1) * p.q_stride + qrow) * e}, {"bounds", bounds, np * p.c.H * 2 * p.c.dh * e},
+              {"table", table, static_cast<size_t>(B) * max_pages * 4}, {"lens", lens, static_cast<size_t>(B) * 4},
+              {"visible", visible, nq * 4}, {"K", p.c.K, np * p.c.H * p.c.page * p.c.dh * e},
+              {"V", p.c.V, np * p.c.H * p.c.vcap * p.c.ds * e}, {"mask", p.c.mask, np * p.c.page * 4},
+              {"slot", p.c.slot, np * p.c.page * 4}});
+  if (st) return st;
+  char* ws = static_cast<char*>(workspace);
+  p.B = B;
+  p.Tq = Tq;
+  p.rep = Hq / p.c.H;
+  p.max_pages = max_pages;
+  p.max_len = static_cast<int>(ml);
+  p.q = q;
+  p.bounds = bounds;
+  p.table = table;
+  p.lens = lens;
+  p.visible = visible;
+  p.ld = static_cast<int>(d.ld);
+  p.scores = reinterpret_cast<float*>(ws);
+  p.counts = reinterpret_cast<int32_t*>(ws + d.off_count);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t err = launch_page_scores(p, dtype == ROLESUB_BF16, s);
+  if (err != hipSuccess) return from_hip(err, fn);
+  EvictParams ev = {static_cast<int>(d.rows), p.ld, n_sel, first, recent, p.scores, d.ld, p.counts, sel,
+                    reinterpret_cast<int32_t*>(ws + d.off_kept), ws + d.off_evict};
+  return from_hip(launch_evict(ev, s), fn);
+}
+
+size_t rolesub_attend_selected_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq, int32_t n_sel) {
+  if (!pages || B <= 0 || Tq <= 0 || n_sel <= 0 || pages->page < 1) return 0;
+  if (static_cast<double>(B) * Tq > 0x7FFFFFFF || static_cast<int64_t>(n_sel) * pages->page > (1 << 30)) return 0;
+  return rolesub_attend_paged_workspace_size(pages, B * Tq, Hq, 1, n_sel * pages->page, 0);
+}
+
+rolesub_status rolesub_attend_selected(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
+                                       const void* q, int64_t q_stride, const int32_t* table, int32_t max_pages,
+                                       const int32_t* lens, const int32_t* visible, const int32_t* sel, int32_t n_sel,
+                                       const void* R, float scale, void* out, rolesub_dtype out_dtype, void* workspace,
+                                       size_t ws_bytes, void* stream) {
+  const char* fn = "rolesub_attend_selected";
+  DecodeParams p = {};
+  rolesub_status st = check_pages(fn, "pages", pages, dtype, B > 0 && Tq > 0, p.c);
+  if (st) return st;
+  if ((st = check_attend(fn, dtype, out_dtype, p.c, B, Hq, Tq, max_pages, scale))) return st;
+  if (n_sel < 1) return fail(ROLESUB_ERR_INVALID_ARG, "%s: n_sel must be >= 1", fn);
+  if (B == 0 || Tq == 0) return ROLESUB_OK;
+  if (static_cast<int64_t>(max_pages) * p.c.page > (1 << 30) || static_cast<int64_t>(n_sel) * p.c.page > (1 << 30) ||
+      static_cast<double>(B) * Tq > 0x7FFFFFFF)
+    return fail(ROLESUB_ERR_UNSUPPORTED, "%s: more than 2^30 tokens, or too many queries", fn);
+  if (!q || !lens || !out || !sel || (max_pages > 0 && !table))
+    return fail(ROLESUB_ERR_INVALID_ARG, "%s: a tensor pointer is NULL", fn);
+  const size_t nq = static_cast<size_t>(B) * Tq;
+  p.B = static_cast<int>(nq);
+  p.Tq = 1;
+  p.per = Tq;
+  p.max_len = n_sel * p.c.page;
+  p.lens = lens;
+  p.visible = visible;
+  p.sel = sel;
+  p.n_sel = n_sel;
+  st = set_attend(fn, p, dtype, Hq, q, q_stride, table, max_pages, R, scale, out, out_dtype, workspace, ws_bytes, B,
+                  {{"lens", lens, static_cast<size_t>(B) * 4}, {"visible", visible, nq * 4},
+                   {"sel", sel, nq * p.c.H * n_sel * 4}});
+  if (st) return st;
+  return from_hip(launch_decode_listed(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
 }
 
 }  // extern "C"

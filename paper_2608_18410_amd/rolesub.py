@@ -30,6 +30,9 @@ EXPORTS = (
     "rolesub_attend_values", "rolesub_route_noalloc",
     "rolesub_rotary", "rolesub_cache_append", "rolesub_attend_paged_workspace_size", "rolesub_attend_paged",
     "rolesub_evict_workspace_size", "rolesub_evict_tokens", "rolesub_cache_compact",
+    "rolesub_norm_rotary", "rolesub_append_rotary", "rolesub_tree_masks", "rolesub_attend_tree_workspace_size",
+    "rolesub_attend_tree", "rolesub_cache_accept", "rolesub_page_bounds", "rolesub_select_pages_workspace_size",
+    "rolesub_select_pages", "rolesub_attend_selected_workspace_size", "rolesub_attend_selected",
 )
 ROUTE_NOALLOC_MAX_BYTES = 8 << 20
 
@@ -114,6 +117,21 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.rolesub_evict_workspace_size.restype = SZ
     lib.rolesub_evict_tokens.argtypes = [I32, I32, P, I64, P, I32, I32, I32, P, P, P, SZ, P]
     lib.rolesub_cache_compact.argtypes = [P, P, C, I32, P, I32, P, P, I32, P, I32, P, I64, P, I64, P]
+    lib.rolesub_norm_rotary.argtypes = [I32, I32, I32, I32, I32, C, P, I64, P, I64, P, P, F, P, I32, P, P, I32, I32, P, P, P]
+    lib.rolesub_append_rotary.argtypes = [P, C, I32, I32, I32, P, I64, P, I64, P, I64, P, P, P, P, F, P, I32, P, P, I32, I32,
+                                          P, I32, P, P, P, P]
+    lib.rolesub_tree_masks.argtypes = [I32, I32, P, P, P, P]
+    lib.rolesub_attend_tree_workspace_size.argtypes = [P, I32, I32, I32, I32]
+    lib.rolesub_attend_tree_workspace_size.restype = SZ
+    lib.rolesub_attend_tree.argtypes = [P, C, I32, I32, I32, P, I64, P, I32, P, P, P, I32, I32, P, F, P, C, P, SZ, P]
+    lib.rolesub_cache_accept.argtypes = [P, C, I32, I32, P, I32, P, P, I32, P, P, P]
+    lib.rolesub_page_bounds.argtypes = [P, C, I32, I32, P, I32, P, P, P]
+    lib.rolesub_select_pages_workspace_size.argtypes = [P, I32, I32, I32]
+    lib.rolesub_select_pages_workspace_size.restype = SZ
+    lib.rolesub_select_pages.argtypes = [P, C, I32, I32, I32, P, I64, P, P, I32, P, P, I32, I32, I32, I32, P, P, SZ, P]
+    lib.rolesub_attend_selected_workspace_size.argtypes = [P, I32, I32, I32, I32]
+    lib.rolesub_attend_selected_workspace_size.restype = SZ
+    lib.rolesub_attend_selected.argtypes = [P, C, I32, I32, I32, P, I64, P, I32, P, P, P, I32, P, F, P, C, P, SZ, P]
     for fn in ("rolesub_rotate_values", "rolesub_route", "rolesub_route_noalloc", "rolesub_pack_kv",
                "rolesub_rotate_pack", "rolesub_attend"):
         getattr(lib, fn).restype = ctypes.c_int
@@ -1002,3 +1020,258 @@ def cache_compact(src: PagedCache, table, keep_idx, n_keep, dst: PagedCache, dst
     _check("rolesub_cache_compact", load().rolesub_cache_compact(
         src.desc(), dst.desc(), _CODES[dt], B, pt, W, pi, pn, keep, pd, D, pm, L or 0, pmo, M or 0, s))
     return mass_out
+
+
+# ----------------------------------------------------------------------------
+# Paged routed cache: normed heads, drafted tokens, few pages of a long history
+# ----------------------------------------------------------------------------
+
+def _positions(positions, B, T, inv_freq, axis, spec):
+    """Positions, frequencies and axes of a call that turns heads, into its spec: (axes, pairs)."""
+    A, n = 1, None
+    if isinstance(positions, _Tensor) and positions.dim() == 3:
+        A = positions.shape[2]
+        spec.append(("positions", positions, (B, T, A), torch.int32))
+    else:
+        spec.append(("positions", positions, (B, T), torch.int32))
+    if isinstance(inv_freq, _Tensor) and inv_freq.dim() == 1:
+        n = inv_freq.shape[0]
+    spec += [("inv_freq", inv_freq, (n,), torch.float32), ("axis", axis, (n,), torch.uint8)]
+    return A, n
+
+
+def _turned(name, x, xs, stride, dense, o, dt, stream):
+    """The output of a call that turns x (new where o is None), and its shape for _args."""
+    if o is None:
+        return (torch.empty_like(x) if dense and stream is None else _empty(xs, dt, x.device, stream)), xs
+    _need(f"{name}_out", o, xs, dt)
+    so, odense = _rows(f"{name}_out", o)
+    if odense is None and (so != stride or o.data_ptr() != x.data_ptr()):
+        raise ValueError(f"{name}_out: must be {name} itself or contiguous")
+    if odense is not None and o.data_ptr() == x.data_ptr() and dense is None and o.numel():
+        raise ValueError(f"{name}_out: must be {name} itself or lie apart from it")
+    return o, odense
+
+
+def norm_rotary(q, k, q_weight, k_weight, eps: float, positions, inv_freq, axis=None, interleaved=False, out=None,
+                stream=None):
+    """rotary of q and k (either may be None) whose heads are first divided by their root
+    mean square and weighted: q_weight and k_weight [dh], None for a tensor that is
+    turned only. out: (q_out, k_out); an input itself is written in place. Returns
+    (q_out, k_out)."""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q and k are both None")
+    shape = some.shape if isinstance(some, _Tensor) else ()
+    if len(shape) != 4 or some.dtype not in _FLOATS:
+        _need("q" if q is not None else "k", some, (None, None, None, None), _FLOATS)
+    B, T, _, dh = shape
+    dt = some.dtype
+    spec = []
+    A, n = _positions(positions, B, T, inv_freq, axis, spec)
+    outs, heads, strides = [None, None] if out is None else list(out), [0, 0], [0, 0]
+    for i, (name, x, w) in enumerate((("q", q, q_weight), ("k", k, k_weight))):
+        if x is None:
+            outs[i] = None
+            spec += [(name, None, None, None)] * 3
+            continue
+        xs, strides[i], dense = _operand(name, x, None, dh, dt)
+        if xs[0] != B or xs[1] != T:
+            _need(name, x, (B, T, None, dh), dt)
+        heads[i] = xs[2]
+        outs[i], odense = _turned(name, x, xs, strides[i], dense, outs[i], dt, stream)
+        spec += [(name, x, dense, dt), (f"{name}_weight", w, (dh,), dt), (f"{name}_out", outs[i], odense, dt)]
+    (pp, pf, pa, pq, pqw, pqo, pk, pkw, pko), s = _args(stream, spec)
+    _check("rolesub_norm_rotary", load().rolesub_norm_rotary(
+        B, T, heads[0], heads[1], dh, _CODES[dt], pq, strides[0], pk, strides[1], pqw, pkw, float(eps), pp, A, pf, pa, n,
+        1 if interleaved else 0, pqo, pko, s))
+    return outs[0], outs[1]
+
+
+def append_rotary(cache: PagedCache, k, v, mask, table, lens, positions, inv_freq, axis=None, R=None, q=None,
+                  q_weight=None, k_weight=None, eps: float = 1e-6, interleaved=False, n_new=None, q_out=None, stream=None):
+    """cache_append of new tokens straight from their projections: keys k [B,T,H,dh]
+    normed (with k_weight [dh]) and turned by their positions, values v [B,T,H,dh]
+    rotated by R [H,dh,dh] (None: kept as they are). Returns the queries q [B,T,Hq,dh],
+    normed (with q_weight) and turned, or None without them."""
+    dt, dh = cache.dtype, cache.dh
+    shape, sk, dk = _operand("k", k, cache.H, dh, dt)
+    B, T = shape[:2]
+    _need("v", v, shape, dt)
+    sv, dv = _rows("v", v)
+    W, Hq, sq = _width(table), 0, 0
+    spec = []
+    A, n = _positions(positions, B, T, inv_freq, axis, spec)
+    if q is None:
+        if q_weight is not None or q_out is not None:
+            raise ValueError("q_weight and q_out need q")
+        spec += [("q", None, None, None)] * 3
+    else:
+        qs, sq, dq = _operand("q", q, None, dh, dt)
+        if qs[0] != B or qs[1] != T:
+            _need("q", q, (B, T, None, dh), dt)
+        Hq = qs[2]
+        q_out, odense = _turned("q", q, qs, sq, dq, q_out, dt, stream)
+        spec += [("q", q, dq, dt), ("q_weight", q_weight, (dh,), dt), ("q_out", q_out, odense, dt)]
+    spec += [("k", k, dk, dt), ("v", v, dv, dt), ("k_weight", k_weight, (dh,), dt), ("R", R, (cache.H, dh, dh), dt),
+             ("mask", mask, (B, T), mask.dtype if getattr(mask, "dtype", None) in _MASK else _MASK),
+             ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32), ("n_new", n_new, (B,), torch.int32)]
+    (pp, pf, pa, pq, pqw, pqo, pk, pv, pkw, pR, pm, pt, pl, pn), s = _args(stream, spec, cache)
+    _check("rolesub_append_rotary", load().rolesub_append_rotary(
+        cache.desc(), _CODES[dt], B, T, Hq, pq, sq, pk, sk, pv, sv, pR, pm, pqw, pkw, float(eps), pp, A, pf, pa, n,
+        1 if interleaved else 0, pt, W, pl, pn, pqo, s))
+    return q_out
+
+
+def tree_masks(parents, out=None, stream=None):
+    """Ancestors of drafted tokens from their parents [B,T] int32 (negative: a child of the
+    cached tokens). Returns (tree [B,T,ceil(T/32)] int32 bits, themselves among them; depth
+    [B,T] int32, how many ancestors)."""
+    shape = parents.shape if isinstance(parents, _Tensor) else ()
+    if len(shape) != 2:
+        _need("parents", parents, (None, None), torch.int32)
+    B, T = shape
+    words = (B, T, (T + 31) // 32)
+    if out is None:
+        out = (_empty(words, torch.int32, parents.device, stream), _empty((B, T), torch.int32, parents.device, stream))
+    tree, depth = out
+    (pp, pt, pd), s = _args(stream, (
+        ("parents", parents, (B, T), torch.int32),
+        ("tree", tree, words, tree.dtype if getattr(tree, "dtype", None) in _MASK else _MASK),
+        ("depth", depth, (B, T), torch.int32)))
+    _check("rolesub_tree_masks", load().rolesub_tree_masks(B, T, pp, pt, pd, s))
+    return tree, depth
+
+
+def _tree(tree, B, T):
+    """A tree's bits for _args, and how many trees there are."""
+    n = tree.shape[0] if isinstance(tree, _Tensor) and tree.dim() == 3 and tree.shape[0] == 1 else B
+    return ("tree", tree, (n, T, (T + 31) // 32), tree.dtype if getattr(tree, "dtype", None) in _MASK else _MASK), n
+
+
+def attend_tree_workspace_size(cache: PagedCache, B, Hq, Tq, max_len) -> int:
+    return load().rolesub_attend_tree_workspace_size(ctypes.byref(cache._desc), B, Hq, Tq, max_len)
+
+
+def attend_tree(q, cache: PagedCache, table, lens, tree, R=None, n_new=None, scale: float = 0.0, max_len: int = 0,
+                workspace=None, out_dtype=None, out=None, stream=None):
+    """Attention of drafted tokens q [B,Tq,Hq,dh], cached from lens [B] on, each over the
+    cached tokens before them and its own bits of tree [B or 1,Tq,ceil(Tq/32)]; rows past
+    n_new [B] (None: Tq) give zeros. Returns [B,Tq,Hq,dh]."""
+    H, dh, dt = cache.H, cache.dh, cache.dtype
+    shape, sq, dq = _operand("q", q, None, dh, dt)
+    B, Tq, Hq, _ = shape
+    W = _width(table)
+    o = _empty(shape, out_dtype or dt, q.device, stream) if out is None else out
+    odt = o.dtype if isinstance(o, _Tensor) and o.dtype in _CODES else _FLOATS
+    if workspace is None:
+        whole = (W or 0) * cache.page
+        need = attend_tree_workspace_size(cache, B, Hq, Tq, min(int(max_len), whole) if max_len else whole)
+        workspace = _empty(max(need, 1), torch.uint8, q.device, stream, output=False)
+    ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
+    bits, trees = _tree(tree, B, Tq)
+    (pq, pt, pl, pn, pb, pR, po, pw), s = _args(stream, (
+        ("q", q, dq, dt), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
+        ("n_new", n_new, (B,), torch.int32), bits, ("R", R, (H, dh, dh), dt), ("out", o, shape, odt),
+        ("workspace", workspace, (ws,), torch.uint8)), cache)
+    _check("rolesub_attend_tree", load().rolesub_attend_tree(
+        cache.desc(), _CODES[dt], B, Hq, Tq, pq, sq, pt, W, pl, pn, pb, trees, int(max_len), pR, float(scale), po,
+        _CODES[odt], pw, ws, s))
+    return o
+
+
+def cache_accept(cache: PagedCache, table, lens, tree, leaf, new_lens=None, stream=None):
+    """Of the drafted tokens cached from lens [B] on, those on the path of token leaf [B]
+    (its bits of tree [B or 1,T,ceil(T/32)]; -1: none) move behind the cached ones.
+    Returns the new lengths [B]."""
+    T = tree.shape[1] if isinstance(tree, _Tensor) and tree.dim() == 3 else 0
+    B = leaf.shape[0] if isinstance(leaf, _Tensor) and leaf.dim() == 1 else None
+    if B is None:
+        _need("leaf", leaf, (None,), torch.int32)
+        raise TypeError("leaf: expected a torch tensor, got None")
+    if new_lens is None:
+        new_lens = _empty((B,), torch.int32, leaf.device, stream)
+    W = _width(table)
+    bits, trees = _tree(tree, B, T)
+    (pl, pt, pn, pb, po), s = _args(stream, (
+        ("leaf", leaf, (B,), torch.int32), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32), bits,
+        ("new_lens", new_lens, (B,), torch.int32)), cache)
+    _check("rolesub_cache_accept", load().rolesub_cache_accept(
+        cache.desc(), _CODES[cache.dtype], B, T, pt, W, pn, pb, trees, pl, po, s))
+    return new_lens
+
+
+def page_bounds(cache: PagedCache, table, lens, bounds, T: int, stream=None):
+    """Bounds [n_pages,H,2,dh] of the keys in the pages that hold each sequence's last T
+    tokens (lens [B] counts them), written over what was there. Returns bounds."""
+    B = lens.shape[0] if isinstance(lens, _Tensor) and lens.dim() == 1 else None
+    W = _width(table)
+    (pt, pl, pb), s = _args(stream, (
+        ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
+        ("bounds", bounds, (cache.K.shape[0], cache.H, 2, cache.dh), cache.dtype)), cache)
+    _check("rolesub_page_bounds", load().rolesub_page_bounds(
+        cache.desc(), _CODES[cache.dtype], B, int(T), pt, W, pl, pb, s))
+    return bounds
+
+
+def select_pages_workspace_size(cache: PagedCache, B, Tq, max_len) -> int:
+    return load().rolesub_select_pages_workspace_size(ctypes.byref(cache._desc), B, Tq, max_len)
+
+
+def select_pages(q, cache: PagedCache, bounds, table, lens, n_sel: int, first: int = 0, recent: int = 0, visible=None,
+                 max_len: int = 0, workspace=None, out=None, stream=None):
+    """The n_sel pages that each query q [B,Tq,Hq,dh] and key head attends to: the first, the
+    recent, and of the others those whose bounds promise the highest scores. Returns
+    [B,Tq,H,n_sel] int32, ascending, then -1."""
+    dh, dt, H = cache.dh, cache.dtype, cache.H
+    shape, sq, dq = _operand("q", q, None, dh, dt)
+    B, Tq, Hq, _ = shape
+    W = _width(table)
+    if out is None:
+        if n_sel < 1:
+            raise ValueError(f"n_sel: expected at least 1, got {n_sel}")
+        out = _empty((B, Tq, H, int(n_sel)), torch.int32, q.device, stream)
+    if workspace is None:
+        whole = (W or 0) * cache.page
+        need = select_pages_workspace_size(cache, B, Tq, min(int(max_len), whole) if max_len else whole)
+        workspace = _empty(max(need, 1), torch.uint8, q.device, stream, output=False)
+    ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
+    (pq, pb, pt, pl, pv, po, pw), s = _args(stream, (
+        ("q", q, dq, dt), ("bounds", bounds, (cache.K.shape[0], H, 2, dh), dt), ("table", table, (B, W), torch.int32),
+        ("lens", lens, (B,), torch.int32), ("visible", visible, (B, Tq), torch.int32),
+        ("sel", out, (B, Tq, H, int(n_sel)), torch.int32), ("workspace", workspace, (ws,), torch.uint8)), cache)
+    _check("rolesub_select_pages", load().rolesub_select_pages(
+        cache.desc(), _CODES[dt], B, Hq, Tq, pq, sq, pb, pt, W, pl, pv, int(max_len), int(n_sel), int(first), int(recent), po,
+        pw, ws, s))
+    return out
+
+
+def attend_selected_workspace_size(cache: PagedCache, B, Hq, Tq, n_sel) -> int:
+    return load().rolesub_attend_selected_workspace_size(ctypes.byref(cache._desc), B, Hq, Tq, n_sel)
+
+
+def attend_selected(q, cache: PagedCache, table, lens, sel, R=None, scale: float = 0.0, visible=None, workspace=None,
+                    out_dtype=None, out=None, stream=None):
+    """attend_paged over the tokens of the listed pages only: sel [B,Tq,H,n_sel] int32 for
+    each query and key head, in any order, -1 for none. Returns [B,Tq,Hq,dh]."""
+    H, dh, dt = cache.H, cache.dh, cache.dtype
+    shape, sq, dq = _operand("q", q, None, dh, dt)
+    B, Tq, Hq, _ = shape
+    W = _width(table)
+    n = sel.shape[3] if isinstance(sel, _Tensor) and sel.dim() == 4 else None
+    if n is None:
+        _need("sel", sel, (B, Tq, H, None), torch.int32)
+        raise TypeError("sel: expected a torch tensor, got None")
+    o = _empty(shape, out_dtype or dt, q.device, stream) if out is None else out
+    odt = o.dtype if isinstance(o, _Tensor) and o.dtype in _CODES else _FLOATS
+    if workspace is None:
+        need = attend_selected_workspace_size(cache, B, Hq, Tq, n)
+        workspace = _empty(max(need, 1), torch.uint8, q.device, stream, output=False)
+    ws = workspace.numel() if isinstance(workspace, _Tensor) else 0
+    (pq, pt, pl, ps, pR, pv, po, pw), s = _args(stream, (
+        ("q", q, dq, dt), ("table", table, (B, W), torch.int32), ("lens", lens, (B,), torch.int32),
+        ("sel", sel, (B, Tq, H, n), torch.int32), ("R", R, (H, dh, dh), dt), ("visible", visible, (B, Tq), torch.int32),
+        ("out", o, shape, odt), ("workspace", workspace, (ws,), torch.uint8)), cache)
+    _check("rolesub_attend_selected", load().rolesub_attend_selected(
+        cache.desc(), _CODES[dt], B, Hq, Tq, pq, sq, pt, W, pl, pv, ps, n, pR, float(scale), po, _CODES[odt], pw, ws, s))
+    return o
