@@ -4,6 +4,7 @@
 // and the same on the way into the paged cache, with the values taken into the routing
 // space, z = R^T v, and their kept groups packed.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "launch.hpp"
@@ -26,80 +27,237 @@ __device__ __forceinline__ Spot spot_of(const TurnParams& p, int64_t tok) {
   return Spot{static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages) ? page : -1, static_cast<int>(t & (c.page - 1))};
 }
 
-// Heads [h0, h1) of one token's rows (queries first, then keys), a wave's work. A lane
-// holds a 16-byte piece of a row, and for all rows the factors of its elements: an
-// element becomes m1 f1 + m2 f2 of itself and the other of its pair, times its row's
-// 1 / root. Without a norm this is in every bit what the rotation's own kernels give,
-// which is why m1 is the pair's first element where they multiply that first. In halves the other
-// elements lie n behind or before: the rows' pieces go through LDS (a wave's rows of a
-// step, with a piece's room before and behind). WHOLE: pieces lie in one half.
-template <class T, bool IL, bool WHOLE, bool CACHE>
-__device__ __forceinline__ void turn_rows(const TurnParams& p, int64_t tok, int h0, int h1, char* stage, float (*cs)[kMaxPairs]) {
-  constexpr int V = 16 / sizeof(T), U = 4;
+// Sum over the LPR lanes of a row, the same bits in all of them.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+  auto dpp = [](float y, auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  x += dpp(x, std::integral_constant<int, 0xB1>{});                            // lanes 1 apart
+  x += dpp(x, std::integral_constant<int, 0x4E>{});                            // 2 apart
+  if constexpr (LPR >= 8) x += dpp(x, std::integral_constant<int, 0x141>{});   // the other half of 8
+  if constexpr (LPR >= 16) x += dpp(x, std::integral_constant<int, 0x140>{});  // the other half of 16
+  if constexpr (LPR >= 32) x = add_xor16(x);
+  return x;
+}
+
+// 1 / sqrt(mean x^2 + eps) of a row from its sum of squares; a lane's elements again, times
+// 2^-64, where the squares pass the range or are not finite.
+template <int LPR, int N>
+__device__ __forceinline__ float inverse_root(float sq, const float (&x)[N], float per, float eps) {
+  float inv = __builtin_amdgcn_rsqf(sq * per + eps);
+  if (__any(!(sq < __builtin_inff()))) {
+    float small = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float y = x[i] * 0x1p-64f;
+      small += y * y;
+    }
+    small = row_sum<LPR>(small);
+    if (!(sq < __builtin_inff())) inv = __builtin_amdgcn_rsqf(small * per) * 0x1p-64f;
+  }
+  return inv;
+}
+
+// Cosines and sines of one token's pairs, a pair a lane, for its wave through LDS.
+__device__ __forceinline__ void put_angles(const TurnParams& p, int64_t tok, float (*cs)[kMaxPairs]) {
   const int lane = threadIdx.x & 63;
-  const int n = p.n_pairs, lpr = p.dh / V, hs = 64 / lpr, hl = lane / lpr, e0 = lane % lpr * V;
+  if (lane < p.n_pairs) {
+    const int ax = p.axis ? p.axis[lane] : 0;
+    float cc = kStays, ss = 0.f;
+    if (ax < p.n_axes) angle(p.positions[tok * p.n_axes + ax], p.inv_freq[lane], cc, ss);
+    cs[0][lane] = cc;
+    cs[1][lane] = ss;
+  }
+  wave_lds_order();
+}
+
+// Queries or keys of one token: where they lie, where they go.
+template <class T>
+struct Segment {
+  const T *in, *weight;
+  T* out;
+  int64_t ld;
+  int h0, h1;
+};
+template <class T, bool CACHE>
+__device__ __forceinline__ Segment<T> segment(const TurnParams& p, int64_t tok, int seg, int h0, int h1, const Spot& spot) {
+  Segment<T> g;
+  g.h0 = seg ? max(h0, p.H) - p.H : h0;
+  g.h1 = seg ? h1 - p.H : min(h1, p.H);
+  g.in = static_cast<const T*>(seg ? p.k : p.q) + tok * (seg ? p.k_stride : p.q_stride);
+  g.weight = static_cast<const T*>(seg ? p.wk : p.wq);
+  g.ld = p.dh;
+  if (CACHE && seg) {
+    if (spot.page < 0) g.h1 = g.h0;  // nowhere
+    g.out = static_cast<T*>(p.c.K) + (((static_cast<int64_t>(spot.page) * p.c.H) << p.c.shift) + spot.row) * p.dh;
+    g.ld <<= p.c.shift;
+  } else {
+    g.out = static_cast<T*>(seg ? p.k_out : p.q_out) + tok * (seg ? p.ko_stride : p.qo_stride);
+  }
+  return g;
+}
+
+// Heads [h0, h1) of one token's rows (queries first, then keys), a wave's work, where
+// 16-byte pieces lie in one half (or hold whole pairs, IL). A lane has two pieces of a
+// row, in halves those whose elements are pairs, so that half as many lanes as pieces
+// share a row and nothing passes between them but the sum of squares. The factors,
+// cosines and sines times the weights, stay in registers for all heads. Without a norm the
+// results are in every bit the rotation's own, whose order of the two products this
+// keeps. Bound by memory: see k_norm_rotary.
+template <class T, int DH, bool IL, bool CACHE>
+__device__ __forceinline__ void turn_whole(const TurnParams& p, int64_t tok, int h0, int h1, float (*cs)[kMaxPairs]) {
+  constexpr int V = 16 / sizeof(T), U = 2, LPR = DH / V / 2, HS = 64 / LPR;
+  const int lane = threadIdx.x & 63, n = p.n_pairs, hl = lane / LPR, u = lane % LPR;
+  // pieces A and B: a turned unit's, or two of those past the pairs
+  const int np = IL ? 0 : n / V;
+  const int oa = IL ? 2 * u * V : u < np ? u * V : 2 * n + (u - np) * 2 * V, ob = !IL && u < np ? oa + n : oa + V;
   Spot spot = {-1, 0};
   if constexpr (CACHE) spot = spot_of(p, tok);
-  bool first = true;
-  float c[V], s[V];  // of the elements' pairs, s with the sign of the other element's share
-  uint32_t turn = 0;
+  bool first = true, some = false;
+  uint32_t stay = 0;  // pairs that are not turned
 #pragma unroll 1
   for (int seg = 0; seg < 2; ++seg) {
-    const int s0 = seg ? max(h0, p.H) - p.H : h0, s1 = seg ? h1 - p.H : min(h1, p.H);
-    if (s0 >= s1 || (CACHE && seg && spot.page < 0)) continue;
-    const T* in = static_cast<const T*>(seg ? p.k : p.q) + tok * (seg ? p.k_stride : p.q_stride) + e0;
-    T* out;
-    int64_t ld = p.dh;
-    if (CACHE && seg) {
-      out = static_cast<T*>(p.c.K) + (((static_cast<int64_t>(spot.page) * p.c.H) << p.c.shift) + spot.row) * p.dh + e0;
-      ld <<= p.c.shift;
-    } else {
-      out = static_cast<T*>(seg ? p.k_out : p.q_out) + tok * (seg ? p.ko_stride : p.qo_stride) + e0;
-    }
-    const T* weight = static_cast<const T*>(seg ? p.wk : p.wq);
-    float f1[V], f2[V], wt[V];
-    const bool high = !IL && e0 >= n && e0 < 2 * n;  // WHOLE: the lane's piece
+    const Segment<T> g = segment<T, CACHE>(p, tok, seg, h0, h1, spot);
+    if (g.h0 >= g.h1) continue;
+    float ca[V], sa[V], sb[V], cb[V];  // y0 = x0 ca - x1 sb, y1 = x0 sa + x1 cb
     bool fresh = true;
-    for (int hb = s0; hb < s1; hb += hs * U) {
-      u32x4 a[U];
+    for (int hb = g.h0; hb < g.h1; hb += HS * U) {
+      u32x4 a[U], b[U];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const int h = min(hb + i * hs + hl, s1 - 1);
-        a[i] = *reinterpret_cast<const u32x4*>(in + static_cast<int64_t>(h) * p.dh);
+        const T* x = g.in + static_cast<int64_t>(min(hb + i * HS + hl, g.h1 - 1)) * DH;
+        a[i] = *reinterpret_cast<const u32x4*>(x + oa);
+        b[i] = *reinterpret_cast<const u32x4*>(x + ob);
       }
-      if (first) {  // while the first rows are on their way: a pair a lane, then through LDS
+      if (first) {  // while the first rows are on their way
         first = false;
-        if (lane < n) {
-          const int ax = p.axis ? p.axis[lane] : 0;
-          float cc = kStays, ss = 0.f;
-          if (ax < p.n_axes) angle(p.positions[tok * p.n_axes + ax], p.inv_freq[lane], cc, ss);
-          cs[0][lane] = cc;
-          cs[1][lane] = ss;
-        }
-        wave_lds_order();
-#pragma unroll
-        for (int x = 0; x < V; ++x) {
-          const int e = e0 + x, i = IL ? e / 2 : e < n ? e : e - n;
-          const bool in2 = e < 2 * n, on = in2 && cs[0][in2 ? i : 0] != kStays, low = IL ? e % 2 == 0 : e < n;
-          c[x] = on ? cs[0][i] : 1.f;
-          s[x] = on ? (low ? -cs[1][i] : cs[1][i]) : -0.f;
-          turn |= on ? 1u << x : 0u;
-        }
+        put_angles(p, tok, cs);
       }
       if (fresh) {
         fresh = false;
+        stay = 0;
 #pragma unroll
         for (int x = 0; x < V; ++x) {
-          const int e = e0 + x, o = IL ? e ^ 1 : e < n ? e + n : e < 2 * n ? e - n : e;
-          wt[x] = weight ? tof(weight[e]) : 1.f;
-          f1[x] = c[x] * wt[x];
-          f2[x] = s[x] * (weight ? tof(weight[o]) : 1.f);
-          // the pair's first element first
-          if ((IL && WHOLE && x % 2) || (WHOLE && high)) {
-            const float y = f1[x];
-            f1[x] = f2[x];
-            f2[x] = y;
+          const int j = u * V + x;  // the pair, in pairs those of piece A, then B
+          const bool in = IL ? j < n : u < np, on = in && cs[0][in ? j : 0] != kStays;
+          const float c = on ? cs[0][j] : 1.f, s = on ? cs[1][j] : 0.f;
+          stay |= on ? 0u : 1u << x;
+          float w0 = 1.f, w1 = 1.f;
+          if (g.weight) {
+            const int e = IL ? oa + 2 * x : oa + x;
+            w0 = tof(g.weight[e]);
+            w1 = tof(g.weight[IL ? e + 1 : ob + x]);
           }
+          ca[x] = c * w0;
+          sa[x] = s * w0;
+          sb[x] = s * w1;
+          cb[x] = c * w1;
+        }
+        some = __any(stay != 0u);
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = hb + i * HS + hl;
+        float v[2 * V];  // x0, x1 of each pair
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          const T* pa = reinterpret_cast<const T*>(&a[i]);
+          const T* pb = reinterpret_cast<const T*>(&b[i]);
+          if constexpr (IL) {
+            v[2 * x] = tof(x < V / 2 ? pa[2 * x] : pb[2 * x - V]);
+            v[2 * x + 1] = tof(x < V / 2 ? pa[2 * x + 1] : pb[2 * x + 1 - V]);
+          } else {
+            v[2 * x] = tof(pa[x]);
+            v[2 * x + 1] = tof(pb[x]);
+          }
+        }
+        float inv = 1.f;
+        if (g.weight) {
+          float sq = 0.f;
+#pragma unroll
+          for (int x = 0; x < 2 * V; ++x) sq = __builtin_fmaf(v[x], v[x], sq);
+          inv = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
+        }
+        u32x4 ya, yb;
+        T* ta = reinterpret_cast<T*>(&ya);
+        T* tb = reinterpret_cast<T*>(&yb);
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          const float x0 = v[2 * x], x1 = v[2 * x + 1];
+          const float y0 = __builtin_fmaf(x0, ca[x], -(x1 * sb[x])) * inv, y1 = __builtin_fmaf(x0, sa[x], x1 * cb[x]) * inv;
+          if constexpr (IL) {
+            (x < V / 2 ? ta : tb)[2 * x % V] = fromf<T>(y0);
+            (x < V / 2 ? ta : tb)[2 * x % V + 1] = fromf<T>(y1);
+          } else {
+            ta[x] = fromf<T>(y0);
+            tb[x] = fromf<T>(y1);
+          }
+        }
+        if (some) {  // pairs that are not turned: weighted, or kept to the bit
+#pragma unroll
+          for (int x = 0; x < V; ++x) {
+            if (!((stay >> x) & 1u)) continue;
+            const T* pa = reinterpret_cast<const T*>(&a[i]);
+            const T* pb = reinterpret_cast<const T*>(&b[i]);
+            const T k0 = IL ? (x < V / 2 ? pa : pb)[2 * x % V] : pa[x], k1 = IL ? (x < V / 2 ? pa : pb)[2 * x % V + 1] : pb[x];
+            const T y0 = g.weight ? fromf<T>(v[2 * x] * ca[x] * inv) : k0, y1 = g.weight ? fromf<T>(v[2 * x + 1] * cb[x] * inv) : k1;
+            if constexpr (IL) {
+              (x < V / 2 ? ta : tb)[2 * x % V] = y0;
+              (x < V / 2 ? ta : tb)[2 * x % V + 1] = y1;
+            } else {
+              ta[x] = y0;
+              tb[x] = y1;
+            }
+          }
+        }
+        if (h < g.h1) {
+          T* y = g.out + h * g.ld;
+          *reinterpret_cast<u32x4*>(y + oa) = ya;
+          *reinterpret_cast<u32x4*>(y + ob) = yb;
+        }
+      }
+    }
+  }
+}
+
+// The same for any number of pairs. A lane holds one 16-byte piece; in halves the other
+// elements of its pairs lie n behind or before, so the rows of a step go through LDS (with
+// room before and behind them), where a piece that element n cuts takes two reads.
+template <class T, int DH, bool IL, bool CACHE>
+__device__ __forceinline__ void turn_any(const TurnParams& p, int64_t tok, int h0, int h1, char* stage, float (*cs)[kMaxPairs]) {
+  constexpr int V = 16 / sizeof(T), U = 2, LPR = DH / V, HS = 64 / LPR;
+  const int lane = threadIdx.x & 63, n = p.n_pairs, hl = lane / LPR, e0 = lane % LPR * V;
+  Spot spot = {-1, 0};
+  if constexpr (CACHE) spot = spot_of(p, tok);
+  bool first = true;
+  uint32_t turn = 0;  // elements that are turned
+#pragma unroll 1
+  for (int seg = 0; seg < 2; ++seg) {
+    const Segment<T> g = segment<T, CACHE>(p, tok, seg, h0, h1, spot);
+    if (g.h0 >= g.h1) continue;
+    float f1[V], f2[V], wt[V];
+    bool fresh = true;
+    for (int hb = g.h0; hb < g.h1; hb += HS * U) {
+      u32x4 a[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        a[i] = *reinterpret_cast<const u32x4*>(g.in + static_cast<int64_t>(min(hb + i * HS + hl, g.h1 - 1)) * DH + e0);
+      if (first) {
+        first = false;
+        put_angles(p, tok, cs);
+      }
+      if (fresh) {
+        fresh = false;
+        turn = 0;
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          const int e = e0 + x, j = IL ? e / 2 : e < n ? e : e - n, o = IL ? e ^ 1 : e < n ? e + n : e < 2 * n ? e - n : e;
+          const bool in = e < 2 * n, on = in && cs[0][in ? j : 0] != kStays, low = IL ? e % 2 == 0 : e < n;
+          turn |= on ? 1u << x : 0u;
+          wt[x] = g.weight ? tof(g.weight[e]) : 1.f;
+          f1[x] = (on ? cs[0][j] : 1.f) * wt[x];
+          f2[x] = (on ? (low ? -cs[1][j] : cs[1][j]) : 0.f) * (g.weight ? tof(g.weight[o]) : 1.f);
         }
       }
       if constexpr (!IL) {
@@ -109,75 +267,61 @@ __device__ __forceinline__ void turn_rows(const TurnParams& p, int64_t tok, int 
       }
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const int h = hb + i * hs + hl;
-        u32x4 b = a[i];
+        const int h = hb + i * HS + hl;
+        u32x4 b = a[i], d = a[i];
         if constexpr (!IL) {
           const char* me = stage + 16 + (i * 64 + lane) * 16;
           const int off = n * static_cast<int>(sizeof(T));
-          if constexpr (WHOLE) {
-            b = u32x4{0, 0, 0, 0};
-            if (e0 < 2 * n) b = *reinterpret_cast<const u32x4*>(high ? me - off : me + off);
-          } else {
-            u32x4 d = b;
-            if (e0 < n) __builtin_memcpy(&b, me + off, 16);
-            if (e0 + V > n && e0 < 2 * n) __builtin_memcpy(&d, me - off, 16);
-            const T* vb = reinterpret_cast<const T*>(&b);
-            T* vd = reinterpret_cast<T*>(&d);
-#pragma unroll
-            for (int x = 0; x < V; ++x) vd[x] = e0 + x < n ? vb[x] : vd[x];
-            b = d;
-          }
+          if (e0 < n) __builtin_memcpy(&b, me + off, 16);
+          if (e0 + V > n && e0 < 2 * n) __builtin_memcpy(&d, me - off, 16);
         }
         const T* xa = reinterpret_cast<const T*>(&a[i]);
         const T* xb = reinterpret_cast<const T*>(&b);
-        float inv = 1.f;
-        if (weight) {
+        const T* xd = reinterpret_cast<const T*>(&d);
+        float v[V], inv = 1.f;
+#pragma unroll
+        for (int x = 0; x < V; ++x) v[x] = tof(xa[x]);
+        if (g.weight) {
           float sq = 0.f;
 #pragma unroll
-          for (int x = 0; x < V; ++x) sq += tof(xa[x]) * tof(xa[x]);
-          for (int o = 1; o < lpr; o <<= 1) sq += __shfl_xor(sq, o, kWave);
-          inv = __builtin_amdgcn_rsqf(sq / static_cast<float>(p.dh) + p.eps);
-          if (__any(!(sq < __builtin_inff()))) {  // squares past the range, or what is not finite: 2^-64 of the elements
-            float small = 0.f;
-#pragma unroll
-            for (int x = 0; x < V; ++x) {
-              const float y = tof(xa[x]) * 0x1p-64f;
-              small += y * y;
-            }
-            for (int o = 1; o < lpr; o <<= 1) small += __shfl_xor(small, o, kWave);
-            if (!(sq < __builtin_inff())) inv = __builtin_amdgcn_rsqf(small / static_cast<float>(p.dh)) * 0x1p-64f;
-          }
+          for (int x = 0; x < V; ++x) sq = __builtin_fmaf(v[x], v[x], sq);
+          inv = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
         }
         u32x4 y;
         T* vy = reinterpret_cast<T*>(&y);
 #pragma unroll
         for (int x = 0; x < V; ++x) {
-          const float me = tof(xa[x]), other = tof(IL ? xa[x ^ 1] : xb[x]);
-          const bool swap = WHOLE && (IL ? x % 2 == 1 : high);
-          float r = __builtin_fmaf(swap ? other : me, f1[x], (swap ? me : other) * f2[x]);
-          if (!((turn >> x) & 1u)) r = me * wt[x];
-          vy[x] = fromf<T>(weight ? r * inv : r);
-          if (!weight && !((turn >> x) & 1u)) vy[x] = xa[x];
+          const float other = tof(IL ? xa[x ^ 1] : e0 + x < n ? xb[x] : xd[x]);
+          const bool on = (turn >> x) & 1u;
+          const float r = on ? __builtin_fmaf(v[x], f1[x], other * f2[x]) : v[x] * wt[x];
+          vy[x] = on || g.weight ? fromf<T>(r * inv) : xa[x];
         }
-        if (h < s1) *reinterpret_cast<u32x4*>(out + h * ld) = y;
+        if (h < g.h1) *reinterpret_cast<u32x4*>(g.out + h * g.ld + e0) = y;
       }
       wave_lds_order();
     }
   }
 }
 
-constexpr int kStage = 4 * 64 * 16 + 32;  // bytes of a wave's rows in LDS
+constexpr int kStage = 2 * 64 * 16 + 32;  // bytes of a wave's rows in LDS
+template <class T, int DH, bool IL, bool WHOLE, bool CACHE>
+__device__ __forceinline__ void turn_rows(const TurnParams& p, int64_t tok, int h0, int h1, char* stage, float (*cs)[kMaxPairs]) {
+  if constexpr (WHOLE)
+    turn_whole<T, DH, IL, CACHE>(p, tok, h0, h1, cs);
+  else
+    turn_any<T, DH, IL, CACHE>(p, tok, h0, h1, stage, cs);
+}
 
 // A wave turns heads [hw * chunk, ...) of one token.
-template <class T, bool IL, bool WHOLE>
-__global__ __launch_bounds__(256) void k_norm_rotary(TurnParams p, int chunks, int chunk) {
-  __shared__ __attribute__((aligned(16))) char stage[4][kStage];
+template <class T, int DH, bool IL, bool WHOLE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k_norm_rotary(TurnParams p, int chunks, int chunk) {
+  __shared__ __attribute__((aligned(16))) char stage[4][WHOLE ? 16 : kStage];
   __shared__ float cs[4][2][kMaxPairs];
   const int w = threadIdx.x >> 6;
   const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + w, tok = job / chunks;
   if (tok >= static_cast<int64_t>(p.B) * p.T) return;
   const int h0 = static_cast<int>(job % chunks) * chunk;
-  turn_rows<T, IL, WHOLE, false>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), stage[w], cs[w]);
+  turn_rows<T, DH, IL, WHOLE, false>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), stage[w], cs[w]);
 }
 
 // Slots of the kRun tokens from n0 on (tokens of all sequences one after another): behind
@@ -299,7 +443,7 @@ __device__ __forceinline__ void rotate_run(const TurnParams& p, int64_t n0, int 
 // An append. The first `vals` workgroups bring the values of one head and run of tokens,
 // the others turn the rows of queries and keys.
 template <class T, int DH, bool IL, bool WHOLE>
-__global__ __launch_bounds__(256) void k_append_rotary(TurnParams p, int vals, int chunks, int chunk) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 4 : 2))) void k_append_rotary(TurnParams p, int vals, int chunks, int chunk) {
   using L = Values<T, DH>;
   constexpr int ROWS = 4 * kStage + 4 * 2 * kMaxPairs * 4;
   constexpr int META = sizeof(RunMeta) + (256 + kRun + 4) * 4;
@@ -335,7 +479,7 @@ __global__ __launch_bounds__(256) void k_append_rotary(TurnParams p, int vals, i
   const int64_t job = static_cast<int64_t>(blockIdx.x - vals) * 4 + w, tok = job / chunks;
   if (tok >= static_cast<int64_t>(p.B) * p.T) return;
   const int h0 = static_cast<int>(job % chunks) * chunk;
-  turn_rows<T, IL, WHOLE, true>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), smem + w * kStage,
+  turn_rows<T, DH, IL, WHOLE, true>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), smem + w * kStage,
                                 reinterpret_cast<float(*)[kMaxPairs]>(smem + 4 * kStage) + 2 * w);
 }
 
@@ -347,13 +491,13 @@ bool whole(const TurnParams& p) {
   return (p.interleaved ? 2 * p.n_pairs : p.n_pairs) % (16 / static_cast<int>(sizeof(T))) == 0;
 }
 
-template <class T>
+template <class T, int DH>
 void launch(const TurnParams& p, hipStream_t s) {
   const int heads = p.H + p.Hkv;
   const size_t tok = static_cast<size_t>(p.B) * p.T;
   const int chunk = heads_of(tok, heads), chunks = (heads + chunk - 1) / chunk;
-  auto kern = p.interleaved ? (whole<T>(p) ? k_norm_rotary<T, true, true> : k_norm_rotary<T, true, false>)
-                            : (whole<T>(p) ? k_norm_rotary<T, false, true> : k_norm_rotary<T, false, false>);
+  auto kern = p.interleaved ? (whole<T>(p) ? k_norm_rotary<T, DH, true, true> : k_norm_rotary<T, DH, true, false>)
+                            : (whole<T>(p) ? k_norm_rotary<T, DH, false, true> : k_norm_rotary<T, DH, false, false>);
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((tok * chunks + 3) / 4)), dim3(256), 0, s, p, chunks, chunk);
 }
 
@@ -373,9 +517,9 @@ void launch_in(const TurnParams& p, hipStream_t s) {
 
 hipError_t launch_norm_rotary(const TurnParams& p, bool bf16, hipStream_t s) {
   if (bf16)
-    launch<__bf16>(p, s);
+    p.dh == 128 ? launch<__bf16, 128>(p, s) : launch<__bf16, 64>(p, s);
   else
-    launch<float>(p, s);
+    p.dh == 128 ? launch<float, 128>(p, s) : launch<float, 64>(p, s);
   return hipGetLastError();
 }
 
