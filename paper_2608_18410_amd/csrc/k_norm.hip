@@ -107,117 +107,110 @@ __device__ __forceinline__ Segment<T> segment(const TurnParams& p, int64_t tok, 
 // keeps. Bound by memory: see k_norm_rotary.
 template <class T, int DH, bool IL, bool CACHE>
 __device__ __forceinline__ void turn_whole(const TurnParams& p, int64_t tok, int h0, int h1, float (*cs)[kMaxPairs]) {
-  constexpr int V = 16 / sizeof(T), U = 2, LPR = DH / V / 2, HS = 64 / LPR;
+  constexpr int V = 16 / sizeof(T), LPR = DH / V / 2, HS = 64 / LPR;
   const int lane = threadIdx.x & 63, n = p.n_pairs, hl = lane / LPR, u = lane % LPR;
   // pieces A and B: a turned unit's, or two of those past the pairs
   const int np = IL ? 0 : n / V;
   const int oa = IL ? 2 * u * V : u < np ? u * V : 2 * n + (u - np) * 2 * V, ob = !IL && u < np ? oa + n : oa + V;
   Spot spot = {-1, 0};
   if constexpr (CACHE) spot = spot_of(p, tok);
-  bool first = true, some = false;
-  uint32_t stay = 0;  // pairs that are not turned
+  const Segment<T> gq = segment<T, CACHE>(p, tok, 0, h0, h1, spot), gk = segment<T, CACHE>(p, tok, 1, h0, h1, spot);
+  // steps of HS heads, those of the queries first; a step's rows are asked for two before
+  const int nq = max(gq.h1 - gq.h0 + HS - 1, 0) / HS, steps = nq + max(gk.h1 - gk.h0 + HS - 1, 0) / HS;
+  u32x4 a, b, a1, b1, a2, b2;
+  auto request = [&](int st, u32x4& x, u32x4& y) {
+    if (st >= steps) return;
+    const T* in = st < nq ? gq.in : gk.in;
+    const int h = st < nq ? min(gq.h0 + st * HS + hl, gq.h1 - 1) : min(gk.h0 + (st - nq) * HS + hl, gk.h1 - 1);
+    x = *reinterpret_cast<const u32x4*>(in + static_cast<int64_t>(h) * DH + oa);
+    y = *reinterpret_cast<const u32x4*>(in + static_cast<int64_t>(h) * DH + ob);
+  };
+  request(0, a, b);
+  request(1, a1, b1);
+  put_angles(p, tok, cs);
+  bool some = false;
+  uint32_t stay = 0;                   // pairs that are not turned
+  float ca[V], sa[V], sb[V], cb[V];    // y0 = x0 ca - x1 sb, y1 = x0 sa + x1 cb
 #pragma unroll 1
-  for (int seg = 0; seg < 2; ++seg) {
-    const Segment<T> g = segment<T, CACHE>(p, tok, seg, h0, h1, spot);
-    if (g.h0 >= g.h1) continue;
-    float ca[V], sa[V], sb[V], cb[V];  // y0 = x0 ca - x1 sb, y1 = x0 sa + x1 cb
-    bool fresh = true;
-    for (int hb = g.h0; hb < g.h1; hb += HS * U) {
-      u32x4 a[U], b[U];
+  for (int st = 0; st < steps; ++st) {
+    const Segment<T>& g = st < nq ? gq : gk;
+    request(st + 2, a2, b2);
+    if (st == 0 || st == nq) {
+      stay = 0;
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const T* x = g.in + static_cast<int64_t>(min(hb + i * HS + hl, g.h1 - 1)) * DH;
-        a[i] = *reinterpret_cast<const u32x4*>(x + oa);
-        b[i] = *reinterpret_cast<const u32x4*>(x + ob);
-      }
-      if (first) {  // while the first rows are on their way
-        first = false;
-        put_angles(p, tok, cs);
-      }
-      if (fresh) {
-        fresh = false;
-        stay = 0;
-#pragma unroll
-        for (int x = 0; x < V; ++x) {
-          const int j = u * V + x;  // the pair, in pairs those of piece A, then B
-          const bool in = IL ? j < n : u < np, on = in && cs[0][in ? j : 0] != kStays;
-          const float c = on ? cs[0][j] : 1.f, s = on ? cs[1][j] : 0.f;
-          stay |= on ? 0u : 1u << x;
-          float w0 = 1.f, w1 = 1.f;
-          if (g.weight) {
-            const int e = IL ? oa + 2 * x : oa + x;
-            w0 = tof(g.weight[e]);
-            w1 = tof(g.weight[IL ? e + 1 : ob + x]);
-          }
-          ca[x] = c * w0;
-          sa[x] = s * w0;
-          sb[x] = s * w1;
-          cb[x] = c * w1;
-        }
-        some = __any(stay != 0u);
-      }
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int h = hb + i * HS + hl;
-        float v[2 * V];  // x0, x1 of each pair
-#pragma unroll
-        for (int x = 0; x < V; ++x) {
-          const T* pa = reinterpret_cast<const T*>(&a[i]);
-          const T* pb = reinterpret_cast<const T*>(&b[i]);
-          if constexpr (IL) {
-            v[2 * x] = tof(x < V / 2 ? pa[2 * x] : pb[2 * x - V]);
-            v[2 * x + 1] = tof(x < V / 2 ? pa[2 * x + 1] : pb[2 * x + 1 - V]);
-          } else {
-            v[2 * x] = tof(pa[x]);
-            v[2 * x + 1] = tof(pb[x]);
-          }
-        }
-        float inv = 1.f;
+      for (int x = 0; x < V; ++x) {
+        const int j = u * V + x;  // the pair, in pairs those of piece A, then B
+        const bool in = IL ? j < n : u < np, on = in && cs[0][in ? j : 0] != kStays;
+        const float c = on ? cs[0][j] : 1.f, s = on ? cs[1][j] : 0.f;
+        stay |= on ? 0u : 1u << x;
+        float w0 = 1.f, w1 = 1.f;
         if (g.weight) {
-          float sq = 0.f;
+          const int e = IL ? oa + 2 * x : oa + x;
+          w0 = tof(g.weight[e]);
+          w1 = tof(g.weight[IL ? e + 1 : ob + x]);
+        }
+        ca[x] = c * w0;
+        sa[x] = s * w0;
+        sb[x] = s * w1;
+        cb[x] = c * w1;
+      }
+      some = __any(stay != 0u);
+    }
+    const int h = st < nq ? gq.h0 + st * HS + hl : gk.h0 + (st - nq) * HS + hl;
+    float v[2 * V];  // x0, x1 of each pair
 #pragma unroll
-          for (int x = 0; x < 2 * V; ++x) sq = __builtin_fmaf(v[x], v[x], sq);
-          inv = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
-        }
-        u32x4 ya, yb;
-        T* ta = reinterpret_cast<T*>(&ya);
-        T* tb = reinterpret_cast<T*>(&yb);
-#pragma unroll
-        for (int x = 0; x < V; ++x) {
-          const float x0 = v[2 * x], x1 = v[2 * x + 1];
-          const float y0 = __builtin_fmaf(x0, ca[x], -(x1 * sb[x])) * inv, y1 = __builtin_fmaf(x0, sa[x], x1 * cb[x]) * inv;
-          if constexpr (IL) {
-            (x < V / 2 ? ta : tb)[2 * x % V] = fromf<T>(y0);
-            (x < V / 2 ? ta : tb)[2 * x % V + 1] = fromf<T>(y1);
-          } else {
-            ta[x] = fromf<T>(y0);
-            tb[x] = fromf<T>(y1);
-          }
-        }
-        if (some) {  // pairs that are not turned: weighted, or kept to the bit
-#pragma unroll
-          for (int x = 0; x < V; ++x) {
-            if (!((stay >> x) & 1u)) continue;
-            const T* pa = reinterpret_cast<const T*>(&a[i]);
-            const T* pb = reinterpret_cast<const T*>(&b[i]);
-            const T k0 = IL ? (x < V / 2 ? pa : pb)[2 * x % V] : pa[x], k1 = IL ? (x < V / 2 ? pa : pb)[2 * x % V + 1] : pb[x];
-            const T y0 = g.weight ? fromf<T>(v[2 * x] * ca[x] * inv) : k0, y1 = g.weight ? fromf<T>(v[2 * x + 1] * cb[x] * inv) : k1;
-            if constexpr (IL) {
-              (x < V / 2 ? ta : tb)[2 * x % V] = y0;
-              (x < V / 2 ? ta : tb)[2 * x % V + 1] = y1;
-            } else {
-              ta[x] = y0;
-              tb[x] = y1;
-            }
-          }
-        }
-        if (h < g.h1) {
-          T* y = g.out + h * g.ld;
-          *reinterpret_cast<u32x4*>(y + oa) = ya;
-          *reinterpret_cast<u32x4*>(y + ob) = yb;
-        }
+    for (int x = 0; x < V; ++x) {
+      const T* pa = reinterpret_cast<const T*>(&a);
+      const T* pb = reinterpret_cast<const T*>(&b);
+      if constexpr (IL) {
+        v[2 * x] = tof(x < V / 2 ? pa[2 * x] : pb[2 * x - V]);
+        v[2 * x + 1] = tof(x < V / 2 ? pa[2 * x + 1] : pb[2 * x + 1 - V]);
+      } else {
+        v[2 * x] = tof(pa[x]);
+        v[2 * x + 1] = tof(pb[x]);
       }
     }
+    float inv = 1.f;
+    if (g.weight) {
+      float sq = 0.f;
+#pragma unroll
+      for (int x = 0; x < 2 * V; ++x) sq = __builtin_fmaf(v[x], v[x], sq);
+      inv = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
+    }
+    float y[2 * V];
+#pragma unroll
+    for (int x = 0; x < V; ++x) {
+      y[2 * x] = __builtin_fmaf(v[2 * x], ca[x], -(v[2 * x + 1] * sb[x])) * inv;
+      y[2 * x + 1] = __builtin_fmaf(v[2 * x], sa[x], v[2 * x + 1] * cb[x]) * inv;
+    }
+    if (some) {  // pairs that are not turned (a zero times what is not finite would reach the other)
+#pragma unroll
+      for (int x = 0; x < V; ++x) {
+        const bool on = !((stay >> x) & 1u);
+        y[2 * x] = on ? y[2 * x] : v[2 * x] * ca[x] * inv;
+        y[2 * x + 1] = on ? y[2 * x + 1] : v[2 * x + 1] * cb[x] * inv;
+      }
+    }
+    u32x4 ya, yb;
+    T* ta = reinterpret_cast<T*>(&ya);
+    T* tb = reinterpret_cast<T*>(&yb);
+#pragma unroll
+    for (int x = 0; x < V; ++x) {
+      if constexpr (IL) {
+        (x < V / 2 ? ta : tb)[2 * x % V] = fromf<T>(y[2 * x]);
+        (x < V / 2 ? ta : tb)[2 * x % V + 1] = fromf<T>(y[2 * x + 1]);
+      } else {
+        ta[x] = fromf<T>(y[2 * x]);
+        tb[x] = fromf<T>(y[2 * x + 1]);
+      }
+    }
+    if (h < g.h1) {
+      T* to = g.out + h * g.ld;
+      *reinterpret_cast<u32x4*>(to + oa) = ya;
+      *reinterpret_cast<u32x4*>(to + ob) = yb;
+    }
+    a = a1, b = b1;
+    a1 = a2, b1 = b2;
   }
 }
 
