@@ -13,18 +13,29 @@
 namespace rolesub {
 namespace {
 
-// Where a call's new token (b, j) goes in the cache.
+// Where a call's new token goes in the cache: first its place in the sequence, then (a
+// load later, which other work can cover) its page.
 struct Spot {
   int page, row;  // -1: nowhere
 };
-__device__ __forceinline__ Spot spot_of(const TurnParams& p, int64_t tok) {
+struct Place {
+  unsigned b;
+  int64_t t;  // -1: nowhere
+};
+__device__ __forceinline__ Place place_of(const TurnParams& p, int64_t tok) {
   const PagedCache& c = p.c;
-  const int b = static_cast<int>(tok / p.T), j = static_cast<int>(tok % p.T);
+  const unsigned b = static_cast<unsigned>(tok) / static_cast<unsigned>(p.T);  // fewer than 2^31 tokens
+  const int j = static_cast<int>(static_cast<unsigned>(tok) - b * static_cast<unsigned>(p.T));
   const int64_t cap = static_cast<int64_t>(p.max_pages) << c.shift;
+  const int n = p.n_new ? p.n_new[b] : p.T;
   const int64_t t = min(static_cast<int64_t>(max(p.lens[b], 0)), cap) + j;
-  if (t >= cap || (p.n_new && j >= p.n_new[b])) return Spot{-1, 0};
-  const int page = p.table[static_cast<int64_t>(b) * p.max_pages + (t >> c.shift)];
-  return Spot{static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages) ? page : -1, static_cast<int>(t & (c.page - 1))};
+  return Place{b, t < cap && j < n ? t : -1};
+}
+__device__ __forceinline__ Spot spot_of(const TurnParams& p, const Place& x) {
+  const PagedCache& c = p.c;
+  if (x.t < 0) return Spot{-1, 0};
+  const int page = p.table[static_cast<int64_t>(x.b) * p.max_pages + (x.t >> c.shift)];
+  return Spot{static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages) ? page : -1, static_cast<int>(x.t & (c.page - 1))};
 }
 
 // Sum over the LPR lanes of a row, the same bits in all of them.
@@ -112,11 +123,11 @@ __device__ __forceinline__ void turn_whole(const TurnParams& p, int64_t tok, int
   // pieces A and B: a turned unit's, or two of those past the pairs
   const int np = IL ? 0 : n / V;
   const int oa = IL ? 2 * u * V : u < np ? u * V : 2 * n + (u - np) * 2 * V, ob = !IL && u < np ? oa + n : oa + V;
-  Spot spot = {-1, 0};
-  if constexpr (CACHE) spot = spot_of(p, tok);
-  const Segment<T> gq = segment<T, CACHE>(p, tok, 0, h0, h1, spot), gk = segment<T, CACHE>(p, tok, 1, h0, h1, spot);
+  const Segment<T> gq = segment<T, false>(p, tok, 0, h0, h1, Spot{-1, 0});
+  Segment<T> gk = segment<T, false>(p, tok, 1, h0, h1, Spot{-1, 0});
   // steps of HS heads, those of the queries first; a step's rows are asked for two before
-  const int nq = max(gq.h1 - gq.h0 + HS - 1, 0) / HS, steps = nq + max(gk.h1 - gk.h0 + HS - 1, 0) / HS;
+  const int nq = max(gq.h1 - gq.h0 + HS - 1, 0) / HS;
+  int steps = nq;
   u32x4 a, b, a1, b1, a2, b2;
   auto request = [&](int st, u32x4& x, u32x4& y) {
     if (st >= steps) return;
@@ -127,7 +138,16 @@ __device__ __forceinline__ void turn_whole(const TurnParams& p, int64_t tok, int
   };
   request(0, a, b);
   request(1, a1, b1);
-  put_angles(p, tok, cs);
+  if constexpr (CACHE) {
+    const Place at = place_of(p, tok);
+    put_angles(p, tok, cs);
+    gk = segment<T, true>(p, tok, 1, h0, h1, spot_of(p, at));
+  } else {
+    put_angles(p, tok, cs);
+  }
+  steps += max(gk.h1 - gk.h0 + HS - 1, 0) / HS;
+  if (nq == 0) request(0, a, b);
+  if (nq <= 1) request(1, a1, b1);
   bool some = false;
   uint32_t stay = 0;                   // pairs that are not turned
   float ca[V], sa[V], sb[V], cb[V];    // y0 = x0 ca - x1 sb, y1 = x0 sa + x1 cb
@@ -222,7 +242,7 @@ __device__ __forceinline__ void turn_any(const TurnParams& p, int64_t tok, int h
   constexpr int V = 16 / sizeof(T), U = 2, LPR = DH / V, HS = 64 / LPR;
   const int lane = threadIdx.x & 63, n = p.n_pairs, hl = lane / LPR, e0 = lane % LPR * V;
   Spot spot = {-1, 0};
-  if constexpr (CACHE) spot = spot_of(p, tok);
+  if constexpr (CACHE) spot = spot_of(p, place_of(p, tok));
   bool first = true;
   uint32_t turn = 0;  // elements that are turned
 #pragma unroll 1
@@ -311,66 +331,74 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k
   __shared__ __attribute__((aligned(16))) char stage[4][WHOLE ? 16 : kStage];
   __shared__ float cs[4][2][kMaxPairs];
   const int w = threadIdx.x >> 6;
-  const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + w, tok = job / chunks;
-  if (tok >= static_cast<int64_t>(p.B) * p.T) return;
-  const int h0 = static_cast<int>(job % chunks) * chunk;
+  const unsigned job = blockIdx.x * 4 + w, tok = job / static_cast<unsigned>(chunks);  // fewer than 2^26
+  if (tok >= static_cast<unsigned>(p.B) * static_cast<unsigned>(p.T)) return;
+  const int h0 = static_cast<int>(job - tok * static_cast<unsigned>(chunks)) * chunk;
   turn_rows<T, DH, IL, WHOLE, false>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), stage[w], cs[w]);
 }
 
-// Slots of the kRun tokens from n0 on (tokens of all sequences one after another): behind
-// their page-mates, by an exclusive sum over the run and the 255 tokens before it.
-constexpr int kRun = 64;
+// Slots of the `run` tokens from n0 on (tokens of all sequences one after another): behind
+// their page-mates, by an exclusive sum over the run and the 256 tokens before it. False
+// if none of them goes anywhere.
+constexpr int kRun = 128;
 struct RunMeta {
-  int64_t page[kRun];  // -1: dropped
+  int page[kRun];  // -1: dropped
   uint32_t mask[kRun];
   int slot[kRun];
+  int sum[256 + kRun], wsum[4], any;
 };
-__device__ __forceinline__ void run_meta(const TurnParams& p, int64_t n0, int h, RunMeta& m, int* s_sum, int* wsum) {
+template <class F>
+__device__ __forceinline__ bool run_meta(const TurnParams& p, int64_t n0, int run, int h, RunMeta& m, F meanwhile) {
   const PagedCache& c = p.c;
   const int tid = threadIdx.x;
-  const int64_t all = static_cast<int64_t>(p.B) * p.T, w0 = n0 - 256;  // the window: 256 + 64 tokens, two a thread
+  const int64_t all = static_cast<int64_t>(p.B) * p.T, w0 = n0 - 256, tok = min(n0 + tid, all - 1);
   const uint32_t gm = group_bits(c.G);
-  int cnt[2];
+  uint32_t mk[2];  // of the window, two tokens a thread
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const int64_t t = w0 + 2 * tid + x;
-    cnt[x] = 2 * tid + x < 256 + kRun && t >= 0 && t < all ? __popc(p.mask[t] & gm) : 0;
+    mk[x] = 2 * tid + x < 256 + run && t >= 0 && t < all ? p.mask[t] & gm : 0u;
   }
-  const int before = group_scan<256, false>(cnt[0] + cnt[1], wsum);
-  if (tid < (256 + kRun) / 2) {
-    s_sum[2 * tid] = before;
-    s_sum[2 * tid + 1] = before + cnt[0];
+  const uint32_t whole = p.mask[tok];
+  Spot s = spot_of(p, place_of(p, tok));
+  if (tid >= run || n0 + tid >= all) s.page = -1;
+  meanwhile();
+  const int j = static_cast<int>(static_cast<unsigned>(tok) % static_cast<unsigned>(p.T));
+  const int64_t meta = (static_cast<int64_t>(s.page) << c.shift) + s.row;
+  int used = 0;
+  if (s.page >= 0 && s.row > j) used = c.slot[meta - j - 1] + __popc(c.mask[meta - j - 1] & gm);
+  if (tid == 0) m.any = 0;
+  const int cnt = __popc(mk[0]), before = group_scan<256, false>(cnt + __popc(mk[1]), m.wsum);
+  if (tid < (256 + run) / 2) {
+    m.sum[2 * tid] = before;
+    m.sum[2 * tid + 1] = before + cnt;
   }
   __syncthreads();
-  if (tid < kRun) {
-    const int64_t tok = n0 + tid;
-    Spot s = {-1, 0};
-    if (tok < all) s = spot_of(p, tok);
+  if (tid < run) {
     m.page[tid] = s.page;
     if (s.page >= 0) {
-      const int j = static_cast<int>(tok % p.T), mates = min(s.row, j);  // new ones before it in its page
-      int used = s_sum[256 + tid] - s_sum[256 + tid - mates];
-      const int64_t meta = static_cast<int64_t>(s.page) << c.shift;
-      if (s.row > j) used += c.slot[meta + s.row - j - 1] + __popc(c.mask[meta + s.row - j - 1] & gm);
-      const uint32_t whole = p.mask[tok];
+      m.any = 1;
+      const int mates = min(s.row, j);  // new ones before it in its page
+      used += m.sum[256 + tid] - m.sum[256 + tid - mates];
       m.mask[tid] = whole & gm;
       m.slot[tid] = used;
       if (h == 0) {
-        c.mask[meta + s.row] = whole;
-        c.slot[meta + s.row] = used;
+        c.mask[meta] = whole;
+        c.slot[meta] = used;
       }
     }
   }
   __syncthreads();
+  return m.any != 0;
 }
 
 // Four dims of a rotated value from dim d on into the groups that keep them.
 template <class T>
-__device__ __forceinline__ void put_dims(const PagedCache& c, int64_t page, int h, uint32_t mask, int slot, int d, f32x4 z) {
+__device__ __forceinline__ void put_dims(const PagedCache& c, int page, int h, uint32_t mask, int slot, int d, f32x4 z) {
   T v[4];
 #pragma unroll
   for (int x = 0; x < 4; ++x) v[x] = fromf<T>(z[x]);
-  T* base = static_cast<T*>(c.V) + (page * c.H + h) * c.vcap * static_cast<int64_t>(c.ds);
+  T* base = static_cast<T*>(c.V) + (static_cast<int64_t>(page) * c.H + h) * c.vcap * c.ds;
   auto at = [&](int g) {  // of group g, or null
     const uint32_t sl = static_cast<uint32_t>(slot) + __popc(mask & ((1u << g) - 1u));
     return ((mask >> g) & 1u) && sl < static_cast<uint32_t>(c.vcap) ? base + static_cast<int64_t>(sl) * c.ds : nullptr;
@@ -395,72 +423,86 @@ struct Values {
   static constexpr int EP = 16 / sizeof(T), ROWB = DH * sizeof(T), KS = ROWB / 64, MB = DH / 16;
   static constexpr int LD = ROWB + (kBf16 ? 32 : 16), BYTES = DH * LD;
 };
-template <class T, int DH>
-__device__ __forceinline__ void rotate_run(const TurnParams& p, int64_t n0, int h, const RunMeta& m, const char* R) {
+template <class T, int DH, class Load>
+__device__ __forceinline__ void rotate_run(const TurnParams& p, int64_t n0, int run, int h, const RunMeta& m, const char* R,
+                                           u32x4 (&vf)[Values<T, DH>::KS], Load load) {
   using L = Values<T, DH>;
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   typedef s16x4 __attribute__((address_space(3))) * p3;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4, i = 16 * w + l16;
-  const int64_t all = static_cast<int64_t>(p.B) * p.T, tok = min(n0 + i, all - 1);
-  const T* v = static_cast<const T*>(p.v) + tok * p.v_stride + static_cast<int64_t>(h) * DH + g4 * L::EP;
-  u32x4 vf[L::KS];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
+#pragma unroll 1
+  for (int t = 16 * w; t < run; t += 64) {
+    f32x4 z[L::MB];
 #pragma unroll
-  for (int j = 0; j < L::KS; ++j) vf[j] = *reinterpret_cast<const u32x4*>(v + 4 * j * L::EP);
-  f32x4 z[L::MB];
+    for (int mb = 0; mb < L::MB; ++mb) z[mb] = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int mb = 0; mb < L::MB; ++mb) z[mb] = f32x4{0, 0, 0, 0};
+    for (int j = 0; j < L::KS; ++j)
 #pragma unroll
-  for (int j = 0; j < L::KS; ++j)
+      for (int mb = 0; mb < L::MB; ++mb) {
+        if constexpr (L::kBf16) {
+          const char* r = R + (32 * j + 8 * g4 + l16 / 4) * L::LD + 8 * (l16 % 4) + 32 * mb;
+          const bf16x4 a0 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)(r)));
+          const bf16x4 a1 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)(r + 4 * L::LD)));
+          z[mb] = mfma_16x16x32(__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(bf16x8, vf[j]), z[mb]);
+        } else {
+          const f32x4 x = __builtin_bit_cast(f32x4, vf[j]);
 #pragma unroll
-    for (int mb = 0; mb < L::MB; ++mb) {
-      if constexpr (L::kBf16) {
-        const char* r = R + (32 * j + 8 * g4 + l16 / 4) * L::LD + 8 * (l16 % 4) + 32 * mb;
-        const bf16x4 a0 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)(r)));
-        const bf16x4 a1 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)(r + 4 * L::LD)));
-        z[mb] = mfma_16x16x32(__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(bf16x8, vf[j]), z[mb]);
-      } else {
-        const f32x4 x = __builtin_bit_cast(f32x4, vf[j]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float a = *reinterpret_cast<const float*>(R + (16 * j + 4 * g4 + k) * L::LD + 4 * (16 * mb + l16));
-          z[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, x[k], z[mb], 0, 0, 0);
+          for (int k = 0; k < 4; ++k) {
+            const float a = *reinterpret_cast<const float*>(R + (16 * j + 4 * g4 + k) * L::LD + 4 * (16 * mb + l16));
+            z[mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, x[k], z[mb], 0, 0, 0);
+          }
         }
       }
-    }
-  settle(z);
-  if (m.page[i] < 0) return;
+    settle(z);
+    if (t + 64 < run) load(t + 64);
+    const int i = t + l16, page = m.page[i];
+    if (page < 0) continue;
 #pragma unroll
-  for (int mb = 0; mb < L::MB; ++mb) put_dims<T>(p.c, m.page[i], h, m.mask[i], m.slot[i], 16 * mb + 4 * g4, z[mb]);
+    for (int mb = 0; mb < L::MB; ++mb) put_dims<T>(p.c, page, h, m.mask[i], m.slot[i], 16 * mb + 4 * g4, z[mb]);
+  }
 }
 
-// An append. The first `vals` workgroups bring the values of one head and run of tokens,
-// the others turn the rows of queries and keys.
+// An append. `vals` of the workgroups, spread evenly among them, bring the values of one
+// head and run of tokens, the others turn the rows of queries and keys: the former wait for
+// R_h and the masks, the latter for memory, and both are on the chip at once.
 template <class T, int DH, bool IL, bool WHOLE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 4 : 2))) void k_append_rotary(TurnParams p, int vals, int chunks, int chunk) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 4 : 2))) void k_append_rotary(TurnParams p, unsigned vals, int run, int chunks, int chunk) {
   using L = Values<T, DH>;
-  constexpr int ROWS = 4 * kStage + 4 * 2 * kMaxPairs * 4;
-  constexpr int META = sizeof(RunMeta) + (256 + kRun + 4) * 4;
+  constexpr int ROWS = (WHOLE ? 0 : 4 * kStage) + 4 * 2 * kMaxPairs * 4, META = sizeof(RunMeta);
   __shared__ __attribute__((aligned(16))) char smem[ROWS > L::BYTES + META ? ROWS : L::BYTES + META];
   const int tid = threadIdx.x, w = tid >> 6;
-  if (static_cast<int>(blockIdx.x) < vals) {
-    const int h = blockIdx.x % p.c.H;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x / p.c.H) * kRun;
+  const unsigned x = blockIdx.x, vi = static_cast<unsigned>(static_cast<uint64_t>(x) * vals / gridDim.x);
+  if (static_cast<unsigned>(static_cast<uint64_t>(x + 1) * vals / gridDim.x) > vi) {
+    const int h = static_cast<int>(vi % p.c.H);
+    const int64_t n0 = static_cast<int64_t>(vi / p.c.H) * run;
     RunMeta& m = *reinterpret_cast<RunMeta*>(smem + L::BYTES);
-    int* s_sum = reinterpret_cast<int*>(smem + L::BYTES + sizeof(RunMeta));
-    int* wsum = s_sum + 256 + kRun;
     if (p.Rm) {
       constexpr int PP = L::ROWB / 16, N = DH * PP / 256;
       const char* R = static_cast<const char*>(p.Rm) + static_cast<int64_t>(h) * DH * L::ROWB;
+      const int64_t last = static_cast<int64_t>(p.B) * p.T - 1;
+      u32x4 vf[L::KS], rf[N];
+      auto load = [&](int t) {  // this lane's part of its tile's values
+        const T* v = static_cast<const T*>(p.v) + min(n0 + t + (tid & 15), last) * p.v_stride + static_cast<int64_t>(h) * DH +
+                     (tid & 63) / 16 * L::EP;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int u = tid + 256 * i;
-        *reinterpret_cast<u32x4*>(smem + u / PP * L::LD + u % PP * 16) = *reinterpret_cast<const u32x4*>(R + u * 16);
-      }
-      run_meta(p, n0, h, m, s_sum, wsum);
-      rotate_run<T, DH>(p, n0, h, m, smem);
+        for (int j = 0; j < L::KS; ++j) vf[j] = *reinterpret_cast<const u32x4*>(v + 4 * j * L::EP);
+      };
+#pragma unroll
+      for (int i = 0; i < N; ++i) rf[i] = *reinterpret_cast<const u32x4*>(R + (tid + 256 * i) * 16);
+      load(16 * w);
+      // R_h goes to LDS while the places are on their way
+      const bool any = run_meta(p, n0, run, h, m, [&] {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int u = tid + 256 * i;
+          *reinterpret_cast<u32x4*>(smem + u / PP * L::LD + u % PP * 16) = rf[i];
+        }
+      });
+      if (!any) return;
+      rotate_run<T, DH>(p, n0, run, h, m, smem, vf, load);
     } else {
-      run_meta(p, n0, h, m, s_sum, wsum);
-      for (int u = tid; u < kRun * (DH / 4); u += 256) {
+      if (!run_meta(p, n0, run, h, m, [] {})) return;
+      for (int u = tid; u < run * (DH / 4); u += 256) {
         const int i = u / (DH / 4), d = u % (DH / 4) * 4;
         if (m.page[i] < 0) continue;
         const T* v = static_cast<const T*>(p.v) + (n0 + i) * p.v_stride + static_cast<int64_t>(h) * DH + d;
@@ -469,11 +511,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
     }
     return;
   }
-  const int64_t job = static_cast<int64_t>(blockIdx.x - vals) * 4 + w, tok = job / chunks;
-  if (tok >= static_cast<int64_t>(p.B) * p.T) return;
-  const int h0 = static_cast<int>(job % chunks) * chunk;
-  turn_rows<T, DH, IL, WHOLE, true>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), smem + w * kStage,
-                                reinterpret_cast<float(*)[kMaxPairs]>(smem + 4 * kStage) + 2 * w);
+  const unsigned job = (x - vi) * 4 + w, tok = job / static_cast<unsigned>(chunks);
+  if (tok >= static_cast<unsigned>(p.B) * static_cast<unsigned>(p.T)) return;
+  const int h0 = static_cast<int>(job - tok * static_cast<unsigned>(chunks)) * chunk;
+  turn_rows<T, DH, IL, WHOLE, true>(p, tok, h0, min(h0 + chunk, p.H + p.Hkv), smem + (WHOLE ? 0 : w * kStage),
+                                    reinterpret_cast<float(*)[kMaxPairs]>(smem + (WHOLE ? 0 : 4 * kStage)) + 2 * w);
 }
 
 // Heads of a wave, as the rotation's kernels choose.
@@ -499,11 +541,14 @@ void launch_in(const TurnParams& p, hipStream_t s) {
   const int heads = p.H + p.Hkv;
   const size_t tok = static_cast<size_t>(p.B) * p.T;
   const int chunk = heads_of(tok, heads), chunks = (heads + chunk - 1) / chunk;
-  const size_t vals = (tok + kRun - 1) / kRun * p.c.H;
+  // runs of 128 tokens, which read R_h half as often, where 64 would make four
+  // workgroups a CU and more
+  const int run = (tok + 63) / 64 * p.c.H > 1024 ? kRun : 64;
+  const size_t vals = (tok + run - 1) / run * p.c.H;
   auto kern = p.interleaved ? (whole<T>(p) ? k_append_rotary<T, DH, true, true> : k_append_rotary<T, DH, true, false>)
                             : (whole<T>(p) ? k_append_rotary<T, DH, false, true> : k_append_rotary<T, DH, false, false>);
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(vals + (tok * chunks + 3) / 4)), dim3(256), 0, s, p, static_cast<int>(vals),
-                     chunks, chunk);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(vals + (tok * chunks + 3) / 4)), dim3(256), 0, s, p, static_cast<unsigned>(vals),
+                     run, chunks, chunk);
 }
 
 }  // namespace
