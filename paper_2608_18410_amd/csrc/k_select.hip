@@ -1,6 +1,7 @@
 // Few pages of a long history: the bounds of each page's keys, and the scores that pages
 // are chosen by for each query.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "launch.hpp"
@@ -63,101 +64,100 @@ __global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
   *reinterpret_cast<u32x4*>(static_cast<char*>(p.bounds) + head * 2 * DH * sizeof(T) + lane * 16) = out;
 }
 
-// Scores of 64 pages of one key head for the rows of a sequence: the highest that a key
-// within the bounds could have, sum_d (q < 0 ? q lo : q hi) = sum_d (q- lo + q+ hi), summed in
-// 64 bits (the products are exact there) and rounded once, so that the choice does not
-// hang on the order of the sum. A page a lane, a quarter of the dims a wave; the queries'
-// parts come from LDS, the same for all lanes.
-template <class T, int DH, int RC>
+// Sum over the LPR lanes of a row, the same bits in all of them.
+template <int LPR>
+__device__ __forceinline__ double row_sum(double x) {
+  auto other = [](double y, auto ctrl) {
+    const u32x2 v = __builtin_bit_cast(u32x2, y);
+    u32x2 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r[i] = __builtin_amdgcn_update_dpp(0, v[i], decltype(ctrl)::value, 0xF, 0xF, true);
+    return __builtin_bit_cast(double, r);
+  };
+  x += other(x, std::integral_constant<int, 0xB1>{});                            // lanes 1 apart
+  x += other(x, std::integral_constant<int, 0x4E>{});                            // 2 apart
+  x += other(x, std::integral_constant<int, 0x141>{});                           // the other half of 8
+  if constexpr (LPR >= 16) x += other(x, std::integral_constant<int, 0x140>{});  // the other half of 16
+  if constexpr (LPR >= 32) x += __shfl_xor(x, 16, kWave);
+  return x;
+}
+
+// Scores of a few pages of one key head for a sequence's queries, a wave's work: the
+// highest that a key within the bounds could have, sum_d (q < 0 ? q lo : q hi), summed in
+// 64 bits and rounded once, so that the choice does not hang on the order of the sum. A
+// lane has a 16-byte piece of both bounds of a page, and its part of RC queries in 64
+// bits; the lanes of a page add up. All bounds of a wave are asked for at once. Bound by
+// memory: 8 sequences of 110001 to 131071 tokens, pages of 64 and 8 key heads of 4 rows (62 MB).
+template <class T, int DH>
 __global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
-  constexpr int V = 16 / sizeof(T), ROWB = 2 * DH * sizeof(T), LD = ROWB + 16, QD = DH / 4;
-  __shared__ __attribute__((aligned(16))) char s_b[64 * LD];
-  __shared__ __attribute__((aligned(16))) double s_q[RC][2][DH];
-  __shared__ double s_sum[4][RC][64];
+  constexpr int V = 16 / sizeof(T), LPR = DH / V, PS = 64 / LPR, U = 4, RC = 4;  // pages of a step, steps, rows at a time
   const PagedCache& c = p.c;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), d0 = lane % LPR * V;
   int lin = blockIdx.x;
-  const int i0 = lin % np * 64;
+  const int i0 = (lin % np * 4 + w) * PS * U;
   lin /= np;
   const int h = lin % c.H, b = lin / c.H;
   const int32_t* table = p.table + static_cast<int64_t>(b) * p.max_pages;
   const int64_t len = min(min(static_cast<int64_t>(max(p.lens[b], 0)), static_cast<int64_t>(p.max_len)),
                           static_cast<int64_t>(p.max_pages) << c.shift);
-  auto pages_of = [&](int j) {
-    const int64_t n = p.visible ? min(len, static_cast<int64_t>(max(p.visible[static_cast<int64_t>(b) * p.Tq + j], 0))) : len;
-    return static_cast<int>((n + c.page - 1) >> c.shift);
-  };
-  if (i0 == 0)
-    for (int j = tid; j < p.Tq; j += 256) p.counts[(static_cast<int64_t>(b) * p.Tq + j) * c.H + h] = pages_of(j);
+  if (i0 == 0) {
+    for (int j = lane; j < p.Tq; j += 64) {
+      const int64_t n = p.visible ? min(len, static_cast<int64_t>(max(p.visible[static_cast<int64_t>(b) * p.Tq + j], 0))) : len;
+      p.counts[(static_cast<int64_t>(b) * p.Tq + j) * c.H + h] = static_cast<int>((n + c.page - 1) >> c.shift);
+    }
+  }
   const int total = static_cast<int>((len + c.page - 1) >> c.shift);
   if (i0 >= total) return;
-  // the bounds, rows of whole pieces
-  constexpr int LPR = ROWB / 16;
-  for (int u = tid; u < 64 * LPR; u += 256) {
-    const int i = i0 + u / LPR;
-    const int page = i < total ? table[i] : -1;
-    u32x4 x = {0, 0, 0, 0};
-    if (static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages))
-      x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.bounds) + (static_cast<int64_t>(page) * c.H + h) * ROWB + u % LPR * 16);
-    *reinterpret_cast<u32x4*>(s_b + u / LPR * LD + u % LPR * 16) = x;
+  u32x4 lo[U], hi[U];
+  bool there[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = i0 + u * PS + lane / LPR, page = i < total ? table[i] : -1;
+    there[u] = static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages);
+    const T* at = static_cast<const T*>(p.bounds) + (static_cast<int64_t>(there[u] ? page : 0) * c.H + h) * 2 * DH + d0;
+    lo[u] = *reinterpret_cast<const u32x4*>(at);
+    hi[u] = *reinterpret_cast<const u32x4*>(at + DH);
   }
-  const int mine = i0 + lane < total ? table[i0 + lane] : -1;
-  const bool there = static_cast<uint32_t>(mine) < static_cast<uint32_t>(c.n_pages);
   const int rows = p.Tq * p.rep;
-  float best = -__builtin_inff();
-  bool nan = false;
-  for (int r0 = 0; r0 < rows; r0 += RC) {
-    __syncthreads();
-    for (int u = tid; u < RC * DH; u += 256) {
-      const int r = r0 + u / DH, d = u % DH;
-      float q = 0.f;
-      if (r < rows)
-        q = tof(static_cast<const T*>(p.q)[(static_cast<int64_t>(b) * p.Tq + r / p.rep) * p.q_stride + (h * p.rep + r % p.rep) * DH + d]);
-      s_q[u / DH][0][d] = q < 0.f ? static_cast<double>(q) : 0.;
-      s_q[u / DH][1][d] = q < 0.f ? 0. : static_cast<double>(q);  // NaN here
-    }
-    __syncthreads();
-    double sum[RC];
+  float best[U];
+  bool nan[U];
 #pragma unroll
-    for (int r = 0; r < RC; ++r) sum[r] = 0.;
+  for (int u = 0; u < U; ++u) best[u] = -__builtin_inff(), nan[u] = false;
 #pragma unroll 1
-    for (int d = w * QD; d < (w + 1) * QD; d += V)
+  for (int r0 = 0; r0 < rows; r0 += RC) {
+    double q[RC][V];
 #pragma unroll
-      for (int side = 0; side < 2; ++side) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(s_b + lane * LD + (side * DH + d) * sizeof(T));
-        const T* x = reinterpret_cast<const T*>(&a);
+    for (int r = 0; r < RC; ++r) {
+      const int rr = min(r0 + r, rows - 1);
+      const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.q) +
+          (static_cast<int64_t>(b) * p.Tq + rr / p.rep) * p.q_stride + (h * p.rep + rr % p.rep) * DH + d0);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const double y = tof(x[i]);
+      for (int i = 0; i < V; ++i) q[r][i] = tof(reinterpret_cast<const T*>(&x)[i]);
+    }
 #pragma unroll
-          for (int r = 0; r < RC; ++r) sum[r] = __builtin_fma(s_q[r][side][d + i], y, sum[r]);
-        }
+    for (int u = 0; u < U; ++u) {
+      const T* l = reinterpret_cast<const T*>(&lo[u]);
+      const T* g = reinterpret_cast<const T*>(&hi[u]);
+      double sum[RC];
+#pragma unroll
+      for (int r = 0; r < RC; ++r) {
+        sum[r] = 0.;
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[r] = __builtin_fma(q[r][i], static_cast<double>(q[r][i] < 0. ? tof(l[i]) : tof(g[i])), sum[r]);
       }
 #pragma unroll
-    for (int r = 0; r < RC; ++r) s_sum[w][r][lane] = sum[r];
-    __syncthreads();
-    // the first wave, row after row: of a query's heads the highest
-    if (w == 0) {
-      for (int r = 0; r < RC && r0 + r < rows; ++r) {
-        float x = static_cast<float>((s_sum[0][r][lane] + s_sum[1][r][lane]) + (s_sum[2][r][lane] + s_sum[3][r][lane]));
-        if (__any(x != x)) {  // an infinite bound times the zero of the other side's part
-          double y = 0.;
-#pragma unroll 1
-          for (int d = 0; d < DH; ++d) {
-            const bool low = s_q[r][0][d] != 0.;
-            y += s_q[r][low ? 0 : 1][d] * tof(reinterpret_cast<const T*>(s_b + lane * LD)[low ? d : DH + d]);
-          }
-          x = x != x ? static_cast<float>(y) : x;
-        }
-        best = fmaxf(best, x);
-        nan |= x != x;
+      for (int r = 0; r < RC; ++r) {
         const int rr = r0 + r;
-        if (rr % p.rep == p.rep - 1) {
-          if (i0 + lane < total)
-            p.scores[((static_cast<int64_t>(b) * p.Tq + rr / p.rep) * c.H + h) * p.ld + i0 + lane] =
-                there && !nan ? best : __builtin_nanf("");
-          best = -__builtin_inff();
-          nan = false;
+        if (rr >= rows) continue;
+        const float x = static_cast<float>(row_sum<LPR>(sum[r]));
+        best[u] = fmaxf(best[u], x);
+        nan[u] |= x != x;
+        if (rr % p.rep == p.rep - 1) {  // of a query's heads the highest
+          const int i = i0 + u * PS + lane / LPR;
+          if (lane % LPR == 0 && i < total)
+            p.scores[((static_cast<int64_t>(b) * p.Tq + rr / p.rep) * c.H + h) * p.ld + i] = there[u] && !nan[u] ? best[u] : __builtin_nanf("");
+          best[u] = -__builtin_inff();
+          nan[u] = false;
         }
       }
     }
@@ -176,11 +176,12 @@ hipError_t launch_page_bounds(const BoundsParams& p, bool bf16, hipStream_t s) {
 }
 
 hipError_t launch_page_scores(const SelectParams& p, bool bf16, hipStream_t s) {
-  const int np = std::max(1, (p.ld + 63) / 64);  // one at least: it writes the counts
+  // pages of a workgroup's four waves: 64 of 256 bytes a bound, 128 of 128, 32 of 512
+  const int wide = p.c.dh * (bf16 ? 2 : 4), some = 4 * 4 * 1024 / wide;
+  const int np = std::max(1, (p.ld + some - 1) / some);  // one at least: it writes the counts
   const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * np;
-  constexpr int RC = 4;
-  auto kern = bf16 ? (p.c.dh == 128 ? k_page_scores<__bf16, 128, RC> : k_page_scores<__bf16, 64, RC>)
-                   : (p.c.dh == 128 ? k_page_scores<float, 128, RC> : k_page_scores<float, 64, RC>);
+  auto kern = bf16 ? (p.c.dh == 128 ? k_page_scores<__bf16, 128> : k_page_scores<__bf16, 64>)
+                   : (p.c.dh == 128 ? k_page_scores<float, 128> : k_page_scores<float, 64>);
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, p, np);
   return hipGetLastError();
 }

@@ -1626,7 +1626,7 @@ rolesub_status rolesub_select_pages(const rolesub_pages* pages, rolesub_dtype dt
   // the selection has up to 64 workgroups of 512 threads a row
   if (static_cast<double>(nq) * p.c.H * 64 * 512 >= static_cast<double>(kMaxThreads) ||
       static_cast<double>(Hq / p.c.H) * Tq > 0x7FFFFFFF || n_sel > (1 << 30) ||
-      static_cast<double>(B) * p.c.H * ((ml / p.c.page + 65) / 64) * 256 >= static_cast<double>(kMaxThreads))
+      static_cast<double>(B) * p.c.H * ((ml / p.c.page + 33) / 32) * 256 >= static_cast<double>(kMaxThreads))
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads, queries or pages", fn);
   const SelectPlan d = select_plan(B, Tq, p.c.H, p.c.page, ml);
   if (!workspace || ws_bytes < d.bytes)
