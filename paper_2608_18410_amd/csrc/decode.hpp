@@ -104,19 +104,20 @@ __device__ __forceinline__ u32x4 bload16_hint(rsrc_t r, uint32_t off) {
 // queries, 32 heads 29.2 -> 31.1 us, 8 of 305 and 305 52 -> 56.5) and nothing where
 // calls are bound by memory. An infinity's other parts are NaN.
 constexpr int kParts = 3;
-__device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8 (&part)[kParts]) {
-  u32x4 v[kParts];
+template <int N>
+__device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8 (&part)[N]) {
+  u32x4 v[N];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f32x2 x = i < 2 ? f32x2{a[2 * i], a[2 * i + 1]} : f32x2{b[2 * i - 4], b[2 * i - 3]};
 #pragma unroll
-    for (int n = 0; n < kParts; ++n) {
+    for (int n = 0; n < N; ++n) {
       v[n][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
       x = f32x2{x[0] - __uint_as_float(v[n][i] << 16), x[1] - __uint_as_float(v[n][i] & 0xFFFF0000u)};
     }
   }
 #pragma unroll
-  for (int n = 0; n < kParts; ++n) part[n] = __builtin_bit_cast(bf16x8, v[n]);
+  for (int n = 0; n < N; ++n) part[n] = __builtin_bit_cast(bf16x8, v[n]);
 }
 
 // Order of N steps of R LDS reads that feed M matrix products each: the reads run A
@@ -417,13 +418,13 @@ __device__ __forceinline__ void soften(const DecodeParams& p, f32x4* s, uint32_t
 }
 
 // The tile's values times its weights s, added to the sums (dims the rows of the
-// product, queries its columns). A: steps by which LDS reads run ahead.
-template <class T, int DH, int A>
+// product, queries its columns). A: steps by which LDS reads run ahead; N: parts of a weight.
+template <class T, int DH, int A, int N>
 __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4* acc) {
   using L = Tile<T, DH>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   if constexpr (L::kBf16) {
-    bf16x8 part[kParts];
+    bf16x8 part[N];
     split_bf16(s[0], s[L::NB - 1], part);
     const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
 #pragma unroll
@@ -431,9 +432,9 @@ __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4
       const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
       const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-      for (int n = 0; n < kParts; ++n) acc[mb] = mfma_16x16x32(a, part[n], acc[mb]);
+      for (int n = 0; n < N; ++n) acc[mb] = mfma_16x16x32(a, part[n], acc[mb]);
     }
-    if constexpr (A > 0) reads_ahead<L::MB, 2, kParts, A>();
+    if constexpr (A > 0) reads_ahead<L::MB, 2, N, A>();
   } else {
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb)
@@ -676,7 +677,7 @@ __device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len
 // GB) 547 us, 6.1 TB/s, and 608 where the scores are stored for the weights, more
 // than their 33 MB explain. Below that by a chain of dependent loads (length, page, mask, key and value): one
 // of 305 tokens 8 us.
-template <class T, int DH, int WR, int SUB, bool ONCE, int S>
+template <class T, int DH, int WR, int SUB, bool ONCE, int S, int PN>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4))) void k_decode(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, NVI = L::NVI, MB = L::MB, RLD = L::RLD;
@@ -872,7 +873,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
         const int k = lane / XL, t = t0 + (k - i % XT) * STEP + lane % XL * 4;
         if (k <= i % XT && t < end) *reinterpret_cast<f32x4*>(px + t) = *reinterpret_cast<const f32x4*>(s_x[w % XW] + 4 * lane);
       }
-      weigh_tile<T, DH, 0>(zt, s, acc);
+      weigh_tile<T, DH, 0, PN>(zt, s, acc);
       wave_lds_order();
     }
   }
@@ -896,7 +897,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 // waiting for data or a barrier and a third for a turn to issue, among 267 vector
 // instructions a tile and wave, 32 of them products; 12 instructions fewer changed nothing.
 // A quarter of the LDS cycles are bank conflicts.
-template <class T, int DH, int SUB, int S>
+template <class T, int DH, int SUB, int S, int PN>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 3 : 4))) void k_decode_rows(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, MB = L::MB;
@@ -1037,6 +1038,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   f32x4 acc[MB];
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0, 0, 0, 0};
+  // a wave without rows takes part in the loads only (a call's last rows)
+  const bool idle = (rtile * 4 + w) * 16 >= p.R;
   uint32_t there0, there1;
   auto move_on = [&](int (&to)[NB], const int (&from)[NB]) {
 #pragma unroll
@@ -1069,6 +1072,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     request_tile(i + 2);
     take_pages(i + 3);
     request_meta(i + 3);
+    if (S != kPrefix && idle) continue;
     f32x4 s[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) s[nb] = f32x4{0, 0, 0, 0};
@@ -1078,7 +1082,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       for (int nb = 0; nb < NB; ++nb)
         s[nb] = score_step<T>(*reinterpret_cast<const u32x4*>(buf + (16 * nb + l16) * KLD + 64 * j + 16 * g4), qf[j], s[nb]);
     soften<T, DH, true, S>(p, s, now, t0, at, v, least, end, r, px, nullptr, m, l, acc);
-    weigh_tile<T, DH, 2>(buf + KB, s, acc);
+    weigh_tile<T, DH, 2, PN>(buf + KB, s, acc);
   }
   __syncthreads();
   bool bad = false;
@@ -1297,20 +1301,31 @@ int row_blocks(int R, bool bf16, int dh) { return R <= 16 ? 1 : R <= 32 && !shar
 // batches would gain (64 of up to 2048, 8 heads of 4 rows 64.6 -> 59.2).
 constexpr int kOnceTokens = 1024;
 
-template <class T, int DH, int WR, int SUB, int S>
+// Parts of a bfloat16 weight: all 24 bits, but in the calls that always took the output's
+// type into account 17 where that is bfloat16 itself, whose half step is 2^-9: a weight is
+// off by 2^-17 of itself. 32 sequences of up to 4096 tokens and 24 drafted ones, 8 key
+// heads of 4 rows: see k_tree.hip.
+template <class T, int DH, int WR, int SUB, int S, int N>
 auto kernel_of(const DecodeParams& p) {
   if constexpr (WR == 4)
-    return k_decode_rows<T, DH, SUB, S>;
+    return k_decode_rows<T, DH, SUB, S, N>;
   else
-    return p.max_len >= kOnceTokens && !p.x ? k_decode<T, DH, WR, SUB, true, S> : k_decode<T, DH, WR, SUB, false, S>;
+    return p.max_len >= kOnceTokens && !p.x ? k_decode<T, DH, WR, SUB, true, S, N> : k_decode<T, DH, WR, SUB, false, S, N>;
+}
+template <class T, int DH, int WR, int SUB, int S>
+auto kernel_for(const DecodeParams& p) {
+  if constexpr (sizeof(T) == 2 && S != kPrefix) {
+    if (!p.out_f32) return kernel_of<T, DH, WR, SUB, S, 2>(p);
+  }
+  return kernel_of<T, DH, WR, SUB, S, kParts>(p);
 }
 
 template <class T, int DH, int WR, int S>
 void go(const DecodeParams& p, hipStream_t s) {
   const int sub = p.c.ds >= Tile<T, DH>::EP ? 1 : Tile<T, DH>::EP / p.c.ds;
-  auto kern = sub == 1 ? kernel_of<T, DH, WR, 1, S>(p) : kernel_of<T, DH, WR, 2, S>(p);
+  auto kern = sub == 1 ? kernel_for<T, DH, WR, 1, S>(p) : kernel_for<T, DH, WR, 2, S>(p);
   if constexpr (sizeof(T) == 2) {
-    if (sub == 4) kern = kernel_of<T, DH, WR, 4, S>(p);
+    if (sub == 4) kern = kernel_for<T, DH, WR, 4, S>(p);
   }
   const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(256), 0, s, p);

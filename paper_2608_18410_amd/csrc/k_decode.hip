@@ -13,6 +13,8 @@ namespace {
 // heads: 12.2 against 14.4 us), but a call's outputs would then depend on whether it
 // adds up weights.
 constexpr int64_t kSplitWgs = 512;
+// The same for drafted tokens.
+constexpr int64_t kTreeWgs = 1024;
 // Splits of more than 2048 tokens cost next to nothing to add up, and up to 2048
 // workgroups of them even out a ragged batch: 34 sequences of 236 to 15420 tokens, 8 key
 // heads of 4 rows 259 -> 183 us, 23 of 7727 to 22794 290 -> 215, 34 of 8192 192 -> 170. Not
@@ -24,13 +26,14 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
 
-DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass) {
+DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, bool tree) {
   DecodePlan d;
+  const int64_t want = tree ? kTreeWgs : kSplitWgs;
   const int nrt = (R + 63) / 64;  // whatever row_blocks says
   const int64_t units = (static_cast<int64_t>(max_len) + 127) / 128;  // of 128 tokens, a tile for each of four waves
   const int64_t wgs = static_cast<int64_t>(B) * H * nrt;
   const int64_t least = (units + kMaxSplits - 1) / kMaxSplits;
-  int64_t per = std::max((units * wgs + kSplitWgs - 1) / kSplitWgs, least);
+  int64_t per = std::max((units * wgs + want - 1) / want, least);
   if (per > kLongUnits && (per < units || wgs > kOrderWgs))
     per = std::max({kLongUnits, (units * wgs + kLongWgs - 1) / kLongWgs, least});
   d.chunk = static_cast<int>(128 * std::max<int64_t>(1, std::min(per, units)));
@@ -41,11 +44,11 @@ DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass) {
   d.off_x = d.off_stat + (d.n_split > 1 || (mass && max_len > 0) ? up256(cells * 8) : 0);
   d.bytes = d.off_x + (mass ? up256(rows * d.x_ld * 4) : 0);
   // what to ask a caller for: a bound on the above that does not fall as B, Tq or
-  // max_len grows (n_split <= kSplitWgs / wgs + 1, or for splits of kLongUnits and more
+  // max_len grows (n_split <= want / wgs + 1, or for splits of kLongUnits and more
   // kLongWgs / wgs + 1 and units / kLongUnits + 1; R <= 64 nrt)
   const size_t r64 = std::min<size_t>(R, 64);
   const size_t longs = std::min(r64 * kLongWgs, rows * static_cast<size_t>(units / kLongUnits)) + rows;
-  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)), std::max(r64 * kSplitWgs + rows, longs));
+  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)), std::max(r64 * want + rows, longs));
   d.ask = up256(most * dh * 4) + up256(most * 8) + (mass ? up256(rows * d.x_ld * 4) : 0);
   return d;
 }

@@ -325,7 +325,7 @@ struct DecodePlan {
   size_t off_stat, off_x, bytes;  // of this call
   size_t ask;  // at least bytes of every call of no more sequences, queries and tokens
 };
-DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass);
+DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, bool tree = false);
 hipError_t launch_decode(const DecodeParams& p, bool bf16, hipStream_t s);
 hipError_t launch_decode_tree(const DecodeParams& p, bool bf16, hipStream_t s);
 hipError_t launch_decode_listed(const DecodeParams& p, bool bf16, hipStream_t s);

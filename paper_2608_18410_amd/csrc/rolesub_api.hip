@@ -995,7 +995,7 @@ rolesub_status set_attend(const char* fn, DecodeParams& p, rolesub_dtype dtype, 
   p.scale = static_cast<float>((scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(c.dh)) : scale) * 1.44269504088896341);
   p.out = out;
   p.out_f32 = out_dtype == ROLESUB_F32;
-  const DecodePlan d = decode_plan(p.B, c.H, p.R, c.dh, p.max_len, false);
+  const DecodePlan d = decode_plan(p.B, c.H, p.R, c.dh, p.max_len, false, p.tree != nullptr);
   if (d.bytes > 0 && (!workspace || ws_bytes < d.bytes))
     return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, %zu given", fn, d.bytes,
                 workspace ? ws_bytes : static_cast<size_t>(0));
@@ -1469,7 +1469,9 @@ rolesub_status rolesub_tree_masks(int32_t B, int32_t T, const int32_t* parents, 
 }
 
 size_t rolesub_attend_tree_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq, int32_t max_len) {
-  return rolesub_attend_paged_workspace_size(pages, B, Hq, Tq, max_len, 0);
+  if (!pages || B <= 0 || pages->H < 1 || Hq < pages->H || Tq <= 0 || max_len <= 0) return 0;
+  if (static_cast<size_t>(Hq / pages->H) * Tq > 0x7FFFFFFF) return 0;
+  return decode_plan(B, pages->H, Hq / pages->H * Tq, pages->dh, max_len, false, true).ask;
 }
 
 rolesub_status rolesub_attend_tree(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
