@@ -64,22 +64,46 @@ __global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
   *reinterpret_cast<u32x4*>(static_cast<char*>(p.bounds) + head * 2 * DH * sizeof(T) + lane * 16) = out;
 }
 
-// Sum over the LPR lanes of a row, the same bits in all of them.
-template <int LPR>
-__device__ __forceinline__ double row_sum(double x) {
-  auto other = [](double y, auto ctrl) {
-    const u32x2 v = __builtin_bit_cast(u32x2, y);
-    u32x2 r;
+// What the lane D away (D in 1, 2, 4, 8, 16; within rows of 2 D lanes) holds.
+template <int D>
+__device__ __forceinline__ uint32_t away(uint32_t x) {
+  constexpr int quad1 = 0xB1, quad2 = 0x4E, mirror8 = 0x141, mirror16 = 0x140, quad_back = 0x1B;
+  if constexpr (D == 1) return __builtin_amdgcn_update_dpp(0, x, quad1, 0xF, 0xF, true);
+  if constexpr (D == 2) return __builtin_amdgcn_update_dpp(0, x, quad2, 0xF, 0xF, true);
+  // lane i of 8 holds what lane 7 - i did, then quads are turned back
+  if constexpr (D == 4)
+    return __builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, x, mirror8, 0xF, 0xF, true), quad_back, 0xF, 0xF, true);
+  // 15 - i, then 7 - i
+  if constexpr (D == 8)
+    return __builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, x, mirror16, 0xF, 0xF, true), mirror8, 0xF, 0xF, true);
+  if constexpr (D == 16) return __shfl_xor(x, 16, kWave);
+}
+template <int D>
+__device__ __forceinline__ double away(double x) {
+  u32x2 v = __builtin_bit_cast(u32x2, x);
+  v[0] = away<D>(v[0]);
+  v[1] = away<D>(v[1]);
+  return __builtin_bit_cast(double, v);
+}
+
+// N sums over the lanes of a row, N = 2^k: each step leaves a lane half of them, the lower
+// one where its bit D is clear, so that at the end the lanes hold one each (N > lanes: a
+// few; N < lanes: several lanes the same). x[0 ..] are the lane's.
+template <int D, int N>
+__device__ __forceinline__ void share_sums(double* x) {
+  if constexpr (D > 0) {
+    if constexpr (N > 1) {
+      const bool up = threadIdx.x & D;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) r[i] = __builtin_amdgcn_update_dpp(0, v[i], decltype(ctrl)::value, 0xF, 0xF, true);
-    return __builtin_bit_cast(double, r);
-  };
-  x += other(x, std::integral_constant<int, 0xB1>{});                            // lanes 1 apart
-  x += other(x, std::integral_constant<int, 0x4E>{});                            // 2 apart
-  x += other(x, std::integral_constant<int, 0x141>{});                           // the other half of 8
-  if constexpr (LPR >= 16) x += other(x, std::integral_constant<int, 0x140>{});  // the other half of 16
-  if constexpr (LPR >= 32) x += __shfl_xor(x, 16, kWave);
-  return x;
+      for (int i = 0; i < N / 2; ++i) {
+        const double keep = up ? x[i + N / 2] : x[i], give = up ? x[i] : x[i + N / 2];
+        x[i] = keep + away<D>(give);
+      }
+    } else {
+      x[0] += away<D>(x[0]);
+    }
+    share_sums<D / 2, (N > 1 ? N / 2 : 1)>(x);
+  }
 }
 
 // Scores of a few pages of one key head for a sequence's queries, a wave's work: the
@@ -88,11 +112,13 @@ __device__ __forceinline__ double row_sum(double x) {
 // lane has a 16-byte piece of both bounds of a page, and its part of RC queries in 64
 // bits; the lanes of a page add up. All bounds of a wave are asked for at once. Bound by
 // memory: 8 sequences of 110001 to 131071 tokens, pages of 64 and 8 key heads of 4 rows (62 MB).
-template <class T, int DH>
+template <class T, int DH, int RC>
 __global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
-  constexpr int V = 16 / sizeof(T), LPR = DH / V, PS = 64 / LPR, U = 4, RC = 4;  // pages of a step, steps, rows at a time
+  // pages of a step, steps; lanes of a page; sums of a lane at the end
+  constexpr int V = 16 / sizeof(T), LPR = DH / V, PS = 64 / LPR, U = 4, N = RC * U, LEFT = N > LPR ? N / LPR : 1;
+  constexpr int SHARED = LPR > N ? LPR / N : 1;  // lanes that end with the same sum
   const PagedCache& c = p.c;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), d0 = lane % LPR * V;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane % LPR, d0 = lr * V;
   int lin = blockIdx.x;
   const int i0 = (lin % np * 4 + w) * PS * U;
   lin /= np;
@@ -109,56 +135,76 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
   const int total = static_cast<int>((len + c.page - 1) >> c.shift);
   if (i0 >= total) return;
   u32x4 lo[U], hi[U];
-  bool there[U];
+  uint32_t there = 0;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int i = i0 + u * PS + lane / LPR, page = i < total ? table[i] : -1;
-    there[u] = static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages);
-    const T* at = static_cast<const T*>(p.bounds) + (static_cast<int64_t>(there[u] ? page : 0) * c.H + h) * 2 * DH + d0;
+    const bool in = static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages);
+    there |= in ? 1u << u : 0u;
+    const T* at = static_cast<const T*>(p.bounds) + (static_cast<int64_t>(in ? page : 0) * c.H + h) * 2 * DH + d0;
     lo[u] = *reinterpret_cast<const u32x4*>(at);
     hi[u] = *reinterpret_cast<const u32x4*>(at + DH);
   }
-  const int rows = p.Tq * p.rep;
-  float best[U];
-  bool nan[U];
+  // The sums' numbers are 4 r + u, their bits from the highest those of the lane from LPR / 2
+  // on: the lane's steps and rows, and which of its LEFT sums are which.
+  const int mine = lr / SHARED * LEFT;
+  for (int j = 0; j < p.Tq; ++j) {
+    float best[LEFT];  // of the query's heads, of the rows that the lane has sums of
+    bool nan[LEFT];
 #pragma unroll
-  for (int u = 0; u < U; ++u) best[u] = -__builtin_inff(), nan[u] = false;
+    for (int x = 0; x < LEFT; ++x) best[x] = -__builtin_inff(), nan[x] = false;
 #pragma unroll 1
-  for (int r0 = 0; r0 < rows; r0 += RC) {
-    double q[RC][V];
+    for (int r0 = 0; r0 < p.rep; r0 += RC) {
+      double q[RC][V], sum[N];
 #pragma unroll
-    for (int r = 0; r < RC; ++r) {
-      const int rr = min(r0 + r, rows - 1);
-      const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.q) +
-          (static_cast<int64_t>(b) * p.Tq + rr / p.rep) * p.q_stride + (h * p.rep + rr % p.rep) * DH + d0);
+      for (int r = 0; r < RC; ++r) {  // past the last head: it again
+        const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.q) + (static_cast<int64_t>(b) * p.Tq + j) * p.q_stride +
+                                                        (h * p.rep + min(r0 + r, p.rep - 1)) * DH + d0);
 #pragma unroll
-      for (int i = 0; i < V; ++i) q[r][i] = tof(reinterpret_cast<const T*>(&x)[i]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const T* l = reinterpret_cast<const T*>(&lo[u]);
-      const T* g = reinterpret_cast<const T*>(&hi[u]);
-      double sum[RC];
-#pragma unroll
-      for (int r = 0; r < RC; ++r) {
-        sum[r] = 0.;
-#pragma unroll
-        for (int i = 0; i < V; ++i) sum[r] = __builtin_fma(q[r][i], static_cast<double>(q[r][i] < 0. ? tof(l[i]) : tof(g[i])), sum[r]);
+        for (int i = 0; i < V; ++i) q[r][i] = tof(reinterpret_cast<const T*>(&x)[i]);
       }
 #pragma unroll
-      for (int r = 0; r < RC; ++r) {
-        const int rr = r0 + r;
-        if (rr >= rows) continue;
-        const float x = static_cast<float>(row_sum<LPR>(sum[r]));
-        best[u] = fmaxf(best[u], x);
-        nan[u] |= x != x;
-        if (rr % p.rep == p.rep - 1) {  // of a query's heads the highest
-          const int i = i0 + u * PS + lane / LPR;
-          if (lane % LPR == 0 && i < total)
-            p.scores[((static_cast<int64_t>(b) * p.Tq + rr / p.rep) * c.H + h) * p.ld + i] = there[u] && !nan[u] ? best[u] : __builtin_nanf("");
-          best[u] = -__builtin_inff();
-          nan[u] = false;
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int r = 0; r < RC; ++r) {
+          const T* l = reinterpret_cast<const T*>(&lo[u]);
+          const T* g = reinterpret_cast<const T*>(&hi[u]);
+          double x = 0.;
+#pragma unroll
+          for (int i = 0; i < V; ++i) x = __builtin_fma(q[r][i], static_cast<double>(q[r][i] < 0. ? tof(l[i]) : tof(g[i])), x);
+          sum[r * U + u] = x;
         }
+      share_sums<LPR / 2, N>(sum);
+#pragma unroll
+      for (int x = 0; x < LEFT; ++x) {
+        const float y = static_cast<float>(sum[x]);
+        best[x] = fmaxf(best[x], y);
+        nan[x] |= y != y;
+      }
+    }
+    // the highest over the rows, which lie on lanes LPR / 2 .. apart (from the highest bit down)
+    uint32_t top[LEFT];  // an order in which NaN is above all numbers
+#pragma unroll
+    for (int x = 0; x < LEFT; ++x) top[x] = nan[x] ? 0xFFFFFFFFu : order_key(best[x]);
+    if constexpr (RC == 4) {
+      if constexpr (LPR >= 2) {
+#pragma unroll
+        for (int x = 0; x < LEFT; ++x) top[x] = max(top[x], away<LPR / 2>(top[x]));
+      }
+      if constexpr (LPR >= 4) {
+#pragma unroll
+        for (int x = 0; x < LEFT; ++x) top[x] = max(top[x], away<LPR / 4>(top[x]));
+      }
+    }
+    // lanes whose rows' bits are clear write: the steps mine % U ..
+    if (mine < U && lr % SHARED == 0) {
+#pragma unroll
+      for (int x = 0; x < LEFT; ++x) {
+        const int u = mine + x, i = i0 + u * PS + lane / LPR;
+        const uint32_t k = top[x];
+        const float y = __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+        if (i < total)
+          p.scores[((static_cast<int64_t>(b) * p.Tq + j) * c.H + h) * p.ld + i] = ((there >> u) & 1u) && k != 0xFFFFFFFFu ? y : __builtin_nanf("");
       }
     }
   }
@@ -180,8 +226,11 @@ hipError_t launch_page_scores(const SelectParams& p, bool bf16, hipStream_t s) {
   const int wide = p.c.dh * (bf16 ? 2 : 4), some = 4 * 4 * 1024 / wide;
   const int np = std::max(1, (p.ld + some - 1) / some);  // one at least: it writes the counts
   const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * np;
-  auto kern = bf16 ? (p.c.dh == 128 ? k_page_scores<__bf16, 128> : k_page_scores<__bf16, 64>)
-                   : (p.c.dh == 128 ? k_page_scores<float, 128> : k_page_scores<float, 64>);
+  auto many = bf16 ? (p.c.dh == 128 ? k_page_scores<__bf16, 128, 4> : k_page_scores<__bf16, 64, 4>)
+                   : (p.c.dh == 128 ? k_page_scores<float, 128, 4> : k_page_scores<float, 64, 4>);
+  auto one = bf16 ? (p.c.dh == 128 ? k_page_scores<__bf16, 128, 1> : k_page_scores<__bf16, 64, 1>)
+                  : (p.c.dh == 128 ? k_page_scores<float, 128, 1> : k_page_scores<float, 64, 1>);
+  auto kern = p.rep == 1 ? one : many;
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, p, np);
   return hipGetLastError();
 }
