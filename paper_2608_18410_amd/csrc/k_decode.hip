@@ -15,6 +15,11 @@ namespace {
 constexpr int64_t kSplitWgs = 512;
 // The same for drafted tokens.
 constexpr int64_t kTreeWgs = 1024;
+// Up to 512 tokens these and listed pages, whose calls add up no weights, have one split
+// where 16 rows or fewer share it: 8 drafted tokens over 305 and 32 heads 24.9 -> 22.2 us
+// with the masks, 24 pages of 16 chosen of 176 35.7 -> 31.9 with the choice. From 60 rows on
+// they are slower (25.2 -> 27.4), and so are 1024 listed tokens (35.6 -> 37.7).
+constexpr int64_t kShortUnits = 4;
 // Splits of more than 2048 tokens cost next to nothing to add up, and up to 2048
 // workgroups of them even out a ragged batch: 34 sequences of 236 to 15420 tokens, 8 key
 // heads of 4 rows 259 -> 183 us, 23 of 7727 to 22794 290 -> 215, 34 of 8192 192 -> 170. Not
@@ -26,9 +31,9 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
 
-DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, bool tree) {
+DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, DecodeKind kind) {
   DecodePlan d;
-  const int64_t want = tree ? kTreeWgs : kSplitWgs;
+  const int64_t want = kind == DecodeKind::tree ? kTreeWgs : kSplitWgs;
   const int nrt = (R + 63) / 64;  // whatever row_blocks says
   const int64_t units = (static_cast<int64_t>(max_len) + 127) / 128;  // of 128 tokens, a tile for each of four waves
   const int64_t wgs = static_cast<int64_t>(B) * H * nrt;
@@ -36,6 +41,7 @@ DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, bool
   int64_t per = std::max((units * wgs + want - 1) / want, least);
   if (per > kLongUnits && (per < units || wgs > kOrderWgs))
     per = std::max({kLongUnits, (units * wgs + kLongWgs - 1) / kLongWgs, least});
+  if (kind != DecodeKind::paged && units <= kShortUnits && R <= 16) per = units;
   d.chunk = static_cast<int>(128 * std::max<int64_t>(1, std::min(per, units)));
   d.n_split = std::max(1, static_cast<int>((static_cast<int64_t>(max_len) + d.chunk - 1) / d.chunk));
   d.x_ld = (max_len + 3) / 4 * 4;

@@ -106,49 +106,54 @@ __device__ __forceinline__ void share_sums(double* x) {
   }
 }
 
+// Tokens of sequence b that any query sees, and pages of them that query j does.
+__device__ __forceinline__ int64_t tokens_of(const SelectParams& p, int b) {
+  return min(min(static_cast<int64_t>(max(p.lens[b], 0)), static_cast<int64_t>(p.max_len)),
+             static_cast<int64_t>(p.max_pages) << p.c.shift);
+}
+__device__ __forceinline__ int pages_of(const SelectParams& p, int b, int j, int64_t len) {
+  if (p.visible) len = min(len, static_cast<int64_t>(max(p.visible[static_cast<int64_t>(b) * p.Tq + j], 0)));
+  return static_cast<int>((len + p.c.page - 1) >> p.c.shift);
+}
+
 // Scores of a few pages of one key head for a sequence's queries, a wave's work: the
 // highest that a key within the bounds could have, sum_d (q < 0 ? q lo : q hi), summed in
 // 64 bits and rounded once, so that the choice does not hang on the order of the sum. A
 // lane has a 16-byte piece of both bounds of a page, and its part of RC queries in 64
-// bits; the lanes of a page add up. All bounds of a wave are asked for at once. Bound by
-// memory: 8 sequences of 110001 to 131071 tokens, pages of 64 and 8 key heads of 4 rows (62 MB).
+// bits; the lanes of a page add up. All bounds of a wave are asked for at once.
 template <class T, int DH, int RC>
-__global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
-  // pages of a step, steps; lanes of a page; sums of a lane at the end
-  constexpr int V = 16 / sizeof(T), LPR = DH / V, PS = 64 / LPR, U = 4, N = RC * U, LEFT = N > LPR ? N / LPR : 1;
-  constexpr int SHARED = LPR > N ? LPR / N : 1;  // lanes that end with the same sum
-  const PagedCache& c = p.c;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane % LPR, d0 = lr * V;
-  int lin = blockIdx.x;
-  const int i0 = (lin % np * 4 + w) * PS * U;
-  lin /= np;
-  const int h = lin % c.H, b = lin / c.H;
-  const int32_t* table = p.table + static_cast<int64_t>(b) * p.max_pages;
-  const int64_t len = min(min(static_cast<int64_t>(max(p.lens[b], 0)), static_cast<int64_t>(p.max_len)),
-                          static_cast<int64_t>(p.max_pages) << c.shift);
-  if (i0 == 0) {
-    for (int j = lane; j < p.Tq; j += 64) {
-      const int64_t n = p.visible ? min(len, static_cast<int64_t>(max(p.visible[static_cast<int64_t>(b) * p.Tq + j], 0))) : len;
-      p.counts[(static_cast<int64_t>(b) * p.Tq + j) * c.H + h] = static_cast<int>((n + c.page - 1) >> c.shift);
-    }
-  }
-  const int total = static_cast<int>((len + c.page - 1) >> c.shift);
-  if (i0 >= total) return;
+struct PageScores {
+  // pages of a step, steps; lanes of a page; sums of a lane at the end, lanes with the same one
+  static constexpr int V = 16 / sizeof(T), LPR = DH / V, PS = 64 / LPR, U = 4, N = RC * U;
+  static constexpr int LEFT = N > LPR ? N / LPR : 1, SHARED = LPR > N ? LPR / N : 1;
   u32x4 lo[U], hi[U];
   uint32_t there = 0;
+
+  // pages i0 .. i0 + PS U - 1 of `total`
+  __device__ __forceinline__ void load(const SelectParams& p, int b, int h, int i0, int total) {
+    const PagedCache& c = p.c;
+    const int lane = threadIdx.x & 63;
+    const int32_t* table = p.table + static_cast<int64_t>(b) * p.max_pages;
+    there = 0;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int i = i0 + u * PS + lane / LPR, page = i < total ? table[i] : -1;
-    const bool in = static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages);
-    there |= in ? 1u << u : 0u;
-    const T* at = static_cast<const T*>(p.bounds) + (static_cast<int64_t>(in ? page : 0) * c.H + h) * 2 * DH + d0;
-    lo[u] = *reinterpret_cast<const u32x4*>(at);
-    hi[u] = *reinterpret_cast<const u32x4*>(at + DH);
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * PS + lane / LPR, page = i < total ? table[i] : -1;
+      const bool in = static_cast<uint32_t>(page) < static_cast<uint32_t>(c.n_pages);
+      there |= in ? 1u << u : 0u;
+      const T* at = static_cast<const T*>(p.bounds) + (static_cast<int64_t>(in ? page : 0) * c.H + h) * 2 * DH + lane % LPR * V;
+      lo[u] = *reinterpret_cast<const u32x4*>(at);
+      hi[u] = *reinterpret_cast<const u32x4*>(at + DH);
+    }
   }
-  // The sums' numbers are 4 r + u, their bits from the highest those of the lane from LPR / 2
-  // on: the lane's steps and rows, and which of its LEFT sums are which.
-  const int mine = lr / SHARED * LEFT;
-  for (int j = 0; j < p.Tq; ++j) {
+
+  // put(i, score) for each of them, for query j
+  template <class Put>
+  __device__ __forceinline__ void score(const SelectParams& p, int b, int j, int h, int i0, int total, Put put) const {
+    const PagedCache& c = p.c;
+    const int lane = threadIdx.x & 63, lr = lane % LPR, d0 = lr * V;
+    // The sums' numbers are 4 r + u, their bits from the highest those of the lane from
+    // LPR / 2 on: the lane's steps and rows, and which of its LEFT sums are which.
+    const int mine = lr / SHARED * LEFT;
     float best[LEFT];  // of the query's heads, of the rows that the lane has sums of
     bool nan[LEFT];
 #pragma unroll
@@ -182,32 +187,95 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
         nan[x] |= y != y;
       }
     }
-    // the highest over the rows, which lie on lanes LPR / 2 .. apart (from the highest bit down)
-    uint32_t top[LEFT];  // an order in which NaN is above all numbers
+    // the highest over the rows, which lie on lanes LPR / 2 and LPR / 4 apart, in an order
+    // in which NaN is above all numbers
 #pragma unroll
-    for (int x = 0; x < LEFT; ++x) top[x] = nan[x] ? 0xFFFFFFFFu : order_key(best[x]);
-    if constexpr (RC == 4) {
-      if constexpr (LPR >= 2) {
-#pragma unroll
-        for (int x = 0; x < LEFT; ++x) top[x] = max(top[x], away<LPR / 2>(top[x]));
+    for (int x = 0; x < LEFT; ++x) {
+      uint32_t k = nan[x] ? 0xFFFFFFFFu : order_key(best[x]);
+      if constexpr (RC == 4) {
+        k = max(k, away<LPR / 2>(k));
+        k = max(k, away<LPR / 4>(k));
       }
-      if constexpr (LPR >= 4) {
-#pragma unroll
-        for (int x = 0; x < LEFT; ++x) top[x] = max(top[x], away<LPR / 4>(top[x]));
-      }
-    }
-    // lanes whose rows' bits are clear write: the steps mine % U ..
-    if (mine < U && lr % SHARED == 0) {
-#pragma unroll
-      for (int x = 0; x < LEFT; ++x) {
-        const int u = mine + x, i = i0 + u * PS + lane / LPR;
-        const uint32_t k = top[x];
-        const float y = __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
-        if (i < total)
-          p.scores[((static_cast<int64_t>(b) * p.Tq + j) * c.H + h) * p.ld + i] = ((there >> u) & 1u) && k != 0xFFFFFFFFu ? y : __builtin_nanf("");
-      }
+      // lanes whose rows' bits are clear have the steps mine ..
+      const int u = mine + x, i = i0 + u * PS + lane / LPR;
+      if (mine < U && lr % SHARED == 0 && i < total)
+        put(i, ((there >> (u & 3)) & 1u) && k != 0xFFFFFFFFu ? __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k) : __builtin_nanf(""));
     }
   }
+};
+
+// Long histories: the scores to memory, for the selection that follows. Bound by memory and
+// by the 64-bit products: 8 sequences of 110001 to 131071 tokens, pages of 64 and 8 key
+// heads of 4 rows (62 MB) 22 us, 2.8 TB/s, with the vector units busy for 10.
+template <class T, int DH, int RC>
+__global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
+  typedef PageScores<T, DH, RC> S;
+  const PagedCache& c = p.c;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int lin = blockIdx.x;
+  const int i0 = (lin % np * 4 + w) * S::PS * S::U;
+  lin /= np;
+  const int h = lin % c.H, b = lin / c.H;
+  const int64_t len = tokens_of(p, b);
+  if (i0 == 0)
+    for (int j = lane; j < p.Tq; j += 64) p.counts[(static_cast<int64_t>(b) * p.Tq + j) * c.H + h] = pages_of(p, b, j, len);
+  const int total = static_cast<int>((len + c.page - 1) >> c.shift);
+  if (i0 >= total) return;
+  S s;
+  s.load(p, b, h, i0, total);
+  for (int j = 0; j < p.Tq; ++j)
+    s.score(p, b, j, h, i0, total, [&](int i, float x) { p.scores[((static_cast<int64_t>(b) * p.Tq + j) * c.H + h) * p.ld + i] = x; });
+}
+
+// Up to kFewPages pages: scores and choice in one workgroup for each query and key head. A
+// page's rank is the number of pages above it, counted by a thread each: no histogram
+// and three barriers, where the selection's own kernel has ten and a launch before it.
+constexpr int kFewWg = 1024;
+template <class T, int DH, int RC>
+__global__ __launch_bounds__(kFewWg) void k_select_few(SelectParams p) {
+  typedef PageScores<T, DH, RC> S;
+  __shared__ __attribute__((aligned(16))) uint64_t s_key[kFewPages + 8];  // the score, then the lower index first
+  __shared__ int s_cnt[kFewWg / 64];
+  const PagedCache& c = p.c;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = blockIdx.x % c.H, j = blockIdx.x / c.H % p.Tq, b = blockIdx.x / c.H / p.Tq;
+  const int n = pages_of(p, b, j, tokens_of(p, b));
+  int32_t* out = p.sel + static_cast<int64_t>(blockIdx.x) * p.n_sel;
+  if (n <= p.n_sel) {
+    for (int i = tid; i < p.n_sel; i += kFewWg) out[i] = i < n ? i : -1;
+    return;
+  }
+  // of pages [lo, hi) the `need` highest, equal ones by lower index
+  const int lo = p.first, hi = n - p.recent, need = p.n_sel - p.first - p.recent;
+  S s;
+  for (int i0 = w * S::PS * S::U; i0 < n; i0 += kFewWg / 64 * S::PS * S::U) {
+    s.load(p, b, h, i0, n);
+    s.score(p, b, j, h, i0, n, [&](int i, float x) {
+      s_key[i] = i >= lo && i < hi ? static_cast<uint64_t>(order_key(x)) << 32 | static_cast<uint32_t>(~i) : 0u;
+    });
+  }
+  if (tid < 8) s_key[n + tid] = 0;  // n is below kFewPages + 1
+  __syncthreads();
+  int rank = 0;
+  if (64 * w < n) {
+    const uint64_t key = s_key[min(tid, n)];
+#pragma unroll 1
+    for (int x = 0; x < n; x += 8) {
+      uint64_t k[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) k[y] = s_key[x + y];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) rank += k[y] > key;
+    }
+  }
+  const bool on = tid < n && (tid < lo || tid >= hi || rank < need);
+  const uint64_t all = __ballot(on);
+  if (lane == 0) s_cnt[w] = __popcll(all);
+  __syncthreads();
+  int at = __popcll(all & ((1ull << lane) - 1ull));
+#pragma unroll
+  for (int v = 0; v < kFewWg / 64; ++v) at += v < w ? s_cnt[v] : 0;
+  if (on) out[at] = tid;
 }
 
 }  // namespace
@@ -230,8 +298,16 @@ hipError_t launch_page_scores(const SelectParams& p, bool bf16, hipStream_t s) {
                    : (p.c.dh == 128 ? k_page_scores<float, 128, 4> : k_page_scores<float, 64, 4>);
   auto one = bf16 ? (p.c.dh == 128 ? k_page_scores<__bf16, 128, 1> : k_page_scores<__bf16, 64, 1>)
                   : (p.c.dh == 128 ? k_page_scores<float, 128, 1> : k_page_scores<float, 64, 1>);
-  auto kern = p.rep == 1 ? one : many;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, p, np);
+  hipLaunchKernelGGL(p.rep == 1 ? one : many, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, p, np);
+  return hipGetLastError();
+}
+
+hipError_t launch_select_few(const SelectParams& p, bool bf16, hipStream_t s) {
+  auto many = bf16 ? (p.c.dh == 128 ? k_select_few<__bf16, 128, 4> : k_select_few<__bf16, 64, 4>)
+                   : (p.c.dh == 128 ? k_select_few<float, 128, 4> : k_select_few<float, 64, 4>);
+  auto one = bf16 ? (p.c.dh == 128 ? k_select_few<__bf16, 128, 1> : k_select_few<__bf16, 64, 1>)
+                  : (p.c.dh == 128 ? k_select_few<float, 128, 1> : k_select_few<float, 64, 1>);
+  hipLaunchKernelGGL(p.rep == 1 ? one : many, dim3(static_cast<unsigned>(p.B) * p.Tq * p.c.H), dim3(kFewWg), 0, s, p);
   return hipGetLastError();
 }
 

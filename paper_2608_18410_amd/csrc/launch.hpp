@@ -325,7 +325,8 @@ struct DecodePlan {
   size_t off_stat, off_x, bytes;  // of this call
   size_t ask;  // at least bytes of every call of no more sequences, queries and tokens
 };
-DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, bool tree = false);
+enum class DecodeKind { paged, tree, listed };
+DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, DecodeKind kind = DecodeKind::paged);
 hipError_t launch_decode(const DecodeParams& p, bool bf16, hipStream_t s);
 hipError_t launch_decode_tree(const DecodeParams& p, bool bf16, hipStream_t s);
 hipError_t launch_decode_listed(const DecodeParams& p, bool bf16, hipStream_t s);
@@ -364,8 +365,12 @@ struct SelectParams {
   int ld;         // pages of max_len
   float* scores;  // [B][Tq][H][ld]
   int32_t* counts;  // [B][Tq][H] pages that a query sees
+  int n_sel, first, recent;
+  int32_t* sel;  // [B][Tq][H][n_sel]
 };
+constexpr int kFewPages = 512;  // up to which launch_select_few takes a call whole
 hipError_t launch_page_scores(const SelectParams& p, bool bf16, hipStream_t s);
+hipError_t launch_select_few(const SelectParams& p, bool bf16, hipStream_t s);
 
 struct TurnParams {
   int B, T, H, Hkv, dh, n_axes, n_pairs, interleaved;  // a head count of 0: that tensor is absent

@@ -974,7 +974,7 @@ rolesub_status check_attend(const char* fn, rolesub_dtype dtype, rolesub_dtype o
 // p.max_len tokens (`seqs` sequences in the table); `more`: what else must not change.
 rolesub_status set_attend(const char* fn, DecodeParams& p, rolesub_dtype dtype, int32_t Hq, const void* q, int64_t q_stride,
                           const int32_t* table, int32_t max_pages, const void* R, float scale, void* out,
-                          rolesub_dtype out_dtype, void* workspace, size_t ws_bytes, int32_t seqs,
+                          rolesub_dtype out_dtype, void* workspace, size_t ws_bytes, int32_t seqs, DecodeKind kind,
                           std::initializer_list<Operand> more) {
   const PagedCache& c = p.c;
   const size_t e = esize(dtype), nq = static_cast<size_t>(p.B) * p.Tq;
@@ -995,7 +995,7 @@ rolesub_status set_attend(const char* fn, DecodeParams& p, rolesub_dtype dtype, 
   p.scale = static_cast<float>((scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(c.dh)) : scale) * 1.44269504088896341);
   p.out = out;
   p.out_f32 = out_dtype == ROLESUB_F32;
-  const DecodePlan d = decode_plan(p.B, c.H, p.R, c.dh, p.max_len, false, p.tree != nullptr);
+  const DecodePlan d = decode_plan(p.B, c.H, p.R, c.dh, p.max_len, false, kind);
   if (d.bytes > 0 && (!workspace || ws_bytes < d.bytes))
     return fail(ROLESUB_ERR_INVALID_ARG, "%s: workspace of %zu bytes needed, %zu given", fn, d.bytes,
                 workspace ? ws_bytes : static_cast<size_t>(0));
@@ -1471,7 +1471,7 @@ rolesub_status rolesub_tree_masks(int32_t B, int32_t T, const int32_t* parents, 
 size_t rolesub_attend_tree_workspace_size(const rolesub_pages* pages, int32_t B, int32_t Hq, int32_t Tq, int32_t max_len) {
   if (!pages || B <= 0 || pages->H < 1 || Hq < pages->H || Tq <= 0 || max_len <= 0) return 0;
   if (static_cast<size_t>(Hq / pages->H) * Tq > 0x7FFFFFFF) return 0;
-  return decode_plan(B, pages->H, Hq / pages->H * Tq, pages->dh, max_len, false, true).ask;
+  return decode_plan(B, pages->H, Hq / pages->H * Tq, pages->dh, max_len, false, DecodeKind::tree).ask;
 }
 
 rolesub_status rolesub_attend_tree(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t Hq, int32_t Tq,
@@ -1503,7 +1503,7 @@ rolesub_status rolesub_attend_tree(const rolesub_pages* pages, rolesub_dtype dty
   p.trees = trees;
   const size_t nq = static_cast<size_t>(B) * Tq;
   st = set_attend(fn, p, dtype, Hq, q, q_stride, table, max_pages, R, scale, out, out_dtype, workspace, ws_bytes, B,
-                  {{"lens", lens, static_cast<size_t>(B) * 4}, {"n_new", n_new, static_cast<size_t>(B) * 4},
+                  DecodeKind::tree, {{"lens", lens, static_cast<size_t>(B) * 4}, {"n_new", n_new, static_cast<size_t>(B) * 4},
                    {"tree", tree, (trees > 1 ? nq : Tq) * ((Tq + 31) / 32) * 4}});
   if (st) return st;
   return from_hip(launch_decode_tree(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
@@ -1625,8 +1625,8 @@ rolesub_status rolesub_select_pages(const rolesub_pages* pages, rolesub_dtype dt
   p.q_stride = q_stride;
   if ((st = check_rows(fn, "q", q, p.q_stride, Hq, p.c.dh, esize(dtype)))) return st;
   const size_t e = esize(dtype), nq = static_cast<size_t>(B) * Tq, qrow = static_cast<size_t>(Hq) * p.c.dh;
-  // the selection has up to 64 workgroups of 512 threads a row
-  if (static_cast<double>(nq) * p.c.H * 64 * 512 >= static_cast<double>(kMaxThreads) ||
+  // the selection has a workgroup of up to 1024 threads a row, of more than 16384 pages 64 of 512
+  if (static_cast<double>(nq) * p.c.H * (ml / p.c.page < 16384 ? 1024 : 64 * 512) >= static_cast<double>(kMaxThreads) ||
       static_cast<double>(Hq / p.c.H) * Tq > 0x7FFFFFFF || n_sel > (1 << 30) ||
       static_cast<double>(B) * p.c.H * ((ml / p.c.page + 33) / 32) * 256 >= static_cast<double>(kMaxThreads))
     return fail(ROLESUB_ERR_UNSUPPORTED, "%s: too many sequences, heads, queries or pages", fn);
@@ -1657,7 +1657,12 @@ rolesub_status rolesub_select_pages(const rolesub_pages* pages, rolesub_dtype dt
   p.ld = static_cast<int>(d.ld);
   p.scores = reinterpret_cast<float*>(ws);
   p.counts = reinterpret_cast<int32_t*>(ws + d.off_count);
+  p.n_sel = n_sel;
+  p.first = first;
+  p.recent = recent;
+  p.sel = sel;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (p.ld <= kFewPages) return from_hip(launch_select_few(p, dtype == ROLESUB_BF16, s), fn);
   const hipError_t err = launch_page_scores(p, dtype == ROLESUB_BF16, s);
   if (err != hipSuccess) return from_hip(err, fn);
   EvictParams ev = {static_cast<int>(d.rows), p.ld, n_sel, first, recent, p.scores, d.ld, p.counts, sel,
@@ -1698,7 +1703,7 @@ rolesub_status rolesub_attend_selected(const rolesub_pages* pages, rolesub_dtype
   p.sel = sel;
   p.n_sel = n_sel;
   st = set_attend(fn, p, dtype, Hq, q, q_stride, table, max_pages, R, scale, out, out_dtype, workspace, ws_bytes, B,
-                  {{"lens", lens, static_cast<size_t>(B) * 4}, {"visible", visible, nq * 4},
+                  DecodeKind::listed, {{"lens", lens, static_cast<size_t>(B) * 4}, {"visible", visible, nq * 4},
                    {"sel", sel, nq * p.c.H * n_sel * 4}});
   if (st) return st;
   return from_hip(launch_decode_listed(p, dtype == ROLESUB_BF16, static_cast<hipStream_t>(stream)), fn);
