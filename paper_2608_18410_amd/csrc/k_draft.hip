@@ -1,5 +1,7 @@
 // Drafted tokens that form a tree: the bits of their ancestors, and the accepted path
 // moved behind the cached tokens.
+#include <algorithm>
+
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -58,15 +60,16 @@ struct Path {
   int n;        // tokens on it
   int64_t len;  // cached tokens before it
 };
+template <int NT>
 __device__ __forceinline__ Path path_of(const AcceptParams& p, int b, int16_t* s_path, int* wsum, int* s_n) {
   const int tid = threadIdx.x, words = (p.T + 31) / 32, leaf = p.leaf[b];
   const int64_t cap = static_cast<int64_t>(p.max_pages) << p.c.shift;
   bool on = false;
   if (tid < p.T && leaf >= 0 && leaf < p.T)
     on = (p.tree[((p.trees > 1 ? static_cast<int64_t>(b) * p.T : 0) + leaf) * words + tid / 32] >> (tid % 32)) & 1u;
-  const int before = group_scan<256, false>(on, wsum);
+  const int before = group_scan<NT, false>(on, wsum);
   if (on) s_path[before] = static_cast<int16_t>(tid);
-  if (tid == 255) *s_n = before + on;
+  if (tid == NT - 1) *s_n = before + on;
   __syncthreads();
   return Path{*s_n, min(static_cast<int64_t>(max(p.lens[b], 0)), cap)};
 }
@@ -89,6 +92,7 @@ struct Move {
   uint32_t mask;
   int old_slot, slot;
 };
+template <int NT>
 __device__ __forceinline__ Move move_of(const AcceptParams& p, int b, const Path& path, const int16_t* s_path, int* wsum, int* s_sum) {
   const PagedCache& c = p.c;
   const int tid = threadIdx.x, r0 = static_cast<int>(path.len & (c.page - 1));
@@ -108,11 +112,11 @@ __device__ __forceinline__ Move move_of(const AcceptParams& p, int b, const Path
       used = c.slot[at] + __popc(c.mask[at] & gm);
     }
   }
-  const int before = group_scan<256, true>(__popc(m.mask & gm), wsum);
-  s_sum[tid] = before;
+  const int before = group_scan<NT, true>(__popc(m.mask & gm), wsum);
+  if (tid < kMaxTree) s_sum[tid] = before;
   __syncthreads();
   const int first = max(((r0 + tid) & ~(c.page - 1)) - r0, 0);  // of the path's tokens in this page
-  m.slot = used + before - s_sum[first];
+  if (tid < path.n) m.slot = used + before - s_sum[first];
   return m;
 }
 
@@ -120,23 +124,26 @@ __device__ __forceinline__ Move move_of(const AcceptParams& p, int b, const Path
 // and so do their groups within a page, so what a step of the loop writes is read by no
 // later one; within a step everything is read before anything is written. A page's other
 // heads are other workgroups' and the masks and slots that all of them read are written
-// by the next launch. VB: bytes of a value piece, the group's or 16.
+// by the next launch, unless a workgroup has all heads (WHOLE). VB: bytes of a value
+// piece, the group's or 16. A chain of dependent loads: one of 8 drafted tokens and 32
+// heads see launch_accept.
 template <int VB> struct Bytes;
 template <> struct Bytes<4> { typedef uint32_t t; };
 template <> struct Bytes<8> { typedef u32x2 t; };
 template <> struct Bytes<16> { typedef u32x4 t; };
-template <int VB>
-__global__ __launch_bounds__(256) void k_accept(AcceptParams p, int hpb, int e) {
+template <int VB, int NT, bool WHOLE>
+__global__ __launch_bounds__(NT) void k_accept(AcceptParams p, int hpb, int e) {
   typedef typename Bytes<VB>::t piece;
   __shared__ int16_t s_path[kMaxTree];
-  __shared__ int wsum[4], s_n, s_sum[256];
+  __shared__ int wsum[NT / 64], s_n, s_sum[kMaxTree];
   __shared__ int64_t s_kfrom[kMaxTree], s_kto[kMaxTree], s_vfrom[kMaxTree], s_vto[kMaxTree];  // of head 0
   __shared__ int s_old[kMaxTree], s_new[kMaxTree], s_cnt[kMaxTree];
   const PagedCache& c = p.c;
   const int b = blockIdx.x, tid = threadIdx.x;
-  const Path path = path_of(p, b, s_path, wsum, &s_n);
+  const Path path = path_of<NT>(p, b, s_path, wsum, &s_n);
+  if (WHOLE && tid == 0 && p.new_lens) p.new_lens[b] = static_cast<int32_t>(path.len + path.n);
   if (path.n == 0) return;
-  const Move m = move_of(p, b, path, s_path, wsum, s_sum);
+  const Move m = move_of<NT>(p, b, path, s_path, wsum, s_sum);
   const int row = c.dh * e, gb = c.ds * e;
   if (tid < path.n) {
     auto rows = [&](Place x) { return ((static_cast<int64_t>(x.page) * c.H) << c.shift) + x.row; };
@@ -152,14 +159,14 @@ __global__ __launch_bounds__(256) void k_accept(AcceptParams p, int hpb, int e) 
   __syncthreads();
   const int h0 = blockIdx.y * hpb, nh = min(hpb, c.H - h0);
   const int kp = row / 16, vp = row / VB, gp = gb / VB, per = kp + vp, items = path.n * nh * per;
-  for (int u0 = 0; u0 < items; u0 += 256 * 4) {
+  for (int u0 = 0; u0 < items; u0 += NT * 4) {
     u32x4 xk[4];
     piece xv[4];
     char* to[4];
     bool key[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int u = u0 + 256 * i + tid, q = u % per, h = h0 + u / per % nh, t = u / (per * nh);
+      const int u = u0 + NT * i + tid, q = u % per, h = h0 + u / per % nh, t = u / (per * nh);
       to[i] = nullptr;
       key[i] = q < kp;
       if (u >= items || s_kto[t] < 0) continue;
@@ -189,18 +196,23 @@ __global__ __launch_bounds__(256) void k_accept(AcceptParams p, int hpb, int e) 
         *reinterpret_cast<piece*>(to[i]) = xv[i];
     }
   }
+  if (WHOLE && tid < path.n && m.to.page >= 0) {
+    const int64_t at = (static_cast<int64_t>(m.to.page) << c.shift) + m.to.row;
+    c.mask[at] = m.mask;
+    c.slot[at] = m.slot;
+  }
 }
 
 // Their masks and slots, and the new lengths.
 __global__ __launch_bounds__(256) void k_accept_meta(AcceptParams p) {
   __shared__ int16_t s_path[kMaxTree];
-  __shared__ int wsum[4], s_n, s_sum[256];
+  __shared__ int wsum[4], s_n, s_sum[kMaxTree];
   const PagedCache& c = p.c;
   const int b = blockIdx.x, tid = threadIdx.x;
-  const Path path = path_of(p, b, s_path, wsum, &s_n);
+  const Path path = path_of<256>(p, b, s_path, wsum, &s_n);
   if (tid == 0 && p.new_lens) p.new_lens[b] = static_cast<int32_t>(path.len + path.n);
   if (path.n == 0) return;
-  const Move m = move_of(p, b, path, s_path, wsum, s_sum);
+  const Move m = move_of<256>(p, b, path, s_path, wsum, s_sum);
   __syncthreads();  // all is read
   if (tid < path.n && m.to.page >= 0) {
     const int64_t at = (static_cast<int64_t>(m.to.page) << c.shift) + m.to.row;
@@ -216,10 +228,18 @@ hipError_t launch_tree_masks(const TreeParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+constexpr int64_t kWholePieces = 32768;
 hipError_t launch_accept(const AcceptParams& p, bool bf16, hipStream_t s) {
   const int e = bf16 ? 2 : 4, gb = p.c.ds * e;
+  // few pieces: one workgroup a sequence, without the second launch
+  const int64_t pieces = static_cast<int64_t>(p.T) * p.c.H * (p.c.dh * e / 16 + p.c.dh * e / std::min(gb, 16));
+  if (pieces <= kWholePieces) {
+    auto kern = gb >= 16 ? k_accept<16, 1024, true> : gb == 8 ? k_accept<8, 1024, true> : k_accept<4, 1024, true>;
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(p.B)), dim3(1024), 0, s, p, p.c.H, e);
+    return hipGetLastError();
+  }
   constexpr int hpb = 4;
-  auto kern = gb >= 16 ? k_accept<16> : gb == 8 ? k_accept<8> : k_accept<4>;
+  auto kern = gb >= 16 ? k_accept<16, 256, false> : gb == 8 ? k_accept<8, 256, false> : k_accept<4, 256, false>;
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(p.B), (p.c.H + hpb - 1) / hpb), dim3(256), 0, s, p, hpb, e);
   hipLaunchKernelGGL(k_accept_meta, dim3(static_cast<unsigned>(p.B)), dim3(256), 0, s, p);
   return hipGetLastError();

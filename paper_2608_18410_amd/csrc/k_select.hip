@@ -12,9 +12,9 @@ namespace {
 // Bounds of a page's keys in every dim, a wave for each page and head: 16-byte pieces of
 // its rows, then the lanes of one piece. fminf and fmaxf pass over NaN. Whole pages are
 // gone over again, as what a page holds may have moved.
-template <class T, int DH>
+template <class T, int DH, int U>
 __global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
-  constexpr int V = 16 / sizeof(T), LPR = DH / V, RPI = 64 / LPR, U = 4;
+  constexpr int V = 16 / sizeof(T), LPR = DH / V, RPI = 64 / LPR;
   const PagedCache& c = p.c;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + w, pages = static_cast<int64_t>(p.B) * np;
@@ -283,8 +283,12 @@ __global__ __launch_bounds__(kFewWg) void k_select_few(SelectParams p) {
 hipError_t launch_page_bounds(const BoundsParams& p, bool bf16, hipStream_t s) {
   const int np = static_cast<int>(std::min<int64_t>(p.max_pages, ((p.c.page - 1 + static_cast<int64_t>(p.T) - 1) >> p.c.shift) + 1));
   const int64_t jobs = static_cast<int64_t>(p.B) * np * p.c.H;
-  auto kern = bf16 ? (p.c.dh == 128 ? k_page_bounds<__bf16, 128> : k_page_bounds<__bf16, 64>)
-                   : (p.c.dh == 128 ? k_page_bounds<float, 128> : k_page_bounds<float, 64>);
+  // loads of a wave in flight: a page's of up to 16 KB
+  auto some = bf16 ? (p.c.dh == 128 ? k_page_bounds<__bf16, 128, 4> : k_page_bounds<__bf16, 64, 4>)
+                   : (p.c.dh == 128 ? k_page_bounds<float, 128, 4> : k_page_bounds<float, 64, 4>);
+  auto many = bf16 ? (p.c.dh == 128 ? k_page_bounds<__bf16, 128, 16> : k_page_bounds<__bf16, 64, 16>)
+                   : (p.c.dh == 128 ? k_page_bounds<float, 128, 16> : k_page_bounds<float, 64, 16>);
+  auto kern = p.c.page * p.c.dh * (bf16 ? 2 : 4) <= 4096 ? some : many;
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((jobs + 3) / 4)), dim3(256), 0, s, p, np);
   return hipGetLastError();
 }

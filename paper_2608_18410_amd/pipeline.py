@@ -5,7 +5,9 @@ four library calls are issued in order on one stream. A batch may also be
 split into micro-batches (contiguous ranges of prefixes, each with views of
 the buffers and its own route workspace) whose calls run on separate streams.
 For decoding token by token, decode_layer grows a paged cache by the new tokens
-and attends from them, and evict_layer takes it back to a budget.
+and attends from them, over all of it or over the pages that promise most, and
+evict_layer takes it back to a budget; draft_layer does the same for drafted tokens
+that form a tree, and accept_layer keeps the path of the last accepted one.
 """
 from __future__ import annotations
 
@@ -162,27 +164,81 @@ def page_count(tokens: int, page: int) -> int:
 def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.PagedCache, table, lens, new_lens,
                  positions=None, inv_freq=None, axis=None, router: rs.Router | None = None, scores_in=None,
                  visible=None, max_len: int = 0, mass=None, decay: float = 1.0, workspace=None, out=None,
-                 stream=None):
-    """The next T tokens of every sequence through one layer: route -> rotary ->
-    rotate -> append -> attend. h [B,T,d], q [B,T,Hq,dh], k and v [B,T,H,dh]; lens are
+                 stream=None, q_weight=None, k_weight=None, eps: float = 1e-6, bounds=None, n_sel: int = 0,
+                 first: int = 1, recent: int = 2):
+    """The next T tokens of every sequence through one layer: route -> append (keys
+    turned, values rotated) -> attend. h [B,T,d], q [B,T,Hq,dh], k and v [B,T,H,dh]; lens are
     the cached tokens before them, new_lens = lens + T after (one pair of tensors
     serves every layer of a stack). Without positions the keys and queries are taken
     as they are. visible defaults to all cached and new tokens, as a chunk of actions
     decoded in parallel sees itself whole; the tokens of a causal prompt (T > 1) must
     pass visible[b, j] = lens[b] + j + 1. With mass the tokens' weight is accumulated
     for evict_layer: past the cached tokens it must hold zeros, as evict_layer leaves
-    it, since new tokens add to what is there. Returns the attention output
-    [B,T,Hq,dh]."""
+    it, since new tokens add to what is there. q_weight and k_weight [dh] norm the heads
+    before they are turned (they need positions). With n_sel each query attends to n_sel
+    pages only, the first, the recent and those whose bounds [n_pages,H,2,dh] promise the
+    highest scores; the bounds of the new tokens' pages are brought up to date on the way
+    (page_bounds with T >= the longest length makes them all), and no weight is
+    accumulated. Returns the attention output [B,T,Hq,dh]."""
+    if n_sel and mass is not None:
+        raise ValueError("mass: no weight is accumulated where few pages are attended to")
+    if n_sel and bounds is None:
+        raise ValueError("n_sel needs bounds")
+    if positions is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("q_weight and k_weight need positions")
     with _current_stream(stream):
         mask = rs.route(types, budget, G, h=h, router=router, scores_in=scores_in, want_scores=False, want_idx=False,
                         want_count=False)["mask"]
-        if positions is not None:
-            q, k = rs.rotary(q, k, positions, inv_freq, axis)
-        z = rs.rotate_values(v, R)
-        rs.cache_append(cache, k, z, mask, table, lens)
-        out = rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
-                              workspace=workspace, out=out)
+        q = _append(cache, q, k, v, R, mask, table, lens, positions, inv_freq, axis, q_weight, k_weight, eps)
+        if n_sel:
+            rs.page_bounds(cache, table, new_lens, bounds, q.shape[1])
+            sel = rs.select_pages(q, cache, bounds, table, new_lens, n_sel, first=first, recent=recent, visible=visible,
+                                  max_len=max_len)
+            out = rs.attend_selected(q, cache, table, new_lens, sel, R, visible=visible, workspace=workspace, out=out)
+        else:
+            out = rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
+                                  workspace=workspace, out=out)
     return _returned(stream, out)[0]
+
+
+def _append(cache, q, k, v, R, mask, table, lens, positions, inv_freq, axis, q_weight=None, k_weight=None, eps=1e-6,
+            n_new=None):
+    """New tokens into their pages, turned where they have positions. Returns the queries."""
+    if positions is not None:
+        return rs.append_rotary(cache, k, v, mask, table, lens, positions, inv_freq, axis, R=R, q=q, q_weight=q_weight,
+                                k_weight=k_weight, eps=eps, n_new=n_new)
+    z = rs.rotate_values(v, R)
+    rs.cache_append(cache, k, z, mask, table, lens, **({} if n_new is None else {"n_new": n_new}))
+    return q
+
+
+def draft_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.PagedCache, table, lens, tree,
+                positions=None, inv_freq=None, axis=None, router: rs.Router | None = None, scores_in=None, n_new=None,
+                max_len: int = 0, workspace=None, out=None, stream=None, q_weight=None, k_weight=None,
+                eps: float = 1e-6):
+    """T drafted tokens of every sequence through one layer, as decode_layer's, each attending
+    to the lens cached tokens and to its ancestors: tree [B or 1,T,ceil(T/32)] as tree_masks
+    makes it, whose depth gives positions = lens + depth. n_new [B] (None: T): drafted
+    tokens of each sequence. The cache holds them behind lens until accept_layer, or the
+    next append there. Returns the attention output [B,T,Hq,dh]."""
+    if positions is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("q_weight and k_weight need positions")
+    with _current_stream(stream):
+        mask = rs.route(types, budget, G, h=h, router=router, scores_in=scores_in, want_scores=False, want_idx=False,
+                        want_count=False)["mask"]
+        q = _append(cache, q, k, v, R, mask, table, lens, positions, inv_freq, axis, q_weight, k_weight, eps, n_new)
+        out = rs.attend_tree(q, cache, table, lens, tree, R, n_new=n_new, max_len=max_len, workspace=workspace, out=out)
+    return _returned(stream, out)[0]
+
+
+def accept_layer(cache: rs.PagedCache, table, lens, tree, leaf, bounds=None, new_lens=None, stream=None):
+    """Of the drafted tokens behind lens those on the path of token leaf [B] (-1: none) stay.
+    With bounds those of the pages they lie in are made again. Returns the new lengths [B]."""
+    with _current_stream(stream):
+        new_lens = rs.cache_accept(cache, table, lens, tree, leaf, new_lens)
+        if bounds is not None:
+            rs.page_bounds(cache, table, new_lens, bounds, tree.shape[1])
+    return _returned(stream, new_lens)[0]
 
 
 def evict_layer(cache: rs.PagedCache, table, lens, mass, keep: int, first: int, recent: int, dst: rs.PagedCache,

@@ -13,7 +13,7 @@ import torch
 
 import paper_2608_18410_amd as rs
 from oracle import paged as O
-from paper_2608_18410_amd.pipeline import page_count
+from paper_2608_18410_amd.pipeline import accept_layer, decode_layer, draft_layer, page_count
 from tests._gpu_util import DEV
 from tests.test_gpu_paged import EPS, HALF, bf, case, dev, f32, full_cache, i32, ints, num, rotations, to_np
 
@@ -615,3 +615,247 @@ def test_workspaces_of_larger_calls_serve_smaller_ones():
         assert torch.equal(sel, rs.select_pages(*a, bd, *at, k, max_len=ml))
         ws.fill_(255)
         assert torch.equal(rs.attend_selected(*a, *at, sel, workspace=ws), rs.attend_selected(*a, *at, sel))
+
+
+# ---- together ----------------------------------------------------------------
+
+class Model:
+    """One layer's weights and a generator of its inputs."""
+
+    def __init__(self, seed, dtype, B, H=2, rep=2, dh=64, G=8, P=16, W=12):
+        self.rng = np.random.default_rng(seed)
+        self.g = torch.Generator(device=DEV).manual_seed(seed)
+        self.dtype, self.B, self.H, self.rep, self.dh, self.G = dtype, B, H, rep, dh, G
+        self.R = rotations(self.rng, H, dh, dtype)
+        self.w = [dev(1 + 0.1 * self.rng.standard_normal(dh), dtype) for _ in range(2)]
+        self.f = torch.from_numpy((100.0 ** (-np.arange(dh // 2) / (dh // 2))).astype(np.float32)).to(DEV)
+        self.budget = rs.make_budget(rs.TOPK, (3, 5, G, 1))
+        self.cache = full_cache(self.rng, B * W, P, H, dh, G, G, dtype)
+        self.table = ints(self.rng.permutation(B * W).reshape(B, W))
+
+    def tokens(self, T):
+        r = lambda *s, dtype=self.dtype: torch.randn(s, generator=self.g, device=DEV, dtype=dtype)  # noqa: E731
+        return dict(q=r(self.B, T, self.H * self.rep, self.dh), k=r(self.B, T, self.H, self.dh), v=r(self.B, T, self.H, self.dh),
+                    types=torch.randint(0, 4, (self.B, T), generator=self.g, device=DEV).to(torch.uint8),
+                    scores=r(self.B, T, self.G, dtype=f32))
+
+    def clone(self):
+        return rs.PagedCache(*(x.clone() for x in self.cache.tensors()))
+
+    def common(self, x, cache):
+        return (None, x["q"], x["k"], x["v"], x["types"], self.R, self.budget, self.G, cache, self.table)
+
+    def kw(self):
+        return dict(inv_freq=self.f, q_weight=self.w[0], k_weight=self.w[1])
+
+
+def _pick(x, b_path):
+    """Of each sequence b its tokens b_path[b] ([B] lists of one length)."""
+    at = torch.tensor(b_path, device=DEV)
+    return {n: torch.stack([t[b, at[b]] for b in range(t.shape[0])]).contiguous() for n, t in x.items()}
+
+
+def _apart(m):
+    """How far two calls that sum the same terms may be apart before they round: weights of 17 bits and 2^-17 of the rest
+    (see _held), of sums no larger than sqrt(dh) (a rotation's rows) times the largest value."""
+    return 2.0 ** -15 * m.dh ** 0.5 * float(m.cache.V.abs().max())
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+def test_drafted_tokens_decode_as_if_one_by_one(dtype):
+    """Two rounds of draft, attend and accept, against a cache that is decoded along each path."""
+    m = Model(1, dtype, 3)
+    prompt = m.tokens(40)
+    zero, lens = ints([0] * 3), ints([40] * 3)
+    pos = torch.arange(40, device=DEV, dtype=i32).expand(3, 40).contiguous()
+    decode_layer(*m.common(prompt, m.cache), zero, lens, positions=pos, scores_in=prompt["scores"], visible=pos + 1, **m.kw())
+    plain = m.clone()
+    T, par = 9, [[-1, 0, 0, 1, 2, 2, -1, 6, 4], [-1, 0, 1, 2, 3, 4, 5, 6, 7], [-1, -1, -1, 0, 1, 2, 3, 4, 6]]
+    for step in range(2):
+        x = m.tokens(T)
+        tree, depth = rs.tree_masks(ints(par))
+        out = draft_layer(*m.common(x, m.cache), lens, tree, positions=lens[:, None] + depth, scores_in=x["scores"], **m.kw())
+        sets = O.tree_masks(par)[0]
+        leaf = [5, 2, 6] if step == 0 else [8, 3, 8]
+        paths = [sorted(sets[b][leaf[b]]) for b in range(3)]
+        assert len({len(p) for p in paths}) == 1
+        n1 = lens
+        for i in range(len(paths[0])):
+            y = _pick(x, [[p[i]] for p in paths])
+            one = decode_layer(*m.common(y, plain), n1, n1 + 1, positions=n1[:, None], scores_in=y["scores"], **m.kw())
+            want, got = num(one), np.stack([num(out[b, paths[b][i]]) for b in range(3)])[:, None]
+            assert (np.abs(want - got) <= 2 * HALF[dtype] * np.abs(want) + _apart(m)).all()
+            n1 = n1 + 1
+        lens = accept_layer(m.cache, m.table, lens, tree, ints(leaf))
+        assert torch.equal(lens, n1)
+        a, b = to_np(m.cache), to_np(plain)
+        for s in range(3):
+            for t in range(int(lens[s])):
+                u, v = O.token(a, m.table[s].tolist(), t), O.token(b, m.table[s].tolist(), t)
+                assert all(np.array_equal(p, q) for p, q in zip(u, v)), (s, t)
+    y = m.tokens(1)
+    outs = [decode_layer(*m.common(y, c), lens, lens + 1, positions=lens[:, None], scores_in=y["scores"], **m.kw()) for c in (m.cache, plain)]
+    assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+def test_decoding_over_few_pages(dtype):
+    m = Model(2, dtype, 3)
+    bounds = torch.zeros((m.cache.K.shape[0], m.H, 2, m.dh), device=DEV, dtype=dtype)
+    lens = ints([0] * 3)
+    plain = m.clone()
+    for T in (70, 1, 1, 9, 16, 1, 33):
+        x = m.tokens(T)
+        pos = lens[:, None] + torch.arange(T, device=DEV, dtype=i32)
+        kw = dict(positions=pos, scores_in=x["scores"], visible=pos + 1, **m.kw())
+        few = decode_layer(*m.common(x, m.cache), lens, lens + T, bounds=bounds, n_sel=4, **kw)
+        everything = decode_layer(*m.common(x, plain), lens, lens + T, **kw)
+        lens = lens + T
+        assert all(same(a, b) for a, b in zip(m.cache.tensors(), plain.tensors()))
+        ref = num(bounds).copy()
+        O.page_bounds(to_np(m.cache), m.table.cpu().numpy(), lens.tolist(), ref, 10 ** 6)
+        assert np.array_equal(num(bounds), ref)
+        # (the turned queries as the layer makes them)
+        q = rs.norm_rotary(x["q"], None, m.w[0], None, 1e-6, pos, m.f)[0]
+        sel = rs.select_pages(q, m.cache, bounds, m.table, lens, 4, 1, 2, visible=pos + 1)
+        assert torch.equal(few, rs.attend_selected(q, m.cache, m.table, lens, sel, m.R, visible=pos + 1))
+        seen = ((pos + 1).max() + 15) // 16
+        if int(seen) <= 4:
+            err = (few.double() - everything.double()).abs()
+            assert bool((err <= 2 * HALF[dtype] * everything.double().abs() + _apart(m)).all())
+        whole = rs.select_pages(q, m.cache, bounds, m.table, lens, m.table.shape[1], visible=pos + 1)
+        got = rs.attend_selected(q, m.cache, m.table, lens, whole, m.R, visible=pos + 1)
+        err = (got.double() - everything.double()).abs()
+        assert bool((err <= 2 * HALF[dtype] * everything.double().abs() + _apart(m)).all())
+
+
+def _buffers(m, T):
+    return dict(tree=torch.empty((m.B, T, 1), device=DEV, dtype=i32), depth=torch.empty((m.B, T), device=DEV, dtype=i32),
+                out=torch.empty((m.B, T, m.H * m.rep, m.dh), device=DEV, dtype=m.dtype), new=torch.empty(m.B, device=DEV, dtype=i32),
+                one=torch.empty((m.B, 1, m.H * m.rep, m.dh), device=DEV, dtype=m.dtype),
+                ws=torch.empty(max(rs.attend_tree_workspace_size(m.cache, m.B, m.H * m.rep, T, 192),
+                                   rs.attend_selected_workspace_size(m.cache, m.B, m.H * m.rep, 1, 5), 1), device=DEV, dtype=torch.uint8))
+
+
+def test_draft_accept_and_few_pages_graph_replays():
+    """A whole step captured: masks, drafted tokens, the accepted path, then a token over few pages."""
+    m = Model(3, bf, 3)
+    T, start = 6, ints([30, 15, 61])
+    other, orig = m.clone(), m.clone()
+    x, y = m.tokens(T), m.tokens(1)
+    par, leaf, lens = ints([[-1, 0, 0, 1, 2, 4]] * 3), ints([5, 3, 0]), start.clone()
+    bounds = torch.stack((m.cache.K.amin(2), m.cache.K.amax(2)), 2).contiguous()
+    first_bounds, b = bounds.clone(), _buffers(m, T)
+
+    def step(cache, bounds, x, y, lens, b):
+        rs.tree_masks(par, out=(b["tree"], b["depth"]))
+        draft_layer(*m.common(x, cache), lens, b["tree"], positions=lens[:, None] + b["depth"], scores_in=x["scores"], workspace=b["ws"],
+                    out=b["out"], **m.kw())
+        accept_layer(cache, m.table, lens, b["tree"], leaf, bounds=bounds, new_lens=b["new"])
+        decode_layer(*m.common(y, cache), b["new"], b["new"] + 1, positions=b["new"][:, None], scores_in=y["scores"], bounds=bounds,
+                     n_sel=5, workspace=b["ws"], out=b["one"], **m.kw())
+        lens.copy_(b["new"] + 1)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(m.cache, bounds, x, y, lens, b)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(m.cache, bounds, x, y, lens, b)
+    lens.copy_(start)
+    bounds.copy_(first_bounds)
+    for a, o in zip(m.cache.tensors(), orig.tensors()):
+        a.copy_(o)
+    lens1, bounds1, b1 = start.clone(), first_bounds.clone(), _buffers(m, T)
+    for i in range(6):
+        for d, n in ((x, m.tokens(T)), (y, m.tokens(1))):
+            for k in d:
+                d[k].copy_(n[k])
+        par.copy_(ints(random_parents(m.rng, 3, T)))
+        leaf.copy_(ints(m.rng.integers(-1, T, 3)))
+        for k in ("tree", "depth", "new"):
+            b[k].fill_(-7)
+        b["out"].fill_(float("nan"))
+        b["ws"].fill_(255)
+        graph.replay()
+        step(other, bounds1, x, y, lens1, b1)
+        torch.cuda.synchronize()
+        assert torch.equal(lens, lens1) and same(bounds, bounds1), i
+        for k in ("tree", "depth", "out", "new", "one"):
+            assert same(b[k], b1[k]), (i, k)
+        for a, o in zip(m.cache.tensors(), other.tensors()):
+            assert same(a, o), i
+
+
+def test_two_streams_at_once():
+    """Two layers with their own caches and workspaces give the bits of one after the other; what a call with stream= makes
+    is ready for the caller after the stream."""
+    ms = [Model(i, bf, 3, dh=128, W=40) for i in (4, 5)]
+    xs = [m.tokens(9) for m in ms]
+    lens = ints([500, 300, 7])
+    par = ints([[-1, 0, 1, 1, 2, 3, 4, 5, 6]] * 3)
+    caches = [[m.clone() for m in ms] for _ in range(2)]
+
+    def run(i, c, stream=None):
+        m, x = ms[i], xs[i]
+        tree, depth = rs.tree_masks(par)
+        out = draft_layer(*m.common(x, c), lens, tree, positions=lens[:, None] + depth, scores_in=x["scores"], stream=stream, **m.kw())
+        new = accept_layer(c, m.table, lens, tree, ints([8, 4, -1]), stream=stream)
+        return out, new
+
+    want = [run(i, caches[0][i]) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        cs = [m.clone() for m in ms]
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        got = [run(i, cs[i], streams[i]) for i in range(2)]
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert same(got[i][0], want[i][0]) and torch.equal(got[i][1], want[i][1])
+            assert all(same(a, b) for a, b in zip(cs[i].tensors(), caches[0][i].tensors()))
+
+
+def test_far_pages():
+    """Pages, bounds and queries whose bytes lie past 2^32 of their tensors."""
+    H, P, dh, G, N = 8, 256, 128, 8, 4300
+    K = torch.empty((N, H, P, dh), dtype=bf, device=DEV)
+    V = torch.empty((N, H, P * G, dh // G), dtype=bf, device=DEV)
+    rng = np.random.default_rng(12)
+    small = full_cache(rng, 4, P, H, dh, G, G, bf)
+    c = rs.PagedCache(K, V, torch.zeros((N, P), dtype=i32, device=DEV), torch.zeros((N, P), dtype=i32, device=DEV))
+    far = [N - 1, N - 2, 4100, 0]
+    for i, p in enumerate(far):
+        for a, b in zip(c.tensors(), small.tensors()):
+            a[p] = b[i]
+    t, ts = ints([[N - 1, 4100], [N - 2, 0]]), ints([[0, 2], [1, 3]])
+    T = 5
+    k, v, q = (dev(rng.standard_normal((2, T, h, dh)), bf) for h in (H, H, H))
+    mask, pos, f = ints(rng.integers(0, 256, (2, T))), ints(rng.integers(0, 99, (2, T))), torch.rand(64, device=DEV)
+    n = ints([300, 255])
+    R = rotations(rng, H, dh, bf)
+    bd, bs = torch.zeros((N, H, 2, dh), device=DEV, dtype=bf), torch.zeros((4, H, 2, dh), device=DEV, dtype=bf)
+    tree, _ = rs.tree_masks(ints([[-1, 0, 0, 2, 1]] * 2))
+    outs = []
+    for cache, table, b in ((c, t, bd), (small, ts, bs)):
+        o = [rs.append_rotary(cache, k, v, mask, table, n, pos, f, R=R, q=q)]
+        o.append(rs.attend_tree(q, cache, table, n, tree, R))
+        o.append(rs.cache_accept(cache, table, n, tree, ints([3, 4])))
+        rs.page_bounds(cache, table, o[-1], b, 10 ** 6)
+        o.append(rs.select_pages(q, cache, b, table, o[2], 1))
+        o.append(rs.attend_selected(q, cache, table, o[2], o[3], R))
+        outs.append(o)
+    for a, b in zip(*outs):
+        assert same(a, b)
+    for i, p in enumerate(far):
+        assert same(bd[p], bs[i])
+        for a, b in zip(c.tensors(), small.tensors()):
+            assert same(a[p], b[i])

@@ -208,7 +208,7 @@ def lib_calls():
                 lens=0x51000000, n_new=0x52000000, visible=0x53000000, tree=0x54000000, parents=0x55000000, leaf=0x56000000,
                 bounds=0x57000000, qo=0x60000000, ko=0x61000000, out=0x62000000, sel=0x63000000, new=0x64000000, depth=0x65000000,
                 ws=0x80000000)
-    size = dict(B=3, T=2, Hq=4, H=2, dh=64, G=8, page=16, n_pages=5, vcap=64, W=20, dtype=rs.BF16, odt=rs.BF16, eps=1e-6, axes=3,
+    size = dict(B=3, T=2, Hq=4, H=2, dh=64, G=8, page=16, n_pages=5, vcap=64, W=60, dtype=rs.BF16, odt=rs.BF16, eps=1e-6, axes=3,
                 pairs=32, n_sel=40, first=1, recent=2, max_len=0, trees=3, scale=0.0, qs=0, ks=0, vs=0, wsb=1 << 26, Tb=1)
 
     def run(name, **kw):
@@ -378,6 +378,66 @@ def test_workspaces_grow_with_the_call():
                 assert all(p <= q for p, q in zip(last.get(a, now), now)), (x, a)
                 last[a] = now
     assert lib.rolesub_attend_tree_workspace_size(None, 1, 16, 1, 9) == lib.rolesub_select_pages_workspace_size(None, 1, 1, 9) == 0
+
+
+# ---- layers ------------------------------------------------------------------
+
+def test_layers_refuse_before_anything_runs():
+    from paper_2608_18410_amd.pipeline import decode_layer, draft_layer
+    for kw, why in ((dict(n_sel=4, bounds=1, mass=1), "no weight"), (dict(n_sel=4), "needs bounds"), (dict(q_weight=1), "need positions"),
+                    (dict(k_weight=1), "need positions")):
+        with pytest.raises(ValueError, match=why):
+            decode_layer(*[None] * 12, **kw)
+    for kw in (dict(q_weight=1), dict(k_weight=1)):
+        with pytest.raises(ValueError, match="need positions"):
+            draft_layer(*[None] * 12, **kw)
+
+
+@pytest.mark.parametrize("stream", [None, "side"])
+def test_layers_calls_and_streams(monkeypatch, stream):
+    """Which calls a layer makes, all with the chain's stream current, and whose its outputs are."""
+    from paper_2608_18410_amd import pipeline
+    made, marked, now = [], [], ["caller"]
+
+    class Out:
+        is_cuda, device, shape = True, "cuda:0", (2, 5)
+
+        def record_stream(self, s):
+            marked.append(s)
+
+    class On:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            now.append(self.s)
+
+        def __exit__(self, *a):
+            now.pop()
+
+    def call(name, out):
+        return lambda *a, **kw: (made.append((name, now[-1])), out)[1]
+
+    monkeypatch.setattr(pipeline.torch.cuda, "stream", On)
+    monkeypatch.setattr(pipeline.torch.cuda, "current_stream", lambda d=None: now[-1])
+    for name in ("append_rotary", "attend_paged", "attend_tree", "attend_selected", "cache_accept", "page_bounds", "select_pages",
+                 "rotate_values", "cache_append"):
+        monkeypatch.setattr(pipeline.rs, name, call(name, Out()))
+    monkeypatch.setattr(pipeline.rs, "route", call("route", {"mask": None}))
+    at = "caller" if stream is None else stream
+    tree = torch.zeros(2, 5, 1)
+    for run, want in (
+            (lambda: pipeline.decode_layer(*[None] * 12, positions=1, stream=stream), ["route", "append_rotary", "attend_paged"]),
+            (lambda: pipeline.decode_layer(*[None] * 12, positions=1, n_sel=3, bounds=1, stream=stream),
+             ["route", "append_rotary", "page_bounds", "select_pages", "attend_selected"]),
+            (lambda: pipeline.draft_layer(*[None] * 12, positions=1, stream=stream), ["route", "append_rotary", "attend_tree"]),
+            (lambda: pipeline.draft_layer(*[None] * 12, n_new=1, stream=stream), ["route", "rotate_values", "cache_append", "attend_tree"]),
+            (lambda: pipeline.accept_layer(None, None, None, tree, None, stream=stream), ["cache_accept"]),
+            (lambda: pipeline.accept_layer(None, None, None, tree, None, bounds=1, stream=stream), ["cache_accept", "page_bounds"])):
+        made.clear()
+        marked.clear()
+        run()
+        assert made == [(x, at) for x in want] and marked == ([] if stream is None else ["caller"])
 
 
 # ---- the assembly ------------------------------------------------------------
