@@ -145,7 +145,7 @@ struct Rotation {
   static constexpr int N = L::MB / 4;
   u32x4 a[N][L::KS];
   __device__ __forceinline__ void load(const DecodeParams& p, int h) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64 % 4, l16 = lane & 15, g4 = lane >> 4;
     if (!p.Rm) return;
     const T* R = static_cast<const T*>(p.Rm) + (static_cast<int64_t>(h) * DH + 16 * w + l16) * DH + g4 * L::EP;
 #pragma unroll
@@ -157,13 +157,14 @@ struct Rotation {
 
 // Output rows [r0, r0 + 16) of key head h from their normalised sums u (LDS, rows of
 // RLD floats; rows past R are zero): out = R_h u on the matrix cores, R's rows as
-// the product's rows. The sums enter as bf16 parts, or in f32. All 256 threads.
+// the product's rows. The sums enter as bf16 parts, or in f32. Four waves (of eight each
+// four with rows of their own).
 template <class T, int DH>
 __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h, int r0, const float* u,
                                             const Rotation<T, DH>& rot) {
   using L = Tile<T, DH>;
   constexpr int KS = L::KS, EP = L::EP, N = L::MB / 4;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid / 64 % 4, l16 = lane & 15, g4 = lane >> 4;
   const int r = r0 + l16;
   const float* ur = u + l16 * L::RLD;
   f32x4 o[N];
@@ -302,16 +303,16 @@ __device__ __forceinline__ View look(const DecodeParams& p, int b, int r, int le
 
 // The bits of N rows from r0 on, as words of LDS rows: loaded, and later put there by the
 // same threads.
-template <int N>
+template <int N, int NT>
 struct TreeBits {
-  static constexpr int kEach = (N * kTreeRow + 255) / 256;
+  static constexpr int kEach = (N * kTreeRow + NT - 1) / NT;
   uint32_t w[kEach];
   __device__ __forceinline__ void load(const DecodeParams& p, int b, int r0) {
     const int n = p.n_new ? min(max(p.n_new[b], 0), p.Tq) : p.Tq, words = (p.Tq + 31) / 32;
     const uint32_t* t = p.tree + (p.trees > 1 ? static_cast<int64_t>(b) * p.Tq * words : 0);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int u = threadIdx.x + 256 * i, r = r0 + u / kTreeRow, x = u % kTreeRow - 1, j = r / p.rep;
+      const int u = threadIdx.x + NT * i, r = r0 + u / kTreeRow, x = u % kTreeRow - 1, j = r / p.rep;
       w[i] = 0;
       if (u < N * kTreeRow && r < p.R && j < n && x >= 0 && 32 * x < n) {
         w[i] = t[j * words + x];
@@ -323,7 +324,7 @@ struct TreeBits {
   __device__ __forceinline__ void put(uint32_t* s_bits, int there) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int u = threadIdx.x + 256 * i, left = there - 32 * (u % kTreeRow - 1);
+      const int u = threadIdx.x + NT * i, left = there - 32 * (u % kTreeRow - 1);
       if (u < N * kTreeRow) s_bits[u] = left >= 32 ? w[i] : left > 0 ? w[i] & ((1u << left) - 1u) : 0u;
     }
   }
@@ -542,12 +543,12 @@ __device__ __forceinline__ void one_by_one(const DecodeParams& p, int b, int h, 
 }
 
 // The end of a split: the sums of the waves of each row block added in their order,
-// and left for k_join or, where there is no other split, finished. All 256 threads.
-template <class T, int DH, int WR>
+// and left for k_join or, where there is no other split, finished. All threads of WV waves.
+template <class T, int DH, int WR, int WV>
 __device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, int rtile, int sp, float m, float l,
                                           const f32x4* acc, char* smem, float (*s_m)[16], float (*s_l)[16]) {
   using L = Tile<T, DH>;
-  constexpr int MB = L::MB, RLD = L::RLD, WT = 4 / WR;
+  constexpr int MB = L::MB, RLD = L::RLD, WT = WV / WR, NT = 64 * WV;
   const PagedCache& c = p.c;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
   Rotation<T, DH> rot;
@@ -572,7 +573,7 @@ __device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, i
   __syncthreads();
   const int64_t rows0 = (static_cast<int64_t>(b) * c.H + h) * p.R;
 #pragma unroll 1
-  for (int u = tid; u < 16 * WR * (DH / 4); u += 256) {
+  for (int u = tid; u < 16 * WR * (DH / 4); u += NT) {
     const int row = u / (DH / 4), d = u % (DH / 4) * 4, rb = row / 16, rr = row % 16, rg = rtile * 16 * WR + row;
     float M = s_m[rb][rr];
 #pragma unroll
@@ -600,7 +601,7 @@ __device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, i
   if (p.n_split == 1) {
     __syncthreads();
 #pragma unroll 1
-    for (int rb = 0; rb < WR; ++rb) {
+    for (int rb = w / 4; rb < WR; rb += WV / 4) {
       const int r0 = (rtile * WR + rb) * 16;
       if (r0 < p.R) finish_rows<T, DH>(p, b, h, r0, red + rb * 16 * RLD, rot);
     }
@@ -702,7 +703,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   u32x4 qf[KS];
   load_query<T, DH>(p, b, h, r, g4, qf);
   __shared__ uint32_t s_bits[S == kTree ? 16 * WR * kTreeRow : 1];
-  TreeBits<16 * WR> bits;
+  TreeBits<16 * WR, 256> bits;
   if constexpr (S == kTree) bits.load(p, b, rtile * WR * 16);
   int top;
   const View v = look<S>(p, b, r, len, s_bits + (S == kTree ? (w % WR * 16 + l16) * kTreeRow : 0), top);
@@ -884,11 +885,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
   if (__any(bad)) one_by_one<T, DH, S>(p, b, h, r, first, STEP, end, v, zt, m, l, acc);
 
-  add_waves<T, DH, WR>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
+  add_waves<T, DH, WR, 4>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
 }
 
-// One split of one key head and 64 rows, 16 a wave: the four waves share each tile of
-// tokens. Its keys and kept groups come into registers a tile ahead, a quarter a
+// One split of one key head and 64 rows, 16 a wave: the four waves (WV; or eight, with 128
+// rows) share each tile of tokens. Its keys and kept groups come into registers a tile ahead, a quarter a
 // wave, and go from there to one of two LDS tiles, so that one barrier a tile is
 // enough: between two barriers the waves write the next tile and compute on this one.
 // (With a tile to each wave, as above, every wave fetches and expands all of it:
@@ -897,20 +898,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 // waiting for data or a barrier and a third for a turn to issue, among 267 vector
 // instructions a tile and wave, 32 of them products; 12 instructions fewer changed nothing.
 // A quarter of the LDS cycles are bank conflicts.
-template <class T, int DH, int SUB, int S, int PN>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 3 : 4))) void k_decode_rows(DecodeParams p) {
+template <class T, int DH, int SUB, int S, int PN, int WV>
+__global__ __launch_bounds__(64 * WV) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (WV == 8 ? 4 : 3) : 4))) void k_decode_rows(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, MB = L::MB;
   constexpr int KLD = L::ROWB + 16, KB = TK * KLD, BUF = KB + L::ZB;
-  constexpr int TPP = 256 / L::LPT, NP = TK / TPP;  // tokens of a pass of the workgroup, passes
+  constexpr int TPP = 64 * WV / L::LPT, NP = TK / TPP, ROWS = 16 * WV;  // tokens of a pass of the workgroup, passes
   static_assert(NP >= 1 && (16 % TPP == 0 || TPP % 16 == 0), "a wave's pass lies in one block of 16 tokens");
-  constexpr int SMEM = 2 * BUF > 4 * L::RB ? 2 * BUF : 4 * L::RB;
+  constexpr int SMEM = 2 * BUF > WV * L::RB ? 2 * BUF : WV * L::RB;
   constexpr int TPG = 64 / NB;  // tiles whose pages one load brings
   __shared__ __attribute__((aligned(16))) char smem[SMEM];
-  __shared__ float s_m[4][16], s_l[4][16];
-  static_assert(SMEM / 4 >= 16 * DH * 4, "a wave's sums fit its quarter");
+  __shared__ float s_m[WV][16], s_l[WV][16];
+  static_assert(SMEM / WV >= 16 * DH * 4, "a wave's sums fit its quarter");
   const PagedCache& c = p.c;
-  const int nrt = (p.R + 63) / 64;
+  const int nrt = (p.R + ROWS - 1) / ROWS;
   __shared__ int s_b;
   int rtile, h, b, sp;
   place(p, nrt, reinterpret_cast<int*>(smem), s_b, rtile, h, b, sp);
@@ -920,12 +921,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   if (c0 >= len && p.n_split > 1) return;
   const uint32_t gm = group_bits(c.G);
   const int shift = c.shift, pmask = c.page - 1, gb = c.ds * static_cast<int>(sizeof(T));
-  const int r = (rtile * 4 + w) * 16 + l16;
+  const int r = (rtile * WV + w) * 16 + l16;
   u32x4 qf[KS];
   load_query<T, DH>(p, b, h, r, g4, qf);
-  __shared__ uint32_t s_bits[S == kTree ? 64 * kTreeRow : 1];
-  TreeBits<64> bits;
-  if constexpr (S == kTree) bits.load(p, b, rtile * 64);
+  __shared__ uint32_t s_bits[S == kTree ? ROWS * kTreeRow : 1];
+  TreeBits<16 * WV, 64 * WV> bits;
+  if constexpr (S == kTree) bits.load(p, b, rtile * ROWS);
   int top;
   const View v = look<S>(p, b, r, len, s_bits + (S == kTree ? (w * 16 + l16) * kTreeRow : 0), top);
   int low = r < p.R ? v.lim : 0x7FFFFFFF;
@@ -940,8 +941,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   if constexpr (S == kTree) bits.put(s_bits, len - v.base);
   __syncthreads();
   const int bound = S == kListed ? __builtin_amdgcn_readfirstlane(__float_as_int(s_l[0][0])) : 0;
-  int all = max(max(__float_as_int(s_m[0][0]), __float_as_int(s_m[1][0])),
-                max(__float_as_int(s_m[2][0]), __float_as_int(s_m[3][0])));
+  int all = __float_as_int(s_m[0][0]);
+#pragma unroll
+  for (int v = 1; v < WV; ++v) all = max(all, __float_as_int(s_m[v][0]));
   if constexpr (S == kListed) all = min(all, listed_end(p, b, h));
   const int end = min(c0 + p.chunk, __builtin_amdgcn_readfirstlane(all));
 
@@ -1039,7 +1041,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0, 0, 0, 0};
   // a wave without rows takes part in the loads only (a call's last rows)
-  const bool idle = (rtile * 4 + w) * 16 >= p.R;
+  const bool idle = (rtile * WV + w) * 16 >= p.R;
   uint32_t there0, there1;
   auto move_on = [&](int (&to)[NB], const int (&from)[NB]) {
 #pragma unroll
@@ -1090,8 +1092,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
     for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
-  if (__any(bad)) one_by_one<T, DH, S>(p, b, h, r, c0, TK, end, v, smem + w * (SMEM / 4), m, l, acc);
-  add_waves<T, DH, 4>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
+  if (__any(bad)) one_by_one<T, DH, S>(p, b, h, r, c0, TK, end, v, smem + w * (SMEM / WV / 16 * 16), m, l, acc);
+  add_waves<T, DH, WV, WV>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
 }
 
 // The maxima and sums of exponentials of J rows from their splits' statistics; `step`
@@ -1307,8 +1309,8 @@ constexpr int kOnceTokens = 1024;
 // heads of 4 rows: see k_tree.hip.
 template <class T, int DH, int WR, int SUB, int S, int N>
 auto kernel_of(const DecodeParams& p) {
-  if constexpr (WR == 4)
-    return k_decode_rows<T, DH, SUB, S, N>;
+  if constexpr (WR >= 4)
+    return k_decode_rows<T, DH, SUB, S, N, WR>;
   else
     return p.max_len >= kOnceTokens && !p.x ? k_decode<T, DH, WR, SUB, true, S, N> : k_decode<T, DH, WR, SUB, false, S, N>;
 }
@@ -1328,16 +1330,21 @@ void go(const DecodeParams& p, hipStream_t s) {
     if (sub == 4) kern = kernel_for<T, DH, WR, 4, S>(p);
   }
   const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(WR == 8 ? 512 : 256), 0, s, p);
 }
 
 template <class T, int DH, int S>
 hipError_t launch(DecodeParams p, hipStream_t s) {
   const int WR = row_blocks(p.R, sizeof(T) == 2, DH);
+  // drafted tokens of many rows: a tile is fetched and expanded for 128 of them at once (4096
+  // tokens, 96 rows 165 -> 150 us)
+  constexpr bool kEight = S == kTree && DH == 128 && sizeof(T) == 2;
   const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * ((p.R + 63) / 64);
   p.ordered = S != kListed && p.n_split == 1 && p.B > 1 && p.B <= kOrderMax && wgs > 256 && wgs <= kOrderWgs && p.max_len >= 512;
   if (WR == 1)
     go<T, DH, 1, S>(p, s);
+  else if (kEight && p.R > kEightRows)
+    go<T, DH, kEight ? 8 : 4, S>(p, s);
   else if (WR == 4)
     go<T, DH, 4, S>(p, s);
   else if constexpr (!share_from_17(sizeof(T) == 2, DH))

@@ -13,8 +13,12 @@ namespace {
 // heads: 12.2 against 14.4 us), but a call's outputs would then depend on whether it
 // adds up weights.
 constexpr int64_t kSplitWgs = 512;
-// The same for drafted tokens.
-constexpr int64_t kTreeWgs = 1024;
+// The same for drafted tokens, whose tiles take longer (32 sequences of 256 to 4096 tokens, 8
+// key heads of 4 rows, 16-row blocks of 24 tokens: 151 us with 512, 136 with 1024, 122 with
+// 1536; of 4096 174, 169 and 170; 8 tokens 107, 101, 113), and for those of more than 64
+// rows, counted in blocks of 64, of which a workgroup of eight waves has two: with 1024, 1536
+// and 3072 137, 131 and 122, of 4096 152, 155 and 164, 60 tokens and 8 sequences 86, 69 and 84.
+constexpr int64_t kTreeWgs = 1024, kEightWgs = 1536;
 // Up to 512 tokens these and listed pages, whose calls add up no weights, have one split
 // where 16 rows or fewer share it: 8 drafted tokens over 305 and 32 heads 24.9 -> 22.2 us
 // with the masks, 24 pages of 16 chosen of 176 35.7 -> 31.9 with the choice. From 60 rows on
@@ -33,7 +37,7 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, DecodeKind kind) {
   DecodePlan d;
-  const int64_t want = kind == DecodeKind::tree ? kTreeWgs : kSplitWgs;
+  const int64_t want = kind != DecodeKind::tree ? kSplitWgs : R > kEightRows ? kEightWgs : kTreeWgs;
   const int nrt = (R + 63) / 64;  // whatever row_blocks says
   const int64_t units = (static_cast<int64_t>(max_len) + 127) / 128;  // of 128 tokens, a tile for each of four waves
   const int64_t wgs = static_cast<int64_t>(B) * H * nrt;
