@@ -303,16 +303,16 @@ __device__ __forceinline__ View look(const DecodeParams& p, int b, int r, int le
 
 // The bits of N rows from r0 on, as words of LDS rows: loaded, and later put there by the
 // same threads.
-template <int N, int NT>
+template <int N>
 struct TreeBits {
-  static constexpr int kEach = (N * kTreeRow + NT - 1) / NT;
+  static constexpr int kEach = (N * kTreeRow + 255) / 256;
   uint32_t w[kEach];
   __device__ __forceinline__ void load(const DecodeParams& p, int b, int r0) {
     const int n = p.n_new ? min(max(p.n_new[b], 0), p.Tq) : p.Tq, words = (p.Tq + 31) / 32;
     const uint32_t* t = p.tree + (p.trees > 1 ? static_cast<int64_t>(b) * p.Tq * words : 0);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int u = threadIdx.x + NT * i, r = r0 + u / kTreeRow, x = u % kTreeRow - 1, j = r / p.rep;
+      const int u = threadIdx.x + 256 * i, r = r0 + u / kTreeRow, x = u % kTreeRow - 1, j = r / p.rep;
       w[i] = 0;
       if (u < N * kTreeRow && r < p.R && j < n && x >= 0 && 32 * x < n) {
         w[i] = t[j * words + x];
@@ -324,7 +324,7 @@ struct TreeBits {
   __device__ __forceinline__ void put(uint32_t* s_bits, int there) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int u = threadIdx.x + NT * i, left = there - 32 * (u % kTreeRow - 1);
+      const int u = threadIdx.x + 256 * i, left = there - 32 * (u % kTreeRow - 1);
       if (u < N * kTreeRow) s_bits[u] = left >= 32 ? w[i] : left > 0 ? w[i] & ((1u << left) - 1u) : 0u;
     }
   }
@@ -447,6 +447,38 @@ __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4
   }
 }
 
+// The same for RB blocks of rows, which share the reads.
+template <class T, int DH, int N, int RB>
+__device__ __forceinline__ void weigh_blocks(const char* zt, const f32x4 (*s)[Tile<T, DH>::NB], f32x4 (*acc)[Tile<T, DH>::MB]) {
+  using L = Tile<T, DH>;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+  if constexpr (L::kBf16) {
+    bf16x8 part[RB][N];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) split_bf16(s[b][0], s[b][L::NB - 1], part[b]);
+    const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb) {
+      const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
+      const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) acc[b][mb] = mfma_16x16x32(a, part[b][n], acc[b][mb]);
+    }
+    reads_ahead<L::MB, 2, N * RB, 2>();
+  } else {
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float a = *reinterpret_cast<const float*>(zt + (4 * g4 + x) * L::ZLD + 4 * (16 * mb + l16));
+#pragma unroll
+        for (int b = 0; b < RB; ++b) acc[b][mb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[b][0][x], acc[b][mb], 0, 0, 0);
+      }
+  }
+}
+
 // A lane's part of row r's query: the dims that its part of a key is multiplied by.
 template <class T, int DH>
 __device__ __forceinline__ void load_query(const DecodeParams& p, int b, int h, int r, int g4, u32x4* qf) {
@@ -543,12 +575,12 @@ __device__ __forceinline__ void one_by_one(const DecodeParams& p, int b, int h, 
 }
 
 // The end of a split: the sums of the waves of each row block added in their order,
-// and left for k_join or, where there is no other split, finished. All threads of WV waves.
-template <class T, int DH, int WR, int WV>
+// and left for k_join or, where there is no other split, finished. All 256 threads.
+template <class T, int DH, int WR>
 __device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, int rtile, int sp, float m, float l,
                                           const f32x4* acc, char* smem, float (*s_m)[16], float (*s_l)[16]) {
   using L = Tile<T, DH>;
-  constexpr int MB = L::MB, RLD = L::RLD, WT = WV / WR, NT = 64 * WV;
+  constexpr int MB = L::MB, RLD = L::RLD, WT = 4 / WR;
   const PagedCache& c = p.c;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g4 = lane >> 4;
   Rotation<T, DH> rot;
@@ -573,7 +605,7 @@ __device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, i
   __syncthreads();
   const int64_t rows0 = (static_cast<int64_t>(b) * c.H + h) * p.R;
 #pragma unroll 1
-  for (int u = tid; u < 16 * WR * (DH / 4); u += NT) {
+  for (int u = tid; u < 16 * WR * (DH / 4); u += 256) {
     const int row = u / (DH / 4), d = u % (DH / 4) * 4, rb = row / 16, rr = row % 16, rg = rtile * 16 * WR + row;
     float M = s_m[rb][rr];
 #pragma unroll
@@ -601,7 +633,7 @@ __device__ __forceinline__ void add_waves(const DecodeParams& p, int b, int h, i
   if (p.n_split == 1) {
     __syncthreads();
 #pragma unroll 1
-    for (int rb = w / 4; rb < WR; rb += WV / 4) {
+    for (int rb = 0; rb < WR; ++rb) {
       const int r0 = (rtile * WR + rb) * 16;
       if (r0 < p.R) finish_rows<T, DH>(p, b, h, r0, red + rb * 16 * RLD, rot);
     }
@@ -644,10 +676,7 @@ __device__ __forceinline__ int in_order(const DecodeParams& p, int o, int wgs, i
 // tokens, 8 key heads of 4 rows: 183 us; with the splits' numbers changing fastest,
 // 256, as full and empty ones then meet on the same XCDs. Four of 30000 to 120000, 16
 // heads: 340, and 410 with the eight apart.
-__device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len, int& s_b, int& rtile, int& h, int& b, int& sp) {
-  int lin = blockIdx.x;
-  rtile = lin % nrt;
-  lin /= nrt;
+__device__ __forceinline__ void place_item(const DecodeParams& p, int lin, int nrt, int* s_len, int& s_b, int& h, int& b, int& sp) {
   if (p.n_split == 1) {
     h = lin % p.c.H;
     b = p.ordered ? in_order(p, lin / p.c.H, p.c.H * nrt, s_len, s_b) : lin / p.c.H;
@@ -662,6 +691,10 @@ __device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len
   h = lin % p.c.H;
   b = lin / p.c.H;
   sp = s0 + (sp + b) % n;
+}
+__device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len, int& s_b, int& rtile, int& h, int& b, int& sp) {
+  rtile = blockIdx.x % nrt;
+  place_item(p, blockIdx.x / nrt, nrt, s_len, s_b, h, b, sp);
 }
 
 // One split of one key head and 16 * WR rows: wave w takes row block w % WR and every
@@ -681,7 +714,7 @@ __device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len
 template <class T, int DH, int WR, int SUB, bool ONCE, int S, int PN>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4))) void k_decode(DecodeParams p) {
   using L = Tile<T, DH>;
-  constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, NVI = L::NVI, MB = L::MB, RLD = L::RLD;
+  constexpr int TK = L::TK, NB = L::NB, KS = L::KS, NVI = L::NVI, MB = L::MB;
   constexpr int WT = 4 / WR, STEP = WT * TK, TPP = 64 / NB;  // tiles whose pages one load brings
   __shared__ __attribute__((aligned(16))) char smem[L::SMEM];
   __shared__ u32x2 s_rec[4][TK];
@@ -703,7 +736,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
   u32x4 qf[KS];
   load_query<T, DH>(p, b, h, r, g4, qf);
   __shared__ uint32_t s_bits[S == kTree ? 16 * WR * kTreeRow : 1];
-  TreeBits<16 * WR, 256> bits;
+  TreeBits<16 * WR> bits;
   if constexpr (S == kTree) bits.load(p, b, rtile * WR * 16);
   int top;
   const View v = look<S>(p, b, r, len, s_bits + (S == kTree ? (w % WR * 16 + l16) * kTreeRow : 0), top);
@@ -885,12 +918,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
     for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
   if (__any(bad)) one_by_one<T, DH, S>(p, b, h, r, first, STEP, end, v, zt, m, l, acc);
 
-  add_waves<T, DH, WR, 4>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
+  add_waves<T, DH, WR>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
 }
 
-// One split of one key head and 64 rows, 16 a wave: the four waves (WV; or eight, with 128
-// rows) share each tile of tokens. Its keys and kept groups come into registers a tile ahead, a quarter a
-// wave, and go from there to one of two LDS tiles, so that one barrier a tile is
+// One split of one key head and 64 rows, 16 a wave: the four waves share each tile of
+// tokens. Its keys and kept groups come into registers a tile ahead, a quarter a wave, and go from there to one of two LDS tiles, so that one barrier a tile is
 // enough: between two barriers the waves write the next tile and compute on this one.
 // (With a tile to each wave, as above, every wave fetches and expands all of it:
 // 16 sequences of up to 361 tokens and 56 queries took 42 us.) Those 16, 32 heads, take 32
@@ -898,20 +930,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 // waiting for data or a barrier and a third for a turn to issue, among 267 vector
 // instructions a tile and wave, 32 of them products; 12 instructions fewer changed nothing.
 // A quarter of the LDS cycles are bank conflicts.
-template <class T, int DH, int SUB, int S, int PN, int WV>
-__global__ __launch_bounds__(64 * WV) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (WV == 8 ? 4 : 3) : 4))) void k_decode_rows(DecodeParams p) {
+template <class T, int DH, int SUB, int S, int PN>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 3 : 4))) void k_decode_rows(DecodeParams p) {
   using L = Tile<T, DH>;
-  constexpr int TK = L::TK, NB = L::NB, EP = L::EP, KS = L::KS, MB = L::MB;
+  constexpr int TK = L::TK, NB = L::NB, KS = L::KS, MB = L::MB;
   constexpr int KLD = L::ROWB + 16, KB = TK * KLD, BUF = KB + L::ZB;
-  constexpr int TPP = 64 * WV / L::LPT, NP = TK / TPP, ROWS = 16 * WV;  // tokens of a pass of the workgroup, passes
+  constexpr int TPP = 256 / L::LPT, NP = TK / TPP;  // tokens of a pass of the workgroup, passes
   static_assert(NP >= 1 && (16 % TPP == 0 || TPP % 16 == 0), "a wave's pass lies in one block of 16 tokens");
-  constexpr int SMEM = 2 * BUF > WV * L::RB ? 2 * BUF : WV * L::RB;
+  constexpr int SMEM = 2 * BUF > 4 * L::RB ? 2 * BUF : 4 * L::RB;
   constexpr int TPG = 64 / NB;  // tiles whose pages one load brings
   __shared__ __attribute__((aligned(16))) char smem[SMEM];
-  __shared__ float s_m[WV][16], s_l[WV][16];
-  static_assert(SMEM / WV >= 16 * DH * 4, "a wave's sums fit its quarter");
+  __shared__ float s_m[4][16], s_l[4][16];
+  static_assert(SMEM / 4 >= 16 * DH * 4, "a wave's sums fit its quarter");
   const PagedCache& c = p.c;
-  const int nrt = (p.R + ROWS - 1) / ROWS;
+  const int nrt = (p.R + 63) / 64;
   __shared__ int s_b;
   int rtile, h, b, sp;
   place(p, nrt, reinterpret_cast<int*>(smem), s_b, rtile, h, b, sp);
@@ -921,14 +953,11 @@ __global__ __launch_bounds__(64 * WV) __attribute__((amdgpu_waves_per_eu(DH == 1
   if (c0 >= len && p.n_split > 1) return;
   const uint32_t gm = group_bits(c.G);
   const int shift = c.shift, pmask = c.page - 1, gb = c.ds * static_cast<int>(sizeof(T));
-  const int r = (rtile * WV + w) * 16 + l16;
+  const int r = (rtile * 4 + w) * 16 + l16;
   u32x4 qf[KS];
   load_query<T, DH>(p, b, h, r, g4, qf);
-  __shared__ uint32_t s_bits[S == kTree ? ROWS * kTreeRow : 1];
-  TreeBits<16 * WV, 64 * WV> bits;
-  if constexpr (S == kTree) bits.load(p, b, rtile * ROWS);
   int top;
-  const View v = look<S>(p, b, r, len, s_bits + (S == kTree ? (w * 16 + l16) * kTreeRow : 0), top);
+  const View v = look<S>(p, b, r, len, nullptr, top);
   int low = r < p.R ? v.lim : 0x7FFFFFFF;
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) {
@@ -938,12 +967,10 @@ __global__ __launch_bounds__(64 * WV) __attribute__((amdgpu_waves_per_eu(DH == 1
   const int least = __builtin_amdgcn_readfirstlane(low);
   if (lane == 0) s_m[w][0] = __int_as_float(top);
   if (S == kListed && tid == 0) s_l[0][0] = __int_as_float(v.lim);  // of all rows
-  if constexpr (S == kTree) bits.put(s_bits, len - v.base);
   __syncthreads();
   const int bound = S == kListed ? __builtin_amdgcn_readfirstlane(__float_as_int(s_l[0][0])) : 0;
-  int all = __float_as_int(s_m[0][0]);
-#pragma unroll
-  for (int v = 1; v < WV; ++v) all = max(all, __float_as_int(s_m[v][0]));
+  int all = max(max(__float_as_int(s_m[0][0]), __float_as_int(s_m[1][0])),
+                max(__float_as_int(s_m[2][0]), __float_as_int(s_m[3][0])));
   if constexpr (S == kListed) all = min(all, listed_end(p, b, h));
   const int end = min(c0 + p.chunk, __builtin_amdgcn_readfirstlane(all));
 
@@ -1041,7 +1068,7 @@ __global__ __launch_bounds__(64 * WV) __attribute__((amdgpu_waves_per_eu(DH == 1
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0, 0, 0, 0};
   // a wave without rows takes part in the loads only (a call's last rows)
-  const bool idle = (rtile * WV + w) * 16 >= p.R;
+  const bool idle = (rtile * 4 + w) * 16 >= p.R;
   uint32_t there0, there1;
   auto move_on = [&](int (&to)[NB], const int (&from)[NB]) {
 #pragma unroll
@@ -1092,8 +1119,8 @@ __global__ __launch_bounds__(64 * WV) __attribute__((amdgpu_waves_per_eu(DH == 1
   for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
     for (int x = 0; x < 4; ++x) bad |= !__builtin_isfinite(acc[mb][x]);
-  if (__any(bad)) one_by_one<T, DH, S>(p, b, h, r, c0, TK, end, v, smem + w * (SMEM / WV / 16 * 16), m, l, acc);
-  add_waves<T, DH, WV, WV>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
+  if (__any(bad)) one_by_one<T, DH, S>(p, b, h, r, c0, TK, end, v, smem + w * (SMEM / 4), m, l, acc);
+  add_waves<T, DH, 4>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
 }
 
 // The maxima and sums of exponentials of J rows from their splits' statistics; `step`
@@ -1303,14 +1330,15 @@ int row_blocks(int R, bool bf16, int dh) { return R <= 16 ? 1 : R <= 32 && !shar
 // batches would gain (64 of up to 2048, 8 heads of 4 rows 64.6 -> 59.2).
 constexpr int kOnceTokens = 1024;
 
-// Parts of a bfloat16 weight: all 24 bits, but in the calls that always took the output's
-// type into account 17 where that is bfloat16 itself, whose half step is 2^-9: a weight is
-// off by 2^-17 of itself. 32 sequences of up to 4096 tokens and 24 drafted ones, 8 key
-// heads of 4 rows: see k_tree.hip.
+// Parts of a bfloat16 weight: three, all its 24 bits. Calls over trees and listed pages with
+// bfloat16 outputs, whose half step is 2^-9, take two, so that a weight is off by 2^-17 of
+// itself at most, and a sum of weighted values by 2^-17 of the sum of their magnitudes (the
+// others keep what they have always answered). 32 sequences of 256 to 4096 tokens, 8 key
+// heads of 96 rows of drafted tokens: 91 us with three, 88 with two.
 template <class T, int DH, int WR, int SUB, int S, int N>
 auto kernel_of(const DecodeParams& p) {
-  if constexpr (WR >= 4)
-    return k_decode_rows<T, DH, SUB, S, N, WR>;
+  if constexpr (WR == 4)
+    return k_decode_rows<T, DH, SUB, S, N>;
   else
     return p.max_len >= kOnceTokens && !p.x ? k_decode<T, DH, WR, SUB, true, S, N> : k_decode<T, DH, WR, SUB, false, S, N>;
 }
@@ -1330,25 +1358,11 @@ void go(const DecodeParams& p, hipStream_t s) {
     if (sub == 4) kern = kernel_for<T, DH, WR, 4, S>(p);
   }
   const int nrt = (p.R + 16 * WR - 1) / (16 * WR);
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(WR == 8 ? 512 : 256), 0, s, p);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(nrt) * p.n_split * p.c.H * p.B), dim3(256), 0, s, p);
 }
 
 template <class T, int DH, int S>
-hipError_t launch(DecodeParams p, hipStream_t s) {
-  const int WR = row_blocks(p.R, sizeof(T) == 2, DH);
-  // drafted tokens of many rows: a tile is fetched and expanded for 128 of them at once (4096
-  // tokens, 96 rows 165 -> 150 us)
-  constexpr bool kEight = S == kTree && DH == 128 && sizeof(T) == 2;
-  const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * ((p.R + 63) / 64);
-  p.ordered = S != kListed && p.n_split == 1 && p.B > 1 && p.B <= kOrderMax && wgs > 256 && wgs <= kOrderWgs && p.max_len >= 512;
-  if (WR == 1)
-    go<T, DH, 1, S>(p, s);
-  else if (kEight && p.R > kEightRows)
-    go<T, DH, kEight ? 8 : 4, S>(p, s);
-  else if (WR == 4)
-    go<T, DH, 4, S>(p, s);
-  else if constexpr (!share_from_17(sizeof(T) == 2, DH))
-    go<T, DH, 2, S>(p, s);
+void launch_join(const DecodeParams& p, hipStream_t s) {
   const int joins = p.n_split > 1 ? (p.R + 15) / 16 * p.c.H * p.B : 0;
   const int64_t blocks = static_cast<int64_t>(p.B) * ((p.max_len + 63) / 64), rows = static_cast<int64_t>(p.c.H) * p.R;
   // many rows and blocks of 64 tokens on half the CUs or fewer: of 16 (305 tokens and 1280
@@ -1361,6 +1375,22 @@ hipError_t launch(DecodeParams p, hipStream_t s) {
   if (joins + nblk > 0)
     hipLaunchKernelGGL((k_join<T, DH, S>), dim3(static_cast<unsigned>(joins) + static_cast<unsigned>(nblk) * p.B), dim3(256),
                        0, s, p, joins, nblk, tb, per);
+}
+
+template <class T, int DH, int S>
+hipError_t launch(DecodeParams p, hipStream_t s) {
+  const int WR = row_blocks(p.R, sizeof(T) == 2, DH);
+  const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * ((p.R + 63) / 64);
+  p.ordered = S != kListed && p.n_split == 1 && p.B > 1 && p.B <= kOrderMax && wgs > 256 && wgs <= kOrderWgs && p.max_len >= 512;
+  if (WR == 1)
+    go<T, DH, 1, S>(p, s);
+  else if constexpr (S == kTree)
+    return hipErrorInvalidValue;  // not called: launch_decode_tree
+  else if (WR == 4)
+    go<T, DH, 4, S>(p, s);
+  else if constexpr (!share_from_17(sizeof(T) == 2, DH))
+    go<T, DH, 2, S>(p, s);
+  launch_join<T, DH, S>(p, s);
   return hipGetLastError();
 }
 

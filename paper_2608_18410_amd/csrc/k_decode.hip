@@ -13,12 +13,13 @@ namespace {
 // heads: 12.2 against 14.4 us), but a call's outputs would then depend on whether it
 // adds up weights.
 constexpr int64_t kSplitWgs = 512;
-// The same for drafted tokens, whose tiles take longer (32 sequences of 256 to 4096 tokens, 8
-// key heads of 4 rows, 16-row blocks of 24 tokens: 151 us with 512, 136 with 1024, 122 with
-// 1536; of 4096 174, 169 and 170; 8 tokens 107, 101, 113), and for those of more than 64
-// rows, counted in blocks of 64, of which a workgroup of eight waves has two: with 1024, 1536
-// and 3072 137, 131 and 122, of 4096 152, 155 and 164, 60 tokens and 8 sequences 86, 69 and 84.
-constexpr int64_t kTreeWgs = 1024, kEightWgs = 1536;
+// The same for drafted tokens of up to 16 rows, whose tiles take longer (32 sequences of 256
+// to 4096 tokens, 8 key heads of 16 rows: 107 us with 512, 101 with 1024, 113 with 1536), and
+// of more, in blocks of kTreeRows: 8 of those sequences, of 96 rows, 60 us with 256, 53 with
+// 512, 46 with 768 and 50 with 1024. Where the blocks fill the card without splits, two to a
+// CU, splits only add: 32 of those sequences of 64 rows 73 us in one, 98 in two, of 96 rows
+// 88 and 113, of 64 rows and up to 16384 tokens 217 and 258; nothing longer was measured.
+constexpr int64_t kTreeWgs = 1024, kTreeRowsWgs = 768, kTreeFull = 512, kTreeWhole = 128;
 // Up to 512 tokens these and listed pages, whose calls add up no weights, have one split
 // where 16 rows or fewer share it: 8 drafted tokens over 305 and 32 heads 24.9 -> 22.2 us
 // with the masks, 24 pages of 16 chosen of 176 35.7 -> 31.9 with the choice. From 60 rows on
@@ -37,14 +38,16 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, DecodeKind kind) {
   DecodePlan d;
-  const int64_t want = kind != DecodeKind::tree ? kSplitWgs : R > kEightRows ? kEightWgs : kTreeWgs;
-  const int nrt = (R + 63) / 64;  // whatever row_blocks says
+  const int64_t want = kind != DecodeKind::tree ? kSplitWgs : R > 16 ? kTreeRowsWgs : kTreeWgs;
+  const int tile = kind == DecodeKind::tree ? kTreeRows : 64;  // rows of a workgroup, whatever row_blocks says
+  const int nrt = (R + tile - 1) / tile;
   const int64_t units = (static_cast<int64_t>(max_len) + 127) / 128;  // of 128 tokens, a tile for each of four waves
   const int64_t wgs = static_cast<int64_t>(B) * H * nrt;
   const int64_t least = (units + kMaxSplits - 1) / kMaxSplits;
   int64_t per = std::max((units * wgs + want - 1) / want, least);
   if (per > kLongUnits && (per < units || wgs > kOrderWgs))
     per = std::max({kLongUnits, (units * wgs + kLongWgs - 1) / kLongWgs, least});
+  if (kind == DecodeKind::tree && R > 16 && wgs >= kTreeFull && units <= kTreeWhole) per = units;
   if (kind != DecodeKind::paged && units <= kShortUnits && R <= 16) per = units;
   d.chunk = static_cast<int>(128 * std::max<int64_t>(1, std::min(per, units)));
   d.n_split = std::max(1, static_cast<int>((static_cast<int64_t>(max_len) + d.chunk - 1) / d.chunk));
@@ -55,10 +58,10 @@ DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, Deco
   d.bytes = d.off_x + (mass ? up256(rows * d.x_ld * 4) : 0);
   // what to ask a caller for: a bound on the above that does not fall as B, Tq or
   // max_len grows (n_split <= want / wgs + 1, or for splits of kLongUnits and more
-  // kLongWgs / wgs + 1 and units / kLongUnits + 1; R <= 64 nrt)
-  const size_t r64 = std::min<size_t>(R, 64);
-  const size_t longs = std::min(r64 * kLongWgs, rows * static_cast<size_t>(units / kLongUnits)) + rows;
-  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)), std::max(r64 * want + rows, longs));
+  // kLongWgs / wgs + 1 and units / kLongUnits + 1; R <= tile * nrt)
+  const size_t most_r = std::min(R, tile);
+  const size_t longs = std::min(most_r * kLongWgs, rows * static_cast<size_t>(units / kLongUnits)) + rows;
+  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)), std::max(most_r * want + rows, longs));
   d.ask = up256(most * dh * 4) + up256(most * 8) + (mass ? up256(rows * d.x_ld * 4) : 0);
   return d;
 }

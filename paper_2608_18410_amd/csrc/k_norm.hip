@@ -464,7 +464,7 @@ __device__ __forceinline__ void rotate_run(const TurnParams& p, int64_t n0, int 
 
 // An append. The first workgroups turn the rows of queries and keys, the last `vals` bring
 // the values of one head and run of tokens. 16 times up to 305 tokens of 32 + 32 heads from
-// a fused a fused projection (157 MB) 46 us, 3.4 TB/s, of which the rows alone would take 30; with
+// a fused projection (157 MB) 46 us, 3.4 TB/s, of which the rows alone would take 30; with
 // the values first 49, with both kinds spread evenly 51. Without the norm 40: the vector
 // units are busy too.
 template <class T, int DH, bool IL, bool WHOLE>

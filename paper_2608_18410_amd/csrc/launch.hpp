@@ -325,8 +325,8 @@ struct DecodePlan {
   size_t off_stat, off_x, bytes;  // of this call
   size_t ask;  // at least bytes of every call of no more sequences, queries and tokens
 };
-// Rows of drafted tokens from which on eight waves share a tile (bf16, dims of 128).
-constexpr int kEightRows = 64;
+// Rows of a workgroup where there are more than 16 of drafted tokens.
+constexpr int kTreeRows = 32;
 enum class DecodeKind { paged, tree, listed };
 DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, DecodeKind kind = DecodeKind::paged);
 hipError_t launch_decode(const DecodeParams& p, bool bf16, hipStream_t s);
