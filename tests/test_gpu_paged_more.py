@@ -324,6 +324,16 @@ def test_tree_rows(H, rep, Tq, dtype, dh):
     check_tree(q, c, t, ints(base), anyb, n_new=few)
 
 
+# as many row tiles as the card holds: whole sequences in one split, the longest first
+@pytest.mark.parametrize("B,H,rep,Tq,top", [(61, 9, 1, 17, 700), (64, 8, 4, 5, 90), (300, 2, 1, 24, 520), (64, 8, 1, 33, 5000)])
+@pytest.mark.parametrize("dtype,dh", [(bf, 64), (bf, 128), (f32, 64), (f32, 128)])
+def test_tree_whole_sequences(B, H, rep, Tq, top, dtype, dh):
+    base = [0, 1, 33, top] + [(29 * i) % 83 for i in range(B - 4)]
+    rng, c, t, n, q = case(4, [x + Tq for x in base], P=32, H=H, rep=rep, Tq=Tq, dh=dh, dtype=dtype)
+    few = ints([Tq if i % 5 else i % (Tq + 1) for i in range(B)])
+    check_tree(q, c, t, ints(base), _trees(rng, B, Tq), rotations(rng, H, dh, dtype), n_new=few)
+
+
 @pytest.mark.parametrize("P", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("dtype", [bf, f32])
 def test_tree_pages_and_bounds(P, dtype):
