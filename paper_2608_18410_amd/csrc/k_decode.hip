@@ -60,8 +60,10 @@ DecodePlan decode_plan(int B, int H, int R, int dh, int max_len, bool mass, Deco
   // max_len grows (n_split <= want / wgs + 1, or for splits of kLongUnits and more
   // kLongWgs / wgs + 1 and units / kLongUnits + 1; R <= tile * nrt)
   const size_t most_r = std::min(R, tile);
+  size_t short_rows = most_r * want;  // n_split times rows, but for one a row
+  if (kind == DecodeKind::tree && R > 16) short_rows = std::max(short_rows, static_cast<size_t>(16 * kTreeWgs));
   const size_t longs = std::min(most_r * kLongWgs, rows * static_cast<size_t>(units / kLongUnits)) + rows;
-  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)), std::max(most_r * want + rows, longs));
+  const size_t most = std::min(rows * static_cast<size_t>(std::min(units, kMaxSplits)), std::max(short_rows + rows, longs));
   d.ask = up256(most * dh * 4) + up256(most * 8) + (mass ? up256(rows * d.x_ld * 4) : 0);
   return d;
 }

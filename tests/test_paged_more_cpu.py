@@ -2,6 +2,7 @@
 without a GPU: the oracle against textbook forms, the binding's shape checks, and the
 library's refusals (all before anything is launched)."""
 import ctypes
+import re
 import os
 import shutil
 import subprocess
@@ -378,6 +379,30 @@ def test_workspaces_grow_with_the_call():
                 assert all(p <= q for p, q in zip(last.get(a, now), now)), (x, a)
                 last[a] = now
     assert lib.rolesub_attend_tree_workspace_size(None, 1, 16, 1, 9) == lib.rolesub_select_pages_workspace_size(None, 1, 1, 9) == 0
+
+
+@pytest.mark.parametrize("name", ["tree", "selected"])
+@pytest.mark.parametrize("H", [1, 8])
+def test_a_workspace_serves_every_smaller_call(name, H):
+    _no_gpu()
+    lib, run = rs.load(), lib_calls()[1]
+    d = ctypes.byref(rs.PagesDesc(9, 64, 64, H, 64, 8, None, None, None, None))
+    need, ask = {}, {}
+    for B in (1, 5, 65, 300):
+        for Tq in (1, 4, 8, 15, 16, 17, 20, 24, 32, 33, 40, 64, 65, 96, 129, 250):
+            for n in (1, 9, 300, 2100):  # pages of 64 tokens
+                ask[B, Tq, n] = (lib.rolesub_attend_tree_workspace_size(d, B, H, Tq, 64 * n) if name == "tree" else
+                                 lib.rolesub_attend_selected_workspace_size(d, B, H, Tq, n))
+                # far apart: the operands of no call overlap, and the refusal comes before a launch
+                kw = {x: (i + 1) << 44 for i, x in enumerate(lib_calls()[0])}
+                st, why = run(name, **{**kw, "ws": None}, B=B, T=Tq, Hq=H, H=H, page=64, W=2100, max_len=64 * n, n_sel=n, trees=1, wsb=0)
+                got = re.search(r"workspace of (\d+) bytes", why) if st == INVALID else None
+                assert got or st == HIP, why
+                need[B, Tq, n] = int(got.group(1)) if got else 0
+    for x, y in need.items():
+        for z_, most in ask.items():
+            if all(i <= j for i, j in zip(x, z_)):
+                assert y <= most, (x, y, z_, most)
 
 
 # ---- layers ------------------------------------------------------------------
