@@ -213,10 +213,10 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectParams p, int np) {
   typedef PageScores<T, DH, RC> S;
   const PagedCache& c = p.c;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int lin = blockIdx.x;
-  const int i0 = (lin % np * 4 + w) * S::PS * S::U;
-  lin /= np;
-  const int h = lin % c.H, b = lin / c.H;
+  int lin = blockIdx.x;  // heads fastest: their bounds lie behind each other
+  const int h = lin % c.H;
+  lin /= c.H;
+  const int i0 = (lin % np * 4 + w) * S::PS * S::U, b = lin / np;
   const int64_t len = tokens_of(p, b);
   if (i0 == 0)
     for (int j = lane; j < p.Tq; j += 64) p.counts[(static_cast<int64_t>(b) * p.Tq + j) * c.H + h] = pages_of(p, b, j, len);
