@@ -324,6 +324,27 @@ def test_tree_rows(H, rep, Tq, dtype, dh):
     check_tree(q, c, t, ints(base), anyb, n_new=few)
 
 
+@pytest.mark.parametrize("dtype,dh", [(bf, 128), (f32, 64)])
+@pytest.mark.parametrize("Tq", [3, 40])
+def test_tree_rows_that_see_nothing(dtype, dh, Tq):
+    rng, c, t, n, q = case(5, [Tq + 9, Tq], H=2, rep=2, Tq=Tq, dh=dh, dtype=dtype)
+    sets, R = _trees(rng, 2, Tq), rotations(rng, 2, dh, dtype)
+    for x in (c.K, c.V):
+        x.fill_(float("nan"))
+    for kw in (dict(n_new=ints([0, -3])), dict(table=t[:, :0].contiguous()), dict(table=torch.full_like(t, -1)),
+               dict(tree=torch.zeros(2, Tq, (Tq + 31) // 32, dtype=torch.int32, device=q.device), lens=ints([0, 0]))):
+        out = torch.full_like(q, 7.0)
+        rs.attend_tree(q, c, kw.get("table", t), kw.get("lens", ints([9, 0])), kw.get("tree", words(sets, Tq)), R,
+                       n_new=kw.get("n_new"), out=out)
+        assert not out.any(), kw
+    # and over the queries themselves
+    inplace = q.clone()
+    for x in (c.K, c.V):
+        x.copy_(torch.randn(x.shape, device=q.device).to(dtype))
+    args = c, t, ints([9, 0]), words(sets, Tq), R
+    assert same(rs.attend_tree(inplace, *args, out=inplace), rs.attend_tree(q, *args))
+
+
 # as many row tiles as the card holds: whole sequences in one split, the longest first
 @pytest.mark.parametrize("B,H,rep,Tq,top", [(61, 9, 1, 17, 700), (64, 8, 4, 5, 90), (300, 2, 1, 24, 520), (64, 8, 1, 33, 5000)])
 @pytest.mark.parametrize("dtype,dh", [(bf, 64), (bf, 128), (f32, 64), (f32, 128)])
