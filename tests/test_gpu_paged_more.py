@@ -821,6 +821,39 @@ def test_draft_accept_and_few_pages_graph_replays():
             assert same(a, o), i
 
 
+@pytest.mark.parametrize("B,H,top", [(3, 2, 900), (64, 8, 600)])  # split, whole
+def test_trees_of_many_rows_graph_replays(B, H, top):
+    Tq = 33
+    rng, c, t, n, q = case(6, [top + Tq] * 2 + [(37 * i) % 71 + Tq for i in range(B - 2)], P=32, H=H, Tq=Tq, dh=128, dtype=bf)
+    sets, R, lens, few = words(_trees(rng, B, Tq), Tq), rotations(rng, H, 128, bf), n - Tq, ints([Tq] * B)
+    max_len = t.shape[1] * 32
+    ws = [torch.empty(max(rs.attend_tree_workspace_size(c, B, H, Tq, max_len), 1), device=DEV, dtype=torch.uint8) for _ in range(2)]
+    out = [torch.empty_like(q) for _ in range(2)]
+
+    def step(i):
+        rs.attend_tree(q, c, t, lens, sets, R, n_new=few, workspace=ws[i], out=out[i])
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(0)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(0)
+    for i in range(5):
+        q.copy_(torch.randn(q.shape, device=DEV).to(bf))
+        lens.copy_(ints(np.roll(lens.cpu().numpy(), 1)))  # other sequences are the long ones; tables that end give what is there
+        few.copy_(ints(rng.integers(0, Tq + 1, B)))
+        out[0].fill_(float("nan"))
+        ws[0].fill_(255)
+        graph.replay()
+        step(1)
+        torch.cuda.synchronize()
+        assert same(*out), i
+
+
 def test_two_streams_at_once():
     """Two layers with their own caches and workspaces give the bits of one after the other; what a call with stream= makes
     is ready for the caller after the stream."""
