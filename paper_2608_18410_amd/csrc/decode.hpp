@@ -104,20 +104,19 @@ __device__ __forceinline__ u32x4 bload16_hint(rsrc_t r, uint32_t off) {
 // queries, 32 heads 29.2 -> 31.1 us, 8 of 305 and 305 52 -> 56.5) and nothing where
 // calls are bound by memory. An infinity's other parts are NaN.
 constexpr int kParts = 3;
-template <int N>
-__device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8 (&part)[N]) {
-  u32x4 v[N];
+__device__ __forceinline__ void split_bf16(f32x4 a, f32x4 b, bf16x8 (&part)[kParts]) {
+  u32x4 v[kParts];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f32x2 x = i < 2 ? f32x2{a[2 * i], a[2 * i + 1]} : f32x2{b[2 * i - 4], b[2 * i - 3]};
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
+    for (int n = 0; n < kParts; ++n) {
       v[n][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
       x = f32x2{x[0] - __uint_as_float(v[n][i] << 16), x[1] - __uint_as_float(v[n][i] & 0xFFFF0000u)};
     }
   }
 #pragma unroll
-  for (int n = 0; n < N; ++n) part[n] = __builtin_bit_cast(bf16x8, v[n]);
+  for (int n = 0; n < kParts; ++n) part[n] = __builtin_bit_cast(bf16x8, v[n]);
 }
 
 // Order of N steps of R LDS reads that feed M matrix products each: the reads run A
@@ -419,13 +418,13 @@ __device__ __forceinline__ void soften(const DecodeParams& p, f32x4* s, uint32_t
 }
 
 // The tile's values times its weights s, added to the sums (dims the rows of the
-// product, queries its columns). A: steps by which LDS reads run ahead; N: parts of a weight.
-template <class T, int DH, int A, int N>
+// product, queries its columns). A: steps by which LDS reads run ahead.
+template <class T, int DH, int A>
 __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4* acc) {
   using L = Tile<T, DH>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   if constexpr (L::kBf16) {
-    bf16x8 part[N];
+    bf16x8 part[kParts];
     split_bf16(s[0], s[L::NB - 1], part);
     const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
 #pragma unroll
@@ -433,9 +432,9 @@ __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4
       const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
       const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-      for (int n = 0; n < N; ++n) acc[mb] = mfma_16x16x32(a, part[n], acc[mb]);
+      for (int n = 0; n < kParts; ++n) acc[mb] = mfma_16x16x32(a, part[n], acc[mb]);
     }
-    if constexpr (A > 0) reads_ahead<L::MB, 2, N, A>();
+    if constexpr (A > 0) reads_ahead<L::MB, 2, kParts, A>();
   } else {
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb)
@@ -448,12 +447,12 @@ __device__ __forceinline__ void weigh_tile(const char* zt, const f32x4* s, f32x4
 }
 
 // The same for RB blocks of rows, which share the reads.
-template <class T, int DH, int N, int RB>
+template <class T, int DH, int RB>
 __device__ __forceinline__ void weigh_blocks(const char* zt, const f32x4 (*s)[Tile<T, DH>::NB], f32x4 (*acc)[Tile<T, DH>::MB]) {
   using L = Tile<T, DH>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   if constexpr (L::kBf16) {
-    bf16x8 part[RB][N];
+    bf16x8 part[RB][kParts];
 #pragma unroll
     for (int b = 0; b < RB; ++b) split_bf16(s[b][0], s[b][L::NB - 1], part[b]);
     const char* zr = zt + (4 * g4 + l16 / 4) * L::ZLD + 8 * (l16 % 4);
@@ -462,11 +461,11 @@ __device__ __forceinline__ void weigh_blocks(const char* zt, const f32x4 (*s)[Ti
       const bf16x4 a0 = lds_read_tr(zr + 32 * mb), a1 = lds_read_tr(zr + 16 * L::ZLD + 32 * mb);
       const bf16x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+      for (int n = 0; n < kParts; ++n)
 #pragma unroll
         for (int b = 0; b < RB; ++b) acc[b][mb] = mfma_16x16x32(a, part[b][n], acc[b][mb]);
     }
-    reads_ahead<L::MB, 2, N * RB, 2>();
+    reads_ahead<L::MB, 2, kParts * RB, 2>();
   } else {
 #pragma unroll
     for (int mb = 0; mb < L::MB; ++mb)
@@ -711,7 +710,7 @@ __device__ __forceinline__ void place(const DecodeParams& p, int nrt, int* s_len
 // GB) 547 us, 6.1 TB/s, and 608 where the scores are stored for the weights, more
 // than their 33 MB explain. Below that by a chain of dependent loads (length, page, mask, key and value): one
 // of 305 tokens 8 us.
-template <class T, int DH, int WR, int SUB, bool ONCE, int S, int PN>
+template <class T, int DH, int WR, int SUB, bool ONCE, int S>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? (sizeof(T) == 2 ? 3 : 2) : 4))) void k_decode(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, KS = L::KS, NVI = L::NVI, MB = L::MB;
@@ -907,7 +906,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
         const int k = lane / XL, t = t0 + (k - i % XT) * STEP + lane % XL * 4;
         if (k <= i % XT && t < end) *reinterpret_cast<f32x4*>(px + t) = *reinterpret_cast<const f32x4*>(s_x[w % XW] + 4 * lane);
       }
-      weigh_tile<T, DH, 0, PN>(zt, s, acc);
+      weigh_tile<T, DH, 0>(zt, s, acc);
       wave_lds_order();
     }
   }
@@ -930,7 +929,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 // waiting for data or a barrier and a third for a turn to issue, among 267 vector
 // instructions a tile and wave, 32 of them products; 12 instructions fewer changed nothing.
 // A quarter of the LDS cycles are bank conflicts.
-template <class T, int DH, int SUB, int S, int PN>
+template <class T, int DH, int SUB, int S>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 3 : 4))) void k_decode_rows(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, KS = L::KS, MB = L::MB;
@@ -1111,7 +1110,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
       for (int nb = 0; nb < NB; ++nb)
         s[nb] = score_step<T>(*reinterpret_cast<const u32x4*>(buf + (16 * nb + l16) * KLD + 64 * j + 16 * g4), qf[j], s[nb]);
     soften<T, DH, true, S>(p, s, now, t0, at, v, least, end, r, px, nullptr, m, l, acc);
-    weigh_tile<T, DH, 2, PN>(buf + KB, s, acc);
+    weigh_tile<T, DH, 2>(buf + KB, s, acc);
   }
   __syncthreads();
   bool bad = false;
@@ -1330,24 +1329,12 @@ int row_blocks(int R, bool bf16, int dh) { return R <= 16 ? 1 : R <= 32 && !shar
 // batches would gain (64 of up to 2048, 8 heads of 4 rows 64.6 -> 59.2).
 constexpr int kOnceTokens = 1024;
 
-// Parts of a bfloat16 weight: three, all its 24 bits. Calls over trees and listed pages with
-// bfloat16 outputs, whose half step is 2^-9, take two, so that a weight is off by 2^-17 of
-// itself at most, and a sum of weighted values by 2^-17 of the sum of their magnitudes (the
-// others keep what they have always answered). 32 sequences of 256 to 4096 tokens, 8 key
-// heads of 96 rows of drafted tokens: 91 us with three, 88 with two.
-template <class T, int DH, int WR, int SUB, int S, int N>
-auto kernel_of(const DecodeParams& p) {
-  if constexpr (WR == 4)
-    return k_decode_rows<T, DH, SUB, S, N>;
-  else
-    return p.max_len >= kOnceTokens && !p.x ? k_decode<T, DH, WR, SUB, true, S, N> : k_decode<T, DH, WR, SUB, false, S, N>;
-}
 template <class T, int DH, int WR, int SUB, int S>
 auto kernel_for(const DecodeParams& p) {
-  if constexpr (sizeof(T) == 2 && S != kPrefix) {
-    if (!p.out_f32) return kernel_of<T, DH, WR, SUB, S, 2>(p);
-  }
-  return kernel_of<T, DH, WR, SUB, S, kParts>(p);
+  if constexpr (WR == 4)
+    return k_decode_rows<T, DH, SUB, S>;
+  else
+    return p.max_len >= kOnceTokens && !p.x ? k_decode<T, DH, WR, SUB, true, S> : k_decode<T, DH, WR, SUB, false, S>;
 }
 
 template <class T, int DH, int WR, int S>

@@ -88,7 +88,7 @@ __device__ __forceinline__ void add_blocks(const DecodeParams& p, int b, int h, 
 // That chain and the longest sequence bound it: of 88 us a tile of tokens and 32 rows keeps
 // the vector and matrix units busy for a half. Sequences of 64 tokens, which have the chain
 // alone, take 33 us where k_decode_rows took 23.
-template <class T, int DH, int SUB, int PN>
+template <class T, int DH, int SUB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_tree_rows(DecodeParams p) {
   using L = Tile<T, DH>;
   constexpr int TK = L::TK, NB = L::NB, KS = L::KS, NVI = L::NVI, MB = L::MB;
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
       for (int n = 0; n < RB; ++n)
         soften<T, DH, true, kTree>(p, s[n], ok, t0, nullptr, v[n], least, end, 0, nullptr, nullptr, m[n], l[n], acc[n]);
-      weigh_blocks<T, DH, PN, RB>(zt, s, acc);
+      weigh_blocks<T, DH, RB>(zt, s, acc);
       wave_lds_order();
     }
   }
@@ -278,12 +278,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   add_blocks<T, DH, RB>(p, b, h, rtile, sp, m, l, acc, smem, s_m, s_l);
 }
 
-template <class T, int DH, int PN>
+template <class T, int DH>
 void go_rows(const DecodeParams& p, hipStream_t s) {
   const int sub = p.c.ds >= Tile<T, DH>::EP ? 1 : Tile<T, DH>::EP / p.c.ds;
-  auto kern = sub == 1 ? k_tree_rows<T, DH, 1, PN> : k_tree_rows<T, DH, 2, PN>;
+  auto kern = sub == 1 ? k_tree_rows<T, DH, 1> : k_tree_rows<T, DH, 2>;
   if constexpr (sizeof(T) == 2) {
-    if (sub == 4) kern = k_tree_rows<T, DH, 4, PN>;
+    if (sub == 4) kern = k_tree_rows<T, DH, 4>;
   }
   const unsigned items = static_cast<unsigned>(p.B) * p.c.H * p.n_split;
   hipLaunchKernelGGL(kern, dim3((items + 7) / 8 * 8 * ((p.R + kTreeRows - 1) / kTreeRows)), dim3(256), 0, s, p);
@@ -292,10 +292,7 @@ void go_rows(const DecodeParams& p, hipStream_t s) {
 template <class T, int DH>
 hipError_t launch_rows(DecodeParams p, hipStream_t s) {
   p.ordered = p.n_split == 1 && p.B > 1 && p.B <= kOrderMax && p.max_len >= 512;
-  if (sizeof(T) == 2 && !p.out_f32)
-    go_rows<T, DH, sizeof(T) == 2 ? 2 : kParts>(p, s);
-  else
-    go_rows<T, DH, kParts>(p, s);
+  go_rows<T, DH>(p, s);
   launch_join<T, DH, kTree>(p, s);
   return hipGetLastError();
 }
