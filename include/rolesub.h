@@ -565,7 +565,8 @@ rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pag
  *   q_weight, k_weight [dh] (dtype) or NULL: that tensor is not normed, only turned
  *   (then with rolesub_rotary's results, bit for bit); eps > 0, finite.
  *   The other arguments, strides, outputs and errors are those of rolesub_rotary.
- * A head whose squares pass the range of 32 bits is normed all the same; an infinity
+ * A head whose squares pass the range of 32 bits or fall below it is normed all the same,
+ * and so are numbers whose products with a weight would; an infinity
  * gives NaN in its place and zeros in its head's other dims before the turn.
  * ------------------------------------------------------------------------ */
 rolesub_status rolesub_norm_rotary(int32_t B, int32_t T, int32_t H, int32_t Hkv, int32_t dh, rolesub_dtype dtype,

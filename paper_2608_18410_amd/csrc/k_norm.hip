@@ -52,22 +52,29 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// 1 / sqrt(mean x^2 + eps) of a row from its sum of squares; a lane's elements again, times
-// 2^-64, where the squares pass the range or are not finite.
+// Factors of a row: x becomes (x by) inv, with inv = 1 / sqrt(mean x^2 + eps). `by` is 1 but
+// where inv is below the normal numbers.
+struct Root {
+  float by, inv;
+};
+// The factors from the row's sum of squares. Where that or eps leaves the range (or the sum
+// is NaN), a lane's elements are squared again, scaled: by 2^-68, so that up to 128 squares of
+// the largest number stay below 2^127, or by 2^64, where x below 2^-46 still has squares
+// and the smallest eps is 2^-21.
 template <int LPR, int N>
-__device__ __forceinline__ float inverse_root(float sq, const float (&x)[N], float per, float eps) {
-  float inv = __builtin_amdgcn_rsqf(sq * per + eps);
-  if (__any(!(sq < __builtin_inff()))) {
-    float small = 0.f;
+__device__ __forceinline__ Root inverse_root(float sq, const float (&x)[N], float per, float eps) {
+  const float a = __builtin_fmaf(sq, per, eps);
+  Root r = {1.f, __builtin_amdgcn_rsqf(a)};
+  const bool high = !(a < __builtin_inff()), far = high || a < 0x1p-100f;
+  if (__any(far)) {
+    const float f = high ? 0x1p-68f : 0x1p64f;
+    float again = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float y = x[i] * 0x1p-64f;
-      small += y * y;
-    }
-    small = row_sum<LPR>(small);
-    if (!(sq < __builtin_inff())) inv = __builtin_amdgcn_rsqf(small * per) * 0x1p-64f;
+    for (int i = 0; i < N; ++i) again = __builtin_fmaf(x[i] * f, x[i] * f, again);
+    const float root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<LPR>(again), per, eps * f * f));
+    if (far) r = high ? Root{0x1p-32f, root * 0x1p-36f} : Root{1.f, root * 0x1p64f};
   }
-  return inv;
+  return r;
 }
 
 // Cosines and sines of one token's pairs, a pair a lane, for its wave through LDS.
@@ -190,25 +197,29 @@ __device__ __forceinline__ void turn_whole(const TurnParams& p, int64_t tok, int
         v[2 * x + 1] = tof(pb[x]);
       }
     }
-    float inv = 1.f;
-    if (g.weight) {
+    if (g.weight) {  // the root before the weights, whose products with x may leave the range
       float sq = 0.f;
 #pragma unroll
       for (int x = 0; x < 2 * V; ++x) sq = __builtin_fmaf(v[x], v[x], sq);
-      inv = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
+      const Root root = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
+      if (__any(root.by != 1.f))
+#pragma unroll
+        for (int x = 0; x < 2 * V; ++x) v[x] *= root.by;
+#pragma unroll
+      for (int x = 0; x < 2 * V; ++x) v[x] *= root.inv;
     }
     float y[2 * V];
 #pragma unroll
     for (int x = 0; x < V; ++x) {
-      y[2 * x] = __builtin_fmaf(v[2 * x], ca[x], -(v[2 * x + 1] * sb[x])) * inv;
-      y[2 * x + 1] = __builtin_fmaf(v[2 * x], sa[x], v[2 * x + 1] * cb[x]) * inv;
+      y[2 * x] = __builtin_fmaf(v[2 * x], ca[x], -(v[2 * x + 1] * sb[x]));
+      y[2 * x + 1] = __builtin_fmaf(v[2 * x], sa[x], v[2 * x + 1] * cb[x]);
     }
     if (some) {  // pairs that are not turned (a zero times what is not finite would reach the other)
 #pragma unroll
       for (int x = 0; x < V; ++x) {
         const bool on = !((stay >> x) & 1u);
-        y[2 * x] = on ? y[2 * x] : v[2 * x] * ca[x] * inv;
-        y[2 * x + 1] = on ? y[2 * x + 1] : v[2 * x + 1] * cb[x] * inv;
+        y[2 * x] = on ? y[2 * x] : v[2 * x] * ca[x];
+        y[2 * x + 1] = on ? y[2 * x + 1] : v[2 * x + 1] * cb[x];
       }
     }
     u32x4 ya, yb;
@@ -292,23 +303,25 @@ __device__ __forceinline__ void turn_any(const TurnParams& p, int64_t tok, int h
         const T* xa = reinterpret_cast<const T*>(&a[i]);
         const T* xb = reinterpret_cast<const T*>(&b);
         const T* xd = reinterpret_cast<const T*>(&d);
-        float v[V], inv = 1.f;
+        float v[V];
+        Root root = {1.f, 1.f};
 #pragma unroll
         for (int x = 0; x < V; ++x) v[x] = tof(xa[x]);
         if (g.weight) {
           float sq = 0.f;
 #pragma unroll
           for (int x = 0; x < V; ++x) sq = __builtin_fmaf(v[x], v[x], sq);
-          inv = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
+          root = inverse_root<LPR>(row_sum<LPR>(sq), v, 1.f / DH, p.eps);
         }
         u32x4 y;
         T* vy = reinterpret_cast<T*>(&y);
 #pragma unroll
         for (int x = 0; x < V; ++x) {
-          const float other = tof(IL ? xa[x ^ 1] : e0 + x < n ? xb[x] : xd[x]);
+          const float mine = v[x] * root.by * root.inv;
+          const float other = tof(IL ? xa[x ^ 1] : e0 + x < n ? xb[x] : xd[x]) * root.by * root.inv;
           const bool on = (turn >> x) & 1u;
-          const float r = on ? __builtin_fmaf(v[x], f1[x], other * f2[x]) : v[x] * wt[x];
-          vy[x] = on || g.weight ? fromf<T>(r * inv) : xa[x];
+          const float r = on ? __builtin_fmaf(mine, f1[x], other * f2[x]) : mine * wt[x];
+          vy[x] = on || g.weight ? fromf<T>(r) : xa[x];
         }
         if (h < g.h1) *reinterpret_cast<u32x4*>(g.out + h * g.ld + e0) = y;
       }

@@ -46,3 +46,57 @@ def test_selected_outputs_round_the_same_sums(rep, n_sel, dh):
     assert same(one, rs.attend_selected(*args, out_dtype=f32).to(bf))
     for _ in range(3):
         assert same(one, rs.attend_selected(*args))
+
+
+# ---- norms at the ends of the range --------------------------------------------
+
+def _ends(rng, dh):
+    """Heads, weights and eps at the ends of float32's range."""
+    x = rng.standard_normal((9, dh))
+    sign = np.where(rng.random((9, dh)) < 0.5, -1.0, 1.0)
+    big = np.minimum(np.abs(x) * 1e38, 3.3e38) * sign
+    two = 1e-3 * x
+    two[:, 7], two[:, dh - 1] = 3e38, -3e38
+    one, w = np.ones(dh), rng.standard_normal(dh)
+    return [
+        ("every dim near the largest number", 3.3e38 * sign, one, 1e-6),
+        ("squares whose sum passes 2^256", 4e37 * sign, w, 1e-6),
+        ("a few of them", two, one, 1e-6),
+        ("with weights", big, 8 * w, 1e-6),
+        ("times the weight past the range", 1e15 * x, 1e30 * w, 1e-6),
+        ("times the weight below the range", 1e-20 * x, 1e-30 * w, 1e-30),
+        ("squares below the range and so is eps", 1e-22 * x, w, 1e-43),
+        ("eps below the normal numbers", 1e-3 * x, w, 1e-40),
+        ("zeros with eps below the normal numbers", 0 * x, w, 1e-44),
+        ("eps near the largest number", 1e19 * x, 1e10 * w, 3e38),
+    ]
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,pairs", [(128, 64), (64, 16), (128, 61), (64, 3)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_norm_rotary_at_the_ends_of_the_range(dtype, dh, pairs, interleaved):
+    rng = np.random.default_rng(31)
+    pos, f = rng.integers(0, 99, (1, 3, 1)), rng.random(pairs).astype(np.float32)
+    ft = torch.from_numpy(f).to(DEV)
+    for name, x, w, eps in _ends(rng, dh):
+        q, wt = dev(x.reshape(1, 3, 3, dh), dtype), dev(w, dtype)
+        assert torch.isfinite(q).all() and torch.isfinite(wt).all()
+        n = O.norm(num(q), num(wt), np.float32(eps))
+        ref = O.rotary(n, pos, f, None, interleaved)
+        got, _ = rs.norm_rotary(q, None, wt, None, float(np.float32(eps)), ints(pos), ft, interleaved=interleaved)
+        assert torch.isfinite(got).all(), name
+        # (below 2^-126 a float32 number is off by 2^-150, a bfloat16 one by 2^-134)
+        err = np.abs(num(got) - ref)
+        assert (err <= _norm_tol(n, ref, dtype) + (2.0 ** -134 if dtype == bf else 2.0 ** -149)).all(), (name, float(err.max()))
+
+
+def test_appended_keys_at_the_ends_of_the_range():
+    rng = np.random.default_rng(32)
+    for dtype in (bf, f32):
+        for name, x, w, eps in _ends(rng, 64):
+            c = full_cache(rng, 2, 16, 3, 64, 8, 8, dtype)
+            k, wk, pos, f = dev(x.reshape(1, 3, 3, 64), dtype), dev(w, dtype), ints([[3, 1, 4]]), torch.rand(32, device=DEV)
+            rs.append_rotary(c, k, torch.zeros_like(k), ints([[1, 2, 3]]), ints([[1]]), ints([5]), pos, f, k_weight=wk, eps=float(np.float32(eps)))
+            want = rs.norm_rotary(None, k, None, wk, float(np.float32(eps)), pos, f)[1]
+            assert same(c.K[1, :, 5:8].transpose(0, 1), want[0]), name
