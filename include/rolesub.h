@@ -563,7 +563,8 @@ rolesub_status rolesub_cache_compact(const rolesub_pages* src, const rolesub_pag
  *   n = x w / sqrt(mean(x^2) + eps)   per token and head, then rolesub_rotary's turn
  * in 32 bits throughout, rounded once.
  *   q_weight, k_weight [dh] (dtype) or NULL: that tensor is not normed, only turned
- *   (then with rolesub_rotary's results, bit for bit); eps > 0, finite.
+ *   (then with rolesub_rotary's results, bit for bit, but for the sign and payload of
+ *   a NaN that a turn makes); eps > 0, finite.
  *   The other arguments, strides, outputs and errors are those of rolesub_rotary.
  * A head whose squares pass the range of 32 bits or fall below it is normed all the same,
  * and so are numbers whose products with a weight would; an infinity

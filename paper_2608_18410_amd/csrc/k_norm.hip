@@ -235,6 +235,23 @@ __device__ __forceinline__ void turn_whole(const TurnParams& p, int64_t tok, int
         tb[x] = fromf<T>(y[2 * x + 1]);
       }
     }
+    if (some && !g.weight) {  // neither normed nor turned: its bits, a NaN's too
+      const T* pa = reinterpret_cast<const T*>(&a);
+      const T* pb = reinterpret_cast<const T*>(&b);
+#pragma unroll
+      for (int x = 0; x < V; ++x) {
+        const bool on = !((stay >> x) & 1u);
+        if constexpr (IL) {
+          T* to = (x < V / 2 ? ta : tb) + 2 * x % V;
+          const T* from = (x < V / 2 ? pa : pb) + 2 * x % V;
+          to[0] = on ? to[0] : from[0];
+          to[1] = on ? to[1] : from[1];
+        } else {
+          ta[x] = on ? ta[x] : pa[x];
+          tb[x] = on ? tb[x] : pb[x];
+        }
+      }
+    }
     if (h < g.h1) {
       T* to = g.out + h * g.ld;
       *reinterpret_cast<u32x4*>(to + oa) = ya;

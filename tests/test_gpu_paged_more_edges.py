@@ -100,3 +100,51 @@ def test_appended_keys_at_the_ends_of_the_range():
             rs.append_rotary(c, k, torch.zeros_like(k), ints([[1, 2, 3]]), ints([[1]]), ints([5]), pos, f, k_weight=wk, eps=float(np.float32(eps)))
             want = rs.norm_rotary(None, k, None, wk, float(np.float32(eps)), pos, f)[1]
             assert same(c.K[1, :, 5:8].transpose(0, 1), want[0]), name
+
+
+# ---- bits that are only moved ---------------------------------------------------
+
+def _payloads(rng, x):
+    """x with NaN of every kind (quiet, signalling, negative, of any payload) in a tenth of its places."""
+    bits = x.view({2: torch.int16, 4: i32}[x.element_size()])
+    wide, top, low = (16, 0x7F80, 7) if x.element_size() == 2 else (32, 0x7F800000, 23)
+    nan = top | rng.integers(1, 1 << low, tuple(x.shape)) | (rng.integers(0, 2, tuple(x.shape)) << (wide - 1))
+    nan = np.where(nan >= 1 << (wide - 1), nan - (1 << wide), nan)
+    put = torch.from_numpy(rng.random(tuple(x.shape)) < 0.1).to(DEV)
+    bits.copy_(torch.where(put, torch.from_numpy(nan).to(DEV), bits.long()).to(bits.dtype))
+    return x
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("pairs", [64, 32, 16, 61, 3])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_dims_that_are_not_turned_keep_their_bits(dtype, pairs, interleaved):
+    rng = np.random.default_rng(41)
+    q, k = (_payloads(rng, dev(rng.standard_normal((2, 9, h, 128)), dtype)) for h in (5, 2))
+    pos, f = ints(rng.integers(0, 99, (2, 9, 2))), torch.rand(pairs, device=DEV)
+    ax = torch.randint(0, 3, (pairs,), device=DEV, dtype=torch.uint8)  # a third of the pairs has no axis
+    want = rs.rotary(q, k, pos, f, ax, interleaved=interleaved)
+    got = rs.norm_rotary(q, k, None, None, 1e-6, pos, f, ax, interleaved=interleaved)
+    e = torch.arange(128, device=DEV)
+    j = (e // 2 if interleaved else torch.where(e < pairs, e, e - pairs)).clamp(max=pairs - 1)
+    still = (e >= 2 * pairs) | (ax[j] >= 2)
+    for x, y, z in ((q, *(o[0] for o in (got, want))), (k, *(o[1] for o in (got, want)))):
+        assert same(y[..., still], x[..., still]) and same(z[..., still], x[..., still])
+        # what a turn makes of a NaN is a NaN whose sign and payload IEEE 754 (6.2, 6.3) leaves open
+        assert torch.equal(torch.isnan(y), torch.isnan(z)) and same(y.nan_to_num(1.0), z.nan_to_num(1.0))
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("G", [8, 32])
+def test_values_kept_as_they_are_keep_their_bits(dtype, G):
+    rng = np.random.default_rng(42)
+    for dh in (64, 128):
+        c = full_cache(rng, 6, 16, 2, dh, G, G, dtype)
+        d = rs.PagedCache(*(x.clone() for x in c.tensors()))
+        k = dev(rng.standard_normal((2, 20, 2, dh)), dtype)
+        v = _payloads(rng, dev(rng.standard_normal((2, 20, 2, dh)), dtype))
+        mask, t, n = ints(rng.integers(0, 1 << min(G, 30), (2, 20))), ints([[0, 1, 2], [3, 4, 5]]), ints([5, 16])
+        pos, f = ints(rng.integers(0, 99, (2, 20))), torch.rand(dh // 2, device=DEV)
+        rs.append_rotary(c, k, v, mask, t, n, pos, f)
+        rs.cache_append(d, rs.rotary(None, k, pos, f)[1], v, mask, t, n)
+        assert all(same(a, b) for a, b in zip(c.tensors(), d.tensors()))
