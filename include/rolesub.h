@@ -663,7 +663,10 @@ rolesub_status rolesub_cache_accept(const rolesub_pages* pages, rolesub_dtype dt
  *   bounds [n_pages,H,2,dh] (dtype), 16-byte aligned, outside the cache and apart from
  *   table and lens; lens [B] int32 counts the new tokens. Other pages' are not written.
  * NaN is passed over (a dim of nothing else has +inf below -inf). To be called after
- * tokens are appended, and, for all pages, after they are moved.
+ * tokens are appended, and, for all pages, after they are moved. Sequences of the call may
+ * share a page, in the same place of their tables: its bounds are then over the tokens of
+ * the longest, also where only shorter ones have it among their last T. Sequences that are
+ * not in the call hold no more tokens in a page whose bounds are written.
  * ------------------------------------------------------------------------ */
 rolesub_status rolesub_page_bounds(const rolesub_pages* pages, rolesub_dtype dtype, int32_t B, int32_t T,
                                    const int32_t* table, int32_t max_pages, const int32_t* lens, void* bounds,

@@ -273,12 +273,13 @@ def accept(cache, table, lens, sets, leaf):
 def page_bounds(cache, table, lens, bounds, T):
     """Writes into bounds [n,H,2,dh] in place."""
     P = cache["K"].shape[2]
+    n = [min(max(int(x), 0), table.shape[1] * P) for x in lens]
     for b in range(table.shape[0]):
-        n = min(max(int(lens[b]), 0), table.shape[1] * P)
-        for i in range(max(n - T, 0) // P, -(-n // P)):
+        for i in range(max(n[b] - T, 0) // P, -(-n[b] // P)):
             pg = int(table[b, i])
             if T > 0 and 0 <= pg < cache["K"].shape[0]:
-                k = cache["K"][pg, :, :min(P, n - i * P)]
+                held = max(n[x] - i * P for x in range(table.shape[0]) if int(table[x, i]) == pg)  # of those that share it
+                k = cache["K"][pg, :, :min(P, held)]
                 bounds[pg, :, 0] = np.fmin.reduce(np.where(np.isnan(k), np.inf, k), axis=1)
                 bounds[pg, :, 1] = np.fmax.reduce(np.where(np.isnan(k), -np.inf, k), axis=1)
 

@@ -11,8 +11,10 @@ namespace {
 
 // Bounds of a page's keys in every dim, a wave for each page and head: 16-byte pieces of
 // its rows, then the lanes of one piece. fminf and fmaxf pass over NaN. Whole pages are
-// gone over again, as what a page holds may have moved. A chain of loads (length, page,
-// rows): 3 us for one of 32 heads, 4.9 for 8 sequences with a page of 64 tokens each.
+// gone over again, as what a page holds may have moved. Where a sequence ends inside a page
+// that others have in the same place, the longest of them counts: all that write its
+// bounds then write the same. A chain of loads (length, page, rows): 3 us for one of 32
+// heads, 4.9 for 8 sequences with a page of 64 tokens each.
 template <class T, int DH, int U>
 __global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
   constexpr int V = 16 / sizeof(T), LPR = DH / V, RPI = 64 / LPR;
@@ -22,12 +24,22 @@ __global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
   if (job >= pages * c.H) return;
   const int h = static_cast<int>(job % c.H), i = static_cast<int>(job / c.H % np), b = static_cast<int>(job / c.H / np);
   const int64_t cap = static_cast<int64_t>(p.max_pages) << c.shift;
+  const int first = p.lens[min(lane, p.B - 1)];  // of the sequences, one a lane
   const int64_t len = min(static_cast<int64_t>(max(p.lens[b], 0)), cap);
   const int64_t pi = (max(len - p.T, static_cast<int64_t>(0)) >> c.shift) + i, t0 = pi << c.shift;
   if (t0 >= len) return;
+  int n = static_cast<int>(min(len - t0, static_cast<int64_t>(c.page)));
   const int page = p.table[static_cast<int64_t>(b) * p.max_pages + pi];
+  if (n < c.page) {
+    for (int x = lane; x < p.B; x += 64) {
+      const int64_t other = min(static_cast<int64_t>(max(x < 64 ? first : p.lens[x], 0)), cap);
+      if (p.table[static_cast<int64_t>(x) * p.max_pages + pi] == page && other > t0 + n)
+        n = static_cast<int>(min(other - t0, static_cast<int64_t>(c.page)));
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) n = max(n, __shfl_xor(n, o, kWave));
+  }
   if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(c.n_pages)) return;
-  const int n = static_cast<int>(min(len - t0, static_cast<int64_t>(c.page)));
   const int64_t head = static_cast<int64_t>(page) * c.H + h;
   const char* k = static_cast<const char*>(c.K) + (head << c.shift) * DH * static_cast<int64_t>(sizeof(T)) + lane % LPR * 16;
   float lo[V], hi[V];

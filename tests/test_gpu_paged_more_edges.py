@@ -148,3 +148,35 @@ def test_values_kept_as_they_are_keep_their_bits(dtype, G):
         rs.append_rotary(c, k, v, mask, t, n, pos, f)
         rs.cache_append(d, rs.rotary(None, k, pos, f)[1], v, mask, t, n)
         assert all(same(a, b) for a, b in zip(c.tensors(), d.tensors()))
+
+
+# ---- bounds of shared pages ---------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("B", [2, 7, 70, 200])
+def test_bounds_of_a_shared_page_hold_for_all_its_sequences(dtype, B):
+    """Sequences with the same first pages and lengths that end in one of them: its bounds are over
+    the tokens of the longest, whichever comes last, and also where only its end is among the last T."""
+    rng = np.random.default_rng(B)
+    P, H, dh, W = 64, 2, 128, 4
+    c = full_cache(rng, 40 + B, P, H, dh, 8, 8, dtype)
+    c.K[:, :, 1::2] *= 3  # later tokens widen the bounds
+    table = rng.permutation(40)[:W][None].repeat(B, 0)
+    table[1::3, 3] = 40 + np.arange(B)[1::3]  # a last page of its own
+    for lens in ([P + 1 + (37 * i) % (2 * P) for i in range(B)], [P + 60 - i % 50 for i in range(B)], [3 * P + 1] + [P + 5] * (B - 1),
+                 [P + 5] * (B - 1) + [3 * P + 1], [P] + [P + 9] * (B - 1)):
+        for T in (1, 5, 10 ** 6):
+            b = dev(rng.standard_normal((40 + B, H, 2, dh)), dtype)
+            ref = num(b).copy()
+            held = {}
+            for s in range(B):
+                for i in range(page_count(lens[s], P)):
+                    held[table[s, i]] = max(held.get(table[s, i], 0), min(P, lens[s] - i * P))
+            for s in range(B):
+                for i in range(max(lens[s] - T, 0) // P, page_count(lens[s], P)):
+                    k = num(c.K[int(table[s, i]), :, : held[table[s, i]]])
+                    ref[table[s, i], :, 0], ref[table[s, i], :, 1] = k.min(1), k.max(1)
+            for _ in range(3):
+                again = b.clone()
+                rs.page_bounds(c, ints(table), ints(lens), again, T)
+                assert np.array_equal(num(again), ref), (lens[:4], T)
