@@ -702,6 +702,8 @@ rolesub_status rolesub_select_pages(const rolesub_pages* pages, rolesub_dtype dt
  *   sel [B,Tq,H,n_sel] int32: pages by their number in the sequence, in any order; a
  *   number outside [0, max_pages) stands for no page, and a page listed twice counts
  *   twice. n_sel >= 1; n_sel*page and max_pages*page at most 2^30.
+ *   There is no max_len: where one that ends inside a page bounded the choice, lens (or
+ *   visible) has to be no more than it.
  *   The other arguments, the workspace (its own size) and errors as
  *   rolesub_attend_paged; no weights are added up.
  * ------------------------------------------------------------------------ */

@@ -194,7 +194,9 @@ def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.Page
             rs.page_bounds(cache, table, new_lens, bounds, q.shape[1])
             sel = rs.select_pages(q, cache, bounds, table, new_lens, n_sel, first=first, recent=recent, visible=visible,
                                   max_len=max_len)
-            out = rs.attend_selected(q, cache, table, new_lens, sel, R, visible=visible, workspace=workspace, out=out)
+            # (a bound inside a page, whose other tokens are not seen either)
+            seen = new_lens.clamp(max=max_len) if max_len and max_len % cache.page else new_lens
+            out = rs.attend_selected(q, cache, table, seen, sel, R, visible=visible, workspace=workspace, out=out)
         else:
             out = rs.attend_paged(q, cache, table, new_lens, R, visible=visible, max_len=max_len, mass=mass, decay=decay,
                                   workspace=workspace, out=out)

@@ -180,3 +180,27 @@ def test_bounds_of_a_shared_page_hold_for_all_its_sequences(dtype, B):
                 again = b.clone()
                 rs.page_bounds(c, ints(table), ints(lens), again, T)
                 assert np.array_equal(num(again), ref), (lens[:4], T)
+
+
+# ---- layers -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("T", [1, 4])
+def test_few_pages_see_nothing_past_max_len(dtype, T):
+    """A bound inside the last chosen page hides what attention over all pages hides too."""
+    m = Model(61, dtype, 3)
+    bounds = torch.zeros((m.cache.K.shape[0], m.H, 2, m.dh), device=DEV, dtype=dtype)
+    lens = ints([60, 75, 70])
+    rs.page_bounds(m.cache, m.table, lens, bounds, 10 ** 6)
+    few, everything = m.clone(), m.clone()
+    x = m.tokens(T)
+    x["v"][:] = float("nan")  # the new tokens of the last two lie past the bound
+    pos = lens[:, None] + torch.arange(T, device=DEV, dtype=i32)
+    args = dict(positions=pos, scores_in=x["scores"], max_len=70, **m.kw())
+    got = decode_layer(*m.common(x, few), lens, lens + T, n_sel=12, bounds=bounds, **args)
+    want = decode_layer(*m.common(x, everything), lens, lens + T, **args)
+    assert torch.isnan(want[0]).any() and not torch.isnan(want[1:]).any()
+    assert not torch.isnan(got[1:]).any()
+    half = 2.0 ** -8 if dtype == bf else 2.0 ** -24
+    apart = 2.0 ** -15 * m.dh ** 0.5 * float(few.V[~torch.isnan(few.V)].abs().max())  # see _apart there
+    assert bool(((got[1:].float() - want[1:].float()).abs() <= 2 * half * want[1:].float().abs() + apart).all())

@@ -1,7 +1,12 @@
 """The paged cache's normed heads, appends, drafted trees and chosen pages at their edges, without a GPU."""
+import types
+
 import numpy as np
+import pytest
+import torch
 
 from oracle import paged as O
+from paper_2608_18410_amd import pipeline
 
 
 def test_oracle_bounds_of_a_shared_page_are_those_of_its_longest_sequence():
@@ -18,3 +23,17 @@ def test_oracle_bounds_of_a_shared_page_are_those_of_its_longest_sequence():
                 k = c["K"][table[s, i], :, : n - i * P]
                 assert (b[table[s, i], :, 0] <= k.min(1)).all() and (b[table[s, i], :, 1] >= k.max(1)).all()
         assert (b[3] == 7.0).all()
+
+
+@pytest.mark.parametrize("max_len,want", [(0, [5, 40, 70]), (64, [5, 40, 70]), (41, [5, 40, 41]), (1000, [5, 40, 70]), (1, [1, 1, 1])])
+def test_few_pages_are_attended_to_up_to_max_len(monkeypatch, max_len, want):
+    """Pages are chosen among the tokens below max_len; one that it ends in is seen so far."""
+    seen = []
+    for name in ("append_rotary", "page_bounds", "select_pages"):
+        monkeypatch.setattr(pipeline.rs, name, lambda *a, **kw: torch.zeros(1, 1))
+    monkeypatch.setattr(pipeline.rs, "route", lambda *a, **kw: {"mask": None})
+    monkeypatch.setattr(pipeline.rs, "attend_selected", lambda q, c, t, lens, *a, **kw: seen.append(lens.tolist()))
+    cache = types.SimpleNamespace(page=16)
+    lens = torch.tensor([5, 40, 70], dtype=torch.int32)
+    pipeline.decode_layer(*[None] * 8, cache, torch.zeros(3, 9), lens - 1, lens, positions=1, n_sel=3, bounds=1, max_len=max_len)
+    assert seen == [want] and lens.tolist() == [5, 40, 70]
