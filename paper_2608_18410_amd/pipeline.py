@@ -203,12 +203,22 @@ def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.Page
     return _returned(stream, out)[0]
 
 
+_REFUSED = (1, 2)  # ROLESUB_ERR_INVALID_ARG, ROLESUB_ERR_UNSUPPORTED: nothing was launched
+
+
 def _append(cache, q, k, v, R, mask, table, lens, positions, inv_freq, axis, q_weight=None, k_weight=None, eps=1e-6,
             n_new=None):
     """New tokens into their pages, turned where they have positions. Returns the queries."""
     if positions is not None:
-        return rs.append_rotary(cache, k, v, mask, table, lens, positions, inv_freq, axis, R=R, q=q, q_weight=q_weight,
-                                k_weight=k_weight, eps=eps, n_new=n_new)
+        try:
+            return rs.append_rotary(cache, k, v, mask, table, lens, positions, inv_freq, axis, R=R, q=q, q_weight=q_weight,
+                                    k_weight=k_weight, eps=eps, n_new=n_new)
+        except rs.RolesubError as e:
+            if e.status not in _REFUSED or R is None:
+                raise
+        # operands that one pass refuses, as those that lie in the cache: the separate calls read
+        # them before anything is appended, and leave the same bits
+        q, k = rs.norm_rotary(q, k, q_weight, k_weight, eps, positions, inv_freq, axis)
     z = rs.rotate_values(v, R)
     rs.cache_append(cache, k, z, mask, table, lens, **({} if n_new is None else {"n_new": n_new}))
     return q

@@ -204,3 +204,21 @@ def test_few_pages_see_nothing_past_max_len(dtype, T):
     half = 2.0 ** -8 if dtype == bf else 2.0 ** -24
     apart = 2.0 ** -15 * m.dh ** 0.5 * float(few.V[~torch.isnan(few.V)].abs().max())  # see _apart there
     assert bool(((got[1:].float() - want[1:].float()).abs() <= 2 * half * want[1:].float().abs() + apart).all())
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+def test_layers_take_operands_that_lie_in_the_cache(dtype):
+    """Queries, keys and values that are views of the pages: read before anything is appended."""
+    m = Model(62, dtype, 2, rep=1)
+    x = m.tokens(3)
+    lens, pos = ints([20, 33]), ints([[20, 21, 22], [33, 34, 35]])
+    n = 2 * 3 * m.H * m.dh
+    for weights in (True, False):
+        kw = dict(positions=pos, scores_in=x["scores"], **(m.kw() if weights else dict(inv_freq=m.f)))
+        for i, name in enumerate(("q", "k", "v")):
+            a, b = m.clone(), m.clone()
+            src = (a.K if i < 2 else a.V).flatten()[i * n: (i + 1) * n].view(2, 3, m.H, m.dh)
+            got = decode_layer(*m.common({**x, name: src}, a), lens, lens + 3, **kw)
+            src = (b.K if i < 2 else b.V).flatten()[i * n: (i + 1) * n].view(2, 3, m.H, m.dh).clone()
+            want = decode_layer(*m.common({**x, name: src}, b), lens, lens + 3, **kw)
+            assert same(got, want) and all(same(u, v) for u, v in zip(a.tensors(), b.tensors())), name

@@ -37,3 +37,28 @@ def test_few_pages_are_attended_to_up_to_max_len(monkeypatch, max_len, want):
     lens = torch.tensor([5, 40, 70], dtype=torch.int32)
     pipeline.decode_layer(*[None] * 8, cache, torch.zeros(3, 9), lens - 1, lens, positions=1, n_sel=3, bounds=1, max_len=max_len)
     assert seen == [want] and lens.tolist() == [5, 40, 70]
+
+
+@pytest.mark.parametrize("status,ways", [(1, 3), (2, 3), (4, 0)])
+def test_what_one_pass_refuses_goes_through_the_separate_calls(monkeypatch, status, ways):
+    """As operands that lie in the cache; a launch that failed is an error."""
+    made = []
+
+    def refuse(*a, **kw):
+        raise pipeline.rs.RolesubError("rolesub_append_rotary", status, "K overlaps q")
+
+    monkeypatch.setattr(pipeline.rs, "append_rotary", refuse)
+    monkeypatch.setattr(pipeline.rs, "route", lambda *a, **kw: {"mask": None})
+    monkeypatch.setattr(pipeline.rs, "norm_rotary", lambda *a, **kw: (made.append("norm_rotary"), ("q", "k"))[1])
+    monkeypatch.setattr(pipeline.rs, "rotate_values", lambda *a, **kw: made.append("rotate_values"))
+    monkeypatch.setattr(pipeline.rs, "cache_append", lambda *a, **kw: made.append("cache_append"))
+    monkeypatch.setattr(pipeline.rs, "attend_paged", lambda q, *a, **kw: q)
+    args = [None] * 5 + ["R"] + [None] * 6
+    if ways:
+        assert pipeline.decode_layer(*args, positions=1) == "q"
+        assert made == ["norm_rotary", "rotate_values", "cache_append"]
+    else:
+        with pytest.raises(pipeline.rs.RolesubError):
+            pipeline.decode_layer(*args, positions=1)
+    with pytest.raises(pipeline.rs.RolesubError):
+        pipeline.decode_layer(*[None] * 12, positions=1)
