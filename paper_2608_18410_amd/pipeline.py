@@ -179,7 +179,9 @@ def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.Page
     pages only, the first, the recent and those whose bounds [n_pages,H,2,dh] promise the
     highest scores; the bounds of the new tokens' pages are brought up to date on the way
     (page_bounds with T >= the longest length makes them all), and no weight is
-    accumulated. Returns the attention output [B,T,Hq,dh]."""
+    accumulated; a workspace of the larger of select_pages_workspace_size and
+    attend_selected_workspace_size serves both calls, one of the latter the attention
+    alone. Returns the attention output [B,T,Hq,dh]."""
     if n_sel and mass is not None:
         raise ValueError("mass: no weight is accumulated where few pages are attended to")
     if n_sel and bounds is None:
@@ -192,8 +194,13 @@ def decode_layer(h, q, k, v, types, R, budget: rs.Budget, G: int, cache: rs.Page
         q = _append(cache, q, k, v, R, mask, table, lens, positions, inv_freq, axis, q_weight, k_weight, eps)
         if n_sel:
             rs.page_bounds(cache, table, new_lens, bounds, q.shape[1])
+            room = workspace
+            if room is not None:  # one that is large enough serves both calls, one after the other
+                whole = table.shape[1] * cache.page
+                need = rs.select_pages_workspace_size(cache, q.shape[0], q.shape[1], min(max_len, whole) if max_len else whole)
+                room = room if room.numel() >= need else None
             sel = rs.select_pages(q, cache, bounds, table, new_lens, n_sel, first=first, recent=recent, visible=visible,
-                                  max_len=max_len)
+                                  max_len=max_len, workspace=room)
             # (a bound inside a page, whose other tokens are not seen either)
             seen = new_lens.clamp(max=max_len) if max_len and max_len % cache.page else new_lens
             out = rs.attend_selected(q, cache, table, seen, sel, R, visible=visible, workspace=workspace, out=out)

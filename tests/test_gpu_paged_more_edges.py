@@ -222,3 +222,22 @@ def test_layers_take_operands_that_lie_in_the_cache(dtype):
             src = (b.K if i < 2 else b.V).flatten()[i * n: (i + 1) * n].view(2, 3, m.H, m.dh).clone()
             want = decode_layer(*m.common({**x, name: src}, b), lens, lens + 3, **kw)
             assert same(got, want) and all(same(u, v) for u, v in zip(a.tensors(), b.tensors())), name
+
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+def test_a_layer_over_few_pages_shares_one_workspace(dtype):
+    m = Model(63, dtype, 3)
+    bounds = torch.zeros((m.cache.K.shape[0], m.H, 2, m.dh), device=DEV, dtype=dtype)
+    lens = ints([60, 75, 170])
+    rs.page_bounds(m.cache, m.table, lens, bounds, 10 ** 6)
+    x = m.tokens(2)
+    pos = lens[:, None] + torch.arange(2, device=DEV, dtype=i32)
+    whole = m.table.shape[1] * 16
+    small = rs.attend_selected_workspace_size(m.cache, 3, m.H * m.rep, 2, 5)
+    both = max(small, rs.select_pages_workspace_size(m.cache, 3, 2, whole))
+    outs = []
+    for ws in (None, small, both):
+        ws = None if ws is None else torch.full((max(ws, 1),), 255, dtype=torch.uint8, device=DEV)
+        outs.append(decode_layer(*m.common(x, m.clone()), lens, lens + 2, positions=pos, scores_in=x["scores"], n_sel=5, bounds=bounds.clone(),
+                                 workspace=ws, **m.kw()))
+    assert same(outs[0], outs[1]) and same(outs[0], outs[2])

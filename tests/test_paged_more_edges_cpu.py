@@ -62,3 +62,22 @@ def test_what_one_pass_refuses_goes_through_the_separate_calls(monkeypatch, stat
             pipeline.decode_layer(*args, positions=1)
     with pytest.raises(pipeline.rs.RolesubError):
         pipeline.decode_layer(*[None] * 12, positions=1)
+
+
+@pytest.mark.parametrize("have,max_len", [(None, 0), (99, 0), (100, 0), (500, 0), (99, 41), (100, 41)])
+def test_a_layer_over_few_pages_gives_both_calls_its_workspace(monkeypatch, have, max_len):
+    """Where it is large enough for the choice: a smaller one serves the attention, as it did."""
+    got, asked = [], []
+    q = torch.zeros(3, 2, 4, 8)
+    monkeypatch.setattr(pipeline.rs, "route", lambda *a, **kw: {"mask": None})
+    monkeypatch.setattr(pipeline.rs, "append_rotary", lambda *a, **kw: q)
+    monkeypatch.setattr(pipeline.rs, "page_bounds", lambda *a, **kw: None)
+    monkeypatch.setattr(pipeline.rs, "select_pages_workspace_size", lambda cache, *a: (asked.append(a), 100)[1])
+    for name in ("select_pages", "attend_selected"):
+        monkeypatch.setattr(pipeline.rs, name, lambda *a, workspace=None, **kw: (got.append(workspace), torch.zeros(1))[1])
+    ws = None if have is None else torch.zeros(have, dtype=torch.uint8)
+    lens = torch.tensor([5, 40, 70], dtype=torch.int32)
+    pipeline.decode_layer(*[None] * 8, types.SimpleNamespace(page=16), torch.zeros(3, 9), lens, lens, positions=1, n_sel=3, bounds=1,
+                          max_len=max_len, workspace=ws)
+    assert asked == ([] if have is None else [(3, 2, max_len or 144)])
+    assert got[0] is (ws if have is not None and have >= 100 else None) and got[1] is ws
