@@ -150,6 +150,80 @@ def test_values_kept_as_they_are_keep_their_bits(dtype, G):
         assert all(same(a, b) for a, b in zip(c.tensors(), d.tensors()))
 
 
+# ---- appends of many tokens and heads -------------------------------------------
+
+@pytest.mark.parametrize("dtype", [bf, f32])
+@pytest.mark.parametrize("dh,P,R", [(128, 16, True), (64, 256, True), (128, 256, False), (64, 16, True), (128, 64, True)])
+def test_append_rotary_long_runs(dtype, dh, P, R):
+    """From 1025 groups of 64 tokens and a head on a workgroup takes 128 tokens."""
+    rng = np.random.default_rng(51)
+    check_append(rng, [0, 5, 300], 700, P=P, H=32, rep=1, dh=dh, dtype=dtype, R=R, ragged=True, fused=P == 256)
+    check_append(rng, [9] * 7 + [250], 301, P=P, H=32, rep=1, dh=dh, G=32 if dh == 128 else 4, dtype=dtype, R=R, with_q=False)
+
+
+# ---- choices among few and many pages ---------------------------------------------
+
+def select_ref(q, bd, table, n_pages, P, lens, n_sel, first, recent, visible, max_len):
+    """The oracle's choice, a sequence's pages at once."""
+    B, Tq, Hq, dh = q.shape
+    H = bd.shape[1]
+    cap = table.shape[1] * P
+    cap = min(cap, max_len) if max_len else cap
+    sel = np.full((B, Tq, H, n_sel), -1, dtype=np.int32)
+    for b in range(B):
+        m0 = page_count(min(max(int(lens[b]), 0), cap), P)
+        if m0 == 0:
+            continue
+        pg = table[b, :m0].long()
+        there = (pg >= 0) & (pg < n_pages)
+        lo, hi = bd[pg.clamp(0, n_pages - 1)].double().permute(2, 1, 0, 3)[:, :, None]  # [H, 1, m, dh]
+        x = q[b].double().unflatten(1, (H, -1))
+        for j in range(Tq):
+            y = x[j][:, :, None]  # [H, rep, 1, dh]
+            s = torch.where(y < 0, y * lo, y * hi).sum(-1).float()
+            s = torch.where(torch.isnan(s).any(1) | ~there, torch.tensor(float("nan"), device=DEV), s.amax(1)).cpu().numpy()
+            n = min(max(int(lens[b]), 0), cap)
+            n = n if visible is None else min(n, max(int(visible[b, j]), 0))
+            m = page_count(n, P)
+            for g in range(H):
+                mine = list(range(m))
+                if m > n_sel:
+                    free = np.arange(first, m - recent)
+                    z = s[g, free]
+                    order = np.lexsort((free, np.where(np.isnan(z), 0.0, -z), np.isnan(z)))
+                    keep = free[order][: n_sel - first - recent].tolist()
+                    mine = sorted(list(range(first)) + keep + list(range(m - recent, m)))
+                sel[b, j, g, : len(mine)] = mine
+    return sel
+
+
+@pytest.mark.parametrize("W", [255, 511, 512, 513, 2000])
+@pytest.mark.parametrize("dtype,dh", [(bf, 64), (bf, 128), (f32, 64), (f32, 128)])
+@pytest.mark.parametrize("rep,Tq", [(1, 1), (4, 2), (5, 1)])
+def test_select_pages_at_the_border_of_one_launch(W, dtype, dh, rep, Tq):
+    P, H = 16, 2
+    rng, g = np.random.default_rng(W + rep), torch.Generator(device=DEV).manual_seed(W)
+    lens = [0, 1, W * P, 17, W * P - 5, 700, W * P + 99, -4]
+    B, N = len(lens), W + 3
+    c = rs.PagedCache(torch.zeros((N, H, P, dh), device=DEV, dtype=dtype), torch.zeros((N, H, 16, 8), device=DEV, dtype=dtype),
+                      torch.zeros((N, P), device=DEV, dtype=i32), torch.zeros((N, P), device=DEV, dtype=i32))
+    bd = torch.randn((N, H, 2, dh), generator=g, device=DEV, dtype=dtype)
+    t = torch.stack([torch.randperm(N, generator=g, device=DEV)[:W] for _ in range(B)]).int()
+    bd[t[2, 5].long()] = bd[t[2, 9].long()]  # equal scores
+    bd[t[4, 50:90].long()] = bd[t[4, 9].long()].clone()
+    bd[t[2, 7].long()] = float("nan")
+    bd[t[4, 11].long(), 1, 0, 3] = float("-inf")
+    t[4, 3], t[2, 20], t[6, 40] = -1, 10 ** 6, N
+    q = torch.randn((B, Tq, rep * H, dh), generator=g, device=DEV, dtype=dtype)
+    vis = ints(rng.integers(-5, W * P + 50, (B, Tq)))
+    ws = torch.full((rs.select_pages_workspace_size(c, B, Tq, W * P),), 255, dtype=torch.uint8, device=DEV)
+    for n_sel, first, recent, v, ml in ((1, 0, 0, None, 0), (7, 1, 2, None, 0), (9, 0, 9, vis, 0), (40, 3, 5, vis, 0), (W + 5, 1, 1, None, 0),
+                                        (W - 1, 0, 0, None, 0), (9, 0, 1, None, W * P // 2 + 3)):
+        want = select_ref(q, bd, t, N, P, lens, n_sel, first, recent, v, ml)
+        got = rs.select_pages(q, c, bd, t, ints(lens), n_sel, first, recent, visible=v, max_len=ml, workspace=ws)
+        assert np.array_equal(got.cpu().numpy(), want), (n_sel, first, recent)
+
+
 # ---- bounds of shared pages ---------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [bf, f32])
