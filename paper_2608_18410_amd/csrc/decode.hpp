@@ -144,7 +144,7 @@ struct Rotation {
   static constexpr int N = L::MB / 4;
   u32x4 a[N][L::KS];
   __device__ __forceinline__ void load(const DecodeParams& p, int h) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x / 64 % 4, l16 = lane & 15, g4 = lane >> 4;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
     if (!p.Rm) return;
     const T* R = static_cast<const T*>(p.Rm) + (static_cast<int64_t>(h) * DH + 16 * w + l16) * DH + g4 * L::EP;
 #pragma unroll
@@ -156,14 +156,13 @@ struct Rotation {
 
 // Output rows [r0, r0 + 16) of key head h from their normalised sums u (LDS, rows of
 // RLD floats; rows past R are zero): out = R_h u on the matrix cores, R's rows as
-// the product's rows. The sums enter as bf16 parts, or in f32. Four waves (of eight each
-// four with rows of their own).
+// the product's rows. The sums enter as bf16 parts, or in f32. All four waves.
 template <class T, int DH>
 __device__ __forceinline__ void finish_rows(const DecodeParams& p, int b, int h, int r0, const float* u,
                                             const Rotation<T, DH>& rot) {
   using L = Tile<T, DH>;
   constexpr int KS = L::KS, EP = L::EP, N = L::MB / 4;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid / 64 % 4, l16 = lane & 15, g4 = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
   const int r = r0 + l16;
   const float* ur = u + l16 * L::RLD;
   f32x4 o[N];
@@ -921,8 +920,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH == 128 ?
 }
 
 // One split of one key head and 64 rows, 16 a wave: the four waves share each tile of
-// tokens. Its keys and kept groups come into registers a tile ahead, a quarter a wave, and go from there to one of two LDS tiles, so that one barrier a tile is
-// enough: between two barriers the waves write the next tile and compute on this one.
+// tokens. Its keys and kept groups come into registers a tile ahead, a quarter a wave, and
+// go from there to one of two LDS tiles, so that one barrier a tile is enough: between two
+// barriers the waves write the next tile and compute on this one.
 // (With a tile to each wave, as above, every wave fetches and expands all of it:
 // 16 sequences of up to 361 tokens and 56 queries took 42 us.) Those 16, 32 heads, take 32
 // us; 64 of 361 108. No one unit bounds it: of the waves' time there a third is spent
@@ -1369,10 +1369,10 @@ hipError_t launch(DecodeParams p, hipStream_t s) {
   const int WR = row_blocks(p.R, sizeof(T) == 2, DH);
   const int64_t wgs = static_cast<int64_t>(p.B) * p.c.H * ((p.R + 63) / 64);
   p.ordered = S != kListed && p.n_split == 1 && p.B > 1 && p.B <= kOrderMax && wgs > 256 && wgs <= kOrderWgs && p.max_len >= 512;
-  if (WR == 1)
+  if constexpr (S == kTree)  // of up to 16 rows: more are launch_decode_tree's
     go<T, DH, 1, S>(p, s);
-  else if constexpr (S == kTree)
-    return hipErrorInvalidValue;  // not called: launch_decode_tree
+  else if (WR == 1)
+    go<T, DH, 1, S>(p, s);
   else if (WR == 4)
     go<T, DH, 4, S>(p, s);
   else if constexpr (!share_from_17(sizeof(T) == 2, DH))
