@@ -18,7 +18,8 @@ constexpr int64_t kSplitWgs = 512;
 // of more, in blocks of kTreeRows: 8 of those sequences, of 96 rows, 60 us with 256, 53 with
 // 512, 46 with 768 and 50 with 1024. Where the blocks fill the card without splits, two to a
 // CU, splits only add: 32 of those sequences of 64 rows 73 us in one, 98 in two, of 96 rows
-// 88 and 113, of 64 rows and up to 16384 tokens 217 and 258; nothing longer was measured.
+// 88 and 113, of 64 rows and up to 16384 tokens 217 and 258; nothing longer was measured, and
+// all of this with two parts of a weight, where three take 3 % more.
 constexpr int64_t kTreeWgs = 1024, kTreeRowsWgs = 768, kTreeFull = 512, kTreeWhole = 128;
 // Up to 512 tokens these and listed pages, whose calls add up no weights, have one split
 // where 16 rows or fewer share it: 8 drafted tokens over 305 and 32 heads 24.9 -> 22.2 us

@@ -358,7 +358,7 @@ __device__ __forceinline__ void turn_rows(const TurnParams& p, int64_t tok, int 
 
 // A wave turns heads [hw * chunk, ...) of one token. Bound by memory: 16 times 2048 tokens
 // of 32 + 8 heads of 128 dims from a fused projection (671 MB) 141 us, 4.8 TB/s, what a copy
-// reaches. One token: 4.2 us, the launch and two loads behind each other.
+// reaches (float32, 1.34 GB, 256 us). One token: 4.2 us, the launch and two loads behind each other.
 template <class T, int DH, bool IL, bool WHOLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k_norm_rotary(TurnParams p, int chunks, int chunk) {
   __shared__ __attribute__((aligned(16))) char stage[4][WHOLE ? 16 : kStage];
@@ -498,8 +498,9 @@ __device__ __forceinline__ void rotate_run(const TurnParams& p, int64_t n0, int 
 // An append. The first workgroups turn the rows of queries and keys, the last `vals` bring
 // the values of one head and run of tokens. 16 times up to 305 tokens of 32 + 32 heads from
 // a fused projection (157 MB) 46 us, 3.4 TB/s, of which the rows alone would take 30; with
-// the values first 49, with both kinds spread evenly 51. Without the norm 40: the vector
-// units are busy too.
+// the values first 49, with both kinds spread evenly 51. Without the norm 39: the vector
+// units are busy too. float32 (314 MB) 105, 3.0 TB/s: R_h fills 66 KB of LDS, so two
+// workgroups share a CU.
 template <class T, int DH, bool IL, bool WHOLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 3 : 2))) void k_append_rotary(TurnParams p, unsigned vals, int run, int chunks, int chunk) {
   using L = Values<T, DH>;
@@ -577,7 +578,7 @@ void launch_in(const TurnParams& p, hipStream_t s) {
   const size_t tok = static_cast<size_t>(p.B) * p.T;
   const int chunk = heads_of(tok, heads), chunks = (heads + chunk - 1) / chunk;
   // runs of 128 tokens, which read R_h half as often, where 64 would make four
-  // workgroups a CU and more (the case above 56 -> 51 us)
+  // workgroups a CU and more (the case above, before its other steps, 56 -> 51 us)
   const int run = (tok + 63) / 64 * p.c.H > 1024 ? kRun : 64;
   const size_t vals = (tok + run - 1) / run * p.c.H;
   auto kern = p.interleaved ? (whole<T>(p) ? k_append_rotary<T, DH, true, true> : k_append_rotary<T, DH, true, false>)

@@ -13,8 +13,8 @@ namespace {
 // its rows, then the lanes of one piece. fminf and fmaxf pass over NaN. Whole pages are
 // gone over again, as what a page holds may have moved. Where a sequence ends inside a page
 // that others have in the same place, the longest of them counts: all that write its
-// bounds then write the same. A chain of loads (length, page, rows): 3 us for one of 32
-// heads, 4.9 for 8 sequences with a page of 64 tokens each.
+// bounds then write the same. A chain of loads (length, page, rows): 3 to 4 us for one
+// of 32 heads, 5.0 for 8 sequences with a page of 64 tokens each.
 template <class T, int DH, int U>
 __global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
   constexpr int V = 16 / sizeof(T), LPR = DH / V, RPI = 64 / LPR;

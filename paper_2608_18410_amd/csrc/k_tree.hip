@@ -80,14 +80,16 @@ __device__ __forceinline__ void add_blocks(const DecodeParams& p, int b, int h, 
 // each, reads every tile from LDS once a wave, which took as long there as the products did,
 // and waits a barrier a tile: as it is, and with eight waves and 128 rows, it took 136 and
 // 129 us for 32 sequences of 256 to 4096 tokens, 8 key heads of 96 rows, against 88 here; 64
-// rows 92 against 73, 240 rows 207 against 176. Three blocks leave one wave a SIMD its
+// rows 92 against 73, 240 rows 207 against 176, all with two parts of a weight. Three, as it
+// is, take 90, 76 and 181 with two input sets in turn, and 83 for the 96 rows where one
+// set stays in the caches. Three blocks leave one wave a SIMD its
 // registers: 184. Eight waves a workgroup, one workgroup a CU: 111, as the chain of loads
 // before the first product and the one behind the last, some 12 us in all, then have
 // nothing beside them.) The row tiles of one item read the same keys and values one after
 // the other on one XCD: half of the reads find their lines in its cache.
-// That chain and the longest sequence bound it: of 88 us a tile of tokens and 32 rows keeps
-// the vector and matrix units busy for a half. Sequences of 64 tokens, which have the chain
-// alone, take 33 us where k_decode_rows took 23.
+// That chain and the longest sequence bound it: of the cycles in which a CU has waves the
+// vector units issue in 47 % and the matrix units work in 24 %. Sequences of 64 tokens, which
+// have the chain alone, take 31 us where k_decode_rows took 23.
 template <class T, int DH, int SUB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_tree_rows(DecodeParams p) {
   using L = Tile<T, DH>;
