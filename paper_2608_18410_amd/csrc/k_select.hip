@@ -9,72 +9,82 @@
 namespace rolesub {
 namespace {
 
-// Bounds of a page's keys in every dim, a wave for each page and head: 16-byte pieces of
+// Bounds of a page's keys in every dim, a wave for each page and hpw heads: 16-byte pieces of
 // its rows, then the lanes of one piece. fminf and fmaxf pass over NaN. Whole pages are
 // gone over again, as what a page holds may have moved. Where a sequence ends inside a page
 // that others have in the same place, the longest of them counts: all that write its
 // bounds then write the same. A chain of loads (length, page, rows): 3 to 4 us for one
-// of 32 heads, 5.0 for 8 sequences with a page of 64 tokens each.
+// of 32 heads, 5.0 for 8 sequences with a page of 64 tokens each. 256 sequences and 32 heads on
+// pages of 16 take 8.4, 1024 22.4: 1.4 of it to look at the others' lengths and pages, where a
+// look for each head took 3 and 47.
 template <class T, int DH, int U>
-__global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np) {
+__global__ __launch_bounds__(256) void k_page_bounds(BoundsParams p, int np, int hpw) {
   constexpr int V = 16 / sizeof(T), LPR = DH / V, RPI = 64 / LPR;
+  __shared__ int s_n[4];
   const PagedCache& c = p.c;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + w, pages = static_cast<int64_t>(p.B) * np;
-  if (job >= pages * c.H) return;
-  const int h = static_cast<int>(job % c.H), i = static_cast<int>(job / c.H % np), b = static_cast<int>(job / c.H / np);
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nt = static_cast<int>(blockDim.x), nw = nt / 64, wh = nw * hpw;
+  const int hb = (c.H + wh - 1) / wh, h0 = static_cast<int>(blockIdx.x % hb) * wh;
+  const int i = static_cast<int>(blockIdx.x / hb % np), b = static_cast<int>(blockIdx.x / hb / np);
   const int64_t cap = static_cast<int64_t>(p.max_pages) << c.shift;
-  const int first = p.lens[min(lane, p.B - 1)];  // of the sequences, one a lane
+  const bool alone = p.B <= 64;  // a wave looks at all sequences itself
+  const int first = p.lens[min(alone ? lane : tid, p.B - 1)];  // of the sequences, one a lane
   const int64_t len = min(static_cast<int64_t>(max(p.lens[b], 0)), cap);
   const int64_t pi = (max(len - p.T, static_cast<int64_t>(0)) >> c.shift) + i, t0 = pi << c.shift;
   if (t0 >= len) return;
   int n = static_cast<int>(min(len - t0, static_cast<int64_t>(c.page)));
   const int page = p.table[static_cast<int64_t>(b) * p.max_pages + pi];
   if (n < c.page) {
-    for (int x = lane; x < p.B; x += 64) {
-      const int64_t other = min(static_cast<int64_t>(max(x < 64 ? first : p.lens[x], 0)), cap);
-      if (p.table[static_cast<int64_t>(x) * p.max_pages + pi] == page && other > t0 + n)
+    for (int x = alone ? lane : tid; x < p.B; x += nt) {
+      const int64_t other = min(static_cast<int64_t>(max(x < nt ? first : p.lens[x], 0)), cap);
+      if (other > t0 + n && p.table[static_cast<int64_t>(x) * p.max_pages + pi] == page)
         n = static_cast<int>(min(other - t0, static_cast<int64_t>(c.page)));
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) n = max(n, __shfl_xor(n, o, kWave));
+    if (!alone) {
+      if (lane == 0) s_n[w] = n;
+      __syncthreads();
+      for (int x = 0; x < nw; ++x) n = max(n, s_n[x]);
+    }
   }
   if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(c.n_pages)) return;
-  const int64_t head = static_cast<int64_t>(page) * c.H + h;
-  const char* k = static_cast<const char*>(c.K) + (head << c.shift) * DH * static_cast<int64_t>(sizeof(T)) + lane % LPR * 16;
-  float lo[V], hi[V];
+  for (int h = h0 + w; h < min(h0 + wh, c.H); h += nw) {
+    const int64_t head = static_cast<int64_t>(page) * c.H + h;
+    const char* k = static_cast<const char*>(c.K) + (head << c.shift) * DH * static_cast<int64_t>(sizeof(T)) + lane % LPR * 16;
+    float lo[V], hi[V];
 #pragma unroll
-  for (int x = 0; x < V; ++x) lo[x] = __builtin_inff(), hi[x] = -__builtin_inff();
-  for (int r0 = lane / LPR; r0 < n; r0 += RPI * U) {
-    u32x4 a[U];
+    for (int x = 0; x < V; ++x) lo[x] = __builtin_inff(), hi[x] = -__builtin_inff();
+    for (int r0 = lane / LPR; r0 < n; r0 += RPI * U) {
+      u32x4 a[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {  // past the last row: it again
-      const int r = min(r0 + u * RPI, n - 1);
-      a[u] = *reinterpret_cast<const u32x4*>(k + r * DH * static_cast<int>(sizeof(T)));
-    }
+      for (int u = 0; u < U; ++u) {  // past the last row: it again
+        const int r = min(r0 + u * RPI, n - 1);
+        a[u] = *reinterpret_cast<const u32x4*>(k + r * DH * static_cast<int>(sizeof(T)));
+      }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const T* x = reinterpret_cast<const T*>(&a[u]);
+      for (int u = 0; u < U; ++u) {
+        const T* x = reinterpret_cast<const T*>(&a[u]);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        lo[i] = fminf(lo[i], tof(x[i]));
-        hi[i] = fmaxf(hi[i], tof(x[i]));
+        for (int v = 0; v < V; ++v) {
+          lo[v] = fminf(lo[v], tof(x[v]));
+          hi[v] = fmaxf(hi[v], tof(x[v]));
+        }
       }
     }
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1)
+#pragma unroll
+      for (int x = 0; x < V; ++x) {
+        lo[x] = fminf(lo[x], __shfl_xor(lo[x], o, kWave));
+        hi[x] = fmaxf(hi[x], __shfl_xor(hi[x], o, kWave));
+      }
+    u32x4 out;
+    T* o = reinterpret_cast<T*>(&out);
+#pragma unroll
+    for (int x = 0; x < V; ++x) o[x] = fromf<T>(lane < LPR ? lo[x] : hi[x]);
+    if (lane < 2 * LPR) *reinterpret_cast<u32x4*>(static_cast<char*>(p.bounds) + head * 2 * DH * sizeof(T) + lane * 16) = out;
   }
-#pragma unroll
-  for (int o = LPR; o < 64; o <<= 1)
-#pragma unroll
-    for (int x = 0; x < V; ++x) {
-      lo[x] = fminf(lo[x], __shfl_xor(lo[x], o, kWave));
-      hi[x] = fmaxf(hi[x], __shfl_xor(hi[x], o, kWave));
-    }
-  if (lane >= 2 * LPR) return;
-  u32x4 out;
-  T* o = reinterpret_cast<T*>(&out);
-#pragma unroll
-  for (int x = 0; x < V; ++x) o[x] = fromf<T>(lane < LPR ? lo[x] : hi[x]);
-  *reinterpret_cast<u32x4*>(static_cast<char*>(p.bounds) + head * 2 * DH * sizeof(T) + lane * 16) = out;
 }
 
 // What the lane D away (D in 1, 2, 4, 8, 16; within rows of 2 D lanes) holds.
@@ -297,14 +307,18 @@ __global__ __launch_bounds__(kFewWg) void k_select_few(SelectParams p) {
 
 hipError_t launch_page_bounds(const BoundsParams& p, bool bf16, hipStream_t s) {
   const int np = static_cast<int>(std::min<int64_t>(p.max_pages, ((p.c.page - 1 + static_cast<int64_t>(p.T) - 1) >> p.c.shift) + 1));
-  const int64_t jobs = static_cast<int64_t>(p.B) * np * p.c.H;
+  // a wave takes one head, or a workgroup takes all where looking at the other sequences is
+  // more than a load, or workgroups are many anyway
+  const int64_t pages = static_cast<int64_t>(p.B) * np;
+  const int nw = std::min(p.c.H, 4), most = (p.c.H + nw - 1) / nw, hpw = p.B > 256 || pages * p.c.H > (1 << 20) ? most : 1;
+  const int64_t wgs = pages * ((most + hpw - 1) / hpw);
   // loads of a wave in flight: a page's of up to 16 KB
   auto some = bf16 ? (p.c.dh == 128 ? k_page_bounds<__bf16, 128, 4> : k_page_bounds<__bf16, 64, 4>)
                    : (p.c.dh == 128 ? k_page_bounds<float, 128, 4> : k_page_bounds<float, 64, 4>);
   auto many = bf16 ? (p.c.dh == 128 ? k_page_bounds<__bf16, 128, 16> : k_page_bounds<__bf16, 64, 16>)
                    : (p.c.dh == 128 ? k_page_bounds<float, 128, 16> : k_page_bounds<float, 64, 16>);
   auto kern = p.c.page * p.c.dh * (bf16 ? 2 : 4) <= 4096 ? some : many;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((jobs + 3) / 4)), dim3(256), 0, s, p, np);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(wgs)), dim3(64 * nw), 0, s, p, np, hpw);
   return hipGetLastError();
 }
 

@@ -227,12 +227,12 @@ def test_select_pages_at_the_border_of_one_launch(W, dtype, dh, rep, Tq):
 # ---- bounds of shared pages ---------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [bf, f32])
-@pytest.mark.parametrize("B", [2, 7, 70, 200])
-def test_bounds_of_a_shared_page_hold_for_all_its_sequences(dtype, B):
+@pytest.mark.parametrize("B,H", [(2, 2), (7, 1), (70, 3), (200, 2), (300, 5), (260, 1)])
+def test_bounds_of_a_shared_page_hold_for_all_its_sequences(dtype, B, H):
     """Sequences with the same first pages and lengths that end in one of them: its bounds are over
     the tokens of the longest, whichever comes last, and also where only its end is among the last T."""
     rng = np.random.default_rng(B)
-    P, H, dh, W = 64, 2, 128, 4
+    P, dh, W = 64, 128, 4
     c = full_cache(rng, 40 + B, P, H, dh, 8, 8, dtype)
     c.K[:, :, 1::2] *= 3  # later tokens widen the bounds
     table = rng.permutation(40)[:W][None].repeat(B, 0)
